@@ -86,6 +86,36 @@ const char* muon_last_error(muon_handle h);
 /* Frees all device memory of the handle (synchronises the device first). */
 void muon_destroy(muon_handle h);
 
+/* ---- stand-alone orthogonalisation ------------------------------------------------------- */
+
+/* X_n of Alg. Muon's iterations for `batch` matrices of rows x cols, as an operator of its own:
+ *   X_0 = M / max(||M||_F, eps),  X' = a_i X + (b_i A + c_i A^2) X,  A = X X^T,  i = 1 .. ns_steps
+ * for a caller that keeps its own momentum (another update rule, momenta gathered from other
+ * ranks) and applies the result itself. It differs from muon_step's iterations in what it takes
+ * and keeps: any sides of 1 .. 65536 (rows * cols < 2^31), any leading dimension >= cols and any
+ * alignment of the type, types of soap_dtype_t in and (the same one) out, and intermediates of 11
+ * bits (bf16) or 22 bits (fp32, fp16) with fp32 accumulation, so that a bf16 result carries its
+ * own rounding and little more, and an fp32 result is fp32-accurate.
+ *
+ * Matrix b starts at M + b * stride elements, row i at i * ld; `out` likewise (out may be M itself
+ * with the same strides, and must not overlap it otherwise). coeffs: host array of 3 * ns_steps floats,
+ * read during the call, or NULL for muon_default_hparams's quintic polynomial. workspace: device
+ * memory, 256-byte aligned, muon_orthogonalize_workspace_bytes(...) bytes (0 from that function:
+ * the sizes or the type are invalid). status: NULL, or a device int32 into which the kernels OR
+ * SOAP_STATUS_NONFINITE (a matrix holds a NaN or an infinity: its result is NaN, the others are
+ * not touched by it) or SOAP_STATUS_TIMEOUT; it is not cleared. Runs on the device that is current
+ * for the calling thread. A zero matrix gives zeros.
+ *
+ * Precision beyond rounding: a step multiplies small singular values by a_i, so rounding noise in
+ * X_0 (2^-12 of an element, bf16: none; 2^-23 for fp32) reappears in the directions whose singular
+ * values lie below that noise; in exact arithmetic those are as undetermined as the input's own
+ * last bit. */
+size_t muon_orthogonalize_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int32_t type);
+soap_status_t muon_orthogonalize(int32_t batch, int64_t rows, int64_t cols, const void* M, int64_t ld, int64_t stride,
+                                 int32_t type, const float* coeffs, int32_t ns_steps, float eps, void* out,
+                                 int64_t ld_out, int64_t stride_out, void* workspace, size_t workspace_bytes,
+                                 int32_t* status, soap_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

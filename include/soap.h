@@ -45,6 +45,10 @@ typedef enum {
   SOAP_ERR_TIMEOUT = 6      /* a bounded device-side wait gave up */
 } soap_status_t;
 
+/* Element types of the stand-alone operators that take more than fp32 (include/muon.h's
+ * muon_orthogonalize, include/layer.h). */
+typedef enum { SOAP_F32 = 0, SOAP_BF16 = 1, SOAP_F16 = 2 } soap_dtype_t;
+
 /* One weight matrix. precond_left = 0 keeps Q_L = I fixed and stores no L (an
  * "identity side"); likewise precond_right for Q_R and R. */
 typedef struct {

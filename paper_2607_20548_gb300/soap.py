@@ -34,7 +34,11 @@ EXPORTS = ("soap_default_hparams", "soap_create", "soap_create_ex", "soap_plan_i
 # every symbol include/muon.h declares
 MUON_EXPORTS = ("muon_default_hparams", "muon_create", "muon_step", "muon_set_lr", "muon_state_get",
                 "muon_state_set", "muon_status", "muon_last_error", "muon_destroy", "muon_profile_begin",
-                "muon_profile_end")
+                "muon_profile_end", "muon_orthogonalize", "muon_orthogonalize_workspace_bytes")
+# every symbol include/layer.h declares
+LAYER_EXPORTS = ("layer_norm_forward", "layer_norm_backward", "layer_norm_workspace_bytes", "layer_route_forward",
+                 "layer_route_backward", "layer_route_workspace_bytes")
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # soap_dtype_t
 KERNEL_FAMILIES = ("gemm_simt", "gemm_tc", "qr_panel", "elementwise", "other", "qr_update")
 PROFILE_SERIAL = 1  # SOAP_PROFILE_SERIAL
 
@@ -129,6 +133,14 @@ def load_library(path: str = LIB_PATH):
         "muon_destroy": (None, [P]),
         "muon_profile_begin": (I32, [P, I64]),
         "muon_profile_end": (I32, [P, P, ctypes.POINTER(soap_kernel_stats), ctypes.POINTER(I32)]),
+        "muon_orthogonalize_workspace_bytes": (SZ, [I32, I64, I64, I32]),
+        "muon_orthogonalize": (I32, [I32, I64, I64, P, I64, I64, I32, P, I32, F, P, I64, I64, P, SZ, P, P]),
+        "layer_norm_forward": (I32, [I64, I64, P, I64, I32, P, P, I32, F, P, I64, P, P, P]),
+        "layer_norm_workspace_bytes": (SZ, [I64, I64]),
+        "layer_norm_backward": (I32, [I64, I64, P, I64, P, I64, I32, P, P, P, I32, P, I64, P, P, P, SZ, P]),
+        "layer_route_workspace_bytes": (SZ, [I64, I32]),
+        "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, SZ, P]),
+        "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
