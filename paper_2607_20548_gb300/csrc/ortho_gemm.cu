@@ -6,12 +6,17 @@
 // lies and no transposed copy exists. Split operands (x = hi + lo, 22 bits) take three products,
 // hi hi + hi lo + lo hi, into the same accumulator from one load of the four tiles.
 //
-// One CTA computes 128 x 128 tiles. Warp 0 issues TMA loads of 64-element K slices into a ring,
-// warp 1 the MMAs into one of two TMEM accumulators, four warps drain the other one: tensor memory
-// -> registers -> alpha/beta -> shared memory -> coalesced stores. A symmetric result computes its
-// tiles on and below the diagonal and stores each twice, the second time transposed. Every
-// mbarrier wait is bounded; one that runs out sets SOAP_STATUS_TIMEOUT and the CTA drains its
-// copies, frees its tensor memory and returns.
+// A CTA pair (cta_group::2) computes tiles of 256 x 256 or 256 x 128, each CTA holding 128 rows of
+// A and half of B's rows, or a single CTA tiles of 128 x 128. Warp 0 issues TMA loads of
+// 64-element K slices into a ring, warp 1 (of the pair's first CTA) the MMAs into one of two TMEM
+// accumulators, four warps drain the other one: tensor memory -> registers -> alpha/beta -> shared
+// memory -> coalesced stores. A symmetric result computes its tiles on and below the diagonal and
+// stores each twice, the second time transposed. Every mbarrier wait is bounded; one that runs out
+// sets SOAP_STATUS_TIMEOUT and the CTA drains its copies, frees its tensor memory and returns.
+//
+// The accumulator truncates: measured, a sum loses 2^-25 of itself per 16 products. With 11-bit
+// operands that is nothing; split ones keep the small products in an accumulator of their own and
+// take K in runs of 512, whose sums the epilogue warps add in fp32 registers.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -30,11 +35,11 @@ namespace {
 
 using namespace tc;
 
-constexpr int BM = 128, BN = 128, BK = 64;
+constexpr int BK = 64;
 constexpr int kBox = 64 * 64 * 2;        // one TMA box: 64 rows of 128 bytes
-constexpr int kTile = 2 * kBox;          // 128 x 64 elements of an operand
-constexpr int kRing = 6 * 2 * kTile;     // bytes of the operand ring
+constexpr int kRing = 192 * 1024;        // bytes of the operand ring
 constexpr int kAcc = 2;                  // TMEM accumulators
+constexpr int kRunBlocks = 8;            // K slices per accumulator run of split operands
 constexpr int kEpiWarps = 4;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kStagePitch16 = 80, kStagePitch32 = 144;  // staged 32-element rows, free of bank conflicts
@@ -61,25 +66,40 @@ __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
 
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-      : "memory");
+// The address of this CTA's shared-memory object in the pair's first CTA.
+__device__ __forceinline__ uint32_t in_leader(const void* p) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  return r;
 }
 
-// An operand's 128 x 64 tile at (row m0, k0) as two boxes: rows m0 .. and m0 + 64 .. of 64 K
-// elements each (K-major), or 64 K rows of the columns m0 .. and m0 + 64 .. (MN-major).
-template <int MAJOR>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int m0, int k0, int z) {
-  if (MAJOR == kRowsK) {
-    tma_box(dst, map, bar, k0, m0, z);
-    tma_box(dst + kBox, map, bar, k0, m0 + 64, z);
-  } else {
-    tma_box(dst, map, bar, m0, k0, z);
-    tma_box(dst + kBox, map, bar, m0 + 64, k0, z);
-  }
+// `bar` is a shared::cluster address: in a pair both CTAs' copies count on the first one's barrier.
+template <int CG>
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  if (CG == 2)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+// ROWS x 64 elements of an operand at (row m0, k0) as boxes of 64: rows of 64 K elements each
+// (K-major), or 64 K rows of 64 columns (MN-major).
+template <int MAJOR, int ROWS, int CG>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int m0, int k0, int z) {
+#pragma unroll
+  for (int i = 0; i < ROWS / 64; ++i)
+    if (MAJOR == kRowsK)
+      tma_box<CG>(dst + i * kBox, map, bar, k0, m0 + i * 64, z);
+    else
+      tma_box<CG>(dst + i * kBox, map, bar, m0 + i * 64, k0, z);
 }
 
 // Descriptor of the 16 K elements at step kk of such a tile. K-major: 32 bytes further along the
@@ -103,26 +123,54 @@ __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, int a_mn, int b_m
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
+template <int CG>
 __device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+  if (CG == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+
+// Arrives on `bar` (in a pair: on both CTAs' barriers at that place) when the MMAs so far are done.
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if (CG == 2)
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+  else
+    umma_commit(bar);
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // Tile t of the launch -> (m0, n0, matrix). Full results go in groups of 8 row tiles (row tile
-// fastest), so that tiles in flight share operands in L2; symmetric ones row by row of the triangle.
+// fastest), so that tiles in flight share operands in L2; symmetric ones row by row of the triangle
+// (R tiles across for each square on the diagonal).
+template <int TM, int TN>
 __device__ __forceinline__ void tile_at(int t, int symmetric, int ntm, int ntn, int& m0, int& n0, int& b) {
+  constexpr int R = TM / TN;
   if (symmetric) {
-    const int per = ntm * (ntm + 1) / 2;
+    const int per = R * (ntm * (ntm + 1) / 2);
     b = t / per;
-    const int r = t - b * per;
+    const int w = t - b * per, r = w / R;
     int i = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
     while (i * (i + 1) / 2 > r) --i;
     while ((i + 1) * (i + 2) / 2 <= r) ++i;
-    m0 = i * BM;
-    n0 = (r - i * (i + 1) / 2) * BN;
+    m0 = i * TM;
+    n0 = ((r - i * (i + 1) / 2) * R + w % R) * TN;
     return;
   }
   const int per = ntm * ntn;
@@ -130,8 +178,8 @@ __device__ __forceinline__ void tile_at(int t, int symmetric, int ntm, int ntn, 
   const int r = t - b * per;
   const int g = r / (8 * ntn), w = r - g * 8 * ntn;
   const int rows = min(8, ntm - g * 8);
-  m0 = (g * 8 + w % rows) * BM;
-  n0 = (w / rows) * BN;
+  m0 = (g * 8 + w % rows) * TM;
+  n0 = (w / rows) * TN;
 }
 
 // 16 bytes of staged row j (part c of 4) to a 32-column block of an internal matrix.
@@ -175,11 +223,102 @@ __device__ __forceinline__ void store_user(uint8_t* stage, const float (&o)[32],
   __syncwarp();
 }
 
-template <int AM, int BMJ, int SPLIT>
+template <int SPLIT>
+struct Cin {
+  uint4 h[4], l[4];
+};
+
+// This lane's 32 elements of C at `src` (the lane's row, `cols` columns left).
+template <int SPLIT>
+__device__ __forceinline__ void load_cin(Cin<SPLIT>& c, const __half* src, int64_t lo, int cols) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (u * 8 < cols) {
+      c.h[u] = *reinterpret_cast<const uint4*>(src + u * 8);
+      if (SPLIT == 2) c.l[u] = *reinterpret_cast<const uint4*>(src + lo + u * 8);
+    }
+}
+
+template <int SPLIT>
+__device__ __forceinline__ void add_cin(const Cin<SPLIT>& c, float beta, int cols, float (&o)[32]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (u * 8 < cols) {
+      const __half* h = reinterpret_cast<const __half*>(&c.h[u]);
+      const __half* l = reinterpret_cast<const __half*>(&c.l[u]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = __half2float(h[e]);
+        if (SPLIT == 2) x += __half2float(l[e]);
+        o[u * 8 + e] = fmaf(beta, x, o[u * 8 + e]);
+      }
+    }
+}
+
+// A warp's 32 x 32 block of the result (row r0 + lane in o): to the caller's matrix, or to an
+// internal one, there also to the mirror position.
+template <int SPLIT>
+__device__ __forceinline__ void store_block(const Args& g, uint8_t* stage, float (&o)[32], int b, int r0, int c0,
+                                            int rows, int cols, bool mirror, int lane) {
+  if (g.user) {
+    const int64_t at = (int64_t)b * g.user_stride + (int64_t)r0 * g.user_ld + c0;
+    if (g.user_type == SOAP_F32)
+      store_user(stage, o, static_cast<float*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
+    else if (g.user_type == SOAP_BF16)
+      store_user(stage, o, static_cast<__nv_bfloat16*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
+    else
+      store_user(stage, o, static_cast<__half*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
+    return;
+  }
+  __half* out = g.out + (int64_t)b * g.stride;
+#pragma unroll
+  for (int h = 0; h < SPLIT; ++h) {
+    uint8_t* st = stage + h * 32 * kStagePitch16;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      Pack<__half, 8> p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p.v[e] = __float2half_rn(o[u * 8 + e]);
+        o[u * 8 + e] -= __half2float(p.v[e]);
+      }
+      *reinterpret_cast<Pack<__half, 8>*>(st + lane * kStagePitch16 + u * 16) = p;
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int h = 0; h < SPLIT; ++h)
+    copy_block16(stage + h * 32 * kStagePitch16, out + h * g.lo + (int64_t)r0 * g.ld + c0, g.ld, rows, cols, lane);
+  if (mirror) {  // read a staged row per lane, write it as a column
+#pragma unroll
+    for (int h = 0; h < SPLIT; ++h) {
+      uint8_t* st = stage + h * 32 * kStagePitch16;
+      Pack<__half, 8> p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = *reinterpret_cast<const Pack<__half, 8>*>(st + lane * kStagePitch16 + u * 16);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        *reinterpret_cast<__half*>(st + j * kStagePitch16 + lane * 2) = p[j / 8].v[j % 8];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < SPLIT; ++h)
+      copy_block16(stage + h * 32 * kStagePitch16, out + h * g.lo + (int64_t)c0 * g.ld + r0, g.ld, cols, rows, lane);
+  }
+  __syncwarp();
+}
+
+template <int AM, int BMJ, int SPLIT, int CG, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const Args g) {
-  constexpr int kStage = 2 * SPLIT * kTile;  // A (hi, lo), B (hi, lo)
+  constexpr int TM = 128 * CG;                   // rows of a tile; 128 of them in each CTA
+  constexpr int NB = BN / CG;                    // rows of B in each CTA
+  constexpr int kTileA = 128 * BK * 2, kTileB = NB * BK * 2;
+  constexpr int kStage = SPLIT * (kTileA + kTileB);  // A (hi, lo), B (hi, lo)
   constexpr int kStages = kRing / kStage;
+  constexpr int kCols = kAcc * SPLIT * BN;       // tensor memory: accumulators of the hi (and lo) products
+  static_assert(kCols <= 512 && (kCols & (kCols - 1)) == 0, "tensor memory columns");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + kRing;
@@ -192,9 +331,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* consumed = abort_flag + 1;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0;  // in the pair
+  const int first = blockIdx.x / CG, step = gridDim.x / CG;
   const int kblocks = (g.K + BK - 1) / BK;
-  const int ntm = (g.M + BM - 1) / BM, ntn = (g.N + BN - 1) / BN;
-  const int ntiles = (g.symmetric ? ntm * (ntm + 1) / 2 : ntm * ntn) * g.batch;
+  const int run = SPLIT == 2 ? kRunBlocks : kblocks;  // K slices per accumulator
+  const int ntm = (g.M + TM - 1) / TM, ntn = (g.N + BN - 1) / BN;
+  const int ntiles = (g.symmetric ? TM / BN * (ntm * (ntm + 1) / 2) : ntm * ntn) * g.batch;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -203,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int a = 0; a < kAcc; ++a) {
       mbar_init(&acc_full[a], 1);
-      mbar_init(&acc_empty[a], kEpiWarps);
+      mbar_init(&acc_empty[a], CG * kEpiWarps);
     }
     *abort_flag = 0;
     *consumed = 0;
@@ -212,79 +354,98 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tb)) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)),
-                 "r"(kAcc * BN));
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)),
+                   "r"(kCols));
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)),
+                   "r"(kCols));
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
   }
   tc_fence_before();
   __syncthreads();
+  if (CG == 2) cluster_sync();  // both CTAs' barriers are ready
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
+  // what is above overlaps the end of the launch before; its results are read and its operands
+  // written over only from here on
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   if (warp == 0) {
     if (lane == 0) {
-      int it = 0, issued = 0;
-      for (int t = blockIdx.x; t < ntiles && !*abort_flag; t += gridDim.x) {
+      int it = 0;
+      for (int t = first; t < ntiles && !*abort_flag; t += step) {
         int m0, n0, b;
-        tile_at(t, g.symmetric, ntm, ntn, m0, n0, b);
+        tile_at<TM, BN>(t, g.symmetric, ntm, ntn, m0, n0, b);
         for (int kb = 0; kb < kblocks; ++kb, ++it) {
           const int s = it % kStages;
           if (!mbar_wait(&empty[s], ((it / kStages) & 1) ^ 1, kWaitNs) || *abort_flag) {
             *abort_flag = 1;
             break;
           }
-          expect_tx(&full[s], kStage);
+          if (rank == 0) expect_tx(&full[s], CG * kStage);
+          const uint32_t bar = CG == 2 ? in_leader(&full[s]) : smem_u32(&full[s]);
           const uint32_t st = smem_u32(smem + s * kStage);
 #pragma unroll
           for (int h = 0; h < SPLIT; ++h) {
-            load_tile<AM>(st + h * kTile, &ta, &full[s], m0, kb * BK, b + h * g.batch);
-            load_tile<BMJ>(st + (SPLIT + h) * kTile, &tb, &full[s], n0, kb * BK, b + h * g.batch);
+            load_tile<AM, 128, CG>(st + h * kTileA, &ta, bar, m0 + rank * 128, kb * BK, b + h * g.batch);
+            load_tile<BMJ, NB, CG>(st + SPLIT * kTileA + h * kTileB, &tb, bar, n0 + rank * NB, kb * BK,
+                                   b + h * g.batch);
           }
-          issued = it + 1;
         }
       }
-      if (*abort_flag)  // copies in flight land before the shared memory goes away
-        for (int i = *consumed; i < issued; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, kWaitNs);
+      // every slice consumed, and its release arrived here, before this CTA's barriers go away
+      for (int i = max(0, it - kStages); i < it && !*abort_flag; ++i)
+        if (!mbar_wait(&empty[i % kStages], (i / kStages) & 1, kWaitNs)) *abort_flag = 1;
+      if (*abort_flag) {
+        // copies in flight land before the shared memory goes away: those of the slices not yet
+        // consumed, whose barriers only the pair's first CTA holds, within a bound far above a copy's time
+        if (rank == 0)
+          for (int i = *consumed; i < it; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, 10000000ull);
+        const uint64_t t0 = globaltimer();
+        while (globaltimer() - t0 < 10000000ull) {
+        }
+      }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_f16(BM, BN, AM, BMJ);
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_f16(TM, BN, AM, BMJ);
       int it = 0, n = 0;
-      for (int t = blockIdx.x; t < ntiles && !*abort_flag; t += gridDim.x, ++n) {
-        const int a = n % kAcc;
-        if (n >= kAcc && !mbar_wait(&acc_empty[a], ((n / kAcc) & 1) ^ 1, kWaitNs)) {
-          *abort_flag = 1;
-          break;
-        }
-        tc_fence_after();
-        const uint32_t d = tmem + static_cast<uint32_t>(a * BN);
-        bool ok = true;
-        for (int kb = 0; kb < kblocks; ++kb, ++it) {
-          const int s = it % kStages;
-          if (!mbar_wait(&full[s], (it / kStages) & 1, kWaitNs) || *abort_flag) {
-            ok = false;
+      for (int t = first; t < ntiles && !*abort_flag; t += step) {
+        for (int k0 = 0; k0 < kblocks && !*abort_flag; k0 += run, ++n) {
+          const int a = n % kAcc;
+          if (n >= kAcc && !mbar_wait(&acc_empty[a], ((n / kAcc) & 1) ^ 1, kWaitNs)) {
+            *abort_flag = 1;
             break;
           }
-          *consumed = it + 1;
           tc_fence_after();
-          const uint32_t as = smem_u32(smem + s * kStage), bs = as + SPLIT * kTile;
-          if (SPLIT == 2) {  // the small products first
+          const uint32_t d = tmem + static_cast<uint32_t>(a * SPLIT * BN);
+          const int k1 = min(kblocks, k0 + run);
+          for (int kb = k0; kb < k1; ++kb, ++it) {
+            const int s = it % kStages;
+            if (!mbar_wait(&full[s], (it / kStages) & 1, kWaitNs) || *abort_flag) {
+              *abort_flag = 1;
+              break;
+            }
+            *consumed = it + 1;
+            tc_fence_after();
+            const uint32_t as = smem_u32(smem + s * kStage), bs = as + SPLIT * kTileA;
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk) {
-              umma_f16(d, tile_desc<AM>(as + kTile, kk), tile_desc<BMJ>(bs, kk), idesc, (kb | kk) != 0);
-              umma_f16(d, tile_desc<AM>(as, kk), tile_desc<BMJ>(bs + kTile, kk), idesc, 1);
+              const uint32_t more = kb > k0 || kk > 0;
+              umma_f16<CG>(d, tile_desc<AM>(as, kk), tile_desc<BMJ>(bs, kk), idesc, more);
+              if (SPLIT == 2) {
+                umma_f16<CG>(d + BN, tile_desc<AM>(as + kTileA, kk), tile_desc<BMJ>(bs, kk), idesc, more);
+                umma_f16<CG>(d + BN, tile_desc<AM>(as, kk), tile_desc<BMJ>(bs + kTileB, kk), idesc, 1);
+              }
             }
+            commit<CG>(&empty[s]);
           }
-#pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk)
-            umma_f16(d, tile_desc<AM>(as, kk), tile_desc<BMJ>(bs, kk), idesc, SPLIT == 2 || (kb | kk) != 0);
-          umma_commit(&empty[s]);
+          if (!*abort_flag) commit<CG>(&acc_full[a]);
         }
-        if (!ok) {
-          *abort_flag = 1;
-          break;
-        }
-        umma_commit(&acc_full[a]);
       }
     }
   } else {
@@ -292,120 +453,101 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* stage = staging + (warp - 2) * kStaging;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16);
     int n = 0;
-    for (int t = blockIdx.x; t < ntiles; t += gridDim.x, ++n) {
+    auto wait_acc = [&](int a) {
+      const bool ok = mbar_wait(&acc_full[a], (n / kAcc) & 1, kWaitNs) && !*abort_flag;
+      if (!ok) {
+        if (lane == 0 && g.status) atomicOr(g.status, kStatusTimeout);
+        *abort_flag = 1;
+      }
+      tc_fence_after();
+      return __all_sync(0xffffffffu, ok);
+    };
+    auto release_acc = [&](int a) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t bar = CG == 2 ? in_leader(&acc_empty[a]) : smem_u32(&acc_empty[a]);
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+      }
+    };
+    for (int t = first; t < ntiles; t += step) {
       int m0, n0, b;
-      tile_at(t, g.symmetric, ntm, ntn, m0, n0, b);
-      const int a = n % kAcc;
-      const int r0 = m0 + 32 * q, r = r0 + lane;
+      tile_at<TM, BN>(t, g.symmetric, ntm, ntn, m0, n0, b);
+      const int r0 = m0 + rank * 128 + 32 * q, r = r0 + lane;
       const int rows = min(32, g.M - r0);
+      const bool mirror = g.symmetric && n0 + BN <= m0;
       float f = 1.f;
       if (g.t_pow > 0) {
         f = g.t[b];
         if (g.t_pow > 1) f *= f;
       }
       const float alpha = g.alpha * f, beta = g.beta * f;
-      if (!mbar_wait(&acc_full[a], (n / kAcc) & 1, kWaitNs) || *abort_flag) {
-        if (lane == 0 && g.status) atomicOr(g.status, kStatusTimeout);
-        *abort_flag = 1;
-        break;
-      }
-      tc_fence_after();
-      for (int c = 0; c < BN / 32; ++c) {
-        const int c0 = n0 + 32 * c;
-        const int cols = min(32, g.N - c0);
-        if (cols <= 0) break;
-        uint4 ch[4], cl[4];
-        const bool has_c = g.cin && r < g.M;
-        if (has_c) {
-          const __half* src = g.cin + (int64_t)b * g.cin_stride + (int64_t)r * g.cin_ld + c0;
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (u * 8 < cols) {
-              ch[u] = *reinterpret_cast<const uint4*>(src + u * 8);
-              if (SPLIT == 2) cl[u] = *reinterpret_cast<const uint4*>(src + g.cin_lo + u * 8);
-            }
-        }
-        float o[32];
-        __syncwarp();
-        tmem_ld32(lanes + static_cast<uint32_t>(a * BN + 32 * c), o);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] *= alpha;
-        if (has_c) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (u * 8 < cols) {
-              const __half* h = reinterpret_cast<const __half*>(&ch[u]);
-              const __half* l = reinterpret_cast<const __half*>(&cl[u]);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                float x = __half2float(h[e]);
-                if (SPLIT == 2) x += __half2float(l[e]);
-                o[u * 8 + e] = fmaf(beta, x, o[u * 8 + e]);
-              }
-            }
-        }
-        if (rows <= 0) continue;
-        if (g.user) {
-          const int64_t at = (int64_t)b * g.user_stride + (int64_t)r0 * g.user_ld + c0;
-          if (g.user_type == SOAP_F32)
-            store_user(stage, o, static_cast<float*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
-          else if (g.user_type == SOAP_BF16)
-            store_user(stage, o, static_cast<__nv_bfloat16*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
-          else
-            store_user(stage, o, static_cast<__half*>(g.user) + at, g.user_ld, rows, cols, g.user_vec, lane);
-          continue;
-        }
-        __half* out = g.out + (int64_t)b * g.stride;
-#pragma unroll
-        for (int h = 0; h < SPLIT; ++h) {
-          uint8_t* st = stage + h * 32 * kStagePitch16;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            Pack<__half, 8> p;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              p.v[e] = __float2half_rn(o[u * 8 + e]);
-              o[u * 8 + e] -= __half2float(p.v[e]);
-            }
-            *reinterpret_cast<Pack<__half, 8>*>(st + lane * kStagePitch16 + u * 16) = p;
-          }
-        }
-        __syncwarp();
-#pragma unroll
-        for (int h = 0; h < SPLIT; ++h)
-          copy_block16(stage + h * 32 * kStagePitch16, out + h * g.lo + (int64_t)r0 * g.ld + c0, g.ld, rows, cols, lane);
-        if (g.symmetric && n0 < m0) {
-          // the mirror block: read a staged row per lane, write it as a column
-#pragma unroll
-          for (int h = 0; h < SPLIT; ++h) {
-            uint8_t* st = stage + h * 32 * kStagePitch16;
-            Pack<__half, 8> p[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) p[u] = *reinterpret_cast<const Pack<__half, 8>*>(st + lane * kStagePitch16 + u * 16);
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              *reinterpret_cast<__half*>(st + j * kStagePitch16 + lane * 2) = p[j / 8].v[j % 8];
-          }
+      const bool has_c = g.cin && r < g.M;
+      const __half* src = g.cin + (int64_t)b * g.cin_stride + (int64_t)r * g.cin_ld + n0;
+      if constexpr (SPLIT == 1) {
+        const int a = n % kAcc;
+        Cin<1> c_now, c_next;
+        if (has_c) load_cin<1>(c_now, src, 0, g.N - n0);
+        if (!wait_acc(a)) break;
+        for (int c = 0; c < BN / 32; ++c) {
+          const int cols = min(32, g.N - n0 - 32 * c);
+          if (cols <= 0) break;
+          if (has_c && c + 1 < BN / 32) load_cin<1>(c_next, src + 32 * (c + 1), 0, g.N - n0 - 32 * (c + 1));
+          float o[32];
           __syncwarp();
+          tmem_ld32(lanes + static_cast<uint32_t>(a * BN + 32 * c), o);
 #pragma unroll
-          for (int h = 0; h < SPLIT; ++h)
-            copy_block16(stage + h * 32 * kStagePitch16, out + h * g.lo + (int64_t)c0 * g.ld + r0, g.ld, cols, rows,
-                         lane);
+          for (int j = 0; j < 32; ++j) o[j] *= alpha;
+          if (has_c) add_cin<1>(c_now, beta, cols, o);
+          if (rows > 0) store_block<1>(g, stage, o, b, r0, n0 + 32 * c, rows, cols, mirror, lane);
+          c_now = c_next;
         }
-        __syncwarp();
+        release_acc(a);
+        ++n;
+      } else {
+        float sum[BN / 32][32];
+        bool ok = true;
+        for (int k0 = 0; k0 < kblocks; k0 += run, ++n) {
+          const int a = n % kAcc;
+          if (!(ok = wait_acc(a))) break;
+#pragma unroll
+          for (int c = 0; c < BN / 32; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float o[32];
+              tmem_ld32(lanes + static_cast<uint32_t>((a * 2 + (h ^ 1)) * BN + 32 * c), o);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sum[c][j] = k0 == 0 && h == 0 ? o[j] : sum[c][j] + o[j];
+            }
+          release_acc(a);
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < BN / 32; ++c) {
+          const int cols = min(32, g.N - n0 - 32 * c);
+          if (cols > 0 && rows > 0) {
+            Cin<2> cin;
+            if (has_c) load_cin<2>(cin, src + 32 * c, g.cin_lo, cols);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[c][j] *= alpha;
+            if (has_c) add_cin<2>(cin, beta, cols, sum[c]);
+            __syncwarp();
+            store_block<2>(g, stage, sum[c], b, r0, n0 + 32 * c, rows, cols, mirror, lane);
+          }
+        }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&acc_empty[a])) : "memory");
     }
   }
 
   tc_fence_before();
   __syncthreads();
+  if (CG == 2) cluster_sync();  // neither CTA leaves while the other may still reach its shared memory
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kAcc * BN));
+    if (CG == 2)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
   }
 }
 
@@ -422,24 +564,53 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-template <int AM, int BMJ, int SPLIT>
-cudaError_t launch(const Mat& a, const Mat& b, const Args& g, cudaStream_t s) {
+template <int AM, int BMJ, int SPLIT, int CG, int BN>
+cudaError_t launch(const Mat& a, const Mat& b, const Args& g, int64_t tiles, int dev, int sms, cudaStream_t s) {
   static std::atomic<uint64_t> attr_set{0};  // one bit per device that has the shared-memory attribute
-  int dev = 0, sms = 152;
-  if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
+  const auto kernel = product_kernel<AM, BMJ, SPLIT, CG, BN>;
   const uint64_t bit = (dev >= 0 && dev < 64) ? uint64_t(1) << dev : 0;
   if (bit == 0 || !(attr_set.load(std::memory_order_relaxed) & bit)) {
-    const cudaError_t e = cudaFuncSetAttribute(product_kernel<AM, BMJ, SPLIT>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     attr_set.fetch_or(bit, std::memory_order_relaxed);
   }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(CG * std::min<int64_t>(tiles, sms / CG)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a.map, b.map, g);
+}
+
+int64_t tile_count(const Args& g, int tm, int tn) {
+  const int64_t ntm = (g.M + tm - 1) / tm, ntn = (g.N + tn - 1) / tn;
+  return (g.symmetric ? tm / tn * (ntm * (ntm + 1) / 2) : ntm * ntn) * g.batch;
+}
+
+// Tile shape by the time of its waves: a 256 x 256 pair tile takes 128 cycles per 16 K elements at
+// the tensor cores' rate, a 256 x 128 one 64 and somewhat more for its operand traffic, a single
+// CTA's 128 x 128 tile 64 and half as much again.
+template <int AM, int BMJ, int SPLIT>
+cudaError_t launch_best(const Mat& a, const Mat& b, const Args& g, cudaStream_t s) {
+  int dev = 0, sms = 152;
+  if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  const int64_t ntm = (g.M + BM - 1) / BM, ntn = (g.N + BN - 1) / BN;
-  const int64_t tiles = (g.symmetric ? ntm * (ntm + 1) / 2 : ntm * ntn) * g.batch;
-  if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;
-  product_kernel<AM, BMJ, SPLIT><<<(int)std::min<int64_t>(tiles, sms), kThreads, kSmem, s>>>(a.map, b.map, g);
-  return cudaGetLastError();
+  const int64_t t256 = tile_count(g, 256, 256), t128 = tile_count(g, 256, 128), t1 = tile_count(g, 128, 128);
+  if (std::max(t1, t128) > (int64_t(1) << 30)) return cudaErrorInvalidValue;
+  const int64_t pairs = std::max(1, sms / 2);
+  const int64_t c256 = (t256 + pairs - 1) / pairs * 128, c128 = (t128 + pairs - 1) / pairs * 75;
+  const int64_t c1 = (t1 + sms - 1) / sms * 100;
+  if (SPLIT == 1 && c256 <= c128 && c256 <= c1) return launch<AM, BMJ, SPLIT, 2, SPLIT == 1 ? 256 : 128>(a, b, g, t256, dev, sms, s);
+  if (c128 <= c1) return launch<AM, BMJ, SPLIT, 2, 128>(a, b, g, t128, dev, sms, s);
+  return launch<AM, BMJ, SPLIT, 1, 128>(a, b, g, t1, dev, sms, s);
 }
 
 }  // namespace
@@ -493,9 +664,11 @@ cudaError_t product(const Product& p, const Mat& a, const Mat& b, cudaStream_t s
   ProfScope prof(kFamGemmTc, 2.0 * half * mn * p.K,
                  2.0 * (p.split ? 2 : 1) * ((double)(p.M + (p.symmetric ? 0 : p.N)) * p.K * p.batch + mn), s);
   if (p.a_major == kRowsK && p.b_major == kRowsK)
-    return p.split ? launch<kRowsK, kRowsK, 2>(a, b, g, s) : launch<kRowsK, kRowsK, 1>(a, b, g, s);
-  if (p.a_major == kRowsK) return p.split ? launch<kRowsK, kRowsM, 2>(a, b, g, s) : launch<kRowsK, kRowsM, 1>(a, b, g, s);
-  if (p.b_major == kRowsM) return p.split ? launch<kRowsM, kRowsM, 2>(a, b, g, s) : launch<kRowsM, kRowsM, 1>(a, b, g, s);
+    return p.split ? launch_best<kRowsK, kRowsK, 2>(a, b, g, s) : launch_best<kRowsK, kRowsK, 1>(a, b, g, s);
+  if (p.a_major == kRowsK)
+    return p.split ? launch_best<kRowsK, kRowsM, 2>(a, b, g, s) : launch_best<kRowsK, kRowsM, 1>(a, b, g, s);
+  if (p.b_major == kRowsM)
+    return p.split ? launch_best<kRowsM, kRowsM, 2>(a, b, g, s) : launch_best<kRowsM, kRowsM, 1>(a, b, g, s);
   return cudaErrorInvalidValue;
 }
 
