@@ -11,7 +11,7 @@
 // (11 bits) per element leaves the iteration's error below the result's own rounding; fp16 and fp32
 // results take hi + lo pairs (22 bits). M enters scaled by a power of two only, which is exact for
 // bf16 and fp16 inputs; the remaining factor t in (1, 2] of 1 / max(||M||_F, eps) is applied in
-// fp32 in the first step's epilogues.
+// fp32 in the first step's results.
 //
 // Range. With sigma <= u before a step, S <= u^2, |B| <= max |b s + c s^2| on [0, u^2] and
 // sigma <= max |sigma (a + b sigma^2 + c sigma^4)| after it, all at the ends or at the roots of a
@@ -31,7 +31,7 @@ namespace ortho {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxParts = 64;  // partial sums of squares per matrix
+constexpr int kMaxParts = 1216;  // partial sums of squares per matrix: 8 CTAs per SM
 
 // Squares of a pack's elements: in fp32 where no square over- or underflows (or the pack is zero),
 // else in double. NaN and inf come out as such either way.
@@ -59,17 +59,24 @@ __global__ void __launch_bounds__(kThreads)
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   double d = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
-    float s = 0.f;
-    int n = 0;
-    for (int64_t c = lane * V; c < cols; c += 32 * V) {
-      add_squares(*reinterpret_cast<const Pack<T, V>*>(m + r * ld + c), s, d);
-      if (++n == 8) {  // short fp32 runs
-        d += (double)s;
-        s = 0.f;
-        n = 0;
+    const T* row = m + r * ld;
+    for (int64_t c0 = lane * V; c0 < cols; c0 += 4 * 32 * V) {  // four loads in flight, one fp32 run
+      Pack<T, V> p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t c = c0 + u * 32 * V;
+        if (c < cols) {
+          p[u] = *reinterpret_cast<const Pack<T, V>*>(row + c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) p[u].v[e] = from_f32<T>(0.f);
+        }
       }
+      float s = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add_squares(p[u], s, d);
+      d += (double)s;
     }
-    d += (double)s;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
@@ -85,12 +92,20 @@ __global__ void __launch_bounds__(kThreads)
 template <typename T, int V, int SPLIT>
 __global__ void __launch_bounds__(kThreads)
     scale_kernel(const T* M, int64_t ld, int64_t stride, int64_t rows, int64_t cols, const double* part, int parts,
-                 float eps, int sx, __half* X, int64_t ld_x, int64_t stride_x, int64_t lo, float* t, int* status) {
+                 float eps, int sx, __half* X, int64_t ld_x, int64_t stride_x, int64_t lo, float* t, int* done,
+                 int* status) {
   __shared__ float scale;
+  __shared__ double red[kThreads / 32];
   const int b = blockIdx.y;
+  double s = 0.0;
+  for (int p = threadIdx.x; p < parts; p += kThreads) s += part[(int64_t)b * parts + p];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = s;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int p = 0; p < parts; ++p) s += part[(int64_t)b * parts + p];
+    if (blockIdx.x == 0) done[b] = 0;
+    for (int w = 1; w < kThreads / 32; ++w) s += red[w];
     const double norm = sqrt(s);
     if (!(norm <= 1.7e308)) {  // NaN or inf: so is the result
       scale = 1.f;
@@ -134,7 +149,7 @@ struct Plan {
   bool split;
   int ld_x, ld_s;
   int64_t x_elems, s_elems;  // per buffer, planes included
-  size_t part_off, t_off, x_off[2], s_off, b_off, bytes;
+  size_t part_off, t_off, done_off, x_off[2], s_off, b_off, bytes;
 };
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -161,6 +176,10 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
   };
   p.part_off = take((size_t)batch * kMaxParts * sizeof(double));
   p.t_off = take((size_t)batch * sizeof(float));
+  p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)batch * sizeof(int));
   p.x_off[0] = take((size_t)p.x_elems * 2);
   p.x_off[1] = take((size_t)p.x_elems * 2);
   p.s_off = take((size_t)p.s_elems * 2);
@@ -214,8 +233,8 @@ double step_bound(double a, double b, double c, double u) {
 }
 
 template <typename T, int V>
-cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float eps, int sx, const Mat& X, double* part,
-                    float* t, int* status, cudaStream_t s) {
+cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float eps, int sx, const Steps& q,
+                    double* part, float* t, cudaStream_t s) {
   const double n = (double)p.batch * p.rows * p.cols;
   const int64_t want = std::max<int64_t>(1, (152 * 8) / p.batch);
   const int parts = (int)std::min<int64_t>({kMaxParts, want, (p.rows + 7) / 8});
@@ -228,106 +247,72 @@ cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float
   ProfScope prof(kFamElementwise, n, n * (sizeof(T) + (p.split ? 4 : 2)), s);
   const int64_t packs = p.rows * ((p.cols + V - 1) / V);
   const dim3 grid((unsigned)std::min<int64_t>(want, (packs + kThreads - 1) / kThreads), (unsigned)p.batch);
-  const int64_t lo = X.stride * p.batch;
+  const int64_t sx_elems = p.rows * q.ld_x, lo = sx_elems * p.batch;
   if (p.split)
-    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, X.p, X.ld,
-                                                    X.stride, lo, t, status);
+    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, q.x[0], q.ld_x,
+                                                    sx_elems, lo, t, q.done, q.status);
   else
-    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, X.p, X.ld,
-                                                    X.stride, lo, t, status);
+    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, q.x[0], q.ld_x,
+                                                    sx_elems, lo, t, q.done, q.status);
   return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t prepare_t(const Plan& p, const void* M, int64_t ld, int64_t stride, float eps, int sx, const Mat& X,
-                      double* part, float* t, int* status, cudaStream_t s) {
+cudaError_t prepare_t(const Plan& p, const void* M, int64_t ld, int64_t stride, float eps, int sx, const Steps& q,
+                      double* part, float* t, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const bool vec = reinterpret_cast<uintptr_t>(M) % 16 == 0 && ld % V == 0 && (p.batch == 1 || stride % V == 0) &&
                    p.cols % V == 0;
   const T* m = static_cast<const T*>(M);
-  return vec ? prepare<T, V>(p, m, ld, stride, eps, sx, X, part, t, status, s)
-             : prepare<T, 1>(p, m, ld, stride, eps, sx, X, part, t, status, s);
+  return vec ? prepare<T, V>(p, m, ld, stride, eps, sx, q, part, t, s)
+             : prepare<T, 1>(p, m, ld, stride, eps, sx, q, part, t, s);
 }
 
 cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_t type, const float* coeffs, int steps,
                 float eps, void* out, int64_t ld_out, int64_t stride_out, uint8_t* ws, int* status, cudaStream_t s) {
-  const int planes = (int)p.batch * (p.split ? 2 : 1);
-  Mat X[2], S, B;
-  for (int i = 0; i < 2; ++i) {
-    X[i] = Mat{reinterpret_cast<__half*>(ws + p.x_off[i]), (int)p.rows, (int)p.cols, p.ld_x, p.rows * p.ld_x, {}};
-    if (!make_map(X[i], planes)) return cudaErrorInvalidValue;
-  }
-  S = Mat{reinterpret_cast<__half*>(ws + p.s_off), p.r, p.r, p.ld_s, (int64_t)p.r * p.ld_s, {}};
-  B = Mat{reinterpret_cast<__half*>(ws + p.b_off), p.r, p.r, p.ld_s, (int64_t)p.r * p.ld_s, {}};
-  if (!make_map(S, planes) || !make_map(B, planes)) return cudaErrorInvalidValue;
-  double* part = reinterpret_cast<double*>(ws + p.part_off);
+  Steps q{};
+  q.rows = (int)p.rows;
+  q.cols = (int)p.cols;
+  q.batch = (int)p.batch;
+  q.steps = steps;
+  q.split = p.split;
+  for (int i = 0; i < 2; ++i) q.x[i] = reinterpret_cast<__half*>(ws + p.x_off[i]);
+  q.s = reinterpret_cast<__half*>(ws + p.s_off);
+  q.b = reinterpret_cast<__half*>(ws + p.b_off);
+  q.ld_x = p.ld_x;
+  q.ld_s = p.ld_s;
   float* t = reinterpret_cast<float*>(ws + p.t_off);
-
-  int sx = scale_exp(2.0);
-  cudaError_t e;
-  if (type == SOAP_F32)
-    e = prepare_t<float>(p, M, ld, stride, eps, sx, X[0], part, t, status, s);
-  else if (type == SOAP_BF16)
-    e = prepare_t<__nv_bfloat16>(p, M, ld, stride, eps, sx, X[0], part, t, status, s);
-  else
-    e = prepare_t<__half>(p, M, ld, stride, eps, sx, X[0], part, t, status, s);
-  if (e != cudaSuccess) return e;
-
+  q.t = t;
+  q.done = reinterpret_cast<int*>(ws + p.done_off);
+  q.out = out;
+  q.out_type = type;
+  q.ld_out = ld_out;
+  q.stride_out = stride_out;
+  q.status = status;
   double u = 1.0;  // bound of the singular values
-  int at = 0;
+  int sx = scale_exp(2.0);
+  const int sx0 = sx;
   for (int i = 0; i < steps; ++i) {
     const double a = coeffs ? coeffs[3 * i] : 15.0 / 8, b = coeffs ? coeffs[3 * i + 1] : -10.0 / 8,
                  c = coeffs ? coeffs[3 * i + 2] : 3.0 / 8;
-    const bool last = i + 1 == steps;
     const int ss = scale_exp(2 * u * u), sb = scale_exp(2 * poly_bound(b, c, u * u));
     u = step_bound(a, b, c, u);
-    const int sn = scale_exp(2 * u);
-    Product q{};
-    q.batch = (int)p.batch;
-    q.split = p.split;
-    q.t = t;
-    q.status = status;
-    // S 2^ss = t^2 2^(ss - 2 sx) (X 2^sx) (X 2^sx)^T
-    q.M = q.N = p.r;
-    q.K = p.k;
-    q.symmetric = true;
-    q.a_major = q.b_major = p.tall ? kRowsM : kRowsK;
-    q.alpha = (float)std::ldexp(1.0, ss - 2 * sx);
-    q.t_pow = i == 0 ? 2 : 0;
-    q.out = &S;
-    e = product(q, X[at], X[at], s);
-    if (e != cudaSuccess) return e;
-    // B 2^sb = c 2^(sb - 2 ss) (S 2^ss)^2 + b 2^(sb - ss) (S 2^ss)
-    q.K = p.r;
-    q.a_major = q.b_major = kRowsK;
-    q.alpha = (float)std::ldexp(c, sb - 2 * ss);
-    q.beta = (float)std::ldexp(b, sb - ss);
-    q.cin = &S;
-    q.t_pow = 0;
-    q.out = &B;
-    e = product(q, S, S, s);
-    if (e != cudaSuccess) return e;
-    // X' 2^sn = t (2^(sn - sb - sx) (B 2^sb) (X 2^sx) + a 2^(sn - sx) (X 2^sx)), or X B for tall ones
-    const int so = last ? 0 : sn;
-    q.M = (int)p.rows;
-    q.N = (int)p.cols;
-    q.symmetric = false;
-    q.b_major = p.tall ? kRowsK : kRowsM;
-    q.alpha = (float)std::ldexp(1.0, so - sb - sx);
-    q.beta = (float)std::ldexp(a, so - sx);
-    q.cin = &X[at];
-    q.t_pow = i == 0 ? 1 : 0;
-    q.out = last ? nullptr : &X[at ^ 1];
-    q.user = out;
-    q.user_type = type;
-    q.user_ld = ld_out;
-    q.user_stride = stride_out;
-    e = p.tall ? product(q, X[at], B, s) : product(q, B, X[at], s);
-    if (e != cudaSuccess) return e;
-    at ^= 1;
+    const int sn = i + 1 == steps ? 0 : scale_exp(2 * u);
+    // S 2^ss = 2^(ss - 2 sx) (X 2^sx) (X 2^sx)^T, B 2^sb = c 2^(sb - 2 ss) (S 2^ss)^2 + b 2^(sb - ss) (S 2^ss),
+    // X' 2^sn = 2^(sn - sb - sx) (B 2^sb) (X 2^sx) + a 2^(sn - sx) (X 2^sx)
+    q.coef[i] = {(float)std::ldexp(1.0, ss - 2 * sx), (float)std::ldexp(c, sb - 2 * ss), (float)std::ldexp(b, sb - ss),
+                 (float)std::ldexp(1.0, sn - sb - sx), (float)std::ldexp(a, sn - sx)};
     sx = sn;
   }
-  return cudaSuccess;
+  double* part = reinterpret_cast<double*>(ws + p.part_off);
+  cudaError_t e;
+  if (type == SOAP_F32)
+    e = prepare_t<float>(p, M, ld, stride, eps, sx0, q, part, t, s);
+  else if (type == SOAP_BF16)
+    e = prepare_t<__nv_bfloat16>(p, M, ld, stride, eps, sx0, q, part, t, s);
+  else
+    e = prepare_t<__half>(p, M, ld, stride, eps, sx0, q, part, t, s);
+  return e == cudaSuccess ? run_steps(q, s) : e;
 }
 
 bool bad_operand(const void* p, int64_t ld, int64_t stride, int64_t batch, int64_t rows, int64_t cols, int32_t type) {
@@ -353,7 +338,7 @@ soap_status_t muon_orthogonalize(int32_t batch, int64_t rows, int64_t cols, cons
                                  int64_t ld_out, int64_t stride_out, void* workspace, size_t workspace_bytes,
                                  int32_t* status, soap_stream_t stream) {
   if (ortho::bad_sizes(batch, rows, cols, type)) return SOAP_ERR_INVALID_ARG;
-  if (ns_steps < 1 || ns_steps > 64 || !(eps > 0.f) || !std::isfinite(eps)) return SOAP_ERR_INVALID_ARG;
+  if (ns_steps < 1 || ns_steps > ortho::kMaxSteps || !(eps > 0.f) || !std::isfinite(eps)) return SOAP_ERR_INVALID_ARG;
   if (coeffs)
     for (int i = 0; i < 3 * ns_steps; ++i)
       if (!std::isfinite(coeffs[i])) return SOAP_ERR_INVALID_ARG;

@@ -1,7 +1,6 @@
 // Internal declarations of the stand-alone orthogonalisation (include/muon.h, muon_orthogonalize).
 #pragma once
 
-#include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -9,37 +8,34 @@
 namespace soap {
 namespace ortho {
 
-// A batch of row-major fp16 matrices with a leading dimension that is a multiple of 8, scaled by a
-// power of two. Split operands hold x = hi + lo as two planes: matrix b's hi part at index b, its
-// lo part at index batch + b. The columns between cols and ld hold nothing that counts.
-struct Mat {
-  __half* p;
-  int rows, cols, ld;
-  int64_t stride;  // elements between matrices (and planes)
-  CUtensorMap map; // boxes of 64 x 64 elements, 128-byte swizzle
+constexpr int kMaxSteps = 64;
+
+// One Newton-Schulz step on scaled fp16 intermediates (the scales are powers of two):
+//   S = s_alpha t^2 X X^T,  B = b_alpha S S + b_beta S,  X' = t (x_alpha B X + x_beta X)
+// with t applied in the first step only.
+struct StepCoef {
+  float s_alpha, b_alpha, b_beta, x_alpha, x_beta;
 };
 
-// How an operand's M (or N) x K elements are stored.
-enum Major : int { kRowsK = 0 /* row m, column k */, kRowsM = 1 /* row k, column m */ };
-
-struct Product {
-  int M, N, K, batch;
-  bool split;      // operands (and an internal result) are hi + lo pairs
-  bool symmetric;  // M = N and the result is symmetric: tiles below the diagonal, mirrored
-  Major a_major, b_major;
-  float alpha, beta;      // out = t^t_pow (alpha A B^T + beta cin)
-  const Mat* cin;         // same rows and columns as the result, or nullptr
-  const float* t;         // per matrix
-  int t_pow;              // 0, 1 or 2
-  const Mat* out;         // internal result, or
-  void* user;             // the caller's matrix: type, leading dimension, stride between matrices
-  int user_type;
-  int64_t user_ld, user_stride;
+// What steps_kernel works on. X: batch matrices of rows x cols (row-major, leading dimension ld_x, a
+// multiple of 8), twice; S and B: batch r x r matrices, r = min(rows, cols). With `split`, every
+// matrix is a hi + lo pair: matrix b's hi plane at index b, its lo plane at index batch + b. The
+// first X is the input; the last step writes the caller's matrices.
+struct Steps {
+  int rows, cols, batch, steps;
+  bool split;
+  __half *x[2], *s, *b;
+  int ld_x, ld_s;
+  const float* t;  // per matrix
+  int* done;       // per matrix, zero
+  void* out;       // out_type (soap_dtype_t), leading dimension, elements between matrices
+  int out_type;
+  int64_t ld_out, stride_out;
   int* status;
+  StepCoef coef[kMaxSteps];
 };
 
-bool make_map(Mat& m, int planes);
-cudaError_t product(const Product& p, const Mat& a, const Mat& b, cudaStream_t s);
+cudaError_t run_steps(const Steps& p, cudaStream_t s);
 
 }  // namespace ortho
 }  // namespace soap
