@@ -109,14 +109,10 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
 
 // 128 x 64 elements of an operand at (row m0, k0) as boxes of 64: rows of 64 K elements each
 // (K-major), or 64 K rows of 64 columns (MN-major).
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int mn_major, int m0,
-                                          int k0, int z) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (mn_major)
-      tma_box(dst + i * kBox, map, bar, m0 + i * 64, k0, z);
-    else
-      tma_box(dst + i * kBox, map, bar, k0, m0 + i * 64, z);
+template <int MN>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int m0, int k0, int z) {
+  tma_box(dst, map, bar, MN ? m0 : k0, MN ? k0 : m0, z);
+  tma_box(dst + kBox, map, bar, MN ? m0 + 64 : k0, MN ? k0 : m0 + 64, z);
 }
 
 // Descriptor of the 16 K elements at step kk of such a tile. K-major: 32 bytes further along the
@@ -362,16 +358,38 @@ __device__ __forceinline__ void store_user_any(uint8_t* stage, const float (&v)[
     store_user(stage, v, static_cast<__half*>(a.out) + at, a.ld_out, rows, cols, vec, lane);
 }
 
-// The state of the MMA-issuing thread: ring slot and its parity.
-struct Issue {
+// A thread's place in the ring: the slot and the parity it waits for.
+struct Ring {
   int s = 0;
   uint32_t parity = 0;
   bool ok = true;
 };
 
+// K slices kb .. to - 1 of a tile into the ring: rows am of A's map and bn of B's.
+template <int SPLIT, int A_MN, int B_MN>
+__device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUtensorMap* ma, const CUtensorMap* mb,
+                                            int am, int bn, int b, int batch, uint32_t ring, uint64_t* full,
+                                            uint64_t* empty, uint32_t leader_full, int rank) {
+  using C = Config<SPLIT>;
+  for (; kb < to; ++kb) {
+    if (!(st.ok = mbar_wait(&empty[st.s], st.parity, kWaitNs))) return;
+    if (rank == 0) expect_tx(&full[st.s], 2 * C::kStage);
+    const uint32_t at = ring + st.s * C::kStage, bar = leader_full + st.s * 8;
+#pragma unroll
+    for (int h = 0; h < SPLIT; ++h) {
+      load_tile<A_MN>(at + h * kTile, ma, bar, am, kb * BK, b + h * batch);
+      load_tile<B_MN>(at + (SPLIT + h) * kTile, mb, bar, bn, kb * BK, b + h * batch);
+    }
+    if (++st.s == C::kStages) {
+      st.s = 0;
+      st.parity ^= 1;
+    }
+  }
+}
+
 // `count` K slices from the ring into the accumulator at d (split: the small products at d + 256).
 template <int SPLIT, int A_MN, int B_MN>
-__device__ __forceinline__ void issue_slices(Issue& st, int count, uint32_t& more, uint32_t ring, uint64_t* full,
+__device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t ring, uint64_t* full,
                                              uint64_t* empty, uint32_t d) {
   using C = Config<SPLIT>;
   constexpr uint32_t idesc = idesc_f16(A_MN, B_MN);
@@ -441,11 +459,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      int s = 0, used = 0;     // ring slot, slots filled so far (up to kStages)
-      uint32_t parity = 1;     // of the slot's release
+      Ring st;
+      st.parity = 1;  // of a slot's release
+      int used = 0;   // slots filled so far (up to kStages)
       const uint32_t ring = smem_u32(smem), bars = in_leader(full);
-      bool ok = true;
-      for (int p = first; p < l.total && ok && !*abort_flag; p += stride) {
+      for (int p = first; p < l.total && st.ok && !*abort_flag; p += stride) {
         const Tile t = tile_at(p, l, a);
         const int kblocks = (t.K + BK - 1) / BK;
         int a_change, b_change;
@@ -453,33 +471,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const CUtensorMap* x = &maps.x[t.step & 1];
         const CUtensorMap* ma = t.phase == 0 ? x : t.phase == 1 ? &maps.s : l.tall ? x : &maps.b;
         const CUtensorMap* mb = t.phase == 0 ? x : t.phase == 1 ? &maps.s : l.tall ? &maps.b : x;
-        if (!(ok = wait_done(a.done + t.b, t.need))) break;
+        if (!(st.ok = wait_done(a.done + t.b, t.need))) break;
         asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
         const int am = t.m0 + rank * 128, bn = t.n0 + rank * 128;
-        for (int kb = 0; kb < kblocks; ++kb) {
-          if (!(ok = mbar_wait(&empty[s], parity, kWaitNs))) break;
-          if (rank == 0) expect_tx(&full[s], 2 * C::kStage);
-          const uint32_t st = ring + s * C::kStage, bar = bars + s * 8;
-#pragma unroll
-          for (int h = 0; h < SPLIT; ++h) {
-            load_tile(st + h * kTile, ma, bar, kb >= a_change, am, kb * BK, t.b + h * a.batch);
-            load_tile(st + (SPLIT + h) * kTile, mb, bar, kb >= b_change, bn, kb * BK, t.b + h * a.batch);
-          }
-          used = min(used + 1, kStages);
-          if (++s == kStages) {
-            s = 0;
-            parity ^= 1;
-          }
+        used = min(used + kblocks, kStages);
+        for (int kb = 0; kb < kblocks && st.ok;) {  // stretches of slices of one order
+          const bool a_mn = kb >= a_change, b_mn = kb >= b_change;
+          const int to = min(a_mn ? kblocks : a_change, b_mn ? kblocks : b_change);
+          if (a_mn && b_mn)
+            load_slices<SPLIT, 1, 1>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
+          else if (a_mn)
+            load_slices<SPLIT, 1, 0>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
+          else if (b_mn)
+            load_slices<SPLIT, 0, 1>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
+          else
+            load_slices<SPLIT, 0, 0>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
+          kb = to;
         }
       }
       // every slice consumed, and its release arrived here, before this CTA's barriers go away
-      for (int i = 0; i < kStages && ok && !*abort_flag; ++i) {
-        if (used == kStages || s - 1 - i >= 0) {
-          const int slot = (s - 1 - i + kStages) % kStages;
-          ok = mbar_wait(&empty[slot], slot < s ? parity ^ 1 : parity, kWaitNs);
+      for (int i = 0; i < kStages && st.ok && !*abort_flag; ++i) {
+        if (used == kStages || st.s - 1 - i >= 0) {
+          const int slot = (st.s - 1 - i + kStages) % kStages;
+          st.ok = mbar_wait(&empty[slot], slot < st.s ? st.parity ^ 1 : st.parity, kWaitNs);
         }
       }
-      if (!ok || *abort_flag) {
+      if (!st.ok || *abort_flag) {
         *abort_flag = 1;
         if (a.status) atomicOr(a.status, kStatusTimeout);
         // copies in flight land before the shared memory goes away: far above a copy's time
@@ -490,7 +507,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      Issue st;
+      Ring st;
       int n = 0;
       const uint32_t ring = smem_u32(smem);
       for (int p = first; p < l.total && st.ok && !*abort_flag; p += stride) {
