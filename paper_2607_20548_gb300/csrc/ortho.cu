@@ -181,6 +181,8 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
   p.done_off = take((size_t)batch * sizeof(int));
   p.done_off = take((size_t)batch * sizeof(int));
   p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)batch * sizeof(int));
   p.x_off[0] = take((size_t)p.x_elems * 2);
   p.x_off[1] = take((size_t)p.x_elems * 2);
   p.s_off = take((size_t)p.s_elems * 2);

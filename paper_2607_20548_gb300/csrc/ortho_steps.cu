@@ -11,7 +11,7 @@
 // Split operands (x = hi + lo, 22 bits) take three products, hi hi, lo hi and hi lo, from one load
 // of the four tiles. The accumulator truncates: measured, a sum loses 2^-25 of itself per 16
 // products. With 11-bit operands that is nothing; split ones keep the small products in an
-// accumulator of their own and take K in runs of at most 768, whose sums the epilogue adds in fp32.
+// accumulator of their own and take K in runs of at most 1024, whose sums the epilogue adds in fp32.
 //
 // Schedule. Persistent CTA pairs (cta_group::2, a pair's 256 x 256 tile has 128 rows in each CTA)
 // walk one list of tiles in turn: for each step all S tiles, then all B tiles, then all X' tiles. A
@@ -52,7 +52,7 @@ using namespace tc;
 constexpr int BK = 64;
 constexpr int kBox = 64 * 64 * 2;      // one TMA box: 64 rows of 128 bytes
 constexpr int kTile = 2 * kBox;        // a CTA's 128 x 64 elements of an operand
-constexpr int kRunBlocks = 12;         // most K slices per accumulator run of split operands
+constexpr int kRunBlocks = 16;         // most K slices per accumulator run of split operands
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kBlock = 32 * 128;       // a staged block: 32 rows of 128 bytes
@@ -157,17 +157,41 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
+// Columns taddr .. taddr + 63, and 16 columns at each of two places, of this lane's accumulator row.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[32], float (&w)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+      "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, "
+      "%42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, "
+      "%62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]),
+        "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]),
+        "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]),
+        "=f"(v[29]), "=f"(v[30]), "=f"(v[31]), "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]),
+        "=f"(w[5]), "=f"(w[6]), "=f"(w[7]), "=f"(w[8]), "=f"(w[9]), "=f"(w[10]), "=f"(w[11]), "=f"(w[12]),
+        "=f"(w[13]), "=f"(w[14]), "=f"(w[15]), "=f"(w[16]), "=f"(w[17]), "=f"(w[18]), "=f"(w[19]),
+        "=f"(w[20]), "=f"(w[21]), "=f"(w[22]), "=f"(w[23]), "=f"(w[24]), "=f"(w[25]), "=f"(w[26]),
+        "=f"(w[27]), "=f"(w[28]), "=f"(w[29]), "=f"(w[30]), "=f"(w[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld16x2(uint32_t t0, uint32_t t1, float (&v)[16], float (&w)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]),
+        "=f"(v[15]), "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]), "=f"(w[5]), "=f"(w[6]),
+        "=f"(w[7]), "=f"(w[8]), "=f"(w[9]), "=f"(w[10]), "=f"(w[11]), "=f"(w[12]), "=f"(w[13]), "=f"(w[14]),
+        "=f"(w[15])
+      : "r"(t0), "r"(t1)
+      : "memory");
 }
 
 __device__ __forceinline__ int load_acquire(const int* p) {
@@ -184,6 +208,24 @@ __device__ __forceinline__ bool wait_done(const int* done, int need) {
     for (int i = 0; i < 64; ++i)
       if (load_acquire(done) >= need) return true;
     if (globaltimer() - t0 > kWaitNs) return false;
+  }
+}
+
+// The count of tiles whose inputs are there, from the loading thread to the CTA's epilogue warps.
+__device__ __forceinline__ void set_ready(uint32_t at, int n) {
+  asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(n) : "memory");
+}
+__device__ __forceinline__ int get_ready(uint32_t at) {
+  int n;
+  asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(at) : "memory");
+  return n;
+}
+__device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
+  const uint64_t t0 = globaltimer();
+  for (;;) {
+    for (int i = 0; i < 64; ++i)
+      if (get_ready(at) >= n) return true;
+    if (globaltimer() - t0 > 2 * kWaitNs) return false;
   }
 }
 
@@ -275,9 +317,15 @@ __device__ __forceinline__ void send_block(const CUtensorMap* map, uint32_t src,
                : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// The sent blocks' buffers have been read / the blocks are in global memory.
-__device__ __forceinline__ void sent_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void sent_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// The buffers of all sent blocks but the last N have been read / those blocks are in global memory.
+template <int N>
+__device__ __forceinline__ void sent_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void sent_done() {
+  asm volatile("cp.async.bulk.wait_group %0;" ::"n"(N) : "memory");
+}
 // This thread's plain accesses to shared memory come before later TMA accesses to it.
 __device__ __forceinline__ void before_tma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -414,6 +462,37 @@ __device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more
   }
 }
 
+// An epilogue warp's part of a tile: up to two blocks of 32 rows x 64 columns from (r0, n0).
+struct Work {
+  Tile t;
+  int r0, n0, blocks;
+  bool has_c, last;    // the result takes C; it goes to the caller's matrix
+  float alpha, beta;
+  const CUtensorMap *cin, *out;
+};
+
+__device__ __forceinline__ Work work_at(const Tile& t, const Steps& a, const Maps& maps, int row, int col) {
+  Work w;
+  w.t = t;
+  w.r0 = t.m0 + row;
+  w.n0 = t.n0 + col;
+  // none below the last row, and to the last column
+  w.blocks = w.r0 < t.M && w.n0 < t.N ? min(2, (t.N - w.n0 + 63) / 64) : 0;
+  w.has_c = t.phase > 0 && w.blocks > 0;
+  w.last = t.phase == 2 && t.step + 1 == a.steps;
+  const StepCoef& c = a.coef[t.step];
+  w.alpha = t.phase == 0 ? c.s_alpha : t.phase == 1 ? c.b_alpha : c.x_alpha;
+  w.beta = t.phase == 1 ? c.b_beta : c.x_beta;
+  if (t.step == 0 && t.phase != 1) {
+    const float f = a.t[t.b];
+    w.alpha *= t.phase == 0 ? f * f : f;
+    w.beta *= f;
+  }
+  w.cin = t.phase == 1 ? &maps.es : &maps.ex[t.step & 1];
+  w.out = t.phase == 0 ? &maps.es : t.phase == 1 ? &maps.eb : &maps.ex[(t.step & 1) ^ 1];
+  return w;
+}
+
 template <int SPLIT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     steps_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Steps a, const Layout l, const int out_vec) {
@@ -429,6 +508,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* cin_full = acc_empty + kAcc;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(cin_full + kEpiWarps * C::kBufs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
+  const uint32_t ready_at = smem_u32(tmem_at + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x & 1);  // in the pair
@@ -445,6 +525,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kEpiWarps * C::kBufs; ++i) mbar_init(&cin_full[i], 1);
     *abort_flag = 0;
+    set_ready(ready_at, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -463,6 +544,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       st.parity = 1;  // of a slot's release
       int used = 0;   // slots filled so far (up to kStages)
       const uint32_t ring = smem_u32(smem), bars = in_leader(full);
+      int ready = 0;
       for (int p = first; p < l.total && st.ok && !*abort_flag; p += stride) {
         const Tile t = tile_at(p, l, a);
         const int kblocks = (t.K + BK - 1) / BK;
@@ -473,6 +555,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const CUtensorMap* mb = t.phase == 0 ? x : t.phase == 1 ? &maps.s : l.tall ? &maps.b : x;
         if (!(st.ok = wait_done(a.done + t.b, t.need))) break;
         asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
+        set_ready(ready_at, ++ready);
         const int am = t.m0 + rank * 128, bn = t.n0 + rank * 128;
         used = min(used + kblocks, kStages);
         for (int kb = 0; kb < kblocks && st.ok;) {  // stretches of slices of one order
@@ -550,125 +633,135 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     uint64_t* cin_bar = cin_full + (warp - 2) * C::kBufs;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16) + 128 * half;
     int n = 0;
-    uint32_t cin_parity[2] = {0, 0};
+    int k = 0;                  // blocks so far: block k uses buffer k % kBufs
+    uint32_t cin_parity = 0;    // one bit per buffer
     int* unreported = nullptr;  // counter of the matrix whose tile this warp has sent but not reported
+    bool ok = true;
     auto wait_acc = [&](int ac) {
-      const bool ok = mbar_wait(&acc_full[ac], (n / kAcc) & 1, kWaitNs) && !*abort_flag;
+      ok = mbar_wait(&acc_full[ac], (n / kAcc) & 1, kWaitNs) && !*abort_flag;
       tc_fence_after();
-      return __all_sync(0xffffffffu, ok);
+      return ok = __all_sync(0xffffffffu, ok);
     };
     auto release_acc = [&](int ac) {
       tc_fence_before();
       __syncwarp();
       if (lane == 0)
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_leader(&acc_empty[ac]))
-                     : "memory");
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_leader(&acc_empty[ac])) : "memory");
     };
-    auto report = [&]() {
+    // Reports the last tile; `newer` blocks of the present one have been sent since.
+    auto report = [&](auto newer) {
       if (unreported && lane == 0) {
-        sent_done();
+        sent_done<decltype(newer)::value>();
         asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(unreported) : "memory");
       }
       unreported = nullptr;
     };
-    bool ok = true;
-    for (int p = first; p < l.total && ok; p += stride) {
-      const Tile t = tile_at(p, l, a);
-      const int r0 = t.m0 + rank * 128 + 32 * q, n0 = t.n0 + 128 * half;
-      const int rows = min(32, t.M - r0);
-      // this warp's 32 x 64 blocks: none below the last row, and to the last column
-      const int blocks = rows > 0 && n0 < t.N ? min(2, (t.N - n0 + 63) / 64) : 0;
-      const bool last = t.phase == 2 && t.step + 1 == a.steps;
-      const StepCoef& c = a.coef[t.step];
-      float alpha = t.phase == 0 ? c.s_alpha : t.phase == 1 ? c.b_alpha : c.x_alpha;
-      float beta = t.phase == 1 ? c.b_beta : c.x_beta;
-      if (t.step == 0 && t.phase != 1) {
-        const float f = a.t[t.b];
-        alpha *= t.phase == 0 ? f * f : f;
-        beta *= f;
+    auto fetch = [&](const Work& w, int i, int h, int buf) {  // w's block i, part h of C
+      if (lane == 0)
+        fetch_block(stage_at + buf * kBlock, w.cin, &cin_bar[buf], w.n0 + 64 * i, w.r0, w.t.b + h * a.batch);
+    };
+    auto fetched = [&](int buf) {
+      ok = mbar_wait(&cin_bar[buf], (cin_parity >> buf) & 1, kWaitNs);
+      cin_parity ^= 1u << buf;
+      return ok = __all_sync(0xffffffffu, ok);
+    };
+    auto send = [&](const Work& w, int i, int h, int buf) {
+      before_tma();
+      __syncwarp();
+      if (lane == 0) send_block(w.out, stage_at + buf * kBlock, w.n0 + 64 * i, w.r0, w.t.b + h * a.batch);
+    };
+    auto to_user = [&](const Work& w, uint8_t* st, int i, int h, const float (&v)[32]) {
+      const int c0 = w.n0 + 64 * i + 32 * h;
+      if (c0 < w.t.N)
+        store_user_any(st, v, a, out_vec, w.t.b, w.r0, c0, min(32, w.t.M - w.r0), min(32, w.t.N - c0), lane);
+    };
+    const int wr = rank * 128 + 32 * q, wc = 128 * half;  // this warp's place in a tile
+    Work w = work_at(tile_at(first, l, a), a, maps, wr, wc);
+    bool asked = false;  // the first block's C is on its way
+    int m = 0;           // tiles so far
+    for (int p = first; p < l.total; p += stride, ++m) {
+      if (!asked) {
+        // a tile that has to wait may wait for this warp's own last one: that is reported first
+        int there = lane == 0 ? get_ready(ready_at) : 0;
+        if (__shfl_sync(0xffffffffu, there, 0) <= m) {
+          report(std::integral_constant<int, 0>());
+          if (lane == 0) ok = wait_ready(ready_at, m + 1);
+          if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
+        }
+        if (w.has_c) {
+          if (lane == 0) sent_read<0>();
+          fetch(w, 0, SPLIT - 1, k % C::kBufs);
+        }
       }
-      const bool has_c = t.phase > 0 && blocks > 0;
-      const CUtensorMap* cin = t.phase == 1 ? &maps.es : &maps.ex[t.step & 1];
-      const CUtensorMap* out = t.phase == 0 ? &maps.es : t.phase == 1 ? &maps.eb : &maps.ex[(t.step & 1) ^ 1];
-      // C is what other CTAs stored; what this tile writes over has been read. A tile that has to wait
-      // may wait for this warp's own last one: that is reported first.
-      int* done = a.done + t.b;
-      if (lane == 0) ok = load_acquire(done) >= t.need;
-      if (!__shfl_sync(0xffffffffu, ok, 0)) {
-        report();
-        if (lane == 0) ok = wait_done(done, t.need);
-        if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
-      }
-      ok = true;
-      auto fetch = [&](int i, int h) {  // block i's part h of C into buffer i % kBufs
-        if (lane == 0)
-          fetch_block(stage_at + (i % C::kBufs) * kBlock, cin, &cin_bar[i % C::kBufs], n0 + 64 * i, r0,
-                      t.b + h * a.batch);
-      };
-      auto fetched = [&](int i) {
-        const int k = i % C::kBufs;
-        ok = mbar_wait(&cin_bar[k], cin_parity[k], kWaitNs);
-        cin_parity[k] ^= 1;
-        ok = __all_sync(0xffffffffu, ok);
-      };
-      auto send = [&](int i, int h) {
-        before_tma();
-        __syncwarp();
-        if (lane == 0) send_block(out, stage_at + (i % C::kBufs) * kBlock, n0 + 64 * i, r0, t.b + h * a.batch);
-      };
-      auto to_user = [&](uint8_t* st, int i, int h, const float (&v)[32]) {
-        const int c0 = n0 + 64 * i + 32 * h;
-        if (c0 < t.N) store_user_any(st, v, a, out_vec, t.b, r0, c0, rows, min(32, t.N - c0), lane);
-      };
-      if (has_c) {
-        asm volatile("fence.proxy.async;" ::: "memory");
-        if (SPLIT == 1)
-          for (int i = 0; i < blocks; ++i) fetch(i, 0);
-        else
-          fetch(0, 1);
-      }
-      report();
+      const bool more = p + stride < l.total;
+      Work next = w;
+      if (more) next = work_at(tile_at(p + stride, l, a), a, maps, wr, wc);
+      asked = false;
+      const float alpha = w.alpha, beta = w.beta;
       if constexpr (SPLIT == 1) {
         const int ac = n % kAcc;
-        if (!(ok = wait_acc(ac))) break;
-        if (blocks == 0) release_acc(ac);
-        for (int i = 0; i < blocks && ok; ++i) {
-          uint8_t* st = stage + i * kBlock;
+        if (!wait_acc(ac)) break;
+        if (w.blocks == 0) release_acc(ac);
+        for (int i = 0; i < w.blocks; ++i, ++k) {
+          const int buf = k & 1;
+          uint8_t* st = stage + buf * kBlock;
           float v[2][32];
-          tmem_ld32(lanes + static_cast<uint32_t>(ac * 256 + 64 * i), v[0]);
-          tmem_ld32(lanes + static_cast<uint32_t>(ac * 256 + 64 * i + 32), v[1]);
-          if (i + 1 == blocks) release_acc(ac);
-          if (has_c) fetched(i);
+          tmem_ld64(lanes + static_cast<uint32_t>(ac * 256 + 64 * i), v[0], v[1]);
+          if (i + 1 == w.blocks) release_acc(ac);
+          // the next block's C, into the buffer of the block before
+          if (i + 1 < w.blocks) {
+            if (w.has_c) {
+              if (lane == 0) sent_read<0>();
+              fetch(w, i + 1, 0, buf ^ 1);
+            }
+          } else if (more && next.has_c) {
+            const int there = lane == 0 ? get_ready(ready_at) : 0;
+            asked = __shfl_sync(0xffffffffu, there, 0) > m + 1;
+            if (asked) {
+              if (lane == 0) sent_read<0>();
+              fetch(next, 0, 0, buf ^ 1);
+            }
+          }
+          if (w.has_c) {
+            if (!fetched(buf)) break;
+          } else {
+            if (lane == 0) sent_read<1>();
+            __syncwarp();
+          }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[h][j] *= alpha;
-            if (has_c) add_row(st, h, beta, v[h], lane);
+            if (w.has_c) add_row(st, h, beta, v[h], lane);
           }
-          if (last) {
+          if (w.last) {
             __syncwarp();
-            to_user(st, i, 0, v[0]);
-            to_user(st, i, 1, v[1]);
+            to_user(w, st, i, 0, v[0]);
+            to_user(w, st, i, 1, v[1]);
             before_tma();
+            __syncwarp();
           } else {
             put_row<false>(st, 0, v[0], lane);
             put_row<false>(st, 1, v[1], lane);
-            send(i, 0);
+            send(w, i, 0, buf);
+            if (i == 0) report(std::integral_constant<int, 1>());
           }
         }
+        if (!ok) break;
         ++n;
+        report(std::integral_constant<int, 0>());  // where this tile sent nothing
       } else {
+        report(std::integral_constant<int, 0>());
         float sum[4][32];
-        const int kblocks = (t.K + BK - 1) / BK;
+        const int kblocks = (w.t.K + BK - 1) / BK;
         const int runs = (kblocks + kRunBlocks - 1) / kRunBlocks;
         for (int i = 0; i < runs; ++i, ++n) {
-          if (!(ok = wait_acc(0))) break;
+          if (!wait_acc(0)) break;
 #pragma unroll
           for (int b = 0; b < 8; ++b)
-            if (b / 4 < blocks) {
+            if (b / 4 < w.blocks) {
               float hi[16], small[16];
-              tmem_ld16(lanes + 16 * b, hi);
-              tmem_ld16(lanes + 256 + 16 * b, small);
+              tmem_ld16x2(lanes + 16 * b, lanes + 256 + 16 * b, hi, small);
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
                 float& x = sum[b / 2][(b & 1) * 16 + j];
@@ -680,7 +773,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (i < blocks && ok) {
+          if (i < w.blocks && ok) {
             float(&v0)[32] = sum[2 * i];
             float(&v1)[32] = sum[2 * i + 1];
 #pragma unroll
@@ -688,42 +781,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               v0[j] *= alpha;
               v1[j] *= alpha;
             }
-            if (has_c) {  // the small part first
-              if (i > 0) fetch(i, 1);
-              fetched(i);
+            if (w.has_c) {  // the small part first
+              if (i > 0) fetch(w, i, 1, 0);
+              if (!fetched(0)) break;
               add_row(stage, 0, beta, v0, lane);
               add_row(stage, 1, beta, v1, lane);
               before_tma();
               __syncwarp();
-              fetch(i, 0);
-              fetched(i);
+              fetch(w, i, 0, 0);
+              if (!fetched(0)) break;
               add_row(stage, 0, beta, v0, lane);
               add_row(stage, 1, beta, v1, lane);
             }
-            if (last) {
+            if (w.last) {
               __syncwarp();
-              to_user(stage, i, 0, v0);
-              to_user(stage, i, 1, v1);
+              to_user(w, stage, i, 0, v0);
+              to_user(w, stage, i, 1, v1);
               before_tma();
             } else {
               put_row<true>(stage, 0, v0, lane);
               put_row<true>(stage, 1, v1, lane);
-              send(i, 0);
-              if (lane == 0) sent_read();
+              send(w, i, 0, 0);
+              if (lane == 0) sent_read<0>();
               __syncwarp();
               put_row<false>(stage, 0, v0, lane);
               put_row<false>(stage, 1, v1, lane);
-              send(i, 1);
-              if (lane == 0) sent_read();
+              send(w, i, 1, 0);
+              if (lane == 0) sent_read<0>();
             }
             __syncwarp();
           }
+        if (!ok) break;
       }
-      if (lane == 0) sent_read();
-      __syncwarp();
-      unreported = done;
+      unreported = a.done + w.t.b;
+      w = next;
     }
-    report();
+    if (ok) report(std::integral_constant<int, 0>());
     if (!ok) {
       *abort_flag = 1;
       if (lane == 0 && a.status) atomicOr(a.status, kStatusTimeout);
