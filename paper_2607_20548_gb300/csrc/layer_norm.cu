@@ -5,9 +5,14 @@
 //   dw = sum_rows dy xh, db = sum_rows dy
 //
 // Bound by memory: x is read and y written once (backward: x and dy read, dx written once). A
-// group of threads holds a row in registers, so that the variance is a second pass over
-// registers (not E[x^2] - mu^2, which cancels) and nothing is read twice.
+// group of threads holds a row in registers, so that the variance is a second pass over registers
+// (not E[x^2] - mu^2, which cancels) and nothing is read twice. CTAs are persistent: each thread
+// keeps its columns' weights (backward: and their gradients' sums) in registers over all its rows
+// (read again for every row, fp32 weights are four times the traffic of a bf16 x through L1: 3.1
+// TB/s at 32768 x 8192), and its rows come in kDepth ahead by cp.async into slots that only it reads,
+// so no barrier waits for them.
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/layer.h"
@@ -18,87 +23,197 @@ namespace soap {
 namespace {
 
 constexpr int kMaxThreads = 512;
+constexpr int kElems = 16;  // most elements of a row per thread
 
-// Sum over a row group's threads (blockDim.x of them, a multiple of 32 when more than a warp).
-// `slot` alternates between the two halves of `buf`, so that one barrier per call is enough: a
-// thread writes a half again only after the barrier of the call in between.
-template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float* buf, int& slot) {
+__device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-  if (blockDim.x <= 32) return;
-  const int nw = blockDim.x >> 5, w = threadIdx.x >> 5;
-  float* p = buf + ((slot * blockDim.y + threadIdx.y) * 32) * N;
-  slot ^= 1;
-  if ((threadIdx.x & 31) == 0)
-#pragma unroll
-    for (int i = 0; i < N; ++i) p[w * N + i] = v[i];
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// One barrier among a row group's threads (blockDim.x of them, more than a warp).
+__device__ __forceinline__ void group_barrier() {
   asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"((int)blockDim.x) : "memory");
+}
+
+// What a row group's warps exchange: two values per warp, in two halves used in turn, so that one
+// barrier per exchange is enough (a half is written again only after the barrier of the exchange
+// between).
+struct Exchange {
+  float2* buf;  // [2][blockDim.y][16]
+  int half = 0;
+  // Afterwards lane l holds warp l's values ((0, 0) from the last warp on).
+  __device__ __forceinline__ float2 all(float x, float y) {
+    float2* p = buf + (half * blockDim.y + threadIdx.y) * 16;
+    half ^= 1;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    if (lane == 0) p[threadIdx.x >> 5] = make_float2(x, y);
+    group_barrier();
+    return lane < warps ? p[lane] : make_float2(0.f, 0.f);
+  }
+};
+
+// N bytes from global to shared memory, asynchronously.
+template <int N>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(N) : "memory");
+}
+
+// A thread's part of the rows of a matrix, NV packs of V elements per row, kDepth rows in flight.
+// Packs of less than 4 bytes cannot be copied asynchronously and are loaded when they are used.
+template <typename T, int V, int NV, int DEPTH>
+struct Rows {
+  static constexpr bool kAsync = V * sizeof(T) >= 4;
+  static constexpr int kSlot = kAsync ? V * sizeof(T) : 0;
+  const T* base;
+  int64_t ld;
+  uint8_t* ring;  // this thread's slots: pack i of stage s at ((s * NV + i) * threads) * kSlot
+
+  __device__ __forceinline__ uint8_t* slot(int s, int i) const {
+    return ring + (size_t)((s * NV + i) * blockDim.x * blockDim.y) * kSlot;
+  }
+  __device__ __forceinline__ void request(int64_t row, int s, int width) const {
+    if constexpr (kAsync) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = 0.f;
-  for (int j = 0; j < nw; ++j)
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * blockDim.x + threadIdx.x) * V;
+        if (c < width) copy_async<V * sizeof(T)>(slot(s, i), base + row * ld + c);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int64_t row, int s, int width, Pack<T, V> (&p)[NV]) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += p[j * N + i];
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * V;
+      if (c < width)
+        p[i] = kAsync ? *reinterpret_cast<const Pack<T, V>*>(slot(s, i))
+                      : *reinterpret_cast<const Pack<T, V>*>(base + row * ld + c);
+    }
+  }
+};
+
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void arrived() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // ---- forward: a group of blockDim.x threads per row, NV packs of V elements each ------------
 
-template <typename T, typename W, int V, int NV>
+template <typename T, typename W, int V, int NV, int DEPTH>
 __global__ void __launch_bounds__(kMaxThreads)
     norm_fwd_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
                     float* mean, float* rstd, int64_t rows, int width) {
-  __shared__ float buf[2 * 16 * 32];
-  int slot = 0;
-  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  if (row >= rows) return;
-  const T* xr = x + row * ld_x;
-  float v[NV * V];
-  float s[1] = {0.f};
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float2 buf[2 * 16 * 16];
+  constexpr int E = NV * V;
+  using R = Rows<T, V, NV, DEPTH>;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x, lane = threadIdx.x & 31;
+  const R in{x, ld_x, smem + (size_t)tid * R::kSlot};
+  Exchange ex{buf};
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s) {
+    if (row + s * step < rows) in.request(row + s * step, s, width);
+    commit();
+  }
+  float w[E], b[E];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * blockDim.x + threadIdx.x) * V;
-    Pack<T, V> p;
-    if (c < width) p = *reinterpret_cast<const Pack<T, V>*>(xr + c);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      v[i * V + e] = c < width ? to_f32(p.v[e]) : 0.f;
-      s[0] += v[i * V + e];
+      w[i * V + e] = weight && c < width ? to_f32(weight[c + e]) : 1.f;
+      b[i * V + e] = bias && c < width ? to_f32(bias[c + e]) : 0.f;
     }
   }
-  group_sum(s, buf, slot);
-  const float mu = s[0] / (float)width;
-  float q[1] = {0.f};
+  // elements of the row in this thread's warp, and in the group's warp `lane`
+  auto warp_count = [&](int warp) {
+    int n = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const bool in = (i * blockDim.x + threadIdx.x) * V < width;
+    for (int i = 0; i < NV; ++i) n += max(0, min(32 * V, width - (int)(i * blockDim.x + warp * 32) * V));
+    return (float)n;
+  };
+  const float here = warp_count(threadIdx.x >> 5), inv = 1.f / (float)width;
+  const float there = lane < (int)blockDim.x / 32 ? warp_count(lane) : 0.f;
+  const float inv_here = here > 0.f ? 1.f / here : 0.f, inv_there = there > 0.f ? 1.f / there : 0.f;
+  int s = 0;
+  for (; row < rows; row += step) {
+    const int64_t ahead = row + (DEPTH - 1) * step;
+    if (ahead < rows) in.request(ahead, s == 0 ? DEPTH - 1 : s - 1, width);
+    commit();
+    arrived<DEPTH - 1>();
+    Pack<T, V> p[NV];
+    in.get(row, s, width, p);
+    s = s + 1 == DEPTH ? 0 : s + 1;
+    // sum and spread of the warp's elements about the warp's mean, then over the warps
+    float v[E], sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      v[i * V + e] -= mu;
-      if (in) q[0] = fmaf(v[i * V + e], v[i * V + e], q[0]);
+    for (int i = 0; i < NV; ++i) {
+      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        v[i * V + e] = in_row ? to_f32(p[i].v[e]) : 0.f;
+        sum += v[i * V + e];
+      }
+    }
+    sum = warp_sum(sum);
+    float mu = sum * inv_here, q = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = v[i * V + e] - mu;
+        if (in_row) q = fmaf(d, d, q);
+      }
+    }
+    q = warp_sum(q);
+    if (blockDim.x > 32) {
+      const float2 o = ex.all(sum, q);
+      mu = warp_sum(o.x) * inv;
+      const float d = o.x * inv_there - mu;
+      q = warp_sum(fmaf(there * d, d, o.y));
+    }
+    const float rs = 1.f / sqrtf(q * inv + eps);
+    if (threadIdx.x == 0) {
+      if (mean) mean[row] = mu;
+      if (rstd) rstd[row] = rs;
+    }
+    T* yr = y + row * ld_y;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * V;
+      if (c >= width) break;
+      Pack<T, V> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(fmaf((v[i * V + e] - mu) * rs, w[i * V + e], b[i * V + e]));
+      *reinterpret_cast<Pack<T, V>*>(yr + c) = o;
     }
   }
-  group_sum(q, buf, slot);
-  const float rs = 1.f / sqrtf(q[0] / (float)width + eps);
-  if (threadIdx.x == 0) {
-    if (mean) mean[row] = mu;
-    if (rstd) rstd[row] = rs;
-  }
-  T* yr = y + row * ld_y;
+  arrived<0>();
+}
+
+// Sum over a one-row CTA's threads, for the kernels that do not hold a row.
+template <int N>
+__device__ __forceinline__ void block_sum(float (&v)[N], float* buf) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * blockDim.x + threadIdx.x) * V;
-    if (c >= width) break;
-    Pack<W, V> w, b;
-    if (weight) w = *reinterpret_cast<const Pack<W, V>*>(weight + c);
-    if (bias) b = *reinterpret_cast<const Pack<W, V>*>(bias + c);
-    Pack<T, V> o;
+  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      o.v[e] = from_f32<T>(fmaf(v[i * V + e] * rs, weight ? to_f32(w.v[e]) : 1.f, bias ? to_f32(b.v[e]) : 0.f));
-    *reinterpret_cast<Pack<T, V>*>(yr + c) = o;
-  }
+    for (int i = 0; i < N; ++i) buf[(threadIdx.x >> 5) * N + i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.f;
+  for (int j = 0; j < (int)blockDim.x / 32; ++j)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += buf[j * N + i];
 }
 
 // Rows too wide for registers: one CTA per row, three passes over the row.
@@ -106,20 +221,19 @@ template <typename T, typename W>
 __global__ void __launch_bounds__(kMaxThreads)
     norm_fwd_wide_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
                          float* mean, float* rstd, int64_t width) {
-  __shared__ float buf[2 * 32];
-  int slot = 0;
+  __shared__ float buf[32];
   const int64_t row = blockIdx.x;
   const T* xr = x + row * ld_x;
   T* yr = y + row * ld_y;
   float s[1] = {0.f}, q[1] = {0.f};
   for (int64_t c = threadIdx.x; c < width; c += blockDim.x) s[0] += to_f32(xr[c]);
-  group_sum(s, buf, slot);
+  block_sum(s, buf);
   const float mu = s[0] / (float)width;
   for (int64_t c = threadIdx.x; c < width; c += blockDim.x) {
     const float d = to_f32(xr[c]) - mu;
     q[0] = fmaf(d, d, q[0]);
   }
-  group_sum(q, buf, slot);
+  block_sum(q, buf);
   const float rs = 1.f / sqrtf(q[0] / (float)width + eps);
   if (threadIdx.x == 0) {
     if (mean) mean[row] = mu;
@@ -136,55 +250,88 @@ __global__ void __launch_bounds__(kMaxThreads)
 // norm_cols_kernel adds the partial rows in order (no atomics: the result does not depend on
 // which CTA finishes first).
 
-template <typename T, typename W, int V, int NV>
+template <typename T, typename W, int V, int NV, int DEPTH>
 __global__ void __launch_bounds__(kMaxThreads)
     norm_bwd_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
                     const W* weight, T* dx, int64_t ld_dx, float* part, int64_t rows, int width) {
-  extern __shared__ float sums[];  // one float per thread and element: the groups' column sums
-  __shared__ float buf[2 * 16 * 32 * 2];
+  extern __shared__ __align__(16) uint8_t smem[];  // the rings; afterwards the groups' column sums
+  __shared__ float2 buf[2 * 16 * 16];
   constexpr int E = NV * V;
-  int slot = 0;
+  using R = Rows<T, V, NV, DEPTH>;
+  const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
+  const R rx{x, ld_x, smem + (size_t)tid * R::kSlot};
+  const R rg{dy, ld_dy, smem + (size_t)(DEPTH * NV * threads + tid) * R::kSlot};
+  Exchange ex{buf};
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s) {
+    if (row + s * step < rows) {
+      rx.request(row + s * step, s, width);
+      rg.request(row + s * step, s, width);
+    }
+    commit();
+  }
   float w[E], aw[E], ab[E];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * blockDim.x + threadIdx.x) * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      w[i * V + e] = c < width ? (weight ? to_f32(weight[c + e]) : 1.f) : 0.f;
+      w[i * V + e] = weight && c < width ? to_f32(weight[c + e]) : 1.f;
       aw[i * V + e] = ab[i * V + e] = 0.f;
     }
   }
   const float inv = 1.f / (float)width;
-  const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < rows; row += step) {
-    const T *xr = x + row * ld_x, *gr = dy + row * ld_dy;
-    Pack<T, V> px[NV], pg[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * V;
-      if (c < width) {
-        px[i] = *reinterpret_cast<const Pack<T, V>*>(xr + c);
-        pg[i] = *reinterpret_cast<const Pack<T, V>*>(gr + c);
-      }
+  float mu = 0.f, rs = 0.f;
+  if (row < rows) {
+    mu = mean[row];
+    rs = rstd[row];
+  }
+  int s = 0;
+  while (row < rows) {
+    const int64_t ahead = row + (DEPTH - 1) * step;
+    if (ahead < rows) {
+      const int to = s == 0 ? DEPTH - 1 : s - 1;
+      rx.request(ahead, to, width);
+      rg.request(ahead, to, width);
     }
-    const float mu = mean[row], rs = rstd[row];
-    float s[2] = {0.f, 0.f};
+    commit();
+    arrived<DEPTH - 1>();
+    Pack<T, V> px[NV], pg[NV];
+    rx.get(row, s, width, px);
+    rg.get(row, s, width, pg);
+    s = s + 1 == DEPTH ? 0 : s + 1;
+    const int64_t next = row + step;
+    float mu_next = 0.f, rs_next = 0.f;
+    if (next < rows) {
+      mu_next = mean[next];
+      rs_next = rstd[next];
+    }
+    float xh[E], g[E], s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const bool in = (i * blockDim.x + threadIdx.x) * V < width;
+      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float d = in ? to_f32(pg[i].v[e]) : 0.f;
-        const float xh = in ? (to_f32(px[i].v[e]) - mu) * rs : 0.f;
-        const float g = d * w[i * V + e];
-        s[0] += g;
-        s[1] = fmaf(g, xh, s[1]);
-        aw[i * V + e] = fmaf(d, xh, aw[i * V + e]);
-        ab[i * V + e] += d;
+        const int k = i * V + e;
+        const float d = in_row ? to_f32(pg[i].v[e]) : 0.f;
+        xh[k] = in_row ? (to_f32(px[i].v[e]) - mu) * rs : 0.f;
+        g[k] = d * w[k];
+        s0 += g[k];
+        s1 = fmaf(g[k], xh[k], s1);
+        aw[k] = fmaf(d, xh[k], aw[k]);
+        ab[k] += d;
       }
     }
-    group_sum(s, buf, slot);
-    const float m1 = s[0] * inv, m2 = s[1] * inv;
+    s0 = warp_sum(s0);
+    s1 = warp_sum(s1);
+    if (blockDim.x > 32) {
+      const float2 o = ex.all(s0, s1);
+      s0 = warp_sum(o.x);
+      s1 = warp_sum(o.y);
+    }
+    const float m1 = s0 * inv, m2 = s1 * inv;
     T* dr = dx + row * ld_dx;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -192,15 +339,17 @@ __global__ void __launch_bounds__(kMaxThreads)
       if (c >= width) break;
       Pack<T, V> o;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float xh = (to_f32(px[i].v[e]) - mu) * rs;
-        o.v[e] = from_f32<T>(rs * (to_f32(pg[i].v[e]) * w[i * V + e] - m1 - xh * m2));
-      }
+      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(rs * (g[i * V + e] - m1 - xh[i * V + e] * m2));
       *reinterpret_cast<Pack<T, V>*>(dr + c) = o;
     }
+    row = next;
+    mu = mu_next;
+    rs = rs_next;
   }
+  arrived<0>();
   if (!part) return;
   // add the groups in order, first dweight's sums, then dbias's
+  float* sums = reinterpret_cast<float*>(smem);
   const int lanes = blockDim.x * E;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -212,7 +361,7 @@ __global__ void __launch_bounds__(kMaxThreads)
         sums[threadIdx.y * lanes + (i * blockDim.x + threadIdx.x) * V + e] = k == 0 ? aw[i * V + e] : ab[i * V + e];
     __syncthreads();
     float* out = part + ((int64_t)blockIdx.x * 2 + k) * width;
-    for (int c = threadIdx.y * blockDim.x + threadIdx.x; c < width; c += blockDim.x * blockDim.y) {
+    for (int c = tid; c < width; c += threads) {
       float t = 0.f;
       for (int gq = 0; gq < (int)blockDim.y; ++gq) t += sums[gq * lanes + c];
       out[c] = t;
@@ -225,8 +374,7 @@ template <typename T, typename W>
 __global__ void __launch_bounds__(kMaxThreads)
     norm_bwd_wide_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
                          const W* weight, T* dx, int64_t ld_dx, int64_t width) {
-  __shared__ float buf[2 * 32 * 2];
-  int slot = 0;
+  __shared__ float buf[32 * 2];
   const int64_t row = blockIdx.x;
   const T *xr = x + row * ld_x, *gr = dy + row * ld_dy;
   T* dr = dx + row * ld_dx;
@@ -237,7 +385,7 @@ __global__ void __launch_bounds__(kMaxThreads)
     s[0] += g;
     s[1] = fmaf(g, (to_f32(xr[c]) - mu) * rs, s[1]);
   }
-  group_sum(s, buf, slot);
+  block_sum(s, buf);
   const float m1 = s[0] / (float)width, m2 = s[1] / (float)width;
   for (int64_t c = threadIdx.x; c < width; c += blockDim.x) {
     const float g = to_f32(gr[c]) * (weight ? to_f32(weight[c]) : 1.f);
@@ -266,6 +414,7 @@ __global__ void __launch_bounds__(kMaxThreads)
 // dweight and dbias from `parts` partial rows each: 32 columns per CTA, 32 row lanes.
 __global__ void norm_cols_kernel(const float* part, int parts, int64_t width, float* dweight, float* dbias) {
   __shared__ float red[32][33];
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch overlaps the end of the kernel before
   const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
   float* out = blockIdx.y == 0 ? dweight : dbias;
   if (!out) return;
@@ -286,22 +435,28 @@ __global__ void norm_cols_kernel(const float* part, int parts, int64_t width, fl
 constexpr int kParts = 152;  // most partial rows: one CTA per SM
 
 struct NormShape {
-  int v, nv, tx, ty;  // elements per access, accesses per thread, threads per row, rows per CTA
+  int nv, tx;  // accesses per thread and row, threads per row
 };
 
 // Threads for a row of `width` elements in accesses of v: at most 16 elements per thread, so that a
-// thread's columns and both of their sums stay in registers; nv = 0: too wide for that.
+// thread's columns and both of their sums stay in registers; nv = 0: too wide for that. Rows that a
+// warp or two can hold take fewer elements per thread.
 NormShape norm_shape(int64_t width, int v) {
   const int64_t packs = (width + v - 1) / v;
-  const int most = 16 / v;
+  const int most = kElems / v;
   for (int nv = 1; nv <= most; nv *= 2)
     for (int tx = 32; tx <= kMaxThreads; tx *= 2)
-      if (packs <= (int64_t)tx * nv && (nv == most || tx <= 64)) return {v, nv, tx, std::max(1, 256 / tx)};
-  return {v, 0, 0, 0};
+      if (packs <= (int64_t)tx * nv && (nv == most || tx <= 64)) return {nv, tx};
+  return {0, 0};
+}
+
+// Rows per CTA: full CTAs, unless the rows would then not reach every SM.
+int norm_groups(int64_t rows, int tx) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxThreads / tx, (rows + kParts - 1) / kParts));
 }
 
 template <typename F>
-auto with_nv(int nv, F&& f) {
+cudaError_t with_nv(int nv, F&& f) {
   switch (nv) {
     case 1: return f(std::integral_constant<int, 1>());
     case 2: return f(std::integral_constant<int, 2>());
@@ -311,8 +466,30 @@ auto with_nv(int nv, F&& f) {
   }
 }
 
-bool aligned(const void* p, int64_t ld, size_t size) {
-  return (reinterpret_cast<uintptr_t>(p) % 16) == 0 && ((size_t)ld * size) % 16 == 0;
+// f(elements per access): the widest access of up to 16 bytes that `bytes` (an OR of all addresses and
+// row lengths in bytes) divides into.
+template <typename T, typename F>
+cudaError_t with_access(uintptr_t bytes, F&& f) {
+  if (bytes % 16 == 0) return f(std::integral_constant<int, 16 / sizeof(T)>());
+  if (bytes % 8 == 0) return f(std::integral_constant<int, 8 / sizeof(T)>());
+  if (sizeof(T) < 4 && bytes % 4 == 0) return f(std::integral_constant<int, std::max<int>(1, 4 / sizeof(T))>());
+  return f(std::integral_constant<int, 1>());
+}
+
+uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+// One bit per device on which the kernel has its shared-memory attribute.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& set) {
+  if (bytes <= 48 * 1024 - 4096) return cudaSuccess;  // beside the static part
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (set.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  if (e == cudaSuccess) set.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 template <typename T, typename W, int V>
@@ -323,12 +500,18 @@ cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W
     norm_fwd_wide_kernel<T, W><<<(unsigned)rows, kMaxThreads, 0, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, width);
     return cudaGetLastError();
   }
-  const unsigned grid = (unsigned)((rows + n.ty - 1) / n.ty);
-  const dim3 block(n.tx, n.ty);
+  const int ty = norm_groups(rows, n.tx);
+  const unsigned grid = (unsigned)std::min<int64_t>(kParts, (rows + ty - 1) / ty);
   return with_nv(n.nv, [&](auto nv) {
-    constexpr int NV = decltype(nv)::value;
-    if constexpr (NV * V <= 16)
-      norm_fwd_kernel<T, W, V, NV><<<grid, block, 0, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, rows, (int)width);
+    constexpr int NV = decltype(nv)::value, DEPTH = 4;
+    if constexpr (NV * V <= kElems) {
+      static std::atomic<uint64_t> set{0};
+      const int smem = DEPTH * NV * n.tx * ty * Rows<T, V, NV, DEPTH>::kSlot;
+      const cudaError_t e = allow_smem(norm_fwd_kernel<T, W, V, NV, DEPTH>, smem, set);
+      if (e != cudaSuccess) return e;
+      norm_fwd_kernel<T, W, V, NV, DEPTH>
+          <<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, rows, (int)width);
+    }
     return cudaGetLastError();
   });
 }
@@ -336,63 +519,68 @@ cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W
 template <typename T, typename W>
 cudaError_t fwd_t(int64_t rows, int64_t width, const void* x, int64_t ld_x, const void* w, const void* b, float eps,
                   void* y, int64_t ld_y, float* mean, float* rstd, cudaStream_t s) {
-  constexpr int V = 16 / sizeof(T);
-  const bool vec = width % V == 0 && aligned(x, ld_x, sizeof(T)) && aligned(y, ld_y, sizeof(T)) && aligned(w, 0, 1) &&
-                   aligned(b, 0, 1);
-  const T* xt = static_cast<const T*>(x);
-  const W *wt = static_cast<const W*>(w), *bt = static_cast<const W*>(b);
-  if (vec) return fwd_v<T, W, V>(rows, width, xt, ld_x, wt, bt, eps, static_cast<T*>(y), ld_y, mean, rstd, s);
-  return fwd_v<T, W, 1>(rows, width, xt, ld_x, wt, bt, eps, static_cast<T*>(y), ld_y, mean, rstd, s);
-}
-
-int norm_parts(int64_t rows, int ty) {
-  return (int)std::min<int64_t>(kParts, (rows + ty - 1) / ty);
+  const uintptr_t bytes = address(x) | address(y) | (ld_x | ld_y | width) * sizeof(T);
+  return with_access<T>(bytes, [&](auto v) {
+    return fwd_v<T, W, decltype(v)::value>(rows, width, static_cast<const T*>(x), ld_x, static_cast<const W*>(w),
+                                           static_cast<const W*>(b), eps, static_cast<T*>(y), ld_y, mean, rstd, s);
+  });
 }
 
 template <typename T, typename W, int V>
 cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x,
                   const float* mean, const float* rstd, const W* w, T* dx, int64_t ld_dx, float* dw, float* db,
                   float* part, cudaStream_t s) {
-  NormShape n = norm_shape(width, V);
+  const NormShape n = norm_shape(width, V);
   float* p = dw || db ? part : nullptr;
-  int parts;
+  int parts = (int)std::min<int64_t>(kParts, rows);
+  cudaError_t e;
   if (n.nv == 0) {
-    parts = norm_parts(rows, 1);
     if (p)
       norm_cols_wide_kernel<T><<<dim3((unsigned)((width + 255) / 256), parts), 256, 0, s>>>(dy, ld_dy, x, ld_x, mean,
                                                                                            rstd, p, rows, width);
     norm_bwd_wide_kernel<T, W><<<(unsigned)rows, kMaxThreads, 0, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx,
                                                                      width);
+    e = cudaGetLastError();
   } else {
-    n.ty = std::max(1, kMaxThreads / n.tx);
-    parts = norm_parts(rows, n.ty);
-    with_nv(n.nv, [&](auto nv) {
-      constexpr int NV = decltype(nv)::value;
-      if constexpr (NV * V <= 16)
-        norm_bwd_kernel<T, W, V, NV><<<parts, dim3(n.tx, n.ty), n.tx * n.ty * NV * V * sizeof(float), s>>>(
-            dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, rows, (int)width);
-      return 0;
+    const int ty = norm_groups(rows, n.tx);
+    parts = (int)std::min<int64_t>(kParts, (rows + ty - 1) / ty);
+    e = with_nv(n.nv, [&](auto nv) {
+      constexpr int NV = decltype(nv)::value, DEPTH = sizeof(T) == 4 ? 3 : 4;
+      if constexpr (NV * V <= kElems) {
+        static std::atomic<uint64_t> set{0};
+        const int threads = n.tx * ty;
+        const int smem = threads * NV * std::max<int>(2 * DEPTH * Rows<T, V, NV, DEPTH>::kSlot, V * 4);
+        const cudaError_t ae = allow_smem(norm_bwd_kernel<T, W, V, NV, DEPTH>, smem, set);
+        if (ae != cudaSuccess) return ae;
+        norm_bwd_kernel<T, W, V, NV, DEPTH><<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx,
+                                                                                ld_dx, p, rows, (int)width);
+      }
+      return cudaGetLastError();
     });
   }
-  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !p) return e;
-  norm_cols_kernel<<<dim3((unsigned)((width + 31) / 32), 2), dim3(32, 32), 0, s>>>(p, parts, width, dw, db);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((width + 31) / 32), 2);
+  cfg.blockDim = dim3(32, 32);
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, norm_cols_kernel, static_cast<const float*>(p), parts, width, dw, db);
 }
 
 template <typename T, typename W>
 cudaError_t bwd_t(int64_t rows, int64_t width, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
                   const float* mean, const float* rstd, const void* w, void* dx, int64_t ld_dx, float* dw, float* db,
                   void* part, cudaStream_t s) {
-  constexpr int V = 16 / sizeof(T);
-  const bool vec = width % V == 0 && aligned(x, ld_x, sizeof(T)) && aligned(dy, ld_dy, sizeof(T)) &&
-                   aligned(dx, ld_dx, sizeof(T));
-  const T *xt = static_cast<const T*>(x), *gt = static_cast<const T*>(dy);
-  const W* wt = static_cast<const W*>(w);
-  T* dt = static_cast<T*>(dx);
-  float* pt = static_cast<float*>(part);
-  if (vec) return bwd_v<T, W, V>(rows, width, gt, ld_dy, xt, ld_x, mean, rstd, wt, dt, ld_dx, dw, db, pt, s);
-  return bwd_v<T, W, 1>(rows, width, gt, ld_dy, xt, ld_x, mean, rstd, wt, dt, ld_dx, dw, db, pt, s);
+  const uintptr_t bytes = address(x) | address(dy) | address(dx) | (ld_x | ld_dy | ld_dx | width) * sizeof(T);
+  return with_access<T>(bytes, [&](auto v) {
+    return bwd_v<T, W, decltype(v)::value>(rows, width, static_cast<const T*>(dy), ld_dy, static_cast<const T*>(x), ld_x,
+                                           mean, rstd, static_cast<const W*>(w), static_cast<T*>(dx), ld_dx, dw, db,
+                                           static_cast<float*>(part), s);
+  });
 }
 
 // f(T(), W()) for an activation and a weight type.
@@ -441,7 +629,7 @@ soap_status_t layer_norm_forward(int64_t rows, int64_t width, const void* x, int
 
 size_t layer_norm_workspace_bytes(int64_t rows, int64_t width) {
   if (rows <= 0 || width <= 0 || rows > INT32_MAX || width > INT32_MAX) return 0;
-  return (size_t)norm_parts(rows, 1) * 2 * (size_t)width * sizeof(float);
+  return (size_t)std::min<int64_t>(kParts, rows) * 2 * (size_t)width * sizeof(float);
 }
 
 soap_status_t layer_norm_backward(int64_t rows, int64_t width, const void* dy, int64_t ld_dy, const void* x,

@@ -4,11 +4,17 @@
 //   loss = coef E / (k n) sum_e counts_e P_e / n
 //   dz_e = p_e (u_e - sum_j p_j u_j),  u = coef dloss E / (k n^2) counts + (d gates -> p)
 //
-// A group of G lanes (8, 16 or 32) takes a token; lane l holds the logits l, l + G, ... in NE
-// registers. The choice runs on 32-bit keys in the logits' order: each lane keeps its keys
-// sorted, and k times the group's largest head is found and popped by its owner. Column sums of
-// p stay in registers over all of a warp's tokens, counts in shared memory, and both leave the
-// CTA as one partial row that a second kernel adds in a fixed order.
+// A group of G lanes (8, 16 or 32) takes a token; a lane holds NE of its logits in registers, V
+// consecutive ones per access, and has asked for its next token's while it works on one. The choice
+// runs on 32-bit keys in the logits' order: each lane keeps its keys sorted (or, many, scans them),
+// and k times the group's largest head is found and popped by its owner. A 16-bit logit's key holds
+// its index below its value, so that keys differ and one comparison settles ties; fp32 keys carry
+// their index beside them. What bounds it is the k exchanges (a shuffle costs an SM quarter 4
+// cycles, a 32-lane reduction 8), so groups are small: a warp takes four tokens of 64 bf16 logits.
+//
+// Column sums of p stay in registers over all of a warp's tokens, counts in shared memory. A cluster
+// adds its CTAs' sums through distributed shared memory in a fixed order; one cluster finishes by
+// itself (few tokens: one launch), several leave a partial row each that a second kernel adds.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -21,8 +27,11 @@ namespace soap {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
 constexpr int kMaxExperts = 1024;
-constexpr int kMaxCtas = 152 * 4;  // most partial rows
+constexpr int kCluster = 8;
+constexpr int kMaxCtas = 152 * 4;          // a multiple of kCluster
+constexpr int kMaxK = 32;
 
 // Keys in the order of the logits: finite values map to 1 .. 2^32 - 1, -inf and "no logit" to 0.
 __device__ __forceinline__ uint32_t order_key(float z) {
@@ -34,6 +43,35 @@ __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
+// A lane's candidate. 16-bit logits differ in the upper 16 bits of their fp32 key (bf16) or, as fp16, in
+// its upper 19 (their 13 low mantissa bits are zero): the complemented index (< 1024) goes below.
+template <bool PACKED>
+struct Best {
+  uint32_t key;
+  int idx;  // not PACKED
+  __device__ __forceinline__ bool before(const Best& o) const {
+    return PACKED ? key > o.key : key > o.key || (key == o.key && idx < o.idx);
+  }
+};
+template <bool PACKED>
+__device__ __forceinline__ Best<PACKED> candidate(float z, int idx) {
+  const uint32_t k = order_key(z);
+  // a finite key stays above the "none" of 0 whatever its index: -fp16/bf16 max has a nonzero upper part
+  if (PACKED) return {k ? (k & ~0x1fffu) | (uint32_t)(0x1fff - idx) : 0u, 0};
+  return {k, idx};
+}
+template <bool PACKED>
+__device__ __forceinline__ int index_of(const Best<PACKED>& b) {
+  return PACKED ? 0x1fff - (int)(b.key & 0x1fffu) : b.idx;
+}
+// The logit a key stands for. A negative value's key is the complement of its bits, whose dropped low
+// bits are ones.
+template <bool PACKED>
+__device__ __forceinline__ float value_of(const Best<PACKED>& b) {
+  if (!PACKED) return key_value(b.key);
+  return key_value(b.key & 0x80000000u ? b.key & ~0x1fffu : b.key | 0x1fffu);
+}
+
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -41,24 +79,60 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 template <int G>
-__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int G, bool PACKED>
+__device__ __forceinline__ Best<PACKED> group_best(Best<PACKED> b) {
   if constexpr (G == 32) {
-    return __reduce_max_sync(0xffffffffu, v);
+    const uint32_t top = __reduce_max_sync(0xffffffffu, b.key);
+    if (PACKED) return {top, 0};
+    // the lowest index among the lanes that hold it: one lane, as a rule
+    const uint32_t who = __ballot_sync(0xffffffffu, b.key == top);
+    if (__popc(who) == 1) return {top, __shfl_sync(0xffffffffu, b.idx, __ffs(who) - 1)};
+    return {top, (int)__reduce_min_sync(0xffffffffu, b.key == top ? (uint32_t)b.idx : 0x7fffffffu)};
   } else {
 #pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    for (int o = G / 2; o > 0; o >>= 1) {
+      Best<PACKED> x{__shfl_xor_sync(0xffffffffu, b.key, o), 0};
+      if (!PACKED) x.idx = __shfl_xor_sync(0xffffffffu, b.idx, o);
+      if (x.before(b)) b = x;
+    }
+    return b;
   }
 }
-template <int G>
-__device__ __forceinline__ uint32_t group_min(uint32_t v) {
-  return ~group_max<G>(~v);
-}
 
-// One token's softmax: z in registers -> e = exp(z - max) with zero for -inf and absent logits.
-// Returns false for a row that is not counted (no finite logit); bad: it holds a NaN or +inf.
+// A group's part of a row: element i of a lane is logit at(lane, i). The number of experts is a
+// multiple of V; whether V logits move as one access depends on the rows' alignment, which lane
+// holds which does not, so that the same logits give the same bits wherever they lie.
+template <typename T, int G, int NE, int V>
+struct Row {
+  Pack<T, V> p[NE / V];
+  static __device__ __forceinline__ int at(int lane, int i) { return ((i / V) * G + lane) * V + i % V; }
+  __device__ __forceinline__ void load(const T* row, int experts, int lane, bool vec) {
+#pragma unroll
+    for (int i = 0; i < NE; i += V)
+      if (at(lane, i) < experts) {
+        if (V == 1 || vec) {
+          p[i / V] = *reinterpret_cast<const Pack<T, V>*>(row + at(lane, i));
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q) p[i / V].v[q] = row[at(lane, i + q)];
+        }
+      }
+  }
+  __device__ __forceinline__ void values(bool live, int experts, int lane, float (&z)[NE]) const {
+#pragma unroll
+    for (int i = 0; i < NE; ++i) z[i] = live && at(lane, i) < experts ? to_f32(p[i / V].v[i % V]) : -INFINITY;
+  }
+};
+
+// One token's softmax: z -> e = exp(z - top), zero for -inf and absent logits, and their sum. bad: the
+// row holds a NaN or +inf. Returns false for a row without a finite logit (and not bad).
 template <int G, int NE>
-__device__ __forceinline__ bool softmax_row(const float (&z)[NE], float (&e)[NE], float& top, float& sum, bool& bad) {
+__device__ __forceinline__ bool softmax_row(const float (&z)[NE], float (&e)[NE], float& top, float& inv, bool& bad) {
   float m = -INFINITY;
   int odd = 0;
 #pragma unroll
@@ -66,57 +140,93 @@ __device__ __forceinline__ bool softmax_row(const float (&z)[NE], float (&e)[NE]
     m = fmaxf(m, z[i]);
     odd |= !(z[i] < INFINITY);
   }
-  const uint32_t top_key = group_max<G>(order_key(m));
-  bad = group_max<G>((uint32_t)odd) != 0;
-  top = key_value(top_key);
-  sum = 0.f;
-  if (top_key == 0) return false;
+  top = group_max<G>(odd ? INFINITY : m);
+  bad = top == INFINITY;
+  const bool counted = top > -INFINITY && !bad;
+  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
-    e[i] = __expf(z[i] - top);
+    e[i] = counted ? __expf(z[i] - top) : 0.f;
     sum += e[i];
   }
-  return true;
+  inv = 1.f / group_sum<G>(sum);
+  return counted;
 }
 
-template <typename T, int G, int NE>
-__device__ __forceinline__ void load_row(const T* row, int experts, int lane, float (&z)[NE]) {
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// The word at p's place in the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t peer_word(const void* p, uint32_t rank) {
+  const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(p));
+  uint32_t r, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
+  return v;
+}
+
+struct Totals {
+  int32_t* counts;
+  int32_t* live;
+  float *mean_probs, *loss;
+  float coef;
+};
+
+// The loss from sum_e counts_e mean_e, summed over a CTA in a fixed order.
+__device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    const int c = lane + i * G;
-    z[i] = c < experts ? to_f32(row[c]) : -INFINITY;
-  }
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) v += red[w];
+  return v;
 }
 
-template <typename T, int G, int NE>
+template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
     route_fwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
-                     int normalize, int32_t* indices, float* gates, float* part_p, int* part_c, int* status) {
-  extern __shared__ int counts[];             // [experts + 1]: the choices, and the tokens counted
-  __shared__ float sums[kThreads / 32][33];
-  const int lane = threadIdx.x % G;
+                     int normalize, int32_t* indices, float* gates, float* part_p, int* part_c, Totals out,
+                     bool vec, int* status) {
+  constexpr bool kPacked = sizeof(T) == 2;
+  constexpr bool kSorted = NE <= 8;
+  constexpr int kRec = kMaxK / G;
+  using R = Row<T, G, NE, V>;
+  extern __shared__ float shared[];       // [warps][experts] column sums (the first row: the CTA's) ...
+  int* counts = reinterpret_cast<int*>(shared + kWarps * experts);  // ... [experts + 1]: choices, tokens counted
+  __shared__ double red[kWarps + 1];
+  const int lane = threadIdx.x % G, warp = threadIdx.x / 32;
   for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
   __syncthreads();
   float acc[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) acc[i] = 0.f;
+  int seen = 0;
   const int64_t groups = (int64_t)gridDim.x * (kThreads / G);
-  const int64_t passes = (tokens + groups - 1) / groups;
-  for (int64_t pass = 0; pass < passes; ++pass) {
-    const int64_t t = pass * groups + (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    const bool live = t < tokens && (!mask || mask[t] != 0);
+  int64_t t = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  R row;
+  bool live = t < tokens && (!mask || mask[t] != 0);
+  if (live) row.load(logits + t * ld, experts, lane, vec);
+  // a warp's tokens are consecutive: all its groups stay while its first one has a token
+  for (int64_t first = t - (threadIdx.x % 32) / G; first < tokens; first += groups, t += groups) {
     float z[NE], e[NE];
-    if (live) {
-      load_row<T, G, NE>(logits + t * ld, experts, lane, z);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NE; ++i) z[i] = -INFINITY;
-    }
-    float top, sum;
+    row.values(live, experts, lane, z);
+    live = t + groups < tokens && (!mask || mask[t + groups] != 0);
+    if (live) row.load(logits + (t + groups) * ld, experts, lane, vec);  // the next token's
+    float top, inv;
     bool bad;
-    const bool counted = softmax_row<G, NE>(z, e, top, sum, bad);
-    sum = group_sum<G>(counted ? sum : 0.f);
-    const float inv = 1.f / sum;
+    const bool counted = softmax_row<G, NE>(z, e, top, inv, bad);
     if (bad) {
 #pragma unroll
       for (int i = 0; i < NE; ++i) acc[i] = NAN;
@@ -125,106 +235,154 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
       for (int i = 0; i < NE; ++i) acc[i] = fmaf(e[i], inv, acc[i]);
     }
-    if (lane == 0 && (counted || bad)) atomicAdd(&counts[experts], 1);
-    // the choice: few keys per lane are kept sorted (falling, equal ones by rising index, i.e. in
-    // place), so that a pop is a shift; more are scanned again after each pop
-    constexpr bool kSorted = NE <= 8;
-    uint32_t key[NE];
-    int idx[NE];
+    seen += counted || bad;
+    Best<kPacked> b[NE];
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      key[i] = bad ? 0u : order_key(z[i]);
-      idx[i] = lane + i * G;
-    }
+    for (int i = 0; i < NE; ++i) b[i] = candidate<kPacked>(bad ? -INFINITY : z[i], R::at(lane, i));
     if (kSorted) {
 #pragma unroll
       for (int i = 1; i < NE; ++i)
 #pragma unroll
         for (int j = i; j > 0; --j) {
-          const bool up = key[j] > key[j - 1];
-          const uint32_t hi = up ? key[j] : key[j - 1], lo = up ? key[j - 1] : key[j];
-          const int ih = up ? idx[j] : idx[j - 1], il = up ? idx[j - 1] : idx[j];
-          key[j - 1] = hi;
-          key[j] = lo;
-          idx[j - 1] = ih;
-          idx[j] = il;
+          const bool up = b[j].before(b[j - 1]);
+          const Best<kPacked> hi = up ? b[j] : b[j - 1], lo = up ? b[j - 1] : b[j];
+          b[j - 1] = hi;
+          b[j] = lo;
         }
     }
-    int my_idx = -1;
-    float my_gate = 0.f;
-    for (int r = 0; r < k; ++r) {
-      uint32_t head = key[0];
-      int head_idx = idx[0];
-      if (!kSorted) {
+    int my_idx[kRec];
+    float my_gate[kRec], total = 0.f;
 #pragma unroll
-        for (int i = 1; i < NE; ++i)
-          if (key[i] > head) {
-            head = key[i];
-            head_idx = idx[i];
+    for (int j = 0; j < kRec; ++j) {
+      my_idx[j] = -1;
+      my_gate[j] = 0.f;
+      for (int r = 0; r < G && j * G + r < k; ++r) {
+        Best<kPacked> head = b[0];
+        if (!kSorted) {
+#pragma unroll
+          for (int i = 1; i < NE; ++i)
+            if (b[i].before(head)) head = b[i];
+        }
+        const Best<kPacked> best = group_best<G>(head);
+        if (best.key != 0) {
+          if (lane == r) {
+            my_idx[j] = index_of(best);
+            my_gate[j] = __expf(value_of(best) - top) * inv;
           }
-      }
-      const uint32_t best = group_max<G>(head);
-      const uint32_t at = group_min<G>(head == best ? (uint32_t)head_idx : 0xffffffffu);
-      const bool some = best != 0;
-      if (some && lane == r) {
-        my_idx = (int)at;
-        my_gate = __expf(key_value(best) - top) * inv;
-      }
-      if (some && head == best && (uint32_t)head_idx == at) {
-        atomicAdd(&counts[at], 1);
-        if (kSorted) {
+          if (kPacked ? head.key == best.key : head.key == best.key && head.idx == best.idx) {
+            atomicAdd(&counts[index_of(best)], 1);
+            if (kSorted) {
 #pragma unroll
-          for (int i = 1; i < NE; ++i) {
-            key[i - 1] = key[i];
-            idx[i - 1] = idx[i];
+              for (int i = 1; i < NE; ++i) b[i - 1] = b[i];
+              b[NE - 1].key = 0u;
+            } else {
+#pragma unroll
+              for (int i = 0; i < NE; ++i)
+                if (kPacked ? b[i].key == best.key : b[i].idx == best.idx) b[i].key = 0u;
+            }
           }
-          key[NE - 1] = 0u;
-        } else {
-#pragma unroll
-          for (int i = 0; i < NE; ++i)
-            if ((uint32_t)idx[i] == at) key[i] = 0u;
         }
       }
+      total += my_gate[j];
     }
     if (normalize) {
-      const float total = group_sum<G>(my_gate);
-      if (total > 0.f) my_gate /= total;
+      total = group_sum<G>(total);
+      if (total > 0.f)
+#pragma unroll
+        for (int j = 0; j < kRec; ++j) my_gate[j] /= total;
     }
-    if (bad) my_gate = NAN;
-    if (t < tokens && lane < k) {
-      indices[t * k + lane] = my_idx;
-      gates[t * k + lane] = my_gate;
-    }
+    if (t < tokens)
+#pragma unroll
+      for (int j = 0; j < kRec; ++j)
+        if (j * G + lane < k) {
+          indices[t * k + j * G + lane] = my_idx[j];
+          gates[t * k + j * G + lane] = bad ? NAN : my_gate[j];
+        }
   }
-  // column sums: the groups of a warp by shuffles, the warps through shared memory in order
-  const int warp = threadIdx.x / 32, wl = threadIdx.x % 32;
+  // column sums: the groups of a warp by shuffles, the warps in order
+  if (lane == 0 && seen) atomicAdd(&counts[experts], seen);
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
     float v = acc[i];
 #pragma unroll
     for (int o = G; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    sums[warp][wl] = v;
-    __syncthreads();
-    const int c = threadIdx.x + i * G;
-    if (threadIdx.x < G && c < experts) {
-      float s = 0.f;
-      for (int w = 0; w < kThreads / 32; ++w) s += sums[w][threadIdx.x];
-      part_p[(int64_t)blockIdx.x * experts + c] = s;
-    }
+    const int c = R::at(lane, i);
+    if (threadIdx.x % 32 < G && c < experts) shared[warp * experts + c] = v;
   }
   __syncthreads();
-  for (int c = threadIdx.x; c <= experts; c += kThreads) part_c[(int64_t)blockIdx.x * (experts + 1) + c] = counts[c];
+  for (int c = threadIdx.x; c < experts; c += kThreads) {
+    float v = shared[c];
+    for (int w = 1; w < kWarps; ++w) v += shared[w * experts + c];
+    shared[c] = v;
+  }
+  // the cluster's CTAs in order, each CTA some of the columns
+  cluster_sync();
+  const uint32_t rank = cluster_rank(), size = cluster_size();
+  const bool alone = gridDim.x == size;  // one cluster: the totals are complete
+  const int64_t part = blockIdx.x / size;
+  int n = 0;
+  for (uint32_t q = 0; q < size; ++q) n += (int)peer_word(&counts[experts], q);
+  double dot = 0.0;
+  for (int c = rank * kThreads + threadIdx.x; c < experts; c += size * kThreads) {
+    float v = 0.f;
+    int cnt = 0;
+    for (uint32_t q = 0; q < size; ++q) {
+      v += __uint_as_float(peer_word(&shared[c], q));
+      cnt += (int)peer_word(&counts[c], q);
+    }
+    if (alone) {
+      const double mean = n > 0 ? (double)v / n : 0.0;
+      out.counts[c] = cnt;
+      if (out.mean_probs) out.mean_probs[c] = (float)mean;
+      dot += (double)cnt * mean;
+    } else {
+      part_p[part * experts + c] = v;
+      part_c[part * (experts + 1) + c] = cnt;
+    }
+  }
+  if (!alone) {
+    if (rank == 0 && threadIdx.x == 0) part_c[part * (experts + 1) + experts] = n;
+  } else {
+    dot = block_sum(dot, red);
+    if (threadIdx.x == 0) red[kWarps] = dot;
+    __syncthreads();
+  }
+  cluster_sync();
+  if (alone && rank == 0 && threadIdx.x == 0) {
+    dot = 0.0;
+    for (uint32_t q = 0; q < size; ++q)
+      dot += __hiloint2double((int)peer_word(reinterpret_cast<const uint32_t*>(&red[kWarps]) + 1, q),
+                              (int)peer_word(&red[kWarps], q));
+    *out.live = n;
+    *out.loss = n > 0 ? (float)((double)out.coef * experts / ((double)k * n) * dot) : 0.f;
+  }
+  if (alone) cluster_sync();  // the first CTA has read the others
 }
 
-// Adds the CTAs' partial rows in a fixed order, a warp to a column; the loss. One CTA of 1024 threads.
+// Adds the clusters' partial rows in a fixed order; the loss. One CTA of 1024 threads: a warp takes 32
+// columns of every few-th row.
 __global__ void __launch_bounds__(1024)
-    route_sum_kernel(const float* part_p, const int* part_c, int parts, int experts, int k, float coef,
-                     int32_t* counts, int32_t* live, float* mean_probs, float* loss) {
+    route_sum_kernel(const float* part_p, const int* part_c, int parts, int experts, int k, Totals out) {
+  __shared__ float sum_p[32][32];
+  __shared__ int sum_c[32][32];
   __shared__ double red[32];
   __shared__ int total;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  if (warp == 0) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch overlaps the end of the kernel before
+  const int blocks = (experts + 31) / 32, ways = 32 / blocks;  // at most 32 blocks of columns
+  const int block = warp % blocks, way = warp / blocks, c = block * 32 + lane;
+  float v = 0.f;
+  int cnt = 0;
+  if (way < ways && c < experts) {
+#pragma unroll 4
+    for (int p = way; p < parts; p += ways) {
+      v += part_p[(int64_t)p * experts + c];
+      cnt += part_c[(int64_t)p * (experts + 1) + c];
+    }
+  }
+  sum_p[warp][lane] = v;
+  sum_c[warp][lane] = cnt;
+  if (warp == 31) {
     int n = 0;
     for (int p = lane; p < parts; p += 32) n += part_c[(int64_t)p * (experts + 1) + experts];
     n = __reduce_add_sync(0xffffffffu, n);
@@ -233,84 +391,90 @@ __global__ void __launch_bounds__(1024)
   __syncthreads();
   const int n = total;
   double dot = 0.0;
-  for (int c = warp; c < experts; c += 32) {
-    int cnt = 0;
+  if (way == 0 && c < experts) {
     double s = 0.0;
-    for (int p = lane; p < parts; p += 32) {
-      cnt += part_c[(int64_t)p * (experts + 1) + c];
-      s += (double)part_p[(int64_t)p * experts + c];
+    cnt = 0;
+    for (int w = 0; w < ways; ++w) {
+      s += (double)sum_p[w * blocks + block][lane];
+      cnt += sum_c[w * blocks + block][lane];
     }
-    cnt = __reduce_add_sync(0xffffffffu, cnt);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     const double mean = n > 0 ? s / n : 0.0;
-    dot += (double)cnt * mean;
-    if (lane == 0) {
-      counts[c] = cnt;
-      if (mean_probs) mean_probs[c] = (float)mean;
-    }
+    out.counts[c] = cnt;
+    if (out.mean_probs) out.mean_probs[c] = (float)mean;
+    dot = (double)cnt * mean;
   }
-  if (lane == 0) red[warp] = dot;
-  __syncthreads();
+  dot = block_sum(dot, red);
   if (threadIdx.x == 0) {
-    double t = 0.0;
-    for (int w = 0; w < 32; ++w) t += red[w];
-    *live = n;
-    *loss = n > 0 ? (float)((double)coef * experts / ((double)k * n) * t) : 0.f;
+    *out.live = n;
+    *out.loss = n > 0 ? (float)((double)out.coef * experts / ((double)k * n) * dot) : 0.f;
   }
 }
 
-template <typename T, int G, int NE>
+template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
     route_bwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
                      int normalize, double scale, const int32_t* indices, const int32_t* counts, const int32_t* live_n,
-                     const float* dgates, T* dlogits, int64_t ld_d) {
+                     const float* dgates, T* dlogits, int64_t ld_d, bool vec) {
+  constexpr int kRec = kMaxK / G;
+  using R = Row<T, G, NE, V>;
   const int lane = threadIdx.x % G;
+  const int64_t groups = (int64_t)gridDim.x * (kThreads / G);
+  int64_t t = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  R row;
+  bool live = t < tokens && (!mask || mask[t] != 0);
+  if (live) row.load(logits + t * ld, experts, lane, vec);
   const int n = *live_n;
-  const double per = n > 0 ? scale / ((double)n * n) : 0.0;
+  const float per = n > 0 ? (float)(scale / ((double)n * n)) : 0.f;
   float up[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
-    const int c = lane + i * G;
-    up[i] = c < experts ? (float)(per * counts[c]) : 0.f;
+    const int c = R::at(lane, i);
+    up[i] = c < experts ? per * (float)counts[c] : 0.f;
   }
-  const int64_t groups = (int64_t)gridDim.x * (kThreads / G);
-  const int64_t passes = (tokens + groups - 1) / groups;
-  for (int64_t pass = 0; pass < passes; ++pass) {
-    const int64_t t = pass * groups + (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    const bool live = t < tokens && (!mask || mask[t] != 0);
+  for (int64_t first = t - (threadIdx.x % 32) / G; first < tokens; first += groups, t += groups) {
+    const bool here = live;
     float z[NE], e[NE];
-    const T* row = logits + t * ld;
-    if (live) {
-      load_row<T, G, NE>(row, experts, lane, z);
-    } else {
+    row.values(here, experts, lane, z);
+    // the gates' gradient at the chosen logits: lane r holds choices r, r + G, ...
+    int at[kRec];
+    float d[kRec], zc[kRec];
 #pragma unroll
-      for (int i = 0; i < NE; ++i) z[i] = -INFINITY;
-    }
-    float top, sum;
-    bool bad;
-    const bool counted = softmax_row<G, NE>(z, e, top, sum, bad);
-    sum = group_sum<G>(counted ? sum : 0.f);
-    const float inv = 1.f / sum;
-    // the gates' gradient at the chosen logits: lane r holds choice r
-    float d = 0.f;
-    int at = -1;
-    float pc = 0.f;
-    if (dgates && live && lane < k) {
-      at = indices[t * k + lane];
-      if (at >= 0 && at < experts) {
-        d = dgates[t * k + lane];
-        pc = __expf(to_f32(row[at]) - top) * inv;
-      } else {
-        at = -1;
+    for (int j = 0; j < kRec; ++j) {
+      at[j] = -1;
+      d[j] = 0.f;
+      zc[j] = -INFINITY;
+      const int r = j * G + lane;
+      if (dgates && here && r < k) {
+        const int a = indices[t * k + r];
+        if (a >= 0 && a < experts) {
+          at[j] = a;
+          d[j] = dgates[t * k + r];
+          zc[j] = to_f32(logits[t * ld + a]);
+        }
       }
     }
-    if (dgates && normalize) {  // gate_r = p_r / S: d p_r = (d gate_r - sum_j d gate_j gate_j) / S
-      const float S = group_sum<G>(pc);
-      const float dg = group_sum<G>(d * pc);
-      if (at >= 0) d = (d - dg / S) / S;
+    live = t + groups < tokens && (!mask || mask[t + groups] != 0);
+    if (live) row.load(logits + (t + groups) * ld, experts, lane, vec);  // the next token's
+    float top, inv;
+    bool bad;
+    const bool counted = softmax_row<G, NE>(z, e, top, inv, bad);
+    float pc[kRec], s = 0.f, dg = 0.f;
+#pragma unroll
+    for (int j = 0; j < kRec; ++j) {
+      pc[j] = at[j] >= 0 ? __expf(zc[j] - top) * inv : 0.f;
+      s += pc[j];
+      dg = fmaf(d[j], pc[j], dg);
     }
-    float dot = pc * d;
+    if (dgates && normalize) {  // gate_r = p_r / S: d p_r = (d gate_r - sum_j d gate_j gate_j) / S
+      s = group_sum<G>(s);
+      dg = group_sum<G>(dg) / s;
+#pragma unroll
+      for (int j = 0; j < kRec; ++j)
+        if (at[j] >= 0) d[j] = (d[j] - dg) / s;
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < kRec; ++j) dot = fmaf(pc[j], d[j], dot);
     if (counted) {
 #pragma unroll
       for (int i = 0; i < NE; ++i) {
@@ -322,33 +486,53 @@ __global__ void __launch_bounds__(kThreads)
     if (t < tokens) {
       T* out = dlogits + t * ld_d;
 #pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        const int c = lane + i * G;
-        if (c < experts) out[c] = from_f32<T>(bad ? NAN : counted ? e[i] * (up[i] - dot) : 0.f);
+      for (int i = 0; i < NE; i += V) {
+        if (R::at(lane, i) >= experts) continue;
+        Pack<T, V> o;
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+          o.v[q] = from_f32<T>(bad ? NAN : counted ? e[i + q] * (up[i + q] - dot) : 0.f);
+        if (V == 1 || vec) {
+          *reinterpret_cast<Pack<T, V>*>(out + R::at(lane, i)) = o;
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q) out[R::at(lane, i + q)] = o.v[q];
+        }
       }
     }
     if (dgates) {  // the chosen ones again, with the gates' part (ordered after the row's stores)
       __syncwarp();
-      if (at >= 0)
-        dlogits[t * ld_d + at] = from_f32<T>(pc * ((float)(per * counts[at]) + d - dot));
+#pragma unroll
+      for (int j = 0; j < kRec; ++j)
+        if (at[j] >= 0)
+          dlogits[t * ld_d + at[j]] = from_f32<T>(pc[j] * (per * (float)counts[at[j]] + d[j] - dot));
     }
   }
 }
 
 // ---- launches ------------------------------------------------------------------------------
 
-// f(group size, registers per lane) for a number of experts: a group just wide enough up to 32.
-template <typename F>
+// f(group size, registers per lane): a lane holds up to 8 logits before the group grows (fp32, whose
+// exchanges move an index too: up to 4), and up to 32 in the end.
+template <typename T, typename F>
 cudaError_t with_shape(int experts, F&& f) {
   using std::integral_constant;
-  if (experts <= 8) return f(integral_constant<int, 8>(), integral_constant<int, 1>());
-  if (experts <= 16) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
-  if (experts <= 32) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
-  if (experts <= 64) return f(integral_constant<int, 32>(), integral_constant<int, 2>());
-  if (experts <= 128) return f(integral_constant<int, 32>(), integral_constant<int, 4>());
-  if (experts <= 256) return f(integral_constant<int, 32>(), integral_constant<int, 8>());
-  if (experts <= 512) return f(integral_constant<int, 32>(), integral_constant<int, 16>());
-  return f(integral_constant<int, 32>(), integral_constant<int, 32>());
+  using I8 = integral_constant<int, 8>;
+  using I16 = integral_constant<int, 16>;
+  using I32 = integral_constant<int, 32>;
+  if (experts <= 8) return f(I8(), integral_constant<int, 1>());
+  if (experts <= 16) return f(I8(), integral_constant<int, 2>());
+  if (experts <= 32) return f(I8(), integral_constant<int, 4>());
+  if constexpr (sizeof(T) == 2) {
+    if (experts <= 64) return f(I8(), I8());
+    if (experts <= 128) return f(I16(), I8());
+  } else {
+    if (experts <= 64) return f(I16(), integral_constant<int, 4>());
+    if (experts <= 128) return f(I32(), integral_constant<int, 4>());
+  }
+  if (experts <= 256) return f(I32(), I8());
+  if (experts <= 512) return f(I32(), I16());
+  return f(I32(), I32());
 }
 
 template <typename F>
@@ -357,11 +541,33 @@ cudaError_t with_type(int32_t type, F&& f) {
   return type == SOAP_BF16 ? f(__nv_bfloat16()) : f(__half());
 }
 
-int group_of(int experts) { return experts <= 8 ? 8 : experts <= 16 ? 16 : 32; }
+// Tokens per CTA and pass, at least (fp32's groups).
+int tokens_per_cta(int experts) { return kThreads / (experts <= 32 ? 8 : experts <= 64 ? 16 : 32); }
 
-int ctas_for(int64_t tokens, int experts) {
-  const int per = kThreads / group_of(experts);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCtas, (tokens + per - 1) / per));
+// CTAs: for few tokens one cluster that finishes alone, of up to 8 CTAs, else whole clusters, up to four
+// CTAs per SM.
+int ctas_for(int64_t tokens, int experts, int* cluster) {
+  const int64_t want = std::max<int64_t>(1, (tokens + tokens_per_cta(experts) - 1) / tokens_per_cta(experts));
+  int c = 1;
+  while (c < kCluster && c < want) c *= 2;
+  *cluster = c;
+  if (want <= 4 * kCluster) return c;
+  return (int)std::min<int64_t>(kMaxCtas, (want + kCluster - 1) / kCluster * kCluster);
+}
+
+// f(T(), group size, registers per lane, logits per access, whether the rows allow such accesses).
+template <int TENSORS, typename F>
+cudaError_t with_row(int32_t type, int experts, const void* a, int64_t ld_a, const void* b, int64_t ld_b, F&& f) {
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    return with_shape<T>(experts, [&](auto g, auto ne) {
+      constexpr int NE = decltype(ne)::value, V = std::min<int>(NE, 16 / sizeof(T));
+      if (V == 1 || experts % V) return f(t, g, ne, std::integral_constant<int, 1>(), true);
+      uintptr_t bytes = reinterpret_cast<uintptr_t>(a) | ld_a * sizeof(T);
+      if (TENSORS == 2) bytes |= reinterpret_cast<uintptr_t>(b) | ld_b * sizeof(T);
+      return f(t, g, ne, std::integral_constant<int, V>(), bytes % (V * sizeof(T)) == 0);
+    });
+  });
 }
 
 bool bad_ptr(const void* p, size_t size) { return !p || reinterpret_cast<uintptr_t>(p) % size; }
@@ -381,7 +587,9 @@ extern "C" {
 
 size_t layer_route_workspace_bytes(int64_t tokens, int32_t experts) {
   if (tokens < 0 || tokens > INT32_MAX || experts < 1 || experts > kMaxExperts) return 0;
-  return (size_t)ctas_for(tokens, experts) * (2 * (size_t)experts + 1) * 4;
+  int cluster;
+  const size_t parts = ctas_for(tokens, experts, &cluster) / cluster;
+  return parts * (2 * (size_t)experts + 1) * 4;
 }
 
 soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
@@ -396,23 +604,39 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
       workspace_bytes < layer_route_workspace_bytes(tokens, experts))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
-  const int parts = ctas_for(tokens, experts);
+  int cluster;
+  const int ctas = ctas_for(tokens, experts, &cluster), parts = ctas / cluster;
   float* part_p = static_cast<float*>(workspace);
   int* part_c = reinterpret_cast<int*>(part_p + (size_t)parts * experts);
+  const Totals out{counts, live, mean_probs, loss, coef};
   const double n = (double)tokens * experts;
   ProfScope prof(kFamElementwise, 6.0 * n, n * dtype_size(type) + 8.0 * tokens * k, s);
-  const cudaError_t e = with_type(type, [&](auto t) {
+  cudaLaunchAttribute attr;
+  cudaLaunchConfig_t cfg{};
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.dynamicSmemBytes = (size_t)((kWarps + 1) * experts + 1) * 4;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaError_t e = with_row<1>(type, experts, logits, ld, nullptr, 0, [&](auto t, auto g, auto ne, auto v, bool vec) {
     using T = decltype(t);
-    return with_shape(experts, [&](auto g, auto ne) {
-      route_fwd_kernel<T, decltype(g)::value, decltype(ne)::value><<<parts, kThreads, (experts + 1) * 4, s>>>(
-          static_cast<const T*>(logits), ld, mask, tokens, experts, k, normalize, indices, gates, part_p, part_c,
-          status);
-      const cudaError_t le = cudaGetLastError();
-      if (le != cudaSuccess) return le;
-      route_sum_kernel<<<1, 1024, 0, s>>>(part_p, part_c, parts, experts, k, coef, counts, live, mean_probs, loss);
-      return cudaGetLastError();
-    });
+    return cudaLaunchKernelEx(&cfg, route_fwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value>,
+                              static_cast<const T*>(logits), ld, mask, tokens, (int)experts, (int)k, (int)normalize,
+                              indices, gates, part_p, part_c, out, vec, (int*)status);
   });
+  if (e == cudaSuccess && parts > 1) {
+    cfg.gridDim = dim3(1);
+    cfg.blockDim = dim3(1024);
+    cfg.dynamicSmemBytes = 0;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    e = cudaLaunchKernelEx(&cfg, route_sum_kernel, (const float*)part_p, (const int*)part_c, parts, (int)experts,
+                           (int)k, out);
+  }
   return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;
 }
 
@@ -426,19 +650,19 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
       (dgates && (bad_ptr(dgates, 4) || bad_ptr(indices, 4))))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
-  const int ctas = ctas_for(tokens, experts);
+  const int64_t want = (tokens + tokens_per_cta(experts) - 1) / tokens_per_cta(experts);
+  const int ctas = (int)std::min<int64_t>(kMaxCtas, want);
   const double n = (double)tokens * experts;
   const double scale = (double)coef * dloss * experts / k;
   ProfScope prof(kFamElementwise, 6.0 * n, 2.0 * n * dtype_size(type) + 12.0 * tokens * k, s);
-  const cudaError_t e = with_type(type, [&](auto t) {
-    using T = decltype(t);
-    return with_shape(experts, [&](auto g, auto ne) {
-      route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value><<<ctas, kThreads, 0, s>>>(
-          static_cast<const T*>(logits), ld, mask, tokens, experts, k, normalize, scale, indices, counts, live, dgates,
-          static_cast<T*>(dlogits), ld_d);
-      return cudaGetLastError();
-    });
-  });
+  const cudaError_t e =
+      with_row<2>(type, experts, logits, ld, dlogits, ld_d, [&](auto t, auto g, auto ne, auto v, bool vec) {
+        using T = decltype(t);
+        route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value><<<ctas, kThreads, 0, s>>>(
+            static_cast<const T*>(logits), ld, mask, tokens, experts, k, normalize, scale, indices, counts, live,
+            dgates, static_cast<T*>(dlogits), ld_d, vec);
+        return cudaGetLastError();
+      });
   return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;
 }
 
