@@ -64,27 +64,30 @@ soap_status_t layer_norm_backward(int64_t rows, int64_t width, const void* dy, i
  * holds a NaN or +inf chooses nothing, has NaN gates and makes mean_probs and the loss NaN, and
  * SOAP_STATUS_NONFINITE is ORed into *status (if not NULL; it is not cleared).
  * indices: int32 [tokens][k]; gates: fp32 [tokens][k]; counts: int32 [experts]; live: int32 [1],
- * receives n; mean_probs: fp32 [experts]; loss: fp32 [1]. tokens = 0 gives zeros.
+ * receives n; mean_probs: fp32 [experts] or NULL; loss: fp32 [1]; stats: fp32 [tokens][2], 8-byte
+ * aligned, for the backward pass (a row's largest logit and 1 / sum of e^(z - largest)), or NULL.
+ * tokens = 0 gives zeros.
  * 1 <= experts <= 1024, 1 <= k <= min(experts, 32), 0 <= tokens < 2^31. `workspace`: 16-byte
  * aligned, layer_route_workspace_bytes(tokens, experts) bytes. */
 size_t layer_route_workspace_bytes(int64_t tokens, int32_t experts);
 soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
                                   int32_t type, const uint8_t* mask, int32_t normalize, float coef,
-                                  int32_t* indices, float* gates, int32_t* counts, int32_t* live,
-                                  float* mean_probs, float* loss, int32_t* status, void* workspace,
-                                  size_t workspace_bytes, soap_stream_t stream);
+                                  int32_t* indices, float* gates, float* stats, int32_t* counts,
+                                  int32_t* live, float* mean_probs, float* loss, int32_t* status,
+                                  void* workspace, size_t workspace_bytes, soap_stream_t stream);
 
 /* The logits' gradient from the gates' (fp32 [tokens][k], or NULL for zero) and the loss's (dloss), the
  * choice itself and the counts held constant:
  *   dp = coef dloss experts / (k n^2) * counts + (what reaches p through the gates),
  *   dz_e = p_e (dp_e - sum_j p_j dp_j)
  * dlogits: `type`, row i at element i * ld_d (may be logits when ld_d = ld). Rows that are masked or
- * not counted get zeros; a row with a NaN or +inf gets NaN. normalize, coef, mask, indices, counts,
- * live: those of the forward call. */
+ * not counted get zeros; a row with a NaN or +inf gets NaN. normalize, coef, mask, indices, stats,
+ * counts, live: those of the forward call (indices may be NULL without dgates). */
 soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
                                    int32_t type, const uint8_t* mask, int32_t normalize, float coef, float dloss,
-                                   const int32_t* indices, const int32_t* counts, const int32_t* live,
-                                   const float* dgates, void* dlogits, int64_t ld_d, soap_stream_t stream);
+                                   const int32_t* indices, const float* stats, const int32_t* counts,
+                                   const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d,
+                                   soap_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -8,9 +8,10 @@
 // consecutive ones per access, and has asked for its next token's while it works on one. The choice
 // runs on 32-bit keys in the logits' order: each lane keeps its keys sorted (or, many, scans them),
 // and k times the group's largest head is found and popped by its owner. A 16-bit logit's key holds
-// its index below its value, so that keys differ and one comparison settles ties; fp32 keys carry
-// their index beside them. What bounds it is the k exchanges (a shuffle costs an SM quarter 4
-// cycles, a 32-lane reduction 8), so groups are small: a warp takes four tokens of 64 bf16 logits.
+// its index below its value, so that keys differ; of equal fp32 keys the lowest index is looked for
+// only when two lanes hold the largest one. Instructions bound it (about 200 per token of 127 fp32
+// logits with k = 6, 80 of 64 bf16 ones with k = 8), so what each exchange does is kept to a minimum
+// and the gates are computed once per choice, by the lane that writes it.
 //
 // Column sums of p stay in registers over all of a warp's tokens, counts in shared memory. A cluster
 // adds its CTAs' sums through distributed shared memory in a fixed order; one cluster finishes by
@@ -33,43 +34,29 @@ constexpr int kCluster = 8;
 constexpr int kMaxCtas = 152 * 4;          // a multiple of kCluster
 constexpr int kMaxK = 32;
 
-// Keys in the order of the logits: finite values map to 1 .. 2^32 - 1, -inf and "no logit" to 0.
+// Keys in the order of the logits. A NaN's is above +inf's: adding 0 makes every NaN the positive one
+// (and -0 a +0). 0 stands for "none".
+constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyInf = 0xff800000u;
 __device__ __forceinline__ uint32_t order_key(float z) {
-  if (z == -INFINITY) return 0u;
-  const uint32_t u = __float_as_uint(z + 0.f);  // -0 counts as +0
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(z + 0.f);
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// A lane's candidate. 16-bit logits differ in the upper 16 bits of their fp32 key (bf16) or, as fp16, in
-// its upper 19 (their 13 low mantissa bits are zero): the complemented index (< 1024) goes below.
-template <bool PACKED>
-struct Best {
-  uint32_t key;
-  int idx;  // not PACKED
-  __device__ __forceinline__ bool before(const Best& o) const {
-    return PACKED ? key > o.key : key > o.key || (key == o.key && idx < o.idx);
-  }
-};
-template <bool PACKED>
-__device__ __forceinline__ Best<PACKED> candidate(float z, int idx) {
-  const uint32_t k = order_key(z);
-  // a finite key stays above the "none" of 0 whatever its index: -fp16/bf16 max has a nonzero upper part
-  if (PACKED) return {k ? (k & ~0x1fffu) | (uint32_t)(0x1fff - idx) : 0u, 0};
-  return {k, idx};
-}
-template <bool PACKED>
-__device__ __forceinline__ int index_of(const Best<PACKED>& b) {
-  return PACKED ? 0x1fff - (int)(b.key & 0x1fffu) : b.idx;
-}
-// The logit a key stands for. A negative value's key is the complement of its bits, whose dropped low
-// bits are ones.
-template <bool PACKED>
-__device__ __forceinline__ float value_of(const Best<PACKED>& b) {
-  if (!PACKED) return key_value(b.key);
-  return key_value(b.key & 0x80000000u ? b.key & ~0x1fffu : b.key | 0x1fffu);
+// 16-bit logits differ in the upper 19 bits of their fp32 key (their 13 low mantissa bits are zero, in a
+// negative one's key ones): the complemented index goes below.
+constexpr uint32_t kLow = 0x1fffu;
+__device__ __forceinline__ uint32_t pack_key(uint32_t key, int idx) { return (key & ~kLow) | (kLow - (uint32_t)idx); }
+__device__ __forceinline__ uint32_t unpack_key(uint32_t b) { return b & 0x80000000u ? b & ~kLow : b | kLow; }
+__device__ __forceinline__ int packed_index(uint32_t b) { return (int)(kLow - (b & kLow)); }
+
+// e^x for x <= 0: one multiplication and the hardware's 2^x (relative error 2^-22 and |x| 2^-24).
+__device__ __forceinline__ float exp_neg(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+  return r;
 }
 
 template <int G>
@@ -79,28 +66,31 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 template <int G>
-__device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-template <int G, bool PACKED>
-__device__ __forceinline__ Best<PACKED> group_best(Best<PACKED> b) {
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
   if constexpr (G == 32) {
-    const uint32_t top = __reduce_max_sync(0xffffffffu, b.key);
-    if (PACKED) return {top, 0};
-    // the lowest index among the lanes that hold it: one lane, as a rule
-    const uint32_t who = __ballot_sync(0xffffffffu, b.key == top);
-    if (__popc(who) == 1) return {top, __shfl_sync(0xffffffffu, b.idx, __ffs(who) - 1)};
-    return {top, (int)__reduce_min_sync(0xffffffffu, b.key == top ? (uint32_t)b.idx : 0x7fffffffu)};
+    return __reduce_max_sync(0xffffffffu, v);
   } else {
 #pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) {
-      Best<PACKED> x{__shfl_xor_sync(0xffffffffu, b.key, o), 0};
-      if (!PACKED) x.idx = __shfl_xor_sync(0xffffffffu, b.idx, o);
-      if (x.before(b)) b = x;
-    }
-    return b;
+    for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  }
+}
+
+// a before b in the sorted list: (key, index) pairs as they stand in one lane.
+template <bool PACKED>
+__device__ __forceinline__ void order(uint32_t& a, int& ia, uint32_t& b, int& ib) {
+  if (PACKED) {
+    const uint32_t hi = max(a, b);
+    b = min(a, b);
+    a = hi;
+  } else {
+    const bool up = b > a;  // equal keys stay as they are, by rising index
+    const uint32_t hi = up ? b : a;
+    b = up ? a : b;
+    a = hi;
+    const int i = up ? ib : ia;
+    ib = up ? ia : ib;
+    ia = i;
   }
 }
 
@@ -128,30 +118,6 @@ struct Row {
     for (int i = 0; i < NE; ++i) z[i] = live && at(lane, i) < experts ? to_f32(p[i / V].v[i % V]) : -INFINITY;
   }
 };
-
-// One token's softmax: z -> e = exp(z - top), zero for -inf and absent logits, and their sum. bad: the
-// row holds a NaN or +inf. Returns false for a row without a finite logit (and not bad).
-template <int G, int NE>
-__device__ __forceinline__ bool softmax_row(const float (&z)[NE], float (&e)[NE], float& top, float& inv, bool& bad) {
-  float m = -INFINITY;
-  int odd = 0;
-#pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    m = fmaxf(m, z[i]);
-    odd |= !(z[i] < INFINITY);
-  }
-  top = group_max<G>(odd ? INFINITY : m);
-  bad = top == INFINITY;
-  const bool counted = top > -INFINITY && !bad;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    e[i] = counted ? __expf(z[i] - top) : 0.f;
-    sum += e[i];
-  }
-  inv = 1.f / group_sum<G>(sum);
-  return counted;
-}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -197,7 +163,7 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
     route_fwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
-                     int normalize, int32_t* indices, float* gates, float* part_p, int* part_c, Totals out,
+                     int normalize, int32_t* indices, float* gates, float2* stats, float* part_p, int* part_c, Totals out,
                      bool vec, int* status) {
   constexpr bool kPacked = sizeof(T) == 2;
   constexpr bool kSorted = NE <= 8;
@@ -206,6 +172,7 @@ __global__ void __launch_bounds__(kThreads)
   extern __shared__ float shared[];       // [warps][experts] column sums (the first row: the CTA's) ...
   int* counts = reinterpret_cast<int*>(shared + kWarps * experts);  // ... [experts + 1]: choices, tokens counted
   __shared__ double red[kWarps + 1];
+  __shared__ int won[kPacked ? 1 : kThreads / G][kPacked ? 1 : kMaxK];  // a group's choices
   const int lane = threadIdx.x % G, warp = threadIdx.x / 32;
   for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
   __syncthreads();
@@ -224,66 +191,109 @@ __global__ void __launch_bounds__(kThreads)
     row.values(live, experts, lane, z);
     live = t + groups < tokens && (!mask || mask[t + groups] != 0);
     if (live) row.load(logits + (t + groups) * ld, experts, lane, vec);  // the next token's
-    float top, inv;
-    bool bad;
-    const bool counted = softmax_row<G, NE>(z, e, top, inv, bad);
+    uint32_t key[NE];
+    int idx[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      key[i] = order_key(z[i]);
+      idx[i] = R::at(lane, i);
+      if (kPacked) key[i] = pack_key(key[i], idx[i]);
+    }
+    auto head_of = [&](uint32_t& head, int& head_idx) {
+      head = key[0];
+      head_idx = idx[0];
+      if (!kSorted) {
+#pragma unroll
+        for (int i = 1; i < NE; ++i) {
+          if (!kPacked && key[i] > head) head_idx = idx[i];
+          head = max(head, key[i]);
+        }
+      }
+    };
+    if (kSorted) {
+      if (kPacked && NE == 8) {  // 19 exchanges
+        constexpr int net[19][2] = {{0, 2}, {1, 3}, {4, 6}, {5, 7}, {0, 4}, {1, 5}, {2, 6}, {3, 7}, {0, 1}, {2, 3},
+                                    {4, 5}, {6, 7}, {2, 4}, {3, 5}, {1, 4}, {3, 6}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+        for (int x = 0; x < 19; ++x)
+          order<kPacked>(key[net[x][0] % NE], idx[net[x][0] % NE], key[net[x][1] % NE], idx[net[x][1] % NE]);
+      } else {
+#pragma unroll
+        for (int i = 1; i < NE; ++i)
+#pragma unroll
+          for (int j = i; j > 0; --j) order<kPacked>(key[j - 1], idx[j - 1], key[j], idx[j]);
+      }
+    }
+    uint32_t head;
+    int head_idx;
+    head_of(head, head_idx);
+    uint32_t top = group_max<G>(head);  // the largest key left
+    const bool bad = (kPacked ? top & ~kLow : top) >= kKeyInf;
+    const bool counted = top > kKeyNegInf && !bad;
+    const float most = key_value(kPacked ? unpack_key(top) : top);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      e[i] = counted ? exp_neg(z[i] - most) : 0.f;
+      sum += e[i];
+    }
+    sum = group_sum<G>(sum);
+    const float inv = 1.f / sum;
+    if (counted)
+#pragma unroll
+      for (int i = 0; i < NE; ++i) acc[i] = fmaf(e[i], inv, acc[i]);
     if (bad) {
 #pragma unroll
       for (int i = 0; i < NE; ++i) acc[i] = NAN;
       if (status && lane == 0) atomicOr(status, SOAP_STATUS_NONFINITE);
-    } else if (counted) {
-#pragma unroll
-      for (int i = 0; i < NE; ++i) acc[i] = fmaf(e[i], inv, acc[i]);
     }
     seen += counted || bad;
-    Best<kPacked> b[NE];
+    if (stats && lane == 0 && t < tokens) stats[t] = bad ? make_float2(NAN, NAN) : make_float2(most, counted ? inv : 0.f);
+    // k times the largest key; what it is stays with lane r of the group
+    uint32_t my_key[kRec];
 #pragma unroll
-    for (int i = 0; i < NE; ++i) b[i] = candidate<kPacked>(bad ? -INFINITY : z[i], R::at(lane, i));
-    if (kSorted) {
-#pragma unroll
-      for (int i = 1; i < NE; ++i)
-#pragma unroll
-        for (int j = i; j > 0; --j) {
-          const bool up = b[j].before(b[j - 1]);
-          const Best<kPacked> hi = up ? b[j] : b[j - 1], lo = up ? b[j - 1] : b[j];
-          b[j - 1] = hi;
-          b[j] = lo;
+    for (int j = 0; j < kRec; ++j) {
+      my_key[j] = 0u;
+      for (int r = 0; r < G && j * G + r < k; ++r) {
+        if (j + r > 0) top = group_max<G>(head);
+        if (lane == r) my_key[j] = top;
+        bool mine = head == top;
+        if (!kPacked) {
+          // of equal keys in several lanes, the one of the lowest index
+          const uint32_t who = __ballot_sync(0xffffffffu, mine) >> ((threadIdx.x % 32) / G * G) & (0xffffffffu >> (32 - G));
+          if (__any_sync(0xffffffffu, (who & (who - 1)) != 0)) {
+            const uint32_t low = ~group_max<G>(mine ? ~(uint32_t)head_idx : 0u);
+            mine = mine && (uint32_t)head_idx == low;
+          }
+          if (mine) won[threadIdx.x / G][j * G + r] = head_idx;
         }
+        if (mine) {
+          if (kSorted) {
+#pragma unroll
+            for (int i = 1; i < NE; ++i) {
+              key[i - 1] = key[i];
+              if (!kPacked) idx[i - 1] = idx[i];
+            }
+            key[NE - 1] = 0u;
+          } else {
+#pragma unroll
+            for (int i = 0; i < NE; ++i)
+              if (kPacked ? key[i] == top : idx[i] == head_idx) key[i] = 0u;
+          }
+        }
+        head_of(head, head_idx);
+      }
     }
+    if (!kPacked) __syncwarp();
     int my_idx[kRec];
     float my_gate[kRec], total = 0.f;
 #pragma unroll
     for (int j = 0; j < kRec; ++j) {
-      my_idx[j] = -1;
-      my_gate[j] = 0.f;
-      for (int r = 0; r < G && j * G + r < k; ++r) {
-        Best<kPacked> head = b[0];
-        if (!kSorted) {
-#pragma unroll
-          for (int i = 1; i < NE; ++i)
-            if (b[i].before(head)) head = b[i];
-        }
-        const Best<kPacked> best = group_best<G>(head);
-        if (best.key != 0) {
-          if (lane == r) {
-            my_idx[j] = index_of(best);
-            my_gate[j] = __expf(value_of(best) - top) * inv;
-          }
-          if (kPacked ? head.key == best.key : head.key == best.key && head.idx == best.idx) {
-            atomicAdd(&counts[index_of(best)], 1);
-            if (kSorted) {
-#pragma unroll
-              for (int i = 1; i < NE; ++i) b[i - 1] = b[i];
-              b[NE - 1].key = 0u;
-            } else {
-#pragma unroll
-              for (int i = 0; i < NE; ++i)
-                if (kPacked ? b[i].key == best.key : b[i].idx == best.idx) b[i].key = 0u;
-            }
-          }
-        }
-      }
+      const bool some = counted && my_key[j] > (kPacked ? kKeyNegInf | kLow : kKeyNegInf);
+      my_idx[j] = !some ? -1 : kPacked ? packed_index(my_key[j]) : won[threadIdx.x / G][j * G + lane];
+      my_gate[j] = some ? exp_neg(key_value(kPacked ? unpack_key(my_key[j]) : my_key[j]) - most) * inv : 0.f;
       total += my_gate[j];
+      if (some) atomicAdd(&counts[my_idx[j]], 1);
     }
     if (normalize) {
       total = group_sum<G>(total);
@@ -298,6 +308,7 @@ __global__ void __launch_bounds__(kThreads)
           indices[t * k + j * G + lane] = my_idx[j];
           gates[t * k + j * G + lane] = bad ? NAN : my_gate[j];
         }
+    if (!kPacked) __syncwarp();  // the choices have been read
   }
   // column sums: the groups of a warp by shuffles, the warps in order
   if (lane == 0 && seen) atomicAdd(&counts[experts], seen);
@@ -414,7 +425,7 @@ template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
     route_bwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
                      int normalize, double scale, const int32_t* indices, const int32_t* counts, const int32_t* live_n,
-                     const float* dgates, T* dlogits, int64_t ld_d, bool vec) {
+                     const float2* stats, const float* dgates, T* dlogits, int64_t ld_d, bool vec) {
   constexpr int kRec = kMaxK / G;
   using R = Row<T, G, NE, V>;
   const int lane = threadIdx.x % G;
@@ -433,54 +444,45 @@ __global__ void __launch_bounds__(kThreads)
   }
   for (int64_t first = t - (threadIdx.x % 32) / G; first < tokens; first += groups, t += groups) {
     const bool here = live;
-    float z[NE], e[NE];
+    float z[NE];
     row.values(here, experts, lane, z);
+    const float2 st = here ? stats[t] : make_float2(0.f, 0.f);  // the largest logit, 1 / sum of e^(z - largest)
+    const bool bad = st.y != st.y;
     // the gates' gradient at the chosen logits: lane r holds choices r, r + G, ...
     int at[kRec];
-    float d[kRec], zc[kRec];
+    float d[kRec], pc[kRec], s = 0.f, dot = 0.f;
 #pragma unroll
     for (int j = 0; j < kRec; ++j) {
       at[j] = -1;
-      d[j] = 0.f;
-      zc[j] = -INFINITY;
+      d[j] = pc[j] = 0.f;
       const int r = j * G + lane;
       if (dgates && here && r < k) {
         const int a = indices[t * k + r];
         if (a >= 0 && a < experts) {
           at[j] = a;
           d[j] = dgates[t * k + r];
-          zc[j] = to_f32(logits[t * ld + a]);
+          pc[j] = exp_neg(to_f32(logits[t * ld + a]) - st.x) * st.y;
+          s += pc[j];
+          dot = fmaf(d[j], pc[j], dot);
         }
       }
     }
     live = t + groups < tokens && (!mask || mask[t + groups] != 0);
     if (live) row.load(logits + (t + groups) * ld, experts, lane, vec);  // the next token's
-    float top, inv;
-    bool bad;
-    const bool counted = softmax_row<G, NE>(z, e, top, inv, bad);
-    float pc[kRec], s = 0.f, dg = 0.f;
-#pragma unroll
-    for (int j = 0; j < kRec; ++j) {
-      pc[j] = at[j] >= 0 ? __expf(zc[j] - top) * inv : 0.f;
-      s += pc[j];
-      dg = fmaf(d[j], pc[j], dg);
-    }
-    if (dgates && normalize) {  // gate_r = p_r / S: d p_r = (d gate_r - sum_j d gate_j gate_j) / S
+    if (dgates && normalize) {
+      // gate_r = p_r / s: d p_r = (d gate_r - sum_j d gate_j gate_j) / s, whose sum with the p_r is zero
       s = group_sum<G>(s);
-      dg = group_sum<G>(dg) / s;
+      dot = group_sum<G>(dot) / s;
 #pragma unroll
       for (int j = 0; j < kRec; ++j)
-        if (at[j] >= 0) d[j] = (d[j] - dg) / s;
+        if (at[j] >= 0) d[j] = (d[j] - dot) / s;
+      dot = 0.f;
     }
-    float dot = 0.f;
+    float p[NE];
 #pragma unroll
-    for (int j = 0; j < kRec; ++j) dot = fmaf(pc[j], d[j], dot);
-    if (counted) {
-#pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        e[i] *= inv;
-        dot = fmaf(e[i], up[i], dot);
-      }
+    for (int i = 0; i < NE; ++i) {
+      p[i] = st.y > 0.f ? exp_neg(z[i] - st.x) * st.y : 0.f;
+      dot = fmaf(p[i], up[i], dot);
     }
     dot = group_sum<G>(dot);
     if (t < tokens) {
@@ -490,8 +492,7 @@ __global__ void __launch_bounds__(kThreads)
         if (R::at(lane, i) >= experts) continue;
         Pack<T, V> o;
 #pragma unroll
-        for (int q = 0; q < V; ++q)
-          o.v[q] = from_f32<T>(bad ? NAN : counted ? e[i + q] * (up[i + q] - dot) : 0.f);
+        for (int q = 0; q < V; ++q) o.v[q] = from_f32<T>(bad ? NAN : p[i + q] * (up[i + q] - dot));
         if (V == 1 || vec) {
           *reinterpret_cast<Pack<T, V>*>(out + R::at(lane, i)) = o;
         } else {
@@ -594,12 +595,13 @@ size_t layer_route_workspace_bytes(int64_t tokens, int32_t experts) {
 
 soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
                                   int32_t type, const uint8_t* mask, int32_t normalize, float coef,
-                                  int32_t* indices, float* gates, int32_t* counts, int32_t* live,
-                                  float* mean_probs, float* loss, int32_t* status, void* workspace,
+                                  int32_t* indices, float* gates, float* stats, int32_t* counts,
+                                  int32_t* live, float* mean_probs, float* loss, int32_t* status, void* workspace,
                                   size_t workspace_bytes, soap_stream_t stream) {
   if (bad_route(tokens, experts, k, logits, ld, type, coef)) return SOAP_ERR_INVALID_ARG;
   if (tokens > 0 && (bad_ptr(indices, 4) || bad_ptr(gates, 4))) return SOAP_ERR_INVALID_ARG;
   if (bad_ptr(counts, 4) || bad_ptr(live, 4) || bad_ptr(loss, 4) || (mean_probs && bad_ptr(mean_probs, 4)) ||
+      (stats && bad_ptr(stats, 8)) ||
       (status && bad_ptr(status, 4)) || bad_ptr(workspace, 16) ||
       workspace_bytes < layer_route_workspace_bytes(tokens, experts))
     return SOAP_ERR_INVALID_ARG;
@@ -626,7 +628,7 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
     using T = decltype(t);
     return cudaLaunchKernelEx(&cfg, route_fwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value>,
                               static_cast<const T*>(logits), ld, mask, tokens, (int)experts, (int)k, (int)normalize,
-                              indices, gates, part_p, part_c, out, vec, (int*)status);
+                              indices, gates, reinterpret_cast<float2*>(stats), part_p, part_c, out, vec, (int*)status);
   });
   if (e == cudaSuccess && parts > 1) {
     cfg.gridDim = dim3(1);
@@ -642,11 +644,11 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
 
 soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
                                    int32_t type, const uint8_t* mask, int32_t normalize, float coef, float dloss,
-                                   const int32_t* indices, const int32_t* counts, const int32_t* live,
-                                   const float* dgates, void* dlogits, int64_t ld_d, soap_stream_t stream) {
+                                   const int32_t* indices, const float* stats, const int32_t* counts,
+                                   const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d, soap_stream_t stream) {
   if (bad_route(tokens, experts, k, logits, ld, type, coef) || !std::isfinite(dloss)) return SOAP_ERR_INVALID_ARG;
   if (tokens == 0) return SOAP_OK;
-  if (bad_ptr(counts, 4) || bad_ptr(live, 4) || bad_ptr(dlogits, dtype_size(type)) || ld_d < experts ||
+  if (bad_ptr(stats, 8) || bad_ptr(counts, 4) || bad_ptr(live, 4) || bad_ptr(dlogits, dtype_size(type)) || ld_d < experts ||
       (dgates && (bad_ptr(dgates, 4) || bad_ptr(indices, 4))))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
@@ -660,7 +662,7 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
         using T = decltype(t);
         route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value><<<ctas, kThreads, 0, s>>>(
             static_cast<const T*>(logits), ld, mask, tokens, experts, k, normalize, scale, indices, counts, live,
-            dgates, static_cast<T*>(dlogits), ld_d, vec);
+            reinterpret_cast<const float2*>(stats), dgates, static_cast<T*>(dlogits), ld_d, vec);
         return cudaGetLastError();
       });
   return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;

@@ -153,13 +153,14 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
 class Routing(NamedTuple):
     """What route_forward decided: int32 indices and fp32 gates [..., k], int32 counts [experts], fp32
     mean_probs [experts], the fp32 scalar loss and the int32 scalar number of tokens counted (live);
-    mask, normalize and coef as given, for route_backward."""
+    for route_backward, each row's softmax statistics, and mask, normalize and coef as given."""
     indices: torch.Tensor
     gates: torch.Tensor
     counts: torch.Tensor
     mean_probs: torch.Tensor
     loss: torch.Tensor
     live: torch.Tensor
+    stats: torch.Tensor
     mask: Optional[torch.Tensor]
     normalize: bool
     coef: float
@@ -194,15 +195,16 @@ def route_forward(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = N
         raise ValueError(f"{name}: needs 1 to 1024 experts and k of 1 to min(experts, 32)")
     gates = z.new_empty(lead + (k,), dtype=torch.float32)
     indices = z.new_empty(lead + (k,), dtype=torch.int32)
+    stats = z.new_empty(lead + (2,), dtype=torch.float32)
     counts, mean_probs = z.new_empty(experts, dtype=torch.int32), z.new_empty(experts, dtype=torch.float32)
     live, loss = z.new_empty((), dtype=torch.int32), z.new_empty((), dtype=torch.float32)
     ws = z.new_empty(ws_bytes, dtype=torch.uint8)
     _done(lib.layer_route_forward(
         tokens, experts, k, z.data_ptr(), ld, DTYPES[z.dtype], None if mask is None else mask.data_ptr(),
-        int(normalize), coef, indices.data_ptr(), gates.data_ptr(), counts.data_ptr(), live.data_ptr(),
+        int(normalize), coef, indices.data_ptr(), gates.data_ptr(), stats.data_ptr(), counts.data_ptr(), live.data_ptr(),
         mean_probs.data_ptr(), loss.data_ptr(), None if status is None else status.data_ptr(), ws.data_ptr(), ws_bytes,
         _raw_stream(dev.index)), name)
-    return Routing(indices, gates, counts, mean_probs, loss, live, mask, bool(normalize), float(coef))
+    return Routing(indices, gates, counts, mean_probs, loss, live, stats, mask, bool(normalize), float(coef))
 
 
 def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torch.Tensor] = None, dloss: float = 1.0,
@@ -229,7 +231,7 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
     _done(load_library().layer_route_backward(
         tokens, shape[-1], shape_k[-1], z.data_ptr(), ld, DTYPES[z.dtype],
         None if routing.mask is None else routing.mask.data_ptr(), int(routing.normalize), routing.coef, dloss,
-        routing.indices.data_ptr(), routing.counts.data_ptr(), routing.live.data_ptr(),
+        routing.indices.data_ptr(), routing.stats.data_ptr(), routing.counts.data_ptr(), routing.live.data_ptr(),
         None if dgates is None else dgates.data_ptr(), dz.data_ptr(), shape[-1], _raw_stream(dev.index)), name)
     return dz
 

@@ -139,8 +139,8 @@ def load_library(path: str = LIB_PATH):
         "layer_norm_workspace_bytes": (SZ, [I64, I64]),
         "layer_norm_backward": (I32, [I64, I64, P, I64, P, I64, I32, P, P, P, I32, P, I64, P, P, P, SZ, P]),
         "layer_route_workspace_bytes": (SZ, [I64, I32]),
-        "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, SZ, P]),
-        "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, I64, P]),
+        "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, P, SZ, P]),
+        "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

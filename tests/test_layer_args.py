@@ -52,17 +52,17 @@ def test_route_refusals():
     assert lib.layer_route_workspace_bytes(9, 0) == lib.layer_route_workspace_bytes(9, 1025) == 0
     assert lib.layer_route_workspace_bytes(-1, 16) == 0
     ok = dict(tokens=9, experts=16, k=4, z=PTR, ld=16, type=0, mask=None, normalize=1, coef=0.1, idx=PTR, gates=PTR,
-              counts=PTR, live=PTR, mean=PTR, loss=PTR, status=None, ws=PTR, bytes=need)
+              stats=PTR, counts=PTR, live=PTR, mean=PTR, loss=PTR, status=None, ws=PTR, bytes=need)
     for change in (dict(tokens=-1), dict(tokens=1 << 31), dict(experts=0), dict(experts=1025), dict(k=0), dict(k=17),
                    dict(experts=64, ld=64, k=33, bytes=1 << 30), dict(z=None), dict(z=ODD), dict(ld=15), dict(type=3),
                    dict(coef=float("nan")), dict(idx=None), dict(gates=None), dict(counts=None), dict(live=None),
-                   dict(loss=None), dict(mean=ODD), dict(status=ODD), dict(ws=None), dict(ws=PTR + 8),
+                   dict(stats=PTR + 4), dict(loss=None), dict(mean=ODD), dict(status=ODD), dict(ws=None), dict(ws=PTR + 8),
                    dict(bytes=need - 1)):
         assert lib.layer_route_forward(*{**ok, **change}.values(), None) == 1, change
     ok = dict(tokens=9, experts=16, k=4, z=PTR, ld=16, type=0, mask=None, normalize=1, coef=0.1, dloss=1.0, idx=PTR,
-              counts=PTR, live=PTR, dgates=PTR, dz=PTR, ld_d=16)
+              stats=PTR, counts=PTR, live=PTR, dgates=PTR, dz=PTR, ld_d=16)
     for change in (dict(tokens=-1), dict(experts=0), dict(k=0), dict(z=None), dict(dz=None), dict(ld_d=15), dict(idx=None),
-                   dict(counts=None), dict(live=None), dict(dgates=ODD), dict(dloss=float("inf"))):
+                   dict(stats=None), dict(counts=None), dict(live=None), dict(dgates=ODD), dict(dloss=float("inf"))):
         assert lib.layer_route_backward(*{**ok, **change}.values(), None) == 1, change
     assert lib.layer_route_backward(*{**ok, "tokens": 0}.values(), None) == 0
 
