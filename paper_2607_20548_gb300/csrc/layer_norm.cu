@@ -22,8 +22,9 @@
 namespace soap {
 namespace {
 
-constexpr int kMaxThreads = 512;
-constexpr int kElems = 16;  // most elements of a row per thread
+constexpr int kMaxThreads = 512;  // of the kernels for rows too wide to be held
+// A CTA's threads by the elements of a row that each holds: few registers, all of an SM's threads.
+constexpr int threads_for(int elems) { return elems <= 8 ? 1024 : 512; }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -40,13 +41,13 @@ __device__ __forceinline__ void group_barrier() {
 // barrier per exchange is enough (a half is written again only after the barrier of the exchange
 // between).
 struct Exchange {
-  float2* buf;  // [2][blockDim.y][16]
+  float2* buf;  // [2][blockDim.y][blockDim.x / 32]
   int half = 0;
   // Afterwards lane l holds warp l's values ((0, 0) from the last warp on).
   __device__ __forceinline__ float2 all(float x, float y) {
-    float2* p = buf + (half * blockDim.y + threadIdx.y) * 16;
-    half ^= 1;
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    float2* p = buf + (half * blockDim.y + threadIdx.y) * warps;
+    half ^= 1;
     if (lane == 0) p[threadIdx.x >> 5] = make_float2(x, y);
     group_barrier();
     return lane < warps ? p[lane] : make_float2(0.f, 0.f);
@@ -65,7 +66,7 @@ __device__ __forceinline__ void copy_async(void* dst, const void* src) {
 
 // A thread's part of the rows of a matrix, NV packs of V elements per row, kDepth rows in flight.
 // Packs of less than 4 bytes cannot be copied asynchronously and are loaded when they are used.
-template <typename T, int V, int NV, int DEPTH>
+template <typename T, int V, int NV, int DEPTH, bool FULL>
 struct Rows {
   static constexpr bool kAsync = V * sizeof(T) >= 4;
   static constexpr int kSlot = kAsync ? V * sizeof(T) : 0;
@@ -81,20 +82,66 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * blockDim.x + threadIdx.x) * V;
-        if (c < width) copy_async<V * sizeof(T)>(slot(s, i), base + row * ld + c);
+        if (FULL || c < width) copy_async<V * sizeof(T)>(slot(s, i), base + row * ld + c);
       }
     }
   }
+  // The row's packs, zero beyond its end.
   __device__ __forceinline__ void get(int64_t row, int s, int width, Pack<T, V> (&p)[NV]) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * blockDim.x + threadIdx.x) * V;
-      if (c < width)
+      if (FULL || c < width) {
         p[i] = kAsync ? *reinterpret_cast<const Pack<T, V>*>(slot(s, i))
                       : *reinterpret_cast<const Pack<T, V>*>(base + row * ld + c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) p[i].v[e] = from_f32<T>(0.f);
+      }
     }
   }
 };
+
+// Elements 2 k and 2 k + 1 of a thread's packs as fp32.
+template <typename T, int V, int NV>
+__device__ __forceinline__ float2 values(const Pack<T, V> (&p)[NV], int k) {
+  if constexpr (V == 1)
+    return make_float2(to_f32(p[2 * k].v[0]), to_f32(p[2 * k + 1].v[0]));
+  else
+    return to_pair(p[2 * k / V].v + 2 * k % V);
+}
+
+// A row's results in pack i (V == 1: packs i and i + 1), rounded once.
+template <typename T, int V, bool FULL>
+__device__ __forceinline__ void put(T* row, int width, int i, const float2* v) {
+#pragma unroll
+  for (int j = 0; j < (V == 1 ? 2 : 1); ++j) {
+    const int c = ((i + j) * blockDim.x + threadIdx.x) * V;
+    if (!FULL && c >= width) break;
+    Pack<T, V> o;
+    if constexpr (V == 1) {
+      o.v[0] = from_f32<T>(j ? v[0].y : v[0].x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) from_pair(v[e / 2], o.v + e);
+    }
+    *reinterpret_cast<Pack<T, V>*>(row + c) = o;
+  }
+}
+
+// A thread's columns of a vector as fp32 pairs (`none` beyond the width, or everywhere without one).
+template <typename W, int V, int NV>
+__device__ __forceinline__ void columns(const W* w, float none, int width, float2 (&v)[NV * V / 2]) {
+#pragma unroll
+  for (int k = 0; k < NV * V; ++k) {
+    const int c = ((k / V) * blockDim.x + threadIdx.x) * V + k % V;
+    const float x = w && c < width ? to_f32(w[c]) : none;
+    if (k % 2)
+      v[k / 2].y = x;
+    else
+      v[k / 2].x = x;
+  }
+}
 
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -104,14 +151,15 @@ __device__ __forceinline__ void arrived() {
 
 // ---- forward: a group of blockDim.x threads per row, NV packs of V elements each ------------
 
-template <typename T, typename W, int V, int NV, int DEPTH>
-__global__ void __launch_bounds__(kMaxThreads)
+// FULL: the group's threads have exactly the row's elements.
+template <typename T, typename W, int V, int NV, int DEPTH, bool FULL>
+__global__ void __launch_bounds__(threads_for(NV * V))
     norm_fwd_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
                     float* mean, float* rstd, int64_t rows, int width) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 buf[2 * 16 * 16];
-  constexpr int E = NV * V;
-  using R = Rows<T, V, NV, DEPTH>;
+  __shared__ float2 buf[2 * 32];
+  constexpr int P = NV * V / 2, kPer = V == 1 ? 2 : 1;
+  using R = Rows<T, V, NV, DEPTH, FULL>;
   const int tid = threadIdx.y * blockDim.x + threadIdx.x, lane = threadIdx.x & 31;
   const R in{x, ld_x, smem + (size_t)tid * R::kSlot};
   Exchange ex{buf};
@@ -122,16 +170,9 @@ __global__ void __launch_bounds__(kMaxThreads)
     if (row + s * step < rows) in.request(row + s * step, s, width);
     commit();
   }
-  float w[E], b[E];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * blockDim.x + threadIdx.x) * V;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      w[i * V + e] = weight && c < width ? to_f32(weight[c + e]) : 1.f;
-      b[i * V + e] = bias && c < width ? to_f32(bias[c + e]) : 0.f;
-    }
-  }
+  float2 w[P], b[P];
+  columns<W, V, NV>(weight, 1.f, width, w);
+  columns<W, V, NV>(bias, 0.f, width, b);
   // elements of the row in this thread's warp, and in the group's warp `lane`
   auto warp_count = [&](int warp) {
     int n = 0;
@@ -142,59 +183,52 @@ __global__ void __launch_bounds__(kMaxThreads)
   const float here = warp_count(threadIdx.x >> 5), inv = 1.f / (float)width;
   const float there = lane < (int)blockDim.x / 32 ? warp_count(lane) : 0.f;
   const float inv_here = here > 0.f ? 1.f / here : 0.f, inv_there = there > 0.f ? 1.f / there : 0.f;
+  // whether this thread's element k is one of the row's
+  auto has = [&](int k) { return ((k / V) * (int)blockDim.x + (int)threadIdx.x) * V + k % V < width; };
   int s = 0;
   for (; row < rows; row += step) {
     const int64_t ahead = row + (DEPTH - 1) * step;
     if (ahead < rows) in.request(ahead, s == 0 ? DEPTH - 1 : s - 1, width);
     commit();
     arrived<DEPTH - 1>();
-    Pack<T, V> p[NV];
-    in.get(row, s, width, p);
+    float2 v[P];
+    Pack<T, V> raw[NV];
+    in.get(row, s, width, raw);
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = values(raw, i);
     s = s + 1 == DEPTH ? 0 : s + 1;
     // sum and spread of the warp's elements about the warp's mean, then over the warps
-    float v[E], sum = 0.f;
+    float2 acc = pair(0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
+    for (int i = 0; i < P; ++i) acc = add2(acc, v[i]);
+    float sum = warp_sum(acc.x + acc.y);
+    float mu = sum * inv_here;
+    acc = pair(0.f);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        v[i * V + e] = in_row ? to_f32(p[i].v[e]) : 0.f;
-        sum += v[i * V + e];
+    for (int i = 0; i < P; ++i) {
+      float2 d = add2(v[i], pair(-mu));
+      if constexpr (!FULL) {
+        if (!has(2 * i)) d.x = 0.f;
+        if (!has(2 * i + 1)) d.y = 0.f;
       }
+      acc = fma2(d, d, acc);
     }
-    sum = warp_sum(sum);
-    float mu = sum * inv_here, q = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = v[i * V + e] - mu;
-        if (in_row) q = fmaf(d, d, q);
-      }
-    }
-    q = warp_sum(q);
+    float q = warp_sum(acc.x + acc.y);
     if (blockDim.x > 32) {
       const float2 o = ex.all(sum, q);
       mu = warp_sum(o.x) * inv;
       const float d = o.x * inv_there - mu;
       q = warp_sum(fmaf(there * d, d, o.y));
     }
-    const float rs = 1.f / sqrtf(q * inv + eps);
+    const float rs = rsqrtf(q * inv + eps);
     if (threadIdx.x == 0) {
       if (mean) mean[row] = mu;
       if (rstd) rstd[row] = rs;
     }
-    T* yr = y + row * ld_y;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * V;
-      if (c >= width) break;
-      Pack<T, V> o;
+    for (int i = 0; i < P; ++i) v[i] = fma2(mul2(add2(v[i], pair(-mu)), pair(rs)), w[i], b[i]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(fmaf((v[i * V + e] - mu) * rs, w[i * V + e], b[i * V + e]));
-      *reinterpret_cast<Pack<T, V>*>(yr + c) = o;
-    }
+    for (int i = 0; i < NV; i += kPer) put<T, V, FULL>(y + row * ld_y, width, i, v + i * V / 2);
   }
   arrived<0>();
 }
@@ -234,7 +268,7 @@ __global__ void __launch_bounds__(kMaxThreads)
     q[0] = fmaf(d, d, q[0]);
   }
   block_sum(q, buf);
-  const float rs = 1.f / sqrtf(q[0] / (float)width + eps);
+  const float rs = rsqrtf(q[0] / (float)width + eps);
   if (threadIdx.x == 0) {
     if (mean) mean[row] = mu;
     if (rstd) rstd[row] = rs;
@@ -250,101 +284,141 @@ __global__ void __launch_bounds__(kMaxThreads)
 // norm_cols_kernel adds the partial rows in order (no atomics: the result does not depend on
 // which CTA finishes first).
 
-template <typename T, typename W, int V, int NV, int DEPTH>
-__global__ void __launch_bounds__(kMaxThreads)
+// R rows of a group go through an iteration side by side, so that one's chain of sums and exchanges
+// fills the other's waits. A thread keeps a row's packs and converts them twice. kSmemW: weights in
+// shared memory (fp32, at their columns), where registers would not hold them beside both sums.
+template <typename T, typename W, int V, int NV, int R, int DEPTH, bool FULL>
+__global__ void __launch_bounds__(threads_for(NV * V))
     norm_bwd_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
                     const W* weight, T* dx, int64_t ld_dx, float* part, int64_t rows, int width) {
-  extern __shared__ __align__(16) uint8_t smem[];  // the rings; afterwards the groups' column sums
-  __shared__ float2 buf[2 * 16 * 16];
-  constexpr int E = NV * V;
-  using R = Rows<T, V, NV, DEPTH>;
+  extern __shared__ __align__(16) uint8_t smem[];  // the rings (and weights); afterwards the groups' column sums
+  __shared__ float4 buf[2 * 32];
+  constexpr int E = NV * V, P = E / 2, kPer = V == 1 ? 2 : 1;
+  constexpr bool kSmemW = E > 16;
+  using S = Rows<T, V, NV, DEPTH * R, FULL>;
   const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
-  const R rx{x, ld_x, smem + (size_t)tid * R::kSlot};
-  const R rg{dy, ld_dy, smem + (size_t)(DEPTH * NV * threads + tid) * R::kSlot};
-  Exchange ex{buf};
+  const S rx{x, ld_x, smem + (size_t)tid * S::kSlot};
+  const S rg{dy, ld_dy, smem + (size_t)(DEPTH * R * NV * threads + tid) * S::kSlot};
+  float* const weights = reinterpret_cast<float*>(smem + (size_t)2 * DEPTH * R * NV * threads * S::kSlot);
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  auto request = [&](int64_t first, int stage) {
 #pragma unroll
-  for (int s = 0; s < DEPTH - 1; ++s) {
-    if (row + s * step < rows) {
-      rx.request(row + s * step, s, width);
-      rg.request(row + s * step, s, width);
-    }
+    for (int r = 0; r < R; ++r)
+      if (first + r * step < rows) {
+        rx.request(first + r * step, stage * R + r, width);
+        rg.request(first + r * step, stage * R + r, width);
+      }
     commit();
+  };
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s) request(row + s * R * step, s);
+  float2 w[kSmemW ? 1 : P], aw[P], ab[P];
+  if constexpr (kSmemW) {
+    for (int c = tid; c < width; c += threads) weights[c] = weight ? to_f32(weight[c]) : 1.f;
+    __syncthreads();
+  } else {
+    columns<W, V, NV>(weight, 1.f, width, w);
   }
-  float w[E], aw[E], ab[E];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * blockDim.x + threadIdx.x) * V;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      w[i * V + e] = weight && c < width ? to_f32(weight[c + e]) : 1.f;
-      aw[i * V + e] = ab[i * V + e] = 0.f;
+  for (int i = 0; i < P; ++i) aw[i] = ab[i] = pair(0.f);
+  // weights of elements 2 k and 2 k + 1 (beyond the row's end any finite value: dy is zero there)
+  auto weight_of = [&](int k) {
+    if constexpr (!kSmemW) {
+      return w[k];
+    } else {
+      const int c = ((2 * k / V) * blockDim.x + threadIdx.x) * V + 2 * k % V;
+      if (V == 1) return make_float2(weights[min(c, width - 1)], weights[min(c + (int)blockDim.x, width - 1)]);
+      return FULL || c < width ? *reinterpret_cast<const float2*>(weights + c) : pair(0.f);
     }
-  }
+  };
   const float inv = 1.f / (float)width;
-  float mu = 0.f, rs = 0.f;
-  if (row < rows) {
-    mu = mean[row];
-    rs = rstd[row];
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  float mu[R], rs[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    mu[r] = rs[r] = 0.f;
+    if (row + r * step < rows) {
+      mu[r] = mean[row + r * step];
+      rs[r] = rstd[row + r * step];
+    }
   }
-  int s = 0;
-  while (row < rows) {
-    const int64_t ahead = row + (DEPTH - 1) * step;
-    if (ahead < rows) {
-      const int to = s == 0 ? DEPTH - 1 : s - 1;
-      rx.request(ahead, to, width);
-      rg.request(ahead, to, width);
-    }
-    commit();
+  int s = 0, half = 0;
+  for (; row < rows; row += R * step) {
+    request(row + (DEPTH - 1) * R * step, s == 0 ? DEPTH - 1 : s - 1);
     arrived<DEPTH - 1>();
-    Pack<T, V> px[NV], pg[NV];
-    rx.get(row, s, width, px);
-    rg.get(row, s, width, pg);
-    s = s + 1 == DEPTH ? 0 : s + 1;
-    const int64_t next = row + step;
-    float mu_next = 0.f, rs_next = 0.f;
-    if (next < rows) {
-      mu_next = mean[next];
-      rs_next = rstd[next];
+    Pack<T, V> px[R][NV], pg[R][NV];
+    float sum[R][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r * step < rows) {
+        rx.get(row + r * step, s * R + r, width, px[r]);
+        rg.get(row + r * step, s * R + r, width, pg[r]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < V; ++e) px[r][i].v[e] = pg[r][i].v[e] = from_f32<T>(0.f);
+      }
+      // beyond the row's end dy is zero, so whatever xh is there counts nowhere
+      float2 a0 = pair(0.f), a1 = pair(0.f);
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const float2 xh = mul2(add2(values(px[r], k), pair(-mu[r])), pair(rs[r]));
+        float2 g = values(pg[r], k);
+        aw[k] = fma2(g, xh, aw[k]);
+        ab[k] = add2(ab[k], g);
+        g = mul2(g, weight_of(k));
+        a0 = add2(a0, g);
+        a1 = fma2(g, xh, a1);
+      }
+      sum[r][0] = a0.x + a0.y;
+      sum[r][1] = a1.x + a1.y;
     }
-    float xh[E], g[E], s0 = 0.f, s1 = 0.f;
+    s = s + 1 == DEPTH ? 0 : s + 1;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const bool in_row = (int)(i * blockDim.x + threadIdx.x) * V < width;
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int k = i * V + e;
-        const float d = in_row ? to_f32(pg[i].v[e]) : 0.f;
-        xh[k] = in_row ? (to_f32(px[i].v[e]) - mu) * rs : 0.f;
-        g[k] = d * w[k];
-        s0 += g[k];
-        s1 = fmaf(g[k], xh[k], s1);
-        aw[k] = fmaf(d, xh[k], aw[k]);
-        ab[k] += d;
+      for (int r = 0; r < 2 * R; ++r) sum[r / 2][r % 2] += __shfl_xor_sync(0xffffffffu, sum[r / 2][r % 2], o);
+    if (warps > 1) {  // the halves of the buffer in turn, as in Exchange
+      float4* p = buf + (half * blockDim.y + threadIdx.y) * warps;
+      half ^= 1;
+      if (lane == 0) p[threadIdx.x >> 5] = make_float4(sum[0][0], sum[0][1], sum[R - 1][0], sum[R - 1][1]);
+      group_barrier();
+      const float4 o = lane < warps ? p[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+      sum[R - 1][0] = o.z;
+      sum[R - 1][1] = o.w;
+      sum[0][0] = o.x;
+      sum[0][1] = o.y;
+#pragma unroll
+      for (int q = 16; q > 0; q >>= 1)
+#pragma unroll
+        for (int r = 0; r < 2 * R; ++r) sum[r / 2][r % 2] += __shfl_xor_sync(0xffffffffu, sum[r / 2][r % 2], q);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t here = row + r * step;
+      if (here < rows) {
+        const float2 m1 = pair(-sum[r][0] * inv * rs[r]), m2 = pair(-sum[r][1] * inv * rs[r]);
+        T* to = dx + here * ld_dx;
+#pragma unroll
+        for (int i = 0; i < NV; i += kPer) {
+          float2 g[kPer * V / 2];
+#pragma unroll
+          for (int j = 0; j < kPer * V / 2; ++j) {
+            const int k = i * V / 2 + j;
+            const float2 xh = mul2(add2(values(px[r], k), pair(-mu[r])), pair(rs[r]));
+            g[j] = fma2(xh, m2, fma2(mul2(values(pg[r], k), weight_of(k)), pair(rs[r]), m1));
+          }
+          put<T, V, FULL>(to, width, i, g);
+        }
+      }
+      const int64_t next = here + R * step;
+      if (next < rows) {
+        mu[r] = mean[next];
+        rs[r] = rstd[next];
       }
     }
-    s0 = warp_sum(s0);
-    s1 = warp_sum(s1);
-    if (blockDim.x > 32) {
-      const float2 o = ex.all(s0, s1);
-      s0 = warp_sum(o.x);
-      s1 = warp_sum(o.y);
-    }
-    const float m1 = s0 * inv, m2 = s1 * inv;
-    T* dr = dx + row * ld_dx;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * V;
-      if (c >= width) break;
-      Pack<T, V> o;
-#pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(rs * (g[i * V + e] - m1 - xh[i * V + e] * m2));
-      *reinterpret_cast<Pack<T, V>*>(dr + c) = o;
-    }
-    row = next;
-    mu = mu_next;
-    rs = rs_next;
   }
   arrived<0>();
   if (!part) return;
@@ -355,10 +429,10 @@ __global__ void __launch_bounds__(kMaxThreads)
   for (int k = 0; k < 2; ++k) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        sums[threadIdx.y * lanes + (i * blockDim.x + threadIdx.x) * V + e] = k == 0 ? aw[i * V + e] : ab[i * V + e];
+    for (int j = 0; j < E; ++j) {
+      const float2 a = k == 0 ? aw[j / 2] : ab[j / 2];
+      sums[threadIdx.y * lanes + ((j / V) * blockDim.x + threadIdx.x) * V + j % V] = j % 2 ? a.y : a.x;
+    }
     __syncthreads();
     float* out = part + ((int64_t)blockIdx.x * 2 + k) * width;
     for (int c = tid; c < width; c += threads) {
@@ -432,27 +506,42 @@ __global__ void norm_cols_kernel(const float* part, int parts, int64_t width, fl
 
 // ---- launch choice -------------------------------------------------------------------------
 
-constexpr int kParts = 152;  // most partial rows: one CTA per SM
+constexpr int kSms = 152;
+constexpr int kParts = 2 * kSms;  // most CTAs, and partial rows
 
 struct NormShape {
   int nv, tx;  // accesses per thread and row, threads per row
 };
 
-// Threads for a row of `width` elements in accesses of v: at most 16 elements per thread, so that a
-// thread's columns and both of their sums stay in registers; nv = 0: too wide for that. Rows that a
-// warp or two can hold take fewer elements per thread.
-NormShape norm_shape(int64_t width, int v) {
+// Threads for a row of `width` elements in accesses of v: a warp where 16 elements per thread are
+// enough, else the fewest that give a thread no more than `elems` elements, or more up to `most` where
+// the row needs it. nv = 0: too wide for that.
+NormShape norm_shape(int64_t width, int v, int elems, int most) {
   const int64_t packs = (width + v - 1) / v;
-  const int most = kElems / v;
-  for (int nv = 1; nv <= most; nv *= 2)
-    for (int tx = 32; tx <= kMaxThreads; tx *= 2)
-      if (packs <= (int64_t)tx * nv && (nv == most || tx <= 64)) return {nv, tx};
+  for (int nv = v == 1 ? 2 : 1; nv * v <= 16; nv *= 2)
+    if (packs <= 32 * nv) return {nv, 32};
+  for (int e = elems; e <= most; e *= 2)
+    for (int tx = 64; tx <= threads_for(e); tx *= 2)
+      if (packs * v <= (int64_t)tx * e) return {e / v, tx};
   return {0, 0};
 }
 
+// With few rows per SM a row's own time counts: 8 elements per thread and many threads. With many, rows
+// side by side in an SM hide each other's chains of sums: more elements per thread, so that more rows
+// fit (forward, 32768 x 8192 bf16: 258 us with 8, 260 with 16, 200 with 32).
+bool many_rows(int64_t rows) { return rows >= 16 * kSms; }
+
+int norm_threads(const NormShape& n, int v) { return n.tx >= 128 ? threads_for(n.nv * v) : 512; }
+
 // Rows per CTA: full CTAs, unless the rows would then not reach every SM.
-int norm_groups(int64_t rows, int tx) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxThreads / tx, (rows + kParts - 1) / kParts));
+int norm_groups(int64_t rows, const NormShape& n, int v) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(norm_threads(n, v) / n.tx, (rows + kSms - 1) / kSms));
+}
+
+// CTAs: two per SM where one does not fill it.
+int norm_ctas(int64_t rows, const NormShape& n, int v, int ty) {
+  const int most = n.tx * ty <= 512 && n.nv * v <= 8 ? kParts : kSms;
+  return (int)std::min<int64_t>(most, (rows + ty - 1) / ty);
 }
 
 template <typename F>
@@ -462,18 +551,26 @@ cudaError_t with_nv(int nv, F&& f) {
     case 2: return f(std::integral_constant<int, 2>());
     case 4: return f(std::integral_constant<int, 4>());
     case 8: return f(std::integral_constant<int, 8>());
-    default: return f(std::integral_constant<int, 16>());
+    case 16: return f(std::integral_constant<int, 16>());
+    default: return f(std::integral_constant<int, 32>());
   }
 }
 
-// f(elements per access): the widest access of up to 16 bytes that `bytes` (an OR of all addresses and
-// row lengths in bytes) divides into.
+// f(elements per access) for rows whose addresses and lengths in bytes, ORed, are `bytes`: 16 bytes, else
+// 8, else 4, else an element.
 template <typename T, typename F>
 cudaError_t with_access(uintptr_t bytes, F&& f) {
   if (bytes % 16 == 0) return f(std::integral_constant<int, 16 / sizeof(T)>());
   if (bytes % 8 == 0) return f(std::integral_constant<int, 8 / sizeof(T)>());
-  if (sizeof(T) < 4 && bytes % 4 == 0) return f(std::integral_constant<int, std::max<int>(1, 4 / sizeof(T))>());
+  if (sizeof(T) == 2 && bytes % 4 == 0) return f(std::integral_constant<int, sizeof(T) == 2 ? 2 : 1>());
   return f(std::integral_constant<int, 1>());
+}
+
+// f(whether the row has exactly the group's elements): told apart for the widest accesses.
+template <int V, typename F>
+cudaError_t with_full(bool full, F&& f) {
+  if (V >= 4 && full) return f(std::integral_constant<bool, (V >= 4)>());
+  return f(std::integral_constant<bool, false>());
 }
 
 uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
@@ -495,24 +592,27 @@ cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& set) {
 template <typename T, typename W, int V>
 cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W* w, const W* b, float eps, T* y,
                   int64_t ld_y, float* mean, float* rstd, cudaStream_t s) {
-  const NormShape n = norm_shape(width, V);
+  const NormShape n = norm_shape(width, V, many_rows(rows) ? 32 : 8, 32);
   if (n.nv == 0) {
     norm_fwd_wide_kernel<T, W><<<(unsigned)rows, kMaxThreads, 0, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, width);
     return cudaGetLastError();
   }
-  const int ty = norm_groups(rows, n.tx);
-  const unsigned grid = (unsigned)std::min<int64_t>(kParts, (rows + ty - 1) / ty);
+  const int ty = norm_groups(rows, n, V);
+  const unsigned grid = (unsigned)norm_ctas(rows, n, V, ty);
   return with_nv(n.nv, [&](auto nv) {
-    constexpr int NV = decltype(nv)::value, DEPTH = 4;
-    if constexpr (NV * V <= kElems) {
-      static std::atomic<uint64_t> set{0};
-      const int smem = DEPTH * NV * n.tx * ty * Rows<T, V, NV, DEPTH>::kSlot;
-      const cudaError_t e = allow_smem(norm_fwd_kernel<T, W, V, NV, DEPTH>, smem, set);
-      if (e != cudaSuccess) return e;
-      norm_fwd_kernel<T, W, V, NV, DEPTH>
-          <<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, rows, (int)width);
+    constexpr int NV = decltype(nv)::value, DEPTH = NV * V * sizeof(T) > 64 ? 3 : 4;
+    if constexpr (NV * V <= 32 && NV * V > 1) {
+      const int smem = DEPTH * NV * n.tx * ty * Rows<T, V, NV, DEPTH, false>::kSlot;
+      return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
+        static std::atomic<uint64_t> set{0};
+        const auto kernel = norm_fwd_kernel<T, W, V, NV, DEPTH, decltype(full)::value>;
+        const cudaError_t e = allow_smem(kernel, smem, set);
+        if (e != cudaSuccess) return e;
+        kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, rows, (int)width);
+        return cudaGetLastError();
+      });
     }
-    return cudaGetLastError();
+    return cudaErrorInvalidValue;
   });
 }
 
@@ -530,9 +630,9 @@ template <typename T, typename W, int V>
 cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x,
                   const float* mean, const float* rstd, const W* w, T* dx, int64_t ld_dx, float* dw, float* db,
                   float* part, cudaStream_t s) {
-  const NormShape n = norm_shape(width, V);
+  const NormShape n = norm_shape(width, V, many_rows(rows) ? 16 : 8, sizeof(T) == 2 ? 32 : 16);
   float* p = dw || db ? part : nullptr;
-  int parts = (int)std::min<int64_t>(kParts, rows);
+  int parts = (int)std::min<int64_t>(kSms, rows);
   cudaError_t e;
   if (n.nv == 0) {
     if (p)
@@ -542,20 +642,28 @@ cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const
                                                                      width);
     e = cudaGetLastError();
   } else {
-    const int ty = norm_groups(rows, n.tx);
-    parts = (int)std::min<int64_t>(kParts, (rows + ty - 1) / ty);
+    const int ty = norm_groups(rows, n, V);
+    parts = norm_ctas(rows, n, V, ty);
     e = with_nv(n.nv, [&](auto nv) {
-      constexpr int NV = decltype(nv)::value, DEPTH = sizeof(T) == 4 ? 3 : 4;
-      if constexpr (NV * V <= kElems) {
-        static std::atomic<uint64_t> set{0};
+      constexpr int NV = decltype(nv)::value, E = NV * V;
+      if constexpr (E <= (sizeof(T) == 2 ? 32 : 16) && E > 1) {
+        // two rows at a time where a CTA has few threads per SM and registers for them; at most 192 KB of rows
+        constexpr int R = E == 16 && sizeof(T) == 2 ? 2 : 1;
+        constexpr int kStage = threads_for(E) * E * (int)sizeof(T) * 2 * R;
+        constexpr int DEPTH = E > 16 ? 2 : std::min(4, 192 * 1024 / kStage);
         const int threads = n.tx * ty;
-        const int smem = threads * NV * std::max<int>(2 * DEPTH * Rows<T, V, NV, DEPTH>::kSlot, V * 4);
-        const cudaError_t ae = allow_smem(norm_bwd_kernel<T, W, V, NV, DEPTH>, smem, set);
-        if (ae != cudaSuccess) return ae;
-        norm_bwd_kernel<T, W, V, NV, DEPTH><<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx,
-                                                                                ld_dx, p, rows, (int)width);
+        const int ring = 2 * DEPTH * R * NV * threads * Rows<T, V, NV, DEPTH, false>::kSlot;
+        const int smem = std::max(ring + (E > 16 ? (int)width * 4 : 0), threads * E * 4);
+        return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
+          static std::atomic<uint64_t> set{0};
+          const auto kernel = norm_bwd_kernel<T, W, V, NV, R, DEPTH, decltype(full)::value>;
+          const cudaError_t ae = allow_smem(kernel, smem, set);
+          if (ae != cudaSuccess) return ae;
+          kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, rows, (int)width);
+          return cudaGetLastError();
+        });
       }
-      return cudaGetLastError();
+      return cudaErrorInvalidValue;
     });
   }
   if (e != cudaSuccess || !p) return e;

@@ -32,6 +32,55 @@ struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack {
   T v[V];
 };
 
+// Pairs of fp32 values, for the instructions that take two at a time.
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+__device__ __forceinline__ uint64_t bits(float2 a) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y));
+  return r;
+}
+__device__ __forceinline__ float2 from_bits(uint64_t a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return from_bits(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return from_bits(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return from_bits(r);
+}
+
+// Two neighbouring elements to fp32 and back (round to nearest).
+__device__ __forceinline__ float2 to_pair(const float* p) { return make_float2(p[0], p[1]); }
+__device__ __forceinline__ float2 to_pair(const __nv_bfloat16* p) {
+  return __bfloat1622float2(__nv_bfloat162(p[0], p[1]));
+}
+__device__ __forceinline__ float2 to_pair(const __half* p) { return __half22float2(__half2(p[0], p[1])); }
+__device__ __forceinline__ void from_pair(float2 v, float* p) {
+  p[0] = v.x;
+  p[1] = v.y;
+}
+__device__ __forceinline__ void from_pair(float2 v, __nv_bfloat16* p) {
+  const __nv_bfloat162 h = __float22bfloat162_rn(v);
+  p[0] = h.x;
+  p[1] = h.y;
+}
+__device__ __forceinline__ void from_pair(float2 v, __half* p) {
+  const __half2 h = __float22half2_rn(v);
+  p[0] = __low2half(h);
+  p[1] = __high2half(h);
+}
+
 inline size_t dtype_size(int32_t t) { return t == 0 ? 4 : 2; }
 
 }  // namespace soap
