@@ -32,24 +32,27 @@ extern "C" {
  *   mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) rstd * weight + bias
  * x, y: x_type, row i at element i * ld; y may be x (in place). weight, bias: `width` elements
  * of w_type (SOAP_F32 or x_type), either may be NULL (1, 0). mean, rstd: fp32 [rows] for the
- * backward pass, either may be NULL. rows = 0 does nothing. SOAP_ERR_INVALID_ARG for rows < 0,
+ * backward pass, either may be NULL. status: NULL, or a device int32 into which the kernels OR
+ * SOAP_STATUS_TIMEOUT if a bounded internal wait gave up (not cleared). rows = 0 does nothing. SOAP_ERR_INVALID_ARG for rows < 0,
  * width < 1, a leading dimension below width, a type out of range, a null or misaligned
  * pointer, or eps < 0. */
 soap_status_t layer_norm_forward(int64_t rows, int64_t width, const void* x, int64_t ld_x, int32_t x_type,
                                  const void* weight, const void* bias, int32_t w_type, float eps, void* y,
-                                 int64_t ld_y, float* mean, float* rstd, soap_stream_t stream);
+                                 int64_t ld_y, float* mean, float* rstd, int32_t* status,
+                                 soap_stream_t stream);
 
 /* The backward pass, from the forward pass's mean and rstd; with xh = (x - mu) rstd, g = dy * weight:
  *   dx = rstd (g - mean(g) - xh mean(g xh)),  dweight = sum over rows of dy xh,  dbias = sum of dy
  * dy, x, dx: x_type (dx may be dy or x). weight: as given forward (NULL: 1). dweight, dbias: fp32
  * [width] or NULL (not formed); rows = 0 sets them to 0. `workspace`: 16-byte aligned device
  * memory of layer_norm_workspace_bytes(rows, width) bytes for the per-CTA column sums (not needed,
- * and may be NULL, when neither gradient is formed). */
+ * and may be NULL, when neither gradient is formed). status: as forward. */
 size_t layer_norm_workspace_bytes(int64_t rows, int64_t width);
 soap_status_t layer_norm_backward(int64_t rows, int64_t width, const void* dy, int64_t ld_dy, const void* x,
                                   int64_t ld_x, int32_t x_type, const float* mean, const float* rstd,
                                   const void* weight, int32_t w_type, void* dx, int64_t ld_dx, float* dweight,
-                                  float* dbias, void* workspace, size_t workspace_bytes, soap_stream_t stream);
+                                  float* dbias, void* workspace, size_t workspace_bytes, int32_t* status,
+                                  soap_stream_t stream);
 
 /* A router's decision for `tokens` rows z of `experts` logits (row i at element i * ld):
  *   p = softmax(z); chosen: the k largest logits, by value and then by the lower index

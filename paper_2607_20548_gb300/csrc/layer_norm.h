@@ -1,0 +1,346 @@
+// What layer norm's forward and backward kernels share: how the rows come in, sums over a row's
+// threads, and the choice of a row's threads. Included by layer_norm.cu and layer_norm_bwd.cu.
+//
+// Bound by memory: x is read and y written once (backward: x and dy read, dx written once). A
+// group of threads holds a row in registers, so that the variance is a second pass over registers
+// (not E[x^2] - mu^2, which cancels) and nothing is read twice. CTAs are persistent: each thread
+// keeps its columns' weights (backward: and their gradients' sums) in registers over all its rows
+// (read again for every row, fp32 weights are four times the traffic of a bf16 x through L1: 345 us
+// at 32768 x 8192), and rows come in ahead, where they are 16-byte aligned by bulk copies into a ring
+// in shared memory (asynchronous 16-byte copies by every thread stopped at 2.7 TB/s of reads),
+// else, a row ahead, into registers. Pairs of elements go through the fp32 pipe together.
+#pragma once
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "../../include/layer.h"
+#include "profile.h"
+#include "tc_ptx.h"
+#include "types.h"
+
+namespace soap {
+namespace {
+
+constexpr int kMaxThreads = 512;  // of the kernels for rows too wide to be held
+// A CTA's threads by the elements of a row that each holds (`bulk`: rows come through shared memory, not
+// registers): few registers, twice the threads.
+constexpr int threads_for(int elems, bool bulk) { return elems <= 8 && bulk ? 1024 : 512; }
+constexpr int kMaxGroups = 16;    // row groups of a CTA
+constexpr uint64_t kWaitNs = 2000000000ull;
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// One barrier among a row group's threads (blockDim.x of them, more than a warp).
+__device__ __forceinline__ void group_barrier() {
+  asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"((int)blockDim.x) : "memory");
+}
+
+// What a row group's warps exchange: two values per warp, in two halves used in turn, so that one
+// barrier per exchange is enough (a half is written again only after the barrier of the exchange
+// between).
+struct Exchange {
+  float2* buf;  // [2][blockDim.y][blockDim.x / 32]
+  int half = 0;
+  // Afterwards lane l holds warp l's values ((0, 0) from the last warp on).
+  __device__ __forceinline__ float2 all(float x, float y) {
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    float2* p = buf + (half * blockDim.y + threadIdx.y) * warps;
+    half ^= 1;
+    if (lane == 0) p[threadIdx.x >> 5] = make_float2(x, y);
+    group_barrier();
+    return lane < warps ? p[lane] : make_float2(0.f, 0.f);
+  }
+};
+
+// The rows of N matrices (x; or dy and x) for a row group, R rows at a time and DEPTH times ahead, NV packs
+// of V elements per thread and row.
+template <typename T, int V, int NV, int N, int R, int DEPTH, bool FULL>
+struct Rows {
+  static constexpr bool kBulk = V * sizeof(T) == 16;  // a ring in shared memory; else registers
+  static constexpr int kRowBytes = NV * 16;           // of the ring, per thread
+  static constexpr int kRing = kBulk ? DEPTH * R * N * kRowBytes : 0;  // bytes per thread
+  static_assert(kBulk || R == 1, "one row at a time in registers");
+  const T* base[N];
+  int64_t ld[N];
+  int64_t rows, step;
+  int width;
+  uint8_t* ring;    // the group's: row slot q at q * blockDim.x * kRowBytes
+  uint64_t* full;   // the group's barriers, one per stage
+  int* status;
+  int s = 0;
+  uint32_t parity = 0;
+  bool dead = false;  // a wait ran out: what follows is invalid, and waits for nothing
+  Pack<T, V> ahead[kBulk ? 1 : N][kBulk ? 1 : NV];
+
+  __device__ __forceinline__ uint8_t* slot(int stage, int r, int n) const {
+    return ring + (size_t)((stage * R + r) * N + n) * blockDim.x * kRowBytes;
+  }
+  // One thread asks for the rows from `row` on (R of them, `step` apart) into a stage.
+  __device__ __forceinline__ void request(int64_t row, int stage) {
+    const uint32_t bytes = (uint32_t)width * sizeof(T);
+    int n = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) n += row + r * step < rows;
+    if (n == 0) return;
+    const uint32_t bar = tc::smem_u32(full + stage);
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * N * bytes) : "memory");
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r < n)
+#pragma unroll
+        for (int m = 0; m < N; ++m)
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                  tc::smem_u32(slot(stage, r, m))),
+              "l"(base[m] + (row + r * step) * ld[m]), "r"(bytes), "r"(bar)
+              : "memory");
+  }
+  __device__ __forceinline__ void load(int64_t row) {
+    if constexpr (!kBulk) {
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int c = (i * blockDim.x + threadIdx.x) * V;
+          if (row < rows && c < width) {
+            ahead[m][i] = *reinterpret_cast<const Pack<T, V>*>(base[m] + row * ld[m] + c);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) ahead[m][i].v[e] = from_f32<T>(0.f);
+          }
+        }
+    }
+  }
+  // Before the first row: called by all threads of the CTA.
+  __device__ __forceinline__ void start(int64_t row) {
+    if constexpr (kBulk) {
+      if (threadIdx.x == 0) {
+        for (int q = 0; q < DEPTH; ++q) tc::mbar_init(full + q, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int q = 0; q < DEPTH; ++q) request(row + q * R * step, q);
+      }
+      __syncthreads();
+    } else {
+      load(row);
+    }
+  }
+  // The rows from `row` on, zero beyond their ends (and for rows that are none).
+  __device__ __forceinline__ void get(int64_t row, Pack<T, V> (&p)[R][N][NV]) {
+    if constexpr (kBulk) {
+      if (!dead && !tc::mbar_wait(full + s, parity, kWaitNs)) {
+        dead = true;
+        if (status) atomicOr(status, SOAP_STATUS_TIMEOUT);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int m = 0; m < N; ++m)
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const int c = i * blockDim.x + threadIdx.x;
+            if ((FULL || c * V < width) && (R == 1 || row + r * step < rows)) {
+              p[r][m][i] = *reinterpret_cast<const Pack<T, V>*>(slot(s, r, m) + c * 16);
+            } else {
+#pragma unroll
+              for (int e = 0; e < V; ++e) p[r][m][i].v[e] = from_f32<T>(0.f);
+            }
+          }
+    } else {
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) p[0][m][i] = ahead[m][i];
+      load(row + step);
+    }
+  }
+  // After a point that all of the group's threads have reached since get(): the slots are free.
+  __device__ __forceinline__ void refill(int64_t row) {
+    if constexpr (kBulk) {
+      if (threadIdx.x == 0) request(row + DEPTH * R * step, s);
+      if (++s == DEPTH) {
+        s = 0;
+        parity ^= 1;
+      }
+    }
+  }
+  __device__ __forceinline__ void finish() const {
+    if (dead) {  // copies in flight land before the shared memory goes away: far above a copy's time
+      const uint64_t t0 = tc::globaltimer();
+      while (tc::globaltimer() - t0 < 10000000ull) {
+      }
+    }
+  }
+};
+
+// Elements 2 k and 2 k + 1 of a thread's packs as fp32.
+template <typename T, int V, int NV>
+__device__ __forceinline__ float2 values(const Pack<T, V> (&p)[NV], int k) {
+  if constexpr (V == 1)
+    return make_float2(to_f32(p[2 * k].v[0]), to_f32(p[2 * k + 1].v[0]));
+  else
+    return to_pair(p[2 * k / V].v + 2 * k % V);
+}
+
+// A row's results in pack i (V == 1: packs i and i + 1), rounded once.
+template <typename T, int V, bool FULL>
+__device__ __forceinline__ void put(T* row, int width, int i, const float2* v) {
+#pragma unroll
+  for (int j = 0; j < (V == 1 ? 2 : 1); ++j) {
+    const int c = ((i + j) * blockDim.x + threadIdx.x) * V;
+    if (!FULL && c >= width) break;
+    Pack<T, V> o;
+    if constexpr (V == 1) {
+      o.v[0] = from_f32<T>(j ? v[0].y : v[0].x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) from_pair(v[e / 2], o.v + e);
+    }
+    *reinterpret_cast<Pack<T, V>*>(row + c) = o;
+  }
+}
+
+// A thread's columns of a vector as fp32 pairs (`none` beyond the width, or everywhere without one).
+template <typename W, int V, int NV>
+__device__ __forceinline__ void columns(const W* w, float none, int width, float2 (&v)[NV * V / 2]) {
+#pragma unroll
+  for (int k = 0; k < NV * V; ++k) {
+    const int c = ((k / V) * blockDim.x + threadIdx.x) * V + k % V;
+    const float x = w && c < width ? to_f32(w[c]) : none;
+    if (k % 2)
+      v[k / 2].y = x;
+    else
+      v[k / 2].x = x;
+  }
+}
+
+// Sum over a one-row CTA's threads, for the kernels that do not hold a row.
+template <int N>
+__device__ __forceinline__ void block_sum(float (&v)[N], float* buf) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) buf[(threadIdx.x >> 5) * N + i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.f;
+  for (int j = 0; j < (int)blockDim.x / 32; ++j)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += buf[j * N + i];
+}
+
+// ---- launch choice -------------------------------------------------------------------------
+
+constexpr int kSms = 152;
+constexpr int kParts = 2 * kSms;  // most CTAs, and partial rows
+
+struct NormShape {
+  int nv, tx;  // accesses per thread and row, threads per row
+};
+
+// Threads for a row of `width` elements in accesses of v: a warp where 16 elements per thread are
+// enough, else the fewest that give a thread no more than `elems` elements, or more up to `most` where
+// the row needs it. nv = 0: too wide for that.
+NormShape norm_shape(int64_t width, int v, bool bulk, int elems, int most) {
+  const int64_t packs = (width + v - 1) / v;
+  for (int nv = v == 1 ? 2 : 1; nv * v <= 16; nv *= 2)
+    if (packs <= 32 * nv) return {nv, 32};
+  for (int e = elems; e <= most; e *= 2)
+    for (int tx = 64; tx <= threads_for(e, bulk); tx *= 2)
+      if (packs * v <= (int64_t)tx * e) return {e / v, tx};
+  return {0, 0};
+}
+
+// With few rows per SM a row's own time counts: 8 elements per thread and many threads. With many, rows
+// side by side in an SM hide each other's chains of sums: more elements per thread, so that more rows
+// fit (forward, 32768 x 8192 bf16: 258 us with 8, 260 with 16, 200 with 32).
+bool many_rows(int64_t rows) { return rows >= 16 * kSms; }
+
+int norm_threads(const NormShape& n, int v, bool bulk) { return n.tx >= 128 ? threads_for(n.nv * v, bulk) : 512; }
+
+// Rows per CTA: full CTAs, unless the rows would then not reach every SM.
+int norm_groups(int64_t rows, const NormShape& n, int v, bool bulk) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(norm_threads(n, v, bulk) / n.tx, (rows + kSms - 1) / kSms));
+}
+
+// CTAs: two per SM where one does not fill it.
+int norm_ctas(int64_t rows, const NormShape& n, int v, int ty) {
+  const int most = n.tx * ty <= 512 && n.nv * v <= 8 ? kParts : kSms;
+  return (int)std::min<int64_t>(most, (rows + ty - 1) / ty);
+}
+
+template <typename F>
+cudaError_t with_nv(int nv, F&& f) {
+  switch (nv) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    case 16: return f(std::integral_constant<int, 16>());
+    default: return f(std::integral_constant<int, 32>());
+  }
+}
+
+// f(elements per access) for rows whose addresses and lengths in bytes, ORed, are `bytes`: 16 bytes, else
+// 8, else 4, else an element.
+template <typename T, typename F>
+cudaError_t with_access(uintptr_t bytes, F&& f) {
+  if (bytes % 16 == 0) return f(std::integral_constant<int, 16 / sizeof(T)>());
+  if (bytes % 8 == 0) return f(std::integral_constant<int, 8 / sizeof(T)>());
+  if (sizeof(T) == 2 && bytes % 4 == 0) return f(std::integral_constant<int, sizeof(T) == 2 ? 2 : 1>());
+  return f(std::integral_constant<int, 1>());
+}
+
+// f(whether the row has exactly the group's elements): told apart for the widest accesses.
+template <int V, typename F>
+cudaError_t with_full(bool full, F&& f) {
+  if (V >= 4 && full) return f(std::integral_constant<bool, (V >= 4)>());
+  return f(std::integral_constant<bool, false>());
+}
+
+uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+// One bit per device on which the kernel has its shared-memory attribute.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& set) {
+  if (bytes <= 48 * 1024 - 4096) return cudaSuccess;  // beside the static part
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (set.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  if (e == cudaSuccess) set.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+// f(T(), W()) for an activation and a weight type.
+template <typename F>
+cudaError_t with_types(int32_t xt, int32_t wt, F&& f) {
+  if (xt == SOAP_F32) return f(float(), float());
+  if (xt == SOAP_BF16)
+    return wt == SOAP_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
+  return wt == SOAP_F32 ? f(__half(), float()) : f(__half(), __half());
+}
+
+bool bad_ptr(const void* p, size_t size) { return p && reinterpret_cast<uintptr_t>(p) % size; }
+
+bool bad_norm(int64_t rows, int64_t width, int32_t xt, const void* w, const void* b, int32_t wt) {
+  if (rows < 0 || width < 1 || rows > INT32_MAX || width > INT32_MAX) return true;
+  if (xt < SOAP_F32 || xt > SOAP_F16 || (wt != SOAP_F32 && wt != xt)) return true;
+  return bad_ptr(w, dtype_size(wt)) || bad_ptr(b, dtype_size(wt));
+}
+
+bool bad_rows(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t t) {
+  return rows > 0 && (!p || bad_ptr(p, dtype_size(t)) || ld < width);
+}
+
+}  // namespace
+}  // namespace soap

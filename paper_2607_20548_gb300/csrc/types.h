@@ -60,25 +60,24 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return from_bits(r);
 }
 
-// Two neighbouring elements to fp32 and back (round to nearest).
+// Two neighbouring elements (4-byte aligned, 16-bit ones) to fp32 and back (round to nearest).
 __device__ __forceinline__ float2 to_pair(const float* p) { return make_float2(p[0], p[1]); }
-__device__ __forceinline__ float2 to_pair(const __nv_bfloat16* p) {
-  return __bfloat1622float2(__nv_bfloat162(p[0], p[1]));
+__device__ __forceinline__ float2 to_pair(const __nv_bfloat16* p) {  // a bf16 is the upper half of its fp32
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-__device__ __forceinline__ float2 to_pair(const __half* p) { return __half22float2(__half2(p[0], p[1])); }
+__device__ __forceinline__ float2 to_pair(const __half* p) {
+  return __half22float2(*reinterpret_cast<const __half2*>(p));
+}
 __device__ __forceinline__ void from_pair(float2 v, float* p) {
   p[0] = v.x;
   p[1] = v.y;
 }
 __device__ __forceinline__ void from_pair(float2 v, __nv_bfloat16* p) {
-  const __nv_bfloat162 h = __float22bfloat162_rn(v);
-  p[0] = h.x;
-  p[1] = h.y;
+  *reinterpret_cast<__nv_bfloat162*>(p) = __float22bfloat162_rn(v);
 }
 __device__ __forceinline__ void from_pair(float2 v, __half* p) {
-  const __half2 h = __float22half2_rn(v);
-  p[0] = __low2half(h);
-  p[1] = __high2half(h);
+  *reinterpret_cast<__half2*>(p) = __float22half2_rn(v);
 }
 
 inline size_t dtype_size(int32_t t) { return t == 0 ? 4 : 2; }

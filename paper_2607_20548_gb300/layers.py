@@ -87,17 +87,20 @@ def _weights(name, x, weight, bias, width):
 
 
 def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-                       eps: float = 1e-5, stream=None):
+                       eps: float = 1e-5, status: Optional[torch.Tensor] = None, stream=None):
     """Layer norm over x's last dimension: (y, mean, rstd), with y of x's shape and type and the fp32
-    statistics of every row, which the backward pass takes. weight and bias: float32 or x's type."""
+    statistics of every row, which the backward pass takes. weight and bias: float32 or x's type.
+    status: an int32 CUDA word that SOAP_STATUS_TIMEOUT is ORed into."""
     name = "layer_norm_forward"
     dev = _operand(name, x)
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:
-            return layer_norm_forward(x, weight, bias, eps)
+            return layer_norm_forward(x, weight, bias, eps, status)
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"{name}: the normalised dimension is empty")
+    if status is not None:
+        _operand(name, status, torch.int32, dev)
     x, rows, ld = _rows(x)
     shape = x.shape
     width = shape[-1]
@@ -107,12 +110,13 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     _done(load_library().layer_norm_forward(
         rows, width, x.data_ptr(), ld, DTYPES[x.dtype], None if weight is None else weight.data_ptr(),
         None if bias is None else bias.data_ptr(), wt, eps, y.data_ptr(), width, mean.data_ptr(), rstd.data_ptr(),
-        _raw_stream(dev.index)), name)
+        None if status is None else status.data_ptr(), _raw_stream(dev.index)), name)
     return y, mean, rstd
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
-                        weight: Optional[torch.Tensor] = None, params: bool = True, stream=None):
+                        weight: Optional[torch.Tensor] = None, params: bool = True,
+                        status: Optional[torch.Tensor] = None, stream=None):
     """(dx, dweight, dbias) of layer_norm_forward from dy and its mean and rstd. dx has x's type;
     dweight and dbias are float32 (the optimizer's gradient type), or None without ``params``."""
     name = "layer_norm_backward"
@@ -121,11 +125,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:
-            return layer_norm_backward(dy, x, mean, rstd, weight, params)
+            return layer_norm_backward(dy, x, mean, rstd, weight, params, status)
     if dy.shape != x.shape:
         raise ValueError(f"{name}: dy and x have different shapes")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"{name}: the normalised dimension is empty")
+    if status is not None:
+        _operand(name, status, torch.int32, dev)
     x, rows, ld = _rows(x)
     dy, _, ld_dy = _rows(dy)
     width = x.shape[-1]
@@ -146,7 +152,8 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     _done(lib.layer_norm_backward(
         rows, width, dy.data_ptr(), ld_dy, x.data_ptr(), ld, DTYPES[x.dtype], mean.data_ptr(), rstd.data_ptr(),
         None if weight is None else weight.data_ptr(), wt, dx.data_ptr(), width, dw.data_ptr() if params else None,
-        db.data_ptr() if params else None, ws, ws_bytes, _raw_stream(dev.index)), name)
+        db.data_ptr() if params else None, ws, ws_bytes, None if status is None else status.data_ptr(),
+        _raw_stream(dev.index)), name)
     return dx, dw, db
 
 

@@ -135,9 +135,9 @@ def load_library(path: str = LIB_PATH):
         "muon_profile_end": (I32, [P, P, ctypes.POINTER(soap_kernel_stats), ctypes.POINTER(I32)]),
         "muon_orthogonalize_workspace_bytes": (SZ, [I32, I64, I64, I32]),
         "muon_orthogonalize": (I32, [I32, I64, I64, P, I64, I64, I32, P, I32, F, P, I64, I64, P, SZ, P, P]),
-        "layer_norm_forward": (I32, [I64, I64, P, I64, I32, P, P, I32, F, P, I64, P, P, P]),
+        "layer_norm_forward": (I32, [I64, I64, P, I64, I32, P, P, I32, F, P, I64, P, P, P, P]),
         "layer_norm_workspace_bytes": (SZ, [I64, I64]),
-        "layer_norm_backward": (I32, [I64, I64, P, I64, P, I64, I32, P, P, P, I32, P, I64, P, P, P, SZ, P]),
+        "layer_norm_backward": (I32, [I64, I64, P, I64, P, I64, I32, P, P, P, I32, P, I64, P, P, P, SZ, P, P]),
         "layer_route_workspace_bytes": (SZ, [I64, I32]),
         "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, P, SZ, P]),
         "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, P, I64, P]),

@@ -28,17 +28,17 @@ def test_every_declared_symbol_is_exported():
 def test_norm_refusals():
     f = _lib().layer_norm_forward
     ok = dict(rows=4, width=8, x=PTR, ld_x=8, x_type=1, w=PTR, b=PTR, w_type=0, eps=1e-5, y=PTR, ld_y=8, mean=PTR,
-              rstd=PTR)
+              rstd=PTR, status=None)
     for change in (dict(rows=-1), dict(rows=1 << 31), dict(width=0), dict(width=1 << 31), dict(x=None), dict(y=None),
                    dict(ld_x=7), dict(ld_y=7), dict(x_type=3), dict(x_type=-1), dict(w_type=2), dict(eps=-1.0),
-                   dict(eps=float("nan")), dict(x=PTR + 1), dict(mean=ODD), dict(w=ODD), dict(x_type=0, x=ODD)):
+                   dict(eps=float("nan")), dict(x=PTR + 1), dict(mean=ODD), dict(w=ODD), dict(x_type=0, x=ODD), dict(status=ODD)):
         assert f(*{**ok, **change}.values(), None) == 1, change
     assert f(*{**ok, "rows": 0, "x": None, "y": None}.values(), None) == 0
     g = _lib().layer_norm_backward
     need = _lib().layer_norm_workspace_bytes(4, 8)
     assert need >= 4 * 2 * 8 * 4 and _lib().layer_norm_workspace_bytes(-1, 8) == 0
     ok = dict(rows=4, width=8, dy=PTR, ld_dy=8, x=PTR, ld_x=8, x_type=1, mean=PTR, rstd=PTR, w=PTR, w_type=0, dx=PTR,
-              ld_dx=8, dw=PTR, db=PTR, ws=PTR, bytes=need)
+              ld_dx=8, dw=PTR, db=PTR, ws=PTR, bytes=need, status=None)
     for change in (dict(rows=-1), dict(width=0), dict(dy=None), dict(x=None), dict(dx=None), dict(mean=None),
                    dict(rstd=None), dict(ld_dx=7), dict(ld_dy=1), dict(ws=None), dict(bytes=need - 1), dict(ws=PTR + 4),
                    dict(dw=ODD), dict(w_type=2)):
