@@ -12,16 +12,16 @@ namespace {
 template <typename T, typename W, int V, int NV, int DEPTH, bool FULL>
 __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
     norm_fwd_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
-                    float* mean, float* rstd, int64_t rows, int width, int* status) {
+                    float* mean, float* rstd, int rows, int width, int* status) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 buf[2 * 32];
   __shared__ uint64_t full[kMaxGroups][DEPTH];
   constexpr int P = NV * V / 2, kPer = V == 1 ? 2 : 1;
-  using Feed = Rows<T, V, NV, 1, 1, DEPTH, FULL>;
+  using Feed = Rows<T, V, NV, 1, DEPTH, FULL>;
   const int lane = threadIdx.x & 31;
   Exchange ex{buf};
-  const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int step = gridDim.x * blockDim.y;
+  int row = blockIdx.x * blockDim.y + threadIdx.y;
   Feed in{{x}, {ld_x}, rows, step, width, smem + (size_t)threadIdx.y * blockDim.x * Feed::kRing, full[threadIdx.y], status};
   in.start(row);
   float2 w[P], b[P];
@@ -40,11 +40,11 @@ __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
   // whether this thread's element k is one of the row's
   auto has = [&](int k) { return ((k / V) * (int)blockDim.x + (int)threadIdx.x) * V + k % V < width; };
   for (; row < rows; row += step) {
-    Pack<T, V> raw[1][1][NV];
+    Pack<T, V> raw[1][NV];
     in.get(row, raw);
     float2 v[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = values(raw[0][0], i);
+    for (int i = 0; i < P; ++i) v[i] = values(raw[0], i);
     // sum and spread of the warp's elements about the warp's mean, then over the warps
     float2 acc = pair(0.f);
 #pragma unroll
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
 #pragma unroll
     for (int i = 0; i < P; ++i) v[i] = fma2(mul2(add2(v[i], pair(-mu)), pair(rs)), w[i], b[i]);
 #pragma unroll
-    for (int i = 0; i < NV; i += kPer) put<T, V, FULL>(y + row * ld_y, width, i, v + i * V / 2);
+    for (int i = 0; i < NV; i += kPer) put<T, V, FULL>(y + (int64_t)row * ld_y, width, i, v + i * V / 2);
   }
   in.finish();
 }
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kMaxThreads)
   __shared__ float buf[32];
   const int64_t row = blockIdx.x;
   const T* xr = x + row * ld_x;
-  T* yr = y + row * ld_y;
+  T* yr = y + (int64_t)row * ld_y;
   float s[1] = {0.f}, q[1] = {0.f};
   for (int64_t c = threadIdx.x; c < width; c += blockDim.x) s[0] += to_f32(xr[c]);
   block_sum(s, buf);
@@ -115,23 +115,24 @@ __global__ void __launch_bounds__(kMaxThreads)
 template <typename T, typename W, int V>
 cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W* w, const W* b, float eps, T* y,
                   int64_t ld_y, float* mean, float* rstd, int* status, cudaStream_t s) {
-  const NormShape n = norm_shape(width, V, V * sizeof(T) == 16, many_rows(rows) ? 32 : 8, 32);
+  constexpr bool kBulk = V * sizeof(T) == 16;
+  const NormShape n = norm_shape(width, V, kBulk, !many_rows(rows) ? 8 : kBulk ? 32 : 16, 32);
   if (n.nv == 0) {
     norm_fwd_wide_kernel<T, W><<<(unsigned)rows, kMaxThreads, 0, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, width);
     return cudaGetLastError();
   }
-  const int ty = norm_groups(rows, n, V, V * sizeof(T) == 16);
+  const int ty = norm_groups(rows, n, V, kBulk);
   const unsigned grid = (unsigned)norm_ctas(rows, n, V, ty);
   return with_nv(n.nv, [&](auto nv) {
     constexpr int NV = decltype(nv)::value, DEPTH = NV * V * sizeof(T) > 64 ? 3 : 4;
     if constexpr (NV * V <= 32 && NV * V > 1) {
-      const int smem = n.tx * ty * Rows<T, V, NV, 1, 1, DEPTH, false>::kRing;
+      const int smem = n.tx * ty * Rows<T, V, NV, 1, DEPTH, false>::kRing;
       return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
         static std::atomic<uint64_t> set{0};
         const auto kernel = norm_fwd_kernel<T, W, V, NV, DEPTH, decltype(full)::value>;
         const cudaError_t e = allow_smem(kernel, smem, set);
         if (e != cudaSuccess) return e;
-        kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, rows, (int)width, status);
+        kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, (int)rows, (int)width, status);
         return cudaGetLastError();
       });
     }

@@ -28,6 +28,7 @@ constexpr int kMaxThreads = 512;  // of the kernels for rows too wide to be held
 // registers): few registers, twice the threads.
 constexpr int threads_for(int elems, bool bulk) { return elems <= 8 && bulk ? 1024 : 512; }
 constexpr int kMaxGroups = 16;    // row groups of a CTA
+constexpr int64_t kMaxRows = INT32_MAX - 65536;  // a row index some steps further on stays an int
 constexpr uint64_t kWaitNs = 2000000000ull;
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -58,18 +59,16 @@ struct Exchange {
   }
 };
 
-// The rows of N matrices (x; or dy and x) for a row group, R rows at a time and DEPTH times ahead, NV packs
-// of V elements per thread and row.
-template <typename T, int V, int NV, int N, int R, int DEPTH, bool FULL>
+// The rows of N matrices (x; or x and dy) for a row group, up to DEPTH rows ahead, NV packs of V elements
+// per thread and row.
+template <typename T, int V, int NV, int N, int DEPTH, bool FULL>
 struct Rows {
   static constexpr bool kBulk = V * sizeof(T) == 16;  // a ring in shared memory; else registers
   static constexpr int kRowBytes = NV * 16;           // of the ring, per thread
-  static constexpr int kRing = kBulk ? DEPTH * R * N * kRowBytes : 0;  // bytes per thread
-  static_assert(kBulk || R == 1, "one row at a time in registers");
+  static constexpr int kRing = kBulk ? DEPTH * N * kRowBytes : 0;  // bytes per thread
   const T* base[N];
   int64_t ld[N];
-  int64_t rows, step;
-  int width;
+  int rows, step, width;
   uint8_t* ring;    // the group's: row slot q at q * blockDim.x * kRowBytes
   uint64_t* full;   // the group's barriers, one per stage
   int* status;
@@ -78,30 +77,23 @@ struct Rows {
   bool dead = false;  // a wait ran out: what follows is invalid, and waits for nothing
   Pack<T, V> ahead[kBulk ? 1 : N][kBulk ? 1 : NV];
 
-  __device__ __forceinline__ uint8_t* slot(int stage, int r, int n) const {
-    return ring + (size_t)((stage * R + r) * N + n) * blockDim.x * kRowBytes;
+  __device__ __forceinline__ uint8_t* slot(int stage, int n) const {
+    return ring + (size_t)(stage * N + n) * blockDim.x * kRowBytes;
   }
-  // One thread asks for the rows from `row` on (R of them, `step` apart) into a stage.
-  __device__ __forceinline__ void request(int64_t row, int stage) {
-    const uint32_t bytes = (uint32_t)width * sizeof(T);
-    int n = 0;
+  // One thread asks for a row into a stage.
+  __device__ __forceinline__ void request(int row, int stage) {
+    if (row >= rows) return;
+    const uint32_t bytes = (uint32_t)width * sizeof(T), bar = tc::smem_u32(full + stage);
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(N * bytes) : "memory");
 #pragma unroll
-    for (int r = 0; r < R; ++r) n += row + r * step < rows;
-    if (n == 0) return;
-    const uint32_t bar = tc::smem_u32(full + stage);
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * N * bytes) : "memory");
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (r < n)
-#pragma unroll
-        for (int m = 0; m < N; ++m)
-          asm volatile(
-              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                  tc::smem_u32(slot(stage, r, m))),
-              "l"(base[m] + (row + r * step) * ld[m]), "r"(bytes), "r"(bar)
-              : "memory");
+    for (int m = 0; m < N; ++m)
+      asm volatile(
+          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+              tc::smem_u32(slot(stage, m))),
+          "l"(base[m] + (int64_t)row * ld[m]), "r"(bytes), "r"(bar)
+          : "memory");
   }
-  __device__ __forceinline__ void load(int64_t row) {
+  __device__ __forceinline__ void load(int row) {
     if constexpr (!kBulk) {
 #pragma unroll
       for (int m = 0; m < N; ++m)
@@ -109,7 +101,7 @@ struct Rows {
         for (int i = 0; i < NV; ++i) {
           const int c = (i * blockDim.x + threadIdx.x) * V;
           if (row < rows && c < width) {
-            ahead[m][i] = *reinterpret_cast<const Pack<T, V>*>(base[m] + row * ld[m] + c);
+            ahead[m][i] = *reinterpret_cast<const Pack<T, V>*>(base[m] + (int64_t)row * ld[m] + c);
           } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) ahead[m][i].v[e] = from_f32<T>(0.f);
@@ -118,51 +110,46 @@ struct Rows {
     }
   }
   // Before the first row: called by all threads of the CTA.
-  __device__ __forceinline__ void start(int64_t row) {
+  __device__ __forceinline__ void start(int row) {
     if constexpr (kBulk) {
       if (threadIdx.x == 0) {
         for (int q = 0; q < DEPTH; ++q) tc::mbar_init(full + q, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int q = 0; q < DEPTH; ++q) request(row + q * R * step, q);
+        for (int q = 0; q < DEPTH; ++q) request(row + q * step, q);
       }
       __syncthreads();
     } else {
       load(row);
     }
   }
-  // The rows from `row` on, zero beyond their ends (and for rows that are none).
-  __device__ __forceinline__ void get(int64_t row, Pack<T, V> (&p)[R][N][NV]) {
+  // The row, zero beyond its end.
+  __device__ __forceinline__ void get(int row, Pack<T, V> (&p)[N][NV]) {
     if constexpr (kBulk) {
       if (!dead && !tc::mbar_wait(full + s, parity, kWaitNs)) {
         dead = true;
         if (status) atomicOr(status, SOAP_STATUS_TIMEOUT);
       }
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int m = 0; m < N; ++m)
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const int c = i * blockDim.x + threadIdx.x;
-            if ((FULL || c * V < width) && (R == 1 || row + r * step < rows)) {
-              p[r][m][i] = *reinterpret_cast<const Pack<T, V>*>(slot(s, r, m) + c * 16);
-            } else {
-#pragma unroll
-              for (int e = 0; e < V; ++e) p[r][m][i].v[e] = from_f32<T>(0.f);
-            }
-          }
-    } else {
-#pragma unroll
-      for (int m = 0; m < N; ++m)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) p[0][m][i] = ahead[m][i];
-      load(row + step);
     }
+#pragma unroll
+    for (int m = 0; m < N; ++m)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = i * blockDim.x + threadIdx.x;
+        if constexpr (!kBulk) {
+          p[m][i] = ahead[m][i];
+        } else if (FULL || c * V < width) {
+          p[m][i] = *reinterpret_cast<const Pack<T, V>*>(slot(s, m) + c * 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) p[m][i].v[e] = from_f32<T>(0.f);
+        }
+      }
+    load(row + step);
   }
   // After a point that all of the group's threads have reached since get(): the slots are free.
-  __device__ __forceinline__ void refill(int64_t row) {
+  __device__ __forceinline__ void refill(int row) {
     if constexpr (kBulk) {
-      if (threadIdx.x == 0) request(row + DEPTH * R * step, s);
+      if (threadIdx.x == 0) request(row + DEPTH * step, s);
       if (++s == DEPTH) {
         s = 0;
         parity ^= 1;
@@ -260,7 +247,8 @@ NormShape norm_shape(int64_t width, int v, bool bulk, int elems, int most) {
 
 // With few rows per SM a row's own time counts: 8 elements per thread and many threads. With many, rows
 // side by side in an SM hide each other's chains of sums: more elements per thread, so that more rows
-// fit (forward, 32768 x 8192 bf16: 258 us with 8, 260 with 16, 200 with 32).
+// fit (forward, 32768 x 8192 bf16: 258 us with 8, 260 with 16, 200 with 32; backward, whose columns'
+// sums take registers too, 495, 472 and spills).
 bool many_rows(int64_t rows) { return rows >= 16 * kSms; }
 
 int norm_threads(const NormShape& n, int v, bool bulk) { return n.tx >= 128 ? threads_for(n.nv * v, bulk) : 512; }
@@ -333,7 +321,7 @@ cudaError_t with_types(int32_t xt, int32_t wt, F&& f) {
 bool bad_ptr(const void* p, size_t size) { return p && reinterpret_cast<uintptr_t>(p) % size; }
 
 bool bad_norm(int64_t rows, int64_t width, int32_t xt, const void* w, const void* b, int32_t wt) {
-  if (rows < 0 || width < 1 || rows > INT32_MAX || width > INT32_MAX) return true;
+  if (rows < 0 || width < 1 || rows > kMaxRows || width > INT32_MAX) return true;
   if (xt < SOAP_F32 || xt > SOAP_F16 || (wt != SOAP_F32 && wt != xt)) return true;
   return bad_ptr(w, dtype_size(wt)) || bad_ptr(b, dtype_size(wt));
 }

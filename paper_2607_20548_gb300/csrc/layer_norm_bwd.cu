@@ -13,28 +13,29 @@ namespace {
 // norm_cols_kernel adds the partial rows in order (no atomics: the result does not depend on
 // which CTA finishes first).
 
-// R rows of a group go through an iteration side by side, so that one's chain of sums and exchanges
-// fills the other's waits. A thread keeps a row's packs and converts them twice. kSmemW: weights in
-// shared memory (fp32, at their columns), where registers would not hold them beside both sums.
-template <typename T, typename W, int V, int NV, int R, int DEPTH, bool FULL>
+// A thread keeps its row's packs and converts them twice. Weights that registers would not hold beside
+// both sums (more than 16 elements per thread) are in shared memory. (Two rows per iteration spilled
+// registers: 360 us in place of 258 at 32768 x 8192.)
+template <typename T, typename W, int V, int NV, int DEPTH, bool FULL>
 __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
     norm_bwd_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
-                    const W* weight, T* dx, int64_t ld_dx, float* part, int64_t rows, int width,
+                    const W* weight, T* dx, int64_t ld_dx, float* part, int rows, int width,
                     int* status) {
   extern __shared__ __align__(16) uint8_t smem[];  // the rings (and weights); afterwards the groups' column sums
-  __shared__ float4 buf[2 * 32];
+  __shared__ float2 buf[2 * 32];
   __shared__ uint64_t full[kMaxGroups][DEPTH];
   constexpr int E = NV * V, P = E / 2, kPer = V == 1 ? 2 : 1;
   constexpr bool kSmemW = E > 16;
-  using Feed = Rows<T, V, NV, 2, R, DEPTH, FULL>;
+  using Feed = Rows<T, V, NV, 2, DEPTH, FULL>;
   const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
   float2* const weights = reinterpret_cast<float2*>(smem + (size_t)threads * Feed::kRing);  // [P][blockDim.x]
-  const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int step = gridDim.x * blockDim.y;
+  int row = blockIdx.x * blockDim.y + threadIdx.y;
   Feed in{{x, dy},    {ld_x, ld_dy}, rows,
           step,       width,         smem + (size_t)threadIdx.y * blockDim.x * Feed::kRing,
           full[threadIdx.y], status};
   in.start(row);
+  Exchange ex{buf};
   float2 w[kSmemW ? 1 : P], aw[P], ab[P];
   if constexpr (kSmemW) {
     if (threadIdx.y == 0) {
@@ -57,91 +58,56 @@ __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
       return w[k];
   };
   const float inv = 1.f / (float)width;
-  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  float mu[R], rs[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    mu[r] = rs[r] = 0.f;
-    if (row + r * step < rows) {
-      mu[r] = mean[row + r * step];
-      rs[r] = rstd[row + r * step];
-    }
+  float mu = 0.f, rs = 0.f;
+  if (row < rows) {
+    mu = mean[row];
+    rs = rstd[row];
   }
-  int half = 0;
-  for (; row < rows; row += R * step) {
-    float mu_next[R], rs_next[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t next = row + (R + r) * step;
-      mu_next[r] = rs_next[r] = 0.f;
-      if (next < rows) {
-        mu_next[r] = mean[next];
-        rs_next[r] = rstd[next];
-      }
+  while (row < rows) {
+    const int next = row + step;
+    float mu_next = 0.f, rs_next = 0.f;
+    if (next < rows) {
+      mu_next = mean[next];
+      rs_next = rstd[next];
     }
-    Pack<T, V> p[R][2][NV];  // x, dy
+    Pack<T, V> p[2][NV];  // x, dy
     in.get(row, p);
-    float sum[R][2];
+    // beyond the row's end dy is zero, so whatever xh is there counts nowhere
+    float2 a0 = pair(0.f), a1 = pair(0.f);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      // beyond the row's end dy is zero, so whatever xh is there counts nowhere
-      float2 a0 = pair(0.f), a1 = pair(0.f);
-#pragma unroll
-      for (int k = 0; k < P; ++k) {
-        const float2 xh = mul2(add2(values(p[r][0], k), pair(-mu[r])), pair(rs[r]));
-        float2 g = values(p[r][1], k);
-        aw[k] = fma2(g, xh, aw[k]);
-        ab[k] = add2(ab[k], g);
-        g = mul2(g, weight_of(k));
-        a0 = add2(a0, g);
-        a1 = fma2(g, xh, a1);
-      }
-      sum[r][0] = a0.x + a0.y;
-      sum[r][1] = a1.x + a1.y;
+    for (int k = 0; k < P; ++k) {
+      const float2 xh = mul2(add2(values(p[0], k), pair(-mu)), pair(rs));
+      float2 g = values(p[1], k);
+      aw[k] = fma2(g, xh, aw[k]);
+      ab[k] = add2(ab[k], g);
+      g = mul2(g, weight_of(k));
+      a0 = add2(a0, g);
+      a1 = fma2(g, xh, a1);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-      for (int r = 0; r < 2 * R; ++r) sum[r / 2][r % 2] += __shfl_xor_sync(0xffffffffu, sum[r / 2][r % 2], o);
-    if (warps > 1) {  // the halves of the buffer in turn, as in Exchange
-      float4* to = buf + (half * blockDim.y + threadIdx.y) * warps;
-      half ^= 1;
-      if (lane == 0) to[threadIdx.x >> 5] = make_float4(sum[0][0], sum[0][1], sum[R - 1][0], sum[R - 1][1]);
-      group_barrier();
-      const float4 o = lane < warps ? to[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
-      sum[R - 1][0] = o.z;
-      sum[R - 1][1] = o.w;
-      sum[0][0] = o.x;
-      sum[0][1] = o.y;
-#pragma unroll
-      for (int q = 16; q > 0; q >>= 1)
-#pragma unroll
-        for (int r = 0; r < 2 * R; ++r) sum[r / 2][r % 2] += __shfl_xor_sync(0xffffffffu, sum[r / 2][r % 2], q);
+    float s0 = warp_sum(a0.x + a0.y), s1 = warp_sum(a1.x + a1.y);
+    if (blockDim.x > 32) {
+      const float2 o = ex.all(s0, s1);
+      s0 = warp_sum(o.x);
+      s1 = warp_sum(o.y);
     } else {
       __syncwarp();
     }
     in.refill(row);
+    const float2 m1 = pair(-s0 * inv * rs), m2 = pair(-s1 * inv * rs);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t here = row + r * step;
-      if (here < rows) {
-        const float2 m1 = pair(-sum[r][0] * inv * rs[r]), m2 = pair(-sum[r][1] * inv * rs[r]);
-        T* to = dx + here * ld_dx;
+    for (int i = 0; i < NV; i += kPer) {
+      float2 g[kPer * V / 2];
 #pragma unroll
-        for (int i = 0; i < NV; i += kPer) {
-          float2 g[kPer * V / 2];
-#pragma unroll
-          for (int j = 0; j < kPer * V / 2; ++j) {
-            const int k = i * V / 2 + j;
-            const float2 xh = mul2(add2(values(p[r][0], k), pair(-mu[r])), pair(rs[r]));
-            g[j] = fma2(xh, m2, fma2(mul2(values(p[r][1], k), weight_of(k)), pair(rs[r]), m1));
-          }
-          put<T, V, FULL>(to, width, i, g);
-        }
+      for (int j = 0; j < kPer * V / 2; ++j) {
+        const int k = i * V / 2 + j;
+        const float2 xh = mul2(add2(values(p[0], k), pair(-mu)), pair(rs));
+        g[j] = fma2(xh, m2, fma2(mul2(values(p[1], k), weight_of(k)), pair(rs), m1));
       }
-      mu[r] = mu_next[r];
-      rs[r] = rs_next[r];
+      put<T, V, FULL>(dx + (int64_t)row * ld_dx, width, i, g);
     }
+    row = next;
+    mu = mu_next;
+    rs = rs_next;
   }
   in.finish();
   if (!part) return;
@@ -231,7 +197,8 @@ template <typename T, typename W, int V>
 cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x,
                   const float* mean, const float* rstd, const W* w, T* dx, int64_t ld_dx, float* dw, float* db,
                   float* part, int* status, cudaStream_t s) {
-  const NormShape n = norm_shape(width, V, V * sizeof(T) == 16, many_rows(rows) ? 16 : 8, sizeof(T) == 2 ? 32 : 16);
+  constexpr bool kBulk = V * sizeof(T) == 16;
+  const NormShape n = norm_shape(width, V, kBulk, kBulk && many_rows(rows) ? 16 : 8, kBulk && sizeof(T) == 2 ? 32 : 16);
   float* p = dw || db ? part : nullptr;
   int parts = (int)std::min<int64_t>(kSms, rows);
   cudaError_t e;
@@ -243,25 +210,22 @@ cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const
                                                                      width);
     e = cudaGetLastError();
   } else {
-    const int ty = norm_groups(rows, n, V, V * sizeof(T) == 16);
+    const int ty = norm_groups(rows, n, V, kBulk);
     parts = norm_ctas(rows, n, V, ty);
     e = with_nv(n.nv, [&](auto nv) {
       constexpr int NV = decltype(nv)::value, E = NV * V;
-      if constexpr (E <= (sizeof(T) == 2 ? 32 : 16) && E > 1) {
-        // two rows at a time where a CTA's threads have registers for them; at most 192 KB of rows
-        constexpr bool kBulk = V * sizeof(T) == 16;
-        constexpr int R = kBulk && E == 16 && sizeof(T) == 2 ? 2 : 1;
-        constexpr int kStage = threads_for(E, kBulk) * E * (int)sizeof(T) * 2 * R;
-        constexpr int DEPTH = E > 16 ? 2 : std::min(4, 192 * 1024 / kStage);
+      if constexpr (E <= (kBulk && sizeof(T) == 2 ? 32 : 16) && E > 1) {
+        constexpr int kStage = threads_for(E, kBulk) * E * (int)sizeof(T) * 2;
+        constexpr int DEPTH = E > 16 ? 2 : std::min(4, 192 * 1024 / kStage);  // at most 192 KB of rows
         const int threads = n.tx * ty;
-        const int ring = threads * Rows<T, V, NV, 2, R, DEPTH, false>::kRing;
+        const int ring = threads * Rows<T, V, NV, 2, DEPTH, false>::kRing;
         const int smem = std::max(ring + (E > 16 ? n.tx * E * 4 : 0), threads * E * 4);
         return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
           static std::atomic<uint64_t> set{0};
-          const auto kernel = norm_bwd_kernel<T, W, V, NV, R, DEPTH, decltype(full)::value>;
+          const auto kernel = norm_bwd_kernel<T, W, V, NV, DEPTH, decltype(full)::value>;
           const cudaError_t ae = allow_smem(kernel, smem, set);
           if (ae != cudaSuccess) return ae;
-          kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, rows, (int)width,
+          kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, (int)rows, (int)width,
                                                      status);
           return cudaGetLastError();
         });
@@ -302,7 +266,7 @@ using namespace soap;
 extern "C" {
 
 size_t layer_norm_workspace_bytes(int64_t rows, int64_t width) {
-  if (rows <= 0 || width <= 0 || rows > INT32_MAX || width > INT32_MAX) return 0;
+  if (rows <= 0 || width <= 0 || rows > kMaxRows || width > INT32_MAX) return 0;
   return (size_t)std::min<int64_t>(kParts, rows) * 2 * (size_t)width * sizeof(float);
 }
 
