@@ -22,42 +22,18 @@
 
 #include "../../include/layer.h"
 #include "profile.h"
-#include "types.h"
+#include "route.h"
 
 namespace soap {
 namespace {
 
+using namespace route;
+
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxExperts = 1024;
-constexpr int kCluster = 8;
-constexpr int kMaxCtas = 152 * 4;          // a multiple of kCluster
+constexpr int kMaxCtas = kCluster * kMaxParts;
 constexpr int kMaxK = 32;
-
-// Keys in the order of the logits. A NaN's is above +inf's: adding 0 makes every NaN the positive one
-// (and -0 a +0). 0 stands for "none".
-constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyInf = 0xff800000u;
-__device__ __forceinline__ uint32_t order_key(float z) {
-  const uint32_t u = __float_as_uint(z + 0.f);
-  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) {
-  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-}
-
-// 16-bit logits differ in the upper 19 bits of their fp32 key (their 13 low mantissa bits are zero, in a
-// negative one's key ones): the complemented index goes below.
-constexpr uint32_t kLow = 0x1fffu;
-__device__ __forceinline__ uint32_t pack_key(uint32_t key, int idx) { return (key & ~kLow) | (kLow - (uint32_t)idx); }
-__device__ __forceinline__ uint32_t unpack_key(uint32_t b) { return b & 0x80000000u ? b & ~kLow : b | kLow; }
-__device__ __forceinline__ int packed_index(uint32_t b) { return (int)(kLow - (b & kLow)); }
-
-// e^x for x <= 0: one multiplication and the hardware's 2^x (relative error 2^-22 and |x| 2^-24).
-__device__ __forceinline__ float exp_neg(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
-  return r;
-}
 
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
@@ -119,56 +95,17 @@ struct Row {
   }
 };
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
-// The word at p's place in the shared memory of the cluster's CTA `rank`.
-__device__ __forceinline__ uint32_t peer_word(const void* p, uint32_t rank) {
-  const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(p));
-  uint32_t r, v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
-  return v;
-}
-
-struct Totals {
-  int32_t* counts;
-  int32_t* live;
-  float *mean_probs, *loss;
-  float coef;
-};
-
-// The loss from sum_e counts_e mean_e, summed over a CTA in a fixed order.
-__device__ __forceinline__ double block_sum(double v, double* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.0;
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) v += red[w];
-  return v;
-}
-
 template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
-    route_fwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
-                     int normalize, int32_t* indices, float* gates, float2* stats, float* part_p, int* part_c, Totals out,
-                     bool vec, int* status) {
+    route_fwd_kernel(const Forward a, const Totals out, const bool vec) {
   constexpr bool kPacked = sizeof(T) == 2;
   constexpr bool kSorted = NE <= 8;
   constexpr int kRec = kMaxK / G;
   using R = Row<T, G, NE, V>;
+  const T* const logits = static_cast<const T*>(a.logits);
+  const int64_t ld = a.ld, tokens = a.tokens;
+  const uint8_t* const mask = a.mask;
+  const int experts = a.experts, k = a.k;
   extern __shared__ float shared[];       // [warps][experts] column sums (the first row: the CTA's) ...
   int* counts = reinterpret_cast<int*>(shared + kWarps * experts);  // ... [experts + 1]: choices, tokens counted
   __shared__ double red[kWarps + 1];
@@ -245,10 +182,10 @@ __global__ void __launch_bounds__(kThreads)
     if (bad) {
 #pragma unroll
       for (int i = 0; i < NE; ++i) acc[i] = NAN;
-      if (status && lane == 0) atomicOr(status, SOAP_STATUS_NONFINITE);
+      if (a.status && lane == 0) atomicOr(a.status, SOAP_STATUS_NONFINITE);
     }
     seen += counted || bad;
-    if (stats && lane == 0 && t < tokens) stats[t] = bad ? make_float2(NAN, NAN) : make_float2(most, counted ? inv : 0.f);
+    if (a.stats && lane == 0 && t < tokens) a.stats[t] = bad ? make_float2(NAN, NAN) : make_float2(most, counted ? inv : 0.f);
     // k times the largest key; what it is stays with lane r of the group
     uint32_t my_key[kRec];
 #pragma unroll
@@ -295,7 +232,7 @@ __global__ void __launch_bounds__(kThreads)
       total += my_gate[j];
       if (some) atomicAdd(&counts[my_idx[j]], 1);
     }
-    if (normalize) {
+    if (a.normalize) {
       total = group_sum<G>(total);
       if (total > 0.f)
 #pragma unroll
@@ -305,8 +242,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
       for (int j = 0; j < kRec; ++j)
         if (j * G + lane < k) {
-          indices[t * k + j * G + lane] = my_idx[j];
-          gates[t * k + j * G + lane] = bad ? NAN : my_gate[j];
+          a.indices[t * k + j * G + lane] = my_idx[j];
+          a.gates[t * k + j * G + lane] = bad ? NAN : my_gate[j];
         }
     if (!kPacked) __syncwarp();  // the choices have been read
   }
@@ -320,54 +257,7 @@ __global__ void __launch_bounds__(kThreads)
     const int c = R::at(lane, i);
     if (threadIdx.x % 32 < G && c < experts) shared[warp * experts + c] = v;
   }
-  __syncthreads();
-  for (int c = threadIdx.x; c < experts; c += kThreads) {
-    float v = shared[c];
-    for (int w = 1; w < kWarps; ++w) v += shared[w * experts + c];
-    shared[c] = v;
-  }
-  // the cluster's CTAs in order, each CTA some of the columns
-  cluster_sync();
-  const uint32_t rank = cluster_rank(), size = cluster_size();
-  const bool alone = gridDim.x == size;  // one cluster: the totals are complete
-  const int64_t part = blockIdx.x / size;
-  int n = 0;
-  for (uint32_t q = 0; q < size; ++q) n += (int)peer_word(&counts[experts], q);
-  double dot = 0.0;
-  for (int c = rank * kThreads + threadIdx.x; c < experts; c += size * kThreads) {
-    float v = 0.f;
-    int cnt = 0;
-    for (uint32_t q = 0; q < size; ++q) {
-      v += __uint_as_float(peer_word(&shared[c], q));
-      cnt += (int)peer_word(&counts[c], q);
-    }
-    if (alone) {
-      const double mean = n > 0 ? (double)v / n : 0.0;
-      out.counts[c] = cnt;
-      if (out.mean_probs) out.mean_probs[c] = (float)mean;
-      dot += (double)cnt * mean;
-    } else {
-      part_p[part * experts + c] = v;
-      part_c[part * (experts + 1) + c] = cnt;
-    }
-  }
-  if (!alone) {
-    if (rank == 0 && threadIdx.x == 0) part_c[part * (experts + 1) + experts] = n;
-  } else {
-    dot = block_sum(dot, red);
-    if (threadIdx.x == 0) red[kWarps] = dot;
-    __syncthreads();
-  }
-  cluster_sync();
-  if (alone && rank == 0 && threadIdx.x == 0) {
-    dot = 0.0;
-    for (uint32_t q = 0; q < size; ++q)
-      dot += __hiloint2double((int)peer_word(reinterpret_cast<const uint32_t*>(&red[kWarps]) + 1, q),
-                              (int)peer_word(&red[kWarps], q));
-    *out.live = n;
-    *out.loss = n > 0 ? (float)((double)out.coef * experts / ((double)k * n) * dot) : 0.f;
-  }
-  if (alone) cluster_sync();  // the first CTA has read the others
+  finish_columns<kWarps>(shared, counts, red, experts, k, a.part_p, a.part_c, out);
 }
 
 // Adds the clusters' partial rows in a fixed order; the loss. One CTA of 1024 threads: a warp takes 32
@@ -423,19 +313,24 @@ __global__ void __launch_bounds__(1024)
 
 template <typename T, int G, int NE, int V>
 __global__ void __launch_bounds__(kThreads)
-    route_bwd_kernel(const T* logits, int64_t ld, const uint8_t* mask, int64_t tokens, int experts, int k,
-                     int normalize, double scale, const int32_t* indices, const int32_t* counts, const int32_t* live_n,
-                     const float2* stats, const float* dgates, T* dlogits, int64_t ld_d, bool vec) {
+    route_bwd_kernel(const Backward a, const bool vec) {
   constexpr int kRec = kMaxK / G;
   using R = Row<T, G, NE, V>;
+  const T* const logits = static_cast<const T*>(a.logits);
+  T* const dlogits = static_cast<T*>(a.dlogits);
+  const int64_t ld = a.ld, ld_d = a.ld_d, tokens = a.tokens;
+  const uint8_t* const mask = a.mask;
+  const int32_t *const indices = a.indices, *const counts = a.counts;
+  const float* const dgates = a.dgates;
+  const int experts = a.experts, k = a.k;
   const int lane = threadIdx.x % G;
   const int64_t groups = (int64_t)gridDim.x * (kThreads / G);
   int64_t t = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
   R row;
   bool live = t < tokens && (!mask || mask[t] != 0);
   if (live) row.load(logits + t * ld, experts, lane, vec);
-  const int n = *live_n;
-  const float per = n > 0 ? (float)(scale / ((double)n * n)) : 0.f;
+  const int n = *a.live;
+  const float per = n > 0 ? (float)(a.scale / ((double)n * n)) : 0.f;
   float up[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
@@ -446,7 +341,7 @@ __global__ void __launch_bounds__(kThreads)
     const bool here = live;
     float z[NE];
     row.values(here, experts, lane, z);
-    const float2 st = here ? stats[t] : make_float2(0.f, 0.f);  // the largest logit, 1 / sum of e^(z - largest)
+    const float2 st = here ? a.stats[t] : make_float2(0.f, 0.f);  // the largest logit, 1 / sum of e^(z - largest)
     const bool bad = st.y != st.y;
     // the gates' gradient at the chosen logits: lane r holds choices r, r + G, ...
     int at[kRec];
@@ -457,11 +352,11 @@ __global__ void __launch_bounds__(kThreads)
       d[j] = pc[j] = 0.f;
       const int r = j * G + lane;
       if (dgates && here && r < k) {
-        const int a = indices[t * k + r];
-        if (a >= 0 && a < experts) {
-          at[j] = a;
+        const int c = indices[t * k + r];
+        if (c >= 0 && c < experts) {
+          at[j] = c;
           d[j] = dgates[t * k + r];
-          pc[j] = exp_neg(to_f32(logits[t * ld + a]) - st.x) * st.y;
+          pc[j] = exp_neg(to_f32(logits[t * ld + c]) - st.x) * st.y;
           s += pc[j];
           dot = fmaf(d[j], pc[j], dot);
         }
@@ -469,7 +364,7 @@ __global__ void __launch_bounds__(kThreads)
     }
     live = t + groups < tokens && (!mask || mask[t + groups] != 0);
     if (live) row.load(logits + (t + groups) * ld, experts, lane, vec);  // the next token's
-    if (dgates && normalize) {
+    if (dgates && a.normalize) {
       // gate_r = p_r / s: d p_r = (d gate_r - sum_j d gate_j gate_j) / s, whose sum with the p_r is zero
       s = group_sum<G>(s);
       dot = group_sum<G>(dot) / s;
@@ -606,30 +501,38 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
       workspace_bytes < layer_route_workspace_bytes(tokens, experts))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
-  int cluster;
-  const int ctas = ctas_for(tokens, experts, &cluster), parts = ctas / cluster;
+  const bool tiles = tile_fits(tokens, experts, k, type);
+  int cluster = kCluster;
+  const int ctas = tiles ? tile_forward_ctas(tokens, experts, k, type) : ctas_for(tokens, experts, &cluster);
+  const int parts = ctas / cluster;
   float* part_p = static_cast<float*>(workspace);
   int* part_c = reinterpret_cast<int*>(part_p + (size_t)parts * experts);
   const Totals out{counts, live, mean_probs, loss, coef};
+  const Forward f{logits, ld, mask, tokens, experts, k, normalize, indices, gates, reinterpret_cast<float2*>(stats),
+                  part_p, part_c, status};
   const double n = (double)tokens * experts;
   ProfScope prof(kFamElementwise, 6.0 * n, n * dtype_size(type) + 8.0 * tokens * k, s);
   cudaLaunchAttribute attr;
   cudaLaunchConfig_t cfg{};
-  cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.dynamicSmemBytes = (size_t)((kWarps + 1) * experts + 1) * 4;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaError_t e = with_row<1>(type, experts, logits, ld, nullptr, 0, [&](auto t, auto g, auto ne, auto v, bool vec) {
-    using T = decltype(t);
-    return cudaLaunchKernelEx(&cfg, route_fwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value>,
-                              static_cast<const T*>(logits), ld, mask, tokens, (int)experts, (int)k, (int)normalize,
-                              indices, gates, reinterpret_cast<float2*>(stats), part_p, part_c, out, vec, (int*)status);
-  });
+  cudaError_t e;
+  if (tiles) {
+    e = tile_forward(f, out, type, s);
+  } else {
+    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.dynamicSmemBytes = (size_t)((kWarps + 1) * experts + 1) * 4;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    e = with_row<1>(type, experts, logits, ld, nullptr, 0, [&](auto t, auto g, auto ne, auto v, bool vec) {
+      using T = decltype(t);
+      return cudaLaunchKernelEx(&cfg, route_fwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value>,
+                                f, out, vec);
+    });
+  }
   if (e == cudaSuccess && parts > 1) {
     cfg.gridDim = dim3(1);
     cfg.blockDim = dim3(1024);
@@ -652,19 +555,22 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
       (dgates && (bad_ptr(dgates, 4) || bad_ptr(indices, 4))))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
-  const int64_t want = (tokens + tokens_per_cta(experts) - 1) / tokens_per_cta(experts);
-  const int ctas = (int)std::min<int64_t>(kMaxCtas, want);
   const double n = (double)tokens * experts;
-  const double scale = (double)coef * dloss * experts / k;
+  const Backward b{logits, ld, mask, tokens, experts, k, normalize, (double)coef * dloss * experts / k, indices,
+                   reinterpret_cast<const float2*>(stats), counts, live, dgates, dlogits, ld_d};
   ProfScope prof(kFamElementwise, 6.0 * n, 2.0 * n * dtype_size(type) + 12.0 * tokens * k, s);
-  const cudaError_t e =
-      with_row<2>(type, experts, logits, ld, dlogits, ld_d, [&](auto t, auto g, auto ne, auto v, bool vec) {
-        using T = decltype(t);
-        route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value><<<ctas, kThreads, 0, s>>>(
-            static_cast<const T*>(logits), ld, mask, tokens, experts, k, normalize, scale, indices, counts, live,
-            reinterpret_cast<const float2*>(stats), dgates, static_cast<T*>(dlogits), ld_d, vec);
-        return cudaGetLastError();
-      });
+  cudaError_t e;
+  if (tile_fits(tokens, experts, k, type)) {
+    e = tile_backward(b, type, s);
+  } else {
+    const int64_t want = (tokens + tokens_per_cta(experts) - 1) / tokens_per_cta(experts);
+    const int ctas = (int)std::min<int64_t>(kMaxCtas, want);
+    e = with_row<2>(type, experts, logits, ld, dlogits, ld_d, [&](auto t, auto g, auto ne, auto v, bool vec) {
+      using T = decltype(t);
+      route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value><<<ctas, kThreads, 0, s>>>(b, vec);
+      return cudaGetLastError();
+    });
+  }
   return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;
 }
 

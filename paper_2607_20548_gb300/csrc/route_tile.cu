@@ -1,0 +1,594 @@
+// Routing of many tokens (include/layer.h): a thread per token.
+//
+// A warp brings 32 rows of logits into shared memory and each lane goes through its own row, 16 bytes
+// at a time; rows lie an odd number of 16-byte units apart, so that neither the lanes' walks along their
+// rows nor the sums down the columns meet in a bank. The k largest are kept by insertion: one
+// compare-exchange (a minimum and a maximum) per place and logit, nothing exchanged between lanes. A
+// 16-bit logit's key holds its index; fp32 values go without theirs, and a second look at the row marks
+// what reaches the k-th value, whose places follow from the list. Probabilities are summed down the
+// columns with a lane per 32-bit word, the sums staying in registers over all of a warp's tiles.
+//
+// What bounds it is instructions: with k = 6 and 127 fp32 logits about 100 per token, where a group of
+// lanes per token (route.cu, few tokens and long rows) takes 440, most of them for exchanges.
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "route.h"
+#include "soap_internal.h"
+
+namespace soap {
+namespace route {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kMaxList = 8;               // places of a thread's list
+constexpr int kMaxWords = 6 * 32;         // 32-bit words of a row
+constexpr int64_t kFewTokens = 152 * 96;  // below: an SM would have only a few warps
+constexpr int kSmemPerSm = 228 * 1024;
+
+int row_bytes(int experts, int32_t type) { return experts * (int)dtype_size(type); }
+__host__ __device__ __forceinline__ int pitch_of(int bytes) { return 16 * (((bytes + 15) / 16) | 1); }
+
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// f(row, unit) for the `units` units of each row in `rows` (a bit per row), spread over a warp's lanes.
+template <typename F>
+__device__ __forceinline__ void each_unit(uint32_t rows, int units, int lane, F&& f) {
+  const int drow = 32 / units, dunit = 32 - drow * units;
+  int row = lane / units, unit = lane - row * units;
+  while (row < 32) {
+    if (rows >> row & 1) f(row, unit);
+    row += drow;
+    unit += dunit;
+    if (unit >= units) {
+      unit -= units;
+      ++row;
+    }
+  }
+}
+
+// Rows of a matrix into a tile. mode: bytes that may move at once (16, 4 or 2).
+template <typename T>
+__device__ __forceinline__ void load_rows(uint8_t* tile, int pitch, const T* base, int64_t ld, uint32_t rows,
+                                          int experts, int mode, int lane) {
+  const int bytes = experts * (int)sizeof(T);
+  const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(tile));
+  const uint8_t* src = reinterpret_cast<const uint8_t*>(base);
+  const int64_t ldb = ld * (int64_t)sizeof(T);
+  if (mode == 16)
+    each_unit(rows, bytes / 16, lane, [&](int r, int u) { copy_async<16>(at + r * pitch + u * 16, src + r * ldb + u * 16); });
+  else if (mode == 4)
+    each_unit(rows, bytes / 4, lane, [&](int r, int u) { copy_async<4>(at + r * pitch + u * 4, src + r * ldb + u * 4); });
+  else
+    each_unit(rows, experts, lane, [&](int r, int u) { reinterpret_cast<T*>(tile + r * pitch)[u] = base[r * ld + u]; });
+  wait_copies();
+  __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void store_rows(const uint8_t* tile, int pitch, T* base, int64_t ld, uint32_t rows,
+                                           int experts, int mode, int lane) {
+  __syncwarp();
+  const int bytes = experts * (int)sizeof(T);
+  uint8_t* dst = reinterpret_cast<uint8_t*>(base);
+  const int64_t ldb = ld * (int64_t)sizeof(T);
+  if (mode == 16)
+    each_unit(rows, bytes / 16, lane, [&](int r, int u) {
+      *reinterpret_cast<uint4*>(dst + r * ldb + u * 16) = *reinterpret_cast<const uint4*>(tile + r * pitch + u * 16);
+    });
+  else if (mode == 4)
+    each_unit(rows, bytes / 4, lane, [&](int r, int u) {
+      *reinterpret_cast<uint32_t*>(dst + r * ldb + u * 4) = *reinterpret_cast<const uint32_t*>(tile + r * pitch + u * 4);
+    });
+  else
+    each_unit(rows, experts, lane, [&](int r, int u) { base[r * ld + u] = reinterpret_cast<const T*>(tile + r * pitch)[u]; });
+  __syncwarp();
+}
+
+// f(j, values) for a row's 16-byte units that are whole, then g(j, value) for the elements left.
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void walk(const uint8_t* row, int experts, F&& f, G&& g) {
+  constexpr int V = 16 / sizeof(T);
+  int j = 0;
+  for (; j + V <= experts; j += V) {
+    const Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
+    float v[V];
+#pragma unroll
+    for (int q = 0; q < V; q += 2) {
+      const float2 x = to_pair(p.v + q);
+      v[q] = x.x;
+      v[q + 1] = x.y;
+    }
+    f(j, v);
+  }
+  for (; j < experts; ++j) g(j, to_f32(reinterpret_cast<const T*>(row)[j]));
+}
+
+// Every lane's row pointer, the live rows as bits, ...
+template <typename T>
+struct Tile {
+  int64_t t0;       // the tile's first token
+  bool here, live;  // this lane's token exists / is not masked
+  uint32_t rows;    // the live ones
+};
+template <typename T>
+__device__ __forceinline__ Tile<T> tile_at(int64_t i, int64_t tokens, const uint8_t* mask, int lane) {
+  Tile<T> t;
+  t.t0 = i * 32;
+  t.here = t.t0 + lane < tokens;
+  t.live = t.here && (!mask || mask[t.t0 + lane] != 0);
+  t.rows = __ballot_sync(0xffffffffu, t.live);
+  return t;
+}
+
+template <typename T, int K, int NW>
+__global__ void __launch_bounds__(kThreads)
+    tile_fwd_kernel(const Forward a, const Totals out, const int mode) {
+  constexpr bool kPacked = sizeof(T) == 2;
+  constexpr int V = 16 / sizeof(T), W = 4 / sizeof(T);  // elements per unit and per word
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ double red[kWarps + 1];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
+  const int pitch = pitch_of(experts * (int)sizeof(T));
+  uint8_t* tile = smem + warp * 32 * pitch;
+  float2* stat = reinterpret_cast<float2*>(smem + kWarps * 32 * pitch) + warp * 32;
+  int32_t* my_idx = reinterpret_cast<int32_t*>(smem + kWarps * 32 * (pitch + 8)) + (warp * 32 + lane) * k;
+  float* my_gate = reinterpret_cast<float*>(my_idx + kThreads * k);
+  int* counts = reinterpret_cast<int*>(smem + kWarps * 32 * (pitch + 8 + 8 * k));
+  for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
+  __syncthreads();
+  uint8_t* row = tile + lane * pitch;
+  float acc[NW * W];
+#pragma unroll
+  for (int i = 0; i < NW * W; ++i) acc[i] = 0.f;
+  int seen = 0;
+  const int64_t tiles = (a.tokens + 31) / 32;
+  for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
+    const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
+    load_rows(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode, lane);
+    const int mine = t.live ? experts : 0;  // elements of this lane's row
+    // the K largest, in falling order: keys with indices, or values
+    using L = std::conditional_t<kPacked, uint32_t, float>;
+    L list[K];
+#pragma unroll
+    for (int q = 0; q < K; ++q) list[q] = kPacked ? (L)0 : (L)-INFINITY;
+    auto insert = [&](int j, float v) {
+      if constexpr (kPacked) {
+        uint32_t x = pack_key(order_key(v), j);
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+          const uint32_t hi = max(list[q], x);
+          x = min(list[q], x);
+          list[q] = hi;
+        }
+      } else {
+        float x = v;
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+          const float hi = fmaxf(list[q], x);
+          x = fminf(list[q], x);
+          list[q] = hi;
+        }
+      }
+    };
+    walk<T>(row, mine,
+            [&](int j, const float (&v)[V]) {
+#pragma unroll
+              for (int q = 0; q < V; ++q) insert(j + q, v[q]);
+            },
+            insert);
+    const float most = kPacked ? key_value(unpack_key((uint32_t)list[0])) : (float)list[0];
+    bool bad = kPacked ? ((uint32_t)list[0] & ~kLow) >= kKeyInf : most == INFINITY;
+    bool counted = (kPacked ? (uint32_t)list[0] > (kKeyNegInf | kLow) : most > -INFINITY) && !bad;
+    // fp32: what reaches the k-th value, a bit per logit, before the row is written over
+    uint32_t marked[NW];
+    if constexpr (!kPacked) {
+      float least = list[0];
+#pragma unroll
+      for (int q = 1; q < K; ++q)
+        if (q < k) least = list[q];
+#pragma unroll
+      for (int b = 0; b < NW; ++b) {
+        uint32_t m = 0;
+        const float* p = reinterpret_cast<const float*>(row) + 32 * b;
+        const int n = min(32, mine - 32 * b);
+        int j = 0;
+        for (; j + 4 <= n; j += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(p + j);
+          const uint32_t four = (v.x >= least ? 1u : 0u) | (v.y >= least ? 2u : 0u) | (v.z >= least ? 4u : 0u) |
+                                (v.w >= least ? 8u : 0u);
+          m |= four << j;
+        }
+        for (; j < n; ++j) m |= (p[j] >= least ? 1u : 0u) << j;
+        marked[b] = m;
+      }
+    }
+    // each lane's choices in its order: index and the logit's difference to the largest
+    for (int q = 0; q < k; ++q) {
+      my_idx[q] = -1;
+      my_gate[q] = 0.f;
+    }
+    if constexpr (kPacked) {
+#pragma unroll
+      for (int q = 0; q < K; ++q)
+        if (q < k && counted && list[q] > (kKeyNegInf | kLow)) {
+          my_idx[q] = packed_index(list[q]);
+          my_gate[q] = exp_neg(key_value(unpack_key(list[q])) - most);
+        }
+    } else {
+      uint32_t used = 0;
+      int base = 0;
+      uint32_t m = marked[0];
+      while (true) {
+        // on to the next marked logit of this lane's row
+#pragma unroll
+        for (int b = 1; b < NW; ++b)
+          if (m == 0 && base < 32 * b) {
+            m = marked[b];
+            base = 32 * b;
+          }
+        if (!__any_sync(0xffffffffu, m != 0)) break;
+        if (m != 0) {
+          const int j = __ffs(m) - 1;
+          m &= m - 1;
+          const float v = reinterpret_cast<const float*>(row)[base + j];
+          int place = 0;
+#pragma unroll
+          for (int q = 0; q < K; ++q) place += list[q] > v;
+          place += __ffs(~(used >> place)) - 1;  // after the equal ones before it
+          if (place < k && v > -INFINITY && counted) {
+            used |= 1u << place;
+            my_idx[place] = base + j;
+            my_gate[place] = exp_neg(v - most);
+          }
+        }
+      }
+    }
+    // the row's exponentials and their sum (fp32: written over the logits)
+    float sum = 0.f;
+    if constexpr (kPacked) {
+      walk<T>(row, mine,
+              [&](int, const float (&v)[V]) {
+#pragma unroll
+                for (int q = 0; q < V; ++q) sum += exp_neg(v[q] - most);
+              },
+              [&](int, float v) { sum += exp_neg(v - most); });
+    } else {
+      const float shift = counted ? most : INFINITY;  // e^-inf for rows that do not count
+      int j = 0;
+      for (; j + 4 <= experts; j += 4) {
+        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
+        v = make_float4(exp_neg(v.x - shift), exp_neg(v.y - shift), exp_neg(v.z - shift), exp_neg(v.w - shift));
+        sum += (v.x + v.y) + (v.z + v.w);
+        if (!counted) v = make_float4(0.f, 0.f, 0.f, 0.f);
+        *reinterpret_cast<float4*>(row + j * 4) = v;
+      }
+      for (; j < experts; ++j) {
+        float* p = reinterpret_cast<float*>(row) + j;
+        const float e = exp_neg(*p - shift);
+        sum += e;
+        *p = counted ? e : 0.f;
+      }
+    }
+    if (t.live && (bad || (counted && sum != sum))) {  // +inf, or a NaN, which no comparison sees
+      bad = true;
+      counted = false;
+      if (a.status) atomicOr(a.status, SOAP_STATUS_NONFINITE);
+    }
+    // a row of nothing but NaN and -inf has no largest value
+    if (t.live && !counted && !bad) {
+      float s = 0.f;
+      if constexpr (kPacked)
+        walk<T>(row, mine, [&](int, const float (&v)[V]) {
+#pragma unroll
+          for (int q = 0; q < V; ++q) s += v[q];
+        }, [&](int, float v) { s += v; });
+      else
+        s = sum;
+      if (s != s) {
+        bad = true;
+        if (a.status) atomicOr(a.status, SOAP_STATUS_NONFINITE);
+      }
+    }
+    seen += counted || bad;
+    const float inv = bad ? NAN : counted ? 1.f / sum : 0.f;
+    stat[lane] = make_float2(most, inv);
+    if (a.stats && t.here) a.stats[t.t0 + lane] = bad ? make_float2(NAN, NAN) : make_float2(most, inv);
+    float total = 0.f;
+    for (int q = 0; q < k; ++q) total += my_gate[q];
+    const float scale = bad ? NAN : a.normalize ? (total > 0.f ? 1.f / total : 0.f) : inv;
+    for (int q = 0; q < k; ++q) {
+      if (bad) my_idx[q] = -1;
+      if (my_idx[q] >= 0) atomicAdd(&counts[my_idx[q]], 1);
+      my_gate[q] *= scale;
+    }
+    __syncwarp();
+    const int64_t n = min((int64_t)32, a.tokens - t.t0) * k;
+    for (int q = lane; q < n; q += 32) {
+      a.indices[t.t0 * k + q] = (my_idx - lane * k)[q];
+      a.gates[t.t0 * k + q] = (my_gate - lane * k)[q];
+    }
+    // sums of probabilities down the columns: a lane per word
+    for (int r = 0; r < 32; ++r) {
+      const float2 st = stat[r];
+      if (st.y == 0.f) continue;  // (the whole warp's)
+#pragma unroll
+      for (int b = 0; b < NW; ++b) {
+        const int c = 32 * b + lane;
+        if (c * W < experts) {
+          if constexpr (kPacked) {
+            const float2 v = to_pair(reinterpret_cast<const T*>(tile + r * pitch) + 2 * c);
+            acc[2 * b] = fmaf(exp_neg(v.x - st.x), st.y, acc[2 * b]);
+            acc[2 * b + 1] = fmaf(exp_neg(v.y - st.x), st.y, acc[2 * b + 1]);
+          } else {
+            acc[b] = fmaf(reinterpret_cast<const float*>(tile + r * pitch)[c], st.y, acc[b]);
+          }
+        }
+      }
+    }
+    __syncwarp();  // the tile may be loaded again
+  }
+  seen = __reduce_add_sync(0xffffffffu, seen);
+  if (lane == 0 && seen) atomicAdd(&counts[experts], seen);
+  __syncthreads();  // the tiles are done with: their place takes the warps' column sums
+  float* shared = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int i = 0; i < NW * W; ++i) {
+    const int c = (32 * (i / W) + lane) * W + i % W;
+    if (c < experts) shared[warp * experts + c] = acc[i];
+  }
+  finish_columns<kWarps>(shared, counts, red, experts, k, a.part_p, a.part_c, out);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, const int mode_in, const int mode_out) {
+  constexpr int V = 16 / sizeof(T);
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
+  const int pitch = pitch_of(experts * (int)sizeof(T));
+  float* up = reinterpret_cast<float*>(smem);  // the balance loss's gradient of the probabilities
+  const int up_bytes = (experts * 4 + 15) / 16 * 16;
+  uint8_t* tile = smem + up_bytes + warp * 32 * pitch;
+  int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * 32 * pitch) + warp * 32 * k;
+  float* dg = reinterpret_cast<float*>(idx + kThreads * k);
+  const int n_live = *a.live;
+  const float per = n_live > 0 ? (float)(a.scale / ((double)n_live * n_live)) : 0.f;
+  for (int c = threadIdx.x; c < experts; c += kThreads) up[c] = per * (float)a.counts[c];
+  __syncthreads();
+  uint8_t* row = tile + lane * pitch;
+  const int64_t tiles = (a.tokens + 31) / 32;
+  for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
+    const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
+    const int64_t n = min((int64_t)32, a.tokens - t.t0) * k;
+    if (a.dgates)
+      for (int q = lane; q < n; q += 32) {
+        idx[q] = a.indices[t.t0 * k + q];
+        dg[q] = a.dgates[t.t0 * k + q];
+      }
+    load_rows(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode_in, lane);
+    const float2 st = t.live ? a.stats[t.t0 + lane] : make_float2(0.f, 0.f);
+    const bool counted = st.y > 0.f;
+    const int mine = counted ? experts : 0;
+    // the gates' gradient at the chosen probabilities, kept as p (what reaches p)
+    float dot = 0.f;
+    if (a.dgates) {
+      float s = 0.f;
+      for (int q = 0; q < k; ++q) {
+        const int at = t.live ? idx[lane * k + q] : -1;
+        if (at < 0 || at >= experts) continue;
+        const float p = exp_neg(to_f32(reinterpret_cast<const T*>(row)[at]) - st.x) * st.y;
+        s += p;
+        dot = fmaf(dg[lane * k + q], p, dot);
+      }
+      if (a.normalize) {
+        // gate_r = p_r / s: d p_r = (d gate_r - sum_j d gate_j gate_j) / s, whose sum with the p_r is zero
+        const float mean = dot / s, inv = 1.f / s;
+        for (int q = 0; q < k; ++q) dg[lane * k + q] = (dg[lane * k + q] - mean) * inv;
+        dot = 0.f;
+      }
+    }
+    float d4[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (sizeof(T) == 4) {  // the probabilities stay in the row
+      int j = 0;
+      for (; j + 4 <= mine; j += 4) {
+        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
+        const float4 u = *reinterpret_cast<const float4*>(up + j);
+        v = make_float4(exp_neg(v.x - st.x) * st.y, exp_neg(v.y - st.x) * st.y, exp_neg(v.z - st.x) * st.y,
+                        exp_neg(v.w - st.x) * st.y);
+        d4[0] = fmaf(v.x, u.x, d4[0]);
+        d4[1] = fmaf(v.y, u.y, d4[1]);
+        d4[2] = fmaf(v.z, u.z, d4[2]);
+        d4[3] = fmaf(v.w, u.w, d4[3]);
+        *reinterpret_cast<float4*>(row + j * 4) = v;
+      }
+      for (; j < mine; ++j) {
+        float* p = reinterpret_cast<float*>(row) + j;
+        *p = exp_neg(*p - st.x) * st.y;
+        d4[0] = fmaf(*p, up[j], d4[0]);
+      }
+    } else {
+      walk<T>(row, mine,
+              [&](int j, const float (&v)[V]) {
+#pragma unroll
+                for (int q = 0; q < V; ++q) d4[q % 4] = fmaf(exp_neg(v[q] - st.x), up[j + q], d4[q % 4]);
+              },
+              [&](int j, float v) { d4[0] = fmaf(exp_neg(v - st.x), up[j], d4[0]); });
+    }
+    float sum = (d4[0] + d4[1]) + (d4[2] + d4[3]);
+    if (sizeof(T) == 2) sum *= st.y;
+    dot += sum;
+    // the chosen logits' own gradients, before the row is written over
+    if (a.dgates)
+      for (int q = 0; q < k; ++q) {
+        const int at = counted ? idx[lane * k + q] : -1;
+        if (at < 0 || at >= experts) {
+          idx[lane * k + q] = -1;
+          continue;
+        }
+        const float x = to_f32(reinterpret_cast<const T*>(row)[at]);
+        const float p = sizeof(T) == 4 ? x : exp_neg(x - st.x) * st.y;
+        dg[lane * k + q] = p * (up[at] + dg[lane * k + q] - dot);
+      }
+    const float fill = t.live && st.y != st.y ? NAN : 0.f;  // a row that holds a NaN or +inf
+    if constexpr (sizeof(T) == 4) {
+      int j = 0;
+      for (; j + 4 <= experts; j += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(up + j);
+        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
+        v = counted ? make_float4(v.x * (u.x - dot), v.y * (u.y - dot), v.z * (u.z - dot), v.w * (u.w - dot))
+                    : make_float4(fill, fill, fill, fill);
+        *reinterpret_cast<float4*>(row + j * 4) = v;
+      }
+      for (; j < experts; ++j) {
+        float* p = reinterpret_cast<float*>(row) + j;
+        *p = counted ? *p * (up[j] - dot) : fill;
+      }
+    } else {
+      int j = 0;
+      for (; j + V <= experts; j += V) {
+        Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
+#pragma unroll
+        for (int q = 0; q < V; q += 2) {
+          float2 v = to_pair(p.v + q);
+          v = counted ? make_float2(exp_neg(v.x - st.x) * st.y * (up[j + q] - dot),
+                                    exp_neg(v.y - st.x) * st.y * (up[j + q + 1] - dot))
+                      : make_float2(fill, fill);
+          from_pair(v, p.v + q);
+        }
+        *reinterpret_cast<Pack<T, V>*>(row + j * sizeof(T)) = p;
+      }
+      for (; j < experts; ++j) {
+        T* p = reinterpret_cast<T*>(row) + j;
+        *p = from_f32<T>(counted ? exp_neg(to_f32(*p) - st.x) * st.y * (up[j] - dot) : fill);
+      }
+    }
+    if (a.dgates)
+      for (int q = 0; q < k; ++q) {
+        const int at = idx[lane * k + q];
+        if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[lane * k + q]);
+      }
+    const uint32_t all = __ballot_sync(0xffffffffu, t.here);
+    store_rows(tile, pitch, static_cast<T*>(a.dlogits) + t.t0 * a.ld_d, a.ld_d, all, experts, mode_out, lane);
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------
+
+size_t fwd_smem(int experts, int k, int32_t type) {
+  return (size_t)kThreads * (pitch_of(row_bytes(experts, type)) + 8 + 8 * k) + (experts + 1) * 4;
+}
+size_t bwd_smem(int experts, int k, int32_t type) {
+  return (experts * 4 + 15) / 16 * 16 + (size_t)kThreads * (pitch_of(row_bytes(experts, type)) + 8 * k);
+}
+
+// Bytes that rows may move at once.
+int mode_of(const void* p, int64_t ld, int experts, int32_t type) {
+  const uintptr_t bytes = reinterpret_cast<uintptr_t>(p) | (uintptr_t)((ld | experts) * dtype_size(type));
+  return bytes % 16 == 0 ? 16 : bytes % 4 == 0 ? 4 : 2;
+}
+
+int per_sm(size_t smem) { return std::max(1, std::min(8, (int)(kSmemPerSm / (smem + 1024 + 64)))); }
+
+template <typename K>
+cudaError_t allow_smem(K kernel, std::atomic<uint64_t>& set) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (set.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  if (e == cudaSuccess) set.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+template <typename T, int K, int NW>
+cudaError_t launch_fwd(const Forward& f, const Totals& out, int ctas, size_t smem, int mode, cudaStream_t s) {
+  static std::atomic<uint64_t> set{0};
+  const auto kernel = tile_fwd_kernel<T, K, NW>;
+  const cudaError_t e = allow_smem(kernel, set);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kCluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, f, out, mode);
+}
+
+template <typename T, int K>
+cudaError_t fwd_words(const Forward& f, const Totals& out, int ctas, size_t smem, int mode, cudaStream_t s) {
+  const int words = (f.experts * (int)sizeof(T) + 3) / 4;
+  if (words <= 32) return launch_fwd<T, K, 1>(f, out, ctas, smem, mode, s);
+  if (words <= 64) return launch_fwd<T, K, 2>(f, out, ctas, smem, mode, s);
+  if (words <= 128) return launch_fwd<T, K, 4>(f, out, ctas, smem, mode, s);
+  return launch_fwd<T, K, 6>(f, out, ctas, smem, mode, s);
+}
+
+template <typename T>
+cudaError_t fwd_list(const Forward& f, const Totals& out, int ctas, size_t smem, int mode, cudaStream_t s) {
+  if (f.k <= 2) return fwd_words<T, 2>(f, out, ctas, smem, mode, s);
+  if (f.k <= 4) return fwd_words<T, 4>(f, out, ctas, smem, mode, s);
+  if (f.k <= 6) return fwd_words<T, 6>(f, out, ctas, smem, mode, s);
+  return fwd_words<T, 8>(f, out, ctas, smem, mode, s);
+}
+
+template <typename T>
+cudaError_t launch_bwd(const Backward& b, int32_t type, cudaStream_t s) {
+  static std::atomic<uint64_t> set{0};
+  const cudaError_t e = allow_smem(tile_bwd_kernel<T>, set);
+  if (e != cudaSuccess) return e;
+  const size_t smem = bwd_smem(b.experts, b.k, type);
+  const int64_t want = (b.tokens + kThreads - 1) / kThreads;
+  const int ctas = (int)std::min<int64_t>(want, 152 * per_sm(smem));
+  tile_bwd_kernel<T><<<ctas, kThreads, smem, s>>>(b, mode_of(b.logits, b.ld, b.experts, type),
+                                                 mode_of(b.dlogits, b.ld_d, b.experts, type));
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool tile_fits(int64_t tokens, int experts, int k, int32_t type) {
+  return tokens >= kFewTokens && k <= kMaxList && row_bytes(experts, type) <= kMaxWords * 4;
+}
+
+int tile_forward_ctas(int64_t tokens, int experts, int k, int32_t type) {
+  const int64_t want = (tokens + kThreads - 1) / kThreads;
+  const int most = std::min(kCluster * kMaxParts, 152 * per_sm(fwd_smem(experts, k, type)));
+  return (int)std::min<int64_t>(most / kCluster, (want + kCluster - 1) / kCluster) * kCluster;
+}
+
+cudaError_t tile_forward(const Forward& f, const Totals& out, int32_t type, cudaStream_t s) {
+  const int ctas = tile_forward_ctas(f.tokens, f.experts, f.k, type);
+  const size_t smem = fwd_smem(f.experts, f.k, type);
+  const int mode = mode_of(f.logits, f.ld, f.experts, type);
+  if (type == SOAP_F32) return fwd_list<float>(f, out, ctas, smem, mode, s);
+  if (type == SOAP_BF16) return fwd_list<__nv_bfloat16>(f, out, ctas, smem, mode, s);
+  return fwd_list<__half>(f, out, ctas, smem, mode, s);
+}
+
+cudaError_t tile_backward(const Backward& b, int32_t type, cudaStream_t s) {
+  if (type == SOAP_F32) return launch_bwd<float>(b, type, s);
+  if (type == SOAP_BF16) return launch_bwd<__nv_bfloat16>(b, type, s);
+  return launch_bwd<__half>(b, type, s);
+}
+
+}  // namespace route
+}  // namespace soap

@@ -101,6 +101,55 @@ def test_many_tokens_and_same_bits(cuda, dtype):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("e,k", [(1, 1), (8, 2), (31, 3), (33, 8), (64, 8), (127, 6), (190, 4), (193, 7), (384, 5), (61, 9)])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_many_tokens_sizes(cuda, e, k, dtype, normalize):
+    """Enough tokens for a thread each, around the sizes where the layout of a row changes, with padding,
+    an unavailable expert, ties and rows that cannot fill their choice."""
+    t = 15000 + e
+    z = _logits(cuda, t, e, dtype, seed=e)
+    z[100:200] = z[100:200].round()
+    if e > 2 * k:
+        z[:, e // 2] = -INF
+        z[300, k - 1:] = -INF
+    if e > 1:
+        z[301] = -INF
+    g = torch.Generator(device=cuda).manual_seed(e)
+    mask = torch.rand(t, device=cuda, generator=g) < 0.9
+    z[~mask] = float("nan")
+    _check(cuda, z, k, mask=mask, normalize=normalize)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("e,k", [(64, 8), (127, 6)])
+def test_many_tokens_layouts_and_nonfinite(cuda, e, k, dtype):
+    """A thread per token: the same bits for any alignment and leading dimension; rows with NaN (of either
+    sign) or +inf; the gradient written over the logits."""
+    z = _logits(cuda, 20000, e, dtype, seed=3)
+    want = route_forward(z, k)
+    dwant = route_backward(z, want, dgates=torch.ones_like(want.gates))
+    for pad, off in ((8, 8), (1, 1), (2, 0), (4, 2)):
+        big = torch.full((20000, e + pad), float("nan"), device=cuda, dtype=dtype)
+        v = big[:, off:off + e]
+        v.copy_(z)
+        got = route_forward(v, k)
+        assert all(torch.equal(a, b) for a, b in zip(want[:6], got[:6]))
+        assert torch.equal(route_backward(v, got, dgates=torch.ones_like(got.gates)), dwant)
+    z[7, 3], z[8, 0], z[9, 1] = float("nan"), INF, -float("nan")
+    z[10] = -INF
+    z[10, 2] = -float("nan")
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    r = route_forward(z, k, status=status)
+    assert int(status) == S.STATUS_NONFINITE and r.loss.isnan()
+    bad = torch.zeros(20000, dtype=torch.bool, device=cuda)
+    bad[7:11] = True
+    assert (r.indices[bad] == -1).all() and r.gates[bad].isnan().all() and r.gates[~bad].isfinite().all()
+    assert torch.equal(r.indices[~bad], want.indices[~bad]) and int(r.live) == 20000
+    dz = route_backward(z, r, dgates=torch.ones_like(r.gates))
+    assert dz[bad].isnan().all() and dz[~bad].isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("e,k", [(6, 3), (64, 8), (100, 5), (300, 7)])
 def test_ties_go_to_the_lower_index(cuda, e, k, dtype):
@@ -150,7 +199,7 @@ def test_nothing_left(cuda):
 @pytest.mark.parametrize("e", [8, 64, 300])
 def test_nonfinite(cuda, e):
     z = _logits(cuda, 40, e, torch.float32)
-    z[3, 2], z[7, 5] = float("nan"), INF
+    z[3, 2], z[7, 5] = -float("nan"), INF
     status = torch.zeros(1, dtype=torch.int32, device=cuda)
     r = route_forward(z, 4, status=status)
     assert int(status) == S.STATUS_NONFINITE
