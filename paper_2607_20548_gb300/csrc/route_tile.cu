@@ -44,56 +44,65 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// f(row, unit) for the `units` units of each row in `rows` (a bit per row), spread over a warp's lanes.
-template <typename F>
-__device__ __forceinline__ void each_unit(uint32_t rows, int units, int lane, F&& f) {
-  const int drow = 32 / units, dunit = 32 - drow * units;
-  int row = lane / units, unit = lane - row * units;
-  while (row < 32) {
-    if (rows >> row & 1) f(row, unit);
-    row += drow;
-    unit += dunit;
-    if (unit >= units) {
-      unit -= units;
-      ++row;
-    }
-  }
+// f(address in the tile, address in the matrix) for the units of UNIT bytes of each row in `rows` (a bit per
+// row): row by row, a lane per unit.
+template <int UNIT, typename F>
+__device__ __forceinline__ void each_unit(uint8_t* tile, int pitch, uint8_t* base, int64_t ld_bytes, uint32_t rows,
+                                          int units, int lane, F&& f) {
+  uint8_t *t = tile + lane * UNIT, *g = base + lane * UNIT;
+  constexpr int kMost = (kMaxWords * 4 / UNIT + 31) / 32;
+#pragma unroll 2
+  for (int r = 0; r < 32; ++r, t += pitch, g += ld_bytes)
+    if (rows >> r & 1)
+#pragma unroll
+      for (int b = 0; b < kMost; ++b) {
+        if (32 * b >= units) break;
+        if (lane + 32 * b < units) f(t + 32 * UNIT * b, g + 32 * UNIT * b);
+      }
 }
 
 // Rows of a matrix into a tile. mode: bytes that may move at once (16, 4 or 2).
 template <typename T>
 __device__ __forceinline__ void load_rows(uint8_t* tile, int pitch, const T* base, int64_t ld, uint32_t rows,
                                           int experts, int mode, int lane) {
+  uint8_t* src = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(base));
   const int bytes = experts * (int)sizeof(T);
-  const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(tile));
-  const uint8_t* src = reinterpret_cast<const uint8_t*>(base);
   const int64_t ldb = ld * (int64_t)sizeof(T);
+  auto async = [](auto unit) {
+    return [](uint8_t* t, const uint8_t* g) {
+      copy_async<decltype(unit)::value>(static_cast<uint32_t>(__cvta_generic_to_shared(t)), g);
+    };
+  };
   if (mode == 16)
-    each_unit(rows, bytes / 16, lane, [&](int r, int u) { copy_async<16>(at + r * pitch + u * 16, src + r * ldb + u * 16); });
+    each_unit<16>(tile, pitch, src, ldb, rows, bytes / 16, lane, async(std::integral_constant<int, 16>()));
   else if (mode == 4)
-    each_unit(rows, bytes / 4, lane, [&](int r, int u) { copy_async<4>(at + r * pitch + u * 4, src + r * ldb + u * 4); });
+    each_unit<4>(tile, pitch, src, ldb, rows, bytes / 4, lane, async(std::integral_constant<int, 4>()));
   else
-    each_unit(rows, experts, lane, [&](int r, int u) { reinterpret_cast<T*>(tile + r * pitch)[u] = base[r * ld + u]; });
+    each_unit<2>(tile, pitch, src, ldb, rows, bytes / 2, lane, [](uint8_t* t, const uint8_t* g) {
+      *reinterpret_cast<uint16_t*>(t) = *reinterpret_cast<const uint16_t*>(g);
+    });
   wait_copies();
   __syncwarp();
 }
 template <typename T>
-__device__ __forceinline__ void store_rows(const uint8_t* tile, int pitch, T* base, int64_t ld, uint32_t rows,
-                                           int experts, int mode, int lane) {
+__device__ __forceinline__ void store_rows(uint8_t* tile, int pitch, T* base, int64_t ld, uint32_t rows, int experts,
+                                           int mode, int lane) {
   __syncwarp();
-  const int bytes = experts * (int)sizeof(T);
   uint8_t* dst = reinterpret_cast<uint8_t*>(base);
+  const int bytes = experts * (int)sizeof(T);
   const int64_t ldb = ld * (int64_t)sizeof(T);
+  auto plain = [](auto type) {
+    return [](const uint8_t* t, uint8_t* g) {
+      using U = decltype(type);
+      *reinterpret_cast<U*>(g) = *reinterpret_cast<const U*>(t);
+    };
+  };
   if (mode == 16)
-    each_unit(rows, bytes / 16, lane, [&](int r, int u) {
-      *reinterpret_cast<uint4*>(dst + r * ldb + u * 16) = *reinterpret_cast<const uint4*>(tile + r * pitch + u * 16);
-    });
+    each_unit<16>(tile, pitch, dst, ldb, rows, bytes / 16, lane, plain(uint4()));
   else if (mode == 4)
-    each_unit(rows, bytes / 4, lane, [&](int r, int u) {
-      *reinterpret_cast<uint32_t*>(dst + r * ldb + u * 4) = *reinterpret_cast<const uint32_t*>(tile + r * pitch + u * 4);
-    });
+    each_unit<4>(tile, pitch, dst, ldb, rows, bytes / 4, lane, plain(uint32_t()));
   else
-    each_unit(rows, experts, lane, [&](int r, int u) { base[r * ld + u] = reinterpret_cast<const T*>(tile + r * pitch)[u]; });
+    each_unit<2>(tile, pitch, dst, ldb, rows, bytes / 2, lane, plain(uint16_t()));
   __syncwarp();
 }
 
@@ -144,9 +153,10 @@ __global__ void __launch_bounds__(kThreads)
   const int pitch = pitch_of(experts * (int)sizeof(T));
   uint8_t* tile = smem + warp * 32 * pitch;
   float2* stat = reinterpret_cast<float2*>(smem + kWarps * 32 * pitch) + warp * 32;
-  int32_t* my_idx = reinterpret_cast<int32_t*>(smem + kWarps * 32 * (pitch + 8)) + (warp * 32 + lane) * k;
-  float* my_gate = reinterpret_cast<float*>(my_idx + kThreads * k);
-  int* counts = reinterpret_cast<int*>(smem + kWarps * 32 * (pitch + 8 + 8 * k));
+  // the tile's choices, choice q of lane l at q * 33 + l
+  int32_t* idx = reinterpret_cast<int32_t*>(smem + kWarps * 32 * (pitch + 8)) + warp * 33 * k;
+  float* gate = reinterpret_cast<float*>(idx + kWarps * 33 * k);
+  int* counts = reinterpret_cast<int*>(smem + kWarps * (32 * (pitch + 8) + 33 * 8 * k));
   for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
   __syncthreads();
   uint8_t* row = tile + lane * pitch;
@@ -215,22 +225,12 @@ __global__ void __launch_bounds__(kThreads)
         marked[b] = m;
       }
     }
-    // each lane's choices in its order: index and the logit's difference to the largest
-    for (int q = 0; q < k; ++q) {
-      my_idx[q] = -1;
-      my_gate[q] = 0.f;
-    }
-    if constexpr (kPacked) {
-#pragma unroll
-      for (int q = 0; q < K; ++q)
-        if (q < k && counted && list[q] > (kKeyNegInf | kLow)) {
-          my_idx[q] = packed_index(list[q]);
-          my_gate[q] = exp_neg(key_value(unpack_key(list[q])) - most);
-        }
-    } else {
+    // fp32: the choices' indices, by their place in the list
+    if constexpr (!kPacked) {
       uint32_t used = 0;
       int base = 0;
       uint32_t m = marked[0];
+      for (int q = 0; q < k; ++q) idx[q * 33 + lane] = -1;
       while (true) {
         // on to the next marked logit of this lane's row
 #pragma unroll
@@ -248,10 +248,9 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
           for (int q = 0; q < K; ++q) place += list[q] > v;
           place += __ffs(~(used >> place)) - 1;  // after the equal ones before it
-          if (place < k && v > -INFINITY && counted) {
+          if (place < k && v > -INFINITY) {
             used |= 1u << place;
-            my_idx[place] = base + j;
-            my_gate[place] = exp_neg(v - most);
+            idx[place * 33 + lane] = base + j;
           }
         }
       }
@@ -272,14 +271,12 @@ __global__ void __launch_bounds__(kThreads)
         float4 v = *reinterpret_cast<const float4*>(row + j * 4);
         v = make_float4(exp_neg(v.x - shift), exp_neg(v.y - shift), exp_neg(v.z - shift), exp_neg(v.w - shift));
         sum += (v.x + v.y) + (v.z + v.w);
-        if (!counted) v = make_float4(0.f, 0.f, 0.f, 0.f);
         *reinterpret_cast<float4*>(row + j * 4) = v;
       }
       for (; j < experts; ++j) {
         float* p = reinterpret_cast<float*>(row) + j;
-        const float e = exp_neg(*p - shift);
-        sum += e;
-        *p = counted ? e : 0.f;
+        *p = exp_neg(*p - shift);
+        sum += *p;
       }
     }
     if (t.live && (bad || (counted && sum != sum))) {  // +inf, or a NaN, which no comparison sees
@@ -306,21 +303,49 @@ __global__ void __launch_bounds__(kThreads)
     const float inv = bad ? NAN : counted ? 1.f / sum : 0.f;
     stat[lane] = make_float2(most, inv);
     if (a.stats && t.here) a.stats[t.t0 + lane] = bad ? make_float2(NAN, NAN) : make_float2(most, inv);
-    float total = 0.f;
-    for (int q = 0; q < k; ++q) total += my_gate[q];
+    // the gates, from the list
+    float mine_g[K], total = 0.f;
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+      bool some;
+      float v;
+      if constexpr (kPacked) {
+        some = counted && q < k && list[q] > (kKeyNegInf | kLow);
+        v = key_value(unpack_key(list[q]));
+      } else {
+        some = counted && q < k && list[q] > -INFINITY;
+        v = list[q];
+      }
+      mine_g[q] = some ? exp_neg(v - most) : 0.f;
+      total += mine_g[q];
+      if (q < k) {
+        int at = -1;
+        if (some) at = kPacked ? packed_index((uint32_t)list[q]) : idx[q * 33 + lane];
+        if (at >= 0) atomicAdd(&counts[at], 1);
+        idx[q * 33 + lane] = at;
+      }
+    }
     const float scale = bad ? NAN : a.normalize ? (total > 0.f ? 1.f / total : 0.f) : inv;
-    for (int q = 0; q < k; ++q) {
-      if (bad) my_idx[q] = -1;
-      if (my_idx[q] >= 0) atomicAdd(&counts[my_idx[q]], 1);
-      my_gate[q] *= scale;
-    }
+#pragma unroll
+    for (int q = 0; q < K; ++q)
+      if (q < k) gate[q * 33 + lane] = mine_g[q] * scale;
     __syncwarp();
-    const int64_t n = min((int64_t)32, a.tokens - t.t0) * k;
-    for (int q = lane; q < n; q += 32) {
-      a.indices[t.t0 * k + q] = (my_idx - lane * k)[q];
-      a.gates[t.t0 * k + q] = (my_gate - lane * k)[q];
+    const int n = (int)min((int64_t)32, a.tokens - t.t0) * k;
+    {
+      int l = lane / k, q = lane - l * k;
+      const int dl = 32 / k, dq = 32 - dl * k;
+      for (int i2 = lane; i2 < n; i2 += 32) {
+        a.indices[t.t0 * k + i2] = idx[q * 33 + l];
+        a.gates[t.t0 * k + i2] = gate[q * 33 + l];
+        l += dl;
+        q += dq;
+        if (q >= k) {
+          q -= k;
+          ++l;
+        }
+      }
     }
-    // sums of probabilities down the columns: a lane per word
+    // sums of probabilities down the columns: a lane per word (rows that do not count hold anything)
     for (int r = 0; r < 32; ++r) {
       const float2 st = stat[r];
       if (st.y == 0.f) continue;  // (the whole warp's)
@@ -361,8 +386,9 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
   float* up = reinterpret_cast<float*>(smem);  // the balance loss's gradient of the probabilities
   const int up_bytes = (experts * 4 + 15) / 16 * 16;
   uint8_t* tile = smem + up_bytes + warp * 32 * pitch;
-  int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * 32 * pitch) + warp * 32 * k;
-  float* dg = reinterpret_cast<float*>(idx + kThreads * k);
+  // the tile's choices and their gates' gradients, choice q of lane l at q * 33 + l
+  int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * 32 * pitch) + warp * 33 * k;
+  float* dg = reinterpret_cast<float*>(idx + kWarps * 33 * k);
   const int n_live = *a.live;
   const float per = n_live > 0 ? (float)(a.scale / ((double)n_live * n_live)) : 0.f;
   for (int c = threadIdx.x; c < experts; c += kThreads) up[c] = per * (float)a.counts[c];
@@ -371,12 +397,21 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
   const int64_t tiles = (a.tokens + 31) / 32;
   for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
     const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
-    const int64_t n = min((int64_t)32, a.tokens - t.t0) * k;
-    if (a.dgates)
-      for (int q = lane; q < n; q += 32) {
-        idx[q] = a.indices[t.t0 * k + q];
-        dg[q] = a.dgates[t.t0 * k + q];
+    if (a.dgates) {
+      const int n = (int)min((int64_t)32, a.tokens - t.t0) * k;
+      int l = lane / k, q = lane - l * k;
+      const int dl = 32 / k, dq = 32 - dl * k;
+      for (int i2 = lane; i2 < n; i2 += 32) {
+        idx[q * 33 + l] = a.indices[t.t0 * k + i2];
+        dg[q * 33 + l] = a.dgates[t.t0 * k + i2];
+        l += dl;
+        q += dq;
+        if (q >= k) {
+          q -= k;
+          ++l;
+        }
       }
+    }
     load_rows(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode_in, lane);
     const float2 st = t.live ? a.stats[t.t0 + lane] : make_float2(0.f, 0.f);
     const bool counted = st.y > 0.f;
@@ -386,16 +421,16 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
     if (a.dgates) {
       float s = 0.f;
       for (int q = 0; q < k; ++q) {
-        const int at = t.live ? idx[lane * k + q] : -1;
+        const int at = t.live ? idx[q * 33 + lane] : -1;
         if (at < 0 || at >= experts) continue;
         const float p = exp_neg(to_f32(reinterpret_cast<const T*>(row)[at]) - st.x) * st.y;
         s += p;
-        dot = fmaf(dg[lane * k + q], p, dot);
+        dot = fmaf(dg[q * 33 + lane], p, dot);
       }
       if (a.normalize) {
         // gate_r = p_r / s: d p_r = (d gate_r - sum_j d gate_j gate_j) / s, whose sum with the p_r is zero
         const float mean = dot / s, inv = 1.f / s;
-        for (int q = 0; q < k; ++q) dg[lane * k + q] = (dg[lane * k + q] - mean) * inv;
+        for (int q = 0; q < k; ++q) dg[q * 33 + lane] = (dg[q * 33 + lane] - mean) * inv;
         dot = 0.f;
       }
     }
@@ -432,52 +467,53 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
     // the chosen logits' own gradients, before the row is written over
     if (a.dgates)
       for (int q = 0; q < k; ++q) {
-        const int at = counted ? idx[lane * k + q] : -1;
+        const int at = counted ? idx[q * 33 + lane] : -1;
         if (at < 0 || at >= experts) {
-          idx[lane * k + q] = -1;
+          idx[q * 33 + lane] = -1;
           continue;
         }
         const float x = to_f32(reinterpret_cast<const T*>(row)[at]);
         const float p = sizeof(T) == 4 ? x : exp_neg(x - st.x) * st.y;
-        dg[lane * k + q] = p * (up[at] + dg[lane * k + q] - dot);
+        dg[q * 33 + lane] = p * (up[at] + dg[q * 33 + lane] - dot);
       }
-    const float fill = t.live && st.y != st.y ? NAN : 0.f;  // a row that holds a NaN or +inf
     if constexpr (sizeof(T) == 4) {
-      int j = 0;
-      for (; j + 4 <= experts; j += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(up + j);
-        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
-        v = counted ? make_float4(v.x * (u.x - dot), v.y * (u.y - dot), v.z * (u.z - dot), v.w * (u.w - dot))
-                    : make_float4(fill, fill, fill, fill);
-        *reinterpret_cast<float4*>(row + j * 4) = v;
-      }
-      for (; j < experts; ++j) {
-        float* p = reinterpret_cast<float*>(row) + j;
-        *p = counted ? *p * (up[j] - dot) : fill;
+      if (counted) {
+        int j = 0;
+        for (; j + 4 <= experts; j += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(up + j);
+          float4 v = *reinterpret_cast<const float4*>(row + j * 4);
+          v = make_float4(v.x * (u.x - dot), v.y * (u.y - dot), v.z * (u.z - dot), v.w * (u.w - dot));
+          *reinterpret_cast<float4*>(row + j * 4) = v;
+        }
+        for (; j < experts; ++j) reinterpret_cast<float*>(row)[j] *= up[j] - dot;
       }
     } else {
-      int j = 0;
-      for (; j + V <= experts; j += V) {
-        Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
+      if (counted) {
+        int j = 0;
+        for (; j + V <= experts; j += V) {
+          Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
 #pragma unroll
-        for (int q = 0; q < V; q += 2) {
-          float2 v = to_pair(p.v + q);
-          v = counted ? make_float2(exp_neg(v.x - st.x) * st.y * (up[j + q] - dot),
-                                    exp_neg(v.y - st.x) * st.y * (up[j + q + 1] - dot))
-                      : make_float2(fill, fill);
-          from_pair(v, p.v + q);
+          for (int q = 0; q < V; q += 2) {
+            const float2 v = to_pair(p.v + q), u = *reinterpret_cast<const float2*>(up + j + q);
+            from_pair(make_float2(exp_neg(v.x - st.x) * st.y * (u.x - dot), exp_neg(v.y - st.x) * st.y * (u.y - dot)),
+                      p.v + q);
+          }
+          *reinterpret_cast<Pack<T, V>*>(row + j * sizeof(T)) = p;
         }
-        *reinterpret_cast<Pack<T, V>*>(row + j * sizeof(T)) = p;
+        for (; j < experts; ++j) {
+          T* p = reinterpret_cast<T*>(row) + j;
+          *p = from_f32<T>(exp_neg(to_f32(*p) - st.x) * st.y * (up[j] - dot));
+        }
       }
-      for (; j < experts; ++j) {
-        T* p = reinterpret_cast<T*>(row) + j;
-        *p = from_f32<T>(counted ? exp_neg(to_f32(*p) - st.x) * st.y * (up[j] - dot) : fill);
-      }
+    }
+    if (!counted) {  // zeros, or NaN for a row that holds a NaN or +inf
+      const T fill = from_f32<T>(t.live && st.y != st.y ? NAN : 0.f);
+      for (int j = 0; j < experts; ++j) reinterpret_cast<T*>(row)[j] = fill;
     }
     if (a.dgates)
       for (int q = 0; q < k; ++q) {
-        const int at = idx[lane * k + q];
-        if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[lane * k + q]);
+        const int at = idx[q * 33 + lane];
+        if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[q * 33 + lane]);
       }
     const uint32_t all = __ballot_sync(0xffffffffu, t.here);
     store_rows(tile, pitch, static_cast<T*>(a.dlogits) + t.t0 * a.ld_d, a.ld_d, all, experts, mode_out, lane);
@@ -487,10 +523,10 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
 // ---- launches ------------------------------------------------------------------------------
 
 size_t fwd_smem(int experts, int k, int32_t type) {
-  return (size_t)kThreads * (pitch_of(row_bytes(experts, type)) + 8 + 8 * k) + (experts + 1) * 4;
+  return (size_t)kWarps * (32 * (pitch_of(row_bytes(experts, type)) + 8) + 33 * 8 * k) + (experts + 1) * 4;
 }
 size_t bwd_smem(int experts, int k, int32_t type) {
-  return (experts * 4 + 15) / 16 * 16 + (size_t)kThreads * (pitch_of(row_bytes(experts, type)) + 8 * k);
+  return (experts * 4 + 15) / 16 * 16 + (size_t)kWarps * (32 * pitch_of(row_bytes(experts, type)) + 33 * 8 * k);
 }
 
 // Bytes that rows may move at once.
