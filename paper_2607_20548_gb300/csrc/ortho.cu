@@ -34,7 +34,8 @@ constexpr int kThreads = 256;
 constexpr int kMaxParts = 1216;  // partial sums of squares per matrix: 8 CTAs per SM
 
 // Squares of a pack's elements: in fp32 where no square over- or underflows (or the pack is zero),
-// else in double. NaN and inf come out as such either way.
+// else in fp64, whose rate is so low that nothing else here uses it. NaN and inf come out as such
+// either way.
 template <typename T, int V>
 __device__ __forceinline__ void add_squares(const Pack<T, V>& p, float& s, double& d) {
   float m = 0.f;
@@ -50,17 +51,20 @@ __device__ __forceinline__ void add_squares(const Pack<T, V>& p, float& s, doubl
   }
 }
 
-// Partial sums of squares: gridDim.x of them for each matrix (gridDim.y). Rows are dealt to warps.
+// Partial sums of squares, gridDim.x of them for each matrix (gridDim.y): in part_f, and in part_d; where
+// fp32's range did not do, part_f's is NaN. Rows are dealt to warps; a thread adds runs of 4 packs.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads)
-    norm_kernel(const T* M, int64_t ld, int64_t stride, int64_t rows, int64_t cols, double* part) {
-  __shared__ double red[kThreads / 32];
+    norm_kernel(const T* M, int64_t ld, int64_t stride, int64_t rows, int64_t cols, float* part_f, double* part_d) {
+  __shared__ float red[kThreads / 32];
+  __shared__ double red_d[kThreads / 32];
   const T* m = M + (int64_t)blockIdx.y * stride;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  float total = 0.f;
   double d = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
     const T* row = m + r * ld;
-    for (int64_t c0 = lane * V; c0 < cols; c0 += 4 * 32 * V) {  // four loads in flight, one fp32 run
+    for (int64_t c0 = lane * V; c0 < cols; c0 += 4 * 32 * V) {
       Pack<T, V> p[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -75,50 +79,72 @@ __global__ void __launch_bounds__(kThreads)
       float s = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) add_squares(p[u], s, d);
-      d += (double)s;
+      total += s;
     }
   }
+  const int64_t at = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const bool wide = __syncthreads_or(!(d == 0.0));
+  float w = total;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-  if (lane == 0) red[warp] = d;
+  for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+  if (lane == 0) red[warp] = w;
+  if (wide) {
+    d += (double)total;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    if (lane == 0) red_d[warp] = d;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 32; ++w) d += red[w];
-    part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = d;
+    for (int q = 1; q < kThreads / 32; ++q) w += red[q];
+    if (wide)
+      for (int q = 1; q < kThreads / 32; ++q) d += red_d[q];
+    part_f[at] = wide ? NAN : w;
+    part_d[at] = wide ? d : (double)w;
   }
 }
 
 // X = M 2^(e + sx) in fp16 (hi, and lo if split), with 1 / max(||M||_F, eps) = t 2^e, t in (1, 2].
 template <typename T, int V, int SPLIT>
 __global__ void __launch_bounds__(kThreads)
-    scale_kernel(const T* M, int64_t ld, int64_t stride, int64_t rows, int64_t cols, const double* part, int parts,
-                 float eps, int sx, __half* X, int64_t ld_x, int64_t stride_x, int64_t lo, float* t, int* done,
-                 int* status) {
+    scale_kernel(const T* M, int64_t ld, int64_t stride, int64_t rows, int64_t cols, const float* part_f,
+                 const double* part_d, int parts, float eps, int sx, __half* X, int64_t ld_x, int64_t stride_x,
+                 int64_t lo, float* t, int* done, int* status) {
   __shared__ float scale;
-  __shared__ double red[kThreads / 32];
+  __shared__ float red[kThreads / 32];
   const int b = blockIdx.y;
-  double s = 0.0;
-  for (int p = threadIdx.x; p < parts; p += kThreads) s += part[(int64_t)b * parts + p];
+  float s = 0.f;
+  for (int p = threadIdx.x; p < parts; p += kThreads) s += part_f[(int64_t)b * parts + p];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    if (blockIdx.x == 0) done[b] = 0;
+    const bool first = blockIdx.x == 0;
+    if (first) done[b] = 0;
     for (int w = 1; w < kThreads / 32; ++w) s += red[w];
-    const double norm = sqrt(s);
-    if (!(norm <= 1.7e308)) {  // NaN or inf: so is the result
+    int e = 0;
+    float f = 0.f;  // norm = f 2^e, f in [0.5, 1)
+    bool finite = true;
+    if (s == 0.f || (s > 1e-30f && s < 1e30f)) {
+      f = frexpf(fmaxf(sqrtf(s), eps), &e);
+    } else {  // beyond fp32's range, or not finite
+      double d = 0.0;
+      for (int p = 0; p < parts; ++p) d += part_d[(int64_t)b * parts + p];
+      d = sqrt(d);
+      finite = d <= 1.7e308;
+      if (finite) f = (float)frexp(d > (double)eps ? d : (double)eps, &e);
+    }
+    if (!finite) {  // NaN or inf: so is the result
       scale = 1.f;
-      if (blockIdx.x == 0) {
+      if (first) {
         t[b] = NAN;
         if (status) atomicOr(status, SOAP_STATUS_NONFINITE);
       }
     } else {
-      int e;
-      const double f = frexp(norm > (double)eps ? norm : (double)eps, &e);  // norm = f 2^e, f in [0.5, 1)
       const int q = min(sx - e, 120);  // a norm near fp32's smallest: t takes what fp32's range leaves
-      scale = (float)ldexp(1.0, q);
-      if (blockIdx.x == 0) t[b] = (float)ldexp(1.0 / f, sx - e - q);
+      scale = ldexpf(1.f, q);
+      if (first) t[b] = ldexpf(1.f / f, sx - e - q);
     }
   }
   __syncthreads();
@@ -174,7 +200,7 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
     off += up((int64_t)bytes, 256);
     return at;
   };
-  p.part_off = take((size_t)batch * kMaxParts * sizeof(double));
+  p.part_off = take((size_t)batch * kMaxParts * (sizeof(double) + sizeof(float)));
   p.t_off = take((size_t)batch * sizeof(float));
   p.done_off = take((size_t)batch * sizeof(int));
   p.done_off = take((size_t)batch * sizeof(int));
@@ -237,13 +263,13 @@ double step_bound(double a, double b, double c, double u) {
 
 template <typename T, int V>
 cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float eps, int sx, const Steps& q,
-                    double* part, float* t, cudaStream_t s) {
+                    float* part_f, double* part_d, float* t, cudaStream_t s) {
   const double n = (double)p.batch * p.rows * p.cols;
   const int64_t want = std::max<int64_t>(1, (152 * 8) / p.batch);
   const int parts = (int)std::min<int64_t>({kMaxParts, want, (p.rows + 7) / 8});
   {
     ProfScope prof(kFamElementwise, 2.0 * n, n * sizeof(T), s);
-    norm_kernel<T, V><<<dim3(parts, (unsigned)p.batch), kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part);
+    norm_kernel<T, V><<<dim3(parts, (unsigned)p.batch), kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d);
   }
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
@@ -252,23 +278,23 @@ cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float
   const dim3 grid((unsigned)std::min<int64_t>(want, (packs + kThreads - 1) / kThreads), (unsigned)p.batch);
   const int64_t sx_elems = p.rows * q.ld_x, lo = sx_elems * p.batch;
   if (p.split)
-    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, q.x[0], q.ld_x,
+    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx, q.x[0], q.ld_x,
                                                     sx_elems, lo, t, q.done, q.status);
   else
-    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part, parts, eps, sx, q.x[0], q.ld_x,
+    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx, q.x[0], q.ld_x,
                                                     sx_elems, lo, t, q.done, q.status);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t prepare_t(const Plan& p, const void* M, int64_t ld, int64_t stride, float eps, int sx, const Steps& q,
-                      double* part, float* t, cudaStream_t s) {
+                      float* part_f, double* part_d, float* t, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const bool vec = reinterpret_cast<uintptr_t>(M) % 16 == 0 && ld % V == 0 && (p.batch == 1 || stride % V == 0) &&
                    p.cols % V == 0;
   const T* m = static_cast<const T*>(M);
-  return vec ? prepare<T, V>(p, m, ld, stride, eps, sx, q, part, t, s)
-             : prepare<T, 1>(p, m, ld, stride, eps, sx, q, part, t, s);
+  return vec ? prepare<T, V>(p, m, ld, stride, eps, sx, q, part_f, part_d, t, s)
+             : prepare<T, 1>(p, m, ld, stride, eps, sx, q, part_f, part_d, t, s);
 }
 
 cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_t type, const float* coeffs, int steps,
@@ -307,14 +333,15 @@ cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_
                  (float)std::ldexp(1.0, sn - sb - sx), (float)std::ldexp(a, sn - sx)};
     sx = sn;
   }
-  double* part = reinterpret_cast<double*>(ws + p.part_off);
+  double* part_d = reinterpret_cast<double*>(ws + p.part_off);
+  float* part_f = reinterpret_cast<float*>(part_d + p.batch * kMaxParts);
   cudaError_t e;
   if (type == SOAP_F32)
-    e = prepare_t<float>(p, M, ld, stride, eps, sx0, q, part, t, s);
+    e = prepare_t<float>(p, M, ld, stride, eps, sx0, q, part_f, part_d, t, s);
   else if (type == SOAP_BF16)
-    e = prepare_t<__nv_bfloat16>(p, M, ld, stride, eps, sx0, q, part, t, s);
+    e = prepare_t<__nv_bfloat16>(p, M, ld, stride, eps, sx0, q, part_f, part_d, t, s);
   else
-    e = prepare_t<__half>(p, M, ld, stride, eps, sx0, q, part, t, s);
+    e = prepare_t<__half>(p, M, ld, stride, eps, sx0, q, part_f, part_d, t, s);
   return e == cudaSuccess ? run_steps(q, s) : e;
 }
 

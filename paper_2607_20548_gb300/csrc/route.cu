@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kThreads)
   const int experts = a.experts, k = a.k;
   extern __shared__ float shared[];       // [warps][experts] column sums (the first row: the CTA's) ...
   int* counts = reinterpret_cast<int*>(shared + kWarps * experts);  // ... [experts + 1]: choices, tokens counted
-  __shared__ double red[kWarps + 1];
+  __shared__ float red[kWarps + 1];
   __shared__ int won[kPacked ? 1 : kThreads / G][kPacked ? 1 : kMaxK];  // a group's choices
   const int lane = threadIdx.x % G, warp = threadIdx.x / 32;
   for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(1024)
     route_sum_kernel(const float* part_p, const int* part_c, int parts, int experts, int k, Totals out) {
   __shared__ float sum_p[32][32];
   __shared__ int sum_c[32][32];
-  __shared__ double red[32];
+  __shared__ float red[32];
   __shared__ int total;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch overlaps the end of the kernel before
@@ -291,23 +291,23 @@ __global__ void __launch_bounds__(1024)
   }
   __syncthreads();
   const int n = total;
-  double dot = 0.0;
+  float dot = 0.f;
   if (way == 0 && c < experts) {
-    double s = 0.0;
+    float s = 0.f;
     cnt = 0;
     for (int w = 0; w < ways; ++w) {
-      s += (double)sum_p[w * blocks + block][lane];
+      s += sum_p[w * blocks + block][lane];
       cnt += sum_c[w * blocks + block][lane];
     }
-    const double mean = n > 0 ? s / n : 0.0;
+    const float mean = n > 0 ? s / (float)n : 0.f;
     out.counts[c] = cnt;
-    if (out.mean_probs) out.mean_probs[c] = (float)mean;
-    dot = (double)cnt * mean;
+    if (out.mean_probs) out.mean_probs[c] = mean;
+    dot = (float)cnt * mean;
   }
   dot = block_sum(dot, red);
   if (threadIdx.x == 0) {
     *out.live = n;
-    *out.loss = n > 0 ? (float)((double)out.coef * experts / ((double)k * n) * dot) : 0.f;
+    *out.loss = loss_of(dot, n, experts, k, out.coef);
   }
 }
 
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kThreads)
   bool live = t < tokens && (!mask || mask[t] != 0);
   if (live) row.load(logits + t * ld, experts, lane, vec);
   const int n = *a.live;
-  const float per = n > 0 ? (float)(a.scale / ((double)n * n)) : 0.f;
+  const float per = n > 0 ? a.scale / (float)n / (float)n : 0.f;
   float up[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
@@ -556,7 +556,7 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   const double n = (double)tokens * experts;
-  const Backward b{logits, ld, mask, tokens, experts, k, normalize, (double)coef * dloss * experts / k, indices,
+  const Backward b{logits, ld, mask, tokens, experts, k, normalize, (float)((double)coef * dloss * experts / k), indices,
                    reinterpret_cast<const float2*>(stats), counts, live, dgates, dlogits, ld_d};
   ProfScope prof(kFamElementwise, 6.0 * n, 2.0 * n * dtype_size(type) + 12.0 * tokens * k, s);
   cudaError_t e;

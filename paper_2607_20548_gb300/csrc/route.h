@@ -39,7 +39,7 @@ struct Backward {
   const uint8_t* mask;
   int64_t tokens;
   int experts, k, normalize;
-  double scale;  // of counts / n^2
+  float scale;  // of counts / n^2
   const int32_t* indices;
   const float2* stats;
   const int32_t *counts, *live;
@@ -102,24 +102,30 @@ __device__ __forceinline__ uint32_t peer_word(const void* p, uint32_t rank) {
   return v;
 }
 
-// The loss from sum_e counts_e mean_e, summed over a CTA in a fixed order.
-__device__ __forceinline__ double block_sum(double v, double* red) {
+// A sum over a CTA in a fixed order. (fp32, as everything here: an SM's fp64 rate is so low that the few
+// dozen fp64 operations of a thread took 17 us of a launch.)
+__device__ __forceinline__ float block_sum(float v, float* red) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   __syncthreads();
   if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
   __syncthreads();
-  v = 0.0;
+  v = 0.f;
   for (int w = 0; w < (int)blockDim.x / 32; ++w) v += red[w];
   return v;
+}
+
+// coef E / (k n) sum_e counts_e mean_e, from the sum.
+__device__ __forceinline__ float loss_of(float sum, int n, int experts, int k, float coef) {
+  return n > 0 ? coef * (float)experts / (float)k * (sum / (float)n) : 0.f;
 }
 
 // The end of a forward kernel: the CTA's warps have left their column sums in shared[warp][experts], and
 // counts[experts + 1] holds its choices and the tokens counted. Adds the cluster's CTAs in order, each CTA
 // some of the columns; one cluster finishes by itself, several leave a partial row each. `red`: kWarps + 1
-// doubles.
+// floats.
 template <int kWarps>
-__device__ __forceinline__ void finish_columns(float* shared, int* counts, double* red, int experts, int k,
+__device__ __forceinline__ void finish_columns(float* shared, int* counts, float* red, int experts, int k,
                                                float* part_p, int* part_c, const Totals& out) {
   constexpr int kThreads = 32 * kWarps;
   __syncthreads();
@@ -135,7 +141,7 @@ __device__ __forceinline__ void finish_columns(float* shared, int* counts, doubl
   const int64_t part = blockIdx.x / size;
   int n = 0;
   for (uint32_t q = 0; q < size; ++q) n += (int)peer_word(&counts[experts], q);
-  double dot = 0.0;
+  float dot = 0.f;
   for (int c = rank * kThreads + threadIdx.x; c < experts; c += size * kThreads) {
     float v = 0.f;
     int cnt = 0;
@@ -144,10 +150,10 @@ __device__ __forceinline__ void finish_columns(float* shared, int* counts, doubl
       cnt += (int)peer_word(&counts[c], q);
     }
     if (alone) {
-      const double mean = n > 0 ? (double)v / n : 0.0;
+      const float mean = n > 0 ? v / (float)n : 0.f;
       out.counts[c] = cnt;
-      if (out.mean_probs) out.mean_probs[c] = (float)mean;
-      dot += (double)cnt * mean;
+      if (out.mean_probs) out.mean_probs[c] = mean;
+      dot = fmaf((float)cnt, mean, dot);
     } else {
       part_p[part * experts + c] = v;
       part_c[part * (experts + 1) + c] = cnt;
@@ -162,12 +168,10 @@ __device__ __forceinline__ void finish_columns(float* shared, int* counts, doubl
   }
   cluster_sync();
   if (alone && rank == 0 && threadIdx.x == 0) {
-    dot = 0.0;
-    for (uint32_t q = 0; q < size; ++q)
-      dot += __hiloint2double((int)peer_word(reinterpret_cast<const uint32_t*>(&red[kWarps]) + 1, q),
-                              (int)peer_word(&red[kWarps], q));
+    dot = 0.f;
+    for (uint32_t q = 0; q < size; ++q) dot += __uint_as_float(peer_word(&red[kWarps], q));
     *out.live = n;
-    *out.loss = n > 0 ? (float)((double)out.coef * experts / ((double)k * n) * dot) : 0.f;
+    *out.loss = loss_of(dot, n, experts, k, out.coef);
   }
   if (alone) cluster_sync();  // the first CTA has read the others
 }

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kThreads)
   constexpr bool kPacked = sizeof(T) == 2;
   constexpr int V = 16 / sizeof(T), W = 4 / sizeof(T);  // elements per unit and per word
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ double red[kWarps + 1];
+  __shared__ float red[kWarps + 1];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
   const int pitch = pitch_of(experts * (int)sizeof(T));
   uint8_t* tile = smem + warp * 32 * pitch;
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
   int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * 32 * pitch) + warp * 33 * k;
   float* dg = reinterpret_cast<float*>(idx + kWarps * 33 * k);
   const int n_live = *a.live;
-  const float per = n_live > 0 ? (float)(a.scale / ((double)n_live * n_live)) : 0.f;
+  const float per = n_live > 0 ? a.scale / (float)n_live / (float)n_live : 0.f;
   for (int c = threadIdx.x; c < experts; c += kThreads) up[c] = per * (float)a.counts[c];
   __syncthreads();
   uint8_t* row = tile + lane * pitch;
