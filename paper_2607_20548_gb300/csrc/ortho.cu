@@ -173,6 +173,7 @@ struct Plan {
   int r, k;       // the smaller side (the Gram matrix's) and the larger
   bool tall;      // rows > cols
   bool split;
+  int cluster;  // CTAs per matrix of the kernel for small sides; 0: run_steps
   int ld_x, ld_s;
   int64_t x_elems, s_elems;  // per buffer, planes included
   size_t part_off, t_off, done_off, x_off[2], s_off, b_off, bytes;
@@ -189,6 +190,11 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
   p.r = (int)std::min(rows, cols);
   p.k = (int)std::max(rows, cols);
   p.split = type != SOAP_BF16;
+  p.cluster = small_cluster((int)rows, (int)cols, (int)batch, p.split);
+  if (p.cluster > 0) {
+    p.bytes = 256;
+    return p;
+  }
   p.ld_x = (int)up(cols, 8);
   p.ld_s = (int)up(p.r, 8);
   const int64_t planes = batch * (p.split ? 2 : 1);
@@ -326,13 +332,15 @@ cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_
                  c = coeffs ? coeffs[3 * i + 2] : 3.0 / 8;
     const int ss = scale_exp(2 * u * u), sb = scale_exp(2 * poly_bound(b, c, u * u));
     u = step_bound(a, b, c, u);
-    const int sn = i + 1 == steps ? 0 : scale_exp(2 * u);
+    const int sn = i + 1 == steps && p.cluster == 0 ? 0 : scale_exp(2 * u);
     // S 2^ss = 2^(ss - 2 sx) (X 2^sx) (X 2^sx)^T, B 2^sb = c 2^(sb - 2 ss) (S 2^ss)^2 + b 2^(sb - ss) (S 2^ss),
     // X' 2^sn = 2^(sn - sb - sx) (B 2^sb) (X 2^sx) + a 2^(sn - sx) (X 2^sx)
     q.coef[i] = {(float)std::ldexp(1.0, ss - 2 * sx), (float)std::ldexp(c, sb - 2 * ss), (float)std::ldexp(b, sb - ss),
                  (float)std::ldexp(1.0, sn - sb - sx), (float)std::ldexp(a, sn - sx)};
     sx = sn;
   }
+  q.out_exp = sx;
+  if (p.cluster > 0) return run_small(q, p.cluster, M, ld, stride, eps, sx0, s);
   double* part_d = reinterpret_cast<double*>(ws + p.part_off);
   float* part_f = reinterpret_cast<float*>(part_d + p.batch * kMaxParts);
   cudaError_t e;

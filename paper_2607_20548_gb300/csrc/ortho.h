@@ -31,11 +31,19 @@ struct Steps {
   void* out;       // out_type (soap_dtype_t), leading dimension, elements between matrices
   int out_type;
   int64_t ld_out, stride_out;
+  int out_exp;     // the last step's result carries 2^out_exp (run_steps: 0)
   int* status;
   StepCoef coef[kMaxSteps];
 };
 
 cudaError_t run_steps(const Steps& p, cudaStream_t s);
+
+// Matrices with a side of up to 128 that a cluster of CTAs can hold on chip, in one launch from the caller's
+// matrices M (leading dimension ld, elements between matrices) to p.out; of p's buffers it uses none. sx: the
+// scale of the first X. small_cluster: the CTAs per matrix, 0 if it does not fit.
+int small_cluster(int rows, int cols, int batch, bool split);
+cudaError_t run_small(const Steps& p, int cluster, const void* M, int64_t ld, int64_t stride, float eps, int sx,
+                      cudaStream_t s);
 
 }  // namespace ortho
 }  // namespace soap
