@@ -32,7 +32,7 @@ using namespace route;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxExperts = 1024;
-constexpr int kMaxCtas = kCluster * kMaxParts;
+constexpr int kMaxCtas = 608;
 constexpr int kMaxK = 32;
 
 template <int G>
@@ -484,7 +484,7 @@ extern "C" {
 size_t layer_route_workspace_bytes(int64_t tokens, int32_t experts) {
   if (tokens < 0 || tokens > INT32_MAX || experts < 1 || experts > kMaxExperts) return 0;
   int cluster;
-  const size_t parts = ctas_for(tokens, experts, &cluster) / cluster;
+  const size_t parts = tokens >= kFewTokens ? kMaxParts : ctas_for(tokens, experts, &cluster) / cluster;
   return parts * (2 * (size_t)experts + 1) * 4;
 }
 
@@ -502,7 +502,7 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   const bool tiles = tile_fits(tokens, experts, k, type);
-  int cluster = kCluster;
+  int cluster = kTileCluster;
   const int ctas = tiles ? tile_forward_ctas(tokens, experts, k, type) : ctas_for(tokens, experts, &cluster);
   const int parts = ctas / cluster;
   float* part_p = static_cast<float*>(workspace);

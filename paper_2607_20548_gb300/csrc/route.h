@@ -12,7 +12,8 @@ namespace soap {
 namespace route {
 
 constexpr int kCluster = 8;
-constexpr int kMaxParts = 76;  // clusters, and partial rows, of a forward launch
+constexpr int kTileCluster = 4;  // with a thread per token
+constexpr int kMaxParts = 152;   // clusters, and partial rows, of a forward launch
 
 struct Forward {
   const void* logits;
@@ -50,6 +51,7 @@ struct Backward {
 
 // The kernels with a thread per token: whether they take a call, and the launches. forward_ctas: whole
 // clusters.
+constexpr int64_t kFewTokens = 152 * 96;  // below: an SM would have only a few warps
 bool tile_fits(int64_t tokens, int experts, int k, int32_t type);
 int tile_forward_ctas(int64_t tokens, int experts, int k, int32_t type);
 cudaError_t tile_forward(const Forward& f, const Totals& out, int32_t type, cudaStream_t s);

@@ -27,7 +27,6 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxList = 8;               // places of a thread's list
 constexpr int kMaxWords = 6 * 32;         // 32-bit words of a row
-constexpr int64_t kFewTokens = 152 * 96;  // below: an SM would have only a few warps
 constexpr int kSmemPerSm = 228 * 1024;
 
 int row_bytes(int experts, int32_t type) { return experts * (int)dtype_size(type); }
@@ -45,64 +44,89 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
 }
 
 // f(address in the tile, address in the matrix) for the units of UNIT bytes of each row in `rows` (a bit per
-// row): row by row, a lane per unit.
-template <int UNIT, typename F>
-__device__ __forceinline__ void each_unit(uint8_t* tile, int pitch, uint8_t* base, int64_t ld_bytes, uint32_t rows,
+// row): row by row, a lane per unit, MOST units per lane at most. What a lane does in a row is the same in
+// all rows, so that the conditions stay in predicates (worked out per row, they took a third of a
+// backward pass's instructions).
+template <int UNIT, int MOST, typename F>
+__device__ __forceinline__ void each_unit(uint32_t tile, int pitch, uint8_t* base, int64_t ld_bytes, uint32_t rows,
                                           int units, int lane, F&& f) {
-  uint8_t *t = tile + lane * UNIT, *g = base + lane * UNIT;
-  constexpr int kMost = (kMaxWords * 4 / UNIT + 31) / 32;
-#pragma unroll 2
-  for (int r = 0; r < 32; ++r, t += pitch, g += ld_bytes)
-    if (rows >> r & 1)
+  uint32_t t = tile + lane * UNIT;
+  uint8_t* g = base + lane * UNIT;
+  bool some[MOST];
 #pragma unroll
-      for (int b = 0; b < kMost; ++b) {
-        if (32 * b >= units) break;
-        if (lane + 32 * b < units) f(t + 32 * UNIT * b, g + 32 * UNIT * b);
+  for (int b = 0; b < MOST; ++b) some[b] = lane + 32 * b < units;
+  auto row = [&] {
+#pragma unroll
+    for (int b = 0; b < MOST; ++b)
+      if (some[b]) f(t + 32 * UNIT * b, g + 32 * UNIT * b);
+    t += pitch;
+    g += ld_bytes;
+  };
+  if (rows == 0xffffffffu) {
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) row();
+  } else {
+    for (int r = 0; r < 32; ++r) {
+      if (rows >> r & 1) {
+        row();
+      } else {
+        t += pitch;
+        g += ld_bytes;
       }
+    }
+  }
 }
 
 // Rows of a matrix into a tile. mode: bytes that may move at once (16, 4 or 2).
-template <typename T>
+template <typename T, int NW>
 __device__ __forceinline__ void load_rows(uint8_t* tile, int pitch, const T* base, int64_t ld, uint32_t rows,
                                           int experts, int mode, int lane) {
   uint8_t* src = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(base));
+  const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(tile));
   const int bytes = experts * (int)sizeof(T);
   const int64_t ldb = ld * (int64_t)sizeof(T);
-  auto async = [](auto unit) {
-    return [](uint8_t* t, const uint8_t* g) {
-      copy_async<decltype(unit)::value>(static_cast<uint32_t>(__cvta_generic_to_shared(t)), g);
-    };
-  };
   if (mode == 16)
-    each_unit<16>(tile, pitch, src, ldb, rows, bytes / 16, lane, async(std::integral_constant<int, 16>()));
+    each_unit<16, (NW + 3) / 4>(dst, pitch, src, ldb, rows, bytes / 16, lane,
+                                [](uint32_t t, const uint8_t* g) { copy_async<16>(t, g); });
   else if (mode == 4)
-    each_unit<4>(tile, pitch, src, ldb, rows, bytes / 4, lane, async(std::integral_constant<int, 4>()));
-  else
-    each_unit<2>(tile, pitch, src, ldb, rows, bytes / 2, lane, [](uint8_t* t, const uint8_t* g) {
-      *reinterpret_cast<uint16_t*>(t) = *reinterpret_cast<const uint16_t*>(g);
+    each_unit<4, NW>(dst, pitch, src, ldb, rows, bytes / 4, lane,
+                     [](uint32_t t, const uint8_t* g) { copy_async<4>(t, g); });
+  else if constexpr (sizeof(T) == 2)
+    each_unit<2, 2 * NW>(dst, pitch, src, ldb, rows, bytes / 2, lane, [](uint32_t t, const uint8_t* g) {
+      asm volatile("st.shared.u16 [%0], %1;" ::"r"(t), "h"(*reinterpret_cast<const uint16_t*>(g)) : "memory");
     });
   wait_copies();
   __syncwarp();
 }
-template <typename T>
+template <typename T, int NW>
 __device__ __forceinline__ void store_rows(uint8_t* tile, int pitch, T* base, int64_t ld, uint32_t rows, int experts,
                                            int mode, int lane) {
   __syncwarp();
   uint8_t* dst = reinterpret_cast<uint8_t*>(base);
+  const uint32_t src = static_cast<uint32_t>(__cvta_generic_to_shared(tile));
   const int bytes = experts * (int)sizeof(T);
   const int64_t ldb = ld * (int64_t)sizeof(T);
-  auto plain = [](auto type) {
-    return [](const uint8_t* t, uint8_t* g) {
-      using U = decltype(type);
-      *reinterpret_cast<U*>(g) = *reinterpret_cast<const U*>(t);
-    };
-  };
   if (mode == 16)
-    each_unit<16>(tile, pitch, dst, ldb, rows, bytes / 16, lane, plain(uint4()));
+    each_unit<16, (NW + 3) / 4>(src, pitch, dst, ldb, rows, bytes / 16, lane, [](uint32_t t, uint8_t* g) {
+      uint4 v;
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                   : "r"(t)
+                   : "memory");
+      *reinterpret_cast<uint4*>(g) = v;
+    });
   else if (mode == 4)
-    each_unit<4>(tile, pitch, dst, ldb, rows, bytes / 4, lane, plain(uint32_t()));
-  else
-    each_unit<2>(tile, pitch, dst, ldb, rows, bytes / 2, lane, plain(uint16_t()));
+    each_unit<4, NW>(src, pitch, dst, ldb, rows, bytes / 4, lane, [](uint32_t t, uint8_t* g) {
+      uint32_t v;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(t) : "memory");
+      *reinterpret_cast<uint32_t*>(g) = v;
+    });
+  else if constexpr (sizeof(T) == 2)
+    each_unit<2, 2 * NW>(src, pitch, dst, ldb, rows, bytes / 2, lane, [](uint32_t t, uint8_t* g) {
+      uint16_t v;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(t) : "memory");
+      *reinterpret_cast<uint16_t*>(g) = v;
+    });
   __syncwarp();
 }
 
@@ -130,7 +154,7 @@ template <typename T>
 struct Tile {
   int64_t t0;       // the tile's first token
   bool here, live;  // this lane's token exists / is not masked
-  uint32_t rows;    // the live ones
+  uint32_t rows;    // the rows to read, a bit each
 };
 template <typename T>
 __device__ __forceinline__ Tile<T> tile_at(int64_t i, int64_t tokens, const uint8_t* mask, int lane) {
@@ -138,8 +162,52 @@ __device__ __forceinline__ Tile<T> tile_at(int64_t i, int64_t tokens, const uint
   t.t0 = i * 32;
   t.here = t.t0 + lane < tokens;
   t.live = t.here && (!mask || mask[t.t0 + lane] != 0);
-  t.rows = __ballot_sync(0xffffffffu, t.live);
+  // a tile with a live row is read whole: to leave single rows out costs more than it saves
+  t.rows = __any_sync(0xffffffffu, t.live) ? __ballot_sync(0xffffffffu, t.here) : 0u;
   return t;
+}
+
+__device__ __forceinline__ void exchange(float& a, float& b) {
+  const float hi = fmaxf(a, b);
+  b = fminf(a, b);
+  a = hi;
+}
+__device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+// One more value into a falling list of the K largest.
+template <int K, typename L>
+__device__ __forceinline__ void insert(L (&list)[K], L x) {
+#pragma unroll
+  for (int q = 0; q < K; ++q) exchange(list[q], x);
+}
+// Four more: sorted, the larger of list[i] and the (K - 1 - i)-th of them are the K largest, falling and then
+// rising, which a bitonic merge puts in order (as if larger values filled the places up to a power of two).
+// 28 minima and maxima for K = 6 (one by one: 48), and most of them do not wait for one another.
+template <int K, typename L>
+__device__ __forceinline__ void insert4(L (&list)[K], L a, L b, L c, L d) {
+  exchange(a, b);
+  exchange(c, d);
+  exchange(a, c);
+  exchange(b, d);
+  exchange(b, c);
+  const L four[4] = {a, b, c, d};
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+    if (K - 1 - i < 4) {
+      if constexpr (std::is_same_v<L, float>)
+        list[i] = fmaxf(list[i], four[K - 1 - i]);
+      else
+        list[i] = max(list[i], four[K - 1 - i]);
+    }
+  constexpr int P = K <= 2 ? 2 : K <= 4 ? 4 : 8, O = P - K;
+#pragma unroll
+  for (int h = P / 2; h > 0; h /= 2)
+#pragma unroll
+    for (int i = O; i < P; ++i)
+      if ((i & h) == 0 && i + h < P) exchange(list[i - O], list[i + h - O]);
 }
 
 template <typename T, int K, int NW>
@@ -167,38 +235,27 @@ __global__ void __launch_bounds__(kThreads)
   const int64_t tiles = (a.tokens + 31) / 32;
   for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
     const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
-    load_rows(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode, lane);
+    load_rows<T, NW>(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode, lane);
     const int mine = t.live ? experts : 0;  // elements of this lane's row
     // the K largest, in falling order: keys with indices, or values
     using L = std::conditional_t<kPacked, uint32_t, float>;
     L list[K];
 #pragma unroll
     for (int q = 0; q < K; ++q) list[q] = kPacked ? (L)0 : (L)-INFINITY;
-    auto insert = [&](int j, float v) {
-      if constexpr (kPacked) {
-        uint32_t x = pack_key(order_key(v), j);
-#pragma unroll
-        for (int q = 0; q < K; ++q) {
-          const uint32_t hi = max(list[q], x);
-          x = min(list[q], x);
-          list[q] = hi;
-        }
-      } else {
-        float x = v;
-#pragma unroll
-        for (int q = 0; q < K; ++q) {
-          const float hi = fmaxf(list[q], x);
-          x = fminf(list[q], x);
-          list[q] = hi;
-        }
-      }
+    auto key = [](int j, float v) -> L {
+      if constexpr (kPacked)
+        return pack_key(order_key(v), j);
+      else
+        return v;
     };
     walk<T>(row, mine,
             [&](int j, const float (&v)[V]) {
 #pragma unroll
-              for (int q = 0; q < V; ++q) insert(j + q, v[q]);
+              for (int q = 0; q < V; q += 4)
+                insert4<K, L>(list, key(j + q, v[q]), key(j + q + 1, v[q + 1]), key(j + q + 2, v[q + 2]),
+                              key(j + q + 3, v[q + 3]));
             },
-            insert);
+            [&](int j, float v) { insert<K, L>(list, key(j, v)); });
     const float most = kPacked ? key_value(unpack_key((uint32_t)list[0])) : (float)list[0];
     bool bad = kPacked ? ((uint32_t)list[0] & ~kLow) >= kKeyInf : most == INFINITY;
     bool counted = (kPacked ? (uint32_t)list[0] > (kKeyNegInf | kLow) : most > -INFINITY) && !bad;
@@ -346,9 +403,8 @@ __global__ void __launch_bounds__(kThreads)
       }
     }
     // sums of probabilities down the columns: a lane per word (rows that do not count hold anything)
-    for (int r = 0; r < 32; ++r) {
+    auto add_row = [&](int r) {
       const float2 st = stat[r];
-      if (st.y == 0.f) continue;  // (the whole warp's)
 #pragma unroll
       for (int b = 0; b < NW; ++b) {
         const int c = 32 * b + lane;
@@ -361,6 +417,16 @@ __global__ void __launch_bounds__(kThreads)
             acc[b] = fmaf(reinterpret_cast<const float*>(tile + r * pitch)[c], st.y, acc[b]);
           }
         }
+      }
+    };
+    const uint32_t count_rows = __ballot_sync(0xffffffffu, counted || bad);
+    for (int r = 0; r < 32; r += 4) {
+      if ((count_rows >> r & 15u) == 15u) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) add_row(r + q);
+      } else {
+        for (int q = r; q < r + 4; ++q)
+          if (count_rows >> q & 1u) add_row(q);
       }
     }
     __syncwarp();  // the tile may be loaded again
@@ -377,7 +443,7 @@ __global__ void __launch_bounds__(kThreads)
   finish_columns<kWarps>(shared, counts, red, experts, k, a.part_p, a.part_c, out);
 }
 
-template <typename T>
+template <typename T, int NW>
 __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, const int mode_in, const int mode_out) {
   constexpr int V = 16 / sizeof(T);
   extern __shared__ __align__(16) uint8_t smem[];
@@ -412,7 +478,7 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
         }
       }
     }
-    load_rows(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode_in, lane);
+    load_rows<T, NW>(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode_in, lane);
     const float2 st = t.live ? a.stats[t.t0 + lane] : make_float2(0.f, 0.f);
     const bool counted = st.y > 0.f;
     const int mine = counted ? experts : 0;
@@ -516,7 +582,7 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
         if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[q * 33 + lane]);
       }
     const uint32_t all = __ballot_sync(0xffffffffu, t.here);
-    store_rows(tile, pitch, static_cast<T*>(a.dlogits) + t.t0 * a.ld_d, a.ld_d, all, experts, mode_out, lane);
+    store_rows<T, NW>(tile, pitch, static_cast<T*>(a.dlogits) + t.t0 * a.ld_d, a.ld_d, all, experts, mode_out, lane);
   }
 }
 
@@ -557,7 +623,7 @@ cudaError_t launch_fwd(const Forward& f, const Totals& out, int ctas, size_t sme
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = kCluster;
+  attr.val.clusterDim.x = kTileCluster;
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
@@ -586,17 +652,26 @@ cudaError_t fwd_list(const Forward& f, const Totals& out, int ctas, size_t smem,
   return fwd_words<T, 8>(f, out, ctas, smem, mode, s);
 }
 
-template <typename T>
+template <typename T, int NW>
 cudaError_t launch_bwd(const Backward& b, int32_t type, cudaStream_t s) {
   static std::atomic<uint64_t> set{0};
-  const cudaError_t e = allow_smem(tile_bwd_kernel<T>, set);
+  const auto kernel = tile_bwd_kernel<T, NW>;
+  const cudaError_t e = allow_smem(kernel, set);
   if (e != cudaSuccess) return e;
   const size_t smem = bwd_smem(b.experts, b.k, type);
   const int64_t want = (b.tokens + kThreads - 1) / kThreads;
   const int ctas = (int)std::min<int64_t>(want, 152 * per_sm(smem));
-  tile_bwd_kernel<T><<<ctas, kThreads, smem, s>>>(b, mode_of(b.logits, b.ld, b.experts, type),
-                                                 mode_of(b.dlogits, b.ld_d, b.experts, type));
+  kernel<<<ctas, kThreads, smem, s>>>(b, mode_of(b.logits, b.ld, b.experts, type),
+                                      mode_of(b.dlogits, b.ld_d, b.experts, type));
   return cudaGetLastError();
+}
+template <typename T>
+cudaError_t bwd_words(const Backward& b, int32_t type, cudaStream_t s) {
+  const int words = (b.experts * (int)sizeof(T) + 3) / 4;
+  if (words <= 32) return launch_bwd<T, 1>(b, type, s);
+  if (words <= 64) return launch_bwd<T, 2>(b, type, s);
+  if (words <= 128) return launch_bwd<T, 4>(b, type, s);
+  return launch_bwd<T, 6>(b, type, s);
 }
 
 }  // namespace
@@ -607,8 +682,8 @@ bool tile_fits(int64_t tokens, int experts, int k, int32_t type) {
 
 int tile_forward_ctas(int64_t tokens, int experts, int k, int32_t type) {
   const int64_t want = (tokens + kThreads - 1) / kThreads;
-  const int most = std::min(kCluster * kMaxParts, 152 * per_sm(fwd_smem(experts, k, type)));
-  return (int)std::min<int64_t>(most / kCluster, (want + kCluster - 1) / kCluster) * kCluster;
+  const int most = std::min(kTileCluster * kMaxParts, 152 * per_sm(fwd_smem(experts, k, type)));
+  return (int)std::min<int64_t>(most / kTileCluster, (want + kTileCluster - 1) / kTileCluster) * kTileCluster;
 }
 
 cudaError_t tile_forward(const Forward& f, const Totals& out, int32_t type, cudaStream_t s) {
@@ -621,9 +696,9 @@ cudaError_t tile_forward(const Forward& f, const Totals& out, int32_t type, cuda
 }
 
 cudaError_t tile_backward(const Backward& b, int32_t type, cudaStream_t s) {
-  if (type == SOAP_F32) return launch_bwd<float>(b, type, s);
-  if (type == SOAP_BF16) return launch_bwd<__nv_bfloat16>(b, type, s);
-  return launch_bwd<__half>(b, type, s);
+  if (type == SOAP_F32) return bwd_words<float>(b, type, s);
+  if (type == SOAP_BF16) return bwd_words<__nv_bfloat16>(b, type, s);
+  return bwd_words<__half>(b, type, s);
 }
 
 }  // namespace route

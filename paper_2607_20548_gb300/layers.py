@@ -15,9 +15,11 @@ import torch
 
 from .soap import DTYPES, SOAP_OK, SoapError, load_library
 
-# The raw cudaStream_t that is current on a device: torch.cuda.current_stream(...).cuda_stream without
-# the Python object, which costs more than the launch of a small operator.
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# What every call asks torch for, without the Python objects around it (torch.cuda.current_stream(...) alone
+# costs as much as half a launch): the cudaStream_t that is current on a device, and the current device.
+_raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_F32, _I32 = torch.float32, torch.int32
+_empty, _empty_like = torch.empty, torch.empty_like
 
 
 def _refuse(name, t, dtype, device):
@@ -40,14 +42,14 @@ def _operand(name, t, dtype=None, device=None):
     return t.device
 
 
-def _elsewhere(dev, stream):
+def _elsewhere(index, stream):
     """The context in which a call has to run and allocate if that is not the present one: the given
     stream (outputs and workspaces then come from its memory pool), or the operands' device."""
     if stream is not None:
-        if torch.device(stream.device).index != dev.index:
-            raise ValueError(f"stream of {stream.device} given for work on {dev}")
+        if torch.device(stream.device).index != index:
+            raise ValueError(f"stream of {stream.device} given for work on cuda:{index}")
         return torch.cuda.stream(stream)
-    return None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    return None if _current() == index else torch.cuda.device(index)
 
 
 def _rows(t):
@@ -69,20 +71,20 @@ def _done(code, name):
         raise SoapError(code, name)
 
 
-def _weights(name, x, weight, bias, width):
-    """Checks weight and bias and returns their soap_dtype_t."""
-    wt = None
-    for what, t in (("weight", weight), ("bias", bias)):
+def _weights(name, x, width, *vectors):
+    """Checks weight and bias (either may be None) and returns their soap_dtype_t."""
+    index, wt = x.get_device(), None
+    for t in vectors:
         if t is None:
             continue
-        dev = _operand(name, t)
-        if t.shape != (width,) or not t.is_contiguous():
-            raise ValueError(f"{name} {what}: expected {width} contiguous elements")
-        if dev != x.device:
-            raise ValueError(f"{name} {what}: on {dev}, expected {x.device}")
-        if t.dtype not in (torch.float32, x.dtype) or (wt is not None and t.dtype != wt):
+        if not isinstance(t, torch.Tensor) or t.get_device() != index:
+            _operand(name, t, None, x.device)
+        dt = t.dtype
+        if dt is not _F32 and dt is not x.dtype or wt is not None and dt is not wt:
             raise TypeError(f"{name}: weight and bias must both be float32 or both {x.dtype}")
-        wt = t.dtype
+        if t.shape != (width,) or not t.is_contiguous():
+            raise ValueError(f"{name}: weight and bias need {width} contiguous elements")
+        wt = dt
     return 0 if wt is None else DTYPES[wt]
 
 
@@ -92,25 +94,27 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     statistics of every row, which the backward pass takes. weight and bias: float32 or x's type.
     status: an int32 CUDA word that SOAP_STATUS_TIMEOUT is ORed into."""
     name = "layer_norm_forward"
-    dev = _operand(name, x)
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in DTYPES:
+        _refuse(name, x, None, None)
+    index = x.get_device()
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream):
             return layer_norm_forward(x, weight, bias, eps, status)
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError(f"{name}: the normalised dimension is empty")
     if status is not None:
-        _operand(name, status, torch.int32, dev)
-    x, rows, ld = _rows(x)
+        _operand(name, status, _I32, x.device)
     shape = x.shape
+    if not shape or shape[-1] < 1:
+        raise ValueError(f"{name}: the normalised dimension is empty")
+    x, rows, ld = _rows(x)
     width = shape[-1]
-    wt = _weights(name, x, weight, bias, width)
-    y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    mean, rstd = x.new_empty((2,) + shape[:-1], dtype=torch.float32).unbind(0)
+    wt = _weights(name, x, width, weight, bias)
+    y = _empty_like(x) if x.is_contiguous() else _empty(shape, dtype=x.dtype, device=x.device)
+    mean = _empty(shape[:-1], dtype=_F32, device=x.device)
+    rstd = _empty_like(mean)
     _done(load_library().layer_norm_forward(
         rows, width, x.data_ptr(), ld, DTYPES[x.dtype], None if weight is None else weight.data_ptr(),
-        None if bias is None else bias.data_ptr(), wt, eps, y.data_ptr(), width, mean.data_ptr(), rstd.data_ptr(),
-        None if status is None else status.data_ptr(), _raw_stream(dev.index)), name)
+        None if bias is None else bias.data_ptr(), wt, eps, y.data_ptr(), width, mean.data_ptr(),
+        rstd.data_ptr(), None if status is None else status.data_ptr(), _raw_stream(index)), name)
     return y, mean, rstd
 
 
@@ -120,40 +124,43 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     """(dx, dweight, dbias) of layer_norm_forward from dy and its mean and rstd. dx has x's type;
     dweight and dbias are float32 (the optimizer's gradient type), or None without ``params``."""
     name = "layer_norm_backward"
-    dev = _operand(name, x)
-    _operand(name, dy, x.dtype, dev)
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in DTYPES:
+        _refuse(name, x, None, None)
+    index = x.get_device()
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream):
             return layer_norm_backward(dy, x, mean, rstd, weight, params, status)
-    if dy.shape != x.shape:
-        raise ValueError(f"{name}: dy and x have different shapes")
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError(f"{name}: the normalised dimension is empty")
+    dev = x.device
+    _operand(name, dy, x.dtype, dev)
     if status is not None:
-        _operand(name, status, torch.int32, dev)
+        _operand(name, status, _I32, dev)
+    shape = x.shape
+    if dy.shape != shape:
+        raise ValueError(f"{name}: dy and x have different shapes")
+    if not shape or shape[-1] < 1:
+        raise ValueError(f"{name}: the normalised dimension is empty")
     x, rows, ld = _rows(x)
     dy, _, ld_dy = _rows(dy)
-    width = x.shape[-1]
+    width = shape[-1]
     for t in (mean, rstd):
-        _operand(name, t, torch.float32, dev)
+        _operand(name, t, _F32, dev)
         if t.numel() != rows or not t.is_contiguous():
             raise ValueError(f"{name}: mean and rstd do not match x's rows")
-    wt = _weights(name, x, weight, None, width)
+    wt = _weights(name, x, width, weight)
     lib = load_library()
-    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-    dw = db = None
-    ws = ws_bytes = 0
+    dx = _empty_like(x) if x.is_contiguous() else _empty(shape, dtype=x.dtype, device=x.device)
+    dw = db = ws = None
+    ws_bytes = 0
     if params:
         ws_bytes = lib.layer_norm_workspace_bytes(rows, width)
-        dw, db = x.new_empty((2, width), dtype=torch.float32).unbind(0)
-        space = x.new_empty(ws_bytes, dtype=torch.uint8)
-        ws = space.data_ptr()
+        dw = _empty(width, dtype=_F32, device=dev)
+        db = _empty_like(dw)
+        ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_norm_backward(
         rows, width, dy.data_ptr(), ld_dy, x.data_ptr(), ld, DTYPES[x.dtype], mean.data_ptr(), rstd.data_ptr(),
         None if weight is None else weight.data_ptr(), wt, dx.data_ptr(), width, dw.data_ptr() if params else None,
-        db.data_ptr() if params else None, ws, ws_bytes, None if status is None else status.data_ptr(),
-        _raw_stream(dev.index)), name)
+        db.data_ptr() if params else None, ws.data_ptr() if params else None, ws_bytes,
+        None if status is None else status.data_ptr(), _raw_stream(index)), name)
     return dx, dw, db
 
 
@@ -180,9 +187,8 @@ def route_forward(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = N
     SOAP_STATUS_NONFINITE is ORed into."""
     name = "route_forward"
     dev = _operand(name, logits)
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream):
             return route_forward(logits, k, mask, normalize, coef, status)
     if logits.dim() < 1:
         raise ValueError(f"{name}: needs at least one dimension")
@@ -194,23 +200,23 @@ def route_forward(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = N
             raise ValueError(f"{name}: the mask needs one value per token")
         mask = mask.contiguous()
     if status is not None:
-        _operand(name, status, torch.int32, dev)
+        _operand(name, status, _I32, dev)
     lib = load_library()
     k = int(k)
     ws_bytes = lib.layer_route_workspace_bytes(tokens, experts)
     if ws_bytes == 0 or not 1 <= k <= min(experts, 32):
         raise ValueError(f"{name}: needs 1 to 1024 experts and k of 1 to min(experts, 32)")
-    gates = z.new_empty(lead + (k,), dtype=torch.float32)
-    indices = z.new_empty(lead + (k,), dtype=torch.int32)
-    stats = z.new_empty(lead + (2,), dtype=torch.float32)
-    counts, mean_probs = z.new_empty(experts, dtype=torch.int32), z.new_empty(experts, dtype=torch.float32)
-    live, loss = z.new_empty((), dtype=torch.int32), z.new_empty((), dtype=torch.float32)
-    ws = z.new_empty(ws_bytes, dtype=torch.uint8)
+    chosen = lead + (k,)
+    gates, indices = _empty(chosen, dtype=_F32, device=dev), _empty(chosen, dtype=_I32, device=dev)
+    stats = _empty(lead + (2,), dtype=_F32, device=dev)
+    mean_probs, counts = _empty(experts, dtype=_F32, device=dev), _empty(experts, dtype=_I32, device=dev)
+    loss, live = _empty((), dtype=_F32, device=dev), _empty((), dtype=_I32, device=dev)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_route_forward(
         tokens, experts, k, z.data_ptr(), ld, DTYPES[z.dtype], None if mask is None else mask.data_ptr(),
-        int(normalize), coef, indices.data_ptr(), gates.data_ptr(), stats.data_ptr(), counts.data_ptr(), live.data_ptr(),
-        mean_probs.data_ptr(), loss.data_ptr(), None if status is None else status.data_ptr(), ws.data_ptr(), ws_bytes,
-        _raw_stream(dev.index)), name)
+        int(normalize), coef, indices.data_ptr(), gates.data_ptr(), stats.data_ptr(), counts.data_ptr(),
+        live.data_ptr(), mean_probs.data_ptr(), loss.data_ptr(), None if status is None else status.data_ptr(),
+        ws.data_ptr(), ws_bytes, _raw_stream(dev.index)), name)
     return Routing(indices, gates, counts, mean_probs, loss, live, stats, mask, bool(normalize), float(coef))
 
 
@@ -219,9 +225,8 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
     """dlogits (logits' shape and type) from the gates' gradient (fp32, None for zero) and the loss's."""
     name = "route_backward"
     dev = _operand(name, logits)
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream):
             return route_backward(logits, routing, dgates, dloss)
     shape, shape_k = logits.shape, routing.indices.shape
     if logits.dim() < 1 or shape_k[:-1] != shape[:-1] or routing.counts.shape[0] != shape[-1]:
@@ -234,7 +239,7 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
             raise ValueError(f"{name}: dgates needs the gates' shape")
         dgates = dgates.contiguous()
     z, tokens, ld = _rows(logits)
-    dz = torch.empty_like(z, memory_format=torch.contiguous_format)
+    dz = _empty_like(z, memory_format=torch.contiguous_format)
     _done(load_library().layer_route_backward(
         tokens, shape[-1], shape_k[-1], z.data_ptr(), ld, DTYPES[z.dtype],
         None if routing.mask is None else routing.mask.data_ptr(), int(routing.normalize), routing.coef, dloss,
@@ -277,25 +282,24 @@ def muon_orthogonalize(M: torch.Tensor, coeffs=None, ns_steps: int = 16, eps: fl
     status: an int32 CUDA word that SOAP_STATUS_* bits are ORed into."""
     name = "muon_orthogonalize"
     dev = _operand(name, M)
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream):
             return muon_orthogonalize(M, coeffs, ns_steps, eps, status)
     if status is not None:
-        _operand(name, status, torch.int32, dev)
+        _operand(name, status, _I32, dev)
     flat = None
     if coeffs is not None:
         ns_steps = len(coeffs)
         flat = (ctypes.c_float * (3 * ns_steps))(*[float(x) for abc in coeffs for x in abc])
     M, batch, rows, cols, ld, stride, swapped = _matrices(name, M)
     if M.numel() == 0:
-        return torch.empty_like(M)
-    out = M.new_empty(M.shape[:-2] + (rows, cols))
+        return _empty_like(M)
+    out = _empty(M.shape[:-2] + (rows, cols), dtype=M.dtype, device=dev)
     lib = load_library()
     ws_bytes = lib.muon_orthogonalize_workspace_bytes(batch, rows, cols, DTYPES[M.dtype])
     if ws_bytes == 0:
         raise ValueError(f"{name}: sides of 1 to 65536, fewer than 2^31 elements and 65536 matrices")
-    ws = M.new_empty(ws_bytes, dtype=torch.uint8)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.muon_orthogonalize(batch, rows, cols, M.data_ptr(), ld, stride, DTYPES[M.dtype], flat, ns_steps, eps,
                                  out.data_ptr(), cols, rows * cols, ws.data_ptr(), ws_bytes,
                                  None if status is None else status.data_ptr(), _raw_stream(dev.index)), name)
