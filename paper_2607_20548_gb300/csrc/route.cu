@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(1024)
   float v = 0.f;
   int cnt = 0;
   if (way < ways && c < experts) {
-#pragma unroll 4
+#pragma unroll 8
     for (int p = way; p < parts; p += ways) {
       v += part_p[(int64_t)p * experts + c];
       cnt += part_c[(int64_t)p * (experts + 1) + c];

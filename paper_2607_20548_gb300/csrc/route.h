@@ -12,8 +12,8 @@ namespace soap {
 namespace route {
 
 constexpr int kCluster = 8;
-constexpr int kTileCluster = 4;  // with a thread per token
-constexpr int kMaxParts = 152;   // clusters, and partial rows, of a forward launch
+constexpr int kTileCluster = 2;  // with a thread per token
+constexpr int kMaxParts = 228;   // clusters, and partial rows, of a forward launch
 
 struct Forward {
   const void* logits;

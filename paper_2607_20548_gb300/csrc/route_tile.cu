@@ -23,8 +23,12 @@ namespace soap {
 namespace route {
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
+constexpr int kRows = 16;                  // a warp's tile: two lanes per row
+constexpr int kTokens = kWarps * kRows;      // a CTA's at a time
+constexpr int kRowBits = (1 << kRows) - 1;
+constexpr int kStride = kRows + 1;         // of the choices' lists
 constexpr int kMaxList = 8;               // places of a thread's list
 constexpr int kMaxWords = 6 * 32;         // 32-bit words of a row
 constexpr int kSmemPerSm = 228 * 1024;
@@ -62,11 +66,11 @@ __device__ __forceinline__ void each_unit(uint32_t tile, int pitch, uint8_t* bas
     t += pitch;
     g += ld_bytes;
   };
-  if (rows == 0xffffffffu) {
+  if (rows == kRowBits) {
 #pragma unroll 4
-    for (int r = 0; r < 32; ++r) row();
+    for (int r = 0; r < kRows; ++r) row();
   } else {
-    for (int r = 0; r < 32; ++r) {
+    for (int r = 0; r < kRows; ++r) {
       if (rows >> r & 1) {
         row();
       } else {
@@ -130,12 +134,12 @@ __device__ __forceinline__ void store_rows(uint8_t* tile, int pitch, T* base, in
   __syncwarp();
 }
 
-// f(j, values) for a row's 16-byte units that are whole, then g(j, value) for the elements left.
+// f(j, values) for a row's 16-byte units that are whole, then g(j, value) for the elements left: every other
+// unit, the first lane of a row from the first one; the elements left are the second's.
 template <typename T, typename F, typename G>
-__device__ __forceinline__ void walk(const uint8_t* row, int experts, F&& f, G&& g) {
+__device__ __forceinline__ void walk(const uint8_t* row, int half, int experts, F&& f, G&& g) {
   constexpr int V = 16 / sizeof(T);
-  int j = 0;
-  for (; j + V <= experts; j += V) {
+  for (int j = half * V; j + V <= experts; j += 2 * V) {
     const Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
     float v[V];
 #pragma unroll
@@ -146,24 +150,32 @@ __device__ __forceinline__ void walk(const uint8_t* row, int experts, F&& f, G&&
     }
     f(j, v);
   }
-  for (; j < experts; ++j) g(j, to_f32(reinterpret_cast<const T*>(row)[j]));
+  if (half)
+    for (int j = experts / V * V; j < experts; ++j) g(j, to_f32(reinterpret_cast<const T*>(row)[j]));
+}
+// The same on fp32 values in place: f(four values, j) and g(one, j).
+template <typename F, typename G>
+__device__ __forceinline__ void each_four(uint8_t* row, int half, int experts, F&& f, G&& g) {
+  for (int j = half * 4; j + 4 <= experts; j += 8) f(*reinterpret_cast<float4*>(row + j * 4), j);
+  if (half)
+    for (int j = experts / 4 * 4; j < experts; ++j) g(reinterpret_cast<float*>(row)[j], j);
 }
 
-// Every lane's row pointer, the live rows as bits, ...
-template <typename T>
+// The sum over a row's two lanes.
+__device__ __forceinline__ float both(float v) { return v + __shfl_xor_sync(0xffffffffu, v, kRows); }
+
 struct Tile {
   int64_t t0;       // the tile's first token
   bool here, live;  // this lane's token exists / is not masked
   uint32_t rows;    // the rows to read, a bit each
 };
-template <typename T>
-__device__ __forceinline__ Tile<T> tile_at(int64_t i, int64_t tokens, const uint8_t* mask, int lane) {
-  Tile<T> t;
-  t.t0 = i * 32;
-  t.here = t.t0 + lane < tokens;
-  t.live = t.here && (!mask || mask[t.t0 + lane] != 0);
+__device__ __forceinline__ Tile tile_at(int64_t i, int64_t tokens, const uint8_t* mask, int r) {
+  Tile t;
+  t.t0 = i * kRows;
+  t.here = t.t0 + r < tokens;
+  t.live = t.here && (!mask || mask[t.t0 + r] != 0);
   // a tile with a live row is read whole: to leave single rows out costs more than it saves
-  t.rows = __any_sync(0xffffffffu, t.live) ? __ballot_sync(0xffffffffu, t.here) : 0u;
+  t.rows = __any_sync(0xffffffffu, t.live) ? __ballot_sync(0xffffffffu, t.here) & kRowBits : 0u;
   return t;
 }
 
@@ -183,24 +195,18 @@ __device__ __forceinline__ void insert(L (&list)[K], L x) {
 #pragma unroll
   for (int q = 0; q < K; ++q) exchange(list[q], x);
 }
-// Four more: sorted, the larger of list[i] and the (K - 1 - i)-th of them are the K largest, falling and then
-// rising, which a bitonic merge puts in order (as if larger values filled the places up to a power of two).
-// 28 minima and maxima for K = 6 (one by one: 48), and most of them do not wait for one another.
-template <int K, typename L>
-__device__ __forceinline__ void insert4(L (&list)[K], L a, L b, L c, L d) {
-  exchange(a, b);
-  exchange(c, d);
-  exchange(a, c);
-  exchange(b, d);
-  exchange(b, c);
-  const L four[4] = {a, b, c, d};
+// list[i] and other[K - 1 - i], the larger of each pair: the K largest of two falling lists (other may be
+// shorter), falling and then rising, which a bitonic merge puts in order (as if larger values filled the
+// places up to a power of two).
+template <int K, int N, typename L>
+__device__ __forceinline__ void merge(L (&list)[K], const L (&other)[N]) {
 #pragma unroll
   for (int i = 0; i < K; ++i)
-    if (K - 1 - i < 4) {
+    if (K - 1 - i < N) {
       if constexpr (std::is_same_v<L, float>)
-        list[i] = fmaxf(list[i], four[K - 1 - i]);
+        list[i] = fmaxf(list[i], other[K - 1 - i]);
       else
-        list[i] = max(list[i], four[K - 1 - i]);
+        list[i] = max(list[i], other[K - 1 - i]);
     }
   constexpr int P = K <= 2 ? 2 : K <= 4 ? 4 : 8, O = P - K;
 #pragma unroll
@@ -209,34 +215,46 @@ __device__ __forceinline__ void insert4(L (&list)[K], L a, L b, L c, L d) {
     for (int i = O; i < P; ++i)
       if ((i & h) == 0 && i + h < P) exchange(list[i - O], list[i + h - O]);
 }
+// Four more values: 28 minima and maxima for K = 6 (one by one: 48), and most of them do not wait for one
+// another.
+template <int K, typename L>
+__device__ __forceinline__ void insert4(L (&list)[K], L a, L b, L c, L d) {
+  exchange(a, b);
+  exchange(c, d);
+  exchange(a, c);
+  exchange(b, d);
+  exchange(b, c);
+  const L four[4] = {a, b, c, d};
+  merge<K, 4, L>(list, four);
+}
 
 template <typename T, int K, int NW>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
     tile_fwd_kernel(const Forward a, const Totals out, const int mode) {
   constexpr bool kPacked = sizeof(T) == 2;
   constexpr int V = 16 / sizeof(T), W = 4 / sizeof(T);  // elements per unit and per word
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float red[kWarps + 1];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
+  const int lane = threadIdx.x % 32, r = lane % kRows, half = lane / kRows, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
   const int pitch = pitch_of(experts * (int)sizeof(T));
-  uint8_t* tile = smem + warp * 32 * pitch;
-  float2* stat = reinterpret_cast<float2*>(smem + kWarps * 32 * pitch) + warp * 32;
-  // the tile's choices, choice q of lane l at q * 33 + l
-  int32_t* idx = reinterpret_cast<int32_t*>(smem + kWarps * 32 * (pitch + 8)) + warp * 33 * k;
-  float* gate = reinterpret_cast<float*>(idx + kWarps * 33 * k);
-  int* counts = reinterpret_cast<int*>(smem + kWarps * (32 * (pitch + 8) + 33 * 8 * k));
+  uint8_t* tile = smem + warp * kRows * pitch;
+  float2* stat = reinterpret_cast<float2*>(smem + kWarps * kRows * pitch) + warp * kRows;
+  // the tile's choices, choice q of row r at q * kStride + r
+  int32_t* idx = reinterpret_cast<int32_t*>(smem + kWarps * kRows * (pitch + 8)) + warp * kStride * k;
+  float* gate = reinterpret_cast<float*>(idx + kWarps * kStride * k);
+  int* counts = reinterpret_cast<int*>(smem + kWarps * (kRows * (pitch + 8) + kStride * 8 * k));
   for (int c = threadIdx.x; c <= experts; c += kThreads) counts[c] = 0;
   __syncthreads();
-  uint8_t* row = tile + lane * pitch;
+  uint8_t* row = tile + r * pitch;
   float acc[NW * W];
 #pragma unroll
   for (int i = 0; i < NW * W; ++i) acc[i] = 0.f;
   int seen = 0;
-  const int64_t tiles = (a.tokens + 31) / 32;
+  const int64_t tiles = (a.tokens + kRows - 1) / kRows;
   for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
-    const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
+    const Tile t = tile_at(i, a.tokens, a.mask, r);
     load_rows<T, NW>(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode, lane);
-    const int mine = t.live ? experts : 0;  // elements of this lane's row
+    const int mine = t.live ? experts : 0;  // elements of the row
     // the K largest, in falling order: keys with indices, or values
     using L = std::conditional_t<kPacked, uint32_t, float>;
     L list[K];
@@ -248,7 +266,7 @@ __global__ void __launch_bounds__(kThreads)
       else
         return v;
     };
-    walk<T>(row, mine,
+    walk<T>(row, half, mine,
             [&](int j, const float (&v)[V]) {
 #pragma unroll
               for (int q = 0; q < V; q += 4)
@@ -256,6 +274,10 @@ __global__ void __launch_bounds__(kThreads)
                               key(j + q + 3, v[q + 3]));
             },
             [&](int j, float v) { insert<K, L>(list, key(j, v)); });
+    L others[K];
+#pragma unroll
+    for (int q = 0; q < K; ++q) others[q] = __shfl_xor_sync(0xffffffffu, list[q], kRows);
+    merge<K, K, L>(list, others);
     const float most = kPacked ? key_value(unpack_key((uint32_t)list[0])) : (float)list[0];
     bool bad = kPacked ? ((uint32_t)list[0] & ~kLow) >= kKeyInf : most == INFINITY;
     bool counted = (kPacked ? (uint32_t)list[0] > (kKeyNegInf | kLow) : most > -INFINITY) && !bad;
@@ -269,17 +291,14 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
       for (int b = 0; b < NW; ++b) {
         uint32_t m = 0;
-        const float* p = reinterpret_cast<const float*>(row) + 32 * b;
-        const int n = min(32, mine - 32 * b);
-        int j = 0;
-        for (; j + 4 <= n; j += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(p + j);
-          const uint32_t four = (v.x >= least ? 1u : 0u) | (v.y >= least ? 2u : 0u) | (v.z >= least ? 4u : 0u) |
-                                (v.w >= least ? 8u : 0u);
-          m |= four << j;
-        }
-        for (; j < n; ++j) m |= (p[j] >= least ? 1u : 0u) << j;
-        marked[b] = m;
+        each_four(row + 128 * b, half, min(32, mine - 32 * b),
+                  [&](const float4& v, int j) {
+                    const uint32_t four = (v.x >= least ? 1u : 0u) | (v.y >= least ? 2u : 0u) |
+                                          (v.z >= least ? 4u : 0u) | (v.w >= least ? 8u : 0u);
+                    m |= four << j;
+                  },
+                  [&](float v, int j) { m |= (v >= least ? 1u : 0u) << j; });
+        marked[b] = m | __shfl_xor_sync(0xffffffffu, m, kRows);
       }
     }
     // fp32: the choices' indices, by their place in the list
@@ -287,9 +306,10 @@ __global__ void __launch_bounds__(kThreads)
       uint32_t used = 0;
       int base = 0;
       uint32_t m = marked[0];
-      for (int q = 0; q < k; ++q) idx[q * 33 + lane] = -1;
+      for (int q = half; q < k; q += 2) idx[q * kStride + r] = -1;
+      __syncwarp();
       while (true) {
-        // on to the next marked logit of this lane's row
+        // on to the row's next marked logit (its two lanes do the same)
 #pragma unroll
         for (int b = 1; b < NW; ++b)
           if (m == 0 && base < 32 * b) {
@@ -307,15 +327,16 @@ __global__ void __launch_bounds__(kThreads)
           place += __ffs(~(used >> place)) - 1;  // after the equal ones before it
           if (place < k && v > -INFINITY) {
             used |= 1u << place;
-            idx[place * 33 + lane] = base + j;
+            if (half == 0) idx[place * kStride + r] = base + j;
           }
         }
       }
     }
     // the row's exponentials and their sum (fp32: written over the logits)
+    __syncwarp();
     float sum = 0.f;
     if constexpr (kPacked) {
-      walk<T>(row, mine,
+      walk<T>(row, half, mine,
               [&](int, const float (&v)[V]) {
 #pragma unroll
                 for (int q = 0; q < V; ++q) sum += exp_neg(v[q] - most);
@@ -323,43 +344,43 @@ __global__ void __launch_bounds__(kThreads)
               [&](int, float v) { sum += exp_neg(v - most); });
     } else {
       const float shift = counted ? most : INFINITY;  // e^-inf for rows that do not count
-      int j = 0;
-      for (; j + 4 <= experts; j += 4) {
-        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
-        v = make_float4(exp_neg(v.x - shift), exp_neg(v.y - shift), exp_neg(v.z - shift), exp_neg(v.w - shift));
-        sum += (v.x + v.y) + (v.z + v.w);
-        *reinterpret_cast<float4*>(row + j * 4) = v;
-      }
-      for (; j < experts; ++j) {
-        float* p = reinterpret_cast<float*>(row) + j;
-        *p = exp_neg(*p - shift);
-        sum += *p;
-      }
+      each_four(row, half, experts,
+                [&](float4& p, int) {
+                  const float4 v = make_float4(exp_neg(p.x - shift), exp_neg(p.y - shift), exp_neg(p.z - shift),
+                                               exp_neg(p.w - shift));
+                  sum += (v.x + v.y) + (v.z + v.w);
+                  p = v;
+                },
+                [&](float& p, int) {
+                  p = exp_neg(p - shift);
+                  sum += p;
+                });
     }
+    sum = both(sum);
+    bool found = false;
     if (t.live && (bad || (counted && sum != sum))) {  // +inf, or a NaN, which no comparison sees
-      bad = true;
+      bad = found = true;
       counted = false;
-      if (a.status) atomicOr(a.status, SOAP_STATUS_NONFINITE);
     }
     // a row of nothing but NaN and -inf has no largest value
-    if (t.live && !counted && !bad) {
+    const bool empty = t.live && !counted && !bad;
+    if (__any_sync(0xffffffffu, empty)) {
       float s = 0.f;
       if constexpr (kPacked)
-        walk<T>(row, mine, [&](int, const float (&v)[V]) {
+        walk<T>(row, half, empty ? experts : 0, [&](int, const float (&v)[V]) {
 #pragma unroll
           for (int q = 0; q < V; ++q) s += v[q];
         }, [&](int, float v) { s += v; });
       else
         s = sum;
-      if (s != s) {
-        bad = true;
-        if (a.status) atomicOr(a.status, SOAP_STATUS_NONFINITE);
-      }
+      s = both(s);
+      if (empty && s != s) bad = found = true;
     }
-    seen += counted || bad;
+    if (found && half == 0 && a.status) atomicOr(a.status, SOAP_STATUS_NONFINITE);
+    seen += half == 0 && (counted || bad);
     const float inv = bad ? NAN : counted ? 1.f / sum : 0.f;
-    stat[lane] = make_float2(most, inv);
-    if (a.stats && t.here) a.stats[t.t0 + lane] = bad ? make_float2(NAN, NAN) : make_float2(most, inv);
+    if (half == 0) stat[r] = make_float2(most, inv);
+    if (half == 0 && a.stats && t.here) a.stats[t.t0 + r] = bad ? make_float2(NAN, NAN) : make_float2(most, inv);
     // the gates, from the list
     float mine_g[K], total = 0.f;
 #pragma unroll
@@ -375,25 +396,25 @@ __global__ void __launch_bounds__(kThreads)
       }
       mine_g[q] = some ? exp_neg(v - most) : 0.f;
       total += mine_g[q];
-      if (q < k) {
+      if (q < k && q % 2 == half) {  // the row's lanes take turns
         int at = -1;
-        if (some) at = kPacked ? packed_index((uint32_t)list[q]) : idx[q * 33 + lane];
+        if (some) at = kPacked ? packed_index((uint32_t)list[q]) : idx[q * kStride + r];
         if (at >= 0) atomicAdd(&counts[at], 1);
-        idx[q * 33 + lane] = at;
+        idx[q * kStride + r] = at;
       }
     }
     const float scale = bad ? NAN : a.normalize ? (total > 0.f ? 1.f / total : 0.f) : inv;
 #pragma unroll
     for (int q = 0; q < K; ++q)
-      if (q < k) gate[q * 33 + lane] = mine_g[q] * scale;
+      if (q < k && q % 2 == half) gate[q * kStride + r] = mine_g[q] * scale;
     __syncwarp();
-    const int n = (int)min((int64_t)32, a.tokens - t.t0) * k;
+    const int n = (int)min((int64_t)kRows, a.tokens - t.t0) * k;
     {
       int l = lane / k, q = lane - l * k;
       const int dl = 32 / k, dq = 32 - dl * k;
       for (int i2 = lane; i2 < n; i2 += 32) {
-        a.indices[t.t0 * k + i2] = idx[q * 33 + l];
-        a.gates[t.t0 * k + i2] = gate[q * 33 + l];
+        a.indices[t.t0 * k + i2] = idx[q * kStride + l];
+        a.gates[t.t0 * k + i2] = gate[q * kStride + l];
         l += dl;
         q += dq;
         if (q >= k) {
@@ -403,29 +424,29 @@ __global__ void __launch_bounds__(kThreads)
       }
     }
     // sums of probabilities down the columns: a lane per word (rows that do not count hold anything)
-    auto add_row = [&](int r) {
-      const float2 st = stat[r];
+    auto add_row = [&](int at) {
+      const float2 st = stat[at];
 #pragma unroll
       for (int b = 0; b < NW; ++b) {
         const int c = 32 * b + lane;
         if (c * W < experts) {
           if constexpr (kPacked) {
-            const float2 v = to_pair(reinterpret_cast<const T*>(tile + r * pitch) + 2 * c);
+            const float2 v = to_pair(reinterpret_cast<const T*>(tile + at * pitch) + 2 * c);
             acc[2 * b] = fmaf(exp_neg(v.x - st.x), st.y, acc[2 * b]);
             acc[2 * b + 1] = fmaf(exp_neg(v.y - st.x), st.y, acc[2 * b + 1]);
           } else {
-            acc[b] = fmaf(reinterpret_cast<const float*>(tile + r * pitch)[c], st.y, acc[b]);
+            acc[b] = fmaf(reinterpret_cast<const float*>(tile + at * pitch)[c], st.y, acc[b]);
           }
         }
       }
     };
     const uint32_t count_rows = __ballot_sync(0xffffffffu, counted || bad);
-    for (int r = 0; r < 32; r += 4) {
-      if ((count_rows >> r & 15u) == 15u) {
+    for (int r4 = 0; r4 < kRows; r4 += 4) {
+      if ((count_rows >> r4 & 15u) == 15u) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) add_row(r + q);
+        for (int q = 0; q < 4; ++q) add_row(r4 + q);
       } else {
-        for (int q = r; q < r + 4; ++q)
+        for (int q = r4; q < r4 + 4; ++q)
           if (count_rows >> q & 1u) add_row(q);
       }
     }
@@ -444,32 +465,35 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 template <typename T, int NW>
-__global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, const int mode_in, const int mode_out) {
+__global__ void __launch_bounds__(kThreads, 3)
+    tile_bwd_kernel(const Backward a, const int mode_in, const int mode_out) {
   constexpr int V = 16 / sizeof(T);
   extern __shared__ __align__(16) uint8_t smem[];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
+  const int lane = threadIdx.x % 32, r = lane % kRows, half = lane / kRows, warp = threadIdx.x / 32;
+  const int experts = a.experts, k = a.k;
   const int pitch = pitch_of(experts * (int)sizeof(T));
   float* up = reinterpret_cast<float*>(smem);  // the balance loss's gradient of the probabilities
   const int up_bytes = (experts * 4 + 15) / 16 * 16;
-  uint8_t* tile = smem + up_bytes + warp * 32 * pitch;
-  // the tile's choices and their gates' gradients, choice q of lane l at q * 33 + l
-  int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * 32 * pitch) + warp * 33 * k;
-  float* dg = reinterpret_cast<float*>(idx + kWarps * 33 * k);
+  uint8_t* tile = smem + up_bytes + warp * kRows * pitch;
+  // the tile's choices and their gates' gradients, choice q of row r at q * kStride + r; choice q is the
+  // business of the row's lane q % 2
+  int32_t* idx = reinterpret_cast<int32_t*>(smem + up_bytes + kWarps * kRows * pitch) + warp * kStride * k;
+  float* dg = reinterpret_cast<float*>(idx + kWarps * kStride * k);
   const int n_live = *a.live;
   const float per = n_live > 0 ? a.scale / (float)n_live / (float)n_live : 0.f;
   for (int c = threadIdx.x; c < experts; c += kThreads) up[c] = per * (float)a.counts[c];
   __syncthreads();
-  uint8_t* row = tile + lane * pitch;
-  const int64_t tiles = (a.tokens + 31) / 32;
+  uint8_t* row = tile + r * pitch;
+  const int64_t tiles = (a.tokens + kRows - 1) / kRows;
   for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < tiles; i += (int64_t)gridDim.x * kWarps) {
-    const Tile<T> t = tile_at<T>(i, a.tokens, a.mask, lane);
+    const Tile t = tile_at(i, a.tokens, a.mask, r);
     if (a.dgates) {
-      const int n = (int)min((int64_t)32, a.tokens - t.t0) * k;
+      const int n = (int)min((int64_t)kRows, a.tokens - t.t0) * k;
       int l = lane / k, q = lane - l * k;
       const int dl = 32 / k, dq = 32 - dl * k;
       for (int i2 = lane; i2 < n; i2 += 32) {
-        idx[q * 33 + l] = a.indices[t.t0 * k + i2];
-        dg[q * 33 + l] = a.dgates[t.t0 * k + i2];
+        idx[q * kStride + l] = a.indices[t.t0 * k + i2];
+        dg[q * kStride + l] = a.dgates[t.t0 * k + i2];
         l += dl;
         q += dq;
         if (q >= k) {
@@ -478,49 +502,49 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
         }
       }
     }
+    const float2 st = t.live ? a.stats[t.t0 + r] : make_float2(0.f, 0.f);
     load_rows<T, NW>(tile, pitch, static_cast<const T*>(a.logits) + t.t0 * a.ld, a.ld, t.rows, experts, mode_in, lane);
-    const float2 st = t.live ? a.stats[t.t0 + lane] : make_float2(0.f, 0.f);
     const bool counted = st.y > 0.f;
     const int mine = counted ? experts : 0;
-    // the gates' gradient at the chosen probabilities, kept as p (what reaches p)
+    // the gates' gradient at the chosen probabilities, kept as what reaches p
     float dot = 0.f;
     if (a.dgates) {
       float s = 0.f;
-      for (int q = 0; q < k; ++q) {
-        const int at = t.live ? idx[q * 33 + lane] : -1;
+      for (int q = half; q < k; q += 2) {
+        const int at = t.live ? idx[q * kStride + r] : -1;
         if (at < 0 || at >= experts) continue;
         const float p = exp_neg(to_f32(reinterpret_cast<const T*>(row)[at]) - st.x) * st.y;
         s += p;
-        dot = fmaf(dg[q * 33 + lane], p, dot);
+        dot = fmaf(dg[q * kStride + r], p, dot);
       }
       if (a.normalize) {
         // gate_r = p_r / s: d p_r = (d gate_r - sum_j d gate_j gate_j) / s, whose sum with the p_r is zero
-        const float mean = dot / s, inv = 1.f / s;
-        for (int q = 0; q < k; ++q) dg[q * 33 + lane] = (dg[q * 33 + lane] - mean) * inv;
+        s = both(s);
+        const float mean = both(dot) / s, inv = 1.f / s;
+        for (int q = half; q < k; q += 2) dg[q * kStride + r] = (dg[q * kStride + r] - mean) * inv;
         dot = 0.f;
       }
     }
+    __syncwarp();  // the chosen logits have been read
     float d4[4] = {0.f, 0.f, 0.f, 0.f};
     if constexpr (sizeof(T) == 4) {  // the probabilities stay in the row
-      int j = 0;
-      for (; j + 4 <= mine; j += 4) {
-        float4 v = *reinterpret_cast<const float4*>(row + j * 4);
-        const float4 u = *reinterpret_cast<const float4*>(up + j);
-        v = make_float4(exp_neg(v.x - st.x) * st.y, exp_neg(v.y - st.x) * st.y, exp_neg(v.z - st.x) * st.y,
-                        exp_neg(v.w - st.x) * st.y);
-        d4[0] = fmaf(v.x, u.x, d4[0]);
-        d4[1] = fmaf(v.y, u.y, d4[1]);
-        d4[2] = fmaf(v.z, u.z, d4[2]);
-        d4[3] = fmaf(v.w, u.w, d4[3]);
-        *reinterpret_cast<float4*>(row + j * 4) = v;
-      }
-      for (; j < mine; ++j) {
-        float* p = reinterpret_cast<float*>(row) + j;
-        *p = exp_neg(*p - st.x) * st.y;
-        d4[0] = fmaf(*p, up[j], d4[0]);
-      }
+      each_four(row, half, mine,
+                [&](float4& p, int j) {
+                  const float4 u = *reinterpret_cast<const float4*>(up + j);
+                  const float4 v = make_float4(exp_neg(p.x - st.x) * st.y, exp_neg(p.y - st.x) * st.y,
+                                               exp_neg(p.z - st.x) * st.y, exp_neg(p.w - st.x) * st.y);
+                  d4[0] = fmaf(v.x, u.x, d4[0]);
+                  d4[1] = fmaf(v.y, u.y, d4[1]);
+                  d4[2] = fmaf(v.z, u.z, d4[2]);
+                  d4[3] = fmaf(v.w, u.w, d4[3]);
+                  p = v;
+                },
+                [&](float& p, int j) {
+                  p = exp_neg(p - st.x) * st.y;
+                  d4[0] = fmaf(p, up[j], d4[0]);
+                });
     } else {
-      walk<T>(row, mine,
+      walk<T>(row, half, mine,
               [&](int j, const float (&v)[V]) {
 #pragma unroll
                 for (int q = 0; q < V; ++q) d4[q % 4] = fmaf(exp_neg(v[q] - st.x), up[j + q], d4[q % 4]);
@@ -529,34 +553,30 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
     }
     float sum = (d4[0] + d4[1]) + (d4[2] + d4[3]);
     if (sizeof(T) == 2) sum *= st.y;
-    dot += sum;
+    dot = both(dot + sum);  // (and the row's other lane has written its probabilities)
     // the chosen logits' own gradients, before the row is written over
     if (a.dgates)
-      for (int q = 0; q < k; ++q) {
-        const int at = counted ? idx[q * 33 + lane] : -1;
+      for (int q = half; q < k; q += 2) {
+        const int at = counted ? idx[q * kStride + r] : -1;
         if (at < 0 || at >= experts) {
-          idx[q * 33 + lane] = -1;
+          idx[q * kStride + r] = -1;
           continue;
         }
         const float x = to_f32(reinterpret_cast<const T*>(row)[at]);
         const float p = sizeof(T) == 4 ? x : exp_neg(x - st.x) * st.y;
-        dg[q * 33 + lane] = p * (up[at] + dg[q * 33 + lane] - dot);
+        dg[q * kStride + r] = p * (up[at] + dg[q * kStride + r] - dot);
       }
-    if constexpr (sizeof(T) == 4) {
-      if (counted) {
-        int j = 0;
-        for (; j + 4 <= experts; j += 4) {
-          const float4 u = *reinterpret_cast<const float4*>(up + j);
-          float4 v = *reinterpret_cast<const float4*>(row + j * 4);
-          v = make_float4(v.x * (u.x - dot), v.y * (u.y - dot), v.z * (u.z - dot), v.w * (u.w - dot));
-          *reinterpret_cast<float4*>(row + j * 4) = v;
-        }
-        for (; j < experts; ++j) reinterpret_cast<float*>(row)[j] *= up[j] - dot;
-      }
-    } else {
-      if (counted) {
-        int j = 0;
-        for (; j + V <= experts; j += V) {
+    __syncwarp();
+    if (counted) {
+      if constexpr (sizeof(T) == 4) {
+        each_four(row, half, experts,
+                  [&](float4& p, int j) {
+                    const float4 u = *reinterpret_cast<const float4*>(up + j);
+                    p = make_float4(p.x * (u.x - dot), p.y * (u.y - dot), p.z * (u.z - dot), p.w * (u.w - dot));
+                  },
+                  [&](float& p, int j) { p *= up[j] - dot; });
+      } else {
+        for (int j = half * V; j + V <= experts; j += 2 * V) {
           Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(row + j * sizeof(T));
 #pragma unroll
           for (int q = 0; q < V; q += 2) {
@@ -566,22 +586,23 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
           }
           *reinterpret_cast<Pack<T, V>*>(row + j * sizeof(T)) = p;
         }
-        for (; j < experts; ++j) {
-          T* p = reinterpret_cast<T*>(row) + j;
-          *p = from_f32<T>(exp_neg(to_f32(*p) - st.x) * st.y * (up[j] - dot));
-        }
+        if (half)
+          for (int j = experts / V * V; j < experts; ++j) {
+            T* p = reinterpret_cast<T*>(row) + j;
+            *p = from_f32<T>(exp_neg(to_f32(*p) - st.x) * st.y * (up[j] - dot));
+          }
       }
-    }
-    if (!counted) {  // zeros, or NaN for a row that holds a NaN or +inf
+    } else {  // zeros, or NaN for a row that holds a NaN or +inf
       const T fill = from_f32<T>(t.live && st.y != st.y ? NAN : 0.f);
-      for (int j = 0; j < experts; ++j) reinterpret_cast<T*>(row)[j] = fill;
+      for (int j = half; j < experts; j += 2) reinterpret_cast<T*>(row)[j] = fill;
     }
+    __syncwarp();
     if (a.dgates)
-      for (int q = 0; q < k; ++q) {
-        const int at = idx[q * 33 + lane];
-        if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[q * 33 + lane]);
+      for (int q = half; q < k; q += 2) {
+        const int at = idx[q * kStride + r];
+        if (counted && at >= 0) reinterpret_cast<T*>(row)[at] = from_f32<T>(dg[q * kStride + r]);
       }
-    const uint32_t all = __ballot_sync(0xffffffffu, t.here);
+    const uint32_t all = __ballot_sync(0xffffffffu, t.here) & kRowBits;
     store_rows<T, NW>(tile, pitch, static_cast<T*>(a.dlogits) + t.t0 * a.ld_d, a.ld_d, all, experts, mode_out, lane);
   }
 }
@@ -589,10 +610,10 @@ __global__ void __launch_bounds__(kThreads) tile_bwd_kernel(const Backward a, co
 // ---- launches ------------------------------------------------------------------------------
 
 size_t fwd_smem(int experts, int k, int32_t type) {
-  return (size_t)kWarps * (32 * (pitch_of(row_bytes(experts, type)) + 8) + 33 * 8 * k) + (experts + 1) * 4;
+  return (size_t)kWarps * (kRows * (pitch_of(row_bytes(experts, type)) + 8) + kStride * 8 * k) + (experts + 1) * 4;
 }
 size_t bwd_smem(int experts, int k, int32_t type) {
-  return (experts * 4 + 15) / 16 * 16 + (size_t)kWarps * (32 * pitch_of(row_bytes(experts, type)) + 33 * 8 * k);
+  return (experts * 4 + 15) / 16 * 16 + (size_t)kWarps * (kRows * pitch_of(row_bytes(experts, type)) + kStride * 8 * k);
 }
 
 // Bytes that rows may move at once.
@@ -601,7 +622,7 @@ int mode_of(const void* p, int64_t ld, int experts, int32_t type) {
   return bytes % 16 == 0 ? 16 : bytes % 4 == 0 ? 4 : 2;
 }
 
-int per_sm(size_t smem) { return std::max(1, std::min(8, (int)(kSmemPerSm / (smem + 1024 + 64)))); }
+int per_sm(size_t smem) { return std::max(1, std::min(3, (int)(kSmemPerSm / (smem + 1024 + 64)))); }
 
 template <typename K>
 cudaError_t allow_smem(K kernel, std::atomic<uint64_t>& set) {
@@ -659,7 +680,7 @@ cudaError_t launch_bwd(const Backward& b, int32_t type, cudaStream_t s) {
   const cudaError_t e = allow_smem(kernel, set);
   if (e != cudaSuccess) return e;
   const size_t smem = bwd_smem(b.experts, b.k, type);
-  const int64_t want = (b.tokens + kThreads - 1) / kThreads;
+  const int64_t want = (b.tokens + kTokens - 1) / kTokens;
   const int ctas = (int)std::min<int64_t>(want, 152 * per_sm(smem));
   kernel<<<ctas, kThreads, smem, s>>>(b, mode_of(b.logits, b.ld, b.experts, type),
                                       mode_of(b.dlogits, b.ld_d, b.experts, type));
@@ -681,7 +702,7 @@ bool tile_fits(int64_t tokens, int experts, int k, int32_t type) {
 }
 
 int tile_forward_ctas(int64_t tokens, int experts, int k, int32_t type) {
-  const int64_t want = (tokens + kThreads - 1) / kThreads;
+  const int64_t want = (tokens + kTokens - 1) / kTokens;
   const int most = std::min(kTileCluster * kMaxParts, 152 * per_sm(fwd_smem(experts, k, type)));
   return (int)std::min<int64_t>(most / kTileCluster, (want + kTileCluster - 1) / kTileCluster) * kTileCluster;
 }
