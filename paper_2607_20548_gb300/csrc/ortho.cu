@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kThreads)
   if (threadIdx.x == 0) {
     const bool first = blockIdx.x == 0;
     if (first) done[b] = 0;
+    if (first && b == 0) done[gridDim.y] = 0;
     for (int w = 1; w < kThreads / 32; ++w) s += red[w];
     int e = 0;
     float f = 0.f;  // norm = f 2^e, f in [0.5, 1)
@@ -208,13 +209,7 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
   };
   p.part_off = take((size_t)batch * kMaxParts * (sizeof(double) + sizeof(float)));
   p.t_off = take((size_t)batch * sizeof(float));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
-  p.done_off = take((size_t)batch * sizeof(int));
+  p.done_off = take((size_t)(batch + 1) * sizeof(int));
   p.x_off[0] = take((size_t)p.x_elems * 2);
   p.x_off[1] = take((size_t)p.x_elems * 2);
   p.s_off = take((size_t)p.s_elems * 2);

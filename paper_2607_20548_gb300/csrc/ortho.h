@@ -27,7 +27,7 @@ struct Steps {
   __half *x[2], *s, *b;
   int ld_x, ld_s;
   const float* t;  // per matrix
-  int* done;       // per matrix, zero
+  int* done;       // per matrix, and the list's next place; zero
   void* out;       // out_type (soap_dtype_t), leading dimension, elements between matrices
   int out_type;
   int64_t ld_out, stride_out;

@@ -13,23 +13,30 @@
 // products. With 11-bit operands that is nothing; split ones keep the small products in an
 // accumulator of their own and take K in runs of at most 1024, whose sums the epilogue adds in fp32.
 //
-// Schedule. Persistent CTA pairs (cta_group::2, a pair's 256 x 256 tile has 128 rows in each CTA)
-// walk one list of tiles in turn: for each step all S tiles, then all B tiles, then all X' tiles. A
-// tile waits until its matrix's tiles of the phase before are stored, which a counter per matrix
-// tells; such a wait always points to tiles earlier in the list, so with all pairs resident (a
-// cooperative launch) it ends. Against a launch per product (measured at 64 matrices of 768 x 2048:
-// 337 us a step) this has no partly filled last wave per product and no launch latency.
+// Schedule. Persistent CTA pairs (cta_group::2, a pair's 256 x 256 tile has 128 rows in each CTA) take
+// tiles from one list, each its next one when it begins the one before: for each step all S tiles, then
+// all B tiles, then all X' tiles. (Every 76th tile for a pair, fixed in advance, takes 5% longer with 3
+// matrices of 2048 x 8192, where S tiles take four times as long as others, and 13% with 5 of 777 x 1365.) A
+// tile waits until its matrix's tiles of the phase before are stored, which a counter per matrix tells;
+// such a wait always points to tiles earlier in the list, which are taken, so with all pairs resident (a
+// cooperative launch) it ends. Against a launch per product (measured at 64 matrices of 768 x 2048: 337 us
+// a step, here 201) this has no partly filled last wave per product and no launch latency.
 //
-// In a CTA, warp 0 issues TMA loads of 64-element K slices into a ring, warp 1 (of the pair's first
-// CTA) the MMAs, and eight epilogue warps drain the accumulator, 32 x 64 elements at a time: C comes
-// in and the result leaves by TMA through shared memory, and a tile is reported stored while the
-// next one's C is on its way (plain stores and a fence per tile took 7 us of a tile's epilogue, more
-// than the MMAs of a tile with K = 768). An MMA that adds to the accumulator of the one before it
-// takes 140 cycles however narrow (measured), so tiles are 256 wide; the issuing thread has little
-// time beside it, so its loops are compiled for each pair of operand orders (with orders chosen at
-// run time a slice took 790 cycles in place of 540). Every
-// wait is bounded; one that runs out sets SOAP_STATUS_TIMEOUT and the CTA drains its copies, frees
-// its tensor memory and returns.
+// In a CTA, one warp takes tiles and waits for their inputs, two issue TMA loads of A's and B's 64-element K
+// slices into a ring (on the diagonal of S and B, A's alone: both operands are the same rows), one (of the
+// pair's first CTA) the MMAs, and eight drain the accumulator, 32 x 64 elements at a time: C comes in and
+// the result leaves by TMA through shared memory, and a tile is reported stored while the next one's C is
+// on its way (plain stores and a fence per tile took 7 us of a tile's epilogue, more than the MMAs of a
+// tile with K = 768). An MMA that adds to the accumulator of the one before it takes 140 cycles however
+// narrow (measured), so tiles are 256 wide; the issuing thread has little time beside it, so its loops are
+// compiled for each pair of operand orders (with orders chosen at run time a slice took 790 cycles in place
+// of 540). Every wait is bounded; one that runs out sets SOAP_STATUS_TIMEOUT and the CTA drains its copies,
+// frees its tensor memory and returns.
+//
+// What bounds it: at 8192 x 8192 the tensor cores (1.83 PFLOP/s, 0.95 of what a library product of that size
+// reaches); with K of 768 to 2048 the operands' way from L2 (1.3 to 1.6 PFLOP/s: with both loading threads
+// ahead and the ring full, the MMAs wait a quarter of the time for data); with a few matrices of a few tiles
+// the chain of phases, each the time of a tile and of handing it on (fp16 1365 x 777: 90 us a step).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -54,9 +61,11 @@ constexpr int kBox = 64 * 64 * 2;      // one TMA box: 64 rows of 128 bytes
 constexpr int kTile = 2 * kBox;        // a CTA's 128 x 64 elements of an operand
 constexpr int kRunBlocks = 16;         // most K slices per accumulator run of split operands
 constexpr int kEpiWarps = 8;
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kLoadB = 2 + kEpiWarps, kScout = kLoadB + 1;  // warps
+constexpr int kThreads = 32 * (kScout + 1);
 constexpr int kBlock = 32 * 128;       // a staged block: 32 rows of 128 bytes
 constexpr int kPerTile = 2 * kEpiWarps;       // what a tile adds to its matrix's counter
+constexpr int kTaken = 16;
 constexpr uint64_t kWaitNs = 2000000000ull;
 
 template <int SPLIT>
@@ -70,13 +79,14 @@ struct Config {
 };
 
 struct Maps {
-  CUtensorMap x[2], s, b;      // boxes of 64 x 64: operands
+  CUtensorMap xk[2], sk, bk;   // boxes of 64 columns x 128 rows: K-major operands
+  CUtensorMap x[2], s, b;      // boxes of 64 x 64: MN-major operands
   CUtensorMap ex[2], es, eb;   // boxes of 64 columns x 32 rows: C and results
 };
 
-// Tiles of the list. Groups of `group` matrices go through all steps one after the other.
+// The list.
 struct Layout {
-  int r, k, tall, group;
+  int r, k, tall;
   int ns, nx, nxm, nxn;  // tiles of S (and B), of X', row and column tiles of X'
   int total;
 };
@@ -85,6 +95,8 @@ struct Tile {
   int step, phase, b;     // phase 0: S, 1: B, 2: X'
   int m0, n0, M, N, K;
   int need;               // the matrix's counter before this tile may start
+  // S and B on the diagonal: both operands are the same rows, which are loaded once
+  __device__ __forceinline__ bool same() const { return phase < 2 && m0 == n0; }
 };
 
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
@@ -107,12 +119,12 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
       : "memory");
 }
 
-// 128 x 64 elements of an operand at (row m0, k0) as boxes of 64: rows of 64 K elements each
-// (K-major), or 64 K rows of 64 columns (MN-major).
+// 128 x 64 elements of an operand at (row m0, k0): 128 rows of 64 K elements (K-major), or two boxes of
+// 64 K rows of 64 columns (MN-major).
 template <int MN>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int m0, int k0, int z) {
   tma_box(dst, map, bar, MN ? m0 : k0, MN ? k0 : m0, z);
-  tma_box(dst + kBox, map, bar, MN ? m0 + 64 : k0, MN ? k0 : m0 + 64, z);
+  if (MN) tma_box(dst + kBox, map, bar, m0 + 64, k0, z);
 }
 
 // Descriptor of the 16 K elements at step kk of such a tile. K-major: 32 bytes further along the
@@ -220,6 +232,18 @@ __device__ __forceinline__ int get_ready(uint32_t at) {
   asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(at) : "memory");
   return n;
 }
+// The same across the pair.
+__device__ __forceinline__ bool wait_given(uint32_t at, int n) {
+  const uint64_t t0 = globaltimer();
+  for (;;) {
+    for (int i = 0; i < 64; ++i) {
+      int v;
+      asm volatile("ld.acquire.cluster.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+      if (v >= n) return true;
+    }
+    if (globaltimer() - t0 > 2 * kWaitNs) return false;
+  }
+}
 __device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
   const uint64_t t0 = globaltimer();
   for (;;) {
@@ -229,35 +253,17 @@ __device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
   }
 }
 
-// Step and phase of list entry p; i: its place among its group's tiles of that phase.
-__device__ __forceinline__ void phase_at(uint32_t p, const Layout& l, const Steps& a, int& group, int& step, int& phase,
-                                         uint32_t& i) {
-  const uint32_t per = 2 * l.ns + l.nx;  // of a matrix in a step
-  uint32_t n = a.batch, w = p;
-  group = 0;
-  if (l.group < a.batch) {
-    const uint32_t per_group = l.group * a.steps * per;
-    group = p / per_group;
-    w = p - group * per_group;
-    n = min(l.group, a.batch - group * l.group);  // the group's matrices
-  }
-  step = w / (n * per);
-  i = w - step * n * per;
-  const uint32_t ns = n * l.ns;
-  phase = i >= 2 * ns ? 2 : i >= ns ? 1 : 0;
-  i -= phase * ns;
-}
-
 __device__ __forceinline__ Tile tile_at(uint32_t p, const Layout& l, const Steps& a) {
   Tile t;
-  int g;
-  uint32_t i;
-  phase_at(p, l, a, g, t.step, t.phase, i);
-  t.need = (t.step * (2 * l.ns + l.nx) + t.phase * l.ns) * kPerTile;
+  const uint32_t per = 2 * l.ns + l.nx, ns = a.batch * l.ns;  // of a matrix in a step; of all in phase 0
+  t.step = p / (a.batch * per);
+  uint32_t i = p - t.step * a.batch * per;
+  t.phase = i >= 2 * ns ? 2 : i >= ns ? 1 : 0;
+  i -= t.phase * ns;
   const uint32_t each = t.phase == 2 ? l.nx : l.ns;
-  const uint32_t b = i / each;
-  i -= b * each;
-  t.b = b + g * l.group;
+  t.b = i / each;
+  i -= t.b * each;
+  t.need = (t.step * per + t.phase * l.ns) * kPerTile;
   if (t.phase < 2) {  // row by row of the triangle
     t.M = t.N = l.r;
     t.K = t.phase == 0 ? l.k : l.r;
@@ -413,21 +419,21 @@ struct Ring {
   bool ok = true;
 };
 
-// K slices kb .. to - 1 of a tile into the ring: rows am of A's map and bn of B's.
-template <int SPLIT, int A_MN, int B_MN>
-__device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUtensorMap* ma, const CUtensorMap* mb,
-                                            int am, int bn, int b, int batch, uint32_t ring, uint64_t* full,
-                                            uint64_t* empty, uint32_t leader_full, int rank) {
+// K slices kb .. to - 1 of an operand's 128 rows from `row` on into the ring at `ring`, the operand's place in
+// the first slot. bytes, if not 0: what this thread tells the barrier that a slot takes, all operands in both
+// CTAs. skip: only keeps pace.
+template <int SPLIT, int MN>
+__device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUtensorMap* map, int row, int b,
+                                            int batch, uint32_t ring, uint64_t* full, uint64_t* empty,
+                                            uint32_t leader_full, uint32_t bytes, bool skip) {
   using C = Config<SPLIT>;
   for (; kb < to; ++kb) {
     if (!(st.ok = mbar_wait(&empty[st.s], st.parity, kWaitNs))) return;
-    if (rank == 0) expect_tx(&full[st.s], 2 * C::kStage);
+    if (bytes) expect_tx(&full[st.s], bytes);
     const uint32_t at = ring + st.s * C::kStage, bar = leader_full + st.s * 8;
 #pragma unroll
-    for (int h = 0; h < SPLIT; ++h) {
-      load_tile<A_MN>(at + h * kTile, ma, bar, am, kb * BK, b + h * batch);
-      load_tile<B_MN>(at + (SPLIT + h) * kTile, mb, bar, bn, kb * BK, b + h * batch);
-    }
+    for (int h = 0; h < SPLIT; ++h)
+      if (!skip) load_tile<MN>(at + h * kTile, map, bar, row, kb * BK, b + h * batch);
     if (++st.s == C::kStages) {
       st.s = 0;
       st.parity ^= 1;
@@ -437,14 +443,14 @@ __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUte
 
 // `count` K slices from the ring into the accumulator at d (split: the small products at d + 256).
 template <int SPLIT, int A_MN, int B_MN>
-__device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t ring, uint64_t* full,
+__device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t b_at, uint32_t ring, uint64_t* full,
                                              uint64_t* empty, uint32_t d) {
   using C = Config<SPLIT>;
   constexpr uint32_t idesc = idesc_f16(A_MN, B_MN);
   for (; count > 0; --count) {
     if (!(st.ok = mbar_wait(&full[st.s], st.parity, kWaitNs))) return;
     tc_fence_after();
-    const uint32_t as = ring + st.s * C::kStage, bs = as + SPLIT * kTile;
+    const uint32_t as = ring + st.s * C::kStage, bs = as + b_at;
 #pragma unroll
     for (int kk = 0; kk < BK / 16; ++kk) {
       umma_f16(d, tile_desc<A_MN>(as, kk), tile_desc<B_MN>(bs, kk), idesc, more);
@@ -508,11 +514,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* cin_full = acc_empty + kAcc;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(cin_full + kEpiWarps * C::kBufs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
-  const uint32_t ready_at = smem_u32(tmem_at + 2);
+  const uint32_t ready_at = smem_u32(tmem_at + 2), begun_at = ready_at + 4, given_at = ready_at + 8;
+  // the list's places that this pair has taken, tile m's at m % kTaken (all roles of a pair are within the
+  // ring's slots and the accumulators of each other), -1 at the end
+  volatile int* taken = reinterpret_cast<volatile int*>(tmem_at + 5);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x & 1);  // in the pair
-  const int first = blockIdx.x / 2, stride = gridDim.x / 2;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -526,6 +534,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kEpiWarps * C::kBufs; ++i) mbar_init(&cin_full[i], 1);
     *abort_flag = 0;
     set_ready(ready_at, 0);
+    set_ready(begun_at, 0);
+    set_ready(given_at, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -538,39 +548,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
 
-  if (warp == 0) {
+  if (warp == kScout) {
+    // the pair's first CTA takes a tile as its loads of the one before begin, and tells the second; each then
+    // waits for the tile's inputs
     if (lane == 0) {
+      bool ok = true;
+      for (int m = 0; ok && !*abort_flag; ++m) {
+        int p;
+        if (rank == 0) {
+          if (!(ok = wait_ready(begun_at, m))) break;
+          p = atomicAdd(a.done + a.batch, 1);
+          if (p >= l.total) p = -1;
+          uint32_t peer;
+          asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at)));
+          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer + 20 + 4 * (m % kTaken)), "r"(p) : "memory");
+          asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 16), "r"(m + 1) : "memory");
+          taken[m % kTaken] = p;
+        } else {
+          if (!(ok = wait_given(given_at, m + 1))) break;
+          p = taken[m % kTaken];
+        }
+        if (p >= 0) {
+          const Tile t = tile_at(p, l, a);
+          if (!(ok = wait_done(a.done + t.b, t.need))) break;
+          asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
+        }
+        set_ready(ready_at, m + 1);
+        if (p < 0) break;
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        if (a.status) atomicOr(a.status, kStatusTimeout);
+      }
+    }
+  } else if (warp == 0 || warp == kLoadB) {
+    if (lane == 0) {
+      const bool is_b = warp == kLoadB;
       Ring st;
       st.parity = 1;  // of a slot's release
       int used = 0;   // slots filled so far (up to kStages)
-      const uint32_t ring = smem_u32(smem), bars = in_leader(full);
-      int ready = 0;
-      for (int p = first; p < l.total && st.ok && !*abort_flag; p += stride) {
+      const uint32_t ring = smem_u32(smem) + (is_b ? SPLIT * kTile : 0), bars = in_leader(full);
+      for (int m = 0; !*abort_flag; ++m) {
+        if (!(st.ok = wait_ready(ready_at, m + 1))) break;
+        const int p = taken[m % kTaken];
+        if (p < 0) break;
+        if (!is_b) set_ready(begun_at, m + 1);
         const Tile t = tile_at(p, l, a);
         const int kblocks = (t.K + BK - 1) / BK;
         int a_change, b_change;
         order_change(t, l.tall, kblocks, a_change, b_change);
-        const CUtensorMap* x = &maps.x[t.step & 1];
-        const CUtensorMap* ma = t.phase == 0 ? x : t.phase == 1 ? &maps.s : l.tall ? x : &maps.b;
-        const CUtensorMap* mb = t.phase == 0 ? x : t.phase == 1 ? &maps.s : l.tall ? &maps.b : x;
-        if (!(st.ok = wait_done(a.done + t.b, t.need))) break;
-        asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
-        set_ready(ready_at, ++ready);
-        const int am = t.m0 + rank * 128, bn = t.n0 + rank * 128;
+        const int change = is_b ? b_change : a_change;
+        const bool of_x = t.phase == 0 || (t.phase == 2 && is_b == !l.tall);
+        const CUtensorMap* mk = of_x ? &maps.xk[t.step & 1] : t.phase == 1 ? &maps.sk : &maps.bk;
+        const CUtensorMap* mn = of_x ? &maps.x[t.step & 1] : t.phase == 1 ? &maps.s : &maps.b;
+        const int row = (is_b ? t.n0 : t.m0) + rank * 128;
+        const uint32_t bytes = rank != 0 || is_b ? 0 : (t.same() ? 1 : 2) * Config<SPLIT>::kStage;
+        const bool skip = is_b && t.same();
         used = min(used + kblocks, kStages);
-        for (int kb = 0; kb < kblocks && st.ok;) {  // stretches of slices of one order
-          const bool a_mn = kb >= a_change, b_mn = kb >= b_change;
-          const int to = min(a_mn ? kblocks : a_change, b_mn ? kblocks : b_change);
-          if (a_mn && b_mn)
-            load_slices<SPLIT, 1, 1>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
-          else if (a_mn)
-            load_slices<SPLIT, 1, 0>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
-          else if (b_mn)
-            load_slices<SPLIT, 0, 1>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
-          else
-            load_slices<SPLIT, 0, 0>(st, kb, to, ma, mb, am, bn, t.b, a.batch, ring, full, empty, bars, rank);
-          kb = to;
-        }
+        if (change > 0)
+          load_slices<SPLIT, 0>(st, 0, change, mk, row, t.b, a.batch, ring, full, empty, bars, bytes, skip);
+        if (st.ok && change < kblocks)
+          load_slices<SPLIT, 1>(st, change, kblocks, mn, row, t.b, a.batch, ring, full, empty, bars, bytes, skip);
+        if (!st.ok) break;
       }
       // every slice consumed, and its release arrived here, before this CTA's barriers go away
       for (int i = 0; i < kStages && st.ok && !*abort_flag; ++i) {
@@ -593,11 +632,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Ring st;
       int n = 0;
       const uint32_t ring = smem_u32(smem);
-      for (int p = first; p < l.total && st.ok && !*abort_flag; p += stride) {
+      for (int m = 0; st.ok && !*abort_flag; ++m) {
+        if (!(st.ok = wait_ready(ready_at, m + 1))) break;
+        const int p = taken[m % kTaken];
+        if (p < 0) break;
         const Tile t = tile_at(p, l, a);
         const int kblocks = (t.K + BK - 1) / BK;
         int a_change, b_change;
         order_change(t, l.tall, kblocks, a_change, b_change);
+        const uint32_t b_at = t.same() ? 0 : SPLIT * kTile;
         const int runs = SPLIT == 2 ? (kblocks + kRunBlocks - 1) / kRunBlocks : 1;
         for (int run = 0; run < runs && st.ok; ++run, ++n) {
           const int ac = n % kAcc;
@@ -611,13 +654,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const bool a_mn = kb >= a_change, b_mn = kb >= b_change;
             const int to = min(k1, min(a_mn ? k1 : a_change, b_mn ? k1 : b_change));
             if (a_mn && b_mn)
-              issue_slices<SPLIT, 1, 1>(st, to - kb, more, ring, full, empty, d);
+              issue_slices<SPLIT, 1, 1>(st, to - kb, more, b_at, ring, full, empty, d);
             else if (a_mn)
-              issue_slices<SPLIT, 1, 0>(st, to - kb, more, ring, full, empty, d);
+              issue_slices<SPLIT, 1, 0>(st, to - kb, more, b_at, ring, full, empty, d);
             else if (b_mn)
-              issue_slices<SPLIT, 0, 1>(st, to - kb, more, ring, full, empty, d);
+              issue_slices<SPLIT, 0, 1>(st, to - kb, more, b_at, ring, full, empty, d);
             else
-              issue_slices<SPLIT, 0, 0>(st, to - kb, more, ring, full, empty, d);
+              issue_slices<SPLIT, 0, 0>(st, to - kb, more, b_at, ring, full, empty, d);
             kb = to;
           }
           if (st.ok) commit_pair(&acc_full[ac]);
@@ -676,11 +719,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         store_user_any(st, v, a, out_vec, w.t.b, w.r0, c0, min(32, w.t.M - w.r0), min(32, w.t.N - c0), lane);
     };
     const int wr = rank * 128 + 32 * q, wc = 128 * half;  // this warp's place in a tile
-    Work w = work_at(tile_at(first, l, a), a, maps, wr, wc);
-    bool asked = false;  // the first block's C is on its way
-    int m = 0;           // tiles so far
-    for (int p = first; p < l.total; p += stride, ++m) {
-      if (!asked) {
+    Work w{}, next{};
+    bool known = false;  // w is the next tile, and the first block of its C is on its way if it takes any
+    for (int m = 0;; ++m) {
+      if (!known) {
         // a tile that has to wait may wait for this warp's own last one: that is reported first
         int there = lane == 0 ? get_ready(ready_at) : 0;
         if (__shfl_sync(0xffffffffu, there, 0) <= m) {
@@ -688,15 +730,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (lane == 0) ok = wait_ready(ready_at, m + 1);
           if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
         }
+        __syncwarp();
+        const int p = taken[m % kTaken];
+        if (p < 0) break;
+        w = work_at(tile_at(p, l, a), a, maps, wr, wc);
         if (w.has_c) {
           if (lane == 0) sent_read<0>();
           fetch(w, 0, SPLIT - 1, k % C::kBufs);
         }
       }
-      const bool more = p + stride < l.total;
-      Work next = w;
-      if (more) next = work_at(tile_at(p + stride, l, a), a, maps, wr, wc);
-      asked = false;
+      known = false;
       const float alpha = w.alpha, beta = w.beta;
       if constexpr (SPLIT == 1) {
         const int ac = n % kAcc;
@@ -714,12 +757,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               if (lane == 0) sent_read<0>();
               fetch(w, i + 1, 0, buf ^ 1);
             }
-          } else if (more && next.has_c) {
+          } else {
             const int there = lane == 0 ? get_ready(ready_at) : 0;
-            asked = __shfl_sync(0xffffffffu, there, 0) > m + 1;
-            if (asked) {
-              if (lane == 0) sent_read<0>();
-              fetch(next, 0, 0, buf ^ 1);
+            if (__shfl_sync(0xffffffffu, there, 0) > m + 1) {
+              __syncwarp();
+              const int p = taken[(m + 1) % kTaken];
+              if (p >= 0) {
+                known = true;
+                next = work_at(tile_at(p, l, a), a, maps, wr, wc);
+                if (next.has_c) {
+                  if (lane == 0) sent_read<0>();
+                  fetch(next, 0, 0, buf ^ 1);
+                }
+              }
             }
           }
           if (w.has_c) {
@@ -814,7 +864,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
       }
       unreported = a.done + w.t.b;
-      w = next;
+      if (known) w = next;
     }
     if (ok) report(std::integral_constant<int, 0>());
     if (!ok) {
@@ -893,7 +943,7 @@ cudaError_t launch(const Maps& maps, const Steps& p, const Layout& l, int out_ve
     if (dev >= 0 && dev < 64) pairs_of[dev].store(pairs, std::memory_order_relaxed);
   }
   // no more pairs than the longest phase has tiles
-  const int64_t most = (int64_t)l.group * std::max(l.ns, l.nx);
+  const int64_t most = (int64_t)p.batch * std::max(l.ns, l.nx);
   cfg.gridDim = dim3((unsigned)(2 * std::min<int64_t>(pairs, most)));
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, steps_kernel<SPLIT>, maps, p, l, out_vec);
@@ -911,20 +961,20 @@ cudaError_t run_steps(const Steps& p, cudaStream_t s) {
   l.nxm = (p.rows + 255) / 256;
   l.nxn = (p.cols + 255) / 256;
   l.nx = l.nxm * l.nxn;
-  l.group = p.batch;
   const int64_t per = 2 * (int64_t)l.ns + l.nx;
-  if (per * p.batch * p.steps > INT32_MAX / kPerTile) l.group = 1;
-  if (per * l.group * p.steps > INT32_MAX / kPerTile) return cudaErrorInvalidValue;
-  if (per * p.batch * p.steps > INT32_MAX - 1024) return cudaErrorInvalidValue;
+  if (per * p.steps > INT32_MAX / kPerTile || per * p.batch * p.steps > INT32_MAX - 1024)
+    return cudaErrorInvalidValue;
   l.total = (int)(per * p.batch * p.steps);
 
   const int planes = p.batch * (p.split ? 2 : 1);
   Maps maps;
   for (int i = 0; i < 2; ++i)
     if (!make_map(&maps.x[i], p.x[i], p.rows, p.cols, p.ld_x, planes, 64) ||
+        !make_map(&maps.xk[i], p.x[i], p.rows, p.cols, p.ld_x, planes, 128) ||
         !make_map(&maps.ex[i], p.x[i], p.rows, p.cols, p.ld_x, planes, 32))
       return cudaErrorInvalidValue;
-  if (!make_map(&maps.s, p.s, l.r, l.r, p.ld_s, planes, 64) || !make_map(&maps.es, p.s, l.r, l.r, p.ld_s, planes, 32) ||
+  if (!make_map(&maps.sk, p.s, l.r, l.r, p.ld_s, planes, 128) ||
+      !make_map(&maps.bk, p.b, l.r, l.r, p.ld_s, planes, 128) || !make_map(&maps.s, p.s, l.r, l.r, p.ld_s, planes, 64) || !make_map(&maps.es, p.s, l.r, l.r, p.ld_s, planes, 32) ||
       !make_map(&maps.b, p.b, l.r, l.r, p.ld_s, planes, 64) || !make_map(&maps.eb, p.b, l.r, l.r, p.ld_s, planes, 32))
     return cudaErrorInvalidValue;
   const size_t size = dtype_size(p.out_type);
