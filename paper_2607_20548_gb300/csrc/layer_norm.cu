@@ -9,20 +9,20 @@ namespace {
 // ---- forward: a group of blockDim.x threads per row, NV packs of V elements each ------------
 
 // FULL: the group's threads have exactly the row's elements.
-template <typename T, typename W, int V, int NV, int DEPTH, bool FULL>
-__global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
+template <typename T, typename W, int V, int NV, int DEPTH, bool FULL, bool RING>
+__global__ void __launch_bounds__(threads_for(NV * V), 1)
     norm_fwd_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
                     float* mean, float* rstd, int rows, int width, int* status) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 buf[2 * 32];
   __shared__ uint64_t full[kMaxGroups][DEPTH];
   constexpr int P = NV * V / 2, kPer = V == 1 ? 2 : 1;
-  using Feed = Rows<T, V, NV, 1, DEPTH, FULL>;
+  using Feed = Rows<T, V, NV, 1, DEPTH, FULL, RING>;
   const int lane = threadIdx.x & 31;
   Exchange ex{buf};
   const int step = gridDim.x * blockDim.y;
   int row = blockIdx.x * blockDim.y + threadIdx.y;
-  Feed in{{x}, {ld_x}, rows, step, width, smem + (size_t)threadIdx.y * blockDim.x * Feed::kRing, full[threadIdx.y], status};
+  Feed in{{x}, {ld_x}, rows, step, width, smem + threadIdx.y * Feed::ring_bytes(blockDim.x), full[threadIdx.y], status};
   in.start(row);
   float2 w[P], b[P];
   columns<W, V, NV>(weight, 1.f, width, w);
@@ -115,24 +115,25 @@ __global__ void __launch_bounds__(kMaxThreads)
 template <typename T, typename W, int V>
 cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W* w, const W* b, float eps, T* y,
                   int64_t ld_y, float* mean, float* rstd, int* status, cudaStream_t s) {
-  constexpr bool kBulk = V * sizeof(T) == 16;
-  const NormShape n = norm_shape(width, V, kBulk, !many_rows(rows) ? 8 : kBulk ? 32 : 16, 32);
+  const NormShape n = norm_shape(width, V, !many_rows(rows) ? 8 : V * sizeof(T) == 16 ? 32 : 16, 32);
   if (n.nv == 0) {
     norm_fwd_wide_kernel<T, W><<<(unsigned)rows, kMaxThreads, 0, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, width);
     return cudaGetLastError();
   }
-  const int ty = norm_groups(rows, n, V, kBulk);
+  const int ty = norm_groups(rows, n, V);
   const unsigned grid = (unsigned)norm_ctas(rows, n, V, ty);
   return with_nv(n.nv, [&](auto nv) {
     constexpr int NV = decltype(nv)::value, DEPTH = NV * V * sizeof(T) > 64 ? 3 : 4;
     if constexpr (NV * V <= 32 && NV * V > 1) {
-      const int smem = n.tx * ty * Rows<T, V, NV, 1, DEPTH, false>::kRing;
-      return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
+      return with_full<V, NV * V>(width == (int64_t)n.tx * NV * V, n.tx, [&](auto full, auto ring) {
         static std::atomic<uint64_t> set{0};
-        const auto kernel = norm_fwd_kernel<T, W, V, NV, DEPTH, decltype(full)::value>;
+        constexpr bool kFull = decltype(full)::value, kRing = decltype(ring)::value;
+        const int smem = ty * Rows<T, V, NV, 1, DEPTH, kFull, kRing>::ring_bytes(n.tx);
+        const auto kernel = norm_fwd_kernel<T, W, V, NV, DEPTH, kFull, kRing>;
         const cudaError_t e = allow_smem(kernel, smem, set);
         if (e != cudaSuccess) return e;
-        kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, (int)rows, (int)width, status);
+        kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, (int)rows, (int)width,
+                                                  status);
         return cudaGetLastError();
       });
     }
@@ -146,7 +147,8 @@ cudaError_t fwd_t(int64_t rows, int64_t width, const void* x, int64_t ld_x, cons
   const uintptr_t bytes = address(x) | address(y) | (ld_x | ld_y | width) * sizeof(T);
   return with_access<T>(bytes, [&](auto v) {
     return fwd_v<T, W, decltype(v)::value>(rows, width, static_cast<const T*>(x), ld_x, static_cast<const W*>(w),
-                                           static_cast<const W*>(b), eps, static_cast<T*>(y), ld_y, mean, rstd, status, s);
+                                           static_cast<const W*>(b), eps, static_cast<T*>(y), ld_y, mean, rstd, status,
+                                           s);
   });
 }
 

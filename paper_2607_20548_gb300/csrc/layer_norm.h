@@ -6,9 +6,12 @@
 // (not E[x^2] - mu^2, which cancels) and nothing is read twice. CTAs are persistent: each thread
 // keeps its columns' weights (backward: and their gradients' sums) in registers over all its rows
 // (read again for every row, fp32 weights are four times the traffic of a bf16 x through L1: 345 us
-// at 32768 x 8192), and rows come in ahead, where they are 16-byte aligned by bulk copies into a ring
-// in shared memory (asynchronous 16-byte copies by every thread stopped at 2.7 TB/s of reads),
-// else, a row ahead, into registers. Pairs of elements go through the fp32 pipe together.
+// at 32768 x 8192), and rows come in ahead by bulk copies into a ring in shared memory (asynchronous
+// 16-byte copies by every thread stopped at 2.7 TB/s of reads). A bulk copy moves whole 16-byte units:
+// of rows that begin or end inside one, the neighbour's part comes along, except before the first row and
+// after the last. Narrow rows, a warp's each, are short of work per copy: they come, a row ahead, into
+// registers (60000 x 100 bf16: 16 us forward, 20 backward; by bulk copies 20 and 26). Pairs of elements go
+// through the fp32 pipe together.
 #pragma once
 
 #include <algorithm>
@@ -24,9 +27,8 @@ namespace soap {
 namespace {
 
 constexpr int kMaxThreads = 512;  // of the kernels for rows too wide to be held
-// A CTA's threads by the elements of a row that each holds (`bulk`: rows come through shared memory, not
-// registers): few registers, twice the threads.
-constexpr int threads_for(int elems, bool bulk) { return elems <= 8 && bulk ? 1024 : 512; }
+// A CTA's threads by the elements of a row that each holds: few registers, twice the threads.
+constexpr int threads_for(int elems) { return elems <= 8 ? 1024 : 512; }
 constexpr int kMaxGroups = 16;    // row groups of a CTA
 constexpr int64_t kMaxRows = INT32_MAX - 65536;  // a row index some steps further on stays an int
 constexpr uint64_t kWaitNs = 2000000000ull;
@@ -61,99 +63,146 @@ struct Exchange {
 
 // The rows of N matrices (x; or x and dy) for a row group, up to DEPTH rows ahead, NV packs of V elements
 // per thread and row.
-template <typename T, int V, int NV, int N, int DEPTH, bool FULL>
+template <typename T, int V, int NV, int N, int DEPTH, bool FULL, bool RING>
 struct Rows {
-  static constexpr bool kBulk = V * sizeof(T) == 16;  // a ring in shared memory; else registers
-  static constexpr int kRowBytes = NV * 16;           // of the ring, per thread
-  static constexpr int kRing = kBulk ? DEPTH * N * kRowBytes : 0;  // bytes per thread
+  static constexpr bool kWhole = V * sizeof(T) == 16;  // rows are whole 16-byte units
   const T* base[N];
   int64_t ld[N];
   int rows, step, width;
-  uint8_t* ring;    // the group's: row slot q at q * blockDim.x * kRowBytes
+  uint8_t* ring;    // the group's: ring_bytes
   uint64_t* full;   // the group's barriers, one per stage
   int* status;
   int s = 0;
   uint32_t parity = 0;
   bool dead = false;  // a wait ran out: what follows is invalid, and waits for nothing
-  Pack<T, V> ahead[kBulk ? 1 : N][kBulk ? 1 : NV];
+  Pack<T, V> ahead[RING ? 1 : N][RING ? 1 : NV];
+
+  // Of a group of `threads`: a row, and the parts of its neighbours that come along.
+  static __host__ __device__ constexpr int slot_bytes(int threads) {
+    return threads * NV * V * (int)sizeof(T) + (kWhole ? 0 : 32);
+  }
+  static __host__ __device__ constexpr int ring_bytes(int threads) {
+    return RING ? DEPTH * N * slot_bytes(threads) : 0;
+  }
 
   __device__ __forceinline__ uint8_t* slot(int stage, int n) const {
-    return ring + (size_t)(stage * N + n) * blockDim.x * kRowBytes;
+    return ring + (stage * N + n) * slot_bytes(blockDim.x);
+  }
+  static __device__ __forceinline__ void copy(uint8_t* dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+            tc::smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(bar)
+        : "memory");
   }
   // One thread asks for a row into a stage.
   __device__ __forceinline__ void request(int row, int stage) {
     if (row >= rows) return;
-    const uint32_t bytes = (uint32_t)width * sizeof(T), bar = tc::smem_u32(full + stage);
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(N * bytes) : "memory");
+    const uint32_t bar = tc::smem_u32(full + stage);
+    if constexpr (kWhole) {
+      const uint32_t bytes = (uint32_t)width * sizeof(T);
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(N * bytes) : "memory");
 #pragma unroll
-    for (int m = 0; m < N; ++m)
-      asm volatile(
-          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-              tc::smem_u32(slot(stage, m))),
-          "l"(base[m] + (int64_t)row * ld[m]), "r"(bytes), "r"(bar)
-          : "memory");
-  }
-  __device__ __forceinline__ void load(int row) {
-    if constexpr (!kBulk) {
-#pragma unroll
-      for (int m = 0; m < N; ++m)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int c = (i * blockDim.x + threadIdx.x) * V;
-          if (row < rows && c < width) {
-            ahead[m][i] = *reinterpret_cast<const Pack<T, V>*>(base[m] + (int64_t)row * ld[m] + c);
-          } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) ahead[m][i].v[e] = from_f32<T>(0.f);
-          }
-        }
-    }
-  }
-  // Before the first row: called by all threads of the CTA.
-  __device__ __forceinline__ void start(int row) {
-    if constexpr (kBulk) {
-      if (threadIdx.x == 0) {
-        for (int q = 0; q < DEPTH; ++q) tc::mbar_init(full + q, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int q = 0; q < DEPTH; ++q) request(row + q * step, q);
-      }
-      __syncthreads();
+      for (int m = 0; m < N; ++m) copy(slot(stage, m), base[m] + (int64_t)row * ld[m], bytes, bar);
     } else {
-      load(row);
-    }
-  }
-  // The row, zero beyond its end.
-  __device__ __forceinline__ void get(int row, Pack<T, V> (&p)[N][NV]) {
-    if constexpr (kBulk) {
-      if (!dead && !tc::mbar_wait(full + s, parity, kWaitNs)) {
-        dead = true;
-        if (status) atomicOr(status, SOAP_STATUS_TIMEOUT);
+      uintptr_t lo[N], hi[N];
+      uint32_t bytes = 0;
+#pragma unroll
+      for (int m = 0; m < N; ++m) {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(base[m] + (int64_t)row * ld[m]);
+        const uintptr_t end = begin + (uintptr_t)width * sizeof(T);
+        lo[m] = begin & ~uintptr_t(15);
+        hi[m] = (end + 15) & ~uintptr_t(15);
+        if (row == 0 || row == rows - 1) {  // nothing from before the first row or after the last
+          uint8_t* const dst = slot(stage, m);
+          const uintptr_t at = lo[m];
+          if (row == 0 && lo[m] < begin) lo[m] += 16;
+          if (row == rows - 1 && hi[m] > end) hi[m] -= 16;
+          if (hi[m] < lo[m]) hi[m] = lo[m];
+          for (uintptr_t a = begin; a < end; a += sizeof(T))
+            if (a < lo[m] || a >= hi[m]) {
+              *reinterpret_cast<T*>(dst + (a - at)) = *reinterpret_cast<const T*>(a);
+            } else {
+              a = hi[m] - sizeof(T);
+            }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before later copies to the place
+        }
+        bytes += (uint32_t)(hi[m] - lo[m]);
+      }
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+#pragma unroll
+      for (int m = 0; m < N; ++m) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(base[m] + (int64_t)row * ld[m]) & ~uintptr_t(15);
+        if (hi[m] > lo[m])
+          copy(slot(stage, m) + (lo[m] - at), reinterpret_cast<const void*>(lo[m]), (uint32_t)(hi[m] - lo[m]), bar);
       }
     }
+  }
+  // A row into registers, zero beyond its end.
+  __device__ __forceinline__ void load(int row) {
 #pragma unroll
     for (int m = 0; m < N; ++m)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
+        const int c = (i * blockDim.x + threadIdx.x) * V;
+        if (row < rows && c < width) {
+          ahead[m][i] = *reinterpret_cast<const Pack<T, V>*>(base[m] + (int64_t)row * ld[m] + c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) ahead[m][i].v[e] = from_f32<T>(0.f);
+        }
+      }
+  }
+  // Before the first row: called by all threads of the CTA.
+  __device__ __forceinline__ void start(int row) {
+    if constexpr (!RING) {
+      load(row);
+      return;
+    }
+    if (threadIdx.x == 0) {
+      for (int q = 0; q < DEPTH; ++q) tc::mbar_init(full + q, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      for (int q = 0; q < DEPTH; ++q) request(row + q * step, q);
+    }
+    __syncthreads();
+  }
+  // The row, zero beyond its end.
+  __device__ __forceinline__ void get(int row, Pack<T, V> (&p)[N][NV]) {
+    if constexpr (!RING) {
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) p[m][i] = ahead[m][i];
+      load(row + step);
+      return;
+    }
+    if (!dead && !tc::mbar_wait(full + s, parity, kWaitNs)) {
+      dead = true;
+      if (status) atomicOr(status, SOAP_STATUS_TIMEOUT);
+    }
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      const uint8_t* from = slot(s, m);
+      if constexpr (!kWhole) from += reinterpret_cast<uintptr_t>(base[m] + (int64_t)row * ld[m]) & 15;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
         const int c = i * blockDim.x + threadIdx.x;
-        if constexpr (!kBulk) {
-          p[m][i] = ahead[m][i];
-        } else if (FULL || c * V < width) {
-          p[m][i] = *reinterpret_cast<const Pack<T, V>*>(slot(s, m) + c * 16);
+        if (FULL || c * V < width) {
+          p[m][i] = reinterpret_cast<const Pack<T, V>*>(from)[c];
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) p[m][i].v[e] = from_f32<T>(0.f);
         }
       }
-    load(row + step);
+    }
   }
   // After a point that all of the group's threads have reached since get(): the slots are free.
   __device__ __forceinline__ void refill(int row) {
-    if constexpr (kBulk) {
-      if (threadIdx.x == 0) request(row + DEPTH * step, s);
-      if (++s == DEPTH) {
-        s = 0;
-        parity ^= 1;
-      }
+    if constexpr (!RING) return;
+    if (threadIdx.x == 0) request(row + DEPTH * step, s);
+    if (++s == DEPTH) {
+      s = 0;
+      parity ^= 1;
     }
   }
   __device__ __forceinline__ void finish() const {
@@ -235,12 +284,12 @@ struct NormShape {
 // Threads for a row of `width` elements in accesses of v: a warp where 16 elements per thread are
 // enough, else the fewest that give a thread no more than `elems` elements, or more up to `most` where
 // the row needs it. nv = 0: too wide for that.
-NormShape norm_shape(int64_t width, int v, bool bulk, int elems, int most) {
+NormShape norm_shape(int64_t width, int v, int elems, int most) {
   const int64_t packs = (width + v - 1) / v;
   for (int nv = v == 1 ? 2 : 1; nv * v <= 16; nv *= 2)
     if (packs <= 32 * nv) return {nv, 32};
   for (int e = elems; e <= most; e *= 2)
-    for (int tx = 64; tx <= threads_for(e, bulk); tx *= 2)
+    for (int tx = 64; tx <= threads_for(e); tx *= 2)
       if (packs * v <= (int64_t)tx * e) return {e / v, tx};
   return {0, 0};
 }
@@ -251,11 +300,11 @@ NormShape norm_shape(int64_t width, int v, bool bulk, int elems, int most) {
 // sums take registers too, 495, 472 and spills).
 bool many_rows(int64_t rows) { return rows >= 16 * kSms; }
 
-int norm_threads(const NormShape& n, int v, bool bulk) { return n.tx >= 128 ? threads_for(n.nv * v, bulk) : 512; }
+int norm_threads(const NormShape& n, int v) { return n.tx >= 128 ? threads_for(n.nv * v) : 512; }
 
 // Rows per CTA: full CTAs, unless the rows would then not reach every SM.
-int norm_groups(int64_t rows, const NormShape& n, int v, bool bulk) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(norm_threads(n, v, bulk) / n.tx, (rows + kSms - 1) / kSms));
+int norm_groups(int64_t rows, const NormShape& n, int v) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(norm_threads(n, v) / n.tx, (rows + kSms - 1) / kSms));
 }
 
 // CTAs: two per SM where one does not fill it.
@@ -286,11 +335,19 @@ cudaError_t with_access(uintptr_t bytes, F&& f) {
   return f(std::integral_constant<int, 1>());
 }
 
-// f(whether the row has exactly the group's elements): told apart for the widest accesses.
-template <int V, typename F>
-cudaError_t with_full(bool full, F&& f) {
-  if (V >= 4 && full) return f(std::integral_constant<bool, (V >= 4)>());
-  return f(std::integral_constant<bool, false>());
+// f(whether the row has exactly the group's elements, whether rows come through shared memory): the first
+// told apart for the widest accesses. Through registers go a warp's rows of up to 8 elements per thread (with
+// 16, 20000 x 511 fp32 takes 27 us forward and 45 backward, through shared memory 25 and 33); more threads
+// per row have 8 elements each at least.
+template <int V, int E, typename F>
+cudaError_t with_full(bool full, int tx, F&& f) {
+  if constexpr (E >= 8)
+    if (E > 8 || tx > 32) {
+      if (V >= 4 && full) return f(std::integral_constant<bool, (V >= 4)>(), std::true_type());
+      return f(std::false_type(), std::true_type());
+    }
+  if constexpr (E <= 8) return f(std::false_type(), std::false_type());
+  return cudaErrorInvalidValue;
 }
 
 uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }

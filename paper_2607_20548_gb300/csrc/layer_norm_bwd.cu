@@ -16,8 +16,8 @@ namespace {
 // A thread keeps its row's packs and converts them twice. Weights that registers would not hold beside
 // both sums (more than 16 elements per thread) are in shared memory. (Two rows per iteration spilled
 // registers: 360 us in place of 258 at 32768 x 8192.)
-template <typename T, typename W, int V, int NV, int DEPTH, bool FULL>
-__global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
+template <typename T, typename W, int V, int NV, int DEPTH, bool FULL, bool RING>
+__global__ void __launch_bounds__(threads_for(NV * V), 1)
     norm_bwd_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
                     const W* weight, T* dx, int64_t ld_dx, float* part, int rows, int width,
                     int* status) {
@@ -26,13 +26,13 @@ __global__ void __launch_bounds__(threads_for(NV * V, V * sizeof(T) == 16))
   __shared__ uint64_t full[kMaxGroups][DEPTH];
   constexpr int E = NV * V, P = E / 2, kPer = V == 1 ? 2 : 1;
   constexpr bool kSmemW = E > 16;
-  using Feed = Rows<T, V, NV, 2, DEPTH, FULL>;
+  using Feed = Rows<T, V, NV, 2, DEPTH, FULL, RING>;
   const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
-  float2* const weights = reinterpret_cast<float2*>(smem + (size_t)threads * Feed::kRing);  // [P][blockDim.x]
+  float2* const weights = reinterpret_cast<float2*>(smem + blockDim.y * Feed::ring_bytes(blockDim.x));  // [P][blockDim.x]
   const int step = gridDim.x * blockDim.y;
   int row = blockIdx.x * blockDim.y + threadIdx.y;
   Feed in{{x, dy},    {ld_x, ld_dy}, rows,
-          step,       width,         smem + (size_t)threadIdx.y * blockDim.x * Feed::kRing,
+          step,       width,         smem + threadIdx.y * Feed::ring_bytes(blockDim.x),
           full[threadIdx.y], status};
   in.start(row);
   Exchange ex{buf};
@@ -197,8 +197,8 @@ template <typename T, typename W, int V>
 cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x,
                   const float* mean, const float* rstd, const W* w, T* dx, int64_t ld_dx, float* dw, float* db,
                   float* part, int* status, cudaStream_t s) {
-  constexpr bool kBulk = V * sizeof(T) == 16;
-  const NormShape n = norm_shape(width, V, kBulk, kBulk && many_rows(rows) ? 16 : 8, kBulk && sizeof(T) == 2 ? 32 : 16);
+  constexpr int kMost = V == 8 ? 32 : 16;  // elements per thread: beyond, registers spill
+  const NormShape n = norm_shape(width, V, many_rows(rows) ? 16 : 8, kMost);
   float* p = dw || db ? part : nullptr;
   int parts = (int)std::min<int64_t>(kSms, rows);
   cudaError_t e;
@@ -210,23 +210,24 @@ cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const
                                                                      width);
     e = cudaGetLastError();
   } else {
-    const int ty = norm_groups(rows, n, V, kBulk);
+    const int ty = norm_groups(rows, n, V);
     parts = norm_ctas(rows, n, V, ty);
     e = with_nv(n.nv, [&](auto nv) {
       constexpr int NV = decltype(nv)::value, E = NV * V;
-      if constexpr (E <= (kBulk && sizeof(T) == 2 ? 32 : 16) && E > 1) {
-        constexpr int kStage = threads_for(E, kBulk) * E * (int)sizeof(T) * 2;
+      if constexpr (E <= kMost && E > 1) {
+        constexpr int kStage = threads_for(E) * E * (int)sizeof(T) * 2;
         constexpr int DEPTH = E > 16 ? 2 : std::min(4, 192 * 1024 / kStage);  // at most 192 KB of rows
         const int threads = n.tx * ty;
-        const int ring = threads * Rows<T, V, NV, 2, DEPTH, false>::kRing;
-        const int smem = std::max(ring + (E > 16 ? n.tx * E * 4 : 0), threads * E * 4);
-        return with_full<V>(width == (int64_t)n.tx * NV * V, [&](auto full) {
+        return with_full<V, E>(width == (int64_t)n.tx * NV * V, n.tx, [&](auto full, auto in_ring) {
           static std::atomic<uint64_t> set{0};
-          const auto kernel = norm_bwd_kernel<T, W, V, NV, DEPTH, decltype(full)::value>;
+          constexpr bool kFull = decltype(full)::value, kRing = decltype(in_ring)::value;
+          const int ring = ty * Rows<T, V, NV, 2, DEPTH, kFull, kRing>::ring_bytes(n.tx);
+          const int smem = std::max(ring + (E > 16 ? n.tx * E * 4 : 0), threads * E * 4);
+          const auto kernel = norm_bwd_kernel<T, W, V, NV, DEPTH, kFull, kRing>;
           const cudaError_t ae = allow_smem(kernel, smem, set);
           if (ae != cudaSuccess) return ae;
-          kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, (int)rows, (int)width,
-                                                     status);
+          kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, (int)rows,
+                                                     (int)width, status);
           return cudaGetLastError();
         });
       }
@@ -252,9 +253,9 @@ cudaError_t bwd_t(int64_t rows, int64_t width, const void* dy, int64_t ld_dy, co
                   void* part, int* status, cudaStream_t s) {
   const uintptr_t bytes = address(x) | address(dy) | address(dx) | (ld_x | ld_dy | ld_dx | width) * sizeof(T);
   return with_access<T>(bytes, [&](auto v) {
-    return bwd_v<T, W, decltype(v)::value>(rows, width, static_cast<const T*>(dy), ld_dy, static_cast<const T*>(x), ld_x,
-                                           mean, rstd, static_cast<const W*>(w), static_cast<T*>(dx), ld_dx, dw, db,
-                                           static_cast<float*>(part), status, s);
+    return bwd_v<T, W, decltype(v)::value>(rows, width, static_cast<const T*>(dy), ld_dy, static_cast<const T*>(x),
+                                           ld_x, mean, rstd, static_cast<const W*>(w), static_cast<T*>(dx), ld_dx, dw,
+                                           db, static_cast<float*>(part), status, s);
   });
 }
 
