@@ -28,7 +28,8 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
   constexpr bool kSmemW = E > 16;
   using Feed = Rows<T, V, NV, 2, DEPTH, FULL, RING>;
   const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
-  float2* const weights = reinterpret_cast<float2*>(smem + blockDim.y * Feed::ring_bytes(blockDim.x));  // [P][blockDim.x]
+  // [P][blockDim.x]
+  float2* const weights = reinterpret_cast<float2*>(smem + blockDim.y * Feed::ring_bytes(blockDim.x));
   const int step = gridDim.x * blockDim.y;
   int row = blockIdx.x * blockDim.y + threadIdx.y;
   Feed in{{x, dy},    {ld_x, ld_dy}, rows,

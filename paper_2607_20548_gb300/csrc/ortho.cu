@@ -270,7 +270,8 @@ cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float
   const int parts = (int)std::min<int64_t>({kMaxParts, want, (p.rows + 7) / 8});
   {
     ProfScope prof(kFamElementwise, 2.0 * n, n * sizeof(T), s);
-    norm_kernel<T, V><<<dim3(parts, (unsigned)p.batch), kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d);
+    norm_kernel<T, V><<<dim3(parts, (unsigned)p.batch), kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f,
+                                                                          part_d);
   }
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
@@ -279,11 +280,11 @@ cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float
   const dim3 grid((unsigned)std::min<int64_t>(want, (packs + kThreads - 1) / kThreads), (unsigned)p.batch);
   const int64_t sx_elems = p.rows * q.ld_x, lo = sx_elems * p.batch;
   if (p.split)
-    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx, q.x[0], q.ld_x,
-                                                    sx_elems, lo, t, q.done, q.status);
+    scale_kernel<T, V, 2><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx,
+                                                    q.x[0], q.ld_x, sx_elems, lo, t, q.done, q.status);
   else
-    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx, q.x[0], q.ld_x,
-                                                    sx_elems, lo, t, q.done, q.status);
+    scale_kernel<T, V, 1><<<grid, kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f, part_d, parts, eps, sx,
+                                                    q.x[0], q.ld_x, sx_elems, lo, t, q.done, q.status);
   return cudaGetLastError();
 }
 

@@ -436,7 +436,8 @@ __global__ void __launch_bounds__(kThreads)
         if (m < mt)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {  // (n, h)
-            uint32_t* x = reinterpret_cast<uint32_t*>(X + (16 * m + c_row + 8 * (q % 2)) * l.x_pitch + n0 + q / 2 * 8 + c_col);
+            uint32_t* x = reinterpret_cast<uint32_t*>(X + (16 * m + c_row + 8 * (q % 2)) * l.x_pitch + n0 + q / 2 * 8 +
+                                                      c_col);
             uint32_t* xl = reinterpret_cast<uint32_t*>(reinterpret_cast<__half*>(x) + x_plane);
             float2 v = bits_half2(*x);
             if (SPLIT == 2) {
@@ -521,10 +522,11 @@ cudaError_t launch_t(const Steps& p, const Layout& l, int cluster, const void* M
 }  // namespace
 
 // By the time of a step, in us, as measured on both sides (in brackets): here 6 for the exchange and
-// 1 / 0.9e6 per product of an SM (2048 x 64: 7.5; 64 of 128 x 1000 with 4 CTAs each, two rounds: 37), CTAs of an
-// SM sharing it; in steps_kernel 0.07 per 16 elements of a tile's K, at least 3.7 a tile (its epilogue),
-// the three phases one after the other plus 6, and all tiles over the pairs, half as much again for
-// the waits between phases (2048 x 64: 20; 64 of 128 x 1000: 35; 20 of 5000 x 100: 96). Split operands take three products for one.
+// 1 / 0.9e6 per product of an SM (2048 x 64: 7.5; 64 of 128 x 1000 with 4 CTAs each, two rounds: 37), CTAs
+// of an SM sharing it; in steps_kernel 0.07 per 16 elements of a tile's K, at least 3.7 a tile (its
+// epilogue), the three phases one after the other plus 6, and all tiles over the pairs, half as much again
+// for the waits between phases (2048 x 64: 20; 64 of 128 x 1000: 35; 20 of 5000 x 100: 96). Split operands
+// take three products for one.
 int small_cluster(int rows, int cols, int batch, bool split) {
   if (std::min(rows, cols) > 128) return 0;
   const double mult = split ? 3 : 1, r = std::min(rows, cols), k = std::max(rows, cols);

@@ -223,7 +223,7 @@ __device__ __forceinline__ bool wait_done(const int* done, int need) {
   }
 }
 
-// The count of tiles whose inputs are there, from the loading thread to the CTA's epilogue warps.
+// Counts between a CTA's warps: of the tiles whose inputs are there, and of those whose loads have begun.
 __device__ __forceinline__ void set_ready(uint32_t at, int n) {
   asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(n) : "memory");
 }
@@ -231,6 +231,14 @@ __device__ __forceinline__ int get_ready(uint32_t at) {
   int n;
   asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(at) : "memory");
   return n;
+}
+__device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
+  const uint64_t t0 = globaltimer();
+  for (;;) {
+    for (int i = 0; i < 64; ++i)
+      if (get_ready(at) >= n) return true;
+    if (globaltimer() - t0 > 2 * kWaitNs) return false;
+  }
 }
 // The same across the pair.
 __device__ __forceinline__ bool wait_given(uint32_t at, int n) {
@@ -241,14 +249,6 @@ __device__ __forceinline__ bool wait_given(uint32_t at, int n) {
       asm volatile("ld.acquire.cluster.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
       if (v >= n) return true;
     }
-    if (globaltimer() - t0 > 2 * kWaitNs) return false;
-  }
-}
-__device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
-  const uint64_t t0 = globaltimer();
-  for (;;) {
-    for (int i = 0; i < 64; ++i)
-      if (get_ready(at) >= n) return true;
     if (globaltimer() - t0 > 2 * kWaitNs) return false;
   }
 }
@@ -443,8 +443,8 @@ __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUte
 
 // `count` K slices from the ring into the accumulator at d (split: the small products at d + 256).
 template <int SPLIT, int A_MN, int B_MN>
-__device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t b_at, uint32_t ring, uint64_t* full,
-                                             uint64_t* empty, uint32_t d) {
+__device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t b_at, uint32_t ring,
+                                             uint64_t* full, uint64_t* empty, uint32_t d) {
   using C = Config<SPLIT>;
   constexpr uint32_t idesc = idesc_f16(A_MN, B_MN);
   for (; count > 0; --count) {
@@ -974,8 +974,11 @@ cudaError_t run_steps(const Steps& p, cudaStream_t s) {
         !make_map(&maps.ex[i], p.x[i], p.rows, p.cols, p.ld_x, planes, 32))
       return cudaErrorInvalidValue;
   if (!make_map(&maps.sk, p.s, l.r, l.r, p.ld_s, planes, 128) ||
-      !make_map(&maps.bk, p.b, l.r, l.r, p.ld_s, planes, 128) || !make_map(&maps.s, p.s, l.r, l.r, p.ld_s, planes, 64) || !make_map(&maps.es, p.s, l.r, l.r, p.ld_s, planes, 32) ||
-      !make_map(&maps.b, p.b, l.r, l.r, p.ld_s, planes, 64) || !make_map(&maps.eb, p.b, l.r, l.r, p.ld_s, planes, 32))
+      !make_map(&maps.bk, p.b, l.r, l.r, p.ld_s, planes, 128) ||
+      !make_map(&maps.s, p.s, l.r, l.r, p.ld_s, planes, 64) ||
+      !make_map(&maps.b, p.b, l.r, l.r, p.ld_s, planes, 64) ||
+      !make_map(&maps.es, p.s, l.r, l.r, p.ld_s, planes, 32) ||
+      !make_map(&maps.eb, p.b, l.r, l.r, p.ld_s, planes, 32))
     return cudaErrorInvalidValue;
   const size_t size = dtype_size(p.out_type);
   const int out_vec = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && (p.ld_out * size) % 16 == 0 &&

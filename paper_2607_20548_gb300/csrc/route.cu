@@ -9,9 +9,10 @@
 // runs on 32-bit keys in the logits' order: each lane keeps its keys sorted (or, many, scans them),
 // and k times the group's largest head is found and popped by its owner. A 16-bit logit's key holds
 // its index below its value, so that keys differ; of equal fp32 keys the lowest index is looked for
-// only when two lanes hold the largest one. Instructions bound it (about 200 per token of 127 fp32
-// logits with k = 6, 80 of 64 bf16 ones with k = 8), so what each exchange does is kept to a minimum
-// and the gates are computed once per choice, by the lane that writes it.
+// only when two lanes hold the largest one. Instructions bound it (measured: 440 per token of 127 fp32
+// logits with k = 6, backward 224; 30000 x 512 fp32, k = 8: 94 us, backward 46), so what each exchange
+// does is kept to a minimum and the gates are computed once per choice, by the lane that writes it. Calls
+// with enough tokens to fill the GPU go to route_tile.cu, at a third of that; few tokens need the lanes.
 //
 // Column sums of p stay in registers over all of a warp's tokens, counts in shared memory. A cluster
 // adds its CTAs' sums through distributed shared memory in a fixed order; one cluster finishes by
@@ -32,7 +33,7 @@ using namespace route;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxExperts = 1024;
-constexpr int kMaxCtas = 608;
+constexpr int kMaxCtas = 608;  // four per SM
 constexpr int kMaxK = 32;
 
 template <int G>
@@ -185,7 +186,8 @@ __global__ void __launch_bounds__(kThreads)
       if (a.status && lane == 0) atomicOr(a.status, SOAP_STATUS_NONFINITE);
     }
     seen += counted || bad;
-    if (a.stats && lane == 0 && t < tokens) a.stats[t] = bad ? make_float2(NAN, NAN) : make_float2(most, counted ? inv : 0.f);
+    if (a.stats && lane == 0 && t < tokens)
+      a.stats[t] = bad ? make_float2(NAN, NAN) : make_float2(most, counted ? inv : 0.f);
     // k times the largest key; what it is stays with lane r of the group
     uint32_t my_key[kRec];
 #pragma unroll
@@ -197,7 +199,8 @@ __global__ void __launch_bounds__(kThreads)
         bool mine = head == top;
         if (!kPacked) {
           // of equal keys in several lanes, the one of the lowest index
-          const uint32_t who = __ballot_sync(0xffffffffu, mine) >> ((threadIdx.x % 32) / G * G) & (0xffffffffu >> (32 - G));
+          const uint32_t who =
+              __ballot_sync(0xffffffffu, mine) >> ((threadIdx.x % 32) / G * G) & (0xffffffffu >> (32 - G));
           if (__any_sync(0xffffffffu, (who & (who - 1)) != 0)) {
             const uint32_t low = ~group_max<G>(mine ? ~(uint32_t)head_idx : 0u);
             mine = mine && (uint32_t)head_idx == low;
@@ -548,16 +551,17 @@ soap_status_t layer_route_forward(int64_t tokens, int32_t experts, int32_t k, co
 soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, const void* logits, int64_t ld,
                                    int32_t type, const uint8_t* mask, int32_t normalize, float coef, float dloss,
                                    const int32_t* indices, const float* stats, const int32_t* counts,
-                                   const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d, soap_stream_t stream) {
+                                   const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d,
+                                   soap_stream_t stream) {
   if (bad_route(tokens, experts, k, logits, ld, type, coef) || !std::isfinite(dloss)) return SOAP_ERR_INVALID_ARG;
   if (tokens == 0) return SOAP_OK;
-  if (bad_ptr(stats, 8) || bad_ptr(counts, 4) || bad_ptr(live, 4) || bad_ptr(dlogits, dtype_size(type)) || ld_d < experts ||
-      (dgates && (bad_ptr(dgates, 4) || bad_ptr(indices, 4))))
+  if (bad_ptr(stats, 8) || bad_ptr(counts, 4) || bad_ptr(live, 4) || bad_ptr(dlogits, dtype_size(type)) ||
+      ld_d < experts || (dgates && (bad_ptr(dgates, 4) || bad_ptr(indices, 4))))
     return SOAP_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   const double n = (double)tokens * experts;
-  const Backward b{logits, ld, mask, tokens, experts, k, normalize, (float)((double)coef * dloss * experts / k), indices,
-                   reinterpret_cast<const float2*>(stats), counts, live, dgates, dlogits, ld_d};
+  const Backward b{logits, ld, mask, tokens, experts, k, normalize, (float)((double)coef * dloss * experts / k),
+                   indices, reinterpret_cast<const float2*>(stats), counts, live, dgates, dlogits, ld_d};
   ProfScope prof(kFamElementwise, 6.0 * n, 2.0 * n * dtype_size(type) + 12.0 * tokens * k, s);
   cudaError_t e;
   if (tile_fits(tokens, experts, k, type)) {
@@ -567,7 +571,8 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
     const int ctas = (int)std::min<int64_t>(kMaxCtas, want);
     e = with_row<2>(type, experts, logits, ld, dlogits, ld_d, [&](auto t, auto g, auto ne, auto v, bool vec) {
       using T = decltype(t);
-      route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value><<<ctas, kThreads, 0, s>>>(b, vec);
+      route_bwd_kernel<T, decltype(g)::value, decltype(ne)::value, decltype(v)::value>
+          <<<ctas, kThreads, 0, s>>>(b, vec);
       return cudaGetLastError();
     });
   }

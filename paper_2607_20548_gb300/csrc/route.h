@@ -1,4 +1,4 @@
-// What the routing kernels share (route.cu: a group of lanes per token; route_tile.cu: a thread per token):
+// What the routing kernels share (route.cu: a group of lanes per token; route_tile.cu: two lanes per token):
 // the logits' order as keys, exponentials, and the way from CTAs' column sums to the totals.
 #pragma once
 
@@ -12,7 +12,7 @@ namespace soap {
 namespace route {
 
 constexpr int kCluster = 8;
-constexpr int kTileCluster = 2;  // with a thread per token
+constexpr int kTileCluster = 2;  // with two lanes per token: clusters of 8 left a quarter of the SMs' time idle
 constexpr int kMaxParts = 228;   // clusters, and partial rows, of a forward launch
 
 struct Forward {
@@ -49,7 +49,7 @@ struct Backward {
   int64_t ld_d;
 };
 
-// The kernels with a thread per token: whether they take a call, and the launches. forward_ctas: whole
+// The kernels with two lanes per token: whether they take a call, and the launches. forward_ctas: whole
 // clusters.
 constexpr int64_t kFewTokens = 152 * 96;  // below: an SM would have only a few warps
 bool tile_fits(int64_t tokens, int experts, int k, int32_t type);

@@ -1,15 +1,18 @@
-// Routing of many tokens (include/layer.h): a thread per token.
+// Routing of many tokens (include/layer.h): two lanes per token.
 //
-// A warp brings 32 rows of logits into shared memory and each lane goes through its own row, 16 bytes
-// at a time; rows lie an odd number of 16-byte units apart, so that neither the lanes' walks along their
-// rows nor the sums down the columns meet in a bank. The k largest are kept by insertion: one
-// compare-exchange (a minimum and a maximum) per place and logit, nothing exchanged between lanes. A
-// 16-bit logit's key holds its index; fp32 values go without theirs, and a second look at the row marks
-// what reaches the k-th value, whose places follow from the list. Probabilities are summed down the
-// columns with a lane per 32-bit word, the sums staying in registers over all of a warp's tiles.
+// A warp brings 16 rows of logits into shared memory and two lanes go through a row, 16 bytes at a time in
+// turn; rows lie an odd number of 16-byte units apart, so that neither the lanes' walks along their
+// rows nor the sums down the columns meet in a bank. The k largest are kept sorted: four logits are sorted
+// and merged in at a time, and the two lanes' lists at the end. A 16-bit logit's key holds its index; fp32
+// values go without theirs, and a second look at the row marks what reaches the k-th value, whose places
+// follow from the list. Probabilities are summed down the columns with a lane per 32-bit word, the sums
+// staying in registers over all of a warp's tiles.
 //
-// What bounds it is instructions: with k = 6 and 127 fp32 logits about 100 per token, where a group of
-// lanes per token (route.cu, few tokens and long rows) takes 440, most of them for exchanges.
+// What bounds it is instructions and their latency, not memory: with k = 6 and 500009 x 127 fp32 logits,
+// 138 us forward (2.0 TB/s) and 134 backward (4.1 TB/s; rows of 128, which move 16 bytes at a time: 122
+// and 99). Before, in that order: a thread per token and 32 rows per warp, so that shared memory held half
+// the warps, 203 and 145; logits inserted one by one, and the copies' conditions worked out per row, 240
+// and 174; a group of lanes per token (route.cu), most of its instructions exchanges, 312 and 241.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -235,7 +238,8 @@ __global__ void __launch_bounds__(kThreads, 3)
   constexpr int V = 16 / sizeof(T), W = 4 / sizeof(T);  // elements per unit and per word
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float red[kWarps + 1];
-  const int lane = threadIdx.x % 32, r = lane % kRows, half = lane / kRows, warp = threadIdx.x / 32, experts = a.experts, k = a.k;
+  const int lane = threadIdx.x % 32, r = lane % kRows, half = lane / kRows, warp = threadIdx.x / 32;
+  const int experts = a.experts, k = a.k;
   const int pitch = pitch_of(experts * (int)sizeof(T));
   uint8_t* tile = smem + warp * kRows * pitch;
   float2* stat = reinterpret_cast<float2*>(smem + kWarps * kRows * pitch) + warp * kRows;
@@ -613,7 +617,8 @@ size_t fwd_smem(int experts, int k, int32_t type) {
   return (size_t)kWarps * (kRows * (pitch_of(row_bytes(experts, type)) + 8) + kStride * 8 * k) + (experts + 1) * 4;
 }
 size_t bwd_smem(int experts, int k, int32_t type) {
-  return (experts * 4 + 15) / 16 * 16 + (size_t)kWarps * (kRows * pitch_of(row_bytes(experts, type)) + kStride * 8 * k);
+  return (experts * 4 + 15) / 16 * 16 +
+         (size_t)kWarps * (kRows * pitch_of(row_bytes(experts, type)) + kStride * 8 * k);
 }
 
 // Bytes that rows may move at once.

@@ -219,3 +219,18 @@ def test_refusals(cuda):
         layer_norm_backward(dy[:2], x, mean, rstd, w)
     with pytest.raises(ValueError):
         layer_norm_backward(dy, x, mean[:2], rstd, w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,width,pad,off", [(1, 301, 3, 1), (2, 511, 1, 0), (1, 4099, 9, 5), (700, 1537, 7, 3),
+                                                (2500, 511, 5, 2), (2500, 2051, 1, 1), (3, 8191, 2, 1), (2, 9001, 3, 2)])
+def test_rows_between_other_data(cuda, dtype, rows, width, pad, off):
+    """Rows that begin and end inside 16-byte units, NaN on both sides of each: nothing of the neighbours counts."""
+    x, w, b, dy = _inputs(cuda, rows, width, dtype, torch.float32, seed=width)
+    bx, bg = (torch.full((rows, width + pad), float("nan"), device=cuda, dtype=dtype) for _ in range(2))
+    vx, vg = bx[:, off:off + width], bg[:, pad - off:pad - off + width]
+    vx.copy_(x)
+    vg.copy_(dy)
+    y, mean, rstd = layer_norm_forward(vx, w, b)
+    _check_forward(x, w, b, 1e-5, y, mean, rstd)
+    _check_backward(x, w, 1e-5, dy, *layer_norm_backward(vg, vx, mean, rstd, w))
