@@ -240,16 +240,16 @@ __device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
     if (globaltimer() - t0 > 2 * kWaitNs) return false;
   }
 }
-// The same across the pair.
+// The same across the pair and for most of a tile's time: with pauses, since a loop of loads takes issue
+// slots and power from the others.
 __device__ __forceinline__ bool wait_given(uint32_t at, int n) {
   const uint64_t t0 = globaltimer();
   for (;;) {
-    for (int i = 0; i < 64; ++i) {
-      int v;
-      asm volatile("ld.acquire.cluster.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-      if (v >= n) return true;
-    }
+    int v;
+    asm volatile("ld.acquire.cluster.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    if (v >= n) return true;
     if (globaltimer() - t0 > 2 * kWaitNs) return false;
+    __nanosleep(100);
   }
 }
 
@@ -556,7 +556,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int m = 0; ok && !*abort_flag; ++m) {
         int p;
         if (rank == 0) {
-          if (!(ok = wait_ready(begun_at, m))) break;
+          if (!(ok = wait_given(begun_at, m))) break;
           p = atomicAdd(a.done + a.batch, 1);
           if (p >= l.total) p = -1;
           uint32_t peer;
