@@ -327,6 +327,11 @@ __global__ void __launch_bounds__(kThreads)
         for (int q = 0; q < 4; ++q) acc[n][q] += small[n][q];
   };
   const int nt = (l.rp + 31) / 32;
+  // lanes per four elements of S, so that all of the cluster's threads have some of its parts to add (by one
+  // thread each, S of 64 x 64 occupies a quarter of a cluster of 16); a warp's are whole
+  int share = 1;
+  while (share < (int)size && 2 * share * l.rp * (l.rp / 4) <= (int)size * kThreads) share *= 2;
+  const int first_quad = (rank * kThreads + threadIdx.x) / share;
 
   for (int step = 0; step < a.steps; ++step) {
     const StepCoef& c = a.coef[step];
@@ -345,17 +350,24 @@ __global__ void __launch_bounds__(kThreads)
         }
     }
     cluster_sync();
-    {  // S: four elements at a time, the cluster's parts in order, to every CTA
+    {  // S: four elements at a time by `share` lanes, each some of the cluster's parts, in order, and then to
+       // some of its CTAs
       const int quads = l.rp / 4;
       const float alpha = c.s_alpha * ft * ft;
-      for (int i = rank * kThreads + threadIdx.x; i < l.rp * quads; i += size * kThreads) {
+      for (int i = first_quad; i < l.rp * quads; i += size * kThreads / share) {
         const int row = i / quads, col = (i - row * quads) * 4;
         const uint32_t at = smem_at(part + row * l.p_pitch + col);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-        for (uint32_t q = 0; q < size; ++q) {
+        for (uint32_t q = lane % share; q < size; q += share) {
           const float4 x = peer_load4(peer(at, q));
           v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+        for (int o = 1; o < share; o *= 2) {
+          v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+          v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+          v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+          v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
         }
         v = make_float4(v.x * alpha, v.y * alpha, v.z * alpha, v.w * alpha);
         const uint32_t h0 = half2_bits(v.x, v.y), h1 = half2_bits(v.z, v.w);
@@ -366,7 +378,7 @@ __global__ void __launch_bounds__(kThreads)
           l0 = half2_bits(v.x - f0.x, v.y - f0.y);
           l1 = half2_bits(v.z - f1.x, v.w - f1.y);
         }
-        for (uint32_t q = 0; q < size; ++q) {
+        for (uint32_t q = lane % share; q < size; q += share) {
           peer_store2(peer(to, q), h0, h1);
           if (SPLIT == 2) peer_store2(peer(to + s_plane * 2, q), l0, l1);
         }
