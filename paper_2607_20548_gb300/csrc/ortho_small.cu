@@ -9,8 +9,10 @@
 // These products are too small for the 5th-generation tensor cores to pay: a 256-wide accumulation of
 // K = 2048 takes 128 dependent instructions of 140 cycles there, 10 us, and its result comes back through
 // tensor memory. Warp-level mma (16 x 8 x 16, fp32 accumulators in registers) does the step's few million
-// products in about a microsecond; what is left is the exchange. 2048 x 64 takes 7.5 us a step; as
-// tiles of steps_kernel, with a signal between the phases, 20.
+// products in a microsecond or two. 2048 x 64 takes 6 us a step, of which 2.5 are S, B and X' themselves and
+// 2.5 the exchange and its barriers (in cycles: S 1300, exchange 4800, B 1400, X' 2100); as tiles of
+// steps_kernel, with a signal between the phases, 20. With r near 128 the mma's rate bounds it (8000 x 100:
+// 24 us a step, more than half of them X').
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -327,6 +329,19 @@ __global__ void __launch_bounds__(kThreads)
         for (int q = 0; q < 4; ++q) acc[n][q] += small[n][q];
   };
   const int nt = (l.rp + 31) / 32;
+  // f(i0, n0, whether to write the mirror image too) for this warp's 16 x 32 tiles of a symmetric matrix. With
+  // more tiles than warps, those on and below the diagonal's 32 x 32 blocks (of r = 100: 16 of 28), which
+  // saves mma's: what bounds such sizes.
+  auto each_tile = [&](auto&& f) {
+    if constexpr (RT == 8) {
+      int i = 0;
+      for (int m = 0; m < mt; ++m)
+        for (int n = 0; n <= m / 2; ++n, ++i)
+          if (i % kWarps == warp) f(16 * m, 32 * n, m / 2 > n);
+    } else {
+      for (int i = warp; i < mt * nt; i += kWarps) f(i / nt * 16, i % nt * 32, false);
+    }
+  };
   // lanes per four elements of S, so that all of the cluster's threads have some of its parts to add (by one
   // thread each, S of 64 x 64 occupies a quarter of a cluster of 16); a warp's are whole
   int share = 1;
@@ -337,8 +352,7 @@ __global__ void __launch_bounds__(kThreads)
     const StepCoef& c = a.coef[step];
     const float ft = step == 0 ? t : 1.f;
     // this CTA's part of X X^T
-    for (int i = warp; i < mt * nt; i += kWarps) {
-      const int i0 = i / nt * 16, n0 = i % nt * 32;
+    each_tile([&](int i0, int n0, bool mirror) {
       float acc[4][4];
       product(acc, x_at, x_plane * 2, l.x_pitch, i0, n0, l.kcp);
 #pragma unroll
@@ -347,8 +361,15 @@ __global__ void __launch_bounds__(kThreads)
           float* p = part + (i0 + c_row) * l.p_pitch + n0 + n * 8 + c_col;
           *reinterpret_cast<float2*>(p) = make_float2(acc[n][0], acc[n][1]);
           *reinterpret_cast<float2*>(p + 8 * l.p_pitch) = make_float2(acc[n][2], acc[n][3]);
+          if (mirror) {
+            float* t = part + (n0 + n * 8 + c_col) * l.p_pitch + i0 + c_row;
+            t[0] = acc[n][0];
+            t[l.p_pitch] = acc[n][1];
+            t[8] = acc[n][2];
+            t[l.p_pitch + 8] = acc[n][3];
+          }
         }
-    }
+    });
     cluster_sync();
     {  // S: four elements at a time by `share` lanes, each some of the cluster's parts, in order, and then to
        // some of its CTAs
@@ -386,8 +407,7 @@ __global__ void __launch_bounds__(kThreads)
     }
     cluster_sync();
     // B = b S + c S S
-    for (int i = warp; i < mt * nt; i += kWarps) {
-      const int i0 = i / nt * 16, n0 = i % nt * 32;
+    each_tile([&](int i0, int n0, bool mirror) {
       float acc[4][4];
       product(acc, s_at, s_plane * 2, l.s_pitch, i0, n0, l.rp);
 #pragma unroll
@@ -405,12 +425,23 @@ __global__ void __launch_bounds__(kThreads)
             const float y = fmaf(c.b_beta, s.y, c.b_alpha * acc[n][2 * h + 1]);
             const uint32_t hi = half2_bits(x, y);
             *reinterpret_cast<uint32_t*>(B + at) = hi;
+            uint32_t lo = 0;
             if (SPLIT == 2) {
               const float2 f = bits_half2(hi);
-              *reinterpret_cast<uint32_t*>(B + s_plane + at) = half2_bits(x - f.x, y - f.y);
+              lo = half2_bits(x - f.x, y - f.y);
+              *reinterpret_cast<uint32_t*>(B + s_plane + at) = lo;
+            }
+            if (mirror) {
+              uint16_t* t = reinterpret_cast<uint16_t*>(B) + (n0 + n * 8 + c_col) * l.s_pitch + i0 + c_row + 8 * h;
+              t[0] = (uint16_t)hi;
+              t[l.s_pitch] = (uint16_t)(hi >> 16);
+              if (SPLIT == 2) {
+                t[s_plane] = (uint16_t)lo;
+                t[s_plane + l.s_pitch] = (uint16_t)(lo >> 16);
+              }
             }
           }
-    }
+    });
     __syncthreads();
     // X' = a X + B X: a warp takes 16 columns at a time, all rows, and writes them over X
     for (int n0 = warp * 16; n0 < l.kcp; n0 += kWarps * 16) {
@@ -534,7 +565,7 @@ cudaError_t launch_t(const Steps& p, const Layout& l, int cluster, const void* M
 }  // namespace
 
 // By the time of a step, in us, as measured on both sides (in brackets): here 6 for the exchange and
-// 1 / 0.9e6 per product of an SM (2048 x 64: 7.5; 64 of 128 x 1000 with 4 CTAs each, two rounds: 37), CTAs
+// 1 / 0.9e6 per product of an SM (2048 x 64: 6; 64 of 128 x 1000 with 4 CTAs each, two rounds: 36), CTAs
 // of an SM sharing it; in steps_kernel 0.07 per 16 elements of a tile's K, at least 3.7 a tile (its
 // epilogue), the three phases one after the other plus 6, and all tiles over the pairs, half as much again
 // for the waits between phases (2048 x 64: 20; 64 of 128 x 1000: 35; 20 of 5000 x 100: 96). Split operands
