@@ -113,7 +113,8 @@ struct Rows {
         const uintptr_t end = begin + (uintptr_t)width * sizeof(T);
         lo[m] = begin & ~uintptr_t(15);
         hi[m] = (end + 15) & ~uintptr_t(15);
-        if (row == 0 || row == rows - 1) {  // nothing from before the first row or after the last
+        // nothing from before the first row or after the last (rows here are longer than a unit)
+        if (row == 0 || row == rows - 1) {
           uint8_t* const dst = slot(stage, m);
           const uintptr_t at = lo[m];
           if (row == 0 && lo[m] < begin) lo[m] += 16;
