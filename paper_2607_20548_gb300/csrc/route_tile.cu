@@ -557,7 +557,8 @@ __global__ void __launch_bounds__(kThreads, 3)
     }
     float sum = (d4[0] + d4[1]) + (d4[2] + d4[3]);
     if (sizeof(T) == 2) sum *= st.y;
-    dot = both(dot + sum);  // (and the row's other lane has written its probabilities)
+    dot = both(dot + sum);
+    __syncwarp();  // fp32: the row's other lane has written its probabilities (a shuffle orders no memory)
     // the chosen logits' own gradients, before the row is written over
     if (a.dgates)
       for (int q = half; q < k; q += 2) {
