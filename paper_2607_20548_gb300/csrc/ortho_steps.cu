@@ -421,11 +421,13 @@ struct Ring {
 
 // K slices kb .. to - 1 of an operand's 128 rows from `row` on into the ring at `ring`, the operand's place in
 // the first slot. bytes, if not 0: what this thread tells the barrier that a slot takes, all operands in both
-// CTAs. skip: only keeps pace.
+// CTAs. is_b: the second operand's thread, whose arrival the barrier counts in either CTA, also where it has
+// nothing to load (skip): otherwise nothing would hold the others back to one that falls behind over a run of
+// diagonal tiles, and two rounds of the ring behind it takes another round's parity for its own.
 template <int SPLIT, int MN>
 __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUtensorMap* map, int row, int b,
                                             int batch, uint32_t ring, uint64_t* full, uint64_t* empty,
-                                            uint32_t leader_full, uint32_t bytes, bool skip) {
+                                            uint32_t leader_full, uint32_t bytes, bool is_b, bool skip) {
   using C = Config<SPLIT>;
   for (; kb < to; ++kb) {
     if (!(st.ok = mbar_wait(&empty[st.s], st.parity, kWaitNs))) return;
@@ -434,6 +436,7 @@ __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUte
 #pragma unroll
     for (int h = 0; h < SPLIT; ++h)
       if (!skip) load_tile<MN>(at + h * kTile, map, bar, row, kb * BK, b + h * batch);
+    if (is_b) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
     if (++st.s == C::kStages) {
       st.s = 0;
       st.parity ^= 1;
@@ -516,7 +519,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
   const uint32_t ready_at = smem_u32(tmem_at + 2), begun_at = ready_at + 4, given_at = ready_at + 8;
   // the list's places that this pair has taken, tile m's at m % kTaken (all roles of a pair are within the
-  // ring's slots and the accumulators of each other), -1 at the end
+  // ring's slots and the accumulators of each other: every slot takes both CTAs' loading threads), -1 at the end
   volatile int* taken = reinterpret_cast<volatile int*>(tmem_at + 5);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -524,7 +527,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], 3);  // the pair's first CTA's first loading thread, both CTAs' second ones
       mbar_init(&empty[s], 1);
     }
     for (int i = 0; i < kAcc; ++i) {
@@ -606,9 +609,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const bool skip = is_b && t.same();
         used = min(used + kblocks, kStages);
         if (change > 0)
-          load_slices<SPLIT, 0>(st, 0, change, mk, row, t.b, a.batch, ring, full, empty, bars, bytes, skip);
+          load_slices<SPLIT, 0>(st, 0, change, mk, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip);
         if (st.ok && change < kblocks)
-          load_slices<SPLIT, 1>(st, change, kblocks, mn, row, t.b, a.batch, ring, full, empty, bars, bytes, skip);
+          load_slices<SPLIT, 1>(st, change, kblocks, mn, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip);
         if (!st.ok) break;
       }
       // every slice consumed, and its release arrived here, before this CTA's barriers go away

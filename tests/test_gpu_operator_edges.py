@@ -1,9 +1,11 @@
 """The stand-alone operators where one part of a kernel hands data to another: lanes of a row, warps of a
 CTA, CTAs of a pair."""
+import math
+
 import pytest
 import torch
 
-from paper_2607_20548_gb300 import route_backward, route_forward
+from paper_2607_20548_gb300 import muon_orthogonalize, route_backward, route_forward
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +49,49 @@ def test_choices_in_the_other_lanes_half(cuda, e, k, shift):
     bound = U * ref.abs() + 4 * 152 * U * mag + 1e-37
     assert bool(((dz.double() - ref).abs() <= bound).all())
     assert torch.equal(dz, route_backward(z, r, dgates=dg))
+
+
+# ---- orthogonalisation ---------------------------------------------------------------------
+
+QUINTIC = (15 / 8, -10 / 8, 3 / 8)
+
+
+def _ortho_ref(M, steps, eps=1e-7):
+    X = M.double()
+    X = X / torch.linalg.matrix_norm(X, keepdim=True).clamp_min(eps)
+    tall = X.shape[-2] > X.shape[-1]
+    X = X.mT if tall else X
+    a, b, c = QUINTIC
+    for _ in range(steps):
+        A = X @ X.mT
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return X.mT if tall else X
+
+
+def _ortho_tol(dtype, steps, m, n):
+    """As in test_gpu_ortho.py: 3 stored results a step of 11 or 22 bits, a gain of 2, one unit of the
+    accumulator per 16 products, one rounding to the type."""
+    b = 11 if dtype == torch.bfloat16 else 22
+    return torch.finfo(dtype).eps / 2 + 2 * math.sqrt(3 * steps) * 2.0 ** -b + math.ceil(max(m, n) / 16) * 2.0 ** -23
+
+
+def _momentum(cuda, shape, dtype, seed=0, scale=1e-3):
+    g = torch.Generator(device=cuda).manual_seed(seed)
+    *lead, m, n = shape
+    q = min(4, m, n)
+    low = torch.randn(*lead, m, q, device=cuda, generator=g) @ torch.randn(*lead, q, n, device=cuda, generator=g)
+    return ((low * (0.5 / math.sqrt(q)) + torch.randn(*lead, m, n, device=cuda, generator=g)) * scale).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", [(700, 150, 190), (700, 190, 150), (400, 256, 256), (300, 129, 600), (150, 256, 260)])
+def test_long_runs_of_diagonal_tiles(cuda, shape, dtype):
+    """Sides of 129 to 256: every tile of S and B lies on the diagonal, where one of a CTA's two loading
+    threads has nothing to load; a large batch gives a pair of CTAs long runs of them."""
+    M = _momentum(cuda, shape, dtype, seed=shape[0])
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    out = muon_orthogonalize(M, ns_steps=6, status=status)
+    assert int(status) == 0
+    ref = _ortho_ref(M, 6)
+    err = torch.linalg.matrix_norm(out.double() - ref) / torch.linalg.matrix_norm(ref)
+    assert float(err.max()) <= _ortho_tol(dtype, 6, *shape[1:])
