@@ -103,8 +103,9 @@ void muon_destroy(muon_handle h);
  * memory, 256-byte aligned, muon_orthogonalize_workspace_bytes(...) bytes (0 from that function:
  * the sizes or the type are invalid). status: NULL, or a device int32 into which the kernels OR
  * SOAP_STATUS_NONFINITE (a matrix holds a NaN or an infinity: its result is NaN, the others are
- * not touched by it) or SOAP_STATUS_TIMEOUT; it is not cleared. Runs on the device that is current
- * for the calling thread. A zero matrix gives zeros.
+ * not touched by it) or SOAP_STATUS_TIMEOUT (a bounded wait gave up, see soap_wait_limit: every
+ * result of the call is NaN); it is not cleared. Runs on the device that is current for the calling
+ * thread. A zero matrix gives zeros.
  *
  * Precision beyond rounding: a step multiplies small singular values by a_i, so rounding noise in
  * X_0 (2^-12 of an element, bf16: none; 2^-23 for fp32) reappears in the directions whose singular

@@ -77,16 +77,6 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
                : "memory");
 }
 
-// Bounded wait until *flag != 0 (a flag set from outside the kernel): false after `limit_ns`.
-__device__ __forceinline__ bool flag_wait(const int* flag, uint64_t limit_ns) {
-  const volatile int* f = flag;
-  if (*f != 0) return true;
-  const uint64_t t0 = globaltimer();
-  while (*f == 0)
-    if (globaltimer() - t0 > limit_ns) return false;
-  return true;
-}
-
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1,
                                             int c2) {
   asm volatile(
@@ -670,6 +660,11 @@ std::atomic<const int*> g_hold{nullptr};
 void set_wait_limit(uint64_t ns, const int* hold) {
   g_wait_ns.store(ns, std::memory_order_relaxed);
   g_hold.store(hold, std::memory_order_relaxed);
+}
+
+WaitLimit wait_limit() {
+  const uint64_t ns = g_wait_ns.load(std::memory_order_relaxed);
+  return {ns ? ns : tc::kWaitNs, g_hold.load(std::memory_order_relaxed)};
 }
 
 cudaError_t gemm_tc_nt(int M, int N, int K, int batch, const TcOperand& A, const TcOperand& B,

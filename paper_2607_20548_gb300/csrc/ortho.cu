@@ -122,7 +122,8 @@ __global__ void __launch_bounds__(kThreads)
   if (threadIdx.x == 0) {
     const bool first = blockIdx.x == 0;
     if (first) done[b] = 0;
-    if (first && b == 0) done[gridDim.y] = 0;
+    if (first && b == 0)
+      for (int i = 0; i < kDoneExtra; ++i) done[gridDim.y + i] = 0;
     for (int w = 1; w < kThreads / 32; ++w) s += red[w];
     int e = 0;
     float f = 0.f;  // norm = f 2^e, f in [0.5, 1)
@@ -209,7 +210,7 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
   };
   p.part_off = take((size_t)batch * kMaxParts * (sizeof(double) + sizeof(float)));
   p.t_off = take((size_t)batch * sizeof(float));
-  p.done_off = take((size_t)(batch + 1) * sizeof(int));
+  p.done_off = take((size_t)(batch + kDoneExtra) * sizeof(int));
   p.x_off[0] = take((size_t)p.x_elems * 2);
   p.x_off[1] = take((size_t)p.x_elems * 2);
   p.s_off = take((size_t)p.s_elems * 2);
@@ -320,6 +321,9 @@ cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_
   q.ld_out = ld_out;
   q.stride_out = stride_out;
   q.status = status;
+  const WaitLimit limit = wait_limit();
+  q.wait_ns = limit.ns;
+  q.hold = limit.hold;
   double u = 1.0;  // bound of the singular values
   int sx = scale_exp(2.0);
   const int sx0 = sx;

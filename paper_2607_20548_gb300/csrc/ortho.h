@@ -9,6 +9,7 @@ namespace soap {
 namespace ortho {
 
 constexpr int kMaxSteps = 64;
+constexpr int kDoneExtra = 3;  // words after the matrices' counters
 
 // One Newton-Schulz step on scaled fp16 intermediates (the scales are powers of two):
 //   S = s_alpha t^2 X X^T,  B = b_alpha S S + b_beta S,  X' = t (x_alpha B X + x_beta X)
@@ -27,12 +28,14 @@ struct Steps {
   __half *x[2], *s, *b;
   int ld_x, ld_s;
   const float* t;  // per matrix
-  int* done;       // per matrix, and the list's next place; zero
+  int* done;       // per matrix, then kDoneExtra: the list's next place, CTAs that are through, whether a wait gave up
   void* out;       // out_type (soap_dtype_t), leading dimension, elements between matrices
   int out_type;
   int64_t ld_out, stride_out;
   int out_exp;     // the last step's result carries 2^out_exp (run_steps: 0)
   int* status;
+  uint64_t wait_ns;  // bound of the waits, and a flag to wait for first (soap_wait_limit)
+  const int* hold;
   StepCoef coef[kMaxSteps];
 };
 

@@ -30,8 +30,8 @@
 // tile with K = 768). An MMA that adds to the accumulator of the one before it takes 140 cycles however
 // narrow (measured), so tiles are 256 wide; the issuing thread has little time beside it, so its loops are
 // compiled for each pair of operand orders (with orders chosen at run time a slice took 790 cycles in place
-// of 540). Every wait is bounded; one that runs out sets SOAP_STATUS_TIMEOUT and the CTA drains its copies,
-// frees its tensor memory and returns.
+// of 540). Every wait is bounded (soap_wait_limit); one that runs out sets SOAP_STATUS_TIMEOUT and the CTA
+// drains its copies, frees its tensor memory and returns; the last CTA then makes all results NaN.
 //
 // What bounds it: at 8192 x 8192 the tensor cores (1.83 PFLOP/s, 0.95 of what a library product of that size
 // reaches); with K of 768 to 2048 the operands' way from L2 (1.3 to 1.6 PFLOP/s: with both loading threads
@@ -66,7 +66,6 @@ constexpr int kThreads = 32 * (kScout + 1);
 constexpr int kBlock = 32 * 128;       // a staged block: 32 rows of 128 bytes
 constexpr int kPerTile = 2 * kEpiWarps;       // what a tile adds to its matrix's counter
 constexpr int kTaken = 16;
-constexpr uint64_t kWaitNs = 2000000000ull;
 
 template <int SPLIT>
 struct Config {
@@ -213,13 +212,13 @@ __device__ __forceinline__ int load_acquire(const int* p) {
 }
 
 // Bounded wait for a matrix's counter.
-__device__ __forceinline__ bool wait_done(const int* done, int need) {
+__device__ __forceinline__ bool wait_done(const int* done, int need, uint64_t limit_ns) {
   if (load_acquire(done) >= need) return true;
   const uint64_t t0 = globaltimer();
   for (;;) {
     for (int i = 0; i < 64; ++i)
       if (load_acquire(done) >= need) return true;
-    if (globaltimer() - t0 > kWaitNs) return false;
+    if (globaltimer() - t0 > limit_ns) return false;
   }
 }
 
@@ -232,23 +231,23 @@ __device__ __forceinline__ int get_ready(uint32_t at) {
   asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(at) : "memory");
   return n;
 }
-__device__ __forceinline__ bool wait_ready(uint32_t at, int n) {
+__device__ __forceinline__ bool wait_ready(uint32_t at, int n, uint64_t limit_ns) {
   const uint64_t t0 = globaltimer();
   for (;;) {
     for (int i = 0; i < 64; ++i)
       if (get_ready(at) >= n) return true;
-    if (globaltimer() - t0 > 2 * kWaitNs) return false;
+    if (globaltimer() - t0 > limit_ns) return false;
   }
 }
 // The same across the pair and for most of a tile's time: with pauses, since a loop of loads takes issue
 // slots and power from the others.
-__device__ __forceinline__ bool wait_given(uint32_t at, int n) {
+__device__ __forceinline__ bool wait_given(uint32_t at, int n, uint64_t limit_ns) {
   const uint64_t t0 = globaltimer();
   for (;;) {
     int v;
     asm volatile("ld.acquire.cluster.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     if (v >= n) return true;
-    if (globaltimer() - t0 > 2 * kWaitNs) return false;
+    if (globaltimer() - t0 > limit_ns) return false;
     __nanosleep(100);
   }
 }
@@ -427,10 +426,10 @@ struct Ring {
 template <int SPLIT, int MN>
 __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUtensorMap* map, int row, int b,
                                             int batch, uint32_t ring, uint64_t* full, uint64_t* empty,
-                                            uint32_t leader_full, uint32_t bytes, bool is_b, bool skip) {
+                                            uint32_t leader_full, uint32_t bytes, bool is_b, bool skip, uint64_t limit_ns) {
   using C = Config<SPLIT>;
   for (; kb < to; ++kb) {
-    if (!(st.ok = mbar_wait(&empty[st.s], st.parity, kWaitNs))) return;
+    if (!(st.ok = mbar_wait(&empty[st.s], st.parity, limit_ns))) return;
     if (bytes) expect_tx(&full[st.s], bytes);
     const uint32_t at = ring + st.s * C::kStage, bar = leader_full + st.s * 8;
 #pragma unroll
@@ -447,11 +446,11 @@ __device__ __forceinline__ void load_slices(Ring& st, int kb, int to, const CUte
 // `count` K slices from the ring into the accumulator at d (split: the small products at d + 256).
 template <int SPLIT, int A_MN, int B_MN>
 __device__ __forceinline__ void issue_slices(Ring& st, int count, uint32_t& more, uint32_t b_at, uint32_t ring,
-                                             uint64_t* full, uint64_t* empty, uint32_t d) {
+                                             uint64_t* full, uint64_t* empty, uint32_t d, uint64_t limit_ns) {
   using C = Config<SPLIT>;
   constexpr uint32_t idesc = idesc_f16(A_MN, B_MN);
   for (; count > 0; --count) {
-    if (!(st.ok = mbar_wait(&full[st.s], st.parity, kWaitNs))) return;
+    if (!(st.ok = mbar_wait(&full[st.s], st.parity, limit_ns))) return;
     tc_fence_after();
     const uint32_t as = ring + st.s * C::kStage, bs = as + b_at;
 #pragma unroll
@@ -524,6 +523,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x & 1);  // in the pair
+  const uint64_t lim = a.wait_ns;          // bound of every wait (for another role of the pair: twice)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -555,11 +555,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // the pair's first CTA takes a tile as its loads of the one before begin, and tells the second; each then
     // waits for the tile's inputs
     if (lane == 0) {
-      bool ok = true;
+      bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
       for (int m = 0; ok && !*abort_flag; ++m) {
         int p;
         if (rank == 0) {
-          if (!(ok = wait_given(begun_at, m))) break;
+          if (!(ok = wait_given(begun_at, m, 2 * lim))) break;
           p = atomicAdd(a.done + a.batch, 1);
           if (p >= l.total) p = -1;
           uint32_t peer;
@@ -568,12 +568,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 16), "r"(m + 1) : "memory");
           taken[m % kTaken] = p;
         } else {
-          if (!(ok = wait_given(given_at, m + 1))) break;
+          if (!(ok = wait_given(given_at, m + 1, 2 * lim))) break;
           p = taken[m % kTaken];
         }
         if (p >= 0) {
           const Tile t = tile_at(p, l, a);
-          if (!(ok = wait_done(a.done + t.b, t.need))) break;
+          if (!(ok = wait_done(a.done + t.b, t.need, lim))) break;
           asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
         }
         set_ready(ready_at, m + 1);
@@ -592,7 +592,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int used = 0;   // slots filled so far (up to kStages)
       const uint32_t ring = smem_u32(smem) + (is_b ? SPLIT * kTile : 0), bars = in_leader(full);
       for (int m = 0; !*abort_flag; ++m) {
-        if (!(st.ok = wait_ready(ready_at, m + 1))) break;
+        if (!(st.ok = wait_ready(ready_at, m + 1, 2 * lim))) break;
         const int p = taken[m % kTaken];
         if (p < 0) break;
         if (!is_b) set_ready(begun_at, m + 1);
@@ -609,16 +609,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const bool skip = is_b && t.same();
         used = min(used + kblocks, kStages);
         if (change > 0)
-          load_slices<SPLIT, 0>(st, 0, change, mk, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip);
+          load_slices<SPLIT, 0>(st, 0, change, mk, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip, lim);
         if (st.ok && change < kblocks)
-          load_slices<SPLIT, 1>(st, change, kblocks, mn, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip);
+          load_slices<SPLIT, 1>(st, change, kblocks, mn, row, t.b, a.batch, ring, full, empty, bars, bytes, is_b, skip, lim);
         if (!st.ok) break;
       }
       // every slice consumed, and its release arrived here, before this CTA's barriers go away
       for (int i = 0; i < kStages && st.ok && !*abort_flag; ++i) {
         if (used == kStages || st.s - 1 - i >= 0) {
           const int slot = (st.s - 1 - i + kStages) % kStages;
-          st.ok = mbar_wait(&empty[slot], slot < st.s ? st.parity ^ 1 : st.parity, kWaitNs);
+          st.ok = mbar_wait(&empty[slot], slot < st.s ? st.parity ^ 1 : st.parity, lim);
         }
       }
       if (!st.ok || *abort_flag) {
@@ -636,7 +636,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int n = 0;
       const uint32_t ring = smem_u32(smem);
       for (int m = 0; st.ok && !*abort_flag; ++m) {
-        if (!(st.ok = wait_ready(ready_at, m + 1))) break;
+        if (!(st.ok = wait_ready(ready_at, m + 1, 2 * lim))) break;
         const int p = taken[m % kTaken];
         if (p < 0) break;
         const Tile t = tile_at(p, l, a);
@@ -647,7 +647,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int runs = SPLIT == 2 ? (kblocks + kRunBlocks - 1) / kRunBlocks : 1;
         for (int run = 0; run < runs && st.ok; ++run, ++n) {
           const int ac = n % kAcc;
-          if (n >= kAcc && !(st.ok = mbar_wait(&acc_empty[ac], ((n / kAcc) & 1) ^ 1, kWaitNs))) break;
+          if (n >= kAcc && !(st.ok = mbar_wait(&acc_empty[ac], ((n / kAcc) & 1) ^ 1, lim))) break;
           tc_fence_after();
           const uint32_t d = tmem + static_cast<uint32_t>(ac * 256);
           const int k1 = SPLIT == 2 ? kblocks * (run + 1) / runs : kblocks;
@@ -657,13 +657,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const bool a_mn = kb >= a_change, b_mn = kb >= b_change;
             const int to = min(k1, min(a_mn ? k1 : a_change, b_mn ? k1 : b_change));
             if (a_mn && b_mn)
-              issue_slices<SPLIT, 1, 1>(st, to - kb, more, b_at, ring, full, empty, d);
+              issue_slices<SPLIT, 1, 1>(st, to - kb, more, b_at, ring, full, empty, d, lim);
             else if (a_mn)
-              issue_slices<SPLIT, 1, 0>(st, to - kb, more, b_at, ring, full, empty, d);
+              issue_slices<SPLIT, 1, 0>(st, to - kb, more, b_at, ring, full, empty, d, lim);
             else if (b_mn)
-              issue_slices<SPLIT, 0, 1>(st, to - kb, more, b_at, ring, full, empty, d);
+              issue_slices<SPLIT, 0, 1>(st, to - kb, more, b_at, ring, full, empty, d, lim);
             else
-              issue_slices<SPLIT, 0, 0>(st, to - kb, more, b_at, ring, full, empty, d);
+              issue_slices<SPLIT, 0, 0>(st, to - kb, more, b_at, ring, full, empty, d, lim);
             kb = to;
           }
           if (st.ok) commit_pair(&acc_full[ac]);
@@ -684,7 +684,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     int* unreported = nullptr;  // counter of the matrix whose tile this warp has sent but not reported
     bool ok = true;
     auto wait_acc = [&](int ac) {
-      ok = mbar_wait(&acc_full[ac], (n / kAcc) & 1, kWaitNs) && !*abort_flag;
+      ok = mbar_wait(&acc_full[ac], (n / kAcc) & 1, lim) && !*abort_flag;
       tc_fence_after();
       return ok = __all_sync(0xffffffffu, ok);
     };
@@ -707,7 +707,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         fetch_block(stage_at + buf * kBlock, w.cin, &cin_bar[buf], w.n0 + 64 * i, w.r0, w.t.b + h * a.batch);
     };
     auto fetched = [&](int buf) {
-      ok = mbar_wait(&cin_bar[buf], (cin_parity >> buf) & 1, kWaitNs);
+      ok = mbar_wait(&cin_bar[buf], (cin_parity >> buf) & 1, lim);
       cin_parity ^= 1u << buf;
       return ok = __all_sync(0xffffffffu, ok);
     };
@@ -730,7 +730,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int there = lane == 0 ? get_ready(ready_at) : 0;
         if (__shfl_sync(0xffffffffu, there, 0) <= m) {
           report(std::integral_constant<int, 0>());
-          if (lane == 0) ok = wait_ready(ready_at, m + 1);
+          if (lane == 0) ok = wait_ready(ready_at, m + 1, 2 * lim);
           if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
         }
         __syncwarp();
@@ -887,6 +887,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
   }
+
+  // Where a wait gave up, the last CTA makes all results NaN, so that none is taken for an answer.
+  if (threadIdx.x == 0) {
+    int* const through = a.done + a.batch + 1;
+    if (*abort_flag) atomicOr(through + 1, 1);
+    __threadfence();  // this CTA's results (and its word) come before its count
+    const bool last = atomicAdd(through, 1) == (int)gridDim.x - 1;
+    __threadfence();
+    *abort_flag = last && atomicOr(through + 1, 0) != 0;
+  }
+  __syncthreads();
+  if (*abort_flag)
+    for (int b = 0; b < a.batch; ++b)
+      for (int r = warp; r < a.rows; r += kThreads / 32)
+        for (int c = lane; c < a.cols; c += 32) {
+          const int64_t at = (int64_t)b * a.stride_out + (int64_t)r * a.ld_out + c;
+          if (a.out_type == SOAP_F32)
+            static_cast<float*>(a.out)[at] = NAN;
+          else if (a.out_type == SOAP_BF16)
+            static_cast<__nv_bfloat16*>(a.out)[at] = from_f32<__nv_bfloat16>(NAN);
+          else
+            static_cast<__half*>(a.out)[at] = from_f32<__half>(NAN);
+        }
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {

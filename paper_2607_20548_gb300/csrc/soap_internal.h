@@ -84,6 +84,12 @@ cudaError_t gemm_tc_nt(int M, int N, int K, int batch, const TcOperand& A, const
 // Bound of the tensor-core products' device waits (0: 2 s) and, for testing the timeout path, a
 // device flag their epilogues first wait for (nullptr: none); applies to later launches.
 void set_wait_limit(uint64_t ns, const int* hold);
+// The same settings (the bound never 0) for the other kernels whose waits they govern.
+struct WaitLimit {
+  uint64_t ns;
+  const int* hold;
+};
+WaitLimit wait_limit();
 // Symmetric product C_b = alpha A_b A_b^T + beta C_b (M x M, A_b M x K): only the 128 x 128 tiles on
 // or below the diagonal are computed, each below it also stored (with its lo part) in the mirror
 // position. Needs a row-major, 16-byte aligned C with its lo part; other forms go to gemm_tc_nt.

@@ -45,7 +45,15 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint64
   }
 }
 
-
+// Bounded wait until *flag != 0 (a flag set from outside the kernel): false after `limit_ns`.
+__device__ __forceinline__ bool flag_wait(const int* flag, uint64_t limit_ns) {
+  const volatile int* f = flag;
+  if (*f != 0) return true;
+  const uint64_t t0 = globaltimer();
+  while (*f == 0)
+    if (globaltimer() - t0 > limit_ns) return false;
+  return true;
+}
 
 // Shared-memory matrix descriptor: K-major, 128-byte swizzle, 8-row atoms 1024 B apart.
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t addr) {

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2607_20548_gb300 import muon_orthogonalize, route_backward, route_forward
+from paper_2607_20548_gb300 import soap as S
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +96,29 @@ def test_long_runs_of_diagonal_tiles(cuda, shape, dtype):
     ref = _ortho_ref(M, 6)
     err = torch.linalg.matrix_norm(out.double() - ref) / torch.linalg.matrix_norm(ref)
     assert float(err.max()) <= _ortho_tol(dtype, 6, *shape[1:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", [(300, 700), (3, 1100, 200)])
+def test_ortho_wait_runs_out(cuda, shape, dtype):
+    """A flag that nothing sets makes every wait run out (20 ms): the kernel returns, the status word says so, no
+    result is left to be taken for one, with or without a status word, and the next call is sound."""
+    M = _momentum(cuda, shape, dtype)
+    want = muon_orthogonalize(M, ns_steps=4)
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    hold = torch.zeros(1, dtype=torch.int32, device=cuda)
+    torch.cuda.synchronize()
+    try:
+        S.soap_wait_limit(20_000_000, hold)
+        got = [muon_orthogonalize(M, ns_steps=4, status=status), muon_orthogonalize(M, ns_steps=4)]
+        torch.cuda.synchronize()
+        hold.fill_(1)
+        free = muon_orthogonalize(M, ns_steps=4)
+        torch.cuda.synchronize()
+    finally:
+        S.soap_wait_limit(0, None)
+    assert int(status) == S.STATUS_TIMEOUT
+    assert all(x.isnan().all() for x in got)
+    assert torch.equal(free, want)
+    status.zero_()
+    assert torch.equal(muon_orthogonalize(M, ns_steps=4, status=status), want) and int(status) == 0
