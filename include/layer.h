@@ -33,7 +33,8 @@ extern "C" {
  * x, y: x_type, row i at element i * ld; y may be x (in place). weight, bias: `width` elements
  * of w_type (SOAP_F32 or x_type), either may be NULL (1, 0). mean, rstd: fp32 [rows] for the
  * backward pass, either may be NULL. status: NULL, or a device int32 into which the kernels OR
- * SOAP_STATUS_TIMEOUT if a bounded internal wait gave up (not cleared). rows = 0 does nothing.
+ * SOAP_STATUS_TIMEOUT if a bounded internal wait gave up (see soap_wait_limit; not cleared): the rows
+ * concerned, forward also their statistics, and backward dweight and dbias are then NaN. rows = 0 does nothing.
  * SOAP_ERR_INVALID_ARG for rows < 0 or > 2^31 - 2^16, width < 1, a leading dimension below width, a
  * type out of range, a null or misaligned pointer, or eps < 0. */
 soap_status_t layer_norm_forward(int64_t rows, int64_t width, const void* x, int64_t ld_x, int32_t x_type,

@@ -258,8 +258,9 @@ soap_status_t soap_profile_records(soap_handle h, soap_launch_record* out, int64
  * nothing sets makes the waits run out, which is how the timeout path is tested without a
  * fault. Applies to launches enqueued after the call, from any thread; soap_wait_limit(0, NULL)
  * restores the defaults. Results of a product whose wait gave up are not valid. The same settings
- * govern muon_orthogonalize (include/muon.h; matrices that it keeps on chip wait for nothing);
- * muon_step's products keep the default limit. */
+ * govern muon_orthogonalize (include/muon.h; matrices that it keeps on chip wait for nothing) and
+ * layer norm's row copies (include/layer.h; narrow rows wait for nothing), whose results are NaN
+ * where a wait gave up; muon_step's products keep the default limit. */
 soap_status_t soap_wait_limit(uint64_t limit_ns, const int32_t* hold);
 
 /* ---- stand-alone sub-steps (the same kernels soap_step runs) ------------------- */

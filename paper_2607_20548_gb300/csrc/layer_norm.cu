@@ -12,7 +12,7 @@ namespace {
 template <typename T, typename W, int V, int NV, int DEPTH, bool FULL, bool RING>
 __global__ void __launch_bounds__(threads_for(NV * V), 1)
     norm_fwd_kernel(const T* x, int64_t ld_x, const W* weight, const W* bias, float eps, T* y, int64_t ld_y,
-                    float* mean, float* rstd, int rows, int width, int* status) {
+                    float* mean, float* rstd, int rows, int width, int* status, const WaitLimit wait) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 buf[2 * 32];
   __shared__ uint64_t full[kMaxGroups][DEPTH];
@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
   Exchange ex{buf};
   const int step = gridDim.x * blockDim.y;
   int row = blockIdx.x * blockDim.y + threadIdx.y;
-  Feed in{{x}, {ld_x}, rows, step, width, smem + threadIdx.y * Feed::ring_bytes(blockDim.x), full[threadIdx.y], status};
+  Feed in{{x}, {ld_x}, rows, step, width, smem + threadIdx.y * Feed::ring_bytes(blockDim.x), full[threadIdx.y], status, wait};
   in.start(row);
   float2 w[P], b[P];
   columns<W, V, NV>(weight, 1.f, width, w);
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
     float2 acc = pair(0.f);
 #pragma unroll
     for (int i = 0; i < P; ++i) acc = add2(acc, v[i]);
-    float sum = warp_sum(acc.x + acc.y);
+    float sum = warp_sum(in.dead() ? NAN : acc.x + acc.y);
     float mu = sum * inv_here;
     acc = pair(0.f);
 #pragma unroll
@@ -133,7 +133,7 @@ cudaError_t fwd_v(int64_t rows, int64_t width, const T* x, int64_t ld_x, const W
         const cudaError_t e = allow_smem(kernel, smem, set);
         if (e != cudaSuccess) return e;
         kernel<<<grid, dim3(n.tx, ty), smem, s>>>(x, ld_x, w, b, eps, y, ld_y, mean, rstd, (int)rows, (int)width,
-                                                  status);
+                                                  status, wait_limit());
         return cudaGetLastError();
       });
     }

@@ -16,10 +16,12 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/layer.h"
 #include "profile.h"
+#include "soap_internal.h"
 #include "tc_ptx.h"
 #include "types.h"
 
@@ -31,7 +33,6 @@ constexpr int kMaxThreads = 512;  // of the kernels for rows too wide to be held
 constexpr int threads_for(int elems) { return elems <= 8 ? 1024 : 512; }
 constexpr int kMaxGroups = 16;    // row groups of a CTA
 constexpr int64_t kMaxRows = INT32_MAX - 65536;  // a row index some steps further on stays an int
-constexpr uint64_t kWaitNs = 2000000000ull;
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -72,9 +73,13 @@ struct Rows {
   uint8_t* ring;    // the group's: ring_bytes
   uint64_t* full;   // the group's barriers, one per stage
   int* status;
+  WaitLimit wait;   // soap_wait_limit's settings
   int s = 0;
+  // kDead: a wait of this thread's ran out. What it gets is invalid (a sum that it takes part in has to become
+  // NaN, and with it the row's results), and it neither waits nor asks for more.
   uint32_t parity = 0;
-  bool dead = false;  // a wait ran out: what follows is invalid, and waits for nothing
+  static constexpr uint32_t kDead = 2;
+  __device__ __forceinline__ bool dead() const { return RING && parity >= kDead; }
   Pack<T, V> ahead[RING ? 1 : N][RING ? 1 : NV];
 
   // Of a group of `threads`: a row, and the parts of its neighbours that come along.
@@ -163,7 +168,9 @@ struct Rows {
     if (threadIdx.x == 0) {
       for (int q = 0; q < DEPTH; ++q) tc::mbar_init(full + q, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      for (int q = 0; q < DEPTH; ++q) request(row + q * step, q);
+      // (a flag that nothing sets: no row comes, and the group's waits run out)
+      const bool held = wait.hold && !tc::flag_wait(wait.hold, wait.ns);
+      for (int q = 0; q < DEPTH && !held; ++q) request(row + q * step, q);
     }
     __syncthreads();
   }
@@ -177,8 +184,8 @@ struct Rows {
       load(row + step);
       return;
     }
-    if (!dead && !tc::mbar_wait(full + s, parity, kWaitNs)) {
-      dead = true;
+    if (!dead() && !tc::mbar_wait(full + s, parity, wait.ns)) {
+      parity |= kDead;
       if (status) atomicOr(status, SOAP_STATUS_TIMEOUT);
     }
 #pragma unroll
@@ -200,14 +207,16 @@ struct Rows {
   // After a point that all of the group's threads have reached since get(): the slots are free.
   __device__ __forceinline__ void refill(int row) {
     if constexpr (!RING) return;
-    if (threadIdx.x == 0) request(row + DEPTH * step, s);
+    if (threadIdx.x == 0 && !dead()) request(row + DEPTH * step, s);  // (no second copy into a slot that never filled)
     if (++s == DEPTH) {
       s = 0;
       parity ^= 1;
     }
   }
+  // After the last row.
   __device__ __forceinline__ void finish() const {
-    if (dead) {  // copies in flight land before the shared memory goes away: far above a copy's time
+    if constexpr (!RING) return;
+    if (dead()) {  // copies in flight land before the shared memory goes away: far above a copy's time
       const uint64_t t0 = tc::globaltimer();
       while (tc::globaltimer() - t0 < 10000000ull) {
       }

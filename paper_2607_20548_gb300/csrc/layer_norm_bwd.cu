@@ -20,7 +20,7 @@ template <typename T, typename W, int V, int NV, int DEPTH, bool FULL, bool RING
 __global__ void __launch_bounds__(threads_for(NV * V), 1)
     norm_bwd_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const float* mean, const float* rstd,
                     const W* weight, T* dx, int64_t ld_dx, float* part, int rows, int width,
-                    int* status) {
+                    int* status, const WaitLimit wait) {
   extern __shared__ __align__(16) uint8_t smem[];  // the rings (and weights); afterwards the groups' column sums
   __shared__ float2 buf[2 * 32];
   __shared__ uint64_t full[kMaxGroups][DEPTH];
@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
   int row = blockIdx.x * blockDim.y + threadIdx.y;
   Feed in{{x, dy},    {ld_x, ld_dy}, rows,
           step,       width,         smem + threadIdx.y * Feed::ring_bytes(blockDim.x),
-          full[threadIdx.y], status};
+          full[threadIdx.y], status, wait};
   in.start(row);
   Exchange ex{buf};
   float2 w[kSmemW ? 1 : P], aw[P], ab[P];
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
       a0 = add2(a0, g);
       a1 = fma2(g, xh, a1);
     }
-    float s0 = warp_sum(a0.x + a0.y), s1 = warp_sum(a1.x + a1.y);
+    float s0 = warp_sum(in.dead() ? NAN : a0.x + a0.y), s1 = warp_sum(a1.x + a1.y);
     if (blockDim.x > 32) {
       const float2 o = ex.all(s0, s1);
       s0 = warp_sum(o.x);
@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
   // add the groups in order, first dweight's sums, then dbias's
   float* sums = reinterpret_cast<float*>(smem);
   const int lanes = blockDim.x * E;
+  const bool none = __syncthreads_or(in.dead());  // (the rings have been read)
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     __syncthreads();
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(threads_for(NV * V), 1)
     for (int c = tid; c < width; c += threads) {
       float t = 0.f;
       for (int gq = 0; gq < (int)blockDim.y; ++gq) t += sums[gq * lanes + c];
-      out[c] = t;
+      out[c] = none ? NAN : t;
     }
   }
 }
@@ -228,7 +229,7 @@ cudaError_t bwd_v(int64_t rows, int64_t width, const T* dy, int64_t ld_dy, const
           const cudaError_t ae = allow_smem(kernel, smem, set);
           if (ae != cudaSuccess) return ae;
           kernel<<<parts, dim3(n.tx, ty), smem, s>>>(dy, ld_dy, x, ld_x, mean, rstd, w, dx, ld_dx, p, (int)rows,
-                                                     (int)width, status);
+                                                     (int)width, status, wait_limit());
           return cudaGetLastError();
         });
       }

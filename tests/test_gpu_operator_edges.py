@@ -5,7 +5,8 @@ import math
 import pytest
 import torch
 
-from paper_2607_20548_gb300 import muon_orthogonalize, route_backward, route_forward
+from paper_2607_20548_gb300 import (layer_norm_backward, layer_norm_forward, muon_orthogonalize, route_backward,
+                                    route_forward)
 from paper_2607_20548_gb300 import soap as S
 
 pytestmark = pytest.mark.gpu
@@ -122,3 +123,41 @@ def test_ortho_wait_runs_out(cuda, shape, dtype):
     assert torch.equal(free, want)
     status.zero_()
     assert torch.equal(muon_orthogonalize(M, ns_steps=4, status=status), want) and int(status) == 0
+
+
+# ---- layer norm ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,width", [(40, 2048), (700, 1537), (5000, 1024)])
+def test_norm_wait_runs_out(cuda, rows, width, dtype):
+    """As for the orthogonalisation: no row comes while the flag is unset, the waits run out (20 ms), and
+    what would have come from the rows is NaN."""
+    g = torch.Generator(device=cuda).manual_seed(width)
+    x, dy = (torch.randn(rows, width, device=cuda, generator=g).to(dtype) for _ in range(2))
+    w = torch.randn(width, device=cuda, generator=g)
+    y, mean, rstd = layer_norm_forward(x, w, w)
+    want = (y, mean, rstd, *layer_norm_backward(dy, x, mean, rstd, w))
+
+    def both(status=None):
+        return (*layer_norm_forward(x, w, w, status=status),
+                *layer_norm_backward(dy, x, mean, rstd, w, status=status))
+
+    status = [torch.zeros(1, dtype=torch.int32, device=cuda) for _ in range(2)]
+    hold = torch.zeros(1, dtype=torch.int32, device=cuda)
+    torch.cuda.synchronize()
+    try:
+        S.soap_wait_limit(20_000_000, hold)
+        layer_norm_forward(x, w, w, status=status[0])
+        layer_norm_backward(dy, x, mean, rstd, w, status=status[1])
+        got = both()
+        torch.cuda.synchronize()
+        hold.fill_(1)
+        free = both()
+        torch.cuda.synchronize()
+    finally:
+        S.soap_wait_limit(0, None)
+    assert [int(s) for s in status] == [S.STATUS_TIMEOUT] * 2
+    assert all(t.isnan().all() for t in got)
+    assert all(torch.equal(a, b) for a, b in zip(free, want))
+    clean = torch.zeros(1, dtype=torch.int32, device=cuda)
+    assert all(torch.equal(a, b) for a, b in zip(both(clean), want)) and int(clean) == 0
