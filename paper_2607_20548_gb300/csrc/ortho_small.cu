@@ -32,6 +32,10 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;  // 8 is what every GPU takes, 16 this one
 constexpr int kMaxSmem = 224 * 1024;
+// Most K elements per accumulator run of split operands. The mma's accumulator truncates as the tensor memory's
+// does, 2^-25 of a sum per 16 products: over the 3136 elements that a CTA has of 16 x 50000, S came out 1.5e-5
+// too small and the result 7.6e-6 too large; 5.4e-7 in runs of 256 that are added in fp32 (4 % of that case's time, 1 to 2 % of others).
+constexpr int kRun = 256;
 
 struct Layout {
   int r, k, tall;
@@ -294,11 +298,11 @@ __global__ void __launch_bounds__(kThreads)
 
   // rows i0 .. + 15 and n0 .. + 31 of P Q^T over K elements, P and Q with rows `pitch` apart
   auto product = [&](float (&acc)[4][4], uint32_t p_at, uint32_t plane, int pitch, int i0, int n0, int K) {
-    float small[4][4];
+    float small[4][4], runs[4][4];
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[n][q] = small[n][q] = 0.f;
+      for (int q = 0; q < 4; ++q) acc[n][q] = small[n][q] = runs[n][q] = 0.f;
     const uint32_t pa = p_at + ((i0 + a_row) * pitch + a_col) * 2;
     const uint32_t pb0 = p_at + ((n0 + b_row) * pitch + b_col) * 2, pb1 = pb0 + 16 * pitch * 2;
     const bool second = n0 + 16 < l.rp;
@@ -321,12 +325,20 @@ __global__ void __launch_bounds__(kThreads)
             mma(small[n], fa, lb[n / 2][n % 2 * 2], lb[n / 2][n % 2 * 2 + 1]);
           }
         }
+      if (SPLIT == 2 && (k + 16) % kRun == 0)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            runs[n][q] += acc[n][q];
+            acc[n][q] = 0.f;
+          }
     }
     if (SPLIT == 2)
 #pragma unroll
       for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc[n][q] += small[n][q];
+        for (int q = 0; q < 4; ++q) acc[n][q] += runs[n][q] + small[n][q];
   };
   const int nt = (l.rp + 31) / 32;
   // f(i0, n0, whether to write the mirror image too) for this warp's 16 x 32 tiles of a symmetric matrix. With

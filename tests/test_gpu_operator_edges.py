@@ -125,6 +125,24 @@ def test_ortho_wait_runs_out(cuda, shape, dtype):
     assert torch.equal(muon_orthogonalize(M, ns_steps=4, status=status), want) and int(status) == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("shape", [(16, 40000), (50000, 16), (13, 48001), (64, 12000), (6000, 100), (2, 40, 9000)])
+def test_accuracy_does_not_fall_with_a_long_side(cuda, shape, dtype):
+    """A small side and a long one. The accumulator truncates, at most a unit of its last place (2^-23) per 16
+    products, so split operands add it up in runs of 256 elements: 16 such units for any length. fp16's own
+    rounding would hide that; the check is then of the scale alone, <out, ref> / <ref, ref>, in which roundings
+    average out: 2^-11 / sqrt(elements), five times."""
+    M = _momentum(cuda, shape, dtype, seed=shape[-1])
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    out, ref = muon_orthogonalize(M, ns_steps=6, status=status).double(), _ortho_ref(M, 6)
+    assert int(status) == 0
+    tol = 2 * math.sqrt(3 * 6) * 2.0 ** -22 + 16 * 2.0 ** -23
+    if dtype == torch.float32:
+        assert float(torch.linalg.norm(out - ref) / torch.linalg.norm(ref)) <= tol + 2.0 ** -24
+    scale = float((out * ref).sum() / (ref * ref).sum())
+    assert abs(scale - 1) <= tol + 5 * torch.finfo(dtype).eps / 2 / math.sqrt(ref.numel())
+
+
 # ---- layer norm ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
