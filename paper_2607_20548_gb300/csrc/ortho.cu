@@ -33,16 +33,16 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxParts = 1216;  // partial sums of squares per matrix: 8 CTAs per SM
 
-// Squares of a pack's elements: in fp32 where no square over- or underflows (or the pack is zero),
-// else in fp64, whose rate is so low that nothing else here uses it. NaN and inf come out as such
-// either way.
+// Squares of a pack's elements: in fp32 where no square underflows and no sum of 2^31 of them
+// overflows (or the pack is zero), else in fp64, whose rate is so low that nothing else here uses
+// it. NaN and inf come out as such either way.
 template <typename T, int V>
 __device__ __forceinline__ void add_squares(const Pack<T, V>& p, float& s, double& d) {
   float m = 0.f;
 #pragma unroll
   for (int e = 0; e < V; ++e) m = fmaxf(m, fabsf(to_f32(p.v[e])));
   if (sizeof(T) == 2 && std::is_same<T, __half>::value) m = 1.f;  // no fp16 square leaves fp32's range
-  if (m == 0.f || (m > 0x1p-40f && m < 0x1p55f)) {
+  if (m == 0.f || (m > 0x1p-40f && m < 0x1p48f)) {
 #pragma unroll
     for (int e = 0; e < V; ++e) s = fmaf(to_f32(p.v[e]), to_f32(p.v[e]), s);
   } else {

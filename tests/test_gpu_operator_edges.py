@@ -143,6 +143,24 @@ def test_accuracy_does_not_fall_with_a_long_side(cuda, shape, dtype):
     assert abs(scale - 1) <= tol + 5 * torch.finfo(dtype).eps / 2 / math.sqrt(ref.numel())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("e", [45, 46, 54, 55, 60, -41, -70])
+def test_norm_of_large_and_small_elements(cuda, e, dtype):
+    """Elements of 2^e to 2^(e + 1), 2^19 of them to a CTA: neither a square nor a sum of them leaves fp32's
+    range unnoticed. X_0 does not depend on a power of two in M, so the result is that of e = 0. Beside the
+    products' error: the sum of squares, whose longest chain has 16 + 128 + 5 + 8 + 17 fp32 additions (a
+    thread's run, its runs, a warp, a CTA, the CTAs), at most 174 u, half of which reaches the norm."""
+    g = torch.Generator(device=cuda).manual_seed(7)
+    M = (1 + torch.rand(136, 65536, device=cuda, generator=g)).to(dtype).clamp_max(1.99)
+    M *= torch.randint(0, 2, M.shape, device=cuda, generator=g).to(dtype) * 2 - 1
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    out = muon_orthogonalize(M * 2.0 ** e, ns_steps=2, eps=1e-37, status=status)
+    assert int(status) == 0
+    ref = _ortho_ref(M, 2)
+    err = float(torch.linalg.norm(out.double() - ref) / torch.linalg.norm(ref))
+    assert err <= _ortho_tol(dtype, 2, 136, 1024) + 87 * U  # K in runs of 1024 at most
+
+
 # ---- layer norm ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
