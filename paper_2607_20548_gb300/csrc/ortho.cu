@@ -31,7 +31,7 @@ namespace ortho {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxParts = 1216;  // partial sums of squares per matrix: 8 CTAs per SM
+constexpr int kMaxParts = 1216;  // partial sums of squares: 8 CTAs per SM, dealt to the matrices
 
 // Squares of a pack's elements: in fp32 where no square underflows and no sum of 2^31 of them
 // overflows (or the pack is zero), else in fp64, whose rate is so low that nothing else here uses
@@ -177,6 +177,7 @@ struct Plan {
   bool split;
   int cluster;  // CTAs per matrix of the kernel for small sides; 0: run_steps
   int ld_x, ld_s;
+  int parts;    // partial sums of squares per matrix
   int64_t x_elems, s_elems;  // per buffer, planes included
   size_t part_off, t_off, done_off, x_off[2], s_off, b_off, bytes;
 };
@@ -197,6 +198,7 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
     p.bytes = 256;
     return p;
   }
+  p.parts = (int)std::min<int64_t>(std::max<int64_t>(1, kMaxParts / batch), (rows + 7) / 8);
   p.ld_x = (int)up(cols, 8);
   p.ld_s = (int)up(p.r, 8);
   const int64_t planes = batch * (p.split ? 2 : 1);
@@ -208,7 +210,7 @@ Plan make_plan(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
     off += up((int64_t)bytes, 256);
     return at;
   };
-  p.part_off = take((size_t)batch * kMaxParts * (sizeof(double) + sizeof(float)));
+  p.part_off = take((size_t)batch * p.parts * (sizeof(double) + sizeof(float)));
   p.t_off = take((size_t)batch * sizeof(float));
   p.done_off = take((size_t)(batch + kDoneExtra) * sizeof(int));
   p.x_off[0] = take((size_t)p.x_elems * 2);
@@ -267,8 +269,8 @@ template <typename T, int V>
 cudaError_t prepare(const Plan& p, const T* M, int64_t ld, int64_t stride, float eps, int sx, const Steps& q,
                     float* part_f, double* part_d, float* t, cudaStream_t s) {
   const double n = (double)p.batch * p.rows * p.cols;
-  const int64_t want = std::max<int64_t>(1, (152 * 8) / p.batch);
-  const int parts = (int)std::min<int64_t>({kMaxParts, want, (p.rows + 7) / 8});
+  const int64_t want = std::max<int64_t>(1, kMaxParts / p.batch);
+  const int parts = p.parts;
   {
     ProfScope prof(kFamElementwise, 2.0 * n, n * sizeof(T), s);
     norm_kernel<T, V><<<dim3(parts, (unsigned)p.batch), kThreads, 0, s>>>(M, ld, stride, p.rows, p.cols, part_f,
@@ -342,7 +344,7 @@ cudaError_t run(const Plan& p, const void* M, int64_t ld, int64_t stride, int32_
   q.out_exp = sx;
   if (p.cluster > 0) return run_small(q, p.cluster, M, ld, stride, eps, sx0, s);
   double* part_d = reinterpret_cast<double*>(ws + p.part_off);
-  float* part_f = reinterpret_cast<float*>(part_d + p.batch * kMaxParts);
+  float* part_f = reinterpret_cast<float*>(part_d + p.batch * p.parts);
   cudaError_t e;
   if (type == SOAP_F32)
     e = prepare_t<float>(p, M, ld, stride, eps, sx0, q, part_f, part_d, t, s);

@@ -1,0 +1,18 @@
+"""What the stand-alone operators' binding and planning do on the host: no GPU is needed."""
+import pytest
+
+from paper_2607_20548_gb300 import build
+from paper_2607_20548_gb300 import soap as S
+
+
+@pytest.mark.parametrize("batch", [1, 30, 5000, 65535])
+@pytest.mark.parametrize("rows,cols,dtype,planes", [(130, 200, 1, 1), (200, 140, 0, 2), (2000, 136, 1, 1)])
+def test_workspace_is_what_the_kernels_use(batch, rows, cols, dtype, planes):
+    """X twice, S and B in fp16 with rows of whole 16-byte units, and for all matrices together no more than
+    1216 partial sums, or one each, a scale and a counter; seven pieces rounded up to 256 bytes."""
+    build.build()
+    got = S.load_library().muon_orthogonalize_workspace_bytes(batch, rows, cols, dtype)
+    up8 = lambda n: (n + 7) // 8 * 8  # noqa: E731
+    r = min(rows, cols)
+    need = 2 * planes * batch * (2 * rows * up8(cols) + 2 * r * up8(r))
+    assert need <= got <= need + 12 * max(1216, batch) + 8 * batch + 12 + 7 * 256
