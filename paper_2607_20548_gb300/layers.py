@@ -16,8 +16,10 @@ import torch
 from .soap import DTYPES, SOAP_OK, SoapError, load_library
 
 # What every call asks torch for, without the Python objects around it (torch.cuda.current_stream(...) alone
-# costs as much as half a launch): the cudaStream_t that is current on a device, and the current device.
-_raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# costs as much as half a launch): the cudaStream_t that is current on a device, and the current device. A
+# torch without CUDA has neither, nor tensors that get as far as them.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current = getattr(torch._C, "_cuda_getDevice", None)
 _F32, _I32 = torch.float32, torch.int32
 _empty, _empty_like = torch.empty, torch.empty_like
 

@@ -1,4 +1,8 @@
 """What the stand-alone operators' binding and planning do on the host: no GPU is needed."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 from paper_2607_20548_gb300 import build
@@ -16,3 +20,22 @@ def test_workspace_is_what_the_kernels_use(batch, rows, cols, dtype, planes):
     r = min(rows, cols)
     need = 2 * planes * batch * (2 * rows * up8(cols) + 2 * r * up8(r))
     assert need <= got <= need + 12 * max(1216, batch) + 8 * batch + 12 + 7 * 256
+
+
+def test_imports_on_a_torch_without_cuda():
+    """A CPU-only torch has none of torch._C's CUDA functions: the package (its oracle-side and planning parts
+    are of use there) imports all the same, and the operators refuse what is no CUDA tensor."""
+    code = """
+import torch
+for name in [n for n in dir(torch._C) if n.startswith("_cuda_")]:
+    delattr(torch._C, name)
+import paper_2607_20548_gb300 as lib
+from paper_2607_20548_gb300 import layerwise, workloads
+try:
+    lib.layer_norm_forward(torch.zeros(2, 8))
+except TypeError:
+    print("refused")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "refused", r.stderr
