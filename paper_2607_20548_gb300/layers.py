@@ -60,8 +60,17 @@ def _rows(t):
     shape = t.shape
     width = shape[-1]
     if not t.is_contiguous():
-        if len(shape) == 2 and (t.stride(1) == 1 or width == 1) and t.stride(0) >= width:
-            return t, shape[0], t.stride(0)
+        rows, ld = 1, width
+        for n, step in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+            if n == 1:
+                continue
+            if rows == 1:
+                ld = step
+            elif step != rows * ld:
+                ld = 0
+            rows *= n
+        if ld >= width and (t.stride(-1) == 1 or width == 1):
+            return t, rows, ld
         t = t.contiguous()
     if len(shape) == 2:
         return t, shape[0], width

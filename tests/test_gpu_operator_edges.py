@@ -197,3 +197,29 @@ def test_norm_wait_runs_out(cuda, rows, width, dtype):
     assert all(torch.equal(a, b) for a, b in zip(free, want))
     clean = torch.zeros(1, dtype=torch.int32, device=cuda)
     assert all(torch.equal(a, b) for a, b in zip(both(clean), want)) and int(clean) == 0
+
+
+# ---- layouts -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("off,width", [(0, 64), (8, 64), (3, 61), (0, 512), (5, 507)])
+def test_slices_of_every_row(cuda, off, width, dtype):
+    """x[..., a:b] of more than two dimensions: read where it lies, with the dense tensor's bits where the rows'
+    alignment leaves the same kernel, and its values to rounding where not."""
+    g = torch.Generator(device=cuda).manual_seed(width)
+    x, dy = (torch.randn(3, 5, 4, width + 16, device=cuda, generator=g).to(dtype)[..., off:off + width] for _ in range(2))
+    assert not x.is_contiguous()
+    w = torch.randn(width, device=cuda, generator=g)
+    y, mean, rstd = layer_norm_forward(x, w, w)
+    want = layer_norm_forward(x.contiguous(), w, w)
+    assert y.shape == x.shape and y.is_contiguous() and mean.shape == x.shape[:-1]
+    tol = dict(rtol=2 * torch.finfo(dtype).eps, atol=64 * U * 8)  # one rounding each; statistics within 64 u
+    torch.testing.assert_close(y, want[0], **tol)
+    got = layer_norm_backward(dy, x, mean, rstd, w)
+    ref = layer_norm_backward(dy.contiguous(), x.contiguous(), *want[1:], w)
+    torch.testing.assert_close(got[0], ref[0], **tol)
+    for a, b in zip(got[1:], ref[1:]):  # 60 rows' sums of terms up to 30
+        torch.testing.assert_close(a, b, rtol=0, atol=60 * 30 * 4 * U)
+    r, q = route_forward(x, 4), route_forward(x.contiguous(), 4)
+    assert all(torch.equal(a, b) for a, b in zip(r[:7], q[:7]))
+    assert torch.equal(route_backward(x, r, dgates=r.gates), route_backward(x.contiguous(), q, dgates=q.gates))

@@ -4,8 +4,9 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
-from paper_2607_20548_gb300 import build
+from paper_2607_20548_gb300 import build, layers
 from paper_2607_20548_gb300 import soap as S
 
 
@@ -39,3 +40,32 @@ except TypeError:
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "refused", r.stderr
+
+
+@pytest.mark.parametrize("make,copies", [
+    (lambda t: t, False),
+    (lambda t: t[..., :5], False),              # a slice of every row
+    (lambda t: t[..., 2:7], False),
+    (lambda t: t[:1, 1:2, :, :5], False),       # dimensions of one
+    (lambda t: t[1:, :, :, 3:], False),
+    (lambda t: t[0], False),
+    (lambda t: t[0, 0, :, 1:], False),
+    (lambda t: t[:, :, 0, :5], False),          # a longer step between rows
+    (lambda t: t[:, :, ::2], False),
+    (lambda t: t[..., 0:1], False),
+    (lambda t: t[0, 0, 0, 1:4], False),
+    (lambda t: t[..., ::2], True),              # elements apart
+    (lambda t: t[:, 1:, :, :5], True),          # two steps between rows
+    (lambda t: t[:, 1:2, :, :5], True),
+    (lambda t: t[:, :, :1, :5].expand(2, 3, 4, 5), True),
+    (lambda t: t.transpose(0, 1)[..., :5], True),
+    (lambda t: t.mT, True),
+    (lambda t: t[0, 0, 0, ::3], True),
+])
+def test_rows_are_copied_only_where_no_leading_dimension_describes_them(make, copies):
+    t = make(torch.arange(2 * 3 * 4 * 9, dtype=torch.float32).view(2, 3, 4, 9))
+    got, rows, ld = layers._rows(t)
+    width = t.shape[-1]
+    assert (got.data_ptr() != t.data_ptr()) == copies
+    assert rows == t.numel() // width and ld >= width
+    assert torch.equal(torch.as_strided(got, (rows, width), (ld, 1), got.storage_offset()), t.reshape(rows, width))
