@@ -4,7 +4,9 @@ backward (include/layer.h), and the orthogonalisation of a momentum (include/muo
 Argument checks and marshalling only, as in ``soap``: outputs and workspaces are allocated here
 with torch, on the operands' device, and everything is computed by libsoap.so on the given stream
 (the current one by default). A tensor that the caller made on another stream has to be ordered
-before the call by the caller, as for any stream-ordered work.
+before the call by the caller, as for any stream-ordered work; it may be dropped as soon as the call
+returns, since the given stream is recorded on it. Results belong to the given stream, as tensors
+made under ``torch.cuda.stream`` do: order their uses elsewhere after it.
 """
 from __future__ import annotations
 
@@ -44,12 +46,16 @@ def _operand(name, t, dtype=None, device=None):
     return t.device
 
 
-def _elsewhere(index, stream):
+def _elsewhere(index, stream, *operands):
     """The context in which a call has to run and allocate if that is not the present one: the given
-    stream (outputs and workspaces then come from its memory pool), or the operands' device."""
+    stream (outputs and workspaces then come from its memory pool; the operands' memory is not given out
+    again before what that stream has of theirs to do), or the operands' device."""
     if stream is not None:
         if torch.device(stream.device).index != index:
             raise ValueError(f"stream of {stream.device} given for work on cuda:{index}")
+        for t in operands:
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
         return torch.cuda.stream(stream)
     return None if _current() == index else torch.cuda.device(index)
 
@@ -109,7 +115,7 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
         _refuse(name, x, None, None)
     index = x.get_device()
     if stream is not None or index != _current():
-        with _elsewhere(index, stream):
+        with _elsewhere(index, stream, x, weight, bias, status):
             return layer_norm_forward(x, weight, bias, eps, status)
     if status is not None:
         _operand(name, status, _I32, x.device)
@@ -139,7 +145,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
         _refuse(name, x, None, None)
     index = x.get_device()
     if stream is not None or index != _current():
-        with _elsewhere(index, stream):
+        with _elsewhere(index, stream, dy, x, mean, rstd, weight, status):
             return layer_norm_backward(dy, x, mean, rstd, weight, params, status)
     dev = x.device
     _operand(name, dy, x.dtype, dev)
@@ -199,7 +205,7 @@ def route_forward(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = N
     name = "route_forward"
     dev = _operand(name, logits)
     if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream):
+        with _elsewhere(dev.index, stream, logits, mask, status):
             return route_forward(logits, k, mask, normalize, coef, status)
     if logits.dim() < 1:
         raise ValueError(f"{name}: needs at least one dimension")
@@ -237,7 +243,7 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
     name = "route_backward"
     dev = _operand(name, logits)
     if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream):
+        with _elsewhere(dev.index, stream, logits, dgates, *routing):
             return route_backward(logits, routing, dgates, dloss)
     shape, shape_k = logits.shape, routing.indices.shape
     if logits.dim() < 1 or shape_k[:-1] != shape[:-1] or routing.counts.shape[0] != shape[-1]:
@@ -294,7 +300,7 @@ def muon_orthogonalize(M: torch.Tensor, coeffs=None, ns_steps: int = 16, eps: fl
     name = "muon_orthogonalize"
     dev = _operand(name, M)
     if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream):
+        with _elsewhere(dev.index, stream, M, status):
             return muon_orthogonalize(M, coeffs, ns_steps, eps, status)
     if status is not None:
         _operand(name, status, _I32, dev)

@@ -223,3 +223,76 @@ def test_slices_of_every_row(cuda, off, width, dtype):
     r, q = route_forward(x, 4), route_forward(x.contiguous(), 4)
     assert all(torch.equal(a, b) for a, b in zip(r[:7], q[:7]))
     assert torch.equal(route_backward(x, r, dgates=r.gates), route_backward(x.contiguous(), q, dgates=q.gates))
+
+
+# ---- streams -------------------------------------------------------------------------------
+
+def _norm_args(cuda):
+    x = torch.ones(3500, 1100, device=cuda)  # 15 MB: a block of its own, which the next such tensor would get
+    w, m = torch.ones(1100, device=cuda), torch.ones(3500, device=cuda)
+    return dict(x=x, w=w, m=m, dy=x.clone())
+
+
+CALLS = {
+    "x forward": ("x", _norm_args, lambda a, s: layer_norm_forward(a["x"], a["w"], a["w"], stream=s)),
+    "x backward": ("x", _norm_args, lambda a, s: layer_norm_backward(a["dy"], a["x"], a["m"], a["m"], a["w"], stream=s)),
+    "dy": ("dy", _norm_args, lambda a, s: layer_norm_backward(a["dy"], a["x"], a["m"], a["m"], a["w"], stream=s)),
+    "logits": ("z", lambda cuda: dict(z=torch.ones(60000, 64, device=cuda)),
+               lambda a, s: route_forward(a["z"], 4, stream=s)),
+    "mask": ("mask", lambda cuda: dict(z=torch.ones(15000000, 1, device=cuda),
+                                          mask=torch.ones(15000000, dtype=torch.bool, device=cuda)),
+             lambda a, s: route_forward(a["z"], 1, mask=a["mask"], stream=s)),
+    "M": ("M", lambda cuda: dict(M=torch.ones(40, 300, 320, device=cuda)),
+          lambda a, s: muon_orthogonalize(a["M"], ns_steps=2, stream=s)),
+}
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_operands_outlive_the_call_on_its_stream(cuda, name):
+    """The caller may drop an operand as soon as a call on another stream returns (a temporary: f(a + b,
+    stream=s)): its memory is not given out again while that stream has yet to read it."""
+    key, make, call = CALLS[name]
+    args = make(cuda)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)  # 0.1 s: the call's kernels wait behind it
+    call(args, s)
+    shape, dtype, at = args[key].shape, args[key].dtype, args[key].data_ptr()
+    del args[key]
+    fresh = torch.empty(shape, dtype=dtype, device=cuda)
+    busy = not s.query()
+    same = fresh.data_ptr() == at
+    s.synchronize()
+    assert busy and not same
+
+
+@pytest.mark.parametrize("key", ["logits", "dgates", "indices", "stats", "mask"])
+def test_routing_outlives_the_backward_call_on_its_stream(cuda, key):
+    t, e, k = 15000000, 2, 1
+    z = torch.zeros(t, e, device=cuda)
+    mask = torch.ones(t, dtype=torch.bool, device=cuda)
+    r = route_forward(z, k, mask=mask)
+    dg = torch.ones(t, k, device=cuda)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    route_backward(z, r, dgates=dg, stream=s)
+    held = dict(logits=z, dgates=dg, indices=r.indices, stats=r.stats, mask=mask)
+    shape, dtype, at = held[key].shape, held[key].dtype, held[key].data_ptr()
+    drop = held.pop(key)
+    if key in ("indices", "stats", "mask"):
+        r = r._replace(**{key: None})
+    if key == "logits":
+        z = None
+    elif key == "dgates":
+        dg = None
+    elif key == "mask":
+        mask = None
+    del drop
+    fresh = torch.empty(shape, dtype=dtype, device=cuda)
+    busy = not s.query()
+    same = fresh.data_ptr() == at
+    s.synchronize()
+    assert busy and not same
