@@ -296,3 +296,136 @@ def test_routing_outlives_the_backward_call_on_its_stream(cuda, key):
     same = fresh.data_ptr() == at
     s.synchronize()
     assert busy and not same
+
+
+# ---- results over operands -----------------------------------------------------------------
+# What the headers allow of the C calls: the binding always makes new results.
+
+def _call(fn, *args):
+    args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
+    assert getattr(S.load_library(), fn)(*args, torch.cuda.current_stream().cuda_stream) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,width", [(3, 1), (500, 100), (4000, 1023), (700, 1537), (5000, 1024), (3000, 2051), (400, 8192),
+                                        (200, 8191), (12, 16384), (5, 20000)])
+def test_norm_in_place(cuda, rows, width, dtype):
+    """y = x, dx = dy and dx = x, among them rows that share 16-byte units with their neighbours, which other
+    CTAs read ahead and write: the bits of the calls with results of their own."""
+    g = torch.Generator(device=cuda).manual_seed(rows)
+    x, dy = (torch.randn(rows, width, device=cuda, generator=g).to(dtype) for _ in range(2))
+    w = torch.randn(width, device=cuda, generator=g)
+    t = S.DTYPES[dtype]
+    y, mean, rstd = layer_norm_forward(x, w, w)
+    dx, dw, db = layer_norm_backward(dy, x, mean, rstd, w)
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    for _ in range(3):
+        buf, m2, r2 = x.clone(), torch.empty_like(mean), torch.empty_like(rstd)
+        _call("layer_norm_forward", rows, width, buf, width, t, w, w, 0, 1e-5, buf, width, m2, r2, status)
+        assert torch.equal(buf, y) and torch.equal(m2, mean) and torch.equal(r2, rstd)
+        need = S.load_library().layer_norm_workspace_bytes(rows, width)
+        for over_x in (False, True):
+            bx, bg, w2, b2 = x.clone(), dy.clone(), torch.empty_like(dw), torch.empty_like(db)
+            ws = torch.empty(need, dtype=torch.uint8, device=cuda)
+            out = bx if over_x else bg
+            _call("layer_norm_backward", rows, width, bg, width, bx, width, t, mean, rstd, w, 0, out, width, w2, b2, ws,
+                  need, status)
+            assert torch.equal(out, dx) and torch.equal(w2, dw) and torch.equal(b2, db)
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,e,k", [(37, 8, 2), (1000, 64, 8), (1000, 127, 6), (3000, 500, 10), (20000, 64, 8), (20001, 127, 6),
+                                        (16000, 33, 3), (16000, 300, 4), (16000, 61, 9)])
+def test_routing_gradient_over_the_logits(cuda, tokens, e, k, dtype):
+    """dlogits = logits, dense and with a leading dimension: the gradient's bits, and nothing written between
+    the rows."""
+    g = torch.Generator(device=cuda).manual_seed(tokens)
+    z = torch.randn(tokens, e, device=cuda, generator=g).to(dtype)
+    mask = torch.rand(tokens, device=cuda, generator=g) < 0.8
+    r = route_forward(z, k, mask=mask, coef=0.3)
+    dg = torch.randn(tokens, k, device=cuda, generator=g)
+    want = route_backward(z, r, dgates=dg, dloss=2.0)
+    for pad in (0, 8, 3):
+        big = torch.full((tokens, e + pad), 7.0, device=cuda, dtype=dtype)
+        big[:, :e] = z
+        _call("layer_route_backward", tokens, e, k, big, e + pad, S.DTYPES[dtype], mask, 1, 0.3, 2.0, r.indices, r.stats,
+              r.counts, r.live, dg, big, e + pad)
+        assert torch.equal(big[:, :e], want) and bool((big[:, e:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 64, 2048), (3, 90, 130), (5, 200, 50), (2, 300, 700), (1, 2400, 300), (3, 333, 257)])
+def test_orthogonalize_in_place(cuda, batch, rows, cols, dtype):
+    """out = M, dense and with padded rows and matrices: the bits of the call with a result of its own."""
+    M = _momentum(cuda, (batch, rows, cols), dtype, seed=rows)
+    lib, t = S.load_library(), S.DTYPES[dtype]
+    need = lib.muon_orthogonalize_workspace_bytes(batch, rows, cols, t)
+    ws = torch.empty(need, dtype=torch.uint8, device=cuda)
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    for pad in (0, 8, 3):
+        ld, stride = cols + pad, (rows + 1) * (cols + pad)
+        buf = torch.full((batch, rows + 1, ld), 7.0, device=cuda, dtype=dtype)
+        buf[:, :rows, :cols] = M
+        out = torch.empty(batch, rows + 1, ld, device=cuda, dtype=dtype)
+        _call("muon_orthogonalize", batch, rows, cols, buf, ld, stride, t, None, 5, 1e-7, out, ld, stride, ws, need, status)
+        _call("muon_orthogonalize", batch, rows, cols, buf, ld, stride, t, None, 5, 1e-7, buf, ld, stride, ws, need, status)
+        assert torch.equal(buf[:, :rows, :cols], out[:, :rows, :cols])
+        assert bool((buf[:, rows:] == 7.0).all()) and bool((buf[:, :rows, cols:] == 7.0).all())
+        ref = _ortho_ref(M, 5)
+        assert float(torch.linalg.norm(buf[:, :rows, :cols].double() - ref) / torch.linalg.norm(ref)) <= _ortho_tol(
+            dtype, 5, rows, cols)
+    assert int(status) == 0
+
+
+# ---- sizes between the kernels' ------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("shape", [(2400, 300), (300, 2400), (2, 4500, 520), (5000, 1100), (128, 20000), (20000, 100), (65, 40000)])
+def test_many_row_tiles_and_long_sides(cuda, shape, dtype):
+    """More than eight row tiles, which are taken in groups of eight, and small sides too long for a cluster."""
+    M = _momentum(cuda, shape, dtype, seed=shape[-1])
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    out = muon_orthogonalize(M, ns_steps=5, status=status)
+    ref = _ortho_ref(M, 5)
+    assert int(status) == 0
+    # split operands: K in runs of at most 1024
+    k = 1024 if dtype != torch.bfloat16 else max(shape[-2:])
+    assert float(torch.linalg.norm(out.double() - ref) / torch.linalg.norm(ref)) <= _ortho_tol(dtype, 5, k, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rows,width", [(6000, 8192), (5000, 8191), (3000, 12288), (2600, 16384), (2500, 16379), (40000, 520),
+                                        (9000, 4096)])
+def test_many_wide_rows(cuda, rows, width, dtype):
+    """Many rows, so that every CTA's loop goes round often with many elements per thread. Bounds: a row's sums
+    within 32 u of their terms' magnitudes and what follows within 64 u (as in test_gpu_layer_norm.py, here with
+    |x - mu| below 6 deviations), one rounding to the type; column sums in runs of rows / 152 terms."""
+    g = torch.Generator(device=cuda).manual_seed(rows)
+    x, dy = (torch.randn(rows, width, device=cuda, generator=g).to(dtype) for _ in range(2))
+    w = 1 + 0.2 * torch.randn(width, device=cuda, generator=g)
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    y, mean, rstd = layer_norm_forward(x, w, w, status=status)
+    dx, dw, db = layer_norm_backward(dy, x, mean, rstd, w, status=status)
+    assert int(status) == 0
+    half = torch.finfo(dtype).eps / 2
+    rw, rb, aw, ab = (torch.zeros(width, dtype=torch.float64, device=cuda) for _ in range(4))
+    for i in range(0, rows, 1000):
+        xd, gd, wd = x[i:i + 1000].double(), dy[i:i + 1000].double(), w.double()
+        var, mu = torch.var_mean(xd, 1, correction=0, keepdim=True)
+        rs = (var + 1e-5).rsqrt()
+        xh = (xd - mu) * rs
+        want = xh * wd + wd
+        assert bool(((y[i:i + 1000].double() - want).abs() <= (half * 1.001 + 4 * U) * want.abs()
+                     + (32 + 64 * 8) * U * wd.abs()).all())
+        gw = gd * wd
+        want = rs * (gw - gw.mean(1, keepdim=True) - xh * (gw * xh).mean(1, keepdim=True))
+        assert bool(((dx[i:i + 1000].double() - want).abs() <= half * 1.001 * want.abs()
+                     + rs * 128 * U * (gw.abs() + gw.abs().mean(1, keepdim=True) + xh.abs() + 1)).all())
+        rw += (gd * xh).sum(0)
+        rb += gd.sum(0)
+        aw += (gd * xh).abs().sum(0)
+        ab += gd.abs().sum(0)
+    k = (rows / 152 + 200) * U
+    assert bool(((dw.double() - rw).abs() <= (k + 128 * U) * aw + 32 * U * ab).all())
+    assert bool(((db.double() - rb).abs() <= k * ab).all())
