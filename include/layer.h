@@ -10,9 +10,10 @@
  * Conventions: those of include/soap.h (stream-ordered calls, host-side validation that returns
  * a status code before anything is enqueued, no kernel traps, the caller owns every buffer,
  * workspaces included) with these differences: a row-major operand may have any alignment its
- * type allows and any leading dimension >= its width (aligned rows are read 16 bytes at a time;
- * others element by element), and its type is one of soap_dtype_t. Sums, statistics and
- * exponentials are fp32 whatever the type; every result is rounded once. The calls run on the
+ * type allows and any leading dimension >= its width (rows that are no whole 16-byte units may
+ * take longer), and its type is one of soap_dtype_t. Sums, statistics and exponentials are fp32
+ * whatever the type (e^x is the hardware's 2^(x log2 e), relative error 2^-22 + |x| 2^-24); every
+ * result is rounded once. The calls run on the
  * device that is current for the calling thread, which must be the operands' and the stream's.
  * The results do not depend on scheduling: the same inputs give the same bits.
  */

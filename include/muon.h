@@ -95,7 +95,9 @@ void muon_destroy(muon_handle h);
  * and keeps: any sides of 1 .. 65536 (rows * cols < 2^31), any leading dimension >= cols and any
  * alignment of the type, types of soap_dtype_t in and (the same one) out, and intermediates of 11
  * bits (bf16) or 22 bits (fp32, fp16) with fp32 accumulation, so that a bf16 result carries its
- * own rounding and little more, and an fp32 result is fp32-accurate.
+ * own rounding and little more (1.8e-3 from the exact result where rounding alone leaves 1.65e-3;
+ * a caller who wants bf16 matrices in 22 bits passes them as fp32, at three products for one), and
+ * an fp32 result is within a few 1e-6.
  *
  * Matrix b starts at M + b * stride elements, row i at i * ld; `out` likewise (out may be M itself
  * with the same strides, and must not overlap it otherwise). coeffs: host array of 3 * ns_steps floats,
@@ -108,9 +110,9 @@ void muon_destroy(muon_handle h);
  * thread. A zero matrix gives zeros.
  *
  * Precision beyond rounding: a step multiplies small singular values by a_i, so rounding noise in
- * X_0 (2^-12 of an element, bf16: none; 2^-23 for fp32) reappears in the directions whose singular
- * values lie below that noise; in exact arithmetic those are as undetermined as the input's own
- * last bit. */
+ * X_0 (2^-23 of an element for fp32, none for bf16 and fp16; for any type at least 2^-37 of the
+ * norm) reappears in the directions whose singular values lie below that noise; in exact arithmetic
+ * those are as undetermined as the input's own last bit. */
 size_t muon_orthogonalize_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int32_t type);
 soap_status_t muon_orthogonalize(int32_t batch, int64_t rows, int64_t cols, const void* M, int64_t ld, int64_t stride,
                                  int32_t type, const float* coeffs, int32_t ns_steps, float eps, void* out,

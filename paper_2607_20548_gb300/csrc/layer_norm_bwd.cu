@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kMaxThreads)
 // dweight and dbias from `parts` partial rows each: 32 columns per CTA, 32 row lanes.
 __global__ void norm_cols_kernel(const float* part, int parts, int64_t width, float* dweight, float* dbias) {
   __shared__ float red[32][33];
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch overlaps the end of the kernel before
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched ahead: it starts as the last CTAs of the kernel before exit
   const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
   float* out = blockIdx.y == 0 ? dweight : dbias;
   if (!out) return;

@@ -34,7 +34,8 @@ constexpr int kMaxCluster = 16;  // 8 is what every GPU takes, 16 this one
 constexpr int kMaxSmem = 224 * 1024;
 // Most K elements per accumulator run of split operands. The mma's accumulator truncates as the tensor memory's
 // does, 2^-25 of a sum per 16 products: over the 3136 elements that a CTA has of 16 x 50000, S came out 1.5e-5
-// too small and the result 7.6e-6 too large; 5.4e-7 in runs of 256 that are added in fp32 (4 % of that case's time, 1 to 2 % of others).
+// too small and the result 7.6e-6 too large; 5.4e-7 in runs of 256 that are added in fp32 (4 % of that case's
+// time, 1 to 2 % of others').
 constexpr int kRun = 256;
 
 struct Layout {

@@ -19,8 +19,9 @@
 // matrices of 2048 x 8192, where S tiles take four times as long as others, and 13% with 5 of 777 x 1365.) A
 // tile waits until its matrix's tiles of the phase before are stored, which a counter per matrix tells;
 // such a wait always points to tiles earlier in the list, which are taken, so with all pairs resident (a
-// cooperative launch) it ends. Against a launch per product (measured at 64 matrices of 768 x 2048: 337 us
-// a step, here 201) this has no partly filled last wave per product and no launch latency.
+// cooperative launch) it ends. Against a launch per product (337 us a step at 64 matrices of 768 x 2048, here
+// 237 in a row of calls under the power limit) this has no partly filled last wave per product and no launch
+// latency.
 //
 // In a CTA, one warp takes tiles and waits for their inputs, two issue TMA loads of A's and B's 64-element K
 // slices into a ring (on the diagonal of S and B, A's alone: both operands are the same rows), one (of the
@@ -36,7 +37,7 @@
 // What bounds it: at 8192 x 8192 the tensor cores (1.83 PFLOP/s, 0.95 of what a library product of that size
 // reaches); with K of 768 to 2048 the operands' way from L2 (1.3 to 1.6 PFLOP/s: with both loading threads
 // ahead and the ring full, the MMAs wait a quarter of the time for data); with a few matrices of a few tiles
-// the chain of phases, each the time of a tile and of handing it on (fp16 1365 x 777: 90 us a step).
+// the chain of phases, each the time of a tile and of handing it on (fp16 1365 x 777: 84 us a step).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -12,7 +12,9 @@
 // only when two lanes hold the largest one. Instructions bound it (measured: 440 per token of 127 fp32
 // logits with k = 6, backward 224; 30000 x 512 fp32, k = 8: 94 us, backward 46), so what each exchange
 // does is kept to a minimum and the gates are computed once per choice, by the lane that writes it. Calls
-// with enough tokens to fill the GPU go to route_tile.cu, at a third of that; few tokens need the lanes.
+// with enough tokens to fill the GPU, k of up to 8 and rows of up to 768 bytes (192 fp32 logits, 384 of 16
+// bits) go to route_tile.cu, at a third of that; few tokens need the lanes, and wider rows and larger k stay
+// here for want of a tile kernel.
 //
 // Column sums of p stay in registers over all of a warp's tokens, counts in shared memory. A cluster
 // adds its CTAs' sums through distributed shared memory in a fixed order; one cluster finishes by
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(1024)
   __shared__ float red[32];
   __shared__ int total;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch overlaps the end of the kernel before
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched ahead: it starts as the last CTAs of the kernel before exit
   const int blocks = (experts + 31) / 32, ways = 32 / blocks;  // at most 32 blocks of columns
   const int block = warp % blocks, way = warp / blocks, c = block * 32 + lane;
   float v = 0.f;

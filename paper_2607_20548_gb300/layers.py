@@ -7,6 +7,10 @@ with torch, on the operands' device, and everything is computed by libsoap.so on
 before the call by the caller, as for any stream-ordered work; it may be dropped as soon as the call
 returns, since the given stream is recorded on it. Results belong to the given stream, as tensors
 made under ``torch.cuda.stream`` do: order their uses elsewhere after it.
+
+The calls know nothing of autograd: a tensor that requires gradients is taken as its values, and results
+are detached (the backward passes are calls of their own). ``status`` is optional everywhere: without it a
+bounded device wait that gave up shows in the results alone, as NaN.
 """
 from __future__ import annotations
 
@@ -239,7 +243,8 @@ def route_forward(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = N
 
 def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torch.Tensor] = None, dloss: float = 1.0,
                    stream=None) -> torch.Tensor:
-    """dlogits (logits' shape and type) from the gates' gradient (fp32, None for zero) and the loss's."""
+    """dlogits (logits' shape and type) from the gates' gradient (fp32, None for zero) and the loss's (dloss, a
+    host number). It is linear in both: a scale of the two that is on the device multiplies the result."""
     name = "route_backward"
     dev = _operand(name, logits)
     if stream is not None or dev.index != _current():

@@ -406,8 +406,9 @@ def soap_qr_static(P: torch.Tensor, tol: float = 0.0, stream=None, return_status
 
 
 def soap_wait_limit(limit_ns: int = 0, hold: torch.Tensor | None = None):
-    """soap_wait_limit: bound of the tensor-core products' device waits (0 = default 2 s) and an
-    optional int32 CUDA flag their epilogues first wait for (testing the timeout path)."""
+    """soap_wait_limit: bound of the device waits (the optimizer's tensor-core products, muon_orthogonalize, layer
+    norm's row copies; 0 = default 2 s) and an optional int32 CUDA flag that they first wait for (testing the
+    timeout path)."""
     if hold is not None:
         _one_device("soap_wait_limit hold", hold, dtype=torch.int32)
     _check(load_library().soap_wait_limit(int(limit_ns), ctypes.c_void_p(hold.data_ptr()) if hold is not None else None))
