@@ -6,6 +6,8 @@
  *                  the bias's gradients
  *   layer_route_*  a mixture-of-experts router's decision: softmax, the k largest logits with
  *                  their gates, per-expert counts, the balance loss, and the logits' gradient
+ *   layer_qk_*     norms of queries and keys for each head and their rotation by position, and the
+ *                  backward pass
  *
  * Conventions: those of include/soap.h (stream-ordered calls, host-side validation that returns
  * a status code before anything is enqueued, no kernel traps, the caller owns every buffer,
@@ -93,6 +95,50 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
                                    const int32_t* indices, const float* stats, const int32_t* counts,
                                    const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d,
                                    soap_stream_t stream);
+
+/* Heads of `dim` contiguous elements: of token s of sequence b, head h, at
+ * b * batch_stride + s * token_stride + h * head_stride. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} layer_heads_t;
+
+/* Queries and keys, `heads` and `kv_heads` of each of batch * length tokens: a root-mean-square norm for each
+ * head and the rotation of its first `rotary` elements by the token's position:
+ *   n = x / sqrt(mean(x^2) + eps),  m = n * weight  (the sum of x^2 is fp32: |x| up to 2^59),
+ *   (a, b) -> (a c - b s, b c + a s) for the pairs (m_j, m_{j + rotary / 2}) or, `interleaved`,
+ *   (m_2j, m_{2j + 1}), with c = cos[p][j], s = sin[p][j]; the other elements stay m
+ * cos, sin: fp32 [places][rotary / 2]. positions: device int32, or int64 with positions_64, [batch * length],
+ * or NULL: a token's place in its sequence. A position outside 0 .. places - 1 makes its token's results NaN, and
+ * SOAP_STATUS_RANGE is ORed into *status (if not NULL; not cleared). q, k and the results: `type`;
+ * q_weight, k_weight: dim elements of w_type (SOAP_F32 or `type`), either may be NULL (1). Results may be
+ * the operands themselves (in place). Sums are fp32, each result is rounded once.
+ * dim: even, 2 .. 512; rotary: even, 0 .. dim (0: cos, sin may be NULL, positions are not read);
+ * heads, kv_heads: 0 .. 32768 (0: q, k and their results are not read and may be NULL); batch * length <=
+ * 2^31 - 2^16; eps >= 0. Operands' strides may be 0 (one head or token for several); results' heads must not
+ * overlap, nor a result's any operand's but its own. Heads whose parts are 16-byte aligned (strides,
+ * rotary / 2 and dim / 2 of whole 16-byte units) move fastest. */
+soap_status_t layer_qk_forward(int64_t batch, int64_t length, int32_t heads, int32_t kv_heads, int32_t dim,
+                               int32_t rotary, int32_t interleaved, const layer_heads_t* q, const layer_heads_t* k,
+                               int32_t type, const void* q_weight, const void* k_weight, int32_t w_type, float eps,
+                               const float* cos, const float* sin, int64_t places, const void* positions,
+                               int32_t positions_64, const layer_heads_t* q_out, const layer_heads_t* k_out,
+                               int32_t* status, soap_stream_t stream);
+
+/* The backward pass from the operands of the forward call: with dm the gradient turned back, g = dm * weight,
+ *   dx = (g - n mean(g n)) / sqrt(mean(x^2) + eps),  dweight = sum over tokens and heads of dm n
+ * dq, dk: the results' gradients; dx_q, dx_k: receive the operands' (may be dq, dk, q or k). d_qweight, d_kweight:
+ * fp32 [dim] or both NULL (not formed); NaN where a position is out of range. `workspace`: 16-byte
+ * aligned, layer_qk_workspace_bytes(...) bytes (NULL when neither is formed). */
+size_t layer_qk_workspace_bytes(int64_t batch, int64_t length, int32_t heads, int32_t kv_heads, int32_t dim);
+soap_status_t layer_qk_backward(int64_t batch, int64_t length, int32_t heads, int32_t kv_heads, int32_t dim,
+                                int32_t rotary, int32_t interleaved, const layer_heads_t* dq,
+                                const layer_heads_t* dk, const layer_heads_t* q, const layer_heads_t* k,
+                                int32_t type, const void* q_weight, const void* k_weight, int32_t w_type, float eps,
+                                const float* cos, const float* sin, int64_t places, const void* positions,
+                                int32_t positions_64, const layer_heads_t* dx_q, const layer_heads_t* dx_k,
+                                float* d_qweight, float* d_kweight, int32_t* status, void* workspace,
+                                size_t workspace_bytes, soap_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -270,6 +270,7 @@ soap_status_t soap_wait_limit(uint64_t limit_ns, const int32_t* hold);
 #define SOAP_STATUS_NONFINITE 1     /* a non-finite value in the input */
 #define SOAP_STATUS_QR_BREAKDOWN 2  /* a QR pivot norm was not finite */
 #define SOAP_STATUS_TIMEOUT 4       /* a bounded device-side wait gave up (results invalid) */
+#define SOAP_STATUS_RANGE 8         /* an index or offset in device memory was out of range */
 
 /* S3, Alg. 1 "QR(L_t Q_L).Q": for `batch` square n x n matrices P (device,
  * contiguous, batch stride n*n), writes Q with P = Q R and diag(R) >= 0 (blocked

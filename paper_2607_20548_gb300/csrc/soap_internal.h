@@ -15,6 +15,7 @@ enum : int {
   kStatusNonFinite = 1,
   kStatusQrBreakdown = 2,
   kStatusTimeout = 4,
+  kStatusRange = 8,
 };
 
 // A batched matrix operand: matrix b starts at (ptrs ? ptrs[b] : base + b * stride) + offset.

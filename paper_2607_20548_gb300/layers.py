@@ -1,5 +1,6 @@
-"""Binding of the stand-alone operators of a training step: layer norm and expert routing, forward and
-backward (include/layer.h), and the orthogonalisation of a momentum (include/muon.h).
+"""Binding of the stand-alone operators of a training step: layer norm, expert routing, and queries' and keys'
+norms with their rotation, forward and backward (include/layer.h), and the orthogonalisation of a momentum
+(include/muon.h).
 
 Argument checks and marshalling only, as in ``soap``: outputs and workspaces are allocated here
 with torch, on the operands' device, and everything is computed by libsoap.so on the given stream
@@ -15,11 +16,12 @@ bounded device wait that gave up shows in the results alone, as NaN.
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import NamedTuple, Optional
 
 import torch
 
-from .soap import DTYPES, SOAP_OK, SoapError, load_library
+from .soap import DTYPES, SOAP_OK, SoapError, layer_heads, load_library
 
 # What every call asks torch for, without the Python objects around it (torch.cuda.current_stream(...) alone
 # costs as much as half a launch): the cudaStream_t that is current on a device, and the current device. A
@@ -268,6 +270,126 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
         routing.indices.data_ptr(), routing.stats.data_ptr(), routing.counts.data_ptr(), routing.live.data_ptr(),
         None if dgates is None else dgates.data_ptr(), dz.data_ptr(), shape[-1], _raw_stream(dev.index)), name)
     return dz
+
+
+def _heads(name, t, dtype, dev):
+    """(tensor, layer_heads, lead shape, batch, length, heads, dim) of [..., heads, dim]: [heads, dim], [length, heads,
+    dim] or [batch, length, heads, dim] where it lies; a copy of more leading dimensions that do not merge, or of
+    heads whose elements lie apart."""
+    _operand(name, t, dtype, dev)
+    if t.dim() < 2:
+        raise ValueError(f"{name}: needs [..., heads, dim]")
+    lead = t.shape[:-2]
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        t = t.contiguous()
+    if len(lead) > 2:
+        t = t.reshape(math.prod(lead[:-1]), *t.shape[-3:])
+    shape, step = (1,) * (4 - t.dim()) + tuple(t.shape), (0,) * (4 - t.dim()) + tuple(t.stride())
+    return t, layer_heads(t.data_ptr(), step[0], step[1], step[2]), lead, *shape
+
+
+def _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status):
+    """Checks what both passes take; the arguments of the C calls from the sizes to the positions in three pieces, and
+    what has to live until the call: operands, batch x length, heads, dimension."""
+    dev = _operand(name, q)
+    q, hq, lead, batch, length, heads, dim = _heads(name, q, None, dev)
+    k, hk, lead_k, _, _, kv_heads, dim_k = _heads(name, k, q.dtype, dev)
+    if lead_k != lead or dim_k != dim:
+        raise ValueError(f"{name}: q and k need the same tokens and the same size of a head")
+    if dim % 2 or not 2 <= dim <= 512 or max(heads, kv_heads) > 32768:
+        raise ValueError(f"{name}: heads need an even size of 2 to 512, and there are 32768 at most")
+    if (cos is None) != (sin is None):
+        raise ValueError(f"{name}: cos and sin come together")
+    places = rotary = wide = 0
+    if cos is not None:
+        for t in (cos, sin):
+            _operand(name, t, _F32, dev)
+            if t.dim() != 2 or t.shape != cos.shape or not t.is_contiguous():
+                raise ValueError(f"{name}: cos and sin need contiguous [places, rotary / 2] elements")
+        places, rotary = cos.shape[0], 2 * cos.shape[1]
+        if rotary > dim:
+            raise ValueError(f"{name}: {rotary} elements to rotate in heads of {dim}")
+    if positions is not None:
+        if not isinstance(positions, torch.Tensor) or positions.dtype not in (_I32, torch.int64):
+            raise TypeError(f"{name}: positions are int32 or int64")
+        _operand(name, positions, positions.dtype, dev)
+        if positions.shape != lead and positions.shape != lead[-1:]:
+            raise ValueError(f"{name}: needs one position per token, or per token of a sequence")
+        positions = positions.expand(lead).contiguous()
+        wide = int(positions.dtype is torch.int64)
+    wt = _weights(name, q, dim, q_weight, k_weight)
+    if status is not None:
+        _operand(name, status, _I32, dev)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    return (dev, (batch, length, heads, kv_heads, dim, rotary), (hq, hk), (ptr(q_weight), ptr(k_weight), wt),
+            (ptr(cos), ptr(sin), places, ptr(positions), wide), (q, k, positions))
+
+
+def _dense_heads(t, sizes, heads):
+    return layer_heads(t.data_ptr(), sizes[1] * heads * sizes[4], heads * sizes[4], sizes[4])
+
+
+def qk_rotary_forward(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tensor] = None,
+                      sin: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                      q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                      eps: float = 1e-6, interleaved: bool = False, status: Optional[torch.Tensor] = None, stream=None):
+    """Queries [..., heads, dim] and keys [..., kv_heads, dim] of the same tokens, each head divided by its root
+    mean square, multiplied by its weight (float32 or q's type) and with its first elements rotated by the token's
+    position (include/layer.h): (q, k) as new dense tensors. cos, sin: float32 [places, rotary / 2], None: no
+    rotation. positions: int32 or int64, one per token or per token of a sequence, None: a token's place in its
+    sequence (the dimension before the heads). Slices and transposes of heads and tokens are read where they lie.
+    status: an int32 CUDA word that SOAP_STATUS_RANGE is ORed into where a position is not in the table; the
+    token's results are NaN."""
+    name = "qk_rotary_forward"
+    dev = _operand(name, q)
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream, q, k, cos, sin, positions, q_weight, k_weight, status):
+            return qk_rotary_forward(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, status)
+    _, sizes, heads, w, table, keep = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
+    out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
+    _done(load_library().layer_qk_forward(
+        *sizes, int(interleaved), *heads, DTYPES[q.dtype], *w, eps, *table, _dense_heads(out_q, sizes, sizes[2]),
+        _dense_heads(out_k, sizes, sizes[3]), None if status is None else status.data_ptr(), _raw_stream(dev.index)),
+        name)
+    return out_q, out_k
+
+
+def qk_rotary_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                       cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                       positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                       k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                       params: bool = True, status: Optional[torch.Tensor] = None, stream=None):
+    """(q's gradient, k's, q_weight's, k_weight's) of qk_rotary_forward from its results' (dq, dk) and its operands.
+    The first two have q's type, the weights' are float32 [dim] (of a weight that is None: as for one of ones), or
+    None without ``params``."""
+    name = "qk_rotary_backward"
+    dev = _operand(name, q)
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream, dq, dk, q, k, cos, sin, positions, q_weight, k_weight, status):
+            return qk_rotary_backward(dq, dk, q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, params,
+                                      status)
+    _, sizes, heads, w, table, keep = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
+    grads = []
+    for d, t in ((dq, q), (dk, k)):
+        shape = d.shape if isinstance(d, torch.Tensor) else None
+        d, h, *_ = _heads(name, d, q.dtype, dev)
+        if shape != t.shape:
+            raise ValueError(f"{name}: a gradient has another shape than its operand")
+        grads.append((d, h))
+    out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
+    lib = load_library()
+    dwq = dwk = ws = None
+    ws_bytes = 0
+    if params:
+        ws_bytes = lib.layer_qk_workspace_bytes(*sizes[:5])
+        dwq, dwk = _empty(sizes[4], dtype=_F32, device=dev), _empty(sizes[4], dtype=_F32, device=dev)
+        ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _done(lib.layer_qk_backward(
+        *sizes, int(interleaved), grads[0][1], grads[1][1], *heads, DTYPES[q.dtype], *w, eps, *table,
+        _dense_heads(out_q, sizes, sizes[2]), _dense_heads(out_k, sizes, sizes[3]), ptr(dwq), ptr(dwk), ptr(status),
+        ptr(ws), ws_bytes, _raw_stream(dev.index)), name)
+    return out_q, out_k, dwq, dwk
 
 
 def _matrices(name, M):

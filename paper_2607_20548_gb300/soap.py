@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", platform.machine(), "libsoap.so")
 
 SOAP_OK = 0
-STATUS_NONFINITE, STATUS_QR_BREAKDOWN, STATUS_TIMEOUT = 1, 2, 4  # device status bits (SOAP_STATUS_*)
+STATUS_NONFINITE, STATUS_QR_BREAKDOWN, STATUS_TIMEOUT, STATUS_RANGE = 1, 2, 4, 8  # device status bits (SOAP_STATUS_*)
 STATUS_NAMES = {0: "SOAP_OK", 1: "SOAP_ERR_INVALID_ARG", 2: "SOAP_ERR_CUDA", 3: "SOAP_ERR_OOM",
                 4: "SOAP_ERR_NONFINITE", 5: "SOAP_ERR_QR_BREAKDOWN", 6: "SOAP_ERR_TIMEOUT"}
 (STATE_M, STATE_V, STATE_L, STATE_QL, STATE_R, STATE_QR, STATE_MHAT, STATE_SKIP_L, STATE_SKIP_R,
@@ -37,7 +37,8 @@ MUON_EXPORTS = ("muon_default_hparams", "muon_create", "muon_step", "muon_set_lr
                 "muon_profile_end", "muon_orthogonalize", "muon_orthogonalize_workspace_bytes")
 # every symbol include/layer.h declares
 LAYER_EXPORTS = ("layer_norm_forward", "layer_norm_backward", "layer_norm_workspace_bytes", "layer_route_forward",
-                 "layer_route_backward", "layer_route_workspace_bytes")
+                 "layer_route_backward", "layer_route_workspace_bytes", "layer_qk_forward", "layer_qk_backward",
+                 "layer_qk_workspace_bytes")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # soap_dtype_t
 KERNEL_FAMILIES = ("gemm_simt", "gemm_tc", "qr_panel", "elementwise", "other", "qr_update")
 PROFILE_SERIAL = 1  # SOAP_PROFILE_SERIAL
@@ -72,6 +73,11 @@ class soap_launch_record(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class layer_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
 class SoapError(RuntimeError):
     def __init__(self, code, msg=""):
         super().__init__(f"{STATUS_NAMES.get(code, code)}: {msg}")
@@ -90,6 +96,7 @@ def load_library(path: str = LIB_PATH):
         raise ImportError(f"libsoap.so not built ({path}); run __graft_entry__.build()")
     lib = ctypes.CDLL(path)
     P, I32, I64, F, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    H = ctypes.POINTER(layer_heads)
     sig = {
         "soap_default_hparams": (None, [ctypes.POINTER(soap_hparams)]),
         "soap_create": (I32, [ctypes.POINTER(soap_shape), I32, ctypes.POINTER(soap_hparams), I32, ctypes.POINTER(P)]),
@@ -141,6 +148,11 @@ def load_library(path: str = LIB_PATH):
         "layer_route_workspace_bytes": (SZ, [I64, I32]),
         "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, P, SZ, P]),
         "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, P, I64, P]),
+        "layer_qk_workspace_bytes": (SZ, [I64, I64, I32, I32, I32]),
+        "layer_qk_forward": (I32, [I64, I64, I32, I32, I32, I32, I32, H, H, I32, P, P, I32, F, P, P, I64, P, I32, H,
+                                   H, P, P]),
+        "layer_qk_backward": (I32, [I64, I64, I32, I32, I32, I32, I32, H, H, H, H, I32, P, P, I32, F, P, P, I64, P,
+                                    I32, H, H, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
