@@ -6,6 +6,8 @@
  *                  the bias's gradients
  *   layer_route_*  a mixture-of-experts router's decision: softmax, the k largest logits with
  *                  their gates, per-expert counts, the balance loss, and the logits' gradient
+ *   layer_ffn_*    a gated feed-forward block, dense or over groups of rows with weights of their
+ *                  own (a router's experts), and its backward pass
  *   layer_qk_*     norms of queries and keys for each head and their rotation by position, and the
  *                  backward pass
  *
@@ -95,6 +97,55 @@ soap_status_t layer_route_backward(int64_t tokens, int32_t experts, int32_t k, c
                                    const int32_t* indices, const float* stats, const int32_t* counts,
                                    const int32_t* live, const float* dgates, void* dlogits, int64_t ld_d,
                                    soap_stream_t stream);
+
+/* A matrix for each group: element (i, j) of group g at g * stride + i * ld + j, or, `columns`
+ * nonzero, at g * stride + i + j * ld (column-major). */
+typedef struct {
+  void* data;
+  int64_t ld, stride;
+  int32_t columns;
+} layer_matrix_t;
+
+typedef enum { LAYER_SILU = 0, LAYER_GELU = 1 } layer_act_t;
+
+/* A gated feed-forward block of `rows` rows x [hidden], for each group of rows with weights of its own:
+ *   g = x Wg,  u = x Wu,  h = act(g) u,  y = h Wd
+ *   silu(g) = g / (1 + e^-g),  gelu(g) = g Phi(g) (Phi: the normal distribution)
+ * Wg, Wu: hidden x width, both row-major or both column-major; Wd: width x hidden; all of x's `type`.
+ * offsets: device int32 [groups + 1]; rows offsets[g] .. offsets[g + 1] - 1 are group g's (none: an empty group).
+ * Rows before offsets[0] and from offsets[groups] on are no group's: their y is 0 whatever they hold. NULL: groups
+ * is 1 and every row its own. Offsets that fall, or are outside 0 .. rows, are raised to the largest before them and
+ * cut at rows, and SOAP_STATUS_RANGE is ORed into *status.
+ * pre: layer_ffn_pre_elems fp32 elements, 16-byte aligned, receives g and u for the backward pass (in an order of the
+ * library's own), or NULL. Products are summed in fp32. For 16-bit types h is rounded to the type before the second
+ * product (the backward pass's dg, du and h too; fp16: a value above 65504 is then infinite), g and u are not.
+ * x, y: row i at element i * ld; y must not overlap an operand. status: NULL, or a device int32 (not cleared); where a
+ * bounded wait gave up (soap_wait_limit), SOAP_STATUS_TIMEOUT is ORed into it and all results are NaN.
+ * 0 <= rows <= 2^31 - 2^16; 1 <= hidden, width <= 65536; 1 <= groups <= 1024. `workspace`: 256-byte aligned,
+ * layer_ffn_workspace_bytes bytes (0 for invalid sizes); aligned: nonzero if every matrix operand of the call
+ * begins on a 16-byte boundary, with leading dimension and stride of whole 16-byte units (others are
+ * copied to the workspace first). */
+size_t layer_ffn_pre_elems(int64_t rows, int64_t width, int32_t groups);
+size_t layer_ffn_workspace_bytes(int64_t rows, int64_t hidden, int64_t width, int32_t groups, int32_t type,
+                                 int32_t aligned, int32_t backward);
+soap_status_t layer_ffn_forward(int64_t rows, int64_t hidden, int64_t width, int32_t groups,
+                                const int32_t* offsets, const void* x, int64_t ld_x, int32_t type,
+                                const layer_matrix_t* gate, const layer_matrix_t* up, const layer_matrix_t* down,
+                                int32_t act, void* y, int64_t ld_y, float* pre, int32_t* status, void* workspace,
+                                size_t workspace_bytes, soap_stream_t stream);
+
+/* The backward pass, from the forward call's pre:
+ *   dh = dy Wd^T,  dg = dh u act'(g),  du = dh act(g)
+ *   dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dWd = h^T dy
+ * d_gate, d_up, d_down: receive the weights' gradients (`type`; 0 for an empty group; each in its weight's order:
+ * columns as there), all three NULL: not formed. Rows of no group have dx 0, whatever their x and dy hold. */
+soap_status_t layer_ffn_backward(int64_t rows, int64_t hidden, int64_t width, int32_t groups,
+                                 const int32_t* offsets, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                                 int32_t type, const layer_matrix_t* gate, const layer_matrix_t* up,
+                                 const layer_matrix_t* down, int32_t act, const float* pre, void* dx, int64_t ld_dx,
+                                 const layer_matrix_t* d_gate, const layer_matrix_t* d_up,
+                                 const layer_matrix_t* d_down, int32_t* status, void* workspace,
+                                 size_t workspace_bytes, soap_stream_t stream);
 
 /* Heads of `dim` contiguous elements: of token s of sequence b, head h, at
  * b * batch_stride + s * token_stride + h * head_stride. */

@@ -1,6 +1,6 @@
-"""Binding of the stand-alone operators of a training step: layer norm, expert routing, and queries' and keys'
-norms with their rotation, forward and backward (include/layer.h), and the orthogonalisation of a momentum
-(include/muon.h).
+"""Binding of the stand-alone operators of a training step: layer norm, expert routing, the gated feed-forward
+block, and queries' and keys' norms with their rotation, forward and backward (include/layer.h), and the
+orthogonalisation of a momentum (include/muon.h).
 
 Argument checks and marshalling only, as in ``soap``: outputs and workspaces are allocated here
 with torch, on the operands' device, and everything is computed by libsoap.so on the given stream
@@ -21,7 +21,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .soap import DTYPES, SOAP_OK, SoapError, layer_heads, load_library
+from .soap import DTYPES, SOAP_OK, SoapError, layer_heads, layer_matrix, load_library
 
 # What every call asks torch for, without the Python objects around it (torch.cuda.current_stream(...) alone
 # costs as much as half a launch): the cudaStream_t that is current on a device, and the current device. A
@@ -448,3 +448,109 @@ def muon_orthogonalize(M: torch.Tensor, coeffs=None, ns_steps: int = 16, eps: fl
                                  out.data_ptr(), cols, rows * cols, ws.data_ptr(), ws_bytes,
                                  None if status is None else status.data_ptr(), _raw_stream(dev.index)), name)
     return out.mT if swapped else out
+
+
+_ACTS = {"silu": 0, "gelu": 1}
+
+
+def _ffn_common(name, x, weights, offsets, act, status):
+    """Checks what both passes take: (rows, hidden, width, groups), x and its leading dimension, the weights as
+    layer_matrix and as tensors, whether all of them lie on 16-byte units."""
+    dev = _operand(name, x)
+    if act not in _ACTS:
+        raise ValueError(f"{name}: act is one of {', '.join(_ACTS)}")
+    if x.dim() < 1:
+        raise ValueError(f"{name}: needs at least one dimension")
+    hidden, size = x.shape[-1], x.element_size()
+    groups = 1
+    if offsets is not None:
+        _operand(name, offsets, _I32, dev)
+        if offsets.dim() != 1 or offsets.numel() < 2:
+            raise ValueError(f"{name}: offsets need groups + 1 elements")
+        offsets = offsets.contiguous()
+        groups = offsets.numel() - 1
+    for w in weights:
+        _operand(name, w, x.dtype, dev)
+        if w.dim() != (2 if offsets is None else 3) or (offsets is not None and w.shape[0] != groups):
+            raise ValueError(f"{name}: needs a matrix of each weight" + ("" if offsets is None else " for each group"))
+    gate, up, down = weights
+    width = gate.shape[-1]
+    if gate.shape[-2] != hidden or up.shape != gate.shape or down.shape[-2:] != (width, hidden):
+        raise ValueError(f"{name}: weights of shapes {tuple(gate.shape)}, {tuple(up.shape)}, {tuple(down.shape)} do not "
+                         f"fit rows of {hidden}")
+    if not 1 <= hidden <= 65536 or not 1 <= width <= 65536 or groups > 1024:
+        raise ValueError(f"{name}: hidden and width of 1 to 65536 and at most 1024 groups")
+    found = [_matrices(name, w) for w in weights]
+    if found[0][6] != found[1][6]:  # of two orders: both row-major
+        found[:2] = [_matrices(name, w.contiguous()) for w in weights[:2]]
+    if status is not None:
+        _operand(name, status, _I32, dev)
+    x, rows, ld = _rows(x)
+    units = [f[0].data_ptr() | f[4] * size | (f[5] * size if groups > 1 else 0) for f in found] + [x.data_ptr() | ld * size]
+    mats = [layer_matrix(f[0].data_ptr(), f[4], f[5], int(f[6])) for f in found]
+    return (rows, hidden, width, groups), x, ld, mats, found, offsets, units
+
+
+def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                offsets: Optional[torch.Tensor] = None, act: str = "silu", keep: bool = False,
+                status: Optional[torch.Tensor] = None, stream=None):
+    """A gated feed-forward block act(x w_gate) * (x w_up) w_down of rows x [..., hidden]: (y, pre). Weights of x's
+    type, row- or column-major: w_gate and w_up [hidden, width], w_down [width, hidden]; with offsets (int32
+    [groups + 1]) a matrix of each for every group, of which group g has the rows offsets[g] to offsets[g + 1] - 1,
+    and rows of no group give 0 (include/layer.h). act: "silu" or "gelu". pre, with ``keep``: what ffn_backward takes of
+    this call (float32, in the library's own order), else None. status: an int32 CUDA word that SOAP_STATUS_TIMEOUT
+    and SOAP_STATUS_RANGE (offsets that fall or pass the rows) are ORed into."""
+    name = "ffn_forward"
+    dev = _operand(name, x)
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream, x, w_gate, w_up, w_down, offsets, status):
+            return ffn_forward(x, w_gate, w_up, w_down, offsets, act, keep, status)
+    shape = x.shape
+    sizes, x, ld, mats, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    lib, t = load_library(), DTYPES[x.dtype]
+    y = _empty(shape, dtype=x.dtype, device=dev)
+    pre = _empty(lib.layer_ffn_pre_elems(sizes[0], sizes[2], sizes[3]), dtype=_F32, device=dev) if keep else None
+    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, int(not any(u % 16 for u in units)), 0)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
+    _done(lib.layer_ffn_forward(
+        *sizes, None if offsets is None else offsets.data_ptr(), x.data_ptr(), ld, t, *mats, _ACTS[act], y.data_ptr(),
+        shape[-1], None if pre is None else pre.data_ptr(), None if status is None else status.data_ptr(),
+        ws.data_ptr(), ws_bytes, _raw_stream(dev.index)), name)
+    return y, pre
+
+
+def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                 w_down: torch.Tensor, offsets: Optional[torch.Tensor] = None, act: str = "silu", params: bool = True,
+                 status: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dw_gate, dw_up, dw_down) of ffn_forward from y's gradient, the call's operands and its pre. All have x's
+    type, the weights' gradients their weights' shapes and orders (None without ``params``)."""
+    name = "ffn_backward"
+    dev = _operand(name, x)
+    if stream is not None or dev.index != _current():
+        with _elsewhere(dev.index, stream, dy, x, pre, w_gate, w_up, w_down, offsets, status):
+            return ffn_backward(dy, x, pre, w_gate, w_up, w_down, offsets, act, params, status)
+    shape = x.shape
+    sizes, x, ld, mats, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    _operand(name, dy, x.dtype, dev)
+    if dy.shape != shape:
+        raise ValueError(f"{name}: dy and x have different shapes")
+    dy, _, ld_dy = _rows(dy)
+    lib, t = load_library(), DTYPES[x.dtype]
+    _operand(name, pre, _F32, dev)
+    if pre.numel() != lib.layer_ffn_pre_elems(sizes[0], sizes[2], sizes[3]) or not pre.is_contiguous():
+        raise ValueError(f"{name}: pre is of another call")
+    dx = _empty(shape, dtype=x.dtype, device=dev)
+    grads, out = [None] * 3, [None] * 3
+    if params:
+        # in the order in which its weight lies: stored [groups, rows, cols], seen transposed if that is column-major
+        made = [_empty(((sizes[3],) if offsets is not None else ()) + f[2:4], dtype=x.dtype, device=dev) for f in held]
+        grads = [layer_matrix(g.data_ptr(), f[3], f[2] * f[3], int(f[6])) for g, f in zip(made, held)]
+        out = [g.mT if f[6] else g for g, f in zip(made, held)]
+    units.append(dy.data_ptr() | ld_dy * dy.element_size())
+    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, int(not any(u % 16 for u in units)), 1)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
+    _done(lib.layer_ffn_backward(
+        *sizes, None if offsets is None else offsets.data_ptr(), dy.data_ptr(), ld_dy, x.data_ptr(), ld, t, *mats,
+        _ACTS[act], pre.data_ptr(), dx.data_ptr(), shape[-1], *grads, None if status is None else status.data_ptr(),
+        ws.data_ptr(), ws_bytes, _raw_stream(dev.index)), name)
+    return dx, *out

@@ -37,7 +37,8 @@ MUON_EXPORTS = ("muon_default_hparams", "muon_create", "muon_step", "muon_set_lr
                 "muon_profile_end", "muon_orthogonalize", "muon_orthogonalize_workspace_bytes")
 # every symbol include/layer.h declares
 LAYER_EXPORTS = ("layer_norm_forward", "layer_norm_backward", "layer_norm_workspace_bytes", "layer_route_forward",
-                 "layer_route_backward", "layer_route_workspace_bytes", "layer_qk_forward", "layer_qk_backward",
+                 "layer_route_backward", "layer_route_workspace_bytes", "layer_ffn_forward", "layer_ffn_backward",
+                 "layer_ffn_workspace_bytes", "layer_ffn_pre_elems", "layer_qk_forward", "layer_qk_backward",
                  "layer_qk_workspace_bytes")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # soap_dtype_t
 KERNEL_FAMILIES = ("gemm_simt", "gemm_tc", "qr_panel", "elementwise", "other", "qr_update")
@@ -73,6 +74,11 @@ class soap_launch_record(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class layer_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("columns", ctypes.c_int32)]
+
+
 class layer_heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
@@ -96,7 +102,7 @@ def load_library(path: str = LIB_PATH):
         raise ImportError(f"libsoap.so not built ({path}); run __graft_entry__.build()")
     lib = ctypes.CDLL(path)
     P, I32, I64, F, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
-    H = ctypes.POINTER(layer_heads)
+    H, M = ctypes.POINTER(layer_heads), ctypes.POINTER(layer_matrix)
     sig = {
         "soap_default_hparams": (None, [ctypes.POINTER(soap_hparams)]),
         "soap_create": (I32, [ctypes.POINTER(soap_shape), I32, ctypes.POINTER(soap_hparams), I32, ctypes.POINTER(P)]),
@@ -148,6 +154,11 @@ def load_library(path: str = LIB_PATH):
         "layer_route_workspace_bytes": (SZ, [I64, I32]),
         "layer_route_forward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, P, P, P, P, P, P, P, P, P, SZ, P]),
         "layer_route_backward": (I32, [I64, I32, I32, P, I64, I32, P, I32, F, F, P, P, P, P, P, P, I64, P]),
+        "layer_ffn_pre_elems": (SZ, [I64, I64, I32]),
+        "layer_ffn_workspace_bytes": (SZ, [I64, I64, I64, I32, I32, I32, I32]),
+        "layer_ffn_forward": (I32, [I64, I64, I64, I32, P, P, I64, I32, M, M, M, I32, P, I64, P, P, P, SZ, P]),
+        "layer_ffn_backward": (I32, [I64, I64, I64, I32, P, P, I64, P, I64, I32, M, M, M, I32, P, P, I64, M, M, M, P,
+                                     P, SZ, P]),
         "layer_qk_workspace_bytes": (SZ, [I64, I64, I32, I32, I32]),
         "layer_qk_forward": (I32, [I64, I64, I32, I32, I32, I32, I32, H, H, I32, P, P, I32, F, P, P, I64, P, I32, H,
                                    H, P, P]),
