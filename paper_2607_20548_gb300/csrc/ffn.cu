@@ -1,157 +1,24 @@
-// The gated feed-forward block and its backward pass (include/layer.h, layer_ffn_*).
-//
-//   g = x Wg,  u = x Wu,  h = act(g) u,  y = h Wd
-//   dh = dy Wd^T,  dg = dh u act'(g),  du = dh act(g),  dx = dg Wg^T + du Wu^T,
-//   dWg = x^T dg,  dWu = x^T du,  dWd = h^T dy        (per group of rows)
-//
-// A launch per product, 64 x 64 tiles on the fp32 pipe: the same for every type, order and size.
+// The gated feed-forward block's C entry points (include/layer.h, layer_ffn_*): checks, the workspace's layout, copies
+// of operands that the products cannot read as they lie, tensor maps. The products are ffn_steps.cu's.
 #include <algorithm>
 #include <cstdint>
 
 #include "../../include/layer.h"
+#include "ffn.h"
+#include "pair.h"
 #include "profile.h"
 #include "soap_internal.h"
-#include "types.h"
 
 namespace soap {
 namespace {
 
-constexpr int kMaxGroups = 1024, kMaxSide = 65536;
+using namespace ffn;
+
+constexpr int kMaxSide = 65536;
 constexpr int64_t kMaxRows = INT32_MAX - 65536;
 
-// One factor pair of a product: A (m, k) at m * am + k * ak, B (k, n) at k * bk + n * bn, elements between groups.
-struct Factors {
-  const void *a, *b;
-  int64_t am, ak, a_group, bk, bn, b_group;
-};
-
-enum Out { kGatedOut, kGradOut, kPlain };
-
-struct Product {
-  const int* bounds;  // the groups' sanitised offsets
-  int rows_are;       // 0: A's rows and the results' are the group's rows; 1: k runs over the group's rows
-  int M, N, K;
-  Factors f[2];
-  int pairs;          // of factors whose products are added (kGatedOut: g from the first, u from the second)
-  int act;
-  void* out;          // (m, n) at m * om + n * on + group * o_group
-  int64_t om, on, o_group;
-  void *h, *dg, *du;  // [rows][N]
-  float* pre;         // [rows][2][N]
-  int64_t width;
-};
-
-__device__ __forceinline__ void activation(int act, float g, float& a, float& da) {
-  if (act == LAYER_SILU) {
-    const float s = 1.f / (1.f + expf(-g));
-    a = g * s;
-    da = s * (1.f + g * (1.f - s));
-  } else {
-    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-    a = g * p;
-    da = p + g * 0.3989422804014327f * expf(-0.5f * g * g);
-  }
-}
-
-template <typename T, int OUT>
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ Product p) {
-  constexpr int BM = 64, BN = 64, BK = 16, NP = OUT == kGatedOut ? 2 : 1;
-  __shared__ float sa[BK][BM + 1], sb[NP][BK][BN + 1];
-  const int group = blockIdx.z, r0 = p.bounds[group], r1 = p.bounds[group + 1];
-  const int M = p.rows_are ? p.M : r1 - r0, K = p.rows_are ? r1 - r0 : p.K;
-  const int m0 = blockIdx.y * BM, n0 = blockIdx.x * BN;
-  if (m0 >= M) return;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[NP][4][4] = {};
-  for (int seg = 0; seg < (OUT == kGatedOut ? 1 : p.pairs); ++seg) {
-    const Factors& f = p.f[seg];
-    const T* A = static_cast<const T*>(f.a) + group * f.a_group + (int64_t)r0 * (p.rows_are ? f.ak : f.am);
-    for (int k0 = 0; k0 < K; k0 += BK) {
-      for (int i = threadIdx.x; i < BM * BK; i += 256) {
-        const bool along = f.ak == 1;
-        const int m = along ? i / BK : i % BM, k = along ? i % BK : i / BM;
-        sa[k][m] = m0 + m < M && k0 + k < K ? to_f32(A[(int64_t)(m0 + m) * f.am + (int64_t)(k0 + k) * f.ak]) : 0.f;
-      }
-#pragma unroll
-      for (int q = 0; q < NP; ++q) {
-        const Factors& fb = p.f[seg + q];
-        const T* B = static_cast<const T*>(fb.b) + group * fb.b_group + (p.rows_are ? (int64_t)r0 * fb.bk : 0);
-        for (int i = threadIdx.x; i < BN * BK; i += 256) {
-          const bool along = fb.bk == 1;
-          const int n = along ? i / BK : i % BN, k = along ? i % BK : i / BN;
-          sb[q][k][n] = n0 + n < p.N && k0 + k < K ? to_f32(B[(int64_t)(k0 + k) * fb.bk + (int64_t)(n0 + n) * fb.bn]) : 0.f;
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < BK; ++k)
-#pragma unroll
-        for (int q = 0; q < NP; ++q)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(sa[k][ty + 16 * i], sb[q][k][tx + 16 * j], acc[q][i][j]);
-      __syncthreads();
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= M || n >= p.N) continue;
-      const int64_t row = (int64_t)r0 + m, at = row * p.width + n;
-      float a, da;
-      if constexpr (OUT == kGatedOut) {
-        activation(p.act, acc[0][i][j], a, da);
-        static_cast<T*>(p.h)[at] = from_f32<T>(a * acc[1][i][j]);
-        if (p.pre) {
-          p.pre[row * 2 * p.width + n] = acc[0][i][j];
-          p.pre[(row * 2 + 1) * p.width + n] = acc[1][i][j];
-        }
-      } else if constexpr (OUT == kGradOut) {
-        const float g = p.pre[row * 2 * p.width + n], u = p.pre[(row * 2 + 1) * p.width + n], dh = acc[0][i][j];
-        activation(p.act, g, a, da);
-        static_cast<T*>(p.h)[at] = from_f32<T>(a * u);
-        static_cast<T*>(p.dg)[at] = from_f32<T>(dh * u * da);
-        static_cast<T*>(p.du)[at] = from_f32<T>(dh * a);
-      } else {
-        static_cast<T*>(p.out)[(p.rows_are ? (int64_t)m : row) * p.om + (int64_t)n * p.on + group * p.o_group] =
-            from_f32<T>(acc[0][i][j]);
-      }
-    }
-}
-
-// bounds[g]: the largest of offsets[0 .. g], within 0 .. rows.
-__global__ void __launch_bounds__(1024) bounds_kernel(const int* offsets, int groups, int rows, int* bounds, int* status) {
-  __shared__ int top[2][kMaxGroups + 1];
-  bool off = false;
-  for (int i = threadIdx.x; i <= groups; i += 1024) {
-    const int v = offsets ? offsets[i] : i == 0 ? 0 : rows;
-    off |= v < 0 || v > rows || (offsets && i > 0 && v < offsets[i - 1]);
-    top[0][i] = min(max(v, 0), rows);
-  }
-  if (off && status) atomicOr(status, kStatusRange);
-  int at = 0;
-  for (int d = 1; d <= groups; d *= 2, at ^= 1) {
-    __syncthreads();
-    for (int i = threadIdx.x; i <= groups; i += 1024) top[at ^ 1][i] = max(top[at][i], i >= d ? top[at][i - d] : 0);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i <= groups; i += 1024) bounds[i] = top[at][i];
-}
-
-// Rows of no group become 0.
-template <typename T>
-__global__ void __launch_bounds__(256) outside_kernel(const int* bounds, int groups, int64_t rows, T* y, int64_t ld, int width) {
-  const int first = bounds[0], last = bounds[groups];
-  for (int64_t r = blockIdx.x; r < first + (rows - last); r += gridDim.x) {
-    T* row = y + (r < first ? r : r - first + last) * ld;
-    for (int c = threadIdx.x; c < width; c += 256) row[c] = from_f32<T>(0.f);
-  }
-}
-
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 
 bool bad_ptr(const void* p, size_t size) { return p && reinterpret_cast<uintptr_t>(p) % size; }
 
@@ -166,118 +33,294 @@ bool bad_sizes(int64_t rows, int64_t hidden, int64_t width, int32_t groups, int3
          groups > kMaxGroups || type < SOAP_F32 || type > SOAP_F16;
 }
 
-// What a call has in hand.
+// Where everything lies in the workspace.
+struct Layout {
+  int64_t row_tiles;              // at most
+  int64_t tiles[3], slots[3];     // at most; of partial sums
+  int64_t units;                  // at most
+  size_t plan, done, done_words, count[3], clips, partial[3], inter[3], x, dy, w[3], bytes;
+  size_t inter_plane, x_plane, w_plane;  // elements of a plane
+};
+
+Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool copies, bool backward) {
+  Layout l{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += up256(bytes);
+    return was;
+  };
+  l.row_tiles = rows / 256 + std::min<int64_t>(groups, rows);
+  l.tiles[0] = l.row_tiles * up_div(width, backward ? 256 : 128);
+  l.tiles[1] = l.row_tiles * up_div(hidden, 256);
+  const int64_t each = 3 * (int64_t)up_div(width, 256) * up_div(hidden, 256);
+  l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
+  const int64_t slices[3] = {up_div(hidden, 64), (backward ? 2 : 1) * (int64_t)up_div(width, 64), up_div(rows, 64)};
+  for (int p = 0; p < 3; ++p) {
+    const int64_t parts = std::max<int64_t>(1, slices[p] / 4), longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
+    l.units += l.tiles[p] * std::max(parts, longest);
+    // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights'
+    // gradients: of groups with more than kMaxSlices slices, less than three parts for each such run of all rows)
+    l.slots[p] = parts > 1 ? std::min<int64_t>(kUnitPairs, l.tiles[p] * parts) : 0;
+    if (longest > 1) l.slots[p] += p < 2 ? l.tiles[p] * longest : 3 * longest * each;
+  }
+  l.plan = take(sizeof(Plan));
+  l.done = at;
+  size_t words = l.row_tiles + groups;
+  for (int p = 0; p < 3; ++p) {
+    l.count[p] = at + words * 4;
+    words += l.slots[p] * 16;
+  }
+  l.done_words = words;
+  take(words * 4);
+  l.clips = take((size_t)groups * kClips * sizeof(CUtensorMap));
+  for (int p = 0; p < 3; ++p) l.partial[p] = take((size_t)l.slots[p] * kPartial * 4);
+  const size_t planes = type == SOAP_F32 ? 3 : 1;
+  l.inter_plane = (size_t)rows * up8(width);
+  for (int i = 0; i < (backward ? 3 : 1); ++i) l.inter[i] = take(planes * l.inter_plane * 2);
+  if (copies || type == SOAP_F32) {
+    l.x_plane = (size_t)rows * up8(hidden);
+    l.x = take(planes * l.x_plane * 2);
+    if (backward) l.dy = take(planes * l.x_plane * 2);
+    l.w_plane = (size_t)groups * std::max(hidden * up8(width), width * up8(hidden));
+    for (int i = 0; i < 3; ++i) l.w[i] = take(planes * l.w_plane * 2);
+  }
+  l.bytes = at;
+  return l;
+}
+
+// Copies of operands with rows of whole 16-byte units: 16-bit elements as they are, fp32 ones as three bf16 planes
+// that add up to the element (8 bits of its significand each; what is not finite: the first plane alone).
+struct CopyJob {
+  const void* src;
+  int64_t ld, stride;   // of rows and of matrices
+  int64_t rows;         // of a matrix
+  int inner, ld_out;
+  int64_t matrices;
+  uint16_t* dst;
+  int64_t plane;
+};
+struct CopyJobs {
+  CopyJob job[5];
+  int n;
+};
+
+template <bool SPLIT>
+__global__ void __launch_bounds__(256) copy_kernel(const __grid_constant__ CopyJobs jobs) {
+  for (int j = 0; j < jobs.n; ++j) {
+    const CopyJob& c = jobs.job[j];
+    const int chunks = c.ld_out / 8;
+    const int64_t all = c.matrices * c.rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+      const int64_t row = i / chunks, m = row / c.rows, r = row - m * c.rows;
+      const int col = (int)(i - row * chunks) * 8, n = min(8, c.inner - col);
+      const int64_t from = m * c.stride + r * c.ld + col;
+      Pack<uint16_t, 8> out[SPLIT ? 3 : 1];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (SPLIT) {
+          const float x = e < n ? static_cast<const float*>(c.src)[from + e] : 0.f;
+          const uint32_t b = __float_as_uint(x);
+          const bool finite = fabsf(x) < INFINITY;
+          const float hi = __uint_as_float(b & 0xffff0000u), rest = finite ? x - hi : 0.f;
+          const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
+          const float low = rest - __uint_as_float(mid);
+          // (a NaN stays one without its lower bits)
+          out[0].v[e] = (uint16_t)((b >> 16) | (x != x ? 0x40u : 0u));
+          out[1].v[e] = (uint16_t)(mid >> 16);
+          out[2].v[e] = (uint16_t)(__float_as_uint(low) >> 16);
+        } else {
+          out[0].v[e] = e < n ? static_cast<const uint16_t*>(c.src)[from + e] : (uint16_t)0;
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < (SPLIT ? 3 : 1); ++p)
+        *reinterpret_cast<Pack<uint16_t, 8>*>(c.dst + p * c.plane + row * c.ld_out + col) = out[p];
+    }
+  }
+}
+
 struct Call {
   int64_t rows;
   int hidden, width, groups;
   const int32_t* offsets;
   int type, act;
-  const layer_matrix_t *gate, *up, *down;
+  const layer_matrix_t* w[3];  // gate, up, down
   int* status;
   uint8_t* ws;
+  size_t ws_bytes;
+  bool backward;
 };
 
-bool bad_call(const Call& c, size_t ws_bytes, bool backward) {
+bool units_of_16(const void* p, int64_t ld, int64_t stride, size_t size) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)size % 16 == 0 && stride * (int64_t)size % 16 == 0;
+}
+
+bool bad_call(const Call& c) {
   const size_t size = dtype_size(c.type);
   return (!c.offsets && c.groups != 1) || bad_ptr(c.offsets, 4) || bad_ptr(c.status, 4) ||
-         (c.act != LAYER_SILU && c.act != LAYER_GELU) || bad_matrix(c.gate, c.hidden, c.width, c.groups, size) ||
-         bad_matrix(c.up, c.hidden, c.width, c.groups, size) || bad_matrix(c.down, c.width, c.hidden, c.groups, size) ||
-         !c.gate->columns != !c.up->columns || !c.ws || bad_ptr(c.ws, 256) ||
-         ws_bytes < layer_ffn_workspace_bytes(c.rows, c.hidden, c.width, c.groups, c.type, 1, backward);
+         (c.act != LAYER_SILU && c.act != LAYER_GELU) || bad_matrix(c.w[0], c.hidden, c.width, c.groups, size) ||
+         bad_matrix(c.w[1], c.hidden, c.width, c.groups, size) || bad_matrix(c.w[2], c.width, c.hidden, c.groups, size) ||
+         !c.w[0]->columns != !c.w[1]->columns || !c.ws || bad_ptr(c.ws, 256);
 }
 
-// (i, j) of a matrix at i * r + j * c
-struct Steps {
-  int64_t r, c;
+// What a row-major matrix (or `matrices` of them, or planes) looks like to the copies.
+struct View {
+  void* p;
+  int64_t rows, ld, stride;
+  int cols, depth;
 };
-Steps steps_of(const layer_matrix_t& m) { return m.columns ? Steps{1, m.ld} : Steps{m.ld, 1}; }
 
-template <typename T, int OUT>
-cudaError_t launch(const Product& p, int64_t rows, int groups, cudaStream_t s) {
-  const int64_t m = p.rows_are ? p.M : rows;
-  if (m == 0) return cudaSuccess;
-  // (a grid is at most 65535 high: tall ones in pieces would need a row offset; the tiled kernel has none)
-  if ((m + 63) / 64 > 65535) return cudaErrorInvalidValue;
-  product_kernel<T, OUT><<<dim3((p.N + 63) / 64, (unsigned)((m + 63) / 64), groups), 256, 0, s>>>(p);
-  return cudaGetLastError();
+bool make_map(CUtensorMap* map, const View& v, int type, int box_cols, int box_rows) {
+  auto fn = tc::encode_fn();
+  if (!fn) return false;
+  const size_t size = dtype_size(type);
+  const cuuint64_t dims[3] = {(cuuint64_t)v.cols, (cuuint64_t)v.rows, (cuuint64_t)v.depth};
+  // (of a single matrix the third step is never taken)
+  const cuuint64_t strides[2] = {(cuuint64_t)v.ld * size, (cuuint64_t)(v.depth > 1 ? v.stride : v.ld) * size};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
+  const CUtensorMapDataType t = type == SOAP_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : type == SOAP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return fn(map, t, 3, v.p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box_cols * size == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T>
-cudaError_t forward(const Call& c, const void* x, int64_t ld_x, void* y, int64_t ld_y, float* pre, cudaStream_t s) {
-  int* bounds = reinterpret_cast<int*>(c.ws);
-  T* h = reinterpret_cast<T*>(c.ws + up256((kMaxGroups + 1) * 4));
-  bounds_kernel<<<1, 1024, 0, s>>>(c.offsets, c.groups, (int)c.rows, bounds, c.status);
-  if (c.offsets) outside_kernel<T><<<256, 256, 0, s>>>(bounds, c.groups, c.rows, static_cast<T*>(y), ld_y, c.hidden);
-  Product p{};
-  p.bounds = bounds;
-  p.N = c.width;
-  p.K = c.hidden;
-  const layer_matrix_t* w[2] = {c.gate, c.up};
-  for (int i = 0; i < 2; ++i) p.f[i] = {x, w[i]->data, ld_x, 1, 0, steps_of(*w[i]).r, steps_of(*w[i]).c, w[i]->stride};
-  p.act = c.act;
-  p.h = h;
-  p.pre = pre;
-  p.width = c.width;
-  cudaError_t e = launch<T, kGatedOut>(p, c.rows, c.groups, s);
-  if (e != cudaSuccess) return e;
-  p.N = c.hidden;
-  p.K = c.width;
-  p.f[0] = {h, c.down->data, c.width, 1, 0, steps_of(*c.down).r, steps_of(*c.down).c, c.down->stride};
-  p.pairs = 1;
-  p.out = y;
-  p.om = ld_y;
-  p.on = 1;
-  return launch<T, kPlain>(p, c.rows, c.groups, s);
-}
+cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, float* pre, void* y,
+                    int64_t ld_y, const layer_matrix_t* const (&grads)[3], cudaStream_t s) {
+  const bool f32 = c.type == SOAP_F32;
+  const int etype = f32 ? (int)SOAP_BF16 : c.type, planes = f32 ? 3 : 1;
+  const size_t size = dtype_size(c.type);
+  const layer_matrix_t& gate = *c.w[0];
+  const layer_matrix_t& down = *c.w[2];
 
-template <typename T>
-cudaError_t backward(const Call& c, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const float* pre, void* dx,
-                     int64_t ld_dx, const layer_matrix_t* const (&grads)[3], cudaStream_t s) {
-  int* bounds = reinterpret_cast<int*>(c.ws);
-  T* h = reinterpret_cast<T*>(c.ws + up256((kMaxGroups + 1) * 4));
-  const size_t n = up256((size_t)c.rows * c.width * sizeof(T)) / sizeof(T);
-  T *dg = h + n, *du = dg + n;
-  bounds_kernel<<<1, 1024, 0, s>>>(c.offsets, c.groups, (int)c.rows, bounds, c.status);
-  if (c.offsets) outside_kernel<T><<<256, 256, 0, s>>>(bounds, c.groups, c.rows, static_cast<T*>(dx), ld_dx, c.hidden);
-  Product p{};
-  p.bounds = bounds;
-  p.N = c.width;
-  p.K = c.hidden;
-  p.f[0] = {dy, c.down->data, ld_dy, 1, 0, steps_of(*c.down).c, steps_of(*c.down).r, c.down->stride};
-  p.pairs = 1;
-  p.act = c.act;
-  p.h = h;
-  p.dg = dg;
-  p.du = du;
-  p.pre = const_cast<float*>(pre);
-  p.width = c.width;
-  cudaError_t e = launch<T, kGradOut>(p, c.rows, c.groups, s);
-  if (e != cudaSuccess) return e;
-  p.N = c.hidden;
-  p.K = c.width;
-  const layer_matrix_t* w[2] = {c.gate, c.up};
-  for (int i = 0; i < 2; ++i)
-    p.f[i] = {i ? du : dg, w[i]->data, c.width, 1, 0, steps_of(*w[i]).c, steps_of(*w[i]).r, w[i]->stride};
-  p.pairs = 2;
-  p.out = dx;
-  p.om = ld_dx;
-  p.on = 1;
-  e = launch<T, kPlain>(p, c.rows, c.groups, s);
-  const void* left[3] = {x, x, h};
-  const void* right[3] = {dg, du, dy};
-  for (int i = 0; i < 3 && e == cudaSuccess && grads[0]; ++i) {
-    p.rows_are = 1;
-    p.M = i < 2 ? c.hidden : c.width;
-    p.N = i < 2 ? c.width : c.hidden;
-    p.pairs = 1;
-    p.f[0] = {left[i], right[i], 1, i < 2 ? ld_x : (int64_t)c.width, 0, i < 2 ? (int64_t)c.width : ld_dy, 1, 0};
-    p.out = grads[i]->data;
-    p.om = steps_of(*grads[i]).r;
-    p.on = steps_of(*grads[i]).c;
-    p.o_group = grads[i]->stride;
-    e = launch<T, kPlain>(p, c.rows, c.groups, s);
+  // operands as they lie, or copies
+  const void* in[5] = {x, dy, c.w[0]->data, c.w[1]->data, c.w[2]->data};
+  bool copy[5];
+  bool any = false;
+  for (int i = 0; i < 5; ++i) {
+    const bool none = i == 1 && !c.backward;
+    copy[i] = !none && (f32 || (i < 2 ? !units_of_16(in[i], i ? ld_dy : ld_x, 0, size)
+                                      : !units_of_16(in[i], c.w[i - 2]->ld, c.groups > 1 ? c.w[i - 2]->stride : 0, size)));
+    any |= copy[i];
   }
-  return e;
+  const Layout l = layout_of(c.rows, c.hidden, c.width, c.groups, c.type, any, c.backward);
+  if (c.ws_bytes < l.bytes) return cudaErrorInvalidValue;
+  const size_t place[5] = {l.x, l.dy, l.w[0], l.w[1], l.w[2]};
+  View v[5];
+  CopyJobs jobs{};
+  int64_t chunks = 0;
+  for (int i = 0; i < 5; ++i) {
+    if (i == 1 && !c.backward) continue;
+    const bool mat = i >= 2;
+    const layer_matrix_t* m = mat ? c.w[i - 2] : nullptr;
+    const int64_t wr = i == 4 ? c.width : c.hidden, wc = i == 4 ? c.hidden : c.width;
+    const int64_t rows = !mat ? c.rows : m->columns ? wc : wr;
+    const int cols = (int)(!mat ? c.hidden : m->columns ? wr : wc);
+    const int n = mat ? c.groups : 1;
+    v[i] = View{const_cast<void*>(in[i]), rows, mat ? m->ld : i ? ld_dy : ld_x, mat ? m->stride : 0, cols, n};
+    if (!copy[i]) continue;
+    CopyJob& j = jobs.job[jobs.n++];
+    j = CopyJob{in[i], v[i].ld, v[i].stride, rows, cols, (int)up8(cols), n, reinterpret_cast<uint16_t*>(c.ws + place[i]), 0};
+    v[i].p = j.dst;
+    v[i].ld = j.ld_out;
+    v[i].stride = rows * j.ld_out;
+    v[i].depth = n * planes;
+    j.plane = n * v[i].stride;
+    chunks = std::max(chunks, n * rows * (j.ld_out / 8));
+  }
+
+  Args a{};
+  a.plan = reinterpret_cast<Plan*>(c.ws + l.plan);
+  a.done_row = reinterpret_cast<int*>(c.ws + l.done);
+  a.done_group = a.done_row + l.row_tiles;
+  a.done_words = (int)l.done_words;
+  for (int p = 0; p < 3; ++p) {
+    a.count[p] = reinterpret_cast<int*>(c.ws + l.count[p]);
+    a.partial[p] = reinterpret_cast<float*>(c.ws + l.partial[p]);
+  }
+  a.clips = c.offsets && c.rows > 0 ? reinterpret_cast<const CUtensorMap*>(c.ws + l.clips) : nullptr;
+  a.backward = c.backward;
+  a.params = grads[0] != nullptr;
+  a.groups = c.groups;
+  a.rows = (int)c.rows;
+  a.hidden = c.hidden;
+  a.width = c.width;
+  // the second factor's K runs down its columns: x Wg by hidden, h Wd by width; dy Wd^T by hidden, dg Wg^T by width
+  a.b_columns[0] = c.backward ? down.columns != 0 : gate.columns == 0;
+  a.b_columns[1] = c.backward ? gate.columns != 0 : down.columns == 0;
+  a.kblocks[0] = up_div(c.hidden, 64);
+  a.kblocks[1] = up_div(c.width, 64);
+  a.segments = c.backward ? 2 : 1;
+  // a gradient in its weight's order: of a column-major weight the transposed product
+  const int left[3] = {kInX, kInX, kInH}, right[3] = {kInDG, kInDU, kInDY};
+  for (int p = 0; p < 3; ++p) {
+    const bool turned = c.w[p]->columns;
+    a.wa[p] = turned ? right[p] : left[p];
+    a.wb[p] = turned ? left[p] : right[p];
+    a.wrows[p] = (p == 2) != turned ? c.width : c.hidden;
+    a.wcols[p] = (p == 2) != turned ? c.hidden : c.width;
+  }
+  a.act = c.act;
+  a.pre = pre;
+  a.y = y;
+  a.ld_y = ld_y;
+  a.status = c.status;
+  const WaitLimit w = wait_limit();
+  a.wait_ns = w.ns;
+  a.hold = w.hold;
+  a.offsets = c.offsets;
+
+  Maps maps{};
+  if (c.rows > 0) {
+    View inter[3];
+    for (int i = 0; i < 3; ++i)
+      inter[i] = View{c.ws + l.inter[i], c.rows, up8(c.width), (int64_t)l.inter_plane, c.width, planes};
+    bool ok = make_map(&maps.a0, v[c.backward ? 1 : 0], etype, 64, 128) &&
+              make_map(&maps.a1[0], inter[c.backward ? 1 : 0], etype, 64, 128) &&
+              make_map(&maps.a1[1], inter[c.backward ? 2 : 0], etype, 64, 128);
+    for (int i = 0; i < 2; ++i) {
+      ok = ok && make_map(&maps.w0[i], v[c.backward ? 4 : 2 + i], etype, 64, a.b_columns[0] ? 64 : 128) &&
+           make_map(&maps.w1[i], v[c.backward ? 2 + i : 4], etype, 64, a.b_columns[1] ? 64 : 128);
+    }
+    ok = ok && make_map(&maps.clip[kH], inter[0], etype, 32, 32);
+    a.y_tma = units_of_16(y, ld_y, 0, size);
+    if (a.y_tma) ok = ok && make_map(&maps.clip[kY], View{y, c.rows, ld_y, 0, c.hidden, 1}, c.type, 32, 32);
+    if (c.backward) {
+      ok = ok && make_map(&maps.clip[kDG], inter[1], etype, 32, 32) && make_map(&maps.clip[kDU], inter[2], etype, 32, 32) &&
+           make_map(&maps.clip[kInX], v[0], etype, 64, 64) && make_map(&maps.clip[kInDY], v[1], etype, 64, 64) &&
+           make_map(&maps.clip[kInH], inter[0], etype, 64, 64) && make_map(&maps.clip[kInDG], inter[1], etype, 64, 64) &&
+           make_map(&maps.clip[kInDU], inter[2], etype, 64, 64);
+    }
+    for (int p = 0; p < 3 && a.params; ++p) {
+      const layer_matrix_t& g = *grads[p];
+      const int64_t r = p < 2 ? c.hidden : c.width, k = p < 2 ? c.width : c.hidden;
+      a.dw_tma[p] = units_of_16(g.data, g.ld, c.groups > 1 ? g.stride : 0, size);
+      if (a.dw_tma[p])
+        ok = ok && make_map(&maps.dw[p], View{g.data, g.columns ? k : r, g.ld, g.stride, (int)(g.columns ? r : k), c.groups},
+                            c.type, 32, 32);
+    }
+    if (!ok) return cudaErrorInvalidValue;
+  }
+  for (int p = 0; p < 3 && a.params; ++p) {
+    a.dw[p] = grads[p]->data;
+    a.ld_dw[p] = grads[p]->ld;
+    a.stride_dw[p] = grads[p]->stride;
+  }
+
+  cudaError_t e = prepare(maps, a, c.type, s);
+  if (e != cudaSuccess || c.rows == 0) return e;
+  if (jobs.n > 0) {
+    const unsigned ctas = (unsigned)std::min<int64_t>(152 * 8, (chunks + 255) / 256);
+    if (f32)
+      copy_kernel<true><<<ctas, 256, 0, s>>>(jobs);
+    else
+      copy_kernel<false><<<ctas, 256, 0, s>>>(jobs);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  return run(maps, a, c.type, l.units, s);
 }
 
 }  // namespace
@@ -289,13 +332,15 @@ extern "C" {
 
 size_t layer_ffn_pre_elems(int64_t rows, int64_t width, int32_t groups) {
   if (bad_sizes(rows, 1, width, groups, SOAP_F32)) return 0;
-  return (size_t)rows * 2 * width;
+  // each group's rows in blocks of 32
+  const int64_t blocks = (rows + 31 * std::min<int64_t>(rows, groups)) / 32;
+  return (size_t)blocks * 32 * 2 * ((width + 31) / 32 * 32);
 }
 
 size_t layer_ffn_workspace_bytes(int64_t rows, int64_t hidden, int64_t width, int32_t groups, int32_t type,
                                  int32_t aligned, int32_t backward) {
   if (bad_sizes(rows, hidden, width, groups, type)) return 0;
-  return up256((kMaxGroups + 1) * 4) + (backward ? 3 : 1) * up256((size_t)rows * width * dtype_size(type));
+  return layout_of(rows, hidden, width, groups, type, !aligned, backward != 0).bytes;
 }
 
 soap_status_t layer_ffn_forward(int64_t rows, int64_t hidden, int64_t width, int32_t groups,
@@ -304,18 +349,18 @@ soap_status_t layer_ffn_forward(int64_t rows, int64_t hidden, int64_t width, int
                                 int32_t act, void* y, int64_t ld_y, float* pre, int32_t* status, void* workspace,
                                 size_t workspace_bytes, soap_stream_t stream) {
   if (bad_sizes(rows, hidden, width, groups, type)) return SOAP_ERR_INVALID_ARG;
-  const Call c{rows, (int)hidden, (int)width, groups, offsets, type, act, gate, up, down, status,
-               static_cast<uint8_t*>(workspace)};
+  const Call c{rows, (int)hidden, (int)width, groups, offsets, type, act, {gate, up, down}, status,
+               static_cast<uint8_t*>(workspace), workspace_bytes, false};
   const size_t size = dtype_size(type);
-  if (bad_call(c, workspace_bytes, false) || bad_ptr(pre, 16)) return SOAP_ERR_INVALID_ARG;
+  if (bad_call(c) || bad_ptr(pre, 16)) return SOAP_ERR_INVALID_ARG;
   if (rows > 0 && (!x || bad_ptr(x, size) || ld_x < hidden || !y || bad_ptr(y, size) || ld_y < hidden))
     return SOAP_ERR_INVALID_ARG;
+  if (rows == 0) return SOAP_OK;
   cudaStream_t s = (cudaStream_t)stream;
   ProfScope prof(kFamGemmTc, 6.0 * rows * hidden * width, 3.0 * groups * hidden * width * size, s);
-  const cudaError_t e = type == SOAP_F32    ? forward<float>(c, x, ld_x, y, ld_y, pre, s)
-                        : type == SOAP_BF16 ? forward<__nv_bfloat16>(c, x, ld_x, y, ld_y, pre, s)
-                                            : forward<__half>(c, x, ld_x, y, ld_y, pre, s);
-  return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;
+  const layer_matrix_t* none[3] = {nullptr, nullptr, nullptr};
+  const cudaError_t e = compute(c, x, ld_x, nullptr, 0, pre, y, ld_y, none, s);
+  return e == cudaSuccess ? SOAP_OK : e == cudaErrorInvalidValue ? SOAP_ERR_INVALID_ARG : SOAP_ERR_CUDA;
 }
 
 soap_status_t layer_ffn_backward(int64_t rows, int64_t hidden, int64_t width, int32_t groups,
@@ -326,29 +371,25 @@ soap_status_t layer_ffn_backward(int64_t rows, int64_t hidden, int64_t width, in
                                  const layer_matrix_t* d_down, int32_t* status, void* workspace,
                                  size_t workspace_bytes, soap_stream_t stream) {
   if (bad_sizes(rows, hidden, width, groups, type)) return SOAP_ERR_INVALID_ARG;
-  const Call c{rows, (int)hidden, (int)width, groups, offsets, type, act, gate, up, down, status,
-               static_cast<uint8_t*>(workspace)};
+  const Call c{rows, (int)hidden, (int)width, groups, offsets, type, act, {gate, up, down}, status,
+               static_cast<uint8_t*>(workspace), workspace_bytes, true};
   const size_t size = dtype_size(type);
-  if (bad_call(c, workspace_bytes, true) || bad_ptr(pre, 16)) return SOAP_ERR_INVALID_ARG;
+  if (bad_call(c) || bad_ptr(pre, 16)) return SOAP_ERR_INVALID_ARG;
   if (rows > 0 && (!x || bad_ptr(x, size) || ld_x < hidden || !dy || bad_ptr(dy, size) || ld_dy < hidden || !dx ||
                    bad_ptr(dx, size) || ld_dx < hidden || !pre))
     return SOAP_ERR_INVALID_ARG;
   const layer_matrix_t* grads[3] = {d_gate, d_up, d_down};
   if (!d_gate != !d_up || !d_gate != !d_down) return SOAP_ERR_INVALID_ARG;
   if (d_gate)
-    for (int i = 0; i < 3; ++i) {
-      const layer_matrix_t* w = i == 0 ? gate : i == 1 ? up : down;
+    for (int i = 0; i < 3; ++i)
       if (bad_matrix(grads[i], i < 2 ? hidden : width, i < 2 ? width : hidden, groups, size) ||
-          !grads[i]->columns != !w->columns)
+          !grads[i]->columns != !c.w[i]->columns)
         return SOAP_ERR_INVALID_ARG;
-    }
+  if (rows == 0 && !d_gate) return SOAP_OK;
   cudaStream_t s = (cudaStream_t)stream;
-  ProfScope prof(kFamGemmTc, 12.0 * rows * hidden * width, 3.0 * groups * hidden * width * size, s);
-  const cudaError_t e =
-      type == SOAP_F32    ? backward<float>(c, dy, ld_dy, x, ld_x, pre, dx, ld_dx, grads, s)
-      : type == SOAP_BF16 ? backward<__nv_bfloat16>(c, dy, ld_dy, x, ld_x, pre, dx, ld_dx, grads, s)
-                          : backward<__half>(c, dy, ld_dy, x, ld_x, pre, dx, ld_dx, grads, s);
-  return e == cudaSuccess ? SOAP_OK : SOAP_ERR_CUDA;
+  ProfScope prof(kFamGemmTc, (d_gate ? 12.0 : 6.0) * rows * hidden * width, 3.0 * groups * hidden * width * size, s);
+  const cudaError_t e = compute(c, x, ld_x, dy, ld_dy, const_cast<float*>(pre), dx, ld_dx, grads, s);
+  return e == cudaSuccess ? SOAP_OK : e == cudaErrorInvalidValue ? SOAP_ERR_INVALID_ARG : SOAP_ERR_CUDA;
 }
 
 }  // extern "C"

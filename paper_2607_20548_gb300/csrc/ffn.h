@@ -1,0 +1,78 @@
+// Internal declarations of the gated feed-forward block (include/layer.h, layer_ffn_*).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace soap {
+namespace ffn {
+
+constexpr int kMaxGroups = 1024;
+constexpr int kUnitPairs = 76;      // pairs of CTAs that a product's parts are shared out among
+constexpr int kMaxSlices = 1024;    // most slices of 64 products that one accumulator adds up
+constexpr int kPartial = 256 * 256; // fp32 elements of a part's sums
+
+// Maps that end at a group's last row, so that loads of its rows give 0 beyond it and stores leave the rows behind it
+// alone: results (boxes of 32 x 32) and factors of the weights' gradients (boxes of 64 x 64).
+enum Clip { kH, kY, kDG, kDU, kInX, kInDY, kInH, kInDG, kInDU, kClips };
+
+struct Maps {
+  CUtensorMap a0;           // factors of 128 rows: x or dy
+  CUtensorMap a1[2];        // h, or dg and du
+  CUtensorMap w0[2];        // gate and up, or down
+  CUtensorMap w1[2];        // down, or gate and up
+  CUtensorMap dw[3];        // results: the weights' gradients
+  CUtensorMap clip[kClips]; // dense: up to the last row; groups: what their own are made from
+};
+
+// What is made on the device before the products run.
+struct Plan {
+  int next, through, gave_up;  // the list's next place; CTAs that are through; whether a wait gave up
+  int total;                   // units in the list
+  int first[3];                // of the phases
+  int tiles[2], splits[2];     // of the row phases
+  int bounds[kMaxGroups + 1];  // the groups' rows
+  int row_tiles[kMaxGroups + 1];  // tiles of 256 rows before each group
+  int blocks[kMaxGroups + 1];     // blocks of 32 rows before each group
+  int parts[kMaxGroups + 1];      // parts along the rows (of the weights' gradients) before each group
+  int slots[kMaxGroups + 1];      // of them those of groups with more than one
+};
+
+struct Args {
+  Plan* plan;
+  int *done_row, *done_group;   // stored parts of h (or dg, du and h), per row tile and per group
+  int *count[3];                // parts that are there, per warp's share of a tile, per phase
+  float* partial[3];
+  int slots[3];                 // of partial
+  const CUtensorMap* clips;     // [groups][kClips], or nullptr: those in Maps
+  int backward, params;
+  int groups, rows, hidden, width;
+  int b_columns[2];             // whether the second factor of a row phase has its K dimension outermost
+  int kblocks[2], segments;     // slices per factor pair; pairs of the second phase
+  int wa[3], wb[3];             // Clip of the factors of the weights' gradients
+  int wrows[3], wcols[3];       // sides of the weights' gradients as they are stored
+  int act;
+  float* pre;
+  void* y;                      // y or dx
+  int64_t ld_y;
+  int y_tma;
+  void* dw[3];
+  int64_t ld_dw[3], stride_dw[3];
+  int dw_tma[3];
+  int* status;
+  uint64_t wait_ns;
+  const int* hold;
+  const int32_t* offsets;       // the caller's
+  int done_words;               // to zero, from done_row on
+};
+
+// type: soap_dtype_t. units: no more than this many are ever in the list.
+cudaError_t run(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s);
+// The plan, the groups' maps, zeros for rows of no group and for the gradients of groups without rows.
+cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s);
+
+inline __host__ __device__ int up_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+}  // namespace ffn
+}  // namespace soap

@@ -1,0 +1,926 @@
+// The products of the gated feed-forward block on the 5th-generation tensor cores: all of a call's in one launch,
+//   forward   g, u = x Wg, x Wu -> h = act(g) u;  y = h Wd
+//   backward  dh = dy Wd^T -> dg, du, h;  dx = dg Wg^T + du Wu^T;  dWg, dWu = x^T dg, x^T du;  dWd = h^T dy
+// for every group of rows, with fp32 accumulation.
+//
+// Operands are read as they lie, with K along their rows (K-major) or down their columns (MN-major), so that no
+// transposed copy exists. 16-bit operands go to the tensor cores as they are. An fp32 operand comes as three bf16
+// planes that hold its 24 bits, and the six products of planes whose terms reach 2^-24 are added, small ones first:
+// the accumulator cuts (a sum loses 2^-25 of itself per 16 products, measured), so that K goes in runs of 256, whose
+// sums the epilogue adds in fp32 registers.
+//
+// Schedule. Persistent CTA pairs (cta_group::2: a pair's 256 x 256 tile has 128 rows in each CTA) take units from one
+// list, each its next one when it begins the one before: a phase's tiles, or parts of them along K where the tiles are
+// fewer than the pairs (the part that is stored last adds up all of them, always in the same order). Tiles of the
+// first phase are 256 rows by 128 columns of both g and u, one CTA of the pair loading Wg's, the other Wu's, so that
+// both values of an element meet in one thread. A unit waits until what it reads of the phase before is stored, which
+// counters per row tile and per group tell; such waits point to earlier units, which are taken by CTAs that run, so
+// that they end.
+//
+// In a CTA, one warp takes units and waits for their inputs, two issue TMA loads of the factors' 64-element K slices
+// into a ring, one (of the pair's first CTA) the MMAs, and eight drain the accumulator in blocks of 32 x 32, which leave
+// by TMA through shared memory. g and u are kept for the backward pass in fp32, in blocks of 32 x 32 with the rows
+// side by side, so that a warp writes and reads them in whole lines without shared memory. Every wait is bounded
+// (soap_wait_limit); one that runs out sets SOAP_STATUS_TIMEOUT, the CTA drains its copies, frees its tensor memory and
+// returns, and the last CTA then makes all results NaN.
+#include <algorithm>
+#include <atomic>
+
+#include "../../include/layer.h"
+#include "ffn.h"
+#include "pair.h"
+#include "profile.h"
+#include "soap_internal.h"
+
+namespace soap {
+namespace ffn {
+namespace {
+
+using namespace tc;
+
+enum Kind { kEnd = -1, kGated, kGrad, kOut, kWeight };
+
+constexpr int kEpiWarps = 8;
+constexpr int kLoadB = 2 + kEpiWarps, kScout = kLoadB + 1;  // warps
+constexpr int kThreads = 32 * (kScout + 1);
+constexpr int kStages = 5, kStage = 2 * kTile;
+constexpr int kStaging = 8192;      // per epilogue warp
+constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
+// units that the roles of a pair may be apart, and more: 1 + 5 + 2 + 1 (every unit takes at least one of the ring's
+// slots, of which each takes both CTAs' loading threads, and one of two accumulators)
+constexpr int kKept = 16;
+constexpr int kRun = 4;             // slices in a run of fp32 operands
+constexpr int kMinPart = 4;         // slices in a part along K, at least
+
+struct Unit {
+  int kind, group, prod;
+  int m0, n0, M, N;  // of the result (a row phase: rows of the group)
+  int start;         // the group's first row
+  int s0, s1;        // slices
+  int splits, part, slot, tile;  // parts along K; this one, its place among the partial sums, and its tile's
+  int row_tile, block;           // among all groups'
+};
+constexpr int kSmem = 1024 + kStages * kStage + kEpiWarps * kStaging + kKept * (int)sizeof(Unit) + 256;
+static_assert(kSmem <= 232448, "shared memory");
+
+template <int TYPE>
+struct Element;
+template <>
+struct Element<SOAP_F32> {
+  using T = float;
+};
+template <>
+struct Element<SOAP_BF16> {
+  using T = __nv_bfloat16;
+};
+template <>
+struct Element<SOAP_F16> {
+  using T = __half;
+};
+
+// kind::f16, M = N = 256: D = f32, A and B bf16 or f16; bits 15 and 16 mark MN-major operands.
+__host__ __device__ constexpr uint32_t idesc_16(bool bf16, int a_mn, int b_mn) {
+  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (static_cast<uint32_t>(a_mn) << 15) |
+         (static_cast<uint32_t>(b_mn) << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+}
+
+// 32 columns at each of two places of this lane's accumulator row.
+__device__ __forceinline__ void tmem_ld32x2(uint32_t t0, uint32_t t1, float (&v)[32], float (&w)[32]) {
+  uint32_t r[64];
+#define SOAP_LD32(o, at)                                                                                              \
+  asm volatile(                                                                                                       \
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "                                                                       \
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "                                       \
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"                       \
+      : "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]),    \
+        "=r"(r[o + 7]), "=r"(r[o + 8]), "=r"(r[o + 9]), "=r"(r[o + 10]), "=r"(r[o + 11]), "=r"(r[o + 12]),             \
+        "=r"(r[o + 13]), "=r"(r[o + 14]), "=r"(r[o + 15]), "=r"(r[o + 16]), "=r"(r[o + 17]), "=r"(r[o + 18]),          \
+        "=r"(r[o + 19]), "=r"(r[o + 20]), "=r"(r[o + 21]), "=r"(r[o + 22]), "=r"(r[o + 23]), "=r"(r[o + 24]),          \
+        "=r"(r[o + 25]), "=r"(r[o + 26]), "=r"(r[o + 27]), "=r"(r[o + 28]), "=r"(r[o + 29]), "=r"(r[o + 30]),          \
+        "=r"(r[o + 31])                                                                                               \
+      : "r"(at))
+  SOAP_LD32(0, t0);
+  SOAP_LD32(32, t1);
+#undef SOAP_LD32
+  // (the values pass through the wait, so that nothing reads them before it)
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) asm volatile("" : "+r"(r[i]));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    v[i] = __uint_as_float(r[i]);
+    w[i] = __uint_as_float(r[32 + i]);
+  }
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t t, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(t)
+      : "memory");
+}
+
+// The largest i with prefix[i] <= q.
+__device__ __forceinline__ int group_of(const int* prefix, int n, int q) {
+  int lo = 0, hi = n;  // prefix[lo] <= q < prefix[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    (prefix[mid] <= q ? lo : hi) = mid;
+  }
+  return lo;
+}
+
+// Tile i of nm x nn in groups of 8 row tiles, row tile fastest, so that tiles in flight share operands in L2.
+__device__ __forceinline__ void tile_place(int i, int nm, int nn, int& m, int& n) {
+  const int of8 = 8 * nn, gr = i / of8, in = i - gr * of8, rows = min(8, nm - gr * 8);
+  n = in / rows;
+  m = gr * 8 + in - n * rows;
+}
+
+__device__ __forceinline__ Unit unit_at(int p, const Args& a) {
+  const Plan& l = *a.plan;
+  Unit u{};
+  const int phase = p >= l.first[2] ? 2 : p >= l.first[1] ? 1 : 0;
+  int i = p - l.first[phase];
+  if (phase < 2) {
+    u.slot = i;
+    const int tiles = l.tiles[phase], wide = phase == 0 && !a.backward ? 128 : 256;
+    u.N = phase == 0 ? a.width : a.hidden;
+    u.kind = phase == 1 ? kOut : a.backward ? kGrad : kGated;
+    u.splits = l.splits[phase];
+    u.part = i / tiles;
+    i -= u.part * tiles;
+    u.tile = i;
+    const int nn = up_div(u.N, wide);
+    u.group = group_of(l.row_tiles, a.groups, i / nn);
+    i -= l.row_tiles[u.group] * nn;
+    int m, n;
+    tile_place(i, l.row_tiles[u.group + 1] - l.row_tiles[u.group], nn, m, n);
+    u.start = l.bounds[u.group];
+    u.M = l.bounds[u.group + 1] - u.start;
+    u.m0 = m * 256;
+    u.n0 = n * wide;
+    u.row_tile = l.row_tiles[u.group] + m;
+    u.block = l.blocks[u.group] + m * 8;
+    const int slices = a.kblocks[phase] * (phase == 1 ? a.segments : 1);
+    u.s0 = (int)((int64_t)slices * u.part / u.splits);
+    u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
+  } else {
+    const int nm = up_div(a.wrows[0], 256), nn = up_div(a.wcols[0], 256), each = nm * nn, q = i / (3 * each);
+    u.kind = kWeight;
+    u.group = group_of(l.parts, a.groups, q);
+    u.splits = l.parts[u.group + 1] - l.parts[u.group];
+    u.part = q - l.parts[u.group];
+    i -= q * 3 * each;
+    u.tile = l.slots[u.group] * 3 * each + i;
+    u.slot = u.tile + u.part * 3 * each;
+    u.prod = i / each;
+    i -= u.prod * each;
+    u.M = a.wrows[u.prod];
+    u.N = a.wcols[u.prod];
+    int m, n;
+    tile_place(i, up_div(u.M, 256), up_div(u.N, 256), m, n);
+    u.m0 = m * 256;
+    u.n0 = n * 256;
+    u.start = l.bounds[u.group];
+    const int slices = up_div(l.bounds[u.group + 1] - u.start, BK);
+    u.s0 = (int)((int64_t)slices * u.part / u.splits);
+    u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
+  }
+  return u;
+}
+
+// Products of planes (of A's, of B's) that an fp32 product is made of, small ones first.
+constexpr int kTerms = 6;
+__device__ __forceinline__ int term_a(int t) { return (0x201100 >> (4 * (5 - t))) & 0xf; }
+__device__ __forceinline__ int term_b(int t) { return (0x021010 >> (4 * (5 - t))) & 0xf; }
+
+// The slices of a unit in the order in which all roles take them.
+template <int TYPE>
+struct Order {
+  static constexpr bool kSplit = TYPE == SOAP_F32;
+  static constexpr int kTermsOf = kSplit ? kTerms : 1;
+  __device__ __forceinline__ static int end_of_run(int from, int s1) { return kSplit ? min(s1, from + kRun) : s1; }
+};
+
+// One factor's slices of a unit into the ring.
+struct Loader {
+  Ring st;
+  uint32_t ring, bars;
+  uint64_t *full, *empty;
+  uint64_t lim;
+};
+
+template <int MN>
+__device__ __forceinline__ void load_run(Loader& l, int kb, int to, int kblocks, int k_at, const CUtensorMap* m0,
+                                         const CUtensorMap* m1, int row, int z, uint32_t bytes) {
+  for (; kb < to; ++kb) {
+    Ring& st = l.st;
+    if (!(st.ok = mbar_wait(&l.empty[st.s], st.parity, l.lim))) return;
+    if (bytes) expect_tx(&l.full[st.s], bytes);
+    const bool second = kb >= kblocks;
+    load_tile<MN>(l.ring + st.s * kStage, second ? m1 : m0, l.bars + st.s * 8, row,
+                  k_at + (second ? kb - kblocks : kb) * BK, z);
+    if (++st.s == kStages) {
+      st.s = 0;
+      st.parity ^= 1;
+    }
+  }
+}
+
+template <int A_MN, int B_MN>
+__device__ __forceinline__ void issue(Ring& st, int count, uint32_t idesc, uint32_t ring, uint64_t* full, uint64_t* empty,
+                                      uint32_t d, uint64_t lim) {
+  uint32_t more = 0;
+  for (; count > 0; --count) {
+    if (!(st.ok = mbar_wait(&full[st.s], st.parity, lim))) return;
+    tc_fence_after();
+    const uint32_t as = ring + st.s * kStage, bs = as + kTile;
+#pragma unroll
+    for (int kk = 0; kk < BK / 16; ++kk) {
+      umma_f16(d, tile_desc<A_MN>(as, kk), tile_desc<B_MN>(bs, kk), idesc, more);
+      more = 1;
+    }
+    commit_pair(&empty[st.s]);
+    if (++st.s == kStages) {
+      st.s = 0;
+      st.parity ^= 1;
+    }
+  }
+}
+
+// act(g) and its derivative. 16-bit results: the hardware's exponential and quotient (2^-21 of the result).
+template <int TYPE>
+__device__ __forceinline__ void activation(int act, float g, float& a, float& da) {
+  if (act == LAYER_SILU) {
+    const float s = TYPE == SOAP_F32 ? 1.f / (1.f + expf(-g)) : __fdividef(1.f, 1.f + __expf(-g));
+    a = g * s;
+    da = s * fmaf(g, 1.f - s, 1.f);
+  } else {
+    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    const float e = TYPE == SOAP_F32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g);
+    a = g * p;
+    da = fmaf(g * 0.3989422804014327f, e, p);
+  }
+}
+
+// Rounds v into this lane's row of a staged block of 32 x 32.
+template <typename T>
+__device__ __forceinline__ void put(uint8_t* slot, const float (&v)[32], int lane) {
+  constexpr int V = 16 / sizeof(T);
+#pragma unroll
+  for (int u = 0; u < 32 / V; ++u) {
+    Pack<T, V> p;
+#pragma unroll
+    for (int e = 0; e < V; e += 2) from_pair(make_float2(v[u * V + e], v[u * V + e + 1]), p.v + e);
+    *reinterpret_cast<Pack<T, V>*>(slot + (sizeof(T) == 4 ? at32(lane, u) : at16(lane, u))) = p;
+  }
+}
+
+// The upper 8 bits of x's significand as bf16, and what is left (nothing of what is not finite).
+__device__ __forceinline__ float upper(float& x) {
+  const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  const bool finite = fabsf(x) < INFINITY;
+  const float r = finite ? hi : x;
+  x = finite ? x - hi : 0.f;
+  return r;
+}
+
+__device__ __forceinline__ void fence_map(const CUtensorMap* m) {
+  asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+}
+
+template <int TYPE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
+  using T = typename Element<TYPE>::T;
+  using O = Order<TYPE>;
+  constexpr bool SPLIT = O::kSplit;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* staging = smem + kStages * kStage;
+  Unit* units = reinterpret_cast<Unit*>(staging + kEpiWarps * kStaging);
+  uint64_t* full = reinterpret_cast<uint64_t*>(units + kKept);
+  uint64_t* empty = full + kStages;
+  uint64_t* acc_full = empty + kStages;
+  uint64_t* acc_empty = acc_full + 2;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
+  volatile int* taken = reinterpret_cast<volatile int*>(tmem_at + 2);  // what the pair's first CTA tells the second
+  // counts of units: known in this CTA, with their inputs there, begun by the first loading thread, given to the second CTA
+  const uint32_t known_at = smem_u32(tmem_at + 2 + kKept), ready_at = known_at + 4, begun_at = known_at + 8,
+                 given_at = known_at + 12;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)(blockIdx.x & 1);  // in the pair
+  const uint64_t lim = a.wait_ns;          // bound of every wait (for another role of the pair: twice)
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 2 * kEpiWarps);
+    }
+    *abort_flag = 0;
+    set_ready(known_at, 0);
+    set_ready(ready_at, 0);
+    set_ready(begun_at, 0);
+    set_ready(given_at, 0);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)), "r"(512));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // both CTAs' barriers are ready
+  tc_fence_after();
+  const uint32_t tmem = *tmem_at;
+
+  if (warp == kScout) {
+    if (lane == 0) {
+      bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
+      const int total = a.plan->total;
+      uint32_t peer;
+      asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at + 2)));
+      for (int m = 0; ok && !*abort_flag; ++m) {
+        int p;
+        if (rank == 0) {
+          if (!(ok = wait_given(begun_at, m, 2 * lim))) break;
+          p = atomicAdd(&a.plan->next, 1);
+          if (p >= total) p = -1;
+          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * (m % kKept)), "r"(p) : "memory");
+          asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * kKept + 12), "r"(m + 1) : "memory");
+        } else {
+          if (!(ok = wait_given(given_at, m + 1, 2 * lim))) break;
+          p = taken[m % kKept];
+        }
+        Unit& u = units[m % kKept];
+        if (p < 0) {
+          u.kind = kEnd;
+        } else {
+          u = unit_at(p, a);
+        }
+        set_ready(known_at, m + 1);
+        if (p >= 0) {
+          if (u.kind == kOut)
+            ok = wait_done(a.done_row + u.row_tile, kPerTile * up_div(a.width, a.backward ? 256 : 128), lim);
+          else if (u.kind == kWeight)
+            ok = wait_done(a.done_group + u.group,
+                           kPerTile * up_div(a.width, 256) * (a.plan->row_tiles[u.group + 1] - a.plan->row_tiles[u.group]), lim);
+          if (!ok) break;
+          asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
+        }
+        set_ready(ready_at, m + 1);
+        if (p < 0) break;
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        if (a.status) atomicOr(a.status, kStatusTimeout);
+      }
+    }
+  } else if (warp == 0 || warp == kLoadB) {
+    if (lane == 0) {
+      const bool is_b = warp == kLoadB;
+      Loader l;
+      l.st.parity = 1;  // of a slot's release
+      l.ring = smem_u32(smem) + (is_b ? kTile : 0);
+      l.bars = in_leader(full);
+      l.full = full;
+      l.empty = empty;
+      l.lim = 2 * lim;
+      int used = 0;  // slots filled so far (up to kStages)
+      for (int m = 0; !*abort_flag; ++m) {
+        // weights do not wait for the phase before
+        if (!(l.st.ok = wait_ready(known_at, m + 1, 2 * lim))) break;
+        const Unit u = units[m % kKept];
+        if (u.kind == kEnd) break;
+        if ((!is_b || u.kind == kWeight) && !(l.st.ok = wait_ready(ready_at, m + 1, 2 * lim))) break;
+        if (!is_b) set_ready(begun_at, m + 1);
+        const CUtensorMap *m0, *m1;
+        int row, z = 0, planes = 0, kblocks, k_at = 0;
+        bool mn;
+        if (u.kind == kWeight) {
+          const int which = is_b ? a.wb[u.prod] : a.wa[u.prod];
+          m0 = m1 = a.clips ? a.clips + u.group * kClips + which : &maps.clip[which];
+          if (a.clips) fence_map(m0);
+          row = (is_b ? u.n0 : u.m0) + rank * 128;
+          kblocks = INT_MAX;
+          k_at = u.start;
+          planes = 1;
+          mn = true;
+        } else {
+          const int phase = u.kind == kOut;
+          kblocks = a.kblocks[phase];
+          if (!is_b) {
+            m0 = phase ? &maps.a1[0] : &maps.a0;
+            m1 = phase ? &maps.a1[1] : m0;
+            row = u.start + u.m0 + rank * 128;
+            planes = 1;
+            mn = false;
+          } else {
+            m0 = phase ? &maps.w1[0] : &maps.w0[u.kind == kGated ? rank : 0];
+            m1 = phase ? &maps.w1[1] : m0;
+            row = u.kind == kGated ? u.n0 : u.n0 + rank * 128;
+            z = u.group;
+            planes = a.groups;
+            mn = a.b_columns[phase];
+          }
+        }
+        const uint32_t bytes = rank != 0 || is_b ? 0 : 2 * kStage;
+        used = min(used + (u.s1 - u.s0) * O::kTermsOf, kStages);
+        for (int kb = u.s0; kb < u.s1 && l.st.ok;) {
+          const int to = O::end_of_run(kb, u.s1);
+          for (int t = 0; t < O::kTermsOf && l.st.ok; ++t) {
+            const int zt = z + (SPLIT ? (is_b ? term_b(t) : term_a(t)) * planes : 0);
+            if (mn)
+              load_run<1>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes);
+            else
+              load_run<0>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes);
+          }
+          kb = to;
+        }
+        if (!l.st.ok) break;
+      }
+      Ring& st = l.st;
+      // every slice consumed, and its release arrived here, before this CTA's barriers go away
+      for (int i = 0; i < kStages && st.ok && !*abort_flag; ++i) {
+        if (used == kStages || st.s - 1 - i >= 0) {
+          const int slot = (st.s - 1 - i + kStages) % kStages;
+          st.ok = mbar_wait(&empty[slot], slot < st.s ? st.parity ^ 1 : st.parity, lim);
+        }
+      }
+      if (!st.ok || *abort_flag) {
+        *abort_flag = 1;
+        if (a.status) atomicOr(a.status, kStatusTimeout);
+        // copies in flight land before the shared memory goes away: far above a copy's time
+        const uint64_t t0 = globaltimer();
+        while (globaltimer() - t0 < 10000000ull) {
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      Ring st;
+      int n = 0;
+      const uint32_t ring = smem_u32(smem);
+      for (int m = 0; st.ok && !*abort_flag; ++m) {
+        if (!(st.ok = wait_ready(known_at, m + 1, 2 * lim))) break;
+        const Unit& u = units[m % kKept];
+        const int kind = u.kind, s1 = u.s1;
+        int kb = u.s0;
+        if (kind == kEnd) break;
+        const bool a_mn = kind == kWeight, b_mn = kind == kWeight || a.b_columns[kind == kOut];
+        const uint32_t idesc = idesc_16(TYPE != SOAP_F16, a_mn, b_mn);
+        for (; kb < s1 && st.ok; ++n) {
+          const int to = O::end_of_run(kb, s1), ac = n & 1, count = (to - kb) * O::kTermsOf;
+          if (n >= 2 && !(st.ok = mbar_wait(&acc_empty[ac], ((n >> 1) & 1) ^ 1, 2 * lim))) break;
+          tc_fence_after();
+          const uint32_t d = tmem + static_cast<uint32_t>(ac * 256);
+          if (a_mn)
+            issue<1, 1>(st, count, idesc, ring, full, empty, d, 2 * lim);
+          else if (b_mn)
+            issue<0, 1>(st, count, idesc, ring, full, empty, d, 2 * lim);
+          else
+            issue<0, 0>(st, count, idesc, ring, full, empty, d, 2 * lim);
+          if (st.ok) commit_pair(&acc_full[ac]);
+          kb = to;
+        }
+      }
+      if (!st.ok) *abort_flag = 1;
+    }
+  } else {
+    const int q = warp & 3;           // accumulator lanes 32 q .. 32 q + 31
+    const int half = (warp - 2) / 4;  // its columns: of g and u 64 each, else 128
+    uint8_t* stage = staging + (warp - 2) * kStaging;
+    constexpr int kSlot = SPLIT ? 4096 : 2048, kSlots = kStaging / kSlot;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16);
+    const int pre_cols = (a.width + 31) / 32;  // blocks
+    int n = 0;  // accumulators so far
+    int k = 0;  // staged blocks so far
+    bool ok = true;
+    // a place for a block whose copy out has been read
+    auto next_slot = [&]() {
+      if (lane == 0) sent_read<kSlots - 1>();
+      __syncwarp();
+      return stage + (k++ % kSlots) * kSlot;
+    };
+    auto send = [&](const CUtensorMap* map, const uint8_t* slot, int x, int y, int z) {
+      before_tma();
+      __syncwarp();
+      if (lane == 0) send_block(map, smem_u32(slot), x, y, z);
+    };
+    for (int m = 0;; ++m) {
+      if (lane == 0) ok = wait_ready(known_at, m + 1, 2 * lim);
+      if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
+      const Unit u = units[m % kKept];
+      if (u.kind == kEnd) break;
+      const int r0 = u.m0 + rank * 128 + 32 * q;
+      const int c0 = u.kind == kGated ? u.n0 + 64 * half : u.n0 + 128 * half, cs = u.kind == kGated ? 32 : 64;
+      // none below the last row, and to the last column
+      const int blocks = r0 < u.M && c0 < u.N ? min(2, (u.N - c0 + cs - 1) / cs) : 0;
+      const uint32_t t0 = lanes + (u.kind == kGated ? 64 * half : 128 * half);
+      const uint32_t t_step = u.kind == kGated ? 32 : 64, t_second = u.kind == kGated ? 128 : 32;
+      const CUtensorMap* const clips = a.clips ? a.clips + u.group * kClips : maps.clip;
+      if (a.clips && lane == 0) {
+        if (u.kind <= kGrad) fence_map(clips + kH);
+        if (u.kind == kGrad) fence_map(clips + kDG), fence_map(clips + kDU);
+        if (u.kind == kOut) fence_map(clips + kY);
+      }
+
+      // h, dg or du: to the second phase's (and the weights' gradients') operand
+      auto to_operand = [&](Clip which, float (&v)[32], int col) {
+#pragma unroll
+        for (int plane = 0; plane < (SPLIT ? 3 : 1); ++plane) {
+          uint8_t* const slot = next_slot();
+          if constexpr (SPLIT) {
+            float w[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j] = upper(v[j]);
+            put<__nv_bfloat16>(slot, w, lane);
+          } else {
+            put<T>(slot, v, lane);
+          }
+          send(clips + which, slot, col, u.start + r0, plane);
+        }
+      };
+      auto to_result = [&](const float (&v)[32], int col) {
+        if (col >= u.N) return;
+        uint8_t* const slot = next_slot();
+        const bool weight = u.kind == kWeight;
+        if (weight ? a.dw_tma[u.prod] : a.y_tma) {
+          put<T>(slot, v, lane);
+          if (weight)
+            send(&maps.dw[u.prod], slot, col, r0, u.group);
+          else
+            send(clips + kY, slot, col, u.start + r0, 0);
+        } else {
+          if (lane == 0) sent_read<0>();  // (blocks stored here are not counted among the copies)
+          __syncwarp();
+          T* const to = weight ? static_cast<T*>(a.dw[u.prod]) + (int64_t)u.group * a.stride_dw[u.prod] : static_cast<T*>(a.y);
+          const int64_t ld = weight ? a.ld_dw[u.prod] : a.ld_y;
+          store_user(slot, v, to + (int64_t)(weight ? r0 : u.start + r0) * ld + col, ld, min(32, u.M - r0),
+                     min(32, u.N - col), false, lane);
+          before_tma();
+        }
+      };
+      auto pre_at = [&](int which, int col) {
+        return reinterpret_cast<float4*>(a.pre) +
+               ((((int64_t)u.block + r0 / 32 - u.m0 / 32) * 2 + which) * pre_cols + col / 32) * 256 + lane;
+      };
+      // block i of the tile: two times 32 columns
+      auto finish = [&](int i, float (&v)[32], float (&w)[32]) {
+        if (u.kind == kGated) {
+          const int col = c0 + 32 * i;
+          if (a.pre) {
+            float4 *pg = pre_at(0, col), *pu = pre_at(1, col);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              pg[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+              pu[32 * j] = make_float4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            float act, slope;
+            activation<TYPE>(a.act, v[j], act, slope);
+            v[j] = act * w[j];
+          }
+          to_operand(kH, v, col);
+        } else if (u.kind == kGrad) {
+          auto part = [&](float (&dh)[32], int col) {
+            if (col >= u.N) return;
+            const float4 *pg = pre_at(0, col), *pu = pre_at(1, col);
+            float g[32], up[32];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float4 x = pg[32 * j], y = pu[32 * j];
+              g[4 * j] = x.x, g[4 * j + 1] = x.y, g[4 * j + 2] = x.z, g[4 * j + 3] = x.w;
+              up[4 * j] = y.x, up[4 * j + 1] = y.y, up[4 * j + 2] = y.z, up[4 * j + 3] = y.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              float act, slope;
+              activation<TYPE>(a.act, g[j], act, slope);
+              g[j] = dh[j] * up[j] * slope;  // dg
+              up[j] = act * up[j];           // h
+              dh[j] *= act;                  // du
+            }
+            to_operand(kDG, g, col);
+            to_operand(kDU, dh, col);
+            if (a.params) to_operand(kH, up, col);
+          };
+          part(v, c0 + 64 * i);
+          part(w, c0 + 64 * i + 32);
+        } else {
+          to_result(v, c0 + 64 * i);
+          to_result(w, c0 + 64 * i + 32);
+        }
+      };
+      const int phase = u.kind == kWeight ? 2 : u.kind == kOut;
+      auto partial_at = [&](int slot, int i) {
+        return reinterpret_cast<float4*>(a.partial[phase]) +
+               (((int64_t)slot * kPerTile + rank * kEpiWarps + warp - 2) * 4 + 2 * i) * 256 + lane;
+      };
+      auto put_partial = [&](int i, const float (&v)[32], const float (&w)[32]) {
+        float4* p = partial_at(u.slot, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          p[256 + 32 * j] = make_float4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+        }
+      };
+      // whether this part is the tile's last; then the sums are formed, in the parts' order
+      auto last_part = [&]() {
+        __threadfence();
+        __syncwarp();
+        int there = 0;
+        if (lane == 0) there = atomicAdd(a.count[phase] + u.tile * kPerTile + rank * kEpiWarps + warp - 2, 1);
+        __threadfence();
+        return __shfl_sync(0xffffffffu, there, 0) == u.splits - 1;
+      };
+      const int tiles = phase < 2 ? a.plan->tiles[phase] : 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256);
+      auto get_partial = [&](int i, float (&v)[32], float (&w)[32]) {
+        const int slot0 = u.slot - u.part * tiles;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = w[j] = 0.f;
+        for (int s = 0; s < u.splits; ++s) {
+          const float4* p = partial_at(slot0 + s * tiles, i);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 x = __ldcg(p + 32 * j), y = __ldcg(p + 256 + 32 * j);
+            v[4 * j] += x.x, v[4 * j + 1] += x.y, v[4 * j + 2] += x.z, v[4 * j + 3] += x.w;
+            w[4 * j] += y.x, w[4 * j + 1] += y.y, w[4 * j + 2] += y.z, w[4 * j + 3] += y.w;
+          }
+        }
+      };
+      auto wait_acc = [&](int ac) {
+        ok = mbar_wait(&acc_full[ac], (n >> 1) & 1, 2 * lim) && !*abort_flag;
+        tc_fence_after();
+        return ok = __all_sync(0xffffffffu, ok);
+      };
+      auto release_acc = [&](int ac) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0)
+          asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_leader(&acc_empty[ac])) : "memory");
+      };
+      if constexpr (!SPLIT) {
+        const int ac = n & 1;
+        if (!wait_acc(ac)) break;
+        if (blocks == 0) release_acc(ac);
+        for (int i = 0; i < blocks; ++i) {
+          float v[32], w[32];
+          const uint32_t t = t0 + static_cast<uint32_t>(ac * 256) + i * t_step;
+          tmem_ld32x2(t, t + t_second, v, w);
+          if (i + 1 == blocks) release_acc(ac);
+          if (u.splits == 1)
+            finish(i, v, w);
+          else
+            put_partial(i, v, w);
+        }
+        ++n;
+      } else {
+        float sum[4][32];
+        bool begun = false;
+        for (int kb = u.s0; kb < u.s1; kb = O::end_of_run(kb, u.s1), ++n) {
+          const int ac = n & 1;
+          if (!wait_acc(ac)) break;
+#pragma unroll
+          for (int b = 0; b < 8; ++b)
+            if (b / 4 < blocks) {
+              float v[16];
+              tmem_ld16(t0 + static_cast<uint32_t>(ac * 256) + b / 4 * t_step + (b / 2 & 1) * t_second + (b & 1) * 16, v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                float& x = sum[b / 2][(b & 1) * 16 + j];
+                x = begun ? x + v[j] : v[j];
+              }
+            }
+          release_acc(ac);
+          begun = true;
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i < blocks) {
+            if (u.splits == 1)
+              finish(i, sum[2 * i], sum[2 * i + 1]);
+            else
+              put_partial(i, sum[2 * i], sum[2 * i + 1]);
+          }
+      }
+      bool done = true;
+      if (u.splits > 1) {
+        done = blocks == 0 ? u.part == 0 : last_part();
+        if (done)
+          for (int i = 0; i < blocks; ++i) {
+            float v[32], w[32];
+            get_partial(i, v, w);
+            finish(i, v, w);
+          }
+      }
+      if (done && u.kind <= kGrad && lane == 0) {  // stored: what waits for it may go on
+        sent_done<0>();
+        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.done_row + u.row_tile) : "memory");
+        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.done_group + u.group) : "memory");
+      }
+      __syncwarp();
+    }
+    if (lane == 0) sent_done<0>();
+    if (!ok) {
+      *abort_flag = 1;
+      if (lane == 0 && a.status) atomicOr(a.status, kStatusTimeout);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // neither CTA leaves while the other may still reach its shared memory
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  }
+
+  // Where a wait gave up, the last CTA makes all results NaN, so that none is taken for an answer.
+  if (threadIdx.x == 0) {
+    if (*abort_flag) atomicOr(&a.plan->gave_up, 1);
+    __threadfence();  // this CTA's results (and its word) come before its count
+    const bool last = atomicAdd(&a.plan->through, 1) == (int)gridDim.x - 1;
+    __threadfence();
+    *abort_flag = last && atomicOr(&a.plan->gave_up, 0) != 0;
+  }
+  __syncthreads();
+  if (*abort_flag) {
+    const T nan = from_f32<T>(NAN);
+    for (int r = warp; r < a.rows; r += kThreads / 32)
+      for (int c = lane; c < a.hidden; c += 32) static_cast<T*>(a.y)[(int64_t)r * a.ld_y + c] = nan;
+    for (int p = 0; p < 3 && a.params; ++p)
+      for (int g = 0; g < a.groups; ++g)
+        for (int r = warp; r < a.wrows[p]; r += kThreads / 32)
+          for (int c = lane; c < a.wcols[p]; c += 32)
+            static_cast<T*>(a.dw[p])[(int64_t)g * a.stride_dw[p] + (int64_t)r * a.ld_dw[p] + c] = nan;
+  }
+}
+
+// ---- before the products ----
+
+constexpr int kPrepThreads = 256;
+
+// bounds[g]: the largest of offsets[0 .. g], within 0 .. rows. All of the CTA's threads; a barrier at the end.
+__device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& bounds, bool tell) {
+  bool off = false;
+  for (int i = threadIdx.x; i <= a.groups; i += kPrepThreads) {
+    const int v = a.offsets ? a.offsets[i] : i == 0 ? 0 : a.rows;
+    off |= v < 0 || v > a.rows || (a.offsets && i > 0 && v < a.offsets[i - 1]);
+    buf[0][i] = min(max(v, 0), a.rows);
+  }
+  if (tell && off && a.status) atomicOr(a.status, kStatusRange);
+  int at = 0;
+  for (int d = 1; d <= a.groups; d *= 2, at ^= 1) {
+    __syncthreads();
+    for (int i = threadIdx.x; i <= a.groups; i += kPrepThreads) buf[at ^ 1][i] = max(buf[at][i], i >= d ? buf[at][i - d] : 0);
+  }
+  __syncthreads();
+  bounds = buf[at];
+}
+
+// The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
+// gradients of groups without rows.
+template <typename T>
+__global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
+  __shared__ int buf[2][kMaxGroups + 1];
+  int* bounds;
+  find_bounds(a, buf, bounds, blockIdx.x == 0);
+  if (blockIdx.x == 0) {
+    Plan& l = *a.plan;
+    for (int i = threadIdx.x; i < a.done_words; i += kPrepThreads) a.done_row[i] = 0;
+    for (int i = threadIdx.x; i <= a.groups; i += kPrepThreads) l.bounds[i] = bounds[i];
+    if (threadIdx.x == 0) {
+      l.next = l.through = l.gave_up = 0;
+      int tiles = 0, blocks = 0, parts = 0, slots = 0, some = 0;
+      for (int g = 0; g < a.groups; ++g) some += bounds[g + 1] > bounds[g];
+      const int each = 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256), most = some > 0 ? kUnitPairs / some / each : 0;
+      for (int g = 0; g <= a.groups; ++g) {
+        l.row_tiles[g] = tiles;
+        l.blocks[g] = blocks;
+        l.parts[g] = parts;
+        l.slots[g] = slots;
+        if (g == a.groups) break;
+        const int len = bounds[g + 1] - bounds[g], s = up_div(len, BK);
+        tiles += up_div(len, 256);
+        blocks += up_div(len, 32);
+        if (!a.params || len == 0) continue;
+        const int n = max(1, max(up_div(s, kMaxSlices), min(most, s / kMinPart)));
+        parts += n;
+        if (n > 1) slots += n;
+      }
+      int at = 0;
+      for (int p = 0; p < 2; ++p) {
+        const int n = tiles * up_div(p == 0 ? a.width : a.hidden, p == 0 && !a.backward ? 128 : 256);
+        const int k = a.kblocks[p] * (p == 1 ? a.segments : 1);
+        l.first[p] = at;
+        l.tiles[p] = n;
+        l.splits[p] = max(max(1, up_div(k, kMaxSlices)), n > 0 ? min(kUnitPairs / n, k / kMinPart) : 1);
+        at += n * l.splits[p];
+      }
+      l.first[2] = at;
+      l.total = at + parts * each;
+    }
+  }
+  if (a.clips) {
+    const CUtensorMap* const from = maps.clip;
+    for (int i = blockIdx.x * kPrepThreads + threadIdx.x; i < a.groups * kClips; i += gridDim.x * kPrepThreads) {
+      const int g = i / kClips, c = i - g * kClips;
+      if (!a.backward && c > kY) continue;
+      const uint4* src = reinterpret_cast<const uint4*>(from + c);
+      uint4* dst = reinterpret_cast<uint4*>(const_cast<CUtensorMap*>(a.clips) + i);
+#pragma unroll
+      for (int w = 0; w < 8; ++w) dst[w] = src[w];
+      // rows end with the group's (of a group without rows nothing is ever copied)
+      asm volatile("tensormap.replace.tile.global_dim.global.b1024.b32 [%0], 1, %1;" ::"l"(reinterpret_cast<uint64_t>(dst)),
+                   "r"(max(bounds[g + 1], 1))
+                   : "memory");
+      asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
+    }
+  }
+  if (!a.offsets && a.rows > 0) return;
+  const int first = bounds[0], last = bounds[a.groups];
+  const T zero = from_f32<T>(0.f);
+  for (int64_t r = blockIdx.x; r < first + (a.rows - last); r += gridDim.x) {
+    T* const row = static_cast<T*>(a.y) + (r < first ? r : r - first + last) * a.ld_y;
+    for (int c = threadIdx.x; c < a.hidden; c += kPrepThreads) row[c] = zero;
+  }
+  if (!a.params) return;
+  for (int g = 0; g < a.groups; ++g) {
+    if (bounds[g + 1] > bounds[g]) continue;
+    for (int p = 0; p < 3; ++p)
+      for (int r = blockIdx.x; r < a.wrows[p]; r += gridDim.x) {
+        T* const row = static_cast<T*>(a.dw[p]) + (int64_t)g * a.stride_dw[p] + (int64_t)r * a.ld_dw[p];
+        for (int c = threadIdx.x; c < a.wcols[p]; c += kPrepThreads) row[c] = zero;
+      }
+  }
+}
+
+template <int TYPE>
+cudaError_t launch(const Maps& maps, const Args& a, int64_t units, cudaStream_t s) {
+  // per device: the pairs that are resident at once, found (with the kernel's shared-memory attribute set) on the
+  // first launch there
+  static std::atomic<int> pairs_of[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int pairs = dev < 64 ? pairs_of[dev].load(std::memory_order_relaxed) : 0;
+  if (pairs == 0) {
+    e = cudaFuncSetAttribute(products_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    e = cudaOccupancyMaxActiveClusters(&pairs, products_kernel<TYPE>, &cfg);
+    if (e != cudaSuccess) return e;
+    if (pairs < 1) return cudaErrorLaunchOutOfResources;
+    if (dev < 64) pairs_of[dev].store(pairs, std::memory_order_relaxed);
+  }
+  cfg.gridDim = dim3((unsigned)(2 * std::max<int64_t>(1, std::min<int64_t>(pairs, units))));
+  return cudaLaunchKernelEx(&cfg, products_kernel<TYPE>, maps, a);
+}
+
+}  // namespace
+
+cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s) {
+  // dense: nothing but the plan; groups: as many CTAs as rows and gradients to zero can keep busy
+  const int ctas = a.offsets || a.rows == 0 ? 304 : 1;
+  if (type == SOAP_F32)
+    prepare_kernel<float><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+  else if (type == SOAP_BF16)
+    prepare_kernel<__nv_bfloat16><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+  else
+    prepare_kernel<__half><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+  return cudaGetLastError();
+}
+
+cudaError_t run(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s) {
+  return type == SOAP_F32    ? launch<SOAP_F32>(maps, a, units, s)
+         : type == SOAP_BF16 ? launch<SOAP_BF16>(maps, a, units, s)
+                             : launch<SOAP_F16>(maps, a, units, s);
+}
+
+}  // namespace ffn
+}  // namespace soap
