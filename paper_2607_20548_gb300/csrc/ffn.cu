@@ -69,7 +69,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   size_t words = l.row_tiles + groups;
   for (int p = 0; p < 3; ++p) {
     l.count[p] = at + words * 4;
-    words += l.slots[p] * 16;
+    words += l.slots[p] * 64;
   }
   l.done_words = words;
   take(words * 4);

@@ -41,10 +41,9 @@ struct Plan {
 
 struct Args {
   Plan* plan;
-  int *done_row, *done_group;   // stored parts of h (or dg, du and h), per row tile and per group
-  int *count[3];                // parts that are there, per warp's share of a tile, per phase
+  int *done_row, *done_group;   // stored blocks of 32 x 32 of h (or dg, du and h), per row tile and per group
+  int *count[3];                // parts that are there, per block of a tile, per phase
   float* partial[3];
-  int slots[3];                 // of partial
   const CUtensorMap* clips;     // [groups][kClips], or nullptr: those in Maps
   int backward, params;
   int groups, rows, hidden, width;

@@ -58,7 +58,13 @@ struct Unit {
   int start;         // the group's first row
   int s0, s1;        // slices
   int splits, part, slot, tile;  // parts along K; this one, its place among the partial sums, and its tile's
+  int tiles;                     // places between two parts' sums
   int row_tile, block;           // among all groups'
+  int need;                      // the group's row tiles
+};
+// The plan's numbers that every unit takes.
+struct Head {
+  int total, first[3], tiles[2], splits[2], parts;
 };
 constexpr int kSmem = 1024 + kStages * kStage + kEpiWarps * kStaging + kKept * (int)sizeof(Unit) + 256;
 static_assert(kSmem <= 232448, "shared memory");
@@ -124,14 +130,16 @@ __device__ __forceinline__ void tmem_ld16(uint32_t t, float (&v)[16]) {
       : "memory");
 }
 
-// The largest i with prefix[i] <= q.
+// The largest i < n with prefix[i] <= q; all lanes of a warp take part (one round of loads for up to 32 groups, two
+// beyond: a binary search's dependent ones took longer than a small unit).
 __device__ __forceinline__ int group_of(const int* prefix, int n, int q) {
-  int lo = 0, hi = n;  // prefix[lo] <= q < prefix[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    (prefix[mid] <= q ? lo : hi) = mid;
-  }
-  return lo;
+  const int lane = threadIdx.x & 31, step = up_div(n, 32);
+  int i = lane * step;
+  const unsigned coarse = __ballot_sync(0xffffffffu, i < n && prefix[i] <= q);
+  const int first = (31 - __clz(coarse)) * step;
+  if (step == 1) return first;
+  i = first + lane;
+  return first + 31 - __clz(__ballot_sync(0xffffffffu, lane < step && i < n && prefix[i] <= q));
 }
 
 // Tile i of nm x nn in groups of 8 row tiles, row tile fastest, so that tiles in flight share operands in L2.
@@ -141,42 +149,63 @@ __device__ __forceinline__ void tile_place(int i, int nm, int nn, int& m, int& n
   m = gr * 8 + in - n * rows;
 }
 
-__device__ __forceinline__ Unit unit_at(int p, const Args& a) {
+__device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
   const Plan& l = *a.plan;
+  const bool dense = a.clips == nullptr;  // then all prefixes are 0 and everything there is
   Unit u{};
-  const int phase = p >= l.first[2] ? 2 : p >= l.first[1] ? 1 : 0;
-  int i = p - l.first[phase];
+  const int phase = p >= h.first[2] ? 2 : p >= h.first[1] ? 1 : 0;
+  int i = p - (phase == 2 ? h.first[2] : phase == 1 ? h.first[1] : 0);
   if (phase < 2) {
     u.slot = i;
-    const int tiles = l.tiles[phase], wide = phase == 0 && !a.backward ? 128 : 256;
+    const int tiles = phase == 0 ? h.tiles[0] : h.tiles[1], wide = phase == 0 && !a.backward ? 128 : 256;
     u.N = phase == 0 ? a.width : a.hidden;
     u.kind = phase == 1 ? kOut : a.backward ? kGrad : kGated;
-    u.splits = l.splits[phase];
+    u.splits = phase == 0 ? h.splits[0] : h.splits[1];
+    u.tiles = tiles;
     u.part = i / tiles;
     i -= u.part * tiles;
     u.tile = i;
     const int nn = up_div(u.N, wide);
-    u.group = group_of(l.row_tiles, a.groups, i / nn);
-    i -= l.row_tiles[u.group] * nn;
+    int nm = up_div(a.rows, 256);
+    u.M = a.rows;
+    if (!dense) {
+      u.group = group_of(l.row_tiles, a.groups, i / nn);
+      u.row_tile = l.row_tiles[u.group];
+      nm = l.row_tiles[u.group + 1] - u.row_tile;
+      i -= u.row_tile * nn;
+      u.start = l.bounds[u.group];
+      u.M = l.bounds[u.group + 1] - u.start;
+      u.block = l.blocks[u.group];
+    }
     int m, n;
-    tile_place(i, l.row_tiles[u.group + 1] - l.row_tiles[u.group], nn, m, n);
-    u.start = l.bounds[u.group];
-    u.M = l.bounds[u.group + 1] - u.start;
+    tile_place(i, nm, nn, m, n);
+    u.need = nm;
     u.m0 = m * 256;
     u.n0 = n * wide;
-    u.row_tile = l.row_tiles[u.group] + m;
-    u.block = l.blocks[u.group] + m * 8;
+    u.row_tile += m;
+    u.block += m * 8;
     const int slices = a.kblocks[phase] * (phase == 1 ? a.segments : 1);
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   } else {
     const int nm = up_div(a.wrows[0], 256), nn = up_div(a.wcols[0], 256), each = nm * nn, q = i / (3 * each);
     u.kind = kWeight;
-    u.group = group_of(l.parts, a.groups, q);
-    u.splits = l.parts[u.group + 1] - l.parts[u.group];
-    u.part = q - l.parts[u.group];
+    u.tiles = 3 * each;
+    int rows = a.rows, slots = 0;
+    u.splits = h.parts;
+    u.part = q;
+    u.need = up_div(rows, 256);
+    if (!dense) {
+      u.group = group_of(l.parts, a.groups, q);
+      u.part = q - l.parts[u.group];
+      u.splits = l.parts[u.group + 1] - l.parts[u.group];
+      slots = l.slots[u.group];
+      u.start = l.bounds[u.group];
+      rows = l.bounds[u.group + 1] - u.start;
+      u.need = l.row_tiles[u.group + 1] - l.row_tiles[u.group];
+    }
     i -= q * 3 * each;
-    u.tile = l.slots[u.group] * 3 * each + i;
+    u.tile = slots * 3 * each + i;
     u.slot = u.tile + u.part * 3 * each;
     u.prod = i / each;
     i -= u.prod * each;
@@ -186,8 +215,7 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a) {
     tile_place(i, up_div(u.M, 256), up_div(u.N, 256), m, n);
     u.m0 = m * 256;
     u.n0 = n * 256;
-    u.start = l.bounds[u.group];
-    const int slices = up_div(l.bounds[u.group + 1] - u.start, BK);
+    const int slices = up_div(rows, BK);
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   }
@@ -254,9 +282,9 @@ __device__ __forceinline__ void issue(Ring& st, int count, uint32_t idesc, uint3
 }
 
 // act(g) and its derivative. 16-bit results: the hardware's exponential and quotient (2^-21 of the result).
-template <int TYPE>
-__device__ __forceinline__ void activation(int act, float g, float& a, float& da) {
-  if (act == LAYER_SILU) {
+template <int TYPE, int ACT>
+__device__ __forceinline__ void activation(float g, float& a, float& da) {
+  if (ACT == LAYER_SILU) {
     const float s = TYPE == SOAP_F32 ? 1.f / (1.f + expf(-g)) : __fdividef(1.f, 1.f + __expf(-g));
     a = g * s;
     da = s * fmaf(g, 1.f - s, 1.f);
@@ -265,6 +293,28 @@ __device__ __forceinline__ void activation(int act, float g, float& a, float& da
     const float e = TYPE == SOAP_F32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g);
     a = g * p;
     da = fmaf(g * 0.3989422804014327f, e, p);
+  }
+}
+// A block's rows: v = act(v) w; or, from g, u and v = dh: g = dg, u = h, v = du. One of two straight pieces of code (a
+// choice per element has the instructions of both fetched: 8 us of a small call's 55).
+template <int TYPE, int ACT>
+__device__ __forceinline__ void gate(float (&v)[32], const float (&w)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    float a, da;
+    activation<TYPE, ACT>(v[j], a, da);
+    v[j] = a * w[j];
+  }
+}
+template <int TYPE, int ACT>
+__device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    float a, da;
+    activation<TYPE, ACT>(g[j], a, da);
+    g[j] = v[j] * u[j] * da;
+    u[j] *= a;
+    v[j] *= a;
   }
 }
 
@@ -288,6 +338,28 @@ __device__ __forceinline__ float upper(float& x) {
   const float r = finite ? hi : x;
   x = finite ? x - hi : 0.f;
   return r;
+}
+
+// 32 elements of this lane's row to or from a block in which the rows' 16-byte pieces lie side by side (at p: this
+// lane's first).
+__device__ __forceinline__ void put_lines(float4* p, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+__device__ __forceinline__ void get_lines(const float4* p, float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 x = p[32 * j];
+    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
+  }
+}
+// (what other CTAs have stored meanwhile: past this SM's L1)
+__device__ __forceinline__ void get_lines_l2(const float4* p, float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 x = __ldcg(p + 32 * j);
+    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
+  }
 }
 
 __device__ __forceinline__ void fence_map(const CUtensorMap* m) {
@@ -335,6 +407,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     set_ready(given_at, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if ((warp == 0 || warp == kLoadB) && lane < 2) {
+    const CUtensorMap* const first = warp == 0 ? (lane == 0 ? &maps.a0 : &maps.a1[0])
+                                               : (lane == 0 ? &maps.w0[rank] : &maps.w1[0]);
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(first)) : "memory");
+  }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)), "r"(512));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
@@ -343,49 +420,59 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   __syncthreads();
   cluster_sync();  // both CTAs' barriers are ready
   tc_fence_after();
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch before has ended: so far, nothing of it was read
   const uint32_t tmem = *tmem_at;
 
   if (warp == kScout) {
-    if (lane == 0) {
-      bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
-      const int total = a.plan->total;
-      uint32_t peer;
-      asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at + 2)));
-      for (int m = 0; ok && !*abort_flag; ++m) {
-        int p;
+    bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
+    const Plan& l = *a.plan;
+    const Head head{l.total, {0, l.first[1], l.first[2]}, {l.tiles[0], l.tiles[1]}, {l.splits[0], l.splits[1]},
+                    a.clips ? 0 : l.parts[1]};
+    uint32_t peer;
+    asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at + 2)));
+    for (int m = 0; ok; ++m) {
+      int p = -1;
+      if (lane == 0) {
         if (rank == 0) {
-          if (!(ok = wait_given(begun_at, m, 2 * lim))) break;
-          p = atomicAdd(&a.plan->next, 1);
-          if (p >= total) p = -1;
-          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * (m % kKept)), "r"(p) : "memory");
-          asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * kKept + 12), "r"(m + 1) : "memory");
-        } else {
-          if (!(ok = wait_given(given_at, m + 1, 2 * lim))) break;
+          if ((ok = wait_given(begun_at, m, 2 * lim))) {
+            p = atomicAdd(&a.plan->next, 1);
+            if (p >= head.total) p = -1;
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * (m % kKept)), "r"(p) : "memory");
+            asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * kKept + 12), "r"(m + 1)
+                         : "memory");
+          }
+        } else if ((ok = wait_given(given_at, m + 1, 2 * lim))) {
           p = taken[m % kKept];
         }
-        Unit& u = units[m % kKept];
-        if (p < 0) {
-          u.kind = kEnd;
-        } else {
-          u = unit_at(p, a);
-        }
+        ok = ok && !*abort_flag;
+      }
+      if (!(ok = __shfl_sync(0xffffffffu, ok, 0))) break;
+      p = __shfl_sync(0xffffffffu, p, 0);
+      Unit u{};
+      if (p < 0)
+        u.kind = kEnd;
+      else
+        u = unit_at(p, a, head);
+      if (lane == 0) {
+        units[m % kKept] = u;
         set_ready(known_at, m + 1);
-        if (p >= 0) {
-          if (u.kind == kOut)
-            ok = wait_done(a.done_row + u.row_tile, kPerTile * up_div(a.width, a.backward ? 256 : 128), lim);
-          else if (u.kind == kWeight)
-            ok = wait_done(a.done_group + u.group,
-                           kPerTile * up_div(a.width, 256) * (a.plan->row_tiles[u.group + 1] - a.plan->row_tiles[u.group]), lim);
-          if (!ok) break;
+        if (u.kind == kOut)
+          ok = wait_done(a.done_row + u.row_tile, kPerTile * (a.backward ? 4 * up_div(a.width, 256) : 2 * up_div(a.width, 128)),
+                         lim);
+        else if (u.kind == kWeight)
+          ok = wait_done(a.done_group + u.group,
+                         kPerTile * 4 * up_div(a.width, 256) * u.need, lim);
+        if (ok) {
           asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
+          set_ready(ready_at, m + 1);
         }
-        set_ready(ready_at, m + 1);
-        if (p < 0) break;
       }
-      if (!ok) {
-        *abort_flag = 1;
-        if (a.status) atomicOr(a.status, kStatusTimeout);
-      }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (p < 0) break;
+    }
+    if (!ok) {
+      *abort_flag = 1;
+      if (lane == 0 && a.status) atomicOr(a.status, kStatusTimeout);
     }
   } else if (warp == 0 || warp == kLoadB) {
     if (lane == 0) {
@@ -499,7 +586,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else {
     const int q = warp & 3;           // accumulator lanes 32 q .. 32 q + 31
-    const int half = (warp - 2) / 4;  // its columns: of g and u 64 each, else 128
+    const int half = (warp - 2) / 4;  // of the columns
     uint8_t* stage = staging + (warp - 2) * kStaging;
     constexpr int kSlot = SPLIT ? 4096 : 2048, kSlots = kStaging / kSlot;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16);
@@ -524,11 +611,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const Unit u = units[m % kKept];
       if (u.kind == kEnd) break;
       const int r0 = u.m0 + rank * 128 + 32 * q;
-      const int c0 = u.kind == kGated ? u.n0 + 64 * half : u.n0 + 128 * half, cs = u.kind == kGated ? 32 : 64;
-      // none below the last row, and to the last column
-      const int blocks = r0 < u.M && c0 < u.N ? min(2, (u.N - c0 + cs - 1) / cs) : 0;
-      const uint32_t t0 = lanes + (u.kind == kGated ? 64 * half : 128 * half);
-      const uint32_t t_step = u.kind == kGated ? 32 : 64, t_second = u.kind == kGated ? 128 : 32;
+      // its columns in blocks of 32 (of g and u 64 each, else 128): none below the last row, and to the last column
+      const bool gated = u.kind == kGated;
+      const int most = gated ? 2 : 4, c0 = u.n0 + 32 * most * half;
+      const int blocks = r0 < u.M && c0 < u.N ? min(most, (u.N - c0 + 31) / 32) : 0;
+      const uint32_t t0 = lanes + 32 * most * half;
       const CUtensorMap* const clips = a.clips ? a.clips + u.group * kClips : maps.clip;
       if (a.clips && lane == 0) {
         if (u.kind <= kGrad) fence_map(clips + kH);
@@ -553,7 +640,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       };
       auto to_result = [&](const float (&v)[32], int col) {
-        if (col >= u.N) return;
         uint8_t* const slot = next_slot();
         const bool weight = u.kind == kWeight;
         if (weight ? a.dw_tma[u.prod] : a.y_tma) {
@@ -574,92 +660,70 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       };
       auto pre_at = [&](int which, int col) {
         return reinterpret_cast<float4*>(a.pre) +
-               ((((int64_t)u.block + r0 / 32 - u.m0 / 32) * 2 + which) * pre_cols + col / 32) * 256 + lane;
+               ((((int64_t)u.block + (r0 - u.m0) / 32) * 2 + which) * pre_cols + col / 32) * 256 + lane;
       };
-      // block i of the tile: two times 32 columns
-      auto finish = [&](int i, float (&v)[32], float (&w)[32]) {
-        if (u.kind == kGated) {
-          const int col = c0 + 32 * i;
-          if (a.pre) {
-            float4 *pg = pre_at(0, col), *pu = pre_at(1, col);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              pg[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-              pu[32 * j] = make_float4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float act, slope;
-            activation<TYPE>(a.act, v[j], act, slope);
-            v[j] = act * w[j];
-          }
-          to_operand(kH, v, col);
-        } else if (u.kind == kGrad) {
-          auto part = [&](float (&dh)[32], int col) {
-            if (col >= u.N) return;
-            const float4 *pg = pre_at(0, col), *pu = pre_at(1, col);
-            float g[32], up[32];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float4 x = pg[32 * j], y = pu[32 * j];
-              g[4 * j] = x.x, g[4 * j + 1] = x.y, g[4 * j + 2] = x.z, g[4 * j + 3] = x.w;
-              up[4 * j] = y.x, up[4 * j + 1] = y.y, up[4 * j + 2] = y.z, up[4 * j + 3] = y.w;
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              float act, slope;
-              activation<TYPE>(a.act, g[j], act, slope);
-              g[j] = dh[j] * up[j] * slope;  // dg
-              up[j] = act * up[j];           // h
-              dh[j] *= act;                  // du
-            }
-            to_operand(kDG, g, col);
-            to_operand(kDU, dh, col);
-            if (a.params) to_operand(kH, up, col);
-          };
-          part(v, c0 + 64 * i);
-          part(w, c0 + 64 * i + 32);
-        } else {
-          to_result(v, c0 + 64 * i);
-          to_result(w, c0 + 64 * i + 32);
+      // block i of g and u
+      auto finish_gated = [&](int i, float (&v)[32], float (&w)[32]) {
+        const int col = c0 + 32 * i;
+        if (a.pre) {
+          put_lines(pre_at(0, col), v);
+          put_lines(pre_at(1, col), w);
         }
+        if (a.act == LAYER_SILU)
+          gate<TYPE, LAYER_SILU>(v, w);
+        else
+          gate<TYPE, LAYER_GELU>(v, w);
+        to_operand(kH, v, col);
       };
+      // block i of any other product
+      auto finish = [&](int i, float (&v)[32]) {
+        const int col = c0 + 32 * i;
+        if (u.kind != kGrad) {
+          to_result(v, col);
+          return;
+        }
+        float g[32], up[32];
+        get_lines(pre_at(0, col), g);
+        get_lines(pre_at(1, col), up);
+        if (a.act == LAYER_SILU)
+          gate_back<TYPE, LAYER_SILU>(g, up, v);
+        else
+          gate_back<TYPE, LAYER_GELU>(g, up, v);
+        to_operand(kDG, g, col);
+        to_operand(kDU, v, col);
+        if (a.params) to_operand(kH, up, col);
+      };
+      // Parts along K: each stores its sums, and the one that is the last to store a block adds up all of them in the
+      // parts' order. A part begins with a block of its own, so that parts that end together finish different blocks.
       const int phase = u.kind == kWeight ? 2 : u.kind == kOut;
-      auto partial_at = [&](int slot, int i) {
+      const int share = rank * kEpiWarps + warp - 2;
+      auto partial_at = [&](int part, int i) {
         return reinterpret_cast<float4*>(a.partial[phase]) +
-               (((int64_t)slot * kPerTile + rank * kEpiWarps + warp - 2) * 4 + 2 * i) * 256 + lane;
+               (((int64_t)(u.slot + (part - u.part) * u.tiles) * kPerTile + share) * 4 + i) * 256 + lane;
       };
-      auto put_partial = [&](int i, const float (&v)[32], const float (&w)[32]) {
-        float4* p = partial_at(u.slot, i);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          p[256 + 32 * j] = make_float4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-        }
-      };
-      // whether this part is the tile's last; then the sums are formed, in the parts' order
-      auto last_part = [&]() {
+      auto last_part = [&](int i) {
         __threadfence();
         __syncwarp();
         int there = 0;
-        if (lane == 0) there = atomicAdd(a.count[phase] + u.tile * kPerTile + rank * kEpiWarps + warp - 2, 1);
+        if (lane == 0) there = atomicAdd(a.count[phase] + (u.tile * kPerTile + share) * 4 + i, 1);
         __threadfence();
         return __shfl_sync(0xffffffffu, there, 0) == u.splits - 1;
       };
-      const int tiles = phase < 2 ? a.plan->tiles[phase] : 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256);
-      auto get_partial = [&](int i, float (&v)[32], float (&w)[32]) {
-        const int slot0 = u.slot - u.part * tiles;
+      auto add_parts = [&](int i, float (&v)[32]) {
+        get_lines_l2(partial_at(0, i), v);
+        int s = 1;
+        for (; s + 1 < u.splits; s += 2) {  // (two on their way at a time)
+          float x[32], y[32];
+          get_lines_l2(partial_at(s, i), x);
+          get_lines_l2(partial_at(s + 1, i), y);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = w[j] = 0.f;
-        for (int s = 0; s < u.splits; ++s) {
-          const float4* p = partial_at(slot0 + s * tiles, i);
+          for (int j = 0; j < 32; ++j) v[j] = (v[j] + x[j]) + y[j];
+        }
+        if (s < u.splits) {
+          float x[32];
+          get_lines_l2(partial_at(s, i), x);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float4 x = __ldcg(p + 32 * j), y = __ldcg(p + 256 + 32 * j);
-            v[4 * j] += x.x, v[4 * j + 1] += x.y, v[4 * j + 2] += x.z, v[4 * j + 3] += x.w;
-            w[4 * j] += y.x, w[4 * j + 1] += y.y, w[4 * j + 2] += y.z, w[4 * j + 3] += y.w;
-          }
+          for (int j = 0; j < 32; ++j) v[j] += x[j];
         }
       };
       auto wait_acc = [&](int ac) {
@@ -673,32 +737,62 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0)
           asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_leader(&acc_empty[ac])) : "memory");
       };
+      // stored: what waits for these blocks may go on
+      auto report = [&](int count) {
+        if (u.kind <= kGrad && lane == 0 && count > 0) {
+          sent_done<0>();
+          asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_row + u.row_tile), "r"(count) : "memory");
+          asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_group + u.group), "r"(count) : "memory");
+        }
+      };
+      const int turn = u.splits > 1 && blocks > 0 ? u.part % blocks : 0;
+      auto turned = [&](int i) { return i + turn < blocks ? i + turn : i + turn - blocks; };
+      int finished = most - blocks;  // (blocks that hold nothing count for the first part)
+      if (u.part > 0) finished = 0;
       if constexpr (!SPLIT) {
         const int ac = n & 1;
         if (!wait_acc(ac)) break;
+        const uint32_t t = t0 + static_cast<uint32_t>(ac * 256);
         if (blocks == 0) release_acc(ac);
-        for (int i = 0; i < blocks; ++i) {
-          float v[32], w[32];
-          const uint32_t t = t0 + static_cast<uint32_t>(ac * 256) + i * t_step;
-          tmem_ld32x2(t, t + t_second, v, w);
-          if (i + 1 == blocks) release_acc(ac);
-          if (u.splits == 1)
-            finish(i, v, w);
-          else
-            put_partial(i, v, w);
+        for (int j = 0; j < blocks; ++j) {
+          const int i = turned(j);
+          float v[32];
+          if (gated) {
+            float w[32];
+            tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
+            if (j + 1 == blocks) release_acc(ac);
+            if (u.splits > 1) {
+              put_lines(partial_at(u.part, 2 * i), v);
+              put_lines(partial_at(u.part, 2 * i + 1), w);
+              if (!last_part(i)) continue;
+              add_parts(2 * i, v);
+              add_parts(2 * i + 1, w);
+            }
+            finish_gated(i, v, w);
+          } else {
+            tmem_ld32(t + 32 * i, v);
+            if (j + 1 == blocks) release_acc(ac);
+            if (u.splits > 1) {
+              put_lines(partial_at(u.part, i), v);
+              if (!last_part(i)) continue;
+              add_parts(i, v);
+            }
+            finish(i, v);
+          }
+          ++finished;
         }
         ++n;
       } else {
-        float sum[4][32];
+        float sum[4][32];  // of g and u: blocks 0 and 1 of g, of u
         bool begun = false;
         for (int kb = u.s0; kb < u.s1; kb = O::end_of_run(kb, u.s1), ++n) {
           const int ac = n & 1;
           if (!wait_acc(ac)) break;
 #pragma unroll
           for (int b = 0; b < 8; ++b)
-            if (b / 4 < blocks) {
+            if (gated ? (b / 2 & 1) < blocks : b / 2 < blocks) {
               float v[16];
-              tmem_ld16(t0 + static_cast<uint32_t>(ac * 256) + b / 4 * t_step + (b / 2 & 1) * t_second + (b & 1) * 16, v);
+              tmem_ld16(t0 + static_cast<uint32_t>(ac * 256) + (gated && b >= 4 ? 128 + 16 * (b - 4) : 16 * b), v);
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
                 float& x = sum[b / 2][(b & 1) * 16 + j];
@@ -709,30 +803,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           begun = true;
         }
         if (!ok) break;
+        if (u.splits > 1) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (i < blocks) {
-            if (u.splits == 1)
-              finish(i, sum[2 * i], sum[2 * i + 1]);
-            else
-              put_partial(i, sum[2 * i], sum[2 * i + 1]);
+          for (int b = 0; b < 4; ++b) {
+            if (gated ? (b & 1) < blocks : b < blocks) put_lines(partial_at(u.part, gated ? 2 * (b & 1) + b / 2 : b), sum[b]);
           }
-      }
-      bool done = true;
-      if (u.splits > 1) {
-        done = blocks == 0 ? u.part == 0 : last_part();
-        if (done)
-          for (int i = 0; i < blocks; ++i) {
-            float v[32], w[32];
-            get_partial(i, v, w);
-            finish(i, v, w);
+          for (int j = 0; j < blocks; ++j) {
+            const int i = turned(j);
+            if (!last_part(i)) continue;
+            float v[32];
+            add_parts(gated ? 2 * i : i, v);
+            if (gated) {
+              float w[32];
+              add_parts(2 * i + 1, w);
+              finish_gated(i, v, w);
+            } else {
+              finish(i, v);
+            }
+            ++finished;
           }
+        } else {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            if (b >= blocks) break;
+            if (gated) {
+              if (b < 2) finish_gated(b, sum[b], sum[b + 2]);
+            } else {
+              finish(b, sum[b]);
+            }
+            ++finished;
+          }
+        }
       }
-      if (done && u.kind <= kGrad && lane == 0) {  // stored: what waits for it may go on
-        sent_done<0>();
-        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.done_row + u.row_tile) : "memory");
-        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.done_group + u.group) : "memory");
-      }
+      report(finished);
       __syncwarp();
     }
     if (lane == 0) sent_done<0>();
@@ -793,47 +896,66 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
   bounds = buf[at];
 }
 
+// Parts along K of a tile of `slices` slices (0: none), where there may be `most` for the pairs' sake: a part of p
+// costs its slices' time, 0.3 us each, and adding up p parts about as much for each, least at p = sqrt(slices).
+__device__ __forceinline__ int parts_of(int slices, int most) {
+  if (slices == 0) return 0;
+  return max(max(1, up_div(slices, kMaxSlices)), min(most, min(slices / kMinPart, (int)sqrtf((float)slices))));
+}
+
 // The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
 // gradients of groups without rows.
 template <typename T>
 __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
   __shared__ int buf[2][kMaxGroups + 1];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the products' CTAs set themselves up meanwhile
   int* bounds;
   find_bounds(a, buf, bounds, blockIdx.x == 0);
   if (blockIdx.x == 0) {
     Plan& l = *a.plan;
     for (int i = threadIdx.x; i < a.done_words; i += kPrepThreads) a.done_row[i] = 0;
     for (int i = threadIdx.x; i <= a.groups; i += kPrepThreads) l.bounds[i] = bounds[i];
-    if (threadIdx.x == 0) {
-      l.next = l.through = l.gave_up = 0;
-      int tiles = 0, blocks = 0, parts = 0, slots = 0, some = 0;
-      for (int g = 0; g < a.groups; ++g) some += bounds[g + 1] > bounds[g];
+    if (threadIdx.x < 32) {
+      const int lane = threadIdx.x;
+      auto length = [&](int g) { return g < a.groups ? bounds[g + 1] - bounds[g] : 0; };
+      int some = 0;
+      for (int g = 0; g < a.groups; g += 32) some += __popc(__ballot_sync(0xffffffffu, length(g + lane) > 0));
       const int each = 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256), most = some > 0 ? kUnitPairs / some / each : 0;
-      for (int g = 0; g <= a.groups; ++g) {
-        l.row_tiles[g] = tiles;
-        l.blocks[g] = blocks;
-        l.parts[g] = parts;
-        l.slots[g] = slots;
-        if (g == a.groups) break;
-        const int len = bounds[g + 1] - bounds[g], s = up_div(len, BK);
-        tiles += up_div(len, 256);
-        blocks += up_div(len, 32);
-        if (!a.params || len == 0) continue;
-        const int n = max(1, max(up_div(s, kMaxSlices), min(most, s / kMinPart)));
-        parts += n;
-        if (n > 1) slots += n;
+      int tiles = 0, blocks = 0, parts = 0, slots = 0;  // of the groups before
+      for (int g0 = 0; g0 <= a.groups; g0 += 32) {
+        const int g = g0 + lane, len = length(g);
+        const int n = a.params ? parts_of(up_div(len, BK), most) : 0;
+        int4 v = make_int4(up_div(len, 256), up_div(len, 32), n, n > 1 ? n : 0);
+        const int4 own = v;
+        for (int d = 1; d < 32; d *= 2) {
+          const int4 o = make_int4(__shfl_up_sync(0xffffffffu, v.x, d), __shfl_up_sync(0xffffffffu, v.y, d),
+                                   __shfl_up_sync(0xffffffffu, v.z, d), __shfl_up_sync(0xffffffffu, v.w, d));
+          if (lane >= d) v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        if (g <= a.groups) {
+          l.row_tiles[g] = tiles + v.x - own.x;
+          l.blocks[g] = blocks + v.y - own.y;
+          l.parts[g] = parts + v.z - own.z;
+          l.slots[g] = slots + v.w - own.w;
+        }
+        tiles += __shfl_sync(0xffffffffu, v.x, 31);
+        blocks += __shfl_sync(0xffffffffu, v.y, 31);
+        parts += __shfl_sync(0xffffffffu, v.z, 31);
+        slots += __shfl_sync(0xffffffffu, v.w, 31);
       }
-      int at = 0;
-      for (int p = 0; p < 2; ++p) {
-        const int n = tiles * up_div(p == 0 ? a.width : a.hidden, p == 0 && !a.backward ? 128 : 256);
-        const int k = a.kblocks[p] * (p == 1 ? a.segments : 1);
-        l.first[p] = at;
-        l.tiles[p] = n;
-        l.splits[p] = max(max(1, up_div(k, kMaxSlices)), n > 0 ? min(kUnitPairs / n, k / kMinPart) : 1);
-        at += n * l.splits[p];
+      if (lane == 0) {
+        l.next = l.through = l.gave_up = 0;
+        int at = 0;
+        for (int p = 0; p < 2; ++p) {
+          const int n = tiles * up_div(p == 0 ? a.width : a.hidden, p == 0 && !a.backward ? 128 : 256);
+          l.first[p] = at;
+          l.tiles[p] = n;
+          l.splits[p] = n > 0 ? parts_of(a.kblocks[p] * (p == 1 ? a.segments : 1), kUnitPairs / n) : 1;
+          at += n * l.splits[p];
+        }
+        l.first[2] = at;
+        l.total = at + parts * each;
       }
-      l.first[2] = at;
-      l.total = at + parts * each;
     }
   }
   if (a.clips) {
@@ -883,10 +1005,12 @@ cudaError_t launch(const Maps& maps, const Args& a, int64_t units, cudaStream_t 
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int pairs = dev < 64 ? pairs_of[dev].load(std::memory_order_relaxed) : 0;
@@ -899,6 +1023,7 @@ cudaError_t launch(const Maps& maps, const Args& a, int64_t units, cudaStream_t 
     if (dev < 64) pairs_of[dev].store(pairs, std::memory_order_relaxed);
   }
   cfg.gridDim = dim3((unsigned)(2 * std::max<int64_t>(1, std::min<int64_t>(pairs, units))));
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, products_kernel<TYPE>, maps, a);
 }
 
