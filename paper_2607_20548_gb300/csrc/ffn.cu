@@ -33,6 +33,21 @@ bool bad_sizes(int64_t rows, int64_t hidden, int64_t width, int32_t groups, int3
          groups > kMaxGroups || type < SOAP_F32 || type > SOAP_F16;
 }
 
+// Rows as the products' columns (ffn_few.cu) or rows. Measured, bf16 forward: dense 2048 x 8192 with 24, 64, 96 rows 36,
+// 42, 50 us as columns, 48, 45, 46 as rows; 64 groups of 2048 x 768 with 3, 32, 64, 94, 128 rows each 99, 105, 111, 118,
+// 127 and 114 (16 rows), 116, 119, 121, 124.
+bool few_rows(int64_t rows, int groups, int type, bool backward) {
+  return !backward && type != SOAP_F32 && rows <= 64 * (int64_t)groups;
+}
+
+Tiles tiles_of(int64_t rows, int groups, int type, bool backward) {
+  if (!few_rows(rows, groups, type, backward)) return Tiles{256, {backward ? 256 : 128, 256}, kSms / 2, 256 * 256, 64};
+  const int64_t each = groups == 1 ? rows : (rows + rows / 2) / groups;
+  int n = 16;
+  while (n < each && n < 128) n *= 2;
+  return Tiles{n, {64, 128}, kSms, 128 * n, 4 * std::max(1, n / 32)};
+}
+
 // Where everything lies in the workspace.
 struct Layout {
   int64_t row_tiles;              // at most
@@ -44,15 +59,16 @@ struct Layout {
 
 Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool copies, bool backward) {
   Layout l{};
+  const Tiles t = tiles_of(rows, groups, type, backward);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
     at += up256(bytes);
     return was;
   };
-  l.row_tiles = rows / 256 + std::min<int64_t>(groups, rows);
-  l.tiles[0] = l.row_tiles * up_div(width, backward ? 256 : 128);
-  l.tiles[1] = l.row_tiles * up_div(hidden, 256);
+  l.row_tiles = rows / t.rows + std::min<int64_t>(groups, rows);
+  l.tiles[0] = l.row_tiles * up_div(width, t.cols[0]);
+  l.tiles[1] = l.row_tiles * up_div(hidden, t.cols[1]);
   const int64_t each = 3 * (int64_t)up_div(width, 256) * up_div(hidden, 256);
   l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
   const int64_t slices[3] = {up_div(hidden, 64), (backward ? 2 : 1) * (int64_t)up_div(width, 64), up_div(rows, 64)};
@@ -61,7 +77,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
     l.units += l.tiles[p] * std::max(parts, longest);
     // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights'
     // gradients: of groups with more than kMaxSlices slices, less than three parts for each such run of all rows)
-    l.slots[p] = parts > 1 ? std::min<int64_t>(kUnitPairs, l.tiles[p] * parts) : 0;
+    l.slots[p] = parts > 1 ? std::min<int64_t>(t.pool, l.tiles[p] * parts) : 0;
     if (longest > 1) l.slots[p] += p < 2 ? l.tiles[p] * longest : 3 * longest * each;
   }
   l.plan = take(sizeof(Plan));
@@ -69,12 +85,12 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   size_t words = l.row_tiles + groups;
   for (int p = 0; p < 3; ++p) {
     l.count[p] = at + words * 4;
-    words += l.slots[p] * 64;
+    words += l.slots[p] * t.blocks;
   }
   l.done_words = words;
   take(words * 4);
   l.clips = take((size_t)groups * kClips * sizeof(CUtensorMap));
-  for (int p = 0; p < 3; ++p) l.partial[p] = take((size_t)l.slots[p] * kPartial * 4);
+  for (int p = 0; p < 3; ++p) l.partial[p] = take((size_t)l.slots[p] * t.partial * 4);
   const size_t planes = type == SOAP_F32 ? 3 : 1;
   l.inter_plane = (size_t)rows * up8(width);
   for (int i = 0; i < (backward ? 3 : 1); ++i) l.inter[i] = take(planes * l.inter_plane * 2);
@@ -240,7 +256,17 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     a.count[p] = reinterpret_cast<int*>(c.ws + l.count[p]);
     a.partial[p] = reinterpret_cast<float*>(c.ws + l.partial[p]);
   }
-  a.clips = c.offsets && c.rows > 0 ? reinterpret_cast<const CUtensorMap*>(c.ws + l.clips) : nullptr;
+  const Tiles t = tiles_of(c.rows, c.groups, c.type, c.backward);
+  const bool few = few_rows(c.rows, c.groups, c.type, c.backward);
+  a.row_tile = t.rows;
+  a.col_tile[0] = t.cols[0];
+  a.col_tile[1] = t.cols[1];
+  a.pool = t.pool;
+  if (few) {
+    a.h = c.ws + l.inter[0];
+    a.ld_h = up8(c.width);
+  }
+  a.clips = c.offsets && c.rows > 0 && !few ? reinterpret_cast<const CUtensorMap*>(c.ws + l.clips) : nullptr;
   a.backward = c.backward;
   a.params = grads[0] != nullptr;
   a.groups = c.groups;
@@ -277,15 +303,16 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     View inter[3];
     for (int i = 0; i < 3; ++i)
       inter[i] = View{c.ws + l.inter[i], c.rows, up8(c.width), (int64_t)l.inter_plane, c.width, planes};
-    bool ok = make_map(&maps.a0, v[c.backward ? 1 : 0], etype, 64, 128) &&
-              make_map(&maps.a1[0], inter[c.backward ? 1 : 0], etype, 64, 128) &&
-              make_map(&maps.a1[1], inter[c.backward ? 2 : 0], etype, 64, 128);
+    const int box = few ? t.rows : 128;
+    bool ok = make_map(&maps.a0, v[c.backward ? 1 : 0], etype, 64, box) &&
+              make_map(&maps.a1[0], inter[c.backward ? 1 : 0], etype, 64, box) &&
+              (!c.backward || make_map(&maps.a1[1], inter[2], etype, 64, box));
     for (int i = 0; i < 2; ++i) {
-      ok = ok && make_map(&maps.w0[i], v[c.backward ? 4 : 2 + i], etype, 64, a.b_columns[0] ? 64 : 128) &&
-           make_map(&maps.w1[i], v[c.backward ? 2 + i : 4], etype, 64, a.b_columns[1] ? 64 : 128);
+      ok = ok && make_map(&maps.w0[i], v[c.backward ? 4 : 2 + i], etype, 64, few || a.b_columns[0] ? 64 : 128) &&
+           ((i == 1 && !c.backward) || make_map(&maps.w1[i], v[c.backward ? 2 + i : 4], etype, 64, few || a.b_columns[1] ? 64 : 128));
     }
-    ok = ok && make_map(&maps.clip[kH], inter[0], etype, 32, 32);
-    a.y_tma = units_of_16(y, ld_y, 0, size);
+    a.y_tma = !few && units_of_16(y, ld_y, 0, size);
+    if (!few) ok = ok && make_map(&maps.clip[kH], inter[0], etype, 32, 32);
     if (a.y_tma) ok = ok && make_map(&maps.clip[kY], View{y, c.rows, ld_y, 0, c.hidden, 1}, c.type, 32, 32);
     if (c.backward) {
       ok = ok && make_map(&maps.clip[kDG], inter[1], etype, 32, 32) && make_map(&maps.clip[kDU], inter[2], etype, 32, 32) &&
@@ -320,7 +347,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  return run(maps, a, c.type, l.units, s);
+  return few ? run_few(maps, a, c.type, l.units, s) : run(maps, a, c.type, l.units, s);
 }
 
 }  // namespace

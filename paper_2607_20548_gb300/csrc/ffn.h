@@ -9,9 +9,8 @@ namespace soap {
 namespace ffn {
 
 constexpr int kMaxGroups = 1024;
-constexpr int kUnitPairs = 76;      // pairs of CTAs that a product's parts are shared out among
+constexpr int kSms = 152;           // that a product's parts are shared out among, one or a pair for each
 constexpr int kMaxSlices = 1024;    // most slices of 64 products that one accumulator adds up
-constexpr int kPartial = 256 * 256; // fp32 elements of a part's sums
 
 // Maps that end at a group's last row, so that loads of its rows give 0 beyond it and stores leave the rows behind it
 // alone: results (boxes of 32 x 32) and factors of the weights' gradients (boxes of 64 x 64).
@@ -26,6 +25,12 @@ struct Maps {
   CUtensorMap clip[kClips]; // dense: up to the last row; groups: what their own are made from
 };
 
+// Tiles of a call: rows, columns of the first and of the second phase; units at a time; of a part's sums the fp32
+// elements and the blocks that are counted.
+struct Tiles {
+  int rows, cols[2], pool, partial, blocks;
+};
+
 // What is made on the device before the products run.
 struct Plan {
   int next, through, gave_up;  // the list's next place; CTAs that are through; whether a wait gave up
@@ -33,7 +38,7 @@ struct Plan {
   int first[3];                // of the phases
   int tiles[2], splits[2];     // of the row phases
   int bounds[kMaxGroups + 1];  // the groups' rows
-  int row_tiles[kMaxGroups + 1];  // tiles of 256 rows before each group
+  int row_tiles[kMaxGroups + 1];  // tiles of rows before each group
   int blocks[kMaxGroups + 1];     // blocks of 32 rows before each group
   int parts[kMaxGroups + 1];      // parts along the rows (of the weights' gradients) before each group
   int slots[kMaxGroups + 1];      // of them those of groups with more than one
@@ -44,9 +49,12 @@ struct Args {
   int *done_row, *done_group;   // stored blocks of 32 x 32 of h (or dg, du and h), per row tile and per group
   int *count[3];                // parts that are there, per block of a tile, per phase
   float* partial[3];
-  const CUtensorMap* clips;     // [groups][kClips], or nullptr: those in Maps
+  const CUtensorMap* clips;     // [groups][kClips], or nullptr: those in Maps (dense, few rows)
   int backward, params;
   int groups, rows, hidden, width;
+  int row_tile, col_tile[2], pool;
+  void* h;                      // few rows: where the first phase's results go
+  int64_t ld_h;
   int b_columns[2];             // whether the second factor of a row phase has its K dimension outermost
   int kblocks[2], segments;     // slices per factor pair; pairs of the second phase
   int wa[3], wb[3];             // Clip of the factors of the weights' gradients
@@ -68,6 +76,8 @@ struct Args {
 
 // type: soap_dtype_t. units: no more than this many are ever in the list.
 cudaError_t run(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s);
+// The same for few rows of 16-bit types, forward.
+cudaError_t run_few(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s);
 // The plan, the groups' maps, zeros for rows of no group and for the gradients of groups without rows.
 cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s);
 

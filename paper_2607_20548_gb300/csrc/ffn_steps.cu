@@ -28,6 +28,7 @@
 
 #include "../../include/layer.h"
 #include "ffn.h"
+#include "ffn_device.h"
 #include "pair.h"
 #include "profile.h"
 #include "soap_internal.h"
@@ -62,27 +63,8 @@ struct Unit {
   int row_tile, block;           // among all groups'
   int need;                      // the group's row tiles
 };
-// The plan's numbers that every unit takes.
-struct Head {
-  int total, first[3], tiles[2], splits[2], parts;
-};
 constexpr int kSmem = 1024 + kStages * kStage + kEpiWarps * kStaging + kKept * (int)sizeof(Unit) + 256;
 static_assert(kSmem <= 232448, "shared memory");
-
-template <int TYPE>
-struct Element;
-template <>
-struct Element<SOAP_F32> {
-  using T = float;
-};
-template <>
-struct Element<SOAP_BF16> {
-  using T = __nv_bfloat16;
-};
-template <>
-struct Element<SOAP_F16> {
-  using T = __half;
-};
 
 // kind::f16, M = N = 256: D = f32, A and B bf16 or f16; bits 15 and 16 mark MN-major operands.
 __host__ __device__ constexpr uint32_t idesc_16(bool bf16, int a_mn, int b_mn) {
@@ -128,25 +110,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t t, float (&v)[16]) {
         "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
       : "r"(t)
       : "memory");
-}
-
-// The largest i < n with prefix[i] <= q; all lanes of a warp take part (one round of loads for up to 32 groups, two
-// beyond: a binary search's dependent ones took longer than a small unit).
-__device__ __forceinline__ int group_of(const int* prefix, int n, int q) {
-  const int lane = threadIdx.x & 31, step = up_div(n, 32);
-  int i = lane * step;
-  const unsigned coarse = __ballot_sync(0xffffffffu, i < n && prefix[i] <= q);
-  const int first = (31 - __clz(coarse)) * step;
-  if (step == 1) return first;
-  i = first + lane;
-  return first + 31 - __clz(__ballot_sync(0xffffffffu, lane < step && i < n && prefix[i] <= q));
-}
-
-// Tile i of nm x nn in groups of 8 row tiles, row tile fastest, so that tiles in flight share operands in L2.
-__device__ __forceinline__ void tile_place(int i, int nm, int nn, int& m, int& n) {
-  const int of8 = 8 * nn, gr = i / of8, in = i - gr * of8, rows = min(8, nm - gr * 8);
-  n = in / rows;
-  m = gr * 8 + in - n * rows;
 }
 
 __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
@@ -281,43 +244,6 @@ __device__ __forceinline__ void issue(Ring& st, int count, uint32_t idesc, uint3
   }
 }
 
-// act(g) and its derivative. 16-bit results: the hardware's exponential and quotient (2^-21 of the result).
-template <int TYPE, int ACT>
-__device__ __forceinline__ void activation(float g, float& a, float& da) {
-  if (ACT == LAYER_SILU) {
-    const float s = TYPE == SOAP_F32 ? 1.f / (1.f + expf(-g)) : __fdividef(1.f, 1.f + __expf(-g));
-    a = g * s;
-    da = s * fmaf(g, 1.f - s, 1.f);
-  } else {
-    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-    const float e = TYPE == SOAP_F32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g);
-    a = g * p;
-    da = fmaf(g * 0.3989422804014327f, e, p);
-  }
-}
-// A block's rows: v = act(v) w; or, from g, u and v = dh: g = dg, u = h, v = du. One of two straight pieces of code (a
-// choice per element has the instructions of both fetched: 8 us of a small call's 55).
-template <int TYPE, int ACT>
-__device__ __forceinline__ void gate(float (&v)[32], const float (&w)[32]) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    float a, da;
-    activation<TYPE, ACT>(v[j], a, da);
-    v[j] = a * w[j];
-  }
-}
-template <int TYPE, int ACT>
-__device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    float a, da;
-    activation<TYPE, ACT>(g[j], a, da);
-    g[j] = v[j] * u[j] * da;
-    u[j] *= a;
-    v[j] *= a;
-  }
-}
-
 // Rounds v into this lane's row of a staged block of 32 x 32.
 template <typename T>
 __device__ __forceinline__ void put(uint8_t* slot, const float (&v)[32], int lane) {
@@ -338,28 +264,6 @@ __device__ __forceinline__ float upper(float& x) {
   const float r = finite ? hi : x;
   x = finite ? x - hi : 0.f;
   return r;
-}
-
-// 32 elements of this lane's row to or from a block in which the rows' 16-byte pieces lie side by side (at p: this
-// lane's first).
-__device__ __forceinline__ void put_lines(float4* p, const float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) p[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-}
-__device__ __forceinline__ void get_lines(const float4* p, float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float4 x = p[32 * j];
-    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
-  }
-}
-// (what other CTAs have stored meanwhile: past this SM's L1)
-__device__ __forceinline__ void get_lines_l2(const float4* p, float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float4 x = __ldcg(p + 32 * j);
-    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
-  }
 }
 
 __device__ __forceinline__ void fence_map(const CUtensorMap* m) {
@@ -920,12 +824,12 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       auto length = [&](int g) { return g < a.groups ? bounds[g + 1] - bounds[g] : 0; };
       int some = 0;
       for (int g = 0; g < a.groups; g += 32) some += __popc(__ballot_sync(0xffffffffu, length(g + lane) > 0));
-      const int each = 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256), most = some > 0 ? kUnitPairs / some / each : 0;
+      const int each = 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256), most = some > 0 ? a.pool / some / each : 0;
       int tiles = 0, blocks = 0, parts = 0, slots = 0;  // of the groups before
       for (int g0 = 0; g0 <= a.groups; g0 += 32) {
         const int g = g0 + lane, len = length(g);
         const int n = a.params ? parts_of(up_div(len, BK), most) : 0;
-        int4 v = make_int4(up_div(len, 256), up_div(len, 32), n, n > 1 ? n : 0);
+        int4 v = make_int4(up_div(len, a.row_tile), up_div(len, 32), n, n > 1 ? n : 0);
         const int4 own = v;
         for (int d = 1; d < 32; d *= 2) {
           const int4 o = make_int4(__shfl_up_sync(0xffffffffu, v.x, d), __shfl_up_sync(0xffffffffu, v.y, d),
@@ -947,10 +851,11 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
         l.next = l.through = l.gave_up = 0;
         int at = 0;
         for (int p = 0; p < 2; ++p) {
-          const int n = tiles * up_div(p == 0 ? a.width : a.hidden, p == 0 && !a.backward ? 128 : 256);
+          const int n = tiles * up_div(p == 0 ? a.width : a.hidden, a.col_tile[p]);
           l.first[p] = at;
           l.tiles[p] = n;
-          l.splits[p] = n > 0 ? parts_of(a.kblocks[p] * (p == 1 ? a.segments : 1), kUnitPairs / n) : 1;
+          l.splits[p] = n > 0 ? parts_of(a.kblocks[p] * (p == 1 ? a.segments : 1), a.pool / n) : 1;
+          if (p == 0 && a.h) l.splits[p] = 1;  // (few rows: g and u meet in the tile)
           at += n * l.splits[p];
         }
         l.first[2] = at;
