@@ -272,61 +272,80 @@ def route_backward(logits: torch.Tensor, routing: Routing, dgates: Optional[torc
     return dz
 
 
-def _heads(name, t, dtype, dev):
-    """(tensor, layer_heads, lead shape, batch, length, heads, dim) of [..., heads, dim]: [heads, dim], [length, heads,
-    dim] or [batch, length, heads, dim] where it lies; a copy of more leading dimensions that do not merge, or of
-    heads whose elements lie apart."""
-    _operand(name, t, dtype, dev)
-    if t.dim() < 2:
+def _heads(name, t, dtype, index):
+    """(layer_heads, lead shape, batch, length, heads, dim) of [..., heads, dim] (and what has to live until the call
+    where that is a copy): [heads, dim], [length, heads, dim] or [batch, length, heads, dim] where it lies; a copy of more
+    leading dimensions that do not merge, or of heads whose elements lie apart."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype is not dtype:
+        _operand(name, t, dtype, torch.device("cuda", index))
+    shape, step, made = t.shape, t.stride(), None
+    n = len(shape)
+    if n < 2:
         raise ValueError(f"{name}: needs [..., heads, dim]")
-    lead = t.shape[:-2]
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        t = t.contiguous()
-    if len(lead) > 2:
-        t = t.reshape(math.prod(lead[:-1]), *t.shape[-3:])
-    shape, step = (1,) * (4 - t.dim()) + tuple(t.shape), (0,) * (4 - t.dim()) + tuple(t.stride())
-    return t, layer_heads(t.data_ptr(), step[0], step[1], step[2]), lead, *shape
+    lead = shape[:-2]
+    if n > 4 or step[-1] != 1:
+        if step[-1] != 1 and shape[-1] > 1:
+            t = t.contiguous()
+        made = t = t if n <= 4 else t.reshape(math.prod(lead[:-1]), *shape[-3:])
+        shape, step = t.shape, t.stride()
+        n = len(shape)
+    if n == 3:
+        return layer_heads(t.data_ptr(), 0, step[0], step[1]), lead, 1, *shape, made
+    if n == 4:
+        return layer_heads(t.data_ptr(), step[0], step[1], step[2]), lead, *shape, made
+    return layer_heads(t.data_ptr(), 0, 0, step[0]), lead, 1, 1, *shape, made
 
 
 def _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status):
-    """Checks what both passes take; the arguments of the C calls from the sizes to the positions in three pieces, and
-    what has to live until the call: operands, batch x length, heads, dimension."""
-    dev = _operand(name, q)
-    q, hq, lead, batch, length, heads, dim = _heads(name, q, None, dev)
-    k, hk, lead_k, _, _, kv_heads, dim_k = _heads(name, k, q.dtype, dev)
+    """Checks what both passes take; the arguments of the C calls from the sizes to the positions in four pieces, and
+    what has to live until the call."""
+    index, dtype = q.get_device(), q.dtype
+    hq, lead, batch, length, heads, dim, made_q = _heads(name, q, dtype, index)
+    hk, lead_k, _, _, kv_heads, dim_k, made_k = _heads(name, k, dtype, index)
     if lead_k != lead or dim_k != dim:
         raise ValueError(f"{name}: q and k need the same tokens and the same size of a head")
-    if dim % 2 or not 2 <= dim <= 512 or max(heads, kv_heads) > 32768:
+    if dim % 2 or not 2 <= dim <= 512 or heads > 32768 or kv_heads > 32768:
         raise ValueError(f"{name}: heads need an even size of 2 to 512, and there are 32768 at most")
     if (cos is None) != (sin is None):
         raise ValueError(f"{name}: cos and sin come together")
-    places = rotary = wide = 0
+    table = (None, None, 0, None, 0)
+    rotary = 0
     if cos is not None:
         for t in (cos, sin):
-            _operand(name, t, _F32, dev)
+            if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype is not _F32:
+                _operand(name, t, _F32, q.device)
             if t.dim() != 2 or t.shape != cos.shape or not t.is_contiguous():
                 raise ValueError(f"{name}: cos and sin need contiguous [places, rotary / 2] elements")
-        places, rotary = cos.shape[0], 2 * cos.shape[1]
+        places, rotary = cos.shape
+        rotary *= 2
         if rotary > dim:
             raise ValueError(f"{name}: {rotary} elements to rotate in heads of {dim}")
+        table = (cos.data_ptr(), sin.data_ptr(), places, None, 0)
     if positions is not None:
-        if not isinstance(positions, torch.Tensor) or positions.dtype not in (_I32, torch.int64):
+        wide = isinstance(positions, torch.Tensor) and positions.dtype is torch.int64
+        if not wide and (not isinstance(positions, torch.Tensor) or positions.dtype is not _I32):
             raise TypeError(f"{name}: positions are int32 or int64")
-        _operand(name, positions, positions.dtype, dev)
-        if positions.shape != lead and positions.shape != lead[-1:]:
-            raise ValueError(f"{name}: needs one position per token, or per token of a sequence")
-        positions = positions.expand(lead).contiguous()
-        wide = int(positions.dtype is torch.int64)
-    wt = _weights(name, q, dim, q_weight, k_weight)
+        if positions.get_device() != index:
+            _operand(name, positions, positions.dtype, q.device)
+        if positions.shape != lead:
+            if positions.shape != lead[-1:]:
+                raise ValueError(f"{name}: needs one position per token, or per token of a sequence")
+            positions = positions.expand(lead)
+        if not positions.is_contiguous():
+            positions = positions.contiguous()
+        table = (*table[:3], positions.data_ptr(), int(wide))
+    weights = (None, None, 0)
+    if q_weight is not None or k_weight is not None:
+        weights = (None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                   _weights(name, q, dim, q_weight, k_weight))
     if status is not None:
-        _operand(name, status, _I32, dev)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    return (dev, (batch, length, heads, kv_heads, dim, rotary), (hq, hk), (ptr(q_weight), ptr(k_weight), wt),
-            (ptr(cos), ptr(sin), places, ptr(positions), wide), (q, k, positions))
+        _operand(name, status, _I32, q.device)
+    return (batch, length, heads, kv_heads, dim, rotary), (hq, hk), weights, table, (made_q, made_k, positions)
 
 
 def _dense_heads(t, sizes, heads):
-    return layer_heads(t.data_ptr(), sizes[1] * heads * sizes[4], heads * sizes[4], sizes[4])
+    dim = sizes[4]
+    return layer_heads(t.data_ptr(), sizes[1] * heads * dim, heads * dim, dim)
 
 
 def qk_rotary_forward(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tensor] = None,
@@ -341,16 +360,17 @@ def qk_rotary_forward(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tens
     status: an int32 CUDA word that SOAP_STATUS_RANGE is ORed into where a position is not in the table; the
     token's results are NaN."""
     name = "qk_rotary_forward"
-    dev = _operand(name, q)
-    if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream, q, k, cos, sin, positions, q_weight, k_weight, status):
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dtype not in DTYPES:
+        _refuse(name, q, None, None)
+    index, dev = q.get_device(), q.device
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream, q, k, cos, sin, positions, q_weight, k_weight, status):
             return qk_rotary_forward(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, status)
-    _, sizes, heads, w, table, keep = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
+    sizes, heads, w, table, held = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
     out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
     _done(load_library().layer_qk_forward(
         *sizes, int(interleaved), *heads, DTYPES[q.dtype], *w, eps, *table, _dense_heads(out_q, sizes, sizes[2]),
-        _dense_heads(out_k, sizes, sizes[3]), None if status is None else status.data_ptr(), _raw_stream(dev.index)),
-        name)
+        _dense_heads(out_k, sizes, sizes[3]), None if status is None else status.data_ptr(), _raw_stream(index)), name)
     return out_q, out_k
 
 
@@ -363,19 +383,20 @@ def qk_rotary_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: t
     The first two have q's type, the weights' are float32 [dim] (of a weight that is None: as for one of ones), or
     None without ``params``."""
     name = "qk_rotary_backward"
-    dev = _operand(name, q)
-    if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream, dq, dk, q, k, cos, sin, positions, q_weight, k_weight, status):
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dtype not in DTYPES:
+        _refuse(name, q, None, None)
+    index, dev = q.get_device(), q.device
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream, dq, dk, q, k, cos, sin, positions, q_weight, k_weight, status):
             return qk_rotary_backward(dq, dk, q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, params,
                                       status)
-    _, sizes, heads, w, table, keep = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
+    sizes, heads, w, table, held = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
     grads = []
     for d, t in ((dq, q), (dk, k)):
-        shape = d.shape if isinstance(d, torch.Tensor) else None
-        d, h, *_ = _heads(name, d, q.dtype, dev)
-        if shape != t.shape:
+        if isinstance(d, torch.Tensor) and d.shape != t.shape:
             raise ValueError(f"{name}: a gradient has another shape than its operand")
-        grads.append((d, h))
+        found = _heads(name, d, q.dtype, index)
+        grads.append((found[0], found[-1]))
     out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
     lib = load_library()
     dwq = dwk = ws = None
@@ -386,9 +407,9 @@ def qk_rotary_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: t
         ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     _done(lib.layer_qk_backward(
-        *sizes, int(interleaved), grads[0][1], grads[1][1], *heads, DTYPES[q.dtype], *w, eps, *table,
+        *sizes, int(interleaved), grads[0][0], grads[1][0], *heads, DTYPES[q.dtype], *w, eps, *table,
         _dense_heads(out_q, sizes, sizes[2]), _dense_heads(out_k, sizes, sizes[3]), ptr(dwq), ptr(dwk), ptr(status),
-        ptr(ws), ws_bytes, _raw_stream(dev.index)), name)
+        ptr(ws), ws_bytes, _raw_stream(index)), name)
     return out_q, out_k, dwq, dwk
 
 
@@ -453,42 +474,58 @@ def muon_orthogonalize(M: torch.Tensor, coeffs=None, ns_steps: int = 16, eps: fl
 _ACTS = {"silu": 0, "gelu": 1}
 
 
+def _ffn_weight(name, w, size, groups):
+    """(layer_matrix, what has to live until the call, transposed, rows, cols as stored, the bits of its 16-byte units)."""
+    rows, cols = w.shape[-2:]
+    if w.is_contiguous():
+        swapped = False
+    else:
+        step = w.stride()
+        if step[-2] != 1 or step[-1] != rows or (len(step) == 3 and step[0] != rows * cols):
+            w, _, rows, cols, ld, stride, swapped = _matrices(name, w)
+            at = w.data_ptr()
+            return layer_matrix(at, ld, stride, swapped), w, swapped, rows, cols, at | ld * size | (groups > 1) * stride * size
+        swapped, rows, cols = True, cols, rows
+    at = w.data_ptr()
+    return layer_matrix(at, cols, rows * cols, swapped), w, swapped, rows, cols, at | cols * size
+
+
 def _ffn_common(name, x, weights, offsets, act, status):
     """Checks what both passes take: (rows, hidden, width, groups), x and its leading dimension, the weights as
-    layer_matrix and as tensors, whether all of them lie on 16-byte units."""
-    dev = _operand(name, x)
+    _ffn_weight finds them, offsets, the bits of the 16-byte units of all of these."""
+    index, dtype, size = x.get_device(), x.dtype, x.element_size()
     if act not in _ACTS:
         raise ValueError(f"{name}: act is one of {', '.join(_ACTS)}")
     if x.dim() < 1:
         raise ValueError(f"{name}: needs at least one dimension")
-    hidden, size = x.shape[-1], x.element_size()
-    groups = 1
+    hidden, groups, dims = x.shape[-1], 1, 2
     if offsets is not None:
-        _operand(name, offsets, _I32, dev)
+        _operand(name, offsets, _I32, x.device)
         if offsets.dim() != 1 or offsets.numel() < 2:
             raise ValueError(f"{name}: offsets need groups + 1 elements")
         offsets = offsets.contiguous()
-        groups = offsets.numel() - 1
+        groups, dims = offsets.numel() - 1, 3
     for w in weights:
-        _operand(name, w, x.dtype, dev)
-        if w.dim() != (2 if offsets is None else 3) or (offsets is not None and w.shape[0] != groups):
+        if not isinstance(w, torch.Tensor) or w.get_device() != index or w.dtype is not dtype:
+            _operand(name, w, dtype, x.device)
+        if w.dim() != dims or (dims == 3 and w.shape[0] != groups):
             raise ValueError(f"{name}: needs a matrix of each weight" + ("" if offsets is None else " for each group"))
     gate, up, down = weights
-    width = gate.shape[-1]
-    if gate.shape[-2] != hidden or up.shape != gate.shape or down.shape[-2:] != (width, hidden):
-        raise ValueError(f"{name}: weights of shapes {tuple(gate.shape)}, {tuple(up.shape)}, {tuple(down.shape)} do not "
+    shape = gate.shape
+    width = shape[-1]
+    if shape[-2] != hidden or up.shape != shape or down.shape[-2] != width or down.shape[-1] != hidden:
+        raise ValueError(f"{name}: weights of shapes {tuple(shape)}, {tuple(up.shape)}, {tuple(down.shape)} do not "
                          f"fit rows of {hidden}")
     if not 1 <= hidden <= 65536 or not 1 <= width <= 65536 or groups > 1024:
         raise ValueError(f"{name}: hidden and width of 1 to 65536 and at most 1024 groups")
-    found = [_matrices(name, w) for w in weights]
-    if found[0][6] != found[1][6]:  # of two orders: both row-major
-        found[:2] = [_matrices(name, w.contiguous()) for w in weights[:2]]
+    found = [_ffn_weight(name, w, size, groups) for w in weights]
+    if found[0][2] != found[1][2]:  # of two orders: both row-major
+        found[:2] = [_ffn_weight(name, w.contiguous(), size, groups) for w in weights[:2]]
     if status is not None:
-        _operand(name, status, _I32, dev)
+        _operand(name, status, _I32, x.device)
     x, rows, ld = _rows(x)
-    units = [f[0].data_ptr() | f[4] * size | (f[5] * size if groups > 1 else 0) for f in found] + [x.data_ptr() | ld * size]
-    mats = [layer_matrix(f[0].data_ptr(), f[4], f[5], int(f[6])) for f in found]
-    return (rows, hidden, width, groups), x, ld, mats, found, offsets, units
+    units = x.data_ptr() | ld * size | found[0][5] | found[1][5] | found[2][5]
+    return (rows, hidden, width, groups), x, ld, found, offsets, units
 
 
 def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
@@ -501,21 +538,23 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     this call (float32, in the library's own order), else None. status: an int32 CUDA word that SOAP_STATUS_TIMEOUT
     and SOAP_STATUS_RANGE (offsets that fall or pass the rows) are ORed into."""
     name = "ffn_forward"
-    dev = _operand(name, x)
-    if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream, x, w_gate, w_up, w_down, offsets, status):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in DTYPES:
+        _refuse(name, x, None, None)
+    index, dev = x.get_device(), x.device
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream, x, w_gate, w_up, w_down, offsets, status):
             return ffn_forward(x, w_gate, w_up, w_down, offsets, act, keep, status)
     shape = x.shape
-    sizes, x, ld, mats, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    sizes, x, ld, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
     lib, t = load_library(), DTYPES[x.dtype]
     y = _empty(shape, dtype=x.dtype, device=dev)
     pre = _empty(lib.layer_ffn_pre_elems(sizes[0], sizes[2], sizes[3]), dtype=_F32, device=dev) if keep else None
-    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, int(not any(u % 16 for u in units)), 0)
+    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, units % 16 == 0, 0)
     ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_ffn_forward(
-        *sizes, None if offsets is None else offsets.data_ptr(), x.data_ptr(), ld, t, *mats, _ACTS[act], y.data_ptr(),
-        shape[-1], None if pre is None else pre.data_ptr(), None if status is None else status.data_ptr(),
-        ws.data_ptr(), ws_bytes, _raw_stream(dev.index)), name)
+        *sizes, None if offsets is None else offsets.data_ptr(), x.data_ptr(), ld, t, held[0][0], held[1][0],
+        held[2][0], _ACTS[act], y.data_ptr(), shape[-1], None if pre is None else pre.data_ptr(),
+        None if status is None else status.data_ptr(), ws.data_ptr(), ws_bytes, _raw_stream(index)), name)
     return y, pre
 
 
@@ -525,12 +564,14 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
     """(dx, dw_gate, dw_up, dw_down) of ffn_forward from y's gradient, the call's operands and its pre. All have x's
     type, the weights' gradients their weights' shapes and orders (None without ``params``)."""
     name = "ffn_backward"
-    dev = _operand(name, x)
-    if stream is not None or dev.index != _current():
-        with _elsewhere(dev.index, stream, dy, x, pre, w_gate, w_up, w_down, offsets, status):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in DTYPES:
+        _refuse(name, x, None, None)
+    index, dev = x.get_device(), x.device
+    if stream is not None or index != _current():
+        with _elsewhere(index, stream, dy, x, pre, w_gate, w_up, w_down, offsets, status):
             return ffn_backward(dy, x, pre, w_gate, w_up, w_down, offsets, act, params, status)
     shape = x.shape
-    sizes, x, ld, mats, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    sizes, x, ld, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
     _operand(name, dy, x.dtype, dev)
     if dy.shape != shape:
         raise ValueError(f"{name}: dy and x have different shapes")
@@ -543,14 +584,14 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
     grads, out = [None] * 3, [None] * 3
     if params:
         # in the order in which its weight lies: stored [groups, rows, cols], seen transposed if that is column-major
-        made = [_empty(((sizes[3],) if offsets is not None else ()) + f[2:4], dtype=x.dtype, device=dev) for f in held]
-        grads = [layer_matrix(g.data_ptr(), f[3], f[2] * f[3], int(f[6])) for g, f in zip(made, held)]
-        out = [g.mT if f[6] else g for g, f in zip(made, held)]
-    units.append(dy.data_ptr() | ld_dy * dy.element_size())
-    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, int(not any(u % 16 for u in units)), 1)
+        made = [_empty(((sizes[3],) if offsets is not None else ()) + f[3:5], dtype=x.dtype, device=dev) for f in held]
+        grads = [layer_matrix(g.data_ptr(), f[4], f[3] * f[4], f[2]) for g, f in zip(made, held)]
+        out = [g.mT if f[2] else g for g, f in zip(made, held)]
+    units |= dy.data_ptr() | ld_dy * dy.element_size()
+    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, units % 16 == 0, 1)
     ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_ffn_backward(
-        *sizes, None if offsets is None else offsets.data_ptr(), dy.data_ptr(), ld_dy, x.data_ptr(), ld, t, *mats,
-        _ACTS[act], pre.data_ptr(), dx.data_ptr(), shape[-1], *grads, None if status is None else status.data_ptr(),
-        ws.data_ptr(), ws_bytes, _raw_stream(dev.index)), name)
+        *sizes, None if offsets is None else offsets.data_ptr(), dy.data_ptr(), ld_dy, x.data_ptr(), ld, t,
+        held[0][0], held[1][0], held[2][0], _ACTS[act], pre.data_ptr(), dx.data_ptr(), shape[-1], *grads,
+        None if status is None else status.data_ptr(), ws.data_ptr(), ws_bytes, _raw_stream(index)), name)
     return dx, *out
