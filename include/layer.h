@@ -159,7 +159,7 @@ typedef struct {
  *   n = x / sqrt(mean(x^2) + eps),  m = n * weight  (the sum of x^2 is fp32: |x| up to 2^59),
  *   (a, b) -> (a c - b s, b c + a s) for the pairs (m_j, m_{j + rotary / 2}) or, `interleaved`,
  *   (m_2j, m_{2j + 1}), with c = cos[p][j], s = sin[p][j]; the other elements stay m
- * cos, sin: fp32 [places][rotary / 2]. positions: device int32, or int64 with positions_64, [batch * length],
+ * cos, sin: fp32 [places][rotary / 2], places < 2^31. positions: device int32, or int64 with positions_64, [batch * length],
  * or NULL: a token's place in its sequence. A position outside 0 .. places - 1 makes its token's results NaN, and
  * SOAP_STATUS_RANGE is ORed into *status (if not NULL; not cleared). q, k and the results: `type`;
  * q_weight, k_weight: dim elements of w_type (SOAP_F32 or `type`), either may be NULL (1). Results may be

@@ -4,8 +4,9 @@
 //   r = 1 / sqrt(mean(x^2) + eps),  n = x r,  m = n w,  (a, b) -> (a c - b s, b c + a s)
 //   dm: dy turned back,  g = dm w,  dx = r (g - n mean(g n)),  dw = sum dm n
 //
-// Bound by memory: x is read and y written once (backward: x and dy read, dx written once). A pair of the
-// rotation stays in one lane, so that turning it exchanges nothing: a lane holds 8 pairs of a head, as units
+// Bound by memory: x is read and y written once (backward: x and dy read, dx written once). Heads that lie on
+// 16-byte units come in by TMA, tiles of tokens and heads into a ring in shared memory; results leave from registers. Others, and calls of a few tokens, are read by
+// the lanes that work on them. A pair of the rotation stays in one lane, so that turning it exchanges nothing: a lane holds 8 pairs of a head, as units
 // of V neighbouring first and V neighbouring second elements (V: up to 16 bytes, as far as the parts' sizes
 // and alignments allow), and 1 to 32 lanes a head. All of a lane's heads are of one token, whose cosines and
 // sines it fetches once; heads that are independent of one another are asked for together. The mean of g n is
@@ -15,6 +16,7 @@
 #include <cstdint>
 
 #include "../../include/layer.h"
+#include "pair.h"
 #include "profile.h"
 #include "soap_internal.h"
 #include "types.h"
@@ -33,12 +35,12 @@ struct Heads {
 };
 
 struct Qk {
-  uint32_t tokens, length;
+  uint32_t tokens, length, period;  // (period: the sequences' own length, where several count as one)
   int heads[2];  // q, k
   int dim, rotary;
   Heads x[2], out[2], dy[2];  // forward: x to out; backward: dy and x to out (dx)
   const void* w[2];
-  float eps;
+  float eps, inv_dim;
   const float *cos, *sin;
   int64_t places;
   const void* positions;
@@ -47,6 +49,13 @@ struct Qk {
   int lanes;        // per head
   int steps;        // of 32 / lanes heads in a chunk
   int chunks[2];    // forward: of q's and k's heads together, in [0]
+  // tiles: heads and tokens in one, tiles along the heads and in all; slots of the ring and their bytes
+  int tile_heads[2], tile_tokens[2], tile_chunks[2];
+  uint32_t along[2];  // tiles along a sequence, 0: there is one sequence
+  uint32_t tiles[2];
+  int slots, slot_bytes;
+  uint64_t wait_ns;
+  const int* hold;
   float* partial;   // backward: [CTAs][dim], q's CTAs first, or nullptr
   uint32_t ctas_q;
 };
@@ -107,25 +116,152 @@ __device__ __forceinline__ void fetch(Raw<T, V>& r, const T* p, const Units<V, I
   }
 }
 
-// The pair j of unit i: elements 2 j and 2 j + 1 of the unit's 2 V, or element j of its halves.
+// A lane's 8 pairs: the first and the second elements, two by two, for the instructions that take two fp32 values.
+struct Eight {
+  float2 a[kPairs / 2], b[kPairs / 2];
+};
+
+// Pairs of unit i: elements 2 j and 2 j + 1 of the unit's 2 V, or element j of its halves.
 template <bool INTER, typename T, int V>
-__device__ __forceinline__ float2 pair_of(const Raw<T, V>& r, int i, int j) {
-  if (!INTER) return make_float2(to_f32(r.a[i].v[j]), to_f32(r.b[i].v[j]));
-  const int e = 2 * j;
-  return make_float2(to_f32(e < V ? r.a[i].v[e % V] : r.b[i].v[e % V]),
-                     to_f32(e + 1 < V ? r.a[i].v[(e + 1) % V] : r.b[i].v[(e + 1) % V]));
+__device__ __forceinline__ Eight unpack(const Raw<T, V>& r) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) {
+    if constexpr (V == 1) {
+      o.a[q] = make_float2(to_f32(r.a[2 * q].v[0]), to_f32(r.a[2 * q + 1].v[0]));
+      o.b[q] = make_float2(to_f32(r.b[2 * q].v[0]), to_f32(r.b[2 * q + 1].v[0]));
+    } else {
+      const int i = 2 * q / V, j = 2 * q % V, e = 2 * j;
+      if constexpr (!INTER) {
+        o.a[q] = to_pair(r.a[i].v + j);
+        o.b[q] = to_pair(r.b[i].v + j);
+      } else {
+        const float2 x = to_pair(e < V ? r.a[i].v + e : r.b[i].v + (e - V));
+        const float2 y = to_pair(e + 2 < V ? r.a[i].v + e + 2 : r.b[i].v + (e + 2 - V));
+        o.a[q] = make_float2(x.x, y.x);
+        o.b[q] = make_float2(x.y, y.y);
+      }
+    }
+  }
+  return o;
 }
 template <bool INTER, typename T, int V>
-__device__ __forceinline__ void set_pair(Raw<T, V>& r, int i, int j, float2 v) {
-  const T x = from_f32<T>(v.x), y = from_f32<T>(v.y);
-  if (!INTER) {
-    r.a[i].v[j] = x;
-    r.b[i].v[j] = y;
-    return;
+__device__ __forceinline__ void pack(const Eight& o, Raw<T, V>& r) {
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) {
+    if constexpr (V == 1) {
+      r.a[2 * q].v[0] = from_f32<T>(o.a[q].x), r.a[2 * q + 1].v[0] = from_f32<T>(o.a[q].y);
+      r.b[2 * q].v[0] = from_f32<T>(o.b[q].x), r.b[2 * q + 1].v[0] = from_f32<T>(o.b[q].y);
+    } else {
+      const int i = 2 * q / V, j = 2 * q % V, e = 2 * j;
+      if constexpr (!INTER) {
+        from_pair(o.a[q], r.a[i].v + j);
+        from_pair(o.b[q], r.b[i].v + j);
+      } else {
+        from_pair(make_float2(o.a[q].x, o.b[q].x), e < V ? r.a[i].v + e : r.b[i].v + (e - V));
+        from_pair(make_float2(o.a[q].y, o.b[q].y), e + 2 < V ? r.a[i].v + e + 2 : r.b[i].v + (e + 2 - V));
+      }
+    }
   }
-  const int e = 2 * j;
-  (e < V ? r.a[i].v[e % V] : r.b[i].v[e % V]) = x;
-  (e + 1 < V ? r.a[i].v[(e + 1) % V] : r.b[i].v[(e + 1) % V]) = y;
+}
+__device__ __forceinline__ float dot(const Eight& x, const Eight& y) {
+  float2 t = mul2(x.a[0], y.a[0]), u = mul2(x.b[0], y.b[0]);
+#pragma unroll
+  for (int q = 1; q < kPairs / 2; ++q) {
+    t = fma2(x.a[q], y.a[q], t);
+    u = fma2(x.b[q], y.b[q], u);
+  }
+  t = add2(t, u);
+  return t.x + t.y;
+}
+__device__ __forceinline__ Eight times(const Eight& x, const Eight& y) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) o.a[q] = mul2(x.a[q], y.a[q]), o.b[q] = mul2(x.b[q], y.b[q]);
+  return o;
+}
+__device__ __forceinline__ Eight times(const Eight& x, float r) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) o.a[q] = mul2(x.a[q], pair(r)), o.b[q] = mul2(x.b[q], pair(r));
+  return o;
+}
+__device__ __forceinline__ Eight times_one(float r) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) o.a[q] = o.b[q] = pair(r);
+  return o;
+}
+__device__ __forceinline__ Eight fma8(const Eight& x, const Eight& y, const Eight& z) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) o.a[q] = fma2(x.a[q], y.a[q], z.a[q]), o.b[q] = fma2(x.b[q], y.b[q], z.b[q]);
+  return o;
+}
+
+// The angles of a lane's pairs: cosines, sines.
+struct Angles {
+  float2 c[kPairs / 2], s[kPairs / 2];
+};
+// Each pair (a, b) -> (a c - b s, b c + a s), or back.
+template <bool BACK>
+__device__ __forceinline__ Eight turn(const Eight& m, const Angles& t) {
+  Eight o;
+#pragma unroll
+  for (int q = 0; q < kPairs / 2; ++q) {
+    const float2 less = make_float2(-t.s[q].x, -t.s[q].y);
+    o.a[q] = fma2(m.b[q], BACK ? t.s[q] : less, mul2(m.a[q], t.c[q]));
+    o.b[q] = fma2(m.a[q], BACK ? less : t.s[q], mul2(m.b[q], t.c[q]));
+  }
+  return o;
+}
+// What is turned by v's angle, from c and s of V neighbouring pairs.
+template <int V>
+__device__ __forceinline__ void load_angles(Angles& t, int i, const float* cos, const float* sin, bool turns) {
+  float c[V], s[V];
+  if (turns) {
+    load_f32<V>(cos, c);
+    load_f32<V>(sin, s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) c[e] = 1.f, s[e] = 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const int p = i * V + e;
+    if (p % 2)
+      t.c[p / 2].y = c[e], t.s[p / 2].y = s[e];
+    else
+      t.c[p / 2].x = c[e], t.s[p / 2].x = s[e];
+  }
+}
+
+// The forward pass of a head in x, whose sum of squares is xx, in place; the backward pass, which adds to dw too.
+template <bool INTER, typename T, int V>
+__device__ __forceinline__ void forward(Raw<T, V>& x, float r, const Eight& w, const Angles& t) {
+  pack<INTER>(turn<false>(times(times(unpack<INTER>(x), r), w), t), x);
+}
+template <bool INTER, typename T, int V>
+__device__ __forceinline__ void backward(Raw<T, V>& x, const Eight& dm, float r, float mean, const Eight& w, Eight& dw) {
+  const Eight n = times(unpack<INTER>(x), r);
+  dw = fma8(dm, n, dw);
+  pack<INTER>(fma8(n, times_one(-r * mean), times(times(dm, w), r)), x);
+}
+
+// The same from shared memory, where there is always something to read.
+template <typename T, int V, bool INTER>
+__device__ __forceinline__ void take(Raw<T, V>& r, const T* p, const Units<V, INTER>& un, int lane, int lanes) {
+#pragma unroll
+  for (int i = 0; i < kPairs / V; ++i) {
+    const int u = i * lanes + lane;
+    if (un.has(u)) {
+      r.a[i] = *reinterpret_cast<const Pack<T, V>*>(p + un.first(u));
+      r.b[i] = *reinterpret_cast<const Pack<T, V>*>(p + un.second(u));
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) r.a[i].v[e] = r.b[i].v[e] = from_f32<T>(0.f);
+    }
+  }
 }
 
 template <typename T, int V, bool INTER>
@@ -142,8 +278,7 @@ __device__ __forceinline__ void store(T* p, const Raw<T, V>& r, const Units<V, I
 
 // A lane's cosines and sines (1 and 0 where nothing turns), and whether the token's position is in range.
 template <int V, bool INTER>
-__device__ __forceinline__ bool angles(const Qk& a, uint32_t token, const Units<V, INTER>& un, int lane, float (&c)[kPairs],
-                                       float (&s)[kPairs]) {
+__device__ __forceinline__ bool angles(const Qk& a, uint32_t token, const Units<V, INTER>& un, int lane, Angles& t) {
   int64_t at = 0;
   bool ok = true;
   if (a.rotary > 0) {
@@ -155,21 +290,15 @@ __device__ __forceinline__ bool angles(const Qk& a, uint32_t token, const Units<
 #pragma unroll
   for (int i = 0; i < kPairs / V; ++i) {
     const int u = i * a.lanes + lane;
-    if (ok && un.turns(u)) {
-      const int64_t j = at * (a.rotary / 2) + u * V;
-      load_f32<V>(a.cos + j, c + i * V);
-      load_f32<V>(a.sin + j, s + i * V);
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) c[i * V + e] = 1.f, s[i * V + e] = 0.f;
-    }
+    const int64_t j = at * (a.rotary / 2) + u * V;
+    load_angles<V>(t, i, a.cos + j, a.sin + j, ok && un.turns(u));
   }
   return ok;
 }
 
 // The weights of a lane's pairs.
 template <typename W, int V, bool INTER>
-__device__ __forceinline__ void weights(const void* w, const Units<V, INTER>& un, int lane, int lanes, float2 (&v)[kPairs]) {
+__device__ __forceinline__ void weights(const void* w, const Units<V, INTER>& un, int lane, int lanes, Eight& v) {
 #pragma unroll
   for (int i = 0; i < kPairs / V; ++i) {
     const int u = i * lanes + lane;
@@ -183,10 +312,13 @@ __device__ __forceinline__ void weights(const void* w, const Units<V, INTER>& un
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (!INTER) v[i * V + j] = make_float2(x[j], y[j]);
+      const int p = i * V + j;
+      const float first = !INTER ? x[j] : 2 * j < V ? x[(2 * j) % V] : y[(2 * j) % V];
+      const float second = !INTER ? y[j] : 2 * j + 1 < V ? x[(2 * j + 1) % V] : y[(2 * j + 1) % V];
+      if (p % 2)
+        v.a[p / 2].y = first, v.b[p / 2].y = second;
       else
-        v[i * V + j] = make_float2(2 * j < V ? x[(2 * j) % V] : y[(2 * j) % V],
-                                   2 * j + 1 < V ? x[(2 * j + 1) % V] : y[(2 * j + 1) % V]);
+        v.a[p / 2].x = first, v.b[p / 2].x = second;
     }
   }
 }
@@ -213,31 +345,48 @@ __global__ void __launch_bounds__(32 * kWarps) qk_fwd_kernel(const __grid_consta
       p = static_cast<const T*>(a.x[k].p) + place_of(a.x[k], a, token, k ? h - a.heads[0] : h);
     fetch(x[s], p, un, lane, lanes);
   }
-  float c[kPairs], sn[kPairs];
-  const bool ok = angles(a, token, un, lane, c, sn);
+  Angles t;
+  const bool ok = angles(a, token, un, lane, t);
   if (!ok && threadIdx.x == 0 && a.status) atomicOr(a.status, kStatusRange);
 #pragma unroll
   for (int s = 0; s < UN; ++s) {
     if (s >= a.steps) break;
     const int h = h0 + s * per, k = h >= a.heads[0];
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const float2 v = pair_of<INTER>(x[s], i / V, i % V);
-      sum = fmaf(v.x, v.x, fmaf(v.y, v.y, sum));
-    }
-    sum = lanes_sum(sum, lanes);
+    const Eight v = unpack<INTER>(x[s]);
+    const float sum = lanes_sum(dot(v, v), lanes);
     if (h >= all) continue;  // (the exchange above takes all lanes)
-    const float r = ok ? 1.f / sqrtf(sum / (float)a.dim + a.eps) : NAN;
-    float2 w[kPairs];
+    const float r = ok ? rsqrtf(fmaf(sum, a.inv_dim, a.eps)) : NAN;
+    Eight w;
     weights<W>(a.w[k], un, lane, lanes, w);
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const float2 v = pair_of<INTER>(x[s], i / V, i % V);
-      const float m0 = v.x * r * w[i].x, m1 = v.y * r * w[i].y;
-      set_pair<INTER>(x[s], i / V, i % V, make_float2(m0 * c[i] - m1 * sn[i], m1 * c[i] + m0 * sn[i]));
-    }
+    forward<INTER>(x[s], r, w, t);
     store(static_cast<T*>(a.out[k].p) + place_of(a.out[k], a, token, k ? h - a.heads[0] : h), x[s], un, lane, lanes);
+  }
+}
+
+// A CTA's part of dweight: the sums over a warp's heads, then over the CTA's warps, always in the same order.
+template <int V, bool INTER>
+__device__ __forceinline__ void put_sums(const Eight& dw, float* row, const Units<V, INTER>& un, int lane, int lanes,
+                                         bool first) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    float x = i % 2 ? dw.a[i / 2].y : dw.a[i / 2].x, y = i % 2 ? dw.b[i / 2].y : dw.b[i / 2].x;
+    for (int o = lanes; o < 32; o <<= 1) {
+      x += __shfl_xor_sync(0xffffffffu, x, o);
+      y += __shfl_xor_sync(0xffffffffu, y, o);
+    }
+    const int u = (i / V) * lanes + lane, j = i % V;
+    if (first && un.has(u)) {
+      row[INTER ? un.first(u) + 2 * j : un.first(u) + j] = x;
+      row[INTER ? un.first(u) + 2 * j + 1 : un.second(u) + j] = y;
+    }
+  }
+}
+__device__ __forceinline__ void add_sums(const float* sums, const Qk& a, int thread, int threads) {
+  for (int j = thread; j < a.dim; j += threads) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) t += sums[i * a.dim + j];
+    a.partial[(int64_t)blockIdx.x * a.dim + j] = t;
   }
 }
 
@@ -252,10 +401,8 @@ __global__ void __launch_bounds__(32 * kWarps) qk_bwd_kernel(const __grid_consta
   const Units<V, INTER> un{a.dim, a.rotary};
   const int all = a.heads[k];
   const uint32_t chunks = a.chunks[k];
-  float2 w[kPairs], dw[kPairs];
+  Eight w, dw = times_one(0.f);
   weights<W>(a.w[k], un, lane, lanes, w);
-#pragma unroll
-  for (int i = 0; i < kPairs; ++i) dw[i] = make_float2(0.f, 0.f);
   const uint32_t step = ctas * kWarps, first = cta * kWarps + threadIdx.y;
   const uint32_t dt = step / chunks, dc = step % chunks;
   uint32_t chunk = first % chunks;
@@ -270,36 +417,18 @@ __global__ void __launch_bounds__(32 * kWarps) qk_bwd_kernel(const __grid_consta
       fetch(x[s], live ? static_cast<const T*>(a.x[k].p) + place_of(a.x[k], a, token, h) : nullptr, un, lane, lanes);
       fetch(dy[s], live ? static_cast<const T*>(a.dy[k].p) + place_of(a.dy[k], a, token, h) : nullptr, un, lane, lanes);
     }
-    float c[kPairs], sn[kPairs];
-    const bool ok = angles(a, token, un, lane, c, sn);
+    Angles t;
+    const bool ok = angles(a, token, un, lane, t);
     if (!ok && threadIdx.x == 0 && a.status) atomicOr(a.status, kStatusRange);
 #pragma unroll
     for (int s = 0; s < UN; ++s) {
       if (s >= a.steps) break;
       const int h = h0 + s * per;
-      float2 dm[kPairs];
-      float xx = 0.f, gx = 0.f;
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        const float2 v = pair_of<INTER>(x[s], i / V, i % V), d = pair_of<INTER>(dy[s], i / V, i % V);
-        dm[i] = make_float2(d.x * c[i] + d.y * sn[i], d.y * c[i] - d.x * sn[i]);
-        xx = fmaf(v.x, v.x, fmaf(v.y, v.y, xx));
-        gx = fmaf(dm[i].x * w[i].x, v.x, fmaf(dm[i].y * w[i].y, v.y, gx));
-      }
-      xx = lanes_sum(xx, lanes);
-      gx = lanes_sum(gx, lanes);
+      const Eight v = unpack<INTER>(x[s]), dm = turn<true>(unpack<INTER>(dy[s]), t);
+      const float xx = lanes_sum(dot(v, v), lanes), gx = lanes_sum(dot(times(dm, w), v), lanes);
       if (h >= all) continue;
-      const float r = ok ? 1.f / sqrtf(xx / (float)a.dim + a.eps) : NAN;
-      const float mean = r * (gx / (float)a.dim);
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        const float2 v = pair_of<INTER>(x[s], i / V, i % V);
-        const float n0 = v.x * r, n1 = v.y * r;
-        dw[i].x = fmaf(dm[i].x, n0, dw[i].x);
-        dw[i].y = fmaf(dm[i].y, n1, dw[i].y);
-        set_pair<INTER>(x[s], i / V, i % V,
-                        make_float2(r * (dm[i].x * w[i].x - n0 * mean), r * (dm[i].y * w[i].y - n1 * mean)));
-      }
+      const float r = ok ? rsqrtf(fmaf(xx, a.inv_dim, a.eps)) : NAN;
+      backward<INTER>(x[s], dm, r, r * (gx * a.inv_dim), w, dw);
       store(static_cast<T*>(a.out[k].p) + place_of(a.out[k], a, token, h), x[s], un, lane, lanes);
     }
     token += dt;
@@ -310,31 +439,176 @@ __global__ void __launch_bounds__(32 * kWarps) qk_bwd_kernel(const __grid_consta
     }
   }
   if (!a.partial) return;
-  // the warp's heads, then the CTA's warps, always in the same order
-#pragma unroll
-  for (int i = 0; i < kPairs; ++i)
-    for (int o = lanes; o < 32; o <<= 1) {
-      dw[i].x += __shfl_xor_sync(0xffffffffu, dw[i].x, o);
-      dw[i].y += __shfl_xor_sync(0xffffffffu, dw[i].y, o);
+  put_sums<V, INTER>(dw, sums + threadIdx.y * a.dim, un, lane, lanes, at == 0);
+  __syncthreads();
+  add_sums(sums, a, threadIdx.y * 32 + threadIdx.x, 32 * kWarps);
+}
+
+// ---- heads in tiles ----
+
+struct QkMaps {
+  CUtensorMap x[2], dy[2];  // of q, of k: (element, head, token, sequence)
+};
+
+constexpr int kRingBytes = 98304;  // two CTAs per SM
+constexpr int kMaxSlots = 12;
+
+__device__ __forceinline__ void load_heads(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int h, int t, int b) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(tc::smem_u32(bar)), "r"(0), "r"(h), "r"(t), "r"(b)
+      : "memory");
+}
+// Where tile i of q's (k = 0) or k's heads is.
+struct Tile {
+  int h0;
+  uint32_t b, t0;  // sequence, first token in it
+};
+__device__ __forceinline__ Tile tile_at(const Qk& a, int k, uint32_t i) {
+  const uint32_t chunks = a.tile_chunks[k];
+  uint32_t row = i, b = 0;
+  if (chunks > 1) row = i / chunks;
+  const int h0 = (int)(i - row * chunks) * a.tile_heads[k];
+  if (a.along[k] > 0) {  // several sequences
+    b = row / a.along[k];
+    row -= b * a.along[k];
+  }
+  return Tile{h0, b, row * a.tile_tokens[k]};
+}
+
+// Persistent CTAs, the first ctas_q of them for q's heads, the others for k's, each with every (its CTAs)-th tile. The
+// angles of a lane's token in the next tile are on their way to its registers while it works on this one, from the L1
+// for all heads of a token but the first, and the position in the tile after that. (Rows of angles brought into the
+// ring by one warp, by bulk copies or 16 bytes a lane, took that warp 100 ns a token: 255 us in place of @@ for 65536
+// tokens of 32 heads of 128 fp16.)
+template <typename T, typename W, int V, bool INTER, bool BACK>
+__global__ void __launch_bounds__(32 * kWarps, 2)
+    qk_tile_kernel(const __grid_constant__ QkMaps maps, const __grid_constant__ Qk a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
+  const int k = blockIdx.x >= a.ctas_q;
+  const uint32_t cta = blockIdx.x - (k ? a.ctas_q : 0), ctas = k ? gridDim.x - a.ctas_q : a.ctas_q;
+  const int lane32 = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int HB = a.tile_heads[k], TB = a.tile_tokens[k];
+  // a slot: x's tile, backward dy's
+  const int tile_bytes = HB * TB * a.dim * (int)sizeof(T), dy_at = (tile_bytes + 127) & ~127;
+  auto request = [&](uint32_t i, int s) {
+    const Tile t = tile_at(a, k, i);
+    uint8_t* const slot = smem + s * a.slot_bytes;
+    tc::expect_tx(&full[s], (BACK ? 2 : 1) * tile_bytes);
+    load_heads(tc::smem_u32(slot), &maps.x[k], &full[s], t.h0, t.t0, t.b);
+    if (BACK) load_heads(tc::smem_u32(slot + dy_at), &maps.dy[k], &full[s], t.h0, t.t0, t.b);
+  };
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < a.slots; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], kWarps);
     }
-  if (at == 0) {
-    float* row = sums + threadIdx.y * a.dim;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    // (a flag that nothing sets: nothing is asked for, and the waits run out)
+    const bool held = a.hold && !tc::flag_wait(a.hold, a.wait_ns);
+    for (int s = 0; s < a.slots && !held; ++s)
+      if (cta + s * ctas < a.tiles[k]) request(cta + s * ctas, s);
+  }
+  const int lanes = a.lanes, lane = lane32 & (lanes - 1), row = threadIdx.x / lanes;
+  const Units<V, INTER> un{a.dim, a.rotary};
+  const int all = a.heads[k], in_tile = row % HB, token_in_tile = row / HB;
+  const bool real = token_in_tile < TB;
+  // (a lane without a head of the tile's reads another one's, and stores nothing)
+  const int from = (real ? row : 0) * a.dim;
+  const Heads& o = a.out[k];
+  T* const out = static_cast<T*>(o.p) + (int64_t)in_tile * o.head + (int64_t)token_in_tile * o.token;
+  // the position of this lane's token in tile i; -1: there is none
+  auto position = [&](uint32_t i) -> int64_t {
+    if (a.rotary == 0 || !real || i >= a.tiles[k]) return -1;
+    const Tile t = tile_at(a, k, i);
+    const uint32_t in = t.t0 + token_in_tile, token = t.b * a.length + in;
+    if (in >= a.length) return -1;
+    if (!a.positions) return token % a.period;
+    return a.positions_64 ? static_cast<const int64_t*>(a.positions)[token] : static_cast<const int32_t*>(a.positions)[token];
+  };
+  auto angles_of = [&](Angles& t, int64_t at) {
+    const bool in = at >= 0 && at < a.places;
+    const int64_t first = (in ? at : 0) * (a.rotary / 2);
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const int u = (i / V) * lanes + lane, j = i % V;
-      if (un.has(u)) {
-        row[INTER ? un.first(u) + 2 * j : un.first(u) + j] = dw[i].x;
-        row[INTER ? un.first(u) + 2 * j + 1 : un.second(u) + j] = dw[i].y;
+    for (int j = 0; j < kPairs / V; ++j) {
+      const int u = j * lanes + lane;
+      load_angles<V>(t, j, a.cos + first + u * V, a.sin + first + u * V, in && un.turns(u));
+    }
+    return in || a.rotary == 0;
+  };
+  Eight w, dw = times_one(0.f);
+  weights<W>(a.w[k], un, lane, lanes, w);
+  Angles turns;
+  bool in_table = angles_of(turns, position(cta));
+  int64_t next_at = position(cta + ctas);
+  __syncthreads();
+  int s = 0;
+  uint32_t parity = 0;
+  bool ok = true;
+  for (uint32_t i = cta; i < a.tiles[k]; i += ctas) {
+    const uint8_t* const slot = smem + s * a.slot_bytes;
+    Angles next;
+    const bool next_in = angles_of(next, next_at);
+    next_at = position(i + 2 * ctas);
+    // after a wait that ran out: nothing more is waited for, all results become NaN
+    if (ok && !tc::mbar_wait(&full[s], parity, 2 * a.wait_ns)) {
+      ok = false;
+      if (a.status) atomicOr(a.status, kStatusTimeout);
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    Raw<T, V> x, dy;
+    take(x, reinterpret_cast<const T*>(slot) + from, un, lane, lanes);
+    if (BACK) take(dy, reinterpret_cast<const T*>(slot + dy_at) + from, un, lane, lanes);
+    __syncwarp();
+    if (lane32 == 0) {
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&empty[s])) : "memory");
+      if (warp == 0 && ok && i != cta) {  // the slot before this one is free, or soon: what comes next there
+        const int before = s > 0 ? s - 1 : a.slots - 1;
+        const uint64_t far = (uint64_t)i + (uint64_t)(a.slots - 1) * ctas;
+        if (far < a.tiles[k]) {
+          if (tc::mbar_wait(&empty[before], s > 0 ? parity : parity ^ 1, 2 * a.wait_ns)) request((uint32_t)far, before);
+        }
       }
     }
+    if (++s == a.slots) {
+      s = 0;
+      parity ^= 1;
+    }
+    const Tile t = tile_at(a, k, i);
+    const Eight v = unpack<INTER>(x);
+    const float r = rsqrtf(fmaf(lanes_sum(dot(v, v), lanes), a.inv_dim, a.eps));
+    const bool live = real && t.h0 + in_tile < all && t.t0 + token_in_tile < a.length, good = ok && in_table;
+    if (live && ok && !in_table && a.status) atomicOr(a.status, kStatusRange);
+    T* const to = out + (int64_t)t.b * o.batch + (int64_t)t.t0 * o.token + (int64_t)t.h0 * o.head;
+    if constexpr (BACK) {
+      const Eight dm = turn<true>(unpack<INTER>(dy), turns);
+      const float gx = lanes_sum(dot(times(dm, w), v), lanes);
+      if (live) {  // (the exchanges above take all lanes)
+        const float rr = good ? r : NAN;
+        backward<INTER>(x, dm, rr, rr * (gx * a.inv_dim), w, dw);
+        store(to, x, un, lane, lanes);
+      }
+    } else if (live) {
+      forward<INTER>(x, good ? r : NAN, w, turns);
+      store(to, x, un, lane, lanes);
+    }
+    turns = next;
+    in_table = next_in;
   }
+  if (!ok) {  // copies in flight land before the shared memory goes away: far above a copy's time
+    const uint64_t t0 = tc::globaltimer();
+    while (tc::globaltimer() - t0 < 10000000ull) {
+    }
+  }
+  if (!BACK || !a.partial) return;
+  __syncthreads();  // nothing of the ring is used any more
+  float* const sums = reinterpret_cast<float*>(smem);
+  put_sums<V, INTER>(dw, sums + warp * a.dim, un, lane, lanes, lane32 < lanes);
   __syncthreads();
-  for (int j = threadIdx.y * 32 + threadIdx.x; j < a.dim; j += 32 * kWarps) {
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) t += sums[i * a.dim + j];
-    a.partial[(int64_t)blockIdx.x * a.dim + j] = t;
-  }
+  add_sums(sums, a, threadIdx.x, blockDim.x);
 }
 
 // dweight[j] = the sum of the CTAs' parts, for 32 columns of q's or k's; a warp adds up every 16th CTA's.
@@ -413,8 +687,115 @@ void plan(Qk& a, int un, int heads, int& chunks) {
   chunks = (steps + un - 1) / un;
 }
 
+void share_ctas(Qk& a, const int64_t (&want)[2], int64_t most, uint32_t (&ctas)[2]) {
+  for (int k = 0; k < 2; ++k) ctas[k] = (uint32_t)std::min(want[k], most);
+  if (want[0] + want[1] > most) {  // shares by their work
+    for (int k = 0; k < 2; ++k)
+      ctas[k] = (uint32_t)std::min<int64_t>(want[k], std::max<int64_t>(want[k] > 0, most * want[k] / (want[0] + want[1])));
+  }
+  a.ctas_q = ctas[0];
+}
+
+cudaError_t sum_parts(const Qk& a, const uint32_t (&ctas)[2], float* dq, float* dk, cudaStream_t s) {
+  if (!a.partial) return cudaSuccess;
+  qk_sum_kernel<<<dim3((a.dim + 31) / 32, 2), dim3(32, kSumWarps), 0, s>>>(a.partial, ctas[0], ctas[0] + ctas[1], a.dim, dq, dk);
+  return cudaGetLastError();
+}
+
+bool heads_map(CUtensorMap* map, const Heads& h, const Qk& a, int k, uint32_t batch, CUtensorMapDataType type, size_t size) {
+  auto fn = tc::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)a.dim, (cuuint64_t)a.heads[k], a.length, batch};
+  // (a step that is never taken: any)
+  auto step = [&](int64_t n, int64_t stride) { return (cuuint64_t)(n > 1 ? stride * (int64_t)size : 16); };
+  const cuuint64_t strides[3] = {step(a.heads[k], h.head), step(a.length, h.token), step(batch, h.batch)};
+  const cuuint32_t box[4] = {(cuuint32_t)a.dim, (cuuint32_t)a.tile_heads[k], (cuuint32_t)a.tile_tokens[k], 1};
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
+  return fn(map, type, 4, h.p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tiles of heads, where they can be copied as such and there is enough to do; done: whether that was so. Below two tiles
+// for every SM the lanes' own loads are as quick.
+template <typename T, typename W, int V, bool INTER, bool BACK>
+cudaError_t tiles_t(Qk a, float* dq, float* dk, cudaStream_t s, bool& done) {
+  done = false;
+  if (a.dim > 256) return cudaSuccess;
+  uint32_t batch = a.tokens / a.length;
+  // sequences that lie one behind the other are one
+  a.period = a.length;
+  bool one = true;
+  for (int k = 0; k < 2 && batch > 1; ++k)
+    for (const Heads* h : {&a.x[k], &a.out[k], &a.dy[k]})
+      one = one && (!h->p || h->batch == (int64_t)a.length * h->token);
+  if (one) {
+    a.length = a.tokens;
+    batch = 1;
+  }
+  const int per_lane = kPairs / V;
+  for (a.lanes = 1; a.lanes * per_lane < a.dim / 2 / V;) a.lanes *= 2;
+  const int rows = kWarps * 32 / a.lanes;
+  int64_t want[2];
+  int bytes = 0;
+  for (int k = 0; k < 2; ++k) {
+    want[k] = a.tiles[k] = 0;
+    if (a.heads[k] == 0) continue;
+    for (const Heads* h : {&a.x[k], &a.dy[k]})
+      if (h->p && ((a.heads[k] > 1 && h->head < a.dim) || (a.length > 1 && h->token < 1) || (batch > 1 && h->batch < 1)))
+        return cudaSuccess;
+    a.tile_heads[k] = std::min(a.heads[k], rows);
+    a.tile_tokens[k] = rows / a.tile_heads[k];
+    a.tile_chunks[k] = (a.heads[k] + a.tile_heads[k] - 1) / a.tile_heads[k];
+    a.along[k] = batch > 1 ? (a.length + a.tile_tokens[k] - 1) / a.tile_tokens[k] : 0;
+    const int64_t n = (int64_t)batch * ((a.length + a.tile_tokens[k] - 1) / a.tile_tokens[k]) * a.tile_chunks[k];
+    if (n > UINT32_MAX / 2 || (int64_t)a.tile_tokens[k] > 8 * (int64_t)a.length) return cudaSuccess;
+    want[k] = a.tiles[k] = (uint32_t)n;
+    const int tile = (a.tile_heads[k] * a.tile_tokens[k] * a.dim * (int)sizeof(T) + 127) & ~127;
+    bytes = std::max(bytes, (BACK ? 2 : 1) * tile);
+  }
+  const int sms = sm_count();
+  if (sms < 1) return cudaErrorInvalidDevice;
+  if (want[0] + want[1] < 2 * sms) return cudaSuccess;
+  a.slot_bytes = (bytes + 127) & ~127;
+  a.slots = std::min(kMaxSlots, kRingBytes / a.slot_bytes);
+  if (a.slots < 2) return cudaSuccess;
+  const CUtensorMapDataType type = sizeof(T) == 4                          ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : std::is_same<T, __nv_bfloat16>::value ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                           : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  QkMaps maps{};
+  for (int k = 0; k < 2; ++k)
+    if (a.heads[k] > 0 && (!heads_map(&maps.x[k], a.x[k], a, k, batch, type, sizeof(T)) ||
+                           (BACK && !heads_map(&maps.dy[k], a.dy[k], a, k, batch, type, sizeof(T)))))
+      return cudaSuccess;  // (steps beyond what a map holds)
+  const WaitLimit limit = wait_limit();
+  a.wait_ns = limit.ns;
+  a.hold = limit.hold;
+  auto kernel = qk_tile_kernel<T, W, V, INTER, BACK>;
+  constexpr int smem = kRingBytes + 128;
+  static std::atomic<bool> set[64];  // the kernel's shared-memory attribute, per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev >= 64 || !set[dev].load(std::memory_order_relaxed))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && dev < 64) set[dev].store(true, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return e;
+  uint32_t ctas[2];
+  share_ctas(a, want, 2 * sms, ctas);
+  kernel<<<ctas[0] + ctas[1], 32 * kWarps, smem, s>>>(maps, a);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = sum_parts(a, ctas, dq, dk, s);
+  done = true;
+  return e;
+}
+
 template <typename T, typename W, int V, bool INTER>
 cudaError_t fwd_t(Qk a, cudaStream_t s) {
+  if constexpr (V * sizeof(T) == 16) {
+    bool done;
+    const cudaError_t e = tiles_t<T, W, V, INTER, false>(a, nullptr, nullptr, s, done);
+    if (done || e != cudaSuccess) return e;
+  }
   constexpr int UN = sizeof(T) == 2 ? 4 : 2;
   const int units = a.dim / 2 / V, per_lane = kPairs / V;
   for (a.lanes = 1; a.lanes * per_lane < units;) a.lanes *= 2;
@@ -428,6 +809,11 @@ cudaError_t fwd_t(Qk a, cudaStream_t s) {
 
 template <typename T, typename W, int V, bool INTER>
 cudaError_t bwd_t(Qk a, float* dq, float* dk, cudaStream_t s) {
+  if constexpr (V * sizeof(T) == 16) {
+    bool done;
+    const cudaError_t e = tiles_t<T, W, V, INTER, true>(a, dq, dk, s, done);
+    if (done || e != cudaSuccess) return e;
+  }
   constexpr int UN = sizeof(T) == 2 ? 2 : 1;
   const int units = a.dim / 2 / V, per_lane = kPairs / V;
   for (a.lanes = 1; a.lanes * per_lane < units;) a.lanes *= 2;
@@ -450,20 +836,11 @@ cudaError_t bwd_t(Qk a, float* dq, float* dk, cudaStream_t s) {
     want[k] = ((int64_t)a.tokens * a.chunks[k] + kWarps - 1) / kWarps;
   }
   const int64_t most = std::min(kBwdCtas, sms * fit);
-  uint32_t ctas[2] = {(uint32_t)std::min(want[0], most), (uint32_t)std::min(want[1], most)};
-  if (want[0] + want[1] > most) {  // shares by their chunks
-    for (int k = 0; k < 2; ++k)
-      ctas[k] = (uint32_t)std::min<int64_t>(want[k], std::max<int64_t>(want[k] > 0, most * want[k] / (want[0] + want[1])));
-  }
-  a.ctas_q = ctas[0];
+  uint32_t ctas[2];
+  share_ctas(a, want, most, ctas);
   qk_bwd_kernel<T, W, V, INTER, UN><<<ctas[0] + ctas[1], dim3(32, kWarps), a.partial ? smem : 0, s>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && a.partial) {
-    qk_sum_kernel<<<dim3((a.dim + 31) / 32, 2), dim3(32, kSumWarps), 0, s>>>(a.partial, ctas[0], ctas[0] + ctas[1], a.dim,
-                                                                             dq, dk);
-    e = cudaGetLastError();
-  }
-  return e;
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? sum_parts(a, ctas, dq, dk, s) : e;
 }
 
 template <typename F>
@@ -509,7 +886,7 @@ bool common(Qk& a, int64_t batch, int64_t length, int32_t heads, int32_t kv_head
   a.rotary = rotary;
   if (rotary > 0) {
     if (odd_ptr(cos, 4) || odd_ptr(sin, 4) || odd_ptr(positions, positions_64 ? 8 : 4)) return false;
-    if (places < 0 || (a.tokens > 0 && (!cos || !sin))) return false;
+    if (places < 0 || places > INT32_MAX || (a.tokens > 0 && (!cos || !sin))) return false;
     a.cos = cos;
     a.sin = sin;
     a.places = places;
@@ -523,6 +900,7 @@ bool common(Qk& a, int64_t batch, int64_t length, int32_t heads, int32_t kv_head
   a.w[0] = q_weight;
   a.w[1] = k_weight;
   a.eps = eps;
+  a.inv_dim = 1.f / (float)dim;
   a.status = status;
   return true;
 }

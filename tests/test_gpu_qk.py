@@ -1,8 +1,7 @@
 """Queries' and keys' norms with the rotation by position (include/layer.h, layer_qk_*) against fp64.
 
 Tolerance (from the arithmetic): with u = 2^-24, a lane adds 16 squares in order and up to 32 lanes' sums pairwise:
-the sum is within 22 u of itself, r within 11 u and the four roundings of the mean, the addition, the root and the
-quotient; n and m add one each and the rotation two of its own terms: within 24 u of the terms' magnitudes, and one
+the sum is within 22 u of itself, r within 11 u, the two roundings of the mean and of eps's addition, half of which reach it, and the root's 4 u; n and m add one each and the rotation two of its own terms: within 24 u of the terms' magnitudes, and one
 rounding to the type. The gradients' terms in the same way: dm within 2 u of its terms, sums of products with it
 within 26 u of the sum of magnitudes. dweight adds up a warp's heads (at most 2 + tokens heads / 2400 of them
 in order), then at most 5 + 8 + 40 + 16 partial sums.
