@@ -4,13 +4,15 @@
 //   r = 1 / sqrt(mean(x^2) + eps),  n = x r,  m = n w,  (a, b) -> (a c - b s, b c + a s)
 //   dm: dy turned back,  g = dm w,  dx = r (g - n mean(g n)),  dw = sum dm n
 //
-// Bound by memory: x is read and y written once (backward: x and dy read, dx written once). Heads that lie on
-// 16-byte units come in by TMA, tiles of tokens and heads into a ring in shared memory; results leave from registers. Others, and calls of a few tokens, are read by
-// the lanes that work on them. A pair of the rotation stays in one lane, so that turning it exchanges nothing: a lane holds 8 pairs of a head, as units
-// of V neighbouring first and V neighbouring second elements (V: up to 16 bytes, as far as the parts' sizes
-// and alignments allow), and 1 to 32 lanes a head. All of a lane's heads are of one token, whose cosines and
-// sines it fetches once; heads that are independent of one another are asked for together. The mean of g n is
-// r times that of g x, so that a head's two sums cross its lanes in one exchange.
+// Bound by memory: x is read and y written once (backward: x and dy read, dx written once). Heads whose rows are whole
+// 16-byte units come in by TMA, tiles of tokens and heads into a ring in shared memory; results leave from registers.
+// Others, and calls of a few tokens, are read by the lanes that work on them. A pair of the rotation stays in one lane,
+// so that turning it exchanges nothing: a lane holds 8 pairs of a head, as units of V neighbouring first and V
+// neighbouring second elements (V: 16 bytes where the parts' sizes and alignments allow, else 2 or 1), and 1 to 32
+// lanes a head. The mean of g n is r times that of g x, so that a head's two sums cross its lanes together. Arithmetic
+// goes two elements at a time: with one, and with the angles, the tile's place and the rest worked out for every head
+// in place of every four (backward two), instructions set the time (65536 tokens x 32 heads of 128 fp16, forward: 324 us,
+// now 172 = 6.3 TB/s; 131072 x 20 bf16, both passes 1769, now 571 = 5.9 TB/s).
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
@@ -49,8 +51,8 @@ struct Qk {
   int lanes;        // per head
   int steps;        // of 32 / lanes heads in a chunk
   int chunks[2];    // forward: of q's and k's heads together, in [0]
-  // tiles: heads and tokens in one, tiles along the heads and in all; slots of the ring and their bytes
-  int tile_heads[2], tile_tokens[2], tile_chunks[2];
+  // tiles: heads and tokens in one, tiles along the heads, heads between a lane's; tiles in all; slots of the ring and their bytes
+  int tile_heads[2], tile_tokens[2], tile_chunks[2], tile_apart[2];
   uint32_t along[2];  // tiles along a sequence, 0: there is one sequence
   uint32_t tiles[2];
   int slots, slot_bytes;
@@ -480,8 +482,7 @@ __device__ __forceinline__ Tile tile_at(const Qk& a, int k, uint32_t i) {
 // Persistent CTAs, the first ctas_q of them for q's heads, the others for k's, each with every (its CTAs)-th tile. The
 // angles of a lane's token in the next tile are on their way to its registers while it works on this one, from the L1
 // for all heads of a token but the first, and the position in the tile after that. (Rows of angles brought into the
-// ring by one warp, by bulk copies or 16 bytes a lane, took that warp 100 ns a token: 255 us in place of @@ for 65536
-// tokens of 32 heads of 128 fp16.)
+// ring by one warp, by bulk copies or 16 bytes a lane, took that warp 100 ns a token.)
 template <typename T, typename W, int V, bool INTER, bool BACK>
 __global__ void __launch_bounds__(32 * kWarps, 2)
     qk_tile_kernel(const __grid_constant__ QkMaps maps, const __grid_constant__ Qk a) {
@@ -512,14 +513,16 @@ __global__ void __launch_bounds__(32 * kWarps, 2)
     for (int s = 0; s < a.slots && !held; ++s)
       if (cta + s * ctas < a.tiles[k]) request(cta + s * ctas, s);
   }
-  const int lanes = a.lanes, lane = lane32 & (lanes - 1), row = threadIdx.x / lanes;
+  // a lane has heads in_tile, in_tile + apart, ... of a token in the tile
+  const int lanes = a.lanes, lane = lane32 & (lanes - 1), group = threadIdx.x / lanes, apart = a.tile_apart[k];
   const Units<V, INTER> un{a.dim, a.rotary};
-  const int all = a.heads[k], in_tile = row % HB, token_in_tile = row / HB;
+  const int in_tile = group % apart, token_in_tile = group / apart;
   const bool real = token_in_tile < TB;
   // (a lane without a head of the tile's reads another one's, and stores nothing)
-  const int from = (real ? row : 0) * a.dim;
+  const int from = (real ? token_in_tile * HB + in_tile : 0) * a.dim;
   const Heads& o = a.out[k];
   T* const out = static_cast<T*>(o.p) + (int64_t)in_tile * o.head + (int64_t)token_in_tile * o.token;
+  const int64_t out_apart = (int64_t)apart * o.head;
   // the position of this lane's token in tile i; -1: there is none
   auto position = [&](uint32_t i) -> int64_t {
     if (a.rotary == 0 || !real || i >= a.tiles[k]) return -1;
@@ -541,9 +544,14 @@ __global__ void __launch_bounds__(32 * kWarps, 2)
   };
   Eight w, dw = times_one(0.f);
   weights<W>(a.w[k], un, lane, lanes, w);
+  // (backward there are no registers for two tiles' angles: they come for this tile, the position is there before)
   Angles turns;
-  bool in_table = angles_of(turns, position(cta));
-  int64_t next_at = position(cta + ctas);
+  bool in_table = true;
+  int64_t next_at = position(cta);
+  if (!BACK) {
+    in_table = angles_of(turns, next_at);
+    next_at = position(cta + ctas);
+  }
   __syncthreads();
   int s = 0;
   uint32_t parity = 0;
@@ -551,21 +559,51 @@ __global__ void __launch_bounds__(32 * kWarps, 2)
   for (uint32_t i = cta; i < a.tiles[k]; i += ctas) {
     const uint8_t* const slot = smem + s * a.slot_bytes;
     Angles next;
-    const bool next_in = angles_of(next, next_at);
-    next_at = position(i + 2 * ctas);
+    bool next_in = true;
+    if (BACK) {
+      in_table = angles_of(turns, next_at);
+      next_at = position(i + ctas);
+    } else {
+      next_in = angles_of(next, next_at);
+      next_at = position(i + 2 * ctas);
+    }
     // after a wait that ran out: nothing more is waited for, all results become NaN
     if (ok && !tc::mbar_wait(&full[s], parity, 2 * a.wait_ns)) {
       ok = false;
       if (a.status) atomicOr(a.status, kStatusTimeout);
     }
     ok = __all_sync(0xffffffffu, ok);
-    Raw<T, V> x, dy;
-    take(x, reinterpret_cast<const T*>(slot) + from, un, lane, lanes);
-    if (BACK) take(dy, reinterpret_cast<const T*>(slot + dy_at) + from, un, lane, lanes);
+    const Tile t = tile_at(a, k, i);
+    const int heads = min(HB, a.heads[k] - t.h0);  // of this tile
+    const bool there = real && t.t0 + token_in_tile < a.length, good = ok && in_table;
+    if (there && ok && !in_table && a.status) atomicOr(a.status, kStatusRange);
+    T* to = out + (int64_t)t.b * o.batch + (int64_t)t.t0 * o.token + (int64_t)t.h0 * o.head;
+    const T* at = reinterpret_cast<const T*>(slot) + from;
+    for (int h = in_tile; h - in_tile < heads; h += apart, to += out_apart, at += apart * a.dim) {
+      Raw<T, V> x, dy;
+      const bool live = there && h < heads;
+      const T* const own = h < HB ? at : at - apart * a.dim;
+      take(x, own, un, lane, lanes);
+      if (BACK) take(dy, reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(own) + dy_at), un, lane, lanes);
+      const Eight v = unpack<INTER>(x);
+      const float r = rsqrtf(fmaf(lanes_sum(dot(v, v), lanes), a.inv_dim, a.eps));
+      if constexpr (BACK) {
+        const Eight dm = turn<true>(unpack<INTER>(dy), turns);
+        const float gx = lanes_sum(dot(times(dm, w), v), lanes);
+        if (live) {  // (the exchanges above take all lanes)
+          const float rr = good ? r : NAN;
+          backward<INTER>(x, dm, rr, rr * (gx * a.inv_dim), w, dw);
+          store(to, x, un, lane, lanes);
+        }
+      } else if (live) {
+        forward<INTER>(x, good ? r : NAN, w, turns);
+        store(to, x, un, lane, lanes);
+      }
+    }
     __syncwarp();
     if (lane32 == 0) {
       asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&empty[s])) : "memory");
-      if (warp == 0 && ok && i != cta) {  // the slot before this one is free, or soon: what comes next there
+      if (warp == (s & (kWarps - 1)) && ok && i != cta) {  // the slot before this one is free, or soon: what comes next there
         const int before = s > 0 ? s - 1 : a.slots - 1;
         const uint64_t far = (uint64_t)i + (uint64_t)(a.slots - 1) * ctas;
         if (far < a.tiles[k]) {
@@ -577,26 +615,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2)
       s = 0;
       parity ^= 1;
     }
-    const Tile t = tile_at(a, k, i);
-    const Eight v = unpack<INTER>(x);
-    const float r = rsqrtf(fmaf(lanes_sum(dot(v, v), lanes), a.inv_dim, a.eps));
-    const bool live = real && t.h0 + in_tile < all && t.t0 + token_in_tile < a.length, good = ok && in_table;
-    if (live && ok && !in_table && a.status) atomicOr(a.status, kStatusRange);
-    T* const to = out + (int64_t)t.b * o.batch + (int64_t)t.t0 * o.token + (int64_t)t.h0 * o.head;
-    if constexpr (BACK) {
-      const Eight dm = turn<true>(unpack<INTER>(dy), turns);
-      const float gx = lanes_sum(dot(times(dm, w), v), lanes);
-      if (live) {  // (the exchanges above take all lanes)
-        const float rr = good ? r : NAN;
-        backward<INTER>(x, dm, rr, rr * (gx * a.inv_dim), w, dw);
-        store(to, x, un, lane, lanes);
-      }
-    } else if (live) {
-      forward<INTER>(x, good ? r : NAN, w, turns);
-      store(to, x, un, lane, lanes);
+    if (!BACK) {
+      turns = next;
+      in_table = next_in;
     }
-    turns = next;
-    in_table = next_in;
   }
   if (!ok) {  // copies in flight land before the shared memory goes away: far above a copy's time
     const uint64_t t0 = tc::globaltimer();
@@ -644,7 +666,7 @@ bool units_fit(const Heads& h, int V, size_t size, bool live) {
 }
 
 int unit_size(const Qk& a, size_t size, size_t w_size, bool backward) {
-  for (int V = (int)(16 / size); V > 1; V /= 2) {
+  for (int V = (int)(16 / size); V > 1; V = V > 2 ? 2 : 1) {  // (8 or 4, 2, 1)
     bool fit = a.dim / 2 % V == 0 && a.rotary / 2 % V == 0;
     for (int k = 0; k < 2; ++k) {
       const bool live = a.heads[k] > 0;
@@ -662,7 +684,7 @@ int unit_size(const Qk& a, size_t size, size_t w_size, bool backward) {
 template <typename F>
 cudaError_t with_unit(int V, F&& f) {
   if (V == 8) return f(std::integral_constant<int, 8>());
-  if (V == 4) return f(std::integral_constant<int, 4>());
+  if (V == 4) return f(std::integral_constant<int, 4>());  // (fp32)
   if (V == 2) return f(std::integral_constant<int, 2>());
   return f(std::integral_constant<int, 1>());
 }
@@ -720,7 +742,11 @@ bool heads_map(CUtensorMap* map, const Heads& h, const Qk& a, int k, uint32_t ba
 template <typename T, typename W, int V, bool INTER, bool BACK>
 cudaError_t tiles_t(Qk a, float* dq, float* dk, cudaStream_t s, bool& done) {
   done = false;
-  if (a.dim > 256) return cudaSuccess;
+  if (a.dim > 256 || a.dim * sizeof(T) % 16) return cudaSuccess;
+  for (int k = 0; k < 2; ++k)
+    if (a.heads[k] > 0 && !(units_fit(a.x[k], 16 / sizeof(T), sizeof(T), true) &&
+                            (!BACK || units_fit(a.dy[k], 16 / sizeof(T), sizeof(T), true))))
+      return cudaSuccess;
   uint32_t batch = a.tokens / a.length;
   // sequences that lie one behind the other are one
   a.period = a.length;
@@ -734,7 +760,7 @@ cudaError_t tiles_t(Qk a, float* dq, float* dk, cudaStream_t s, bool& done) {
   }
   const int per_lane = kPairs / V;
   for (a.lanes = 1; a.lanes * per_lane < a.dim / 2 / V;) a.lanes *= 2;
-  const int rows = kWarps * 32 / a.lanes;
+  const int rows = kWarps * 32 / a.lanes, several = sizeof(T) == 4 ? 1 : BACK ? 2 : 4;
   int64_t want[2];
   int bytes = 0;
   for (int k = 0; k < 2; ++k) {
@@ -743,8 +769,10 @@ cudaError_t tiles_t(Qk a, float* dq, float* dk, cudaStream_t s, bool& done) {
     for (const Heads* h : {&a.x[k], &a.dy[k]})
       if (h->p && ((a.heads[k] > 1 && h->head < a.dim) || (a.length > 1 && h->token < 1) || (batch > 1 && h->batch < 1)))
         return cudaSuccess;
-    a.tile_heads[k] = std::min(a.heads[k], rows);
-    a.tile_tokens[k] = rows / a.tile_heads[k];
+    // (a lane takes up to `several` heads of its token: what a tile costs beside its heads is shared by them)
+    a.tile_heads[k] = std::min({a.heads[k], rows * several, 256});
+    a.tile_apart[k] = (a.tile_heads[k] + several - 1) / several;
+    a.tile_tokens[k] = std::min(256, rows / a.tile_apart[k]);
     a.tile_chunks[k] = (a.heads[k] + a.tile_heads[k] - 1) / a.tile_heads[k];
     a.along[k] = batch > 1 ? (a.length + a.tile_tokens[k] - 1) / a.tile_tokens[k] : 0;
     const int64_t n = (int64_t)batch * ((a.length + a.tile_tokens[k] - 1) / a.tile_tokens[k]) * a.tile_chunks[k];
@@ -791,11 +819,9 @@ cudaError_t tiles_t(Qk a, float* dq, float* dk, cudaStream_t s, bool& done) {
 
 template <typename T, typename W, int V, bool INTER>
 cudaError_t fwd_t(Qk a, cudaStream_t s) {
-  if constexpr (V * sizeof(T) == 16) {
-    bool done;
-    const cudaError_t e = tiles_t<T, W, V, INTER, false>(a, nullptr, nullptr, s, done);
-    if (done || e != cudaSuccess) return e;
-  }
+  bool done;
+  const cudaError_t e = tiles_t<T, W, V, INTER, false>(a, nullptr, nullptr, s, done);
+  if (done || e != cudaSuccess) return e;
   constexpr int UN = sizeof(T) == 2 ? 4 : 2;
   const int units = a.dim / 2 / V, per_lane = kPairs / V;
   for (a.lanes = 1; a.lanes * per_lane < units;) a.lanes *= 2;
@@ -809,11 +835,9 @@ cudaError_t fwd_t(Qk a, cudaStream_t s) {
 
 template <typename T, typename W, int V, bool INTER>
 cudaError_t bwd_t(Qk a, float* dq, float* dk, cudaStream_t s) {
-  if constexpr (V * sizeof(T) == 16) {
-    bool done;
-    const cudaError_t e = tiles_t<T, W, V, INTER, true>(a, dq, dk, s, done);
-    if (done || e != cudaSuccess) return e;
-  }
+  bool done;
+  const cudaError_t tiled = tiles_t<T, W, V, INTER, true>(a, dq, dk, s, done);
+  if (done || tiled != cudaSuccess) return tiled;
   constexpr int UN = sizeof(T) == 2 ? 2 : 1;
   const int units = a.dim / 2 / V, per_lane = kPairs / V;
   for (a.lanes = 1; a.lanes * per_lane < units;) a.lanes *= 2;
@@ -935,7 +959,7 @@ soap_status_t layer_qk_forward(int64_t batch, int64_t length, int32_t heads, int
     using W = decltype(w);
     return with_unit(unit_size(a, size, sizeof(W), false), [&](auto v) {
       constexpr int V = decltype(v)::value;
-      if constexpr (V * sizeof(T) > 16) return cudaErrorInvalidValue;
+      if constexpr (V > 2 && V * sizeof(T) != 16) return cudaErrorInvalidValue;
       else return interleaved ? fwd_t<T, W, V, true>(a, s) : fwd_t<T, W, V, false>(a, s);
     });
   });
@@ -991,7 +1015,7 @@ soap_status_t layer_qk_backward(int64_t batch, int64_t length, int32_t heads, in
     using W = decltype(w);
     return with_unit(unit_size(a, size, sizeof(W), true), [&](auto v) {
       constexpr int V = decltype(v)::value;
-      if constexpr (V * sizeof(T) > 16) return cudaErrorInvalidValue;
+      if constexpr (V > 2 && V * sizeof(T) != 16) return cudaErrorInvalidValue;
       else
         return interleaved ? bwd_t<T, W, V, true>(a, d_qweight, d_kweight, s)
                            : bwd_t<T, W, V, false>(a, d_qweight, d_kweight, s);
