@@ -73,7 +73,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
   const int64_t slices[3] = {up_div(hidden, 64), (backward ? 2 : 1) * (int64_t)up_div(width, 64), up_div(rows, 64)};
   for (int p = 0; p < 3; ++p) {
-    const int64_t parts = std::max<int64_t>(1, slices[p] / 4), longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
+    const int64_t parts = slices[p] < kMinParted ? 1 : slices[p] / 4, longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
     l.units += l.tiles[p] * std::max(parts, longest);
     // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights'
     // gradients: of groups with more than kMaxSlices slices, less than three parts for each such run of all rows)

@@ -10,7 +10,8 @@ namespace ffn {
 
 constexpr int kMaxGroups = 1024;
 constexpr int kSms = 152;           // that a product's parts are shared out among, one or a pair for each
-constexpr int kMaxSlices = 1024;    // most slices of 64 products that one accumulator adds up
+constexpr int kMinParted = 24;      // fewer slices of 64 products stay in one part
+constexpr int kMaxSlices = 1024;    // most slices that one accumulator adds up
 
 // Maps that end at a group's last row, so that loads of its rows give 0 beyond it and stores leave the rows behind it
 // alone: results (boxes of 32 x 32) and factors of the weights' gradients (boxes of 64 x 64).

@@ -51,7 +51,6 @@ constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
 // slots, of which each takes both CTAs' loading threads, and one of two accumulators)
 constexpr int kKept = 16;
 constexpr int kRun = 4;             // slices in a run of fp32 operands
-constexpr int kMinPart = 4;         // slices in a part along K, at least
 
 struct Unit {
   int kind, group, prod;
@@ -605,9 +604,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         return reinterpret_cast<float4*>(a.partial[phase]) +
                (((int64_t)(u.slot + (part - u.part) * u.tiles) * kPerTile + share) * 4 + i) * 256 + lane;
       };
-      auto last_part = [&](int i) {
+      auto parts_stored = [&] {  // this part's sums come before its counts
         __threadfence();
         __syncwarp();
+      };
+      auto last_part = [&](int i) {
         int there = 0;
         if (lane == 0) there = atomicAdd(a.count[phase] + (u.tile * kPerTile + share) * 4 + i, 1);
         __threadfence();
@@ -657,29 +658,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int ac = n & 1;
         if (!wait_acc(ac)) break;
         const uint32_t t = t0 + static_cast<uint32_t>(ac * 256);
-        if (blocks == 0) release_acc(ac);
+        if (u.splits > 1) {
+          for (int i = 0; i < (gated ? 2 * blocks : blocks); ++i) {  // (g's and u's blocks in turn)
+            float v[32];
+            tmem_ld32(t + (gated ? 128 * (i & 1) + 32 * (i >> 1) : 32 * i), v);
+            put_lines(partial_at(u.part, i), v);
+          }
+          release_acc(ac);
+          parts_stored();
+        } else if (blocks == 0) {
+          release_acc(ac);
+        }
         for (int j = 0; j < blocks; ++j) {
           const int i = turned(j);
+          if (u.splits > 1 && !last_part(i)) continue;
           float v[32];
           if (gated) {
             float w[32];
-            tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
-            if (j + 1 == blocks) release_acc(ac);
             if (u.splits > 1) {
-              put_lines(partial_at(u.part, 2 * i), v);
-              put_lines(partial_at(u.part, 2 * i + 1), w);
-              if (!last_part(i)) continue;
               add_parts(2 * i, v);
               add_parts(2 * i + 1, w);
+            } else {
+              tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
+              if (j + 1 == blocks) release_acc(ac);
             }
             finish_gated(i, v, w);
           } else {
-            tmem_ld32(t + 32 * i, v);
-            if (j + 1 == blocks) release_acc(ac);
             if (u.splits > 1) {
-              put_lines(partial_at(u.part, i), v);
-              if (!last_part(i)) continue;
               add_parts(i, v);
+            } else {
+              tmem_ld32(t + 32 * i, v);
+              if (j + 1 == blocks) release_acc(ac);
             }
             finish(i, v);
           }
@@ -712,6 +721,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int b = 0; b < 4; ++b) {
             if (gated ? (b & 1) < blocks : b < blocks) put_lines(partial_at(u.part, gated ? 2 * (b & 1) + b / 2 : b), sum[b]);
           }
+          parts_stored();
           for (int j = 0; j < blocks; ++j) {
             const int i = turned(j);
             if (!last_part(i)) continue;
@@ -801,10 +811,12 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
 }
 
 // Parts along K of a tile of `slices` slices (0: none), where there may be `most` for the pairs' sake: a part of p
-// costs its slices' time, 0.3 us each, and adding up p parts about as much for each, least at p = sqrt(slices).
+// costs its slices' time, 0.3 us each, and adding up p parts 5 us and about as much as a slice for each, so that
+// short sums stay whole, and the best p for others is about sqrt(slices).
 __device__ __forceinline__ int parts_of(int slices, int most) {
   if (slices == 0) return 0;
-  return max(max(1, up_div(slices, kMaxSlices)), min(most, min(slices / kMinPart, (int)sqrtf((float)slices))));
+  const int whole = max(1, up_div(slices, kMaxSlices));
+  return slices < kMinParted ? whole : max(whole, min(most, (int)sqrtf((float)slices)));
 }
 
 // The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
