@@ -368,21 +368,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = mbar_wait(&given[q & 1], turn, 2 * lim);
             if (!(ok = __all_sync(0xffffffffu, ok))) break;
             T* const h = static_cast<T*>(a.h) + (row0 + c * kChunk) * a.ld_h + f;
-            if (a.act == LAYER_SILU) {
+            float w[kChunk];
 #pragma unroll
-              for (int j = 0; j < kChunk; ++j) {
-                float act, slope;
-                activation<TYPE, LAYER_SILU>(v[j], act, slope);
-                v[j] = act * box[32 * j];
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < kChunk; ++j) {
-                float act, slope;
-                activation<TYPE, LAYER_GELU>(v[j], act, slope);
-                v[j] = act * box[32 * j];
-              }
-            }
+            for (int j = 0; j < kChunk; ++j) w[j] = box[32 * j];
+            if (a.act == LAYER_SILU)
+              gate<TYPE, LAYER_SILU>(v, w);
+            else
+              gate<TYPE, LAYER_GELU>(v, w);
 #pragma unroll
             for (int j = 0; j < kChunk; ++j)
               if (j < left && f < a.width) h[j * a.ld_h] = from_f32<T>(v[j]);

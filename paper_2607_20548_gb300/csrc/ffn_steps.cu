@@ -42,8 +42,10 @@ using namespace tc;
 enum Kind { kEnd = -1, kGated, kGrad, kOut, kWeight };
 
 constexpr int kEpiWarps = 8;
-constexpr int kLoadB = 2 + kEpiWarps, kScout = kLoadB + 1;  // warps
-constexpr int kThreads = 32 * (kScout + 1);
+constexpr int kLoadB = 2, kScout = 3, kFirstEpi = 4;  // warps
+constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
+// registers of a launch's 168 per thread as the roles' warps share them: 4 x 72 + 8 x 216 = 12 x 168
+constexpr int kFewRegisters = 72, kManyRegisters = 216;
 constexpr int kStages = 5, kStage = 2 * kTile;
 constexpr int kStaging = 8192;      // per epilogue warp
 constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
@@ -326,6 +328,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch before has ended: so far, nothing of it was read
   const uint32_t tmem = *tmem_at;
 
+  if (!SPLIT && warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   if (warp == kScout) {
     bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
     const Plan& l = *a.plan;
@@ -488,9 +491,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (!st.ok) *abort_flag = 1;
     }
   } else {
+    if (!SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
     const int q = warp & 3;           // accumulator lanes 32 q .. 32 q + 31
-    const int half = (warp - 2) / 4;  // of the columns
-    uint8_t* stage = staging + (warp - 2) * kStaging;
+    const int half = (warp - kFirstEpi) / 4;  // of the columns
+    uint8_t* stage = staging + (warp - kFirstEpi) * kStaging;
     constexpr int kSlot = SPLIT ? 4096 : 2048, kSlots = kStaging / kSlot;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16);
     const int pre_cols = (a.width + 31) / 32;  // blocks
@@ -578,28 +582,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           gate<TYPE, LAYER_GELU>(v, w);
         to_operand(kH, v, col);
       };
-      // block i of any other product
-      auto finish = [&](int i, float (&v)[32]) {
+      // block i of dh, whose g and u are in g and up; then the next block's (next, if any) come
+      auto finish_grad = [&](int i, float (&v)[32], float (&g)[32], float (&up)[32], int next) {
         const int col = c0 + 32 * i;
-        if (u.kind != kGrad) {
-          to_result(v, col);
-          return;
-        }
-        float g[32], up[32];
-        get_lines(pre_at(0, col), g);
-        get_lines(pre_at(1, col), up);
         if (a.act == LAYER_SILU)
           gate_back<TYPE, LAYER_SILU>(g, up, v);
         else
           gate_back<TYPE, LAYER_GELU>(g, up, v);
         to_operand(kDG, g, col);
-        to_operand(kDU, v, col);
+        if (next < blocks) get_lines(pre_at(0, c0 + 32 * next), g);
         if (a.params) to_operand(kH, up, col);
+        if (next < blocks) get_lines(pre_at(1, c0 + 32 * next), up);
+        to_operand(kDU, v, col);
       };
       // Parts along K: each stores its sums, and the one that is the last to store a block adds up all of them in the
       // parts' order. A part begins with a block of its own, so that parts that end together finish different blocks.
       const int phase = u.kind == kWeight ? 2 : u.kind == kOut;
-      const int share = rank * kEpiWarps + warp - 2;
+      const int share = rank * kEpiWarps + warp - kFirstEpi;
       auto partial_at = [&](int part, int i) {
         return reinterpret_cast<float4*>(a.partial[phase]) +
                (((int64_t)(u.slot + (part - u.part) * u.tiles) * kPerTile + share) * 4 + i) * 256 + lane;
@@ -656,9 +655,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (u.part > 0) finished = 0;
       if constexpr (!SPLIT) {
         const int ac = n & 1;
-        if (!wait_acc(ac)) break;
         const uint32_t t = t0 + static_cast<uint32_t>(ac * 256);
-        if (u.splits > 1) {
+        const bool whole = u.splits == 1;
+        float g[32], up[32];  // of the block that is next
+        if (u.kind == kGrad && whole && blocks > 0) {  // (the first block's come while the products are formed)
+          get_lines(pre_at(0, c0), g);
+          get_lines(pre_at(1, c0), up);
+        }
+        if (!wait_acc(ac)) break;
+        if (!whole) {
           for (int i = 0; i < (gated ? 2 * blocks : blocks); ++i) {  // (g's and u's blocks in turn)
             float v[32];
             tmem_ld32(t + (gated ? 128 * (i & 1) + 32 * (i >> 1) : 32 * i), v);
@@ -671,26 +676,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         for (int j = 0; j < blocks; ++j) {
           const int i = turned(j);
-          if (u.splits > 1 && !last_part(i)) continue;
+          if (!whole && !last_part(i)) continue;
           float v[32];
           if (gated) {
             float w[32];
-            if (u.splits > 1) {
-              add_parts(2 * i, v);
-              add_parts(2 * i + 1, w);
-            } else {
+            if (whole) {
               tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
               if (j + 1 == blocks) release_acc(ac);
+            } else {
+              add_parts(2 * i, v);
+              add_parts(2 * i + 1, w);
             }
             finish_gated(i, v, w);
           } else {
-            if (u.splits > 1) {
-              add_parts(i, v);
-            } else {
+            if (whole) {
               tmem_ld32(t + 32 * i, v);
               if (j + 1 == blocks) release_acc(ac);
+            } else {
+              add_parts(i, v);
             }
-            finish(i, v);
+            if (u.kind == kGrad) {
+              if (!whole) {
+                get_lines(pre_at(0, c0 + 32 * i), g);
+                get_lines(pre_at(1, c0 + 32 * i), up);
+              }
+              finish_grad(i, v, g, up, whole ? i + 1 : blocks);
+            } else {
+              to_result(v, c0 + 32 * i);
+            }
           }
           ++finished;
         }
@@ -731,8 +744,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               float w[32];
               add_parts(2 * i + 1, w);
               finish_gated(i, v, w);
+            } else if (u.kind == kGrad) {
+              float g[32], up[32];
+              get_lines(pre_at(0, c0 + 32 * i), g);
+              get_lines(pre_at(1, c0 + 32 * i), up);
+              finish_grad(i, v, g, up, blocks);
             } else {
-              finish(i, v);
+              to_result(v, c0 + 32 * i);
             }
             ++finished;
           }
@@ -742,8 +760,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (b >= blocks) break;
             if (gated) {
               if (b < 2) finish_gated(b, sum[b], sum[b + 2]);
+            } else if (u.kind == kGrad) {
+              float g[32], up[32];
+              get_lines(pre_at(0, c0 + 32 * b), g);
+              get_lines(pre_at(1, c0 + 32 * b), up);
+              finish_grad(b, sum[b], g, up, blocks);
             } else {
-              finish(b, sum[b]);
+              to_result(sum[b], c0 + 32 * b);
             }
             ++finished;
           }
