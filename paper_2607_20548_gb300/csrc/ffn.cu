@@ -40,12 +40,31 @@ bool few_rows(int64_t rows, int groups, int type, bool backward) {
   return !backward && type != SOAP_F32 && rows <= 64 * (int64_t)groups;
 }
 
+// Planes that h, dg and du are kept in: fp32 three of bf16; 16-bit types their rounding, and for few rows and small
+// weights, where a few latencies set the time, what that leaves too (100 rows over 8 groups of 256 x 512 bf16, both
+// passes: 2% longer, and y, dx and the weights' gradients as near as one rounding; with large weights it is worth
+// less than it takes: 24 rows of 2048 x 8192 128 us in one plane, 152 in two, 192 rows over 64 groups of 2048 x 768
+// forward 99 and 111).
+int planes_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type) {
+  return type == SOAP_F32 ? 3 : rows <= 64 * (int64_t)groups && groups * hidden * width <= 1 << 23 ? 2 : 1;
+}
+
 Tiles tiles_of(int64_t rows, int groups, int type, bool backward) {
   if (!few_rows(rows, groups, type, backward)) return Tiles{256, {backward ? 256 : 128, 256}, kSms / 2, 256 * 256, 64};
   const int64_t each = groups == 1 ? rows : (rows + rows / 2) / groups;
   int n = 16;
   while (n < each && n < 128) n *= 2;
   return Tiles{n, {64, 128}, kSms, 128 * n, 4 * std::max(1, n / 32)};
+}
+
+// Slices of a tile's sums, per phase (of the weights' gradients: of all rows). Planes of 16-bit types are added one
+// after the other, but for few rows, where one load of the weights serves both.
+struct Slices {
+  int64_t n[3];
+};
+Slices slices_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool backward) {
+  const int twice = backward && type != SOAP_F32 && planes_of(rows, hidden, width, groups, type) == 2 ? 2 : 1;
+  return Slices{{up_div(hidden, 64), twice * (backward ? 2 : 1) * (int64_t)up_div(width, 64), twice * (int64_t)up_div(rows, 64)}};
 }
 
 // Where everything lies in the workspace.
@@ -71,7 +90,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   l.tiles[1] = l.row_tiles * up_div(hidden, t.cols[1]);
   const int64_t each = 3 * (int64_t)up_div(width, 256) * up_div(hidden, 256);
   l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
-  const int64_t slices[3] = {up_div(hidden, 64), (backward ? 2 : 1) * (int64_t)up_div(width, 64), up_div(rows, 64)};
+  const auto [slices] = slices_of(rows, hidden, width, groups, type, backward);
   for (int p = 0; p < 3; ++p) {
     const int64_t parts = slices[p] < kMinParted ? 1 : slices[p] / 4, longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
     l.units += l.tiles[p] * std::max(parts, longest);
@@ -93,7 +112,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   for (int p = 0; p < 3; ++p) l.partial[p] = take((size_t)l.slots[p] * t.partial * 4);
   const size_t planes = type == SOAP_F32 ? 3 : 1;
   l.inter_plane = (size_t)rows * up8(width);
-  for (int i = 0; i < (backward ? 3 : 1); ++i) l.inter[i] = take(planes * l.inter_plane * 2);
+  for (int i = 0; i < (backward ? 3 : 1); ++i) l.inter[i] = take(planes_of(rows, hidden, width, groups, type) * l.inter_plane * 2);
   if (copies || type == SOAP_F32) {
     l.x_plane = (size_t)rows * up8(hidden);
     l.x = take(planes * l.x_plane * 2);
@@ -262,9 +281,12 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
   a.col_tile[0] = t.cols[0];
   a.col_tile[1] = t.cols[1];
   a.pool = t.pool;
+  const int kept = planes_of(c.rows, c.hidden, c.width, c.groups, c.type);
+  a.plane_bits = c.type != SOAP_F32 && kept == 2;
   if (few) {
     a.h = c.ws + l.inter[0];
     a.ld_h = up8(c.width);
+    a.h_plane = (int64_t)l.inter_plane;
   }
   a.clips = c.offsets && c.rows > 0 && !few ? reinterpret_cast<const CUtensorMap*>(c.ws + l.clips) : nullptr;
   a.backward = c.backward;
@@ -278,7 +300,8 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
   a.b_columns[1] = c.backward ? gate.columns != 0 : down.columns == 0;
   a.kblocks[0] = up_div(c.hidden, 64);
   a.kblocks[1] = up_div(c.width, 64);
-  a.segments = c.backward ? 2 : 1;
+  const Slices n = slices_of(c.rows, c.hidden, c.width, c.groups, c.type, c.backward);
+  for (int p = 0; p < 2; ++p) a.slices[p] = (int)n.n[p];
   // a gradient in its weight's order: of a column-major weight the transposed product
   const int left[3] = {kInX, kInX, kInH}, right[3] = {kInDG, kInDU, kInDY};
   for (int p = 0; p < 3; ++p) {
@@ -302,7 +325,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
   if (c.rows > 0) {
     View inter[3];
     for (int i = 0; i < 3; ++i)
-      inter[i] = View{c.ws + l.inter[i], c.rows, up8(c.width), (int64_t)l.inter_plane, c.width, planes};
+      inter[i] = View{c.ws + l.inter[i], c.rows, up8(c.width), (int64_t)l.inter_plane, c.width, kept};
     const int box = few ? t.rows : 128;
     bool ok = make_map(&maps.a0, v[c.backward ? 1 : 0], etype, 64, box) &&
               make_map(&maps.a1[0], inter[c.backward ? 1 : 0], etype, 64, box) &&

@@ -55,9 +55,11 @@ struct Args {
   int groups, rows, hidden, width;
   int row_tile, col_tile[2], pool;
   void* h;                      // few rows: where the first phase's results go
-  int64_t ld_h;
+  int64_t ld_h, h_plane;
+  int plane_bits;               // log2 of the planes of h, dg and du (16-bit types)
   int b_columns[2];             // whether the second factor of a row phase has its K dimension outermost
-  int kblocks[2], segments;     // slices per factor pair; pairs of the second phase
+  int kblocks[2];               // slices of a factor pair, per row phase
+  int slices[2];                // of a tile, per row phase: of all pairs and planes that are added
   int wa[3], wb[3];             // Clip of the factors of the weights' gradients
   int wrows[3], wcols[3];       // sides of the weights' gradients as they are stored
   int act;

@@ -96,6 +96,13 @@ __device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float 
   }
 }
 
+// What the rounding of x to a type has left (nothing of what is not finite there).
+template <typename T>
+__device__ __forceinline__ float rest_of(float x, T rounded) {
+  const float r = to_f32(rounded);
+  return fabsf(r) < INFINITY ? x - r : 0.f;
+}
+
 // 32 elements of this lane's row to or from a block in which the rows' 16-byte pieces lie side by side (at p: this
 // lane's first).
 __device__ __forceinline__ void put_lines(float4* p, const float (&v)[32]) {

@@ -8,6 +8,9 @@
 // memory. An MMA that adds to the accumulator of the one before takes 140 cycles however narrow: the slices' four go to
 // accumulators of their own, which the epilogue adds up.
 //
+// Where h is kept as two planes, its rounding to the type and what that leaves, both products come from one load of the
+// weights, and h's rounding does not reach y.
+//
 // A CTA per SM takes units from one list, as in ffn_steps.cu: the first phase's tiles, then parts along K of the
 // second's. One warp takes units, one loads weights (which wait for nothing: while the first phase ends, the ring, all
 // of shared memory, fills with the second's), one loads rows, one issues the MMAs, four drain the accumulators.
@@ -47,14 +50,14 @@ struct Unit {
 template <int NT>
 struct Config {
   static constexpr int kRowsTile = NT * 128;           // 64 elements of each of NT rows
-  static constexpr int kStage = kTile + kRowsTile;
-  static constexpr int kStages = 204800 / kStage;
+  static constexpr int kRing = 204800;
+  static constexpr int kMostStages = kRing / (kTile + kRowsTile);
   static constexpr int kAcc = NT <= 64 ? 4 : 2;        // accumulators of a unit
   static constexpr int kChunk = NT < 32 ? NT : 32;     // rows that a thread drains at a time
   static constexpr int kChunks = NT / kChunk;
   static constexpr uint32_t kColumns = 2 * kAcc * NT;  // of tensor memory
-  static constexpr int kSmem = 1024 + kStages * kStage + 2 * 32 * 32 * 4 + kKept * (int)sizeof(Unit) + 512;
-  static_assert(kSmem <= 232448 && kStages + 4 <= kKept, "shared memory");
+  static constexpr int kSmem = 1024 + kRing + 2 * 32 * 32 * 4 + kKept * (int)sizeof(Unit) + 512;
+  static_assert(kSmem <= 232448 && kMostStages + 4 <= kKept, "shared memory");
 };
 
 __host__ __device__ constexpr uint32_t idesc_few(bool bf16, int a_mn, int n) {
@@ -128,7 +131,7 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
   u.n0 = n * wide;
   u.m0 = m * NT;
   u.row_tile += m;
-  const int slices = a.kblocks[phase];
+  const int slices = a.slices[phase];
   u.s0 = (int)((int64_t)slices * u.part / u.splits);
   u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   return u;
@@ -139,14 +142,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
   using T = typename Element<TYPE>::T;
   using C = Config<NT>;
-  constexpr int kStages = C::kStages, kStage = C::kStage, kAcc = C::kAcc, kChunk = C::kChunk;
+  constexpr int kAcc = C::kAcc, kChunk = C::kChunk;
+  const int planes = 1 + a.plane_bits;  // of h, whose tiles lie beside one another
+  const int kStage = kTile + planes * C::kRowsTile, kStages = C::kRing / kStage;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* handed = reinterpret_cast<float*>(smem + kStages * kStage);  // [2][rows][features]: u's values for a warp of g's
+  float* handed = reinterpret_cast<float*>(smem + C::kRing);  // [2][rows][features]: u's values for a warp of g's
   Unit* units = reinterpret_cast<Unit*>(handed + 2 * 32 * 32);
   uint64_t* full = reinterpret_cast<uint64_t*>(units + kKept);
-  uint64_t* empty = full + kStages;
-  uint64_t* acc_full = empty + kStages;
+  uint64_t* empty = full + C::kMostStages;
+  uint64_t* acc_full = empty + C::kMostStages;
   uint64_t* acc_empty = acc_full + 2;
   uint64_t* given = acc_empty + 2;  // per half: u's values are there; they have been taken
   uint64_t* got = given + 2;
@@ -254,8 +259,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int k = kb * BK;
           if (of_rows) {
             load_box(slot + kTile, m0, &full[st.s], k, u.start + u.m0, 0);
+            if (phase && planes > 1) load_box(slot + kTile + C::kRowsTile, m0, &full[st.s], k, u.start + u.m0, 1);
           } else {
-            expect_tx(&full[st.s], kStage);
+            expect_tx(&full[st.s], kTile + (phase ? planes : 1) * C::kRowsTile);
             load_box(slot, m0, &full[st.s], mn ? at0 : k, mn ? k : at0, u.group);
             load_box(slot + kBox, m1, &full[st.s], mn ? at1 : k, mn ? k : at1, u.group);
           }
@@ -304,6 +310,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < BK / 16; ++kk)
             mma(d + (kk % kAcc) * NT, mn ? tile_desc<1>(as, kk) : tile_desc<0>(as, kk), tile_desc<0>(bs, kk), idesc,
                 i > 0 || kk >= kAcc);
+          if (kind == kOut && planes > 1) {
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk)
+              mma(d + (kk % kAcc) * NT, mn ? tile_desc<1>(as, kk) : tile_desc<0>(as, kk),
+                  tile_desc<0>(bs + C::kRowsTile, kk), idesc, 1);
+          }
           umma_commit(&empty[st.s]);
           if (++st.s == kStages) {
             st.s = 0;
@@ -377,7 +389,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               gate<TYPE, LAYER_GELU>(v, w);
 #pragma unroll
             for (int j = 0; j < kChunk; ++j)
-              if (j < left && f < a.width) h[j * a.ld_h] = from_f32<T>(v[j]);
+              if (j < left && f < a.width) {
+                const T upper = from_f32<T>(v[j]);
+                h[j * a.ld_h] = upper;
+                if (planes > 1) h[a.h_plane + j * a.ld_h] = from_f32<T>(rest_of(v[j], upper));
+              }
             __syncwarp();
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&got[q & 1])) : "memory");
           }

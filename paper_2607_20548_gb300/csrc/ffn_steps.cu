@@ -148,7 +148,7 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
     u.n0 = n * wide;
     u.row_tile += m;
     u.block += m * 8;
-    const int slices = a.kblocks[phase] * (phase == 1 ? a.segments : 1);
+    const int slices = a.slices[phase];
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   } else {
@@ -179,7 +179,7 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
     tile_place(i, up_div(u.M, 256), up_div(u.N, 256), m, n);
     u.m0 = m * 256;
     u.n0 = n * 256;
-    const int slices = up_div(rows, BK);
+    const int slices = up_div(rows, BK) << a.plane_bits;
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   }
@@ -208,15 +208,17 @@ struct Loader {
 };
 
 template <int MN>
-__device__ __forceinline__ void load_run(Loader& l, int kb, int to, int kblocks, int k_at, const CUtensorMap* m0,
-                                         const CUtensorMap* m1, int row, int z, uint32_t bytes) {
-  for (; kb < to; ++kb) {
+__device__ __forceinline__ void load_run(Loader& l, int from, int to, int kblocks, int k_at, const CUtensorMap* m0,
+                                         const CUtensorMap* m1, int row, int z, uint32_t bytes, int bits, int planes) {
+  for (; from < to; ++from) {
+    // (slices of both planes one after the other, so that the other factor's second load comes from L2)
+    const int kb = from >> bits;
     Ring& st = l.st;
     if (!(st.ok = mbar_wait(&l.empty[st.s], st.parity, l.lim))) return;
     if (bytes) expect_tx(&l.full[st.s], bytes);
     const bool second = kb >= kblocks;
     load_tile<MN>(l.ring + st.s * kStage, second ? m1 : m0, l.bars + st.s * 8, row,
-                  k_at + (second ? kb - kblocks : kb) * BK, z);
+                  k_at + (second ? kb - kblocks : kb) * BK, z + (from & planes));
     if (++st.s == kStages) {
       st.s = 0;
       st.parity ^= 1;
@@ -400,12 +402,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!is_b) set_ready(begun_at, m + 1);
         const CUtensorMap *m0, *m1;
         int row, z = 0, planes = 0, kblocks, k_at = 0;
-        bool mn;
+        bool mn, of_planes = false;  // whether the planes are this factor's
         if (u.kind == kWeight) {
           const int which = is_b ? a.wb[u.prod] : a.wa[u.prod];
           m0 = m1 = a.clips ? a.clips + u.group * kClips + which : &maps.clip[which];
           if (a.clips) fence_map(m0);
           row = (is_b ? u.n0 : u.m0) + rank * 128;
+          of_planes = which >= kInH;
           kblocks = INT_MAX;
           k_at = u.start;
           planes = 1;
@@ -418,6 +421,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             m1 = phase ? &maps.a1[1] : m0;
             row = u.start + u.m0 + rank * 128;
             planes = 1;
+            of_planes = phase;
             mn = false;
           } else {
             m0 = phase ? &maps.w1[0] : &maps.w0[u.kind == kGated ? rank : 0];
@@ -429,15 +433,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
         }
         const uint32_t bytes = rank != 0 || is_b ? 0 : 2 * kStage;
+        const int bits = u.kind >= kOut ? a.plane_bits : 0, plane = of_planes ? bits : 0;
         used = min(used + (u.s1 - u.s0) * O::kTermsOf, kStages);
         for (int kb = u.s0; kb < u.s1 && l.st.ok;) {
           const int to = O::end_of_run(kb, u.s1);
           for (int t = 0; t < O::kTermsOf && l.st.ok; ++t) {
             const int zt = z + (SPLIT ? (is_b ? term_b(t) : term_a(t)) * planes : 0);
             if (mn)
-              load_run<1>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes);
+              load_run<1>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane);
             else
-              load_run<0>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes);
+              load_run<0>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane);
           }
           kb = to;
         }
@@ -532,8 +537,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
       // h, dg or du: to the second phase's (and the weights' gradients') operand
       auto to_operand = [&](Clip which, float (&v)[32], int col) {
-#pragma unroll
-        for (int plane = 0; plane < (SPLIT ? 3 : 1); ++plane) {
+#pragma unroll 1  // (instructions that are fetched once)
+        for (int plane = 0; plane <= (SPLIT ? 2 : a.plane_bits); ++plane) {
           uint8_t* const slot = next_slot();
           if constexpr (SPLIT) {
             float w[32];
@@ -542,6 +547,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             put<__nv_bfloat16>(slot, w, lane);
           } else {
             put<T>(slot, v, lane);
+            if (plane < a.plane_bits) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = rest_of(v[j], from_f32<T>(v[j]));
+            }
           }
           send(clips + which, slot, col, u.start + r0, plane);
         }
@@ -863,7 +872,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       int tiles = 0, blocks = 0, parts = 0, slots = 0;  // of the groups before
       for (int g0 = 0; g0 <= a.groups; g0 += 32) {
         const int g = g0 + lane, len = length(g);
-        const int n = a.params ? parts_of(up_div(len, BK), most) : 0;
+        const int n = a.params ? parts_of(up_div(len, BK) << a.plane_bits, most) : 0;
         int4 v = make_int4(up_div(len, a.row_tile), up_div(len, 32), n, n > 1 ? n : 0);
         const int4 own = v;
         for (int d = 1; d < 32; d *= 2) {
@@ -889,7 +898,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
           const int n = tiles * up_div(p == 0 ? a.width : a.hidden, a.col_tile[p]);
           l.first[p] = at;
           l.tiles[p] = n;
-          l.splits[p] = n > 0 ? parts_of(a.kblocks[p] * (p == 1 ? a.segments : 1), a.pool / n) : 1;
+          l.splits[p] = n > 0 ? parts_of(a.slices[p], a.pool / n) : 1;
           if (p == 0 && a.h) l.splits[p] = 1;  // (few rows: g and u meet in the tile)
           at += n * l.splits[p];
         }

@@ -151,7 +151,9 @@ def test_slices(cuda, t, pad):
 
 
 @pytest.mark.parametrize("t,rows,hidden,width", [(BF, 24, 1024, 2048), (BF, 2000, 512, 1024), (F32, 600, 512, 768),
-                                                 (HF, 5000, 128, 64), (BF, 1, 4096, 64), (F32, 3000, 64, 64)])
+                                                 (HF, 5000, 128, 64), (BF, 1, 4096, 64), (F32, 3000, 64, 64), (HF, 60, 128, 1000),
+                                                 (BF, 64, 64, 2100), (BF, 20, 2100, 100), (BF, 65, 100, 4000),
+                                                 (HF, 17, 1600, 1600)])
 def test_larger(cuda, t, rows, hidden, width):
     _run(cuda, [rows], hidden, width, t, dense=True)
 
@@ -160,6 +162,24 @@ def test_larger(cuda, t, rows, hidden, width):
 def test_serving(cuda, t):
     _run(cuda, [1], 512, 1536, t, dense=True, train=False)
     _run(cuda, [2, 0, 1, 7], 256, 192, t, train=False, behind=2)
+
+
+@pytest.mark.parametrize("rows,hidden,width", [(1, 512, 512), (64, 300, 200)])
+@pytest.mark.parametrize("t", [BF, HF])
+def test_few_rows_and_small_weights_round_once(cuda, t, rows, hidden, width):
+    """h, dg and du are kept to twice the type's bits: the results' own rounding is all that is left of 16 bits."""
+    x, dy, w, _ = _operands(cuda, [rows], hidden, width, t, dense=True)
+    y, pre = ffn_forward(x, *w, keep=True)
+    got = [y, *ffn_backward(dy, x, pre, *w)]
+    leaves = [v.double().requires_grad_() for v in (x, *w)]
+    g = leaves[0] @ leaves[1]
+    out = (g * torch.sigmoid(g) * (leaves[0] @ leaves[2])) @ leaves[3]
+    want = [out.detach(), *torch.autograd.grad(out, leaves, dy.double())]
+    for a, b in zip(got, want):
+        # a rounding's error is spread evenly over a step of 2^-m to 2^(1-m) of the value, at most 0.58 of half the
+        # step's largest part in root mean square; fp16's smallest steps do not count here
+        err = float((a.double() - b).norm() / b.norm())
+        assert err <= 0.6 * HALF[t] + 1e-5, err
 
 
 def test_leading_dimensions_and_without_params(cuda):
