@@ -59,6 +59,7 @@ Tiles tiles_of(int64_t rows, int groups, int type, bool backward) {
 
 // Slices of a tile's sums, per phase (of the weights' gradients: of all rows). Planes of 16-bit types are added one
 // after the other, but for few rows, where one load of the weights serves both.
+int products_of(int type) { return type == SOAP_F32 ? 6 : 1; }  // of planes, per slice
 struct Slices {
   int64_t n[3];
 };
@@ -92,7 +93,7 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
   const auto [slices] = slices_of(rows, hidden, width, groups, type, backward);
   for (int p = 0; p < 3; ++p) {
-    const int64_t parts = slices[p] < kMinParted ? 1 : slices[p] / 4, longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
+    const int64_t parts = slices[p] * products_of(type) < kMinParted ? 1 : slices[p], longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
     l.units += l.tiles[p] * std::max(parts, longest);
     // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights'
     // gradients: of groups with more than kMaxSlices slices, less than three parts for each such run of all rows)
@@ -151,10 +152,21 @@ __global__ void __launch_bounds__(256) copy_kernel(const __grid_constant__ CopyJ
       const int col = (int)(i - row * chunks) * 8, n = min(8, c.inner - col);
       const int64_t from = m * c.stride + r * c.ld + col;
       Pack<uint16_t, 8> out[SPLIT ? 3 : 1];
+      alignas(16) float in[SPLIT ? 8 : 1];
+      if constexpr (SPLIT) {
+        const float* const p = static_cast<const float*>(c.src) + from;
+        if (n == 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+          *reinterpret_cast<float4*>(in) = *reinterpret_cast<const float4*>(p);
+          *reinterpret_cast<float4*>(in + 4) = *reinterpret_cast<const float4*>(p + 4);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) in[e] = e < n ? p[e] : 0.f;
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (SPLIT) {
-          const float x = e < n ? static_cast<const float*>(c.src)[from + e] : 0.f;
+          const float x = in[e];
           const uint32_t b = __float_as_uint(x);
           const bool finite = fabsf(x) < INFINITY;
           const float hi = __uint_as_float(b & 0xffff0000u), rest = finite ? x - hi : 0.f;
@@ -302,6 +314,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
   a.kblocks[1] = up_div(c.width, 64);
   const Slices n = slices_of(c.rows, c.hidden, c.width, c.groups, c.type, c.backward);
   for (int p = 0; p < 2; ++p) a.slices[p] = (int)n.n[p];
+  a.products = products_of(c.type);
   // a gradient in its weight's order: of a column-major weight the transposed product
   const int left[3] = {kInX, kInX, kInH}, right[3] = {kInDG, kInDU, kInDY};
   for (int p = 0; p < 3; ++p) {

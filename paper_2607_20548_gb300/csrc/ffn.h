@@ -10,7 +10,7 @@ namespace ffn {
 
 constexpr int kMaxGroups = 1024;
 constexpr int kSms = 152;           // that a product's parts are shared out among, one or a pair for each
-constexpr int kMinParted = 24;      // fewer slices of 64 products stay in one part
+constexpr int kMinParted = 24;      // fewer slices of 64 products (fp32: times 6) stay in one part
 constexpr int kMaxSlices = 1024;    // most slices that one accumulator adds up
 
 // Maps that end at a group's last row, so that loads of its rows give 0 beyond it and stores leave the rows behind it
@@ -59,6 +59,7 @@ struct Args {
   int plane_bits;               // log2 of the planes of h, dg and du (16-bit types)
   int b_columns[2];             // whether the second factor of a row phase has its K dimension outermost
   int kblocks[2];               // slices of a factor pair, per row phase
+  int products;                 // of planes, per slice
   int slices[2];                // of a tile, per row phase: of all pairs and planes that are added
   int wa[3], wb[3];             // Clip of the factors of the weights' gradients
   int wrows[3], wcols[3];       // sides of the weights' gradients as they are stored

@@ -46,49 +46,43 @@ __device__ __forceinline__ void tile_place(int i, int nm, int nn, int& m, int& n
   m = gr * 8 + in - n * rows;
 }
 
-// act(g) and its derivative for two elements at a time. 16-bit results: the hardware's exponential and reciprocal
-// (2^-21 of the result).
-template <int TYPE, int ACT>
+// act(g) and its derivative for two elements at a time, with the hardware's exponential (relative error 2^-22 + |g|
+// 2^-24) and quotient.
+template <int ACT>
 __device__ __forceinline__ void activation(float2 g, float2& a, float2& da) {
   const float2 one = pair(1.f);
   if (ACT == LAYER_SILU) {
-    float2 s;
-    if (TYPE == SOAP_F32) {
-      s = make_float2(1.f / (1.f + expf(-g.x)), 1.f / (1.f + expf(-g.y)));
-    } else {
-      s = add2(make_float2(__expf(-g.x), __expf(-g.y)), one);
-      s = make_float2(__fdividef(1.f, s.x), __fdividef(1.f, s.y));
-    }
+    const float2 e = add2(make_float2(__expf(-g.x), __expf(-g.y)), one);
+    const float2 s = make_float2(__fdividef(1.f, e.x), __fdividef(1.f, e.y));
     a = mul2(g, s);
     da = fma2(a, add2(one, make_float2(-s.x, -s.y)), s);  // s (1 + g (1 - s))
   } else {
     const float2 p = make_float2(0.5f * (1.f + erff(g.x * 0.70710678118654752f)), 0.5f * (1.f + erff(g.y * 0.70710678118654752f)));
     const float2 h = mul2(mul2(g, g), pair(-0.5f));
-    const float2 e = TYPE == SOAP_F32 ? make_float2(expf(h.x), expf(h.y)) : make_float2(__expf(h.x), __expf(h.y));
     a = mul2(g, p);
-    da = fma2(mul2(g, pair(0.3989422804014327f)), e, p);
+    da = fma2(mul2(g, pair(0.3989422804014327f)), make_float2(__expf(h.x), __expf(h.y)), p);
   }
 }
 // A block's rows: v = act(v) w; or, from g, u and v = dh: g = dg, u = h, v = du. One of two straight pieces of code (a
 // choice per element has the instructions of both fetched: 8 us of a small call's 55), two elements at a time: the
 // instructions of 32 x 32 elements set an epilogue's pace (backward 0.75 us a block of a warp with one at a time).
-template <int TYPE, int ACT, int N>
+template <int ACT, int N>
 __device__ __forceinline__ void gate(float (&v)[N], const float (&w)[N]) {
 #pragma unroll
   for (int j = 0; j < N; j += 2) {
     float2 a, da;
-    activation<TYPE, ACT>(make_float2(v[j], v[j + 1]), a, da);
+    activation<ACT>(make_float2(v[j], v[j + 1]), a, da);
     a = mul2(a, make_float2(w[j], w[j + 1]));
     v[j] = a.x, v[j + 1] = a.y;
   }
 }
-template <int TYPE, int ACT>
+template <int ACT>
 __device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&v)[32]) {
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
     const float2 uj = make_float2(u[j], u[j + 1]), vj = make_float2(v[j], v[j + 1]);
     float2 a, da;
-    activation<TYPE, ACT>(make_float2(g[j], g[j + 1]), a, da);
+    activation<ACT>(make_float2(g[j], g[j + 1]), a, da);
     const float2 dg = mul2(mul2(vj, uj), da), h = mul2(uj, a), du = mul2(vj, a);
     g[j] = dg.x, g[j + 1] = dg.y;
     u[j] = h.x, u[j + 1] = h.y;

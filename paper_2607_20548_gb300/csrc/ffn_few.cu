@@ -384,9 +384,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) w[j] = box[32 * j];
             if (a.act == LAYER_SILU)
-              gate<TYPE, LAYER_SILU>(v, w);
+              gate<LAYER_SILU>(v, w);
             else
-              gate<TYPE, LAYER_GELU>(v, w);
+              gate<LAYER_GELU>(v, w);
 #pragma unroll
             for (int j = 0; j < kChunk; ++j)
               if (j < left && f < a.width) {

@@ -7,7 +7,8 @@
 // transposed copy exists. 16-bit operands go to the tensor cores as they are. An fp32 operand comes as three bf16
 // planes that hold its 24 bits, and the six products of planes whose terms reach 2^-24 are added, small ones first:
 // the accumulator cuts (a sum loses 2^-25 of itself per 16 products, measured), so that K goes in runs of 256, whose
-// sums the epilogue adds in fp32 registers.
+// sums the epilogue adds up, rounding to nearest, in the other half of the tensor memory (in registers, 128 a thread,
+// the compiler spilled them: 5 groups of 2048 x 768, 2000 rows, both passes 595 us in place of @@).
 //
 // Schedule. Persistent CTA pairs (cta_group::2: a pair's 256 x 256 tile has 128 rows in each CTA) take units from one
 // list, each its next one when it begins the one before: a phase's tiles, or parts of them along K where the tiles are
@@ -47,7 +48,7 @@ constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 // registers of a launch's 168 per thread as the roles' warps share them: 4 x 72 + 8 x 216 = 12 x 168
 constexpr int kFewRegisters = 72, kManyRegisters = 216;
 constexpr int kStages = 5, kStage = 2 * kTile;
-constexpr int kStaging = 8192;      // per epilogue warp
+constexpr int kStaging = 8192;      // per epilogue warp: 4 blocks of 32 x 32 of 16 bits, 2 of fp32
 constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
 // units that the roles of a pair may be apart, and more: 1 + 5 + 2 + 1 (every unit takes at least one of the ring's
 // slots, of which each takes both CTAs' loading threads, and one of two accumulators)
@@ -110,6 +111,31 @@ __device__ __forceinline__ void tmem_ld16(uint32_t t, float (&v)[16]) {
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
         "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
       : "r"(t)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld16x2(uint32_t t0, uint32_t t1, float (&v)[16], float (&w)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]),
+        "=f"(v[15]), "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]), "=f"(w[5]), "=f"(w[6]),
+        "=f"(w[7]), "=f"(w[8]), "=f"(w[9]), "=f"(w[10]), "=f"(w[11]), "=f"(w[12]), "=f"(w[13]), "=f"(w[14]),
+        "=f"(w[15])
+      : "r"(t0), "r"(t1)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t t, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n\t"
+      "tcgen05.wait::st.sync.aligned;" ::"f"(v[0]),
+      "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+      "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "r"(t)
       : "memory");
 }
 
@@ -279,6 +305,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   using T = typename Element<TYPE>::T;
   using O = Order<TYPE>;
   constexpr bool SPLIT = O::kSplit;
+  constexpr int kAcc = SPLIT ? 1 : 2;  // accumulators
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + kStages * kStage;
@@ -330,7 +357,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the launch before has ended: so far, nothing of it was read
   const uint32_t tmem = *tmem_at;
 
-  if (!SPLIT && warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+  if (warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   if (warp == kScout) {
     bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
     const Plan& l = *a.plan;
@@ -479,8 +506,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const bool a_mn = kind == kWeight, b_mn = kind == kWeight || a.b_columns[kind == kOut];
         const uint32_t idesc = idesc_16(TYPE != SOAP_F16, a_mn, b_mn);
         for (; kb < s1 && st.ok; ++n) {
-          const int to = O::end_of_run(kb, s1), ac = n & 1, count = (to - kb) * O::kTermsOf;
-          if (n >= 2 && !(st.ok = mbar_wait(&acc_empty[ac], ((n >> 1) & 1) ^ 1, 2 * lim))) break;
+          const int to = O::end_of_run(kb, s1), ac = n % kAcc, count = (to - kb) * O::kTermsOf;
+          if (n >= kAcc && !(st.ok = mbar_wait(&acc_empty[ac], ((n / kAcc) & 1) ^ 1, 2 * lim))) break;
           tc_fence_after();
           const uint32_t d = tmem + static_cast<uint32_t>(ac * 256);
           if (a_mn)
@@ -496,21 +523,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (!st.ok) *abort_flag = 1;
     }
   } else {
-    if (!SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
     const int q = warp & 3;           // accumulator lanes 32 q .. 32 q + 31
     const int half = (warp - kFirstEpi) / 4;  // of the columns
     uint8_t* stage = staging + (warp - kFirstEpi) * kStaging;
-    constexpr int kSlot = SPLIT ? 4096 : 2048, kSlots = kStaging / kSlot;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * q) << 16);
     const int pre_cols = (a.width + 31) / 32;  // blocks
     int n = 0;  // accumulators so far
     int k = 0;  // staged blocks so far
     bool ok = true;
-    // a place for a block whose copy out has been read
-    auto next_slot = [&]() {
-      if (lane == 0) sent_read<kSlots - 1>();
+    // A place for a block of `half` (2 KB: 16-bit elements) or whole size (fp32), whose copies out have been read: four of
+    // one, two of the other, and no copy on its way where one size follows the other.
+    bool halves = true;
+    auto next_slot = [&](bool half) {
+      if (SPLIT && half != halves) {
+        if (lane == 0) sent_read<0>();
+        halves = half;
+      } else if (lane == 0) {
+        if (half)
+          sent_read<3>();
+        else
+          sent_read<1>();
+      }
       __syncwarp();
-      return stage + (k++ % kSlots) * kSlot;
+      const int at = k++;
+      return stage + (half ? at % 4 * 2048 : at % 2 * 4096);
     };
     auto send = [&](const CUtensorMap* map, const uint8_t* slot, int x, int y, int z) {
       before_tma();
@@ -539,7 +576,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       auto to_operand = [&](Clip which, float (&v)[32], int col) {
 #pragma unroll 1  // (instructions that are fetched once)
         for (int plane = 0; plane <= (SPLIT ? 2 : a.plane_bits); ++plane) {
-          uint8_t* const slot = next_slot();
+          uint8_t* const slot = next_slot(true);
           if constexpr (SPLIT) {
             float w[32];
 #pragma unroll
@@ -556,7 +593,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       };
       auto to_result = [&](const float (&v)[32], int col) {
-        uint8_t* const slot = next_slot();
+        uint8_t* const slot = next_slot(sizeof(T) == 2);
         const bool weight = u.kind == kWeight;
         if (weight ? a.dw_tma[u.prod] : a.y_tma) {
           put<T>(slot, v, lane);
@@ -586,18 +623,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           put_lines(pre_at(1, col), w);
         }
         if (a.act == LAYER_SILU)
-          gate<TYPE, LAYER_SILU>(v, w);
+          gate<LAYER_SILU>(v, w);
         else
-          gate<TYPE, LAYER_GELU>(v, w);
+          gate<LAYER_GELU>(v, w);
         to_operand(kH, v, col);
       };
       // block i of dh, whose g and u are in g and up; then the next block's (next, if any) come
       auto finish_grad = [&](int i, float (&v)[32], float (&g)[32], float (&up)[32], int next) {
         const int col = c0 + 32 * i;
         if (a.act == LAYER_SILU)
-          gate_back<TYPE, LAYER_SILU>(g, up, v);
+          gate_back<LAYER_SILU>(g, up, v);
         else
-          gate_back<TYPE, LAYER_GELU>(g, up, v);
+          gate_back<LAYER_GELU>(g, up, v);
         to_operand(kDG, g, col);
         if (next < blocks) get_lines(pre_at(0, c0 + 32 * next), g);
         if (a.params) to_operand(kH, up, col);
@@ -640,7 +677,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       };
       auto wait_acc = [&](int ac) {
-        ok = mbar_wait(&acc_full[ac], (n >> 1) & 1, 2 * lim) && !*abort_flag;
+        ok = mbar_wait(&acc_full[ac], (n / kAcc) & 1, 2 * lim) && !*abort_flag;
         tc_fence_after();
         return ok = __all_sync(0xffffffffu, ok);
       };
@@ -662,125 +699,82 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       auto turned = [&](int i) { return i + turn < blocks ? i + turn : i + turn - blocks; };
       int finished = most - blocks;  // (blocks that hold nothing count for the first part)
       if (u.part > 0) finished = 0;
-      if constexpr (!SPLIT) {
-        const int ac = n & 1;
-        const uint32_t t = t0 + static_cast<uint32_t>(ac * 256);
-        const bool whole = u.splits == 1;
-        float g[32], up[32];  // of the block that is next
-        if (u.kind == kGrad && whole && blocks > 0) {  // (the first block's come while the products are formed)
-          get_lines(pre_at(0, c0), g);
-          get_lines(pre_at(1, c0), up);
-        }
-        if (!wait_acc(ac)) break;
-        if (!whole) {
-          for (int i = 0; i < (gated ? 2 * blocks : blocks); ++i) {  // (g's and u's blocks in turn)
-            float v[32];
-            tmem_ld32(t + (gated ? 128 * (i & 1) + 32 * (i >> 1) : 32 * i), v);
-            put_lines(partial_at(u.part, i), v);
-          }
-          release_acc(ac);
-          parts_stored();
-        } else if (blocks == 0) {
-          release_acc(ac);
-        }
-        for (int j = 0; j < blocks; ++j) {
-          const int i = turned(j);
-          if (!whole && !last_part(i)) continue;
-          float v[32];
-          if (gated) {
-            float w[32];
-            if (whole) {
-              tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
-              if (j + 1 == blocks) release_acc(ac);
-            } else {
-              add_parts(2 * i, v);
-              add_parts(2 * i + 1, w);
-            }
-            finish_gated(i, v, w);
-          } else {
-            if (whole) {
-              tmem_ld32(t + 32 * i, v);
-              if (j + 1 == blocks) release_acc(ac);
-            } else {
-              add_parts(i, v);
-            }
-            if (u.kind == kGrad) {
-              if (!whole) {
-                get_lines(pre_at(0, c0 + 32 * i), g);
-                get_lines(pre_at(1, c0 + 32 * i), up);
-              }
-              finish_grad(i, v, g, up, whole ? i + 1 : blocks);
-            } else {
-              to_result(v, c0 + 32 * i);
-            }
-          }
-          ++finished;
-        }
-        ++n;
-      } else {
-        float sum[4][32];  // of g and u: blocks 0 and 1 of g, of u
-        bool begun = false;
+      // fp32: the runs' sums are added up in the tensor memory's other half, 16 columns at a time
+      const bool summed = SPLIT && u.s1 - u.s0 > kRun;
+      if (summed) {
         for (int kb = u.s0; kb < u.s1; kb = O::end_of_run(kb, u.s1), ++n) {
-          const int ac = n & 1;
-          if (!wait_acc(ac)) break;
+          if (!wait_acc(n % kAcc)) break;
+#pragma unroll 1
+          for (int i = 0; i < (gated ? 4 : 2) * blocks; ++i) {
+            const uint32_t at = t0 + (gated ? 128 * (i & 1) + 16 * (i >> 1) : 16 * i);
+            float v[16], w[16];
+            if (kb == u.s0) {
+              tmem_ld16(at, v);
+            } else {
+              tmem_ld16x2(at, at + 256, v, w);
 #pragma unroll
-          for (int b = 0; b < 8; ++b)
-            if (gated ? (b / 2 & 1) < blocks : b / 2 < blocks) {
-              float v[16];
-              tmem_ld16(t0 + static_cast<uint32_t>(ac * 256) + (gated && b >= 4 ? 128 + 16 * (b - 4) : 16 * b), v);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                float& x = sum[b / 2][(b & 1) * 16 + j];
-                x = begun ? x + v[j] : v[j];
-              }
+              for (int j = 0; j < 16; ++j) v[j] += w[j];
             }
-          release_acc(ac);
-          begun = true;
+            tmem_st16(at + 256, v);
+          }
+          release_acc(n % kAcc);
         }
         if (!ok) break;
-        if (u.splits > 1) {
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            if (gated ? (b & 1) < blocks : b < blocks) put_lines(partial_at(u.part, gated ? 2 * (b & 1) + b / 2 : b), sum[b]);
+      }
+      const int ac = n % kAcc;
+      const uint32_t t = t0 + static_cast<uint32_t>(summed ? 256 : ac * 256);
+      const bool whole = u.splits == 1;
+      float g[32], up[32];  // of the block that is next
+      if (u.kind == kGrad && whole && blocks > 0) {  // (the first block's come while the products are formed)
+        get_lines(pre_at(0, c0), g);
+        get_lines(pre_at(1, c0), up);
+      }
+      if (!summed && !wait_acc(ac)) break;
+      if (!whole) {
+        for (int i = 0; i < (gated ? 2 * blocks : blocks); ++i) {  // (g's and u's blocks in turn)
+          float v[32];
+          tmem_ld32(t + (gated ? 128 * (i & 1) + 32 * (i >> 1) : 32 * i), v);
+          put_lines(partial_at(u.part, i), v);
+        }
+        if (!summed) release_acc(ac);
+        parts_stored();
+      } else if (blocks == 0 && !summed) {
+        release_acc(ac);
+      }
+      for (int j = 0; j < blocks; ++j) {
+        const int i = turned(j);
+        if (!whole && !last_part(i)) continue;
+        float v[32];
+        if (gated) {
+          float w[32];
+          if (whole) {
+            tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
+            if (j + 1 == blocks && !summed) release_acc(ac);
+          } else {
+            add_parts(2 * i, v);
+            add_parts(2 * i + 1, w);
           }
-          parts_stored();
-          for (int j = 0; j < blocks; ++j) {
-            const int i = turned(j);
-            if (!last_part(i)) continue;
-            float v[32];
-            add_parts(gated ? 2 * i : i, v);
-            if (gated) {
-              float w[32];
-              add_parts(2 * i + 1, w);
-              finish_gated(i, v, w);
-            } else if (u.kind == kGrad) {
-              float g[32], up[32];
+          finish_gated(i, v, w);
+        } else {
+          if (whole) {
+            tmem_ld32(t + 32 * i, v);
+            if (j + 1 == blocks && !summed) release_acc(ac);
+          } else {
+            add_parts(i, v);
+          }
+          if (u.kind == kGrad) {
+            if (!whole) {
               get_lines(pre_at(0, c0 + 32 * i), g);
               get_lines(pre_at(1, c0 + 32 * i), up);
-              finish_grad(i, v, g, up, blocks);
-            } else {
-              to_result(v, c0 + 32 * i);
             }
-            ++finished;
-          }
-        } else {
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            if (b >= blocks) break;
-            if (gated) {
-              if (b < 2) finish_gated(b, sum[b], sum[b + 2]);
-            } else if (u.kind == kGrad) {
-              float g[32], up[32];
-              get_lines(pre_at(0, c0 + 32 * b), g);
-              get_lines(pre_at(1, c0 + 32 * b), up);
-              finish_grad(b, sum[b], g, up, blocks);
-            } else {
-              to_result(sum[b], c0 + 32 * b);
-            }
-            ++finished;
+            finish_grad(i, v, g, up, whole ? i + 1 : blocks);
+          } else {
+            to_result(v, c0 + 32 * i);
           }
         }
+        ++finished;
       }
+      if (!summed) ++n;
       report(finished);
       __syncwarp();
     }
@@ -843,12 +837,12 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
 }
 
 // Parts along K of a tile of `slices` slices (0: none), where there may be `most` for the pairs' sake: a part of p
-// costs its slices' time, 0.3 us each, and adding up p parts 5 us and about as much as a slice for each, so that
-// short sums stay whole, and the best p for others is about sqrt(slices).
-__device__ __forceinline__ int parts_of(int slices, int most) {
+// costs its slices' time, 0.3 us for each of their products of planes, and adding up p parts 5 us and about as much as a slice for each, so that
+// short sums stay whole, and the best p for others is about the root of those products' number.
+__device__ __forceinline__ int parts_of(int slices, int most, int products) {
   if (slices == 0) return 0;
-  const int whole = max(1, up_div(slices, kMaxSlices));
-  return slices < kMinParted ? whole : max(whole, min(most, (int)sqrtf((float)slices)));
+  const int whole = max(1, up_div(slices, kMaxSlices)), cost = slices * products;
+  return cost < kMinParted ? whole : max(whole, min(most, min(slices, (int)sqrtf((float)cost))));
 }
 
 // The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
@@ -872,7 +866,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       int tiles = 0, blocks = 0, parts = 0, slots = 0;  // of the groups before
       for (int g0 = 0; g0 <= a.groups; g0 += 32) {
         const int g = g0 + lane, len = length(g);
-        const int n = a.params ? parts_of(up_div(len, BK) << a.plane_bits, most) : 0;
+        const int n = a.params ? parts_of(up_div(len, BK) << a.plane_bits, most, a.products) : 0;
         int4 v = make_int4(up_div(len, a.row_tile), up_div(len, 32), n, n > 1 ? n : 0);
         const int4 own = v;
         for (int d = 1; d < 32; d *= 2) {
@@ -898,7 +892,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
           const int n = tiles * up_div(p == 0 ? a.width : a.hidden, a.col_tile[p]);
           l.first[p] = at;
           l.tiles[p] = n;
-          l.splits[p] = n > 0 ? parts_of(a.slices[p], a.pool / n) : 1;
+          l.splits[p] = n > 0 ? parts_of(a.slices[p], a.pool / n, a.products) : 1;
           if (p == 0 && a.h) l.splits[p] = 1;  // (few rows: g and u meet in the tile)
           at += n * l.splits[p];
         }
