@@ -85,7 +85,14 @@ cudaError_t run_few(const Maps& maps, const Args& a, int type, int64_t units, cu
 // The plan, the groups' maps, zeros for rows of no group and for the gradients of groups without rows.
 cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s);
 
-inline __host__ __device__ int up_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+// (a 64-bit division takes a scout longer than its loads)
+template <typename A, typename B>
+inline __host__ __device__ int up_div(A a, B b) {
+  if constexpr (sizeof(A) <= 4 && sizeof(B) <= 4)
+    return (int)((uint32_t)(a + b - 1) / (uint32_t)b);
+  else
+    return (int)(((int64_t)a + b - 1) / b);
+}
 
 }  // namespace ffn
 }  // namespace soap

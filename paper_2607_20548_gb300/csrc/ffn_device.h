@@ -27,6 +27,32 @@ struct Element<SOAP_F16> {
 struct Head {
   int total, first[3], tiles[2], splits[2], parts;
 };
+// Parts along K of a tile of `slices` slices (0: none), where there may be `most` for the pairs' sake: a part of p
+// costs its slices' time, 0.3 us for each of their products of planes, and adding up p parts 5 us and about as much as a slice for each, so that
+// short sums stay whole, and the best p for others is about the root of those products' number.
+__device__ __forceinline__ int parts_of(int slices, int most, int products) {
+  if (slices == 0) return 0;
+  const int whole = max(1, up_div(slices, kMaxSlices)), cost = slices * products;
+  return cost < kMinParted ? whole : max(whole, min(most, min(slices, (int)sqrtf((float)cost))));
+}
+
+// The list of `tiles` row tiles, and of `parts` parts along the rows for each tile of the weights' gradients.
+__device__ __forceinline__ Head head_of(const Args& a, int tiles, int parts) {
+  Head h;
+  int at = 0;
+  for (int p = 0; p < 2; ++p) {
+    const int n = tiles * up_div(p == 0 ? a.width : a.hidden, a.col_tile[p]);
+    h.first[p] = at;
+    h.tiles[p] = n;
+    h.splits[p] = n > 0 ? parts_of(a.slices[p], a.pool / n, a.products) : 1;
+    if (p == 0 && a.h) h.splits[p] = 1;  // (few rows: g and u meet in the tile)
+    at += n * h.splits[p];
+  }
+  h.first[2] = at;
+  h.parts = parts;
+  h.total = at + parts * 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256);
+  return h;
+}
 // The largest i < n with prefix[i] <= q; all lanes of a warp take part (one round of loads for up to 32 groups, two
 // beyond: a binary search's dependent ones took longer than a small unit).
 __device__ __forceinline__ int group_of(const int* prefix, int n, int q) {

@@ -8,7 +8,7 @@
 // planes that hold its 24 bits, and the six products of planes whose terms reach 2^-24 are added, small ones first:
 // the accumulator cuts (a sum loses 2^-25 of itself per 16 products, measured), so that K goes in runs of 256, whose
 // sums the epilogue adds up, rounding to nearest, in the other half of the tensor memory (in registers, 128 a thread,
-// the compiler spilled them: 5 groups of 2048 x 768, 2000 rows, both passes 595 us in place of @@).
+// the compiler spilled them: 5 groups of 2048 x 768, 2000 rows, both passes 595 us in place of 453).
 //
 // Schedule. Persistent CTA pairs (cta_group::2: a pair's 256 x 256 tile has 128 rows in each CTA) take units from one
 // list, each its next one when it begins the one before: a phase's tiles, or parts of them along K where the tiles are
@@ -361,8 +361,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == kScout) {
     bool ok = rank != 0 || !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
     const Plan& l = *a.plan;
-    const Head head{l.total, {0, l.first[1], l.first[2]}, {l.tiles[0], l.tiles[1]}, {l.splits[0], l.splits[1]},
-                    a.clips ? 0 : l.parts[1]};
+    // (from memory: working it out here for one group took longer, its instructions being fetched for this once)
+    const Head head{l.total, {0, l.first[1], l.first[2]}, {l.tiles[0], l.tiles[1]}, {l.splits[0], l.splits[1]}, l.parts[1]};
     uint32_t peer;
     asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at + 2)));
     for (int m = 0; ok; ++m) {
@@ -836,13 +836,21 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
   bounds = buf[at];
 }
 
-// Parts along K of a tile of `slices` slices (0: none), where there may be `most` for the pairs' sake: a part of p
-// costs its slices' time, 0.3 us for each of their products of planes, and adding up p parts 5 us and about as much as a slice for each, so that
-// short sums stay whole, and the best p for others is about the root of those products' number.
-__device__ __forceinline__ int parts_of(int slices, int most, int products) {
-  if (slices == 0) return 0;
-  const int whole = max(1, up_div(slices, kMaxSlices)), cost = slices * products;
-  return cost < kMinParted ? whole : max(whole, min(most, min(slices, (int)sqrtf((float)cost))));
+// All CTAs: `rows` rows of `cols` elements become 0; from row `first` on those that follow row `last`.
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* p, int64_t ld, int64_t rows, int cols, int64_t first, int64_t last) {
+  const bool whole = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0;
+  const int step = whole ? 16 / (int)sizeof(T) : 1;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    T* const row = p + (r < first ? r : r - first + last) * ld;
+    for (int c = threadIdx.x * step; c < cols; c += kPrepThreads * step) {
+      if (whole && c + step <= cols) {
+        *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+      } else {
+        for (int e = c; e < min(cols, c + step); ++e) row[e] = from_f32<T>(0.f);
+      }
+    }
+  }
 }
 
 // The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
@@ -887,17 +895,10 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       }
       if (lane == 0) {
         l.next = l.through = l.gave_up = 0;
-        int at = 0;
-        for (int p = 0; p < 2; ++p) {
-          const int n = tiles * up_div(p == 0 ? a.width : a.hidden, a.col_tile[p]);
-          l.first[p] = at;
-          l.tiles[p] = n;
-          l.splits[p] = n > 0 ? parts_of(a.slices[p], a.pool / n, a.products) : 1;
-          if (p == 0 && a.h) l.splits[p] = 1;  // (few rows: g and u meet in the tile)
-          at += n * l.splits[p];
-        }
-        l.first[2] = at;
-        l.total = at + parts * each;
+        const Head h = head_of(a, tiles, parts);
+        l.total = h.total;
+        for (int p = 0; p < 3; ++p) l.first[p] = h.first[p];
+        for (int p = 0; p < 2; ++p) l.tiles[p] = h.tiles[p], l.splits[p] = h.splits[p];
       }
     }
   }
@@ -919,19 +920,13 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
   }
   if (!a.offsets && a.rows > 0) return;
   const int first = bounds[0], last = bounds[a.groups];
-  const T zero = from_f32<T>(0.f);
-  for (int64_t r = blockIdx.x; r < first + (a.rows - last); r += gridDim.x) {
-    T* const row = static_cast<T*>(a.y) + (r < first ? r : r - first + last) * a.ld_y;
-    for (int c = threadIdx.x; c < a.hidden; c += kPrepThreads) row[c] = zero;
-  }
+  const int64_t outside = first + (a.rows - last);
+  zero_rows(static_cast<T*>(a.y), a.ld_y, outside, a.hidden, first, last);
   if (!a.params) return;
   for (int g = 0; g < a.groups; ++g) {
     if (bounds[g + 1] > bounds[g]) continue;
     for (int p = 0; p < 3; ++p)
-      for (int r = blockIdx.x; r < a.wrows[p]; r += gridDim.x) {
-        T* const row = static_cast<T*>(a.dw[p]) + (int64_t)g * a.stride_dw[p] + (int64_t)r * a.ld_dw[p];
-        for (int c = threadIdx.x; c < a.wcols[p]; c += kPrepThreads) row[c] = zero;
-      }
+      zero_rows(static_cast<T*>(a.dw[p]) + (int64_t)g * a.stride_dw[p], a.ld_dw[p], a.wrows[p], a.wcols[p], a.wrows[p], 0);
   }
 }
 
