@@ -49,14 +49,6 @@ int planes_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type)
   return type == SOAP_F32 ? 3 : rows <= 64 * (int64_t)groups && groups * hidden * width <= 1 << 23 ? 2 : 1;
 }
 
-Tiles tiles_of(int64_t rows, int groups, int type, bool backward) {
-  if (!few_rows(rows, groups, type, backward)) return Tiles{256, {backward ? 256 : 128, 256}, kSms / 2, 256 * 256, 64};
-  const int64_t each = groups == 1 ? rows : (rows + rows / 2) / groups;
-  int n = 16;
-  while (n < each && n < 128) n *= 2;
-  return Tiles{n, {64, 128}, kSms, 128 * n, 4 * std::max(1, n / 32)};
-}
-
 // Slices of a tile's sums, per phase (of the weights' gradients: of all rows). Planes of 16-bit types are added one
 // after the other, but for few rows, where one load of the weights serves both.
 int products_of(int type) { return type == SOAP_F32 ? 6 : 1; }  // of planes, per slice
@@ -66,6 +58,26 @@ struct Slices {
 Slices slices_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool backward) {
   const int twice = backward && type != SOAP_F32 && planes_of(rows, hidden, width, groups, type) == 2 ? 2 : 1;
   return Slices{{up_div(hidden, 64), twice * (backward ? 2 : 1) * (int64_t)up_div(width, 64), twice * (int64_t)up_div(rows, 64)}};
+}
+
+// Rows as columns: 64 and 128 features by the rows that a group has on average, and half as many again. Else 256 x 256
+// (the first phase forward: 128 of g and of u), or half the columns where that leaves no pair without a tile and sums are
+// too short to go in parts: a tile's products take as long, what follows them half as long.
+Tiles tiles_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool backward) {
+  if (few_rows(rows, groups, type, backward)) {
+    const int64_t each = groups == 1 ? rows : (rows + rows / 2) / groups;
+    int n = 16;
+    while (n < each && n < 128) n *= 2;
+    return Tiles{n, {64, 128, 0}, kSms, 128 * n, 4 * std::max(1, n / 32)};
+  }
+  Tiles t{256, {backward ? 256 : 128, 256, 256}, kSms / 2, 256 * 256, 64};
+  const Slices n = slices_of(rows, hidden, width, groups, type, backward);
+  const int64_t some = std::min<int64_t>(groups, rows), row_tiles = rows / 256 + some;
+  const int64_t tiles[3] = {row_tiles * up_div(width, t.cols[0]), row_tiles * up_div(hidden, 256),
+                            some * 3 * up_div(width, 256) * up_div(hidden, 256)};
+  for (int p = 0; p < 3; ++p)
+    if (2 * tiles[p] <= t.pool && n.n[p] * products_of(type) < kMinParted) t.cols[p] /= 2;
+  return t;
 }
 
 // Where everything lies in the workspace.
@@ -79,7 +91,7 @@ struct Layout {
 
 Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool copies, bool backward) {
   Layout l{};
-  const Tiles t = tiles_of(rows, groups, type, backward);
+  const Tiles t = tiles_of(rows, hidden, width, groups, type, backward);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -89,7 +101,9 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   l.row_tiles = rows / t.rows + std::min<int64_t>(groups, rows);
   l.tiles[0] = l.row_tiles * up_div(width, t.cols[0]);
   l.tiles[1] = l.row_tiles * up_div(hidden, t.cols[1]);
-  const int64_t each = 3 * (int64_t)up_div(width, 256) * up_div(hidden, 256);
+  // (of either order of the weights)
+  const int64_t each = backward ? 3 * std::max((int64_t)up_div(width, 256) * up_div(hidden, t.cols[2]),
+                                               (int64_t)up_div(width, t.cols[2]) * up_div(hidden, 256)) : 0;
   l.tiles[2] = backward ? std::min<int64_t>(groups, rows) * each : 0;
   const auto [slices] = slices_of(rows, hidden, width, groups, type, backward);
   for (int p = 0; p < 3; ++p) {
@@ -287,11 +301,15 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     a.count[p] = reinterpret_cast<int*>(c.ws + l.count[p]);
     a.partial[p] = reinterpret_cast<float*>(c.ws + l.partial[p]);
   }
-  const Tiles t = tiles_of(c.rows, c.groups, c.type, c.backward);
+  const Tiles t = tiles_of(c.rows, c.hidden, c.width, c.groups, c.type, c.backward);
   const bool few = few_rows(c.rows, c.groups, c.type, c.backward);
   a.row_tile = t.rows;
-  a.col_tile[0] = t.cols[0];
-  a.col_tile[1] = t.cols[1];
+  for (int p = 0; p < 3; ++p) {
+    a.col_tile[p] = t.cols[p];
+    a.narrow[p] = !few && t.cols[p] < (p == 0 && !c.backward ? 128 : 256);
+  }
+  // every warp of both CTAs counts its share of a tile: blocks of 32 columns of h, or of dg, du and h
+  a.stored = 16 * ((c.backward ? 4 : 2) >> a.narrow[0]) * up_div(c.width, t.cols[0]);
   a.pool = t.pool;
   const int kept = planes_of(c.rows, c.hidden, c.width, c.groups, c.type);
   a.plane_bits = c.type != SOAP_F32 && kept == 2;
@@ -323,6 +341,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     a.wb[p] = turned ? left[p] : right[p];
     a.wrows[p] = (p == 2) != turned ? c.width : c.hidden;
     a.wcols[p] = (p == 2) != turned ? c.hidden : c.width;
+    a.each[p] = c.backward ? up_div(a.wrows[p], 256) * up_div(a.wcols[p], t.cols[2]) : 0;
   }
   a.act = c.act;
   a.pre = pre;
@@ -344,8 +363,8 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
               make_map(&maps.a1[0], inter[c.backward ? 1 : 0], etype, 64, box) &&
               (!c.backward || make_map(&maps.a1[1], inter[2], etype, 64, box));
     for (int i = 0; i < 2; ++i) {
-      ok = ok && make_map(&maps.w0[i], v[c.backward ? 4 : 2 + i], etype, 64, few || a.b_columns[0] ? 64 : 128) &&
-           ((i == 1 && !c.backward) || make_map(&maps.w1[i], v[c.backward ? 2 + i : 4], etype, 64, few || a.b_columns[1] ? 64 : 128));
+      ok = ok && make_map(&maps.w0[i], v[c.backward ? 4 : 2 + i], etype, 64, few || a.b_columns[0] || a.narrow[0] ? 64 : 128) &&
+           ((i == 1 && !c.backward) || make_map(&maps.w1[i], v[c.backward ? 2 + i : 4], etype, 64, few || a.b_columns[1] || a.narrow[1] ? 64 : 128));
     }
     a.y_tma = !few && units_of_16(y, ld_y, 0, size);
     if (!few) ok = ok && make_map(&maps.clip[kH], inter[0], etype, 32, 32);

@@ -26,10 +26,10 @@ struct Maps {
   CUtensorMap clip[kClips]; // dense: up to the last row; groups: what their own are made from
 };
 
-// Tiles of a call: rows, columns of the first and of the second phase; units at a time; of a part's sums the fp32
-// elements and the blocks that are counted.
+// Tiles of a call: rows, columns per phase; units at a time; of a part's sums the fp32 elements and the blocks that are
+// counted.
 struct Tiles {
-  int rows, cols[2], pool, partial, blocks;
+  int rows, cols[3], pool, partial, blocks;
 };
 
 // What is made on the device before the products run.
@@ -53,7 +53,10 @@ struct Args {
   const CUtensorMap* clips;     // [groups][kClips], or nullptr: those in Maps (dense, few rows)
   int backward, params;
   int groups, rows, hidden, width;
-  int row_tile, col_tile[2], pool;
+  int row_tile, col_tile[3], pool;
+  int narrow[3];                // whether a phase's tiles have half the columns (g's and u's 64 each, others' 128)
+  int each[3];                  // tiles of a group's weights' gradients
+  int stored;                   // blocks that the first phase stores for a row tile
   void* h;                      // few rows: where the first phase's results go
   int64_t ld_h, h_plane;
   int plane_bits;               // log2 of the planes of h, dg and du (16-bit types)

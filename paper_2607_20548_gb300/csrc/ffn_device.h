@@ -50,7 +50,7 @@ __device__ __forceinline__ Head head_of(const Args& a, int tiles, int parts) {
   }
   h.first[2] = at;
   h.parts = parts;
-  h.total = at + parts * 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256);
+  h.total = at + parts * (a.each[0] + a.each[1] + a.each[2]);
   return h;
 }
 // The largest i < n with prefix[i] <= q; all lanes of a warp take part (one round of loads for up to 32 groups, two

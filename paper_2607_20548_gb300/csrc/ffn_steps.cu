@@ -68,10 +68,10 @@ struct Unit {
 constexpr int kSmem = 1024 + kStages * kStage + kEpiWarps * kStaging + kKept * (int)sizeof(Unit) + 256;
 static_assert(kSmem <= 232448, "shared memory");
 
-// kind::f16, M = N = 256: D = f32, A and B bf16 or f16; bits 15 and 16 mark MN-major operands.
-__host__ __device__ constexpr uint32_t idesc_16(bool bf16, int a_mn, int b_mn) {
+// kind::f16, M = 256: D = f32, A and B bf16 or f16; bits 15 and 16 mark MN-major operands.
+__host__ __device__ constexpr uint32_t idesc_16(bool bf16, int a_mn, int b_mn, int n) {
   return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (static_cast<uint32_t>(a_mn) << 15) |
-         (static_cast<uint32_t>(b_mn) << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+         (static_cast<uint32_t>(b_mn) << 16) | (static_cast<uint32_t>(n >> 3) << 17) | ((256u >> 4) << 24);
 }
 
 // 32 columns at each of two places of this lane's accumulator row.
@@ -147,7 +147,7 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
   int i = p - (phase == 2 ? h.first[2] : phase == 1 ? h.first[1] : 0);
   if (phase < 2) {
     u.slot = i;
-    const int tiles = phase == 0 ? h.tiles[0] : h.tiles[1], wide = phase == 0 && !a.backward ? 128 : 256;
+    const int tiles = phase == 0 ? h.tiles[0] : h.tiles[1], wide = phase == 0 ? a.col_tile[0] : a.col_tile[1];
     u.N = phase == 0 ? a.width : a.hidden;
     u.kind = phase == 1 ? kOut : a.backward ? kGrad : kGated;
     u.splits = phase == 0 ? h.splits[0] : h.splits[1];
@@ -178,9 +178,9 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
   } else {
-    const int nm = up_div(a.wrows[0], 256), nn = up_div(a.wcols[0], 256), each = nm * nn, q = i / (3 * each);
+    const int each = a.each[0] + a.each[1] + a.each[2], q = i / each;
     u.kind = kWeight;
-    u.tiles = 3 * each;
+    u.tiles = each;
     int rows = a.rows, slots = 0;
     u.splits = h.parts;
     u.part = q;
@@ -194,17 +194,17 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
       rows = l.bounds[u.group + 1] - u.start;
       u.need = l.row_tiles[u.group + 1] - l.row_tiles[u.group];
     }
-    i -= q * 3 * each;
-    u.tile = slots * 3 * each + i;
-    u.slot = u.tile + u.part * 3 * each;
-    u.prod = i / each;
-    i -= u.prod * each;
+    i -= q * each;
+    u.tile = slots * each + i;
+    u.slot = u.tile + u.part * each;
+    u.prod = i >= a.each[0] + a.each[1] ? 2 : i >= a.each[0] ? 1 : 0;
+    i -= u.prod == 2 ? a.each[0] + a.each[1] : u.prod == 1 ? a.each[0] : 0;
     u.M = a.wrows[u.prod];
     u.N = a.wcols[u.prod];
     int m, n;
-    tile_place(i, up_div(u.M, 256), up_div(u.N, 256), m, n);
+    tile_place(i, up_div(u.M, 256), up_div(u.N, a.col_tile[2]), m, n);
     u.m0 = m * 256;
-    u.n0 = n * 256;
+    u.n0 = n * a.col_tile[2];
     const int slices = up_div(rows, BK) << a.plane_bits;
     u.s0 = (int)((int64_t)slices * u.part / u.splits);
     u.s1 = (int)((int64_t)slices * (u.part + 1) / u.splits);
@@ -235,7 +235,7 @@ struct Loader {
 
 template <int MN>
 __device__ __forceinline__ void load_run(Loader& l, int from, int to, int kblocks, int k_at, const CUtensorMap* m0,
-                                         const CUtensorMap* m1, int row, int z, uint32_t bytes, int bits, int planes) {
+                                         const CUtensorMap* m1, int row, int z, uint32_t bytes, int bits, int planes, bool half) {
   for (; from < to; ++from) {
     // (slices of both planes one after the other, so that the other factor's second load comes from L2)
     const int kb = from >> bits;
@@ -243,8 +243,11 @@ __device__ __forceinline__ void load_run(Loader& l, int from, int to, int kblock
     if (!(st.ok = mbar_wait(&l.empty[st.s], st.parity, l.lim))) return;
     if (bytes) expect_tx(&l.full[st.s], bytes);
     const bool second = kb >= kblocks;
-    load_tile<MN>(l.ring + st.s * kStage, second ? m1 : m0, l.bars + st.s * 8, row,
-                  k_at + (second ? kb - kblocks : kb) * BK, z + (from & planes));
+    const int k = k_at + (second ? kb - kblocks : kb) * BK, zk = z + (from & planes);
+    if (half)  // 64 of its rows (K-major: the map's boxes)
+      tma_box(l.ring + st.s * kStage, second ? m1 : m0, l.bars + st.s * 8, MN ? row : k, MN ? k : row, zk);
+    else
+      load_tile<MN>(l.ring + st.s * kStage, second ? m1 : m0, l.bars + st.s * 8, row, k, zk);
     if (++st.s == kStages) {
       st.s = 0;
       st.parity ^= 1;
@@ -392,11 +395,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         units[m % kKept] = u;
         set_ready(known_at, m + 1);
         if (u.kind == kOut)
-          ok = wait_done(a.done_row + u.row_tile, kPerTile * (a.backward ? 4 * up_div(a.width, 256) : 2 * up_div(a.width, 128)),
-                         lim);
+          ok = wait_done(a.done_row + u.row_tile, a.stored, lim);
         else if (u.kind == kWeight)
-          ok = wait_done(a.done_group + u.group,
-                         kPerTile * 4 * up_div(a.width, 256) * u.need, lim);
+          ok = wait_done(a.done_group + u.group, a.stored * u.need, lim);
         if (ok) {
           asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
           set_ready(ready_at, m + 1);
@@ -429,12 +430,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!is_b) set_ready(begun_at, m + 1);
         const CUtensorMap *m0, *m1;
         int row, z = 0, planes = 0, kblocks, k_at = 0;
+        const int narrow = a.narrow[u.kind == kWeight ? 2 : u.kind == kOut];
         bool mn, of_planes = false;  // whether the planes are this factor's
         if (u.kind == kWeight) {
           const int which = is_b ? a.wb[u.prod] : a.wa[u.prod];
           m0 = m1 = a.clips ? a.clips + u.group * kClips + which : &maps.clip[which];
           if (a.clips) fence_map(m0);
-          row = (is_b ? u.n0 : u.m0) + rank * 128;
+          row = is_b ? u.n0 + rank * (128 >> narrow) : u.m0 + rank * 128;
           of_planes = which >= kInH;
           kblocks = INT_MAX;
           k_at = u.start;
@@ -453,13 +455,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           } else {
             m0 = phase ? &maps.w1[0] : &maps.w0[u.kind == kGated ? rank : 0];
             m1 = phase ? &maps.w1[1] : m0;
-            row = u.kind == kGated ? u.n0 : u.n0 + rank * 128;
+            row = u.kind == kGated ? u.n0 : u.n0 + rank * (128 >> narrow);
             z = u.group;
             planes = a.groups;
             mn = a.b_columns[phase];
           }
         }
-        const uint32_t bytes = rank != 0 || is_b ? 0 : 2 * kStage;
+        const uint32_t bytes = rank != 0 || is_b ? 0 : 2 * (kTile + (kTile >> narrow));
         const int bits = u.kind >= kOut ? a.plane_bits : 0, plane = of_planes ? bits : 0;
         used = min(used + (u.s1 - u.s0) * O::kTermsOf, kStages);
         for (int kb = u.s0; kb < u.s1 && l.st.ok;) {
@@ -467,9 +469,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int t = 0; t < O::kTermsOf && l.st.ok; ++t) {
             const int zt = z + (SPLIT ? (is_b ? term_b(t) : term_a(t)) * planes : 0);
             if (mn)
-              load_run<1>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane);
+              load_run<1>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane, is_b && narrow);
             else
-              load_run<0>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane);
+              load_run<0>(l, kb, to, kblocks, k_at, m0, m1, row, zt, bytes, bits, plane, is_b && narrow);
           }
           kb = to;
         }
@@ -504,7 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int kb = u.s0;
         if (kind == kEnd) break;
         const bool a_mn = kind == kWeight, b_mn = kind == kWeight || a.b_columns[kind == kOut];
-        const uint32_t idesc = idesc_16(TYPE != SOAP_F16, a_mn, b_mn);
+        const uint32_t idesc = idesc_16(TYPE != SOAP_F16, a_mn, b_mn, 256 >> a.narrow[kind == kWeight ? 2 : kind == kOut]);
         for (; kb < s1 && st.ok; ++n) {
           const int to = O::end_of_run(kb, s1), ac = n % kAcc, count = (to - kb) * O::kTermsOf;
           if (n >= kAcc && !(st.ok = mbar_wait(&acc_empty[ac], ((n / kAcc) & 1) ^ 1, 2 * lim))) break;
@@ -560,11 +562,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const Unit u = units[m % kKept];
       if (u.kind == kEnd) break;
       const int r0 = u.m0 + rank * 128 + 32 * q;
-      // its columns in blocks of 32 (of g and u 64 each, else 128): none below the last row, and to the last column
+      // its columns in blocks of 32 (of g and u 64 each, else 128, or half of that): none below the last row, and to the last column
       const bool gated = u.kind == kGated;
-      const int most = gated ? 2 : 4, c0 = u.n0 + 32 * most * half;
+      const int narrow = a.narrow[u.kind == kWeight ? 2 : u.kind == kOut];
+      const int most = (gated ? 2 : 4) >> narrow, c0 = u.n0 + 32 * most * half;
       const int blocks = r0 < u.M && c0 < u.N ? min(most, (u.N - c0 + 31) / 32) : 0;
-      const uint32_t t0 = lanes + 32 * most * half;
+      const uint32_t t0 = lanes + 32 * most * half, u_at = 128 >> narrow;  // (u's columns behind g's)
       const CUtensorMap* const clips = a.clips ? a.clips + u.group * kClips : maps.clip;
       if (a.clips && lane == 0) {
         if (u.kind <= kGrad) fence_map(clips + kH);
@@ -706,7 +709,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (!wait_acc(n % kAcc)) break;
 #pragma unroll 1
           for (int i = 0; i < (gated ? 4 : 2) * blocks; ++i) {
-            const uint32_t at = t0 + (gated ? 128 * (i & 1) + 16 * (i >> 1) : 16 * i);
+            const uint32_t at = t0 + (gated ? u_at * (i & 1) + 16 * (i >> 1) : 16 * i);
             float v[16], w[16];
             if (kb == u.s0) {
               tmem_ld16(at, v);
@@ -733,7 +736,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (!whole) {
         for (int i = 0; i < (gated ? 2 * blocks : blocks); ++i) {  // (g's and u's blocks in turn)
           float v[32];
-          tmem_ld32(t + (gated ? 128 * (i & 1) + 32 * (i >> 1) : 32 * i), v);
+          tmem_ld32(t + (gated ? u_at * (i & 1) + 32 * (i >> 1) : 32 * i), v);
           put_lines(partial_at(u.part, i), v);
         }
         if (!summed) release_acc(ac);
@@ -748,7 +751,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (gated) {
           float w[32];
           if (whole) {
-            tmem_ld32x2(t + 32 * i, t + 128 + 32 * i, v, w);
+            tmem_ld32x2(t + 32 * i, t + u_at + 32 * i, v, w);
             if (j + 1 == blocks && !summed) release_acc(ac);
           } else {
             add_parts(2 * i, v);
@@ -870,7 +873,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       auto length = [&](int g) { return g < a.groups ? bounds[g + 1] - bounds[g] : 0; };
       int some = 0;
       for (int g = 0; g < a.groups; g += 32) some += __popc(__ballot_sync(0xffffffffu, length(g + lane) > 0));
-      const int each = 3 * up_div(a.wrows[0], 256) * up_div(a.wcols[0], 256), most = some > 0 ? a.pool / some / each : 0;
+      const int each = a.each[0] + a.each[1] + a.each[2], most = some > 0 && each > 0 ? a.pool / some / each : 0;
       int tiles = 0, blocks = 0, parts = 0, slots = 0;  // of the groups before
       for (int g0 = 0; g0 <= a.groups; g0 += 32) {
         const int g = g0 + lane, len = length(g);
