@@ -47,10 +47,11 @@ constexpr int kLoadB = 2, kScout = 3, kFirstEpi = 4;  // warps
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 // registers of a launch's 168 per thread as the roles' warps share them: 4 x 72 + 8 x 216 = 12 x 168
 constexpr int kFewRegisters = 72, kManyRegisters = 216;
-constexpr int kStages = 5, kStage = 2 * kTile;
-constexpr int kStaging = 8192;      // per epilogue warp: 4 blocks of 32 x 32 of 16 bits, 2 of fp32
+constexpr int kStages = 6, kStage = 2 * kTile;
+constexpr int kStaging = 4096;      // per epilogue warp: 2 blocks of 32 x 32 of 16 bits, 1 of fp32 (two of it and a stage
+                                    // of the ring less: 2% longer)
 constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
-// units that the roles of a pair may be apart, and more: 1 + 5 + 2 + 1 (every unit takes at least one of the ring's
+// units that the roles of a pair may be apart, and more: 1 + 6 + 2 + 1 (every unit takes at least one of the ring's
 // slots, of which each takes both CTAs' loading threads, and one of two accumulators)
 constexpr int kKept = 16;
 constexpr int kRun = 4;             // slices in a run of fp32 operands
@@ -461,6 +462,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             mn = a.b_columns[phase];
           }
         }
+        // (also rows that the group has not in the second CTA's half of the tile: a thread that loads nothing is held back
+        // by nothing, and one that falls two rounds of the ring behind takes another round's parity for its own)
         const uint32_t bytes = rank != 0 || is_b ? 0 : 2 * (kTile + (kTile >> narrow));
         const int bits = u.kind >= kOut ? a.plane_bits : 0, plane = of_planes ? bits : 0;
         used = min(used + (u.s1 - u.s0) * O::kTermsOf, kStages);
@@ -534,22 +537,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     int n = 0;  // accumulators so far
     int k = 0;  // staged blocks so far
     bool ok = true;
-    // A place for a block of `half` (2 KB: 16-bit elements) or whole size (fp32), whose copies out have been read: four of
-    // one, two of the other, and no copy on its way where one size follows the other.
+    // A place for a block of `half` (2 KB: 16-bit elements) or whole size (fp32), whose copies out have been read: two of
+    // one, one of the other, and no copy on its way where one size follows the other.
     bool halves = true;
     auto next_slot = [&](bool half) {
-      if (SPLIT && half != halves) {
-        if (lane == 0) sent_read<0>();
-        halves = half;
-      } else if (lane == 0) {
-        if (half)
-          sent_read<3>();
-        else
+      if (lane == 0) {
+        if (half && halves)
           sent_read<1>();
+        else
+          sent_read<0>();
       }
+      halves = half;
       __syncwarp();
-      const int at = k++;
-      return stage + (half ? at % 4 * 2048 : at % 2 * 4096);
+      return stage + (half ? (k++ & 1) * 2048 : 0);
     };
     auto send = [&](const CUtensorMap* map, const uint8_t* slot, int x, int y, int z) {
       before_tma();
