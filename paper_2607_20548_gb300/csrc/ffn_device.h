@@ -1,8 +1,11 @@
 // What the feed-forward block's two kernels share on the device.
 #pragma once
 
+#include <climits>
+
 #include "../../include/layer.h"
 #include "ffn.h"
+#include "pair.h"
 #include "types.h"
 
 namespace soap {
@@ -64,6 +67,53 @@ __device__ __forceinline__ int group_of(const int* prefix, int n, int q) {
   i = first + lane;
   return first + 31 - __clz(__ballot_sync(0xffffffffu, lane < step && i < n && prefix[i] <= q));
 }
+
+// What a scout's lanes hold of up to 64 groups, lane and lane + 32 of each, so that a unit's place takes no loads (a
+// chain of five, 4 us with the memory busy, when the units of 8 slices took 2.3). Dense: one group of all rows.
+struct Groups {
+  bool held;      // else there are more, and units look in memory
+  bool all_done;  // the first phase is stored: nothing more is waited for
+  int tiles[2], length[2], start[2], blocks[2], parts[2], part_count[2], slots[2];
+
+  __device__ __forceinline__ void load(const Args& a) {
+    const Plan& l = *a.plan;
+    const int lane = threadIdx.x & 31;
+    all_done = false;
+    held = a.groups <= 64;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int g = lane + 32 * h;
+      const bool in = held && g < a.groups;
+      tiles[h] = in ? l.row_tiles[g] : INT_MAX;
+      start[h] = in ? l.bounds[g] : 0;
+      length[h] = in ? l.bounds[g + 1] - l.bounds[g] : 0;
+      blocks[h] = in ? l.blocks[g] : 0;
+      parts[h] = in ? l.parts[g] : INT_MAX;
+      part_count[h] = in ? l.parts[g + 1] - l.parts[g] : 0;
+      slots[h] = in ? l.slots[g] : 0;
+    }
+  }
+  // The last group whose count before it is at most q.
+  __device__ __forceinline__ static int find(const int (&before)[2], int q) {
+    const unsigned lo = __ballot_sync(0xffffffffu, before[0] <= q), hi = __ballot_sync(0xffffffffu, before[1] <= q);
+    return hi ? 63 - __clz(hi) : 31 - __clz(lo);
+  }
+  __device__ __forceinline__ static int of(const int (&v)[2], int g) {
+    const int lo = __shfl_sync(0xffffffffu, v[0], g & 31), hi = __shfl_sync(0xffffffffu, v[1], g & 31);
+    return g < 32 ? lo : hi;
+  }
+  // Whether all groups' rows of the first phase are stored, `stored` blocks for each tile of them.
+  __device__ __forceinline__ bool done(const Args& a) {
+    if (all_done || !held) return all_done;
+    const int lane = threadIdx.x & 31;
+    bool ok = true;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (length[h] > 0) ok = ok && tc::load_acquire(a.done_group + lane + 32 * h) >= a.stored * up_div(length[h], a.row_tile);
+    __syncwarp();
+    return all_done = __all_sync(0xffffffffu, ok);
+  }
+};
 
 // Tile i of nm x nn in groups of 8 row tiles, row tile fastest, so that tiles in flight share operands in L2.
 __device__ __forceinline__ void tile_place(int i, int nm, int nn, int& m, int& n) {

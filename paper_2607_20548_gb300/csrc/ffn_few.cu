@@ -101,7 +101,7 @@ __device__ __forceinline__ void drain(uint32_t t, float (&v)[N]) {
 // A unit as all lanes of a warp work it out. Units go group by group, and a group's row by row of feature tiles: the
 // row tiles of a group with more than one take the same weights one after another.
 template <int NT>
-__device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
+__device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h, const Groups& c) {
   const Plan& l = *a.plan;
   const bool dense = a.offsets == nullptr;
   Unit u{};
@@ -119,13 +119,21 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
   int nm = up_div(a.rows, NT);
   u.M = a.rows;
   if (!dense) {
-    u.group = group_of(l.row_tiles, a.groups, i / nn);
-    u.row_tile = l.row_tiles[u.group];
-    nm = l.row_tiles[u.group + 1] - u.row_tile;
+    if (c.held) {
+      u.group = Groups::find(c.tiles, i / nn);
+      u.row_tile = Groups::of(c.tiles, u.group);
+      u.start = Groups::of(c.start, u.group);
+      u.M = Groups::of(c.length, u.group);
+      u.block = Groups::of(c.blocks, u.group);
+    } else {
+      u.group = group_of(l.row_tiles, a.groups, i / nn);
+      u.row_tile = l.row_tiles[u.group];
+      u.start = l.bounds[u.group];
+      u.M = l.bounds[u.group + 1] - u.start;
+      u.block = l.blocks[u.group];
+    }
+    nm = up_div(u.M, NT);
     i -= u.row_tile * nn;
-    u.start = l.bounds[u.group];
-    u.M = l.bounds[u.group + 1] - u.start;
-    u.block = l.blocks[u.group];
   }
   const int n = i / nm, m = i - n * nm;
   u.n0 = n * wide;
@@ -199,6 +207,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = !a.hold || flag_wait(a.hold, lim);  // a flag that nothing sets: every role's wait runs out
     const Plan& l = *a.plan;
     const Head head{l.total, {0, l.first[1], 0}, {l.tiles[0], l.tiles[1]}, {1, l.splits[1]}, 0};
+    Groups groups;
+    groups.load(a);
     for (int m = 0; ok; ++m) {
       int p = -1;
       if (lane == 0 && (ok = wait_given(begun_at, m, 2 * lim) && !*abort_flag)) {
@@ -211,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (p < 0)
         u.kind = kEnd;
       else
-        u = unit_at<NT>(p, a, head);
+        u = unit_at<NT>(p, a, head, groups);
       if (lane == 0) {
         units[m % kKept] = u;
         set_ready(known_at, m + 1);

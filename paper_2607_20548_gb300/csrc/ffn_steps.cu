@@ -51,9 +51,10 @@ constexpr int kStages = 6, kStage = 2 * kTile;
 constexpr int kStaging = 4096;      // per epilogue warp: 2 blocks of 32 x 32 of 16 bits, 1 of fp32 (two of it and a stage
                                     // of the ring less: 2% longer)
 constexpr int kPerTile = 2 * kEpiWarps;  // what a tile adds to its counters
-// units that the roles of a pair may be apart, and more: 1 + 6 + 2 + 1 (every unit takes at least one of the ring's
+// units that the roles of a pair may be apart, and more: 2 + 6 + 2 + 1 (every unit takes at least one of the ring's
 // slots, of which each takes both CTAs' loading threads, and one of two accumulators)
 constexpr int kKept = 16;
+constexpr int kShort = 16;          // slices of a unit that is short
 constexpr int kRun = 4;             // slices in a run of fp32 operands
 
 struct Unit {
@@ -140,7 +141,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t t, const float (&v)[16]) {
       : "memory");
 }
 
-__device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
+__device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h, const Groups& c) {
   const Plan& l = *a.plan;
   const bool dense = a.clips == nullptr;  // then all prefixes are 0 and everything there is
   Unit u{};
@@ -160,13 +161,21 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
     int nm = up_div(a.rows, 256);
     u.M = a.rows;
     if (!dense) {
-      u.group = group_of(l.row_tiles, a.groups, i / nn);
-      u.row_tile = l.row_tiles[u.group];
-      nm = l.row_tiles[u.group + 1] - u.row_tile;
+      if (c.held) {
+        u.group = Groups::find(c.tiles, i / nn);
+        u.row_tile = Groups::of(c.tiles, u.group);
+        u.start = Groups::of(c.start, u.group);
+        u.M = Groups::of(c.length, u.group);
+        u.block = Groups::of(c.blocks, u.group);
+      } else {
+        u.group = group_of(l.row_tiles, a.groups, i / nn);
+        u.row_tile = l.row_tiles[u.group];
+        u.start = l.bounds[u.group];
+        u.M = l.bounds[u.group + 1] - u.start;
+        u.block = l.blocks[u.group];
+      }
+      nm = up_div(u.M, 256);
       i -= u.row_tile * nn;
-      u.start = l.bounds[u.group];
-      u.M = l.bounds[u.group + 1] - u.start;
-      u.block = l.blocks[u.group];
     }
     int m, n;
     tile_place(i, nm, nn, m, n);
@@ -185,16 +194,24 @@ __device__ __forceinline__ Unit unit_at(int p, const Args& a, const Head& h) {
     int rows = a.rows, slots = 0;
     u.splits = h.parts;
     u.part = q;
-    u.need = up_div(rows, 256);
     if (!dense) {
-      u.group = group_of(l.parts, a.groups, q);
-      u.part = q - l.parts[u.group];
-      u.splits = l.parts[u.group + 1] - l.parts[u.group];
-      slots = l.slots[u.group];
-      u.start = l.bounds[u.group];
-      rows = l.bounds[u.group + 1] - u.start;
-      u.need = l.row_tiles[u.group + 1] - l.row_tiles[u.group];
+      if (c.held) {
+        u.group = Groups::find(c.parts, q);
+        u.part = q - Groups::of(c.parts, u.group);
+        u.splits = Groups::of(c.part_count, u.group);
+        slots = Groups::of(c.slots, u.group);
+        u.start = Groups::of(c.start, u.group);
+        rows = Groups::of(c.length, u.group);
+      } else {
+        u.group = group_of(l.parts, a.groups, q);
+        u.part = q - l.parts[u.group];
+        u.splits = l.parts[u.group + 1] - l.parts[u.group];
+        slots = l.slots[u.group];
+        u.start = l.bounds[u.group];
+        rows = l.bounds[u.group + 1] - u.start;
+      }
     }
+    u.need = up_div(rows, 256);
     i -= q * each;
     u.tile = slots * each + i;
     u.slot = u.tile + u.part * each;
@@ -369,12 +386,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const Head head{l.total, {0, l.first[1], l.first[2]}, {l.tiles[0], l.tiles[1]}, {l.splits[0], l.splits[1]}, l.parts[1]};
     uint32_t peer;
     asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(peer) : "r"(smem_u32(tmem_at + 2)));
+    Groups groups;
+    groups.load(a);
+    // Short units: the next one is taken as this one becomes known, and not only when its loads begin, so that the trip to
+    // the list's counter is over by then. (Of long ones a pair would hold one while others end.)
+    bool ahead = false;
+    int held = -1;
     for (int m = 0; ok; ++m) {
       int p = -1;
       if (lane == 0) {
         if (rank == 0) {
-          if ((ok = wait_given(begun_at, m, 2 * lim))) {
-            p = atomicAdd(&a.plan->next, 1);
+          if ((ok = wait_given(begun_at, ahead ? m - 1 : m, 2 * lim))) {
+            p = ahead ? held : atomicAdd(&a.plan->next, 1);
             if (p >= head.total) p = -1;
             asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * (m % kKept)), "r"(p) : "memory");
             asm volatile("st.release.cluster.shared::cluster.b32 [%0], %1;" ::"r"(peer + 4 * kKept + 12), "r"(m + 1)
@@ -391,14 +414,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (p < 0)
         u.kind = kEnd;
       else
-        u = unit_at(p, a, head);
+        u = unit_at(p, a, head, groups);
       if (lane == 0) {
         units[m % kKept] = u;
         set_ready(known_at, m + 1);
-        if (u.kind == kOut)
-          ok = wait_done(a.done_row + u.row_tile, a.stored, lim);
-        else if (u.kind == kWeight)
-          ok = wait_done(a.done_group + u.group, a.stored * u.need, lim);
+        ahead = p >= 0 && (u.s1 - u.s0) * O::kTermsOf <= kShort;
+        if (ahead && rank == 0) held = atomicAdd(&a.plan->next, 1);
+      }
+      const bool free = u.kind < kOut || groups.done(a);
+      if (lane == 0) {
+        if (!free)
+          ok = u.kind == kOut ? wait_done(a.done_row + u.row_tile, a.stored, lim)
+                              : wait_done(a.done_group + u.group, a.stored * u.need, lim);
         if (ok) {
           asm volatile("fence.proxy.async;" ::: "memory");  // what other CTAs stored, before copies of it
           set_ready(ready_at, m + 1);
