@@ -139,7 +139,8 @@ soap_status_t layer_ffn_forward(int64_t rows, int64_t hidden, int64_t width, int
  *   dh = dy Wd^T,  dg = dh u act'(g),  du = dh act(g)
  *   dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dWd = h^T dy
  * d_gate, d_up, d_down: receive the weights' gradients (`type`; 0 for an empty group; each in its weight's order:
- * columns as there), all three NULL: not formed. Rows of no group have dx 0, whatever their x and dy hold. */
+ * columns as there), all three NULL: not formed. Rows of no group have dx 0, whatever their x and dy hold. Results
+ * must not overlap an operand. */
 soap_status_t layer_ffn_backward(int64_t rows, int64_t hidden, int64_t width, int32_t groups,
                                  const int32_t* offsets, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
                                  int32_t type, const layer_matrix_t* gate, const layer_matrix_t* up,

@@ -277,3 +277,33 @@ def test_operands_off_their_units(cuda):
     assert torch.equal(y, y2)
     assert all(torch.equal(a, b) for a, b in zip(grads, ffn_backward(move(dy), move(x), pre2, *ms)))
     _check(x, w, "silu", y, dy, grads)
+
+
+@pytest.mark.parametrize("tokens,dim", [(3, 64), (4000, 128), (900, 50)])
+@pytest.mark.parametrize("t", [BF, F32])
+def test_heads_in_place(cuda, t, tokens, dim):
+    """Results over their operands (C interface): the bits of results of their own."""
+    lib, dt = S.load_library(), S.DTYPES[t]
+    q, k = torch.randn(tokens, 6, dim, device=cuda).to(t), torch.randn(tokens, 2, dim, device=cuda).to(t)
+    dq, dk = torch.randn(q.shape, device=cuda).to(t), torch.randn(k.shape, device=cuda).to(t)
+    w = 1 + 0.1 * torch.randn(dim, device=cuda)
+    cos, sin = torch.randn(tokens, dim // 2, device=cuda), torch.randn(tokens, dim // 2, device=cuda)
+    want = qk_rotary_forward(q, k, cos, sin, None, w, w)
+    back = qk_rotary_backward(dq, dk, q, k, cos, sin, None, w, w)
+    h = lambda v: S.layer_heads(v.data_ptr(), 0, v.stride(0), v.stride(1))  # noqa: E731
+    sizes = (1, tokens, 6, 2, dim, dim, 0)
+    how = (dt, w.data_ptr(), w.data_ptr(), 0, 1e-6, cos.data_ptr(), sin.data_ptr(), tokens, None, 0)
+    stream = torch.cuda.current_stream(cuda).cuda_stream
+    a, b = q.clone(), k.clone()
+    assert lib.layer_qk_forward(*sizes, h(a), h(b), *how, h(a), h(b), None, stream) == 0
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+    size = lib.layer_qk_workspace_bytes(1, tokens, 6, 2, dim)
+    ws, dw = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device=cuda), torch.empty(2, dim, device=cuda)
+    for over_q in (False, True):
+        a, b, c, d = dq.clone(), dk.clone(), q.clone(), k.clone()
+        to = (c, d) if over_q else (a, b)
+        assert lib.layer_qk_backward(*sizes, h(a), h(b), h(c), h(d), *how, h(to[0]), h(to[1]), dw[0].data_ptr(),
+                                     dw[1].data_ptr(), None, ws.data_ptr(), size, stream) == 0
+        assert torch.equal(to[0], back[0]) and torch.equal(to[1], back[1])
+        assert torch.equal(dw[0], back[2]) and torch.equal(dw[1], back[3])
+    assert bool((ws[size:] == 0xA5).all())
