@@ -721,8 +721,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       auto report = [&](int count) {
         if (u.kind <= kGrad && lane == 0 && count > 0) {
           sent_done<0>();
-          asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_row + u.row_tile), "r"(count) : "memory");
-          asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_group + u.group), "r"(count) : "memory");
+          asm volatile("fence.acq_rel.gpu;" ::: "memory");  // (once for both)
+          asm volatile("red.relaxed.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_row + u.row_tile), "r"(count) : "memory");
+          asm volatile("red.relaxed.gpu.global.add.s32 [%0], %1;" ::"l"(a.done_group + u.group), "r"(count) : "memory");
         }
       };
       const int turn = u.splits > 1 && blocks > 0 ? u.part % blocks : 0;

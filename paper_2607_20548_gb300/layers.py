@@ -16,6 +16,7 @@ bounded device wait that gave up shows in the results alone, as NaN.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from typing import NamedTuple, Optional
 
@@ -30,6 +31,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current = getattr(torch._C, "_cuda_getDevice", None)
 _F32, _I32 = torch.float32, torch.int32
 _empty, _empty_like = torch.empty, torch.empty_like
+
+
+@functools.lru_cache(4096)
+def _size(function, *args):
+    """What one of the library's functions of sizes alone gives (asked through ctypes, 1 us each time)."""
+    return getattr(load_library(), function)(*args)
 
 
 def _refuse(name, t, dtype, device):
@@ -343,6 +350,10 @@ def _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status):
     return (batch, length, heads, kv_heads, dim, rotary), (hq, hk), weights, table, (made_q, made_k, positions)
 
 
+def _dense_like(t, dev):
+    return _empty_like(t) if t.is_contiguous() else _empty(t.shape, dtype=t.dtype, device=dev)
+
+
 def _dense_heads(t, sizes, heads):
     dim = sizes[4]
     return layer_heads(t.data_ptr(), sizes[1] * heads * dim, heads * dim, dim)
@@ -367,7 +378,7 @@ def qk_rotary_forward(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tens
         with _elsewhere(index, stream, q, k, cos, sin, positions, q_weight, k_weight, status):
             return qk_rotary_forward(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, status)
     sizes, heads, w, table, held = _qk_common(name, q, k, cos, sin, positions, q_weight, k_weight, status)
-    out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
+    out_q, out_k = _dense_like(q, dev), _dense_like(k, dev)
     _done(load_library().layer_qk_forward(
         *sizes, int(interleaved), *heads, DTYPES[q.dtype], *w, eps, *table, _dense_heads(out_q, sizes, sizes[2]),
         _dense_heads(out_k, sizes, sizes[3]), None if status is None else status.data_ptr(), _raw_stream(index)), name)
@@ -397,12 +408,12 @@ def qk_rotary_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: t
             raise ValueError(f"{name}: a gradient has another shape than its operand")
         found = _heads(name, d, q.dtype, index)
         grads.append((found[0], found[-1]))
-    out_q, out_k = _empty(q.shape, dtype=q.dtype, device=dev), _empty(k.shape, dtype=q.dtype, device=dev)
+    out_q, out_k = _dense_like(q, dev), _dense_like(k, dev)
     lib = load_library()
     dwq = dwk = ws = None
     ws_bytes = 0
     if params:
-        ws_bytes = lib.layer_qk_workspace_bytes(*sizes[:5])
+        ws_bytes = _size("layer_qk_workspace_bytes", *sizes[:5])
         dwq, dwk = _empty(sizes[4], dtype=_F32, device=dev), _empty(sizes[4], dtype=_F32, device=dev)
         ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
@@ -547,9 +558,9 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     shape = x.shape
     sizes, x, ld, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
     lib, t = load_library(), DTYPES[x.dtype]
-    y = _empty(shape, dtype=x.dtype, device=dev)
-    pre = _empty(lib.layer_ffn_pre_elems(sizes[0], sizes[2], sizes[3]), dtype=_F32, device=dev) if keep else None
-    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, units % 16 == 0, 0)
+    y = _dense_like(x, dev)
+    pre = _empty(_size("layer_ffn_pre_elems", sizes[0], sizes[2], sizes[3]), dtype=_F32, device=dev) if keep else None
+    ws_bytes = _size("layer_ffn_workspace_bytes", *sizes, t, units % 16 == 0, 0)
     ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_ffn_forward(
         *sizes, None if offsets is None else offsets.data_ptr(), x.data_ptr(), ld, t, held[0][0], held[1][0],
@@ -578,9 +589,9 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
     dy, _, ld_dy = _rows(dy)
     lib, t = load_library(), DTYPES[x.dtype]
     _operand(name, pre, _F32, dev)
-    if pre.numel() != lib.layer_ffn_pre_elems(sizes[0], sizes[2], sizes[3]) or not pre.is_contiguous():
+    if pre.numel() != _size("layer_ffn_pre_elems", sizes[0], sizes[2], sizes[3]) or not pre.is_contiguous():
         raise ValueError(f"{name}: pre is of another call")
-    dx = _empty(shape, dtype=x.dtype, device=dev)
+    dx = _dense_like(x, dev)
     grads, out = [None] * 3, [None] * 3
     if params:
         # in the order in which its weight lies: stored [groups, rows, cols], seen transposed if that is column-major
@@ -588,7 +599,7 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
         grads = [layer_matrix(g.data_ptr(), f[4], f[3] * f[4], f[2]) for g, f in zip(made, held)]
         out = [g.mT if f[2] else g for g, f in zip(made, held)]
     units |= dy.data_ptr() | ld_dy * dy.element_size()
-    ws_bytes = lib.layer_ffn_workspace_bytes(*sizes, t, units % 16 == 0, 1)
+    ws_bytes = _size("layer_ffn_workspace_bytes", *sizes, t, units % 16 == 0, 1)
     ws = _empty(ws_bytes, dtype=torch.uint8, device=dev)
     _done(lib.layer_ffn_backward(
         *sizes, None if offsets is None else offsets.data_ptr(), dy.data_ptr(), ld_dy, x.data_ptr(), ld, t,
