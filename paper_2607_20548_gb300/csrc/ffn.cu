@@ -139,68 +139,6 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   return l;
 }
 
-// Copies of operands with rows of whole 16-byte units: 16-bit elements as they are, fp32 ones as three bf16 planes
-// that add up to the element (8 bits of its significand each; what is not finite: the first plane alone).
-struct CopyJob {
-  const void* src;
-  int64_t ld, stride;   // of rows and of matrices
-  int64_t rows;         // of a matrix
-  int inner, ld_out;
-  int64_t matrices;
-  uint16_t* dst;
-  int64_t plane;
-};
-struct CopyJobs {
-  CopyJob job[5];
-  int n;
-};
-
-template <bool SPLIT>
-__global__ void __launch_bounds__(256) copy_kernel(const __grid_constant__ CopyJobs jobs) {
-  for (int j = 0; j < jobs.n; ++j) {
-    const CopyJob& c = jobs.job[j];
-    const int chunks = c.ld_out / 8;
-    const int64_t all = c.matrices * c.rows * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-      const int64_t row = i / chunks, m = row / c.rows, r = row - m * c.rows;
-      const int col = (int)(i - row * chunks) * 8, n = min(8, c.inner - col);
-      const int64_t from = m * c.stride + r * c.ld + col;
-      Pack<uint16_t, 8> out[SPLIT ? 3 : 1];
-      alignas(16) float in[SPLIT ? 8 : 1];
-      if constexpr (SPLIT) {
-        const float* const p = static_cast<const float*>(c.src) + from;
-        if (n == 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
-          *reinterpret_cast<float4*>(in) = *reinterpret_cast<const float4*>(p);
-          *reinterpret_cast<float4*>(in + 4) = *reinterpret_cast<const float4*>(p + 4);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) in[e] = e < n ? p[e] : 0.f;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (SPLIT) {
-          const float x = in[e];
-          const uint32_t b = __float_as_uint(x);
-          const bool finite = fabsf(x) < INFINITY;
-          const float hi = __uint_as_float(b & 0xffff0000u), rest = finite ? x - hi : 0.f;
-          const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
-          const float low = rest - __uint_as_float(mid);
-          // (a NaN stays one without its lower bits)
-          out[0].v[e] = (uint16_t)((b >> 16) | (x != x ? 0x40u : 0u));
-          out[1].v[e] = (uint16_t)(mid >> 16);
-          out[2].v[e] = (uint16_t)(__float_as_uint(low) >> 16);
-        } else {
-          out[0].v[e] = e < n ? static_cast<const uint16_t*>(c.src)[from + e] : (uint16_t)0;
-        }
-      }
-#pragma unroll
-      for (int p = 0; p < (SPLIT ? 3 : 1); ++p)
-        *reinterpret_cast<Pack<uint16_t, 8>*>(c.dst + p * c.plane + row * c.ld_out + col) = out[p];
-    }
-  }
-}
-
 struct Call {
   int64_t rows;
   int hidden, width, groups;
@@ -281,7 +219,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     const int cols = (int)(!mat ? c.hidden : m->columns ? wr : wc);
     const int n = mat ? c.groups : 1;
     v[i] = View{const_cast<void*>(in[i]), rows, mat ? m->ld : i ? ld_dy : ld_x, mat ? m->stride : 0, cols, n};
-    if (!copy[i]) continue;
+    if (!copy[i] || c.rows == 0) continue;
     CopyJob& j = jobs.job[jobs.n++];
     j = CopyJob{in[i], v[i].ld, v[i].stride, rows, cols, (int)up8(cols), n, reinterpret_cast<uint16_t*>(c.ws + place[i]), 0};
     v[i].p = j.dst;
@@ -391,17 +329,8 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     a.stride_dw[p] = grads[p]->stride;
   }
 
-  cudaError_t e = prepare(maps, a, c.type, s);
+  const cudaError_t e = prepare(maps, a, jobs, chunks, c.type, s);
   if (e != cudaSuccess || c.rows == 0) return e;
-  if (jobs.n > 0) {
-    const unsigned ctas = (unsigned)std::min<int64_t>(152 * 8, (chunks + 255) / 256);
-    if (f32)
-      copy_kernel<true><<<ctas, 256, 0, s>>>(jobs);
-    else
-      copy_kernel<false><<<ctas, 256, 0, s>>>(jobs);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-  }
   return few ? run_few(maps, a, c.type, l.units, s) : run(maps, a, c.type, l.units, s);
 }
 

@@ -81,12 +81,29 @@ struct Args {
   int done_words;               // to zero, from done_row on
 };
 
+// Copies of operands with rows of whole 16-byte units: 16-bit elements as they are, fp32 ones as three bf16 planes
+// that add up to the element (8 bits of its significand each; what is not finite: the first plane alone).
+struct CopyJob {
+  const void* src;
+  int64_t ld, stride;   // of rows and of matrices
+  int64_t rows;         // of a matrix
+  int inner, ld_out;
+  int64_t matrices;
+  uint16_t* dst;
+  int64_t plane;
+};
+struct CopyJobs {
+  CopyJob job[5];
+  int n;
+};
+
 // type: soap_dtype_t. units: no more than this many are ever in the list.
 cudaError_t run(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s);
 // The same for few rows of 16-bit types, forward.
 cudaError_t run_few(const Maps& maps, const Args& a, int type, int64_t units, cudaStream_t s);
-// The plan, the groups' maps, zeros for rows of no group and for the gradients of groups without rows.
-cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s);
+// The plan, the groups' maps, zeros for rows of no group and for the gradients of groups without rows, and the copies
+// (`chunks`: of 8 elements, in the largest of them).
+cudaError_t prepare(const Maps& maps, const Args& a, const CopyJobs& jobs, int64_t chunks, int type, cudaStream_t s);
 
 // (a 64-bit division takes a scout longer than its loads)
 template <typename A, typename B>

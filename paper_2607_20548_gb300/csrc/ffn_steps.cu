@@ -867,6 +867,52 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
   bounds = buf[at];
 }
 
+template <bool SPLIT>
+__device__ __forceinline__ void copy_operands(const CopyJobs& jobs) {
+  for (int j = 0; j < jobs.n; ++j) {
+    const CopyJob& c = jobs.job[j];
+    const int chunks = c.ld_out / 8;
+    const int64_t all = c.matrices * c.rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kPrepThreads) {
+      const int64_t row = i / chunks, m = row / c.rows, r = row - m * c.rows;
+      const int col = (int)(i - row * chunks) * 8, n = min(8, c.inner - col);
+      const int64_t from = m * c.stride + r * c.ld + col;
+      Pack<uint16_t, 8> out[SPLIT ? 3 : 1];
+      alignas(16) float in[SPLIT ? 8 : 1];
+      if constexpr (SPLIT) {
+        const float* const p = static_cast<const float*>(c.src) + from;
+        if (n == 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+          *reinterpret_cast<float4*>(in) = *reinterpret_cast<const float4*>(p);
+          *reinterpret_cast<float4*>(in + 4) = *reinterpret_cast<const float4*>(p + 4);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) in[e] = e < n ? p[e] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (SPLIT) {
+          const float x = in[e];
+          const uint32_t b = __float_as_uint(x);
+          const bool finite = fabsf(x) < INFINITY;
+          const float hi = __uint_as_float(b & 0xffff0000u), rest = finite ? x - hi : 0.f;
+          const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
+          const float low = rest - __uint_as_float(mid);
+          // (a NaN stays one without its lower bits)
+          out[0].v[e] = (uint16_t)((b >> 16) | (x != x ? 0x40u : 0u));
+          out[1].v[e] = (uint16_t)(mid >> 16);
+          out[2].v[e] = (uint16_t)(__float_as_uint(low) >> 16);
+        } else {
+          out[0].v[e] = e < n ? static_cast<const uint16_t*>(c.src)[from + e] : (uint16_t)0;
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < (SPLIT ? 3 : 1); ++p)
+        *reinterpret_cast<Pack<uint16_t, 8>*>(c.dst + p * c.plane + row * c.ld_out + col) = out[p];
+    }
+  }
+}
+
 // All CTAs: `rows` rows of `cols` elements become 0; from row `first` on those that follow row `last`.
 template <typename T>
 __device__ __forceinline__ void zero_rows(T* p, int64_t ld, int64_t rows, int cols, int64_t first, int64_t last) {
@@ -887,7 +933,7 @@ __device__ __forceinline__ void zero_rows(T* p, int64_t ld, int64_t rows, int co
 // The first CTA: the plan and zeros for the counters. All: the groups' maps, zeros for rows of no group and for the
 // gradients of groups without rows.
 template <typename T>
-__global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a, const __grid_constant__ CopyJobs jobs) {
   __shared__ int buf[2][kMaxGroups + 1];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the products' CTAs set themselves up meanwhile
   int* bounds;
@@ -949,6 +995,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
     }
   }
+  copy_operands<sizeof(T) == 4>(jobs);
   if (!a.offsets && a.rows > 0) return;
   const int first = bounds[0], last = bounds[a.groups];
   const int64_t outside = first + (a.rows - last);
@@ -998,15 +1045,16 @@ cudaError_t launch(const Maps& maps, const Args& a, int64_t units, cudaStream_t 
 
 }  // namespace
 
-cudaError_t prepare(const Maps& maps, const Args& a, int type, cudaStream_t s) {
-  // dense: nothing but the plan; groups: as many CTAs as rows and gradients to zero can keep busy
-  const int ctas = a.offsets || a.rows == 0 ? 304 : 1;
+cudaError_t prepare(const Maps& maps, const Args& a, const CopyJobs& jobs, int64_t chunks, int type, cudaStream_t s) {
+  // dense: nothing but the plan; groups: as many CTAs as rows and gradients to zero can keep busy; copies: as they can
+  int64_t ctas = a.offsets || a.rows == 0 ? 304 : 1;
+  if (jobs.n > 0) ctas = std::max(ctas, std::min<int64_t>(kSms * 8, (chunks + kPrepThreads - 1) / kPrepThreads));
   if (type == SOAP_F32)
-    prepare_kernel<float><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+    prepare_kernel<float><<<(unsigned)ctas, kPrepThreads, 0, s>>>(maps, a, jobs);
   else if (type == SOAP_BF16)
-    prepare_kernel<__nv_bfloat16><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+    prepare_kernel<__nv_bfloat16><<<(unsigned)ctas, kPrepThreads, 0, s>>>(maps, a, jobs);
   else
-    prepare_kernel<__half><<<ctas, kPrepThreads, 0, s>>>(maps, a);
+    prepare_kernel<__half><<<(unsigned)ctas, kPrepThreads, 0, s>>>(maps, a, jobs);
   return cudaGetLastError();
 }
 
