@@ -40,13 +40,11 @@ bool few_rows(int64_t rows, int groups, int type, bool backward) {
   return !backward && type != SOAP_F32 && rows <= 64 * (int64_t)groups;
 }
 
-// Planes that h, dg and du are kept in: fp32 three of bf16; 16-bit types their rounding, and for few rows and small
-// weights, where a few latencies set the time, what that leaves too (100 rows over 8 groups of 256 x 512 bf16, both
-// passes: 2% longer, and y, dx and the weights' gradients as near as one rounding; with large weights it is worth
-// less than it takes: 24 rows of 2048 x 8192 128 us in one plane, 152 in two, 192 rows over 64 groups of 2048 x 768
-// forward 99 and 111).
+// Planes that h, dg and du are kept in: fp32 three of bf16; 16-bit types their rounding and, where there are few results
+// in whose errors it would not average out, and a few latencies set the time (small weights), also what that leaves
+// (1 row of 64 x 64 bf16, both passes: 33 us in one plane, 36 in two; 24 rows of 1024 x 1024, which have one, 56 and 67).
 int planes_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type) {
-  return type == SOAP_F32 ? 3 : rows <= 64 * (int64_t)groups && groups * hidden * width <= 1 << 23 ? 2 : 1;
+  return type == SOAP_F32 ? 3 : rows * hidden <= 16384 && groups * hidden * width <= 1 << 23 ? 2 : 1;
 }
 
 // Slices of a tile's sums, per phase (of the weights' gradients: of all rows). Planes of 16-bit types are added one
