@@ -54,7 +54,8 @@ struct Slices {
   int64_t n[3];
 };
 Slices slices_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type, bool backward) {
-  const int twice = backward && type != SOAP_F32 && planes_of(rows, hidden, width, groups, type) == 2 ? 2 : 1;
+  const bool few = few_rows(rows, groups, type, backward);
+  const int twice = !few && type != SOAP_F32 && planes_of(rows, hidden, width, groups, type) == 2 ? 2 : 1;
   return Slices{{up_div(hidden, 64), twice * (backward ? 2 : 1) * (int64_t)up_div(width, 64), twice * (int64_t)up_div(rows, 64)}};
 }
 

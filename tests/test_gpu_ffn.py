@@ -164,7 +164,8 @@ def test_serving(cuda, t):
     _run(cuda, [2, 0, 1, 7], 256, 192, t, train=False, behind=2)
 
 
-@pytest.mark.parametrize("rows,hidden,width", [(1, 512, 512), (13, 300, 200), (1, 4096, 70), (64, 64, 1000)])
+@pytest.mark.parametrize("rows,hidden,width", [(1, 512, 512), (13, 300, 200), (1, 4096, 70), (64, 64, 1000),
+                                               (200, 64, 500), (1500, 8, 300)])
 @pytest.mark.parametrize("t", [BF, HF])
 def test_few_results_round_once(cuda, t, rows, hidden, width):
     """h, dg and du are kept to twice the type's bits: the results' own rounding is all that is left of 16 bits."""
