@@ -220,7 +220,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
     v[i] = View{const_cast<void*>(in[i]), rows, mat ? m->ld : i ? ld_dy : ld_x, mat ? m->stride : 0, cols, n};
     if (!copy[i] || c.rows == 0) continue;
     CopyJob& j = jobs.job[jobs.n++];
-    j = CopyJob{in[i], v[i].ld, v[i].stride, rows, cols, (int)up8(cols), n, reinterpret_cast<uint16_t*>(c.ws + place[i]), 0};
+    j = CopyJob{in[i], v[i].ld, v[i].stride, rows, cols, (int)up8(cols), n, mat, reinterpret_cast<uint16_t*>(c.ws + place[i]), 0};
     v[i].p = j.dst;
     v[i].ld = j.ld_out;
     v[i].stride = rows * j.ld_out;

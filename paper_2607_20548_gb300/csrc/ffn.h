@@ -89,6 +89,7 @@ struct CopyJob {
   int64_t rows;         // of a matrix
   int inner, ld_out;
   int64_t matrices;
+  int of_groups;        // whether they are the groups'
   uint16_t* dst;
   int64_t plane;
 };

@@ -868,13 +868,14 @@ __device__ void find_bounds(const Args& a, int (&buf)[2][kMaxGroups + 1], int*& 
 }
 
 template <bool SPLIT>
-__device__ __forceinline__ void copy_operands(const CopyJobs& jobs) {
+__device__ __forceinline__ void copy_operands(const CopyJobs& jobs, const int* bounds) {
   for (int j = 0; j < jobs.n; ++j) {
     const CopyJob& c = jobs.job[j];
     const int chunks = c.ld_out / 8;
     const int64_t all = c.matrices * c.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kPrepThreads) {
       const int64_t row = i / chunks, m = row / c.rows, r = row - m * c.rows;
+      if (c.of_groups && bounds[m + 1] == bounds[m]) continue;  // nothing reads them
       const int col = (int)(i - row * chunks) * 8, n = min(8, c.inner - col);
       const int64_t from = m * c.stride + r * c.ld + col;
       Pack<uint16_t, 8> out[SPLIT ? 3 : 1];
@@ -995,7 +996,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const __grid_cons
       asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
     }
   }
-  copy_operands<sizeof(T) == 4>(jobs);
+  copy_operands<sizeof(T) == 4>(jobs, bounds);
   if (!a.offsets && a.rows > 0) return;
   const int first = bounds[0], last = bounds[a.groups];
   const int64_t outside = first + (a.rows - last);
