@@ -120,6 +120,9 @@ typedef enum { LAYER_SILU = 0, LAYER_GELU = 1 } layer_act_t;
  * library's own), or NULL. Products are summed in fp32. For 16-bit types h is rounded to the type before the second
  * product (the backward pass's dg, du and h too; fp16: a value above 65504 is then infinite), but for up to 16384
  * elements of x and small weights to twice its bits; g and u are not.
+ * Infinite elements give the infinities and NaN of products in the type, with two exceptions that give NaN in a sum
+ * that an infinity would decide: fp32 beside elements below 2^-62, which are used in parts that may be 0, and 16-bit
+ * types where h, dg and du have twice the bits.
  * x, y: row i at element i * ld; y must not overlap an operand. status: NULL, or a device int32 (not cleared); where a
  * bounded wait gave up (soap_wait_limit), SOAP_STATUS_TIMEOUT is ORed into it and all results are NaN.
  * 0 <= rows <= 2^31 - 2^16; 1 <= hidden, width <= 65536; 1 <= groups <= 1024. `workspace`: 256-byte aligned,

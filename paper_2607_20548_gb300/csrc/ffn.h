@@ -82,7 +82,13 @@ struct Args {
 };
 
 // Copies of operands with rows of whole 16-byte units: 16-bit elements as they are, fp32 ones as three bf16 planes
-// that add up to the element (8 bits of its significand each; what is not finite: the first plane alone).
+// that add up to the element (8 bits of its significand each).
+//
+// Every plane is multiplied by planes of the other operand, of which one may be infinite: a lower plane that is 0 (one in
+// 256 of them, and all of bf16 values') would make NaN of what is an infinity. So a plane is at least kLeast of what the
+// plane before it was taken from, with its sign: 2^-32 of the element, 2^-8 of an fp32 rounding. That is a bf16 value for
+// elements from 2^-62 on; all of an infinity's planes are infinite, all of a zero's 0 (0 x inf is NaN).
+constexpr float kLeast = 2.3283064365386963e-10f;  // 2^-32
 struct CopyJob {
   const void* src;
   int64_t ld, stride;   // of rows and of matrices

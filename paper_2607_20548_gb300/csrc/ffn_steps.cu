@@ -307,13 +307,12 @@ __device__ __forceinline__ void put(uint8_t* slot, const float (&v)[32], int lan
   }
 }
 
-// The upper 8 bits of x's significand as bf16, and what is left (nothing of what is not finite).
+// The upper 8 bits of x's significand as bf16, and what is left in x, kLeast of it at least (of an infinity that, the
+// difference of two infinities being a NaN, which fmaxf passes over).
 __device__ __forceinline__ float upper(float& x) {
   const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-  const bool finite = fabsf(x) < INFINITY;
-  const float r = finite ? hi : x;
-  x = finite ? x - hi : 0.f;
-  return r;
+  x = copysignf(fmaxf(fabsf(x) - fabsf(hi), fabsf(x) * kLeast), hi);
+  return hi;
 }
 
 __device__ __forceinline__ void fence_map(const CUtensorMap* m) {
@@ -893,16 +892,11 @@ __device__ __forceinline__ void copy_operands(const CopyJobs& jobs, const int* b
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (SPLIT) {
-          const float x = in[e];
-          const uint32_t b = __float_as_uint(x);
-          const bool finite = fabsf(x) < INFINITY;
-          const float hi = __uint_as_float(b & 0xffff0000u), rest = finite ? x - hi : 0.f;
-          const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
-          const float low = rest - __uint_as_float(mid);
+          float x = in[e];
           // (a NaN stays one without its lower bits)
-          out[0].v[e] = (uint16_t)((b >> 16) | (x != x ? 0x40u : 0u));
-          out[1].v[e] = (uint16_t)(mid >> 16);
-          out[2].v[e] = (uint16_t)(__float_as_uint(low) >> 16);
+          const uint32_t quiet = x != x ? 0x40u : 0u;
+#pragma unroll
+          for (int p = 0; p < 3; ++p) out[p].v[e] = (uint16_t)((__float_as_uint(upper(x)) >> 16) | quiet);
         } else {
           out[0].v[e] = e < n ? static_cast<const uint16_t*>(c.src)[from + e] : (uint16_t)0;
         }

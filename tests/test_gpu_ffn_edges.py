@@ -1,0 +1,63 @@
+"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements."""
+import pytest
+import torch
+
+from paper_2607_20548_gb300 import ffn_backward, ffn_forward
+from tests.test_gpu_ffn import F32, U, _act, _operands
+
+pytestmark = pytest.mark.gpu
+
+
+def _both(x, dy, w, off=None, act="silu"):
+    y, pre = ffn_forward(x, *w, offsets=off, act=act, keep=True)
+    return [y, *ffn_backward(dy, x, pre, *w, offsets=off, act=act)]
+
+
+def _exact(x, dy, w, lengths=None, act="silu"):
+    """In 64 bits, one group after another: y, dx and the weights' gradients."""
+    if lengths is not None:
+        parts = [_exact(x[at:at + n], dy[at:at + n], [m[i] for m in w], act=act)
+                 for i, (at, n) in enumerate(zip([sum(lengths[:i]) for i in range(len(lengths))], lengths))]
+        return [torch.cat([p[i] for p in parts]) for i in range(2)] + [torch.stack([p[i] for p in parts]) for i in (2, 3, 4)]
+    x, dy, wg, wu, wd = (v.double() for v in (x, dy, *w))
+    g, u = x @ wg, x @ wu
+    a, da = _act(g, act)
+    h, dh = a * u, dy @ wd.mT
+    dg, du = dh * u * da, dh * a
+    return [h @ wd, dg @ wg.mT + du @ wu.mT, x.mT @ dg, x.mT @ du, h.mT @ dy]
+
+
+def _same(got, want, rel):
+    """Infinities and NaN where the 64-bit values have them, the others near."""
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.isinf(), want.isinf()) and torch.equal(got[got.isinf()].double(), want[want.isinf()])
+    at = want.isfinite()
+    assert bool(((got.double() - want)[at].abs() <= rel * want[at].abs() + 1e-37).all())
+
+
+@pytest.mark.parametrize("hidden,width,lengths", [(64, 96, [40]), (300, 520, [40]), (72, 40, [5, 0, 300])])
+@pytest.mark.parametrize("full", [False, True])
+def test_infinite_elements(cuda, hidden, width, lengths, full):
+    """fp32: an infinite element gives what products of infinities give, whether or not the others have more bits than
+    a bf16 value. All terms are positive, so that no two infinities meet."""
+    x, dy, w, off = _operands(cuda, lengths, hidden, width, F32)
+    cut = (lambda v: v.abs() + 0.01) if full else (lambda v: (v.abs() + 0.01).bfloat16().float())
+    x, dy, w = cut(x), cut(dy), [cut(m) for m in w]
+    rel = 1000 * U  # all terms have one sign: 64 + K / 64 u in each of three sums in turn, a few products between them
+    x0, dy0 = x.clone(), dy.clone()
+    x[3, 5] = float("inf")
+    want = _exact(x, dy, w, lengths)
+    assert bool(want[0][3].isinf().all())
+    _same(ffn_forward(x, *w, offsets=off)[0], want[0], rel)
+    dy[2, 1] = -float("inf")
+    want = _exact(x0, dy, w, lengths)
+    assert bool(want[1][2].isinf().all()) and bool(want[2][0].isinf().all()) and bool(want[4][0, :, 1].isinf().all())
+    for a, b in zip(_both(x0, dy, w, off), want):
+        _same(a, b, rel)
+    w[2][0, 2, 1] = float("inf")
+    want = _exact(x0, dy0, w, lengths)
+    for a, b in zip(_both(x0, dy0, w, off), want):
+        _same(a, b, rel)
+    w[0][0, 2, 1] = float("inf")
+    x0[0, 2] = 0.0  # and no product with a zero
+    _same(ffn_forward(x0, *w, offsets=off)[0], _exact(x0, dy0, w, lengths)[0], rel)
