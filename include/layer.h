@@ -124,7 +124,7 @@ typedef enum { LAYER_SILU = 0, LAYER_GELU = 1 } layer_act_t;
  * that an infinity would decide: fp32 beside elements below 2^-62, which are used in parts that may be 0, and 16-bit
  * types where h, dg and du have twice the bits.
  * x, y: row i at element i * ld; y must not overlap an operand. status: NULL, or a device int32 (not cleared); where a
- * bounded wait gave up (soap_wait_limit), SOAP_STATUS_TIMEOUT is ORed into it and all results are NaN.
+ * bounded wait gave up (soap_wait_limit), SOAP_STATUS_TIMEOUT is ORed into it and all results, pre among them, are NaN.
  * 0 <= rows <= 2^31 - 2^16; 1 <= hidden, width <= 65536; 1 <= groups <= 1024. `workspace`: 256-byte aligned,
  * layer_ffn_workspace_bytes bytes (0 for invalid sizes); aligned: nonzero if every matrix operand of the call
  * begins on a 16-byte boundary, with leading dimension and stride of whole 16-byte units (others are

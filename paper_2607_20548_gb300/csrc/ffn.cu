@@ -282,6 +282,7 @@ cudaError_t compute(const Call& c, const void* x, int64_t ld_x, const void* dy, 
   }
   a.act = c.act;
   a.pre = pre;
+  a.pre_elems = (int64_t)layer_ffn_pre_elems(c.rows, c.width, c.groups);
   a.y = y;
   a.ld_y = ld_y;
   a.status = c.status;

@@ -68,6 +68,7 @@ struct Args {
   int wrows[3], wcols[3];       // sides of the weights' gradients as they are stored
   int act;
   float* pre;
+  int64_t pre_elems;
   void* y;                      // y or dx
   int64_t ld_y;
   int y_tma;

@@ -477,6 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   if (*abort_flag) {
+    spoil_pre(a);
     const T nan = from_f32<T>(NAN);
     for (int r = warp; r < a.rows; r += kThreads / 32)
       for (int c = lane; c < a.hidden; c += 32) static_cast<T*>(a.y)[(int64_t)r * a.ld_y + c] = nan;

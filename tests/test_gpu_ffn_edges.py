@@ -1,9 +1,10 @@
-"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements."""
+"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, waits that run out."""
 import pytest
 import torch
 
 from paper_2607_20548_gb300 import ffn_backward, ffn_forward
-from tests.test_gpu_ffn import F32, U, _act, _operands
+from paper_2607_20548_gb300 import soap as S
+from tests.test_gpu_ffn import BF, F32, U, _act, _operands
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +62,24 @@ def test_infinite_elements(cuda, hidden, width, lengths, full):
     w[0][0, 2, 1] = float("inf")
     x0[0, 2] = 0.0  # and no product with a zero
     _same(ffn_forward(x0, *w, offsets=off)[0], _exact(x0, dy0, w, lengths)[0], rel)
+
+
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("lengths", [[3], [300], [200, 0, 150], [1, 2, 3]])
+def test_wait_runs_out_in_what_is_kept(cuda, t, lengths):
+    """pre is a result too: after a wait that gave up (20 ms) it is NaN, and so is what a backward call makes of it."""
+    x, dy, w, off = _operands(cuda, lengths, 64, 96, t)
+    status, hold = (torch.zeros(1, dtype=torch.int32, device=cuda) for _ in range(2))
+    torch.cuda.synchronize()
+    try:
+        S.soap_wait_limit(20_000_000, hold)
+        y, pre = ffn_forward(x, *w, offsets=off, keep=True, status=status)
+        torch.cuda.synchronize()
+    finally:
+        S.soap_wait_limit(0, None)
+    assert int(status) == S.STATUS_TIMEOUT
+    assert bool(y.isnan().all()) and bool(pre.isnan().all())
+    grads = ffn_backward(dy, x, pre, *w, offsets=off)
+    assert bool(grads[0].isnan().all())
+    for m in grads[1:]:
+        assert all(bool(m[i].isnan().all()) for i, n in enumerate(lengths) if n)
