@@ -503,7 +503,8 @@ def _ffn_weight(name, w, size, groups):
 
 def _ffn_common(name, x, weights, offsets, act, status):
     """Checks what both passes take: (rows, hidden, width, groups), x and its leading dimension, the weights as
-    _ffn_weight finds them, offsets, the bits of the 16-byte units of all of these."""
+    _ffn_weight finds them, which of them (gate: 0, up: 1) was copied into the other's order, offsets, the bits of the
+    16-byte units of all of these."""
     index, dtype, size = x.get_device(), x.dtype, x.element_size()
     if act not in _ACTS:
         raise ValueError(f"{name}: act is one of {', '.join(_ACTS)}")
@@ -530,20 +531,23 @@ def _ffn_common(name, x, weights, offsets, act, status):
     if not 1 <= hidden <= 65536 or not 1 <= width <= 65536 or groups > 1024:
         raise ValueError(f"{name}: hidden and width of 1 to 65536 and at most 1024 groups")
     found = [_ffn_weight(name, w, size, groups) for w in weights]
-    if found[0][2] != found[1][2]:  # of two orders: both row-major
-        found[:2] = [_ffn_weight(name, w.contiguous(), size, groups) for w in weights[:2]]
+    turned = None
+    if found[0][2] != found[1][2]:  # of two orders: a row-major copy of the other one, whose gradient is turned back
+        turned = 0 if found[0][2] else 1
+        found[turned] = _ffn_weight(name, weights[turned].contiguous(), size, groups)
     if status is not None:
         _operand(name, status, _I32, x.device)
     x, rows, ld = _rows(x)
     units = x.data_ptr() | ld * size | found[0][5] | found[1][5] | found[2][5]
-    return (rows, hidden, width, groups), x, ld, found, offsets, units
+    return (rows, hidden, width, groups), x, ld, found, turned, offsets, units
 
 
 def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
                 offsets: Optional[torch.Tensor] = None, act: str = "silu", keep: bool = False,
                 status: Optional[torch.Tensor] = None, stream=None):
     """A gated feed-forward block act(x w_gate) * (x w_up) w_down of rows x [..., hidden]: (y, pre). Weights of x's
-    type, row- or column-major: w_gate and w_up [hidden, width], w_down [width, hidden]; with offsets (int32
+    type, row- or column-major (w_gate and w_up of different orders: the column-major one is copied in each call): w_gate
+    and w_up [hidden, width], w_down [width, hidden]; with offsets (int32
     [groups + 1]) a matrix of each for every group, of which group g has the rows offsets[g] to offsets[g + 1] - 1,
     and rows of no group give 0 (include/layer.h). act: "silu" or "gelu". pre, with ``keep``: what ffn_backward takes of
     this call (float32, in the library's own order), else None. status: an int32 CUDA word that SOAP_STATUS_TIMEOUT
@@ -556,7 +560,7 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
         with _elsewhere(index, stream, x, w_gate, w_up, w_down, offsets, status):
             return ffn_forward(x, w_gate, w_up, w_down, offsets, act, keep, status)
     shape = x.shape
-    sizes, x, ld, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    sizes, x, ld, held, _, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
     lib, t = load_library(), DTYPES[x.dtype]
     y = _dense_like(x, dev)
     pre = _empty(_size("layer_ffn_pre_elems", sizes[0], sizes[2], sizes[3]), dtype=_F32, device=dev) if keep else None
@@ -582,7 +586,7 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
         with _elsewhere(index, stream, dy, x, pre, w_gate, w_up, w_down, offsets, status):
             return ffn_backward(dy, x, pre, w_gate, w_up, w_down, offsets, act, params, status)
     shape = x.shape
-    sizes, x, ld, held, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
+    sizes, x, ld, held, turned, offsets, units = _ffn_common(name, x, (w_gate, w_up, w_down), offsets, act, status)
     _operand(name, dy, x.dtype, dev)
     if dy.shape != shape:
         raise ValueError(f"{name}: dy and x have different shapes")
@@ -605,4 +609,6 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_gate: t
         *sizes, None if offsets is None else offsets.data_ptr(), dy.data_ptr(), ld_dy, x.data_ptr(), ld, t,
         held[0][0], held[1][0], held[2][0], _ACTS[act], pre.data_ptr(), dx.data_ptr(), shape[-1], *grads,
         None if status is None else status.data_ptr(), ws.data_ptr(), ws_bytes, _raw_stream(index)), name)
+    if params and turned is not None:
+        out[turned] = made[turned].mT.contiguous().mT
     return dx, *out

@@ -1,4 +1,5 @@
-"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, waits that run out."""
+"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, weights of different orders,
+waits that run out."""
 import pytest
 import torch
 
@@ -62,6 +63,22 @@ def test_infinite_elements(cuda, hidden, width, lengths, full):
     w[0][0, 2, 1] = float("inf")
     x0[0, 2] = 0.0  # and no product with a zero
     _same(ffn_forward(x0, *w, offsets=off)[0], _exact(x0, dy0, w, lengths)[0], rel)
+
+
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("dense", [True, False])
+@pytest.mark.parametrize("gate,up", [(True, False), (False, True)])
+def test_orders_of_gate_and_up(cuda, gate, up, dense, t):
+    """Weights of different orders: the results of one order, each gradient in its own weight's."""
+    x, dy, w, off = _operands(cuda, [70] if dense else [30, 0, 40], 72, 136, t, dense=dense)
+    want = _both(x, dy, w, off)
+    turn = lambda m, columns: m.mT.contiguous().mT if columns else m  # noqa: E731
+    mixed = [turn(w[0], gate), turn(w[1], up), w[2]]
+    got = _both(x, dy, mixed, off)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for a, m in zip(got[2:], mixed):
+        assert a.stride() == m.stride()
 
 
 @pytest.mark.parametrize("t", [BF, F32])
