@@ -162,6 +162,9 @@ bool bad_call(const Call& c) {
          !c.w[0]->columns != !c.w[1]->columns || !c.ws || bad_ptr(c.ws, 256);
 }
 
+// Whether a call has something to do beside its results: to look at the offsets.
+bool tells(const Call& c) { return c.offsets && c.status; }
+
 // What a row-major matrix (or `matrices` of them, or planes) looks like to the copies.
 struct View {
   void* p;
@@ -366,7 +369,7 @@ soap_status_t layer_ffn_forward(int64_t rows, int64_t hidden, int64_t width, int
   if (bad_call(c) || bad_ptr(pre, 16)) return SOAP_ERR_INVALID_ARG;
   if (rows > 0 && (!x || bad_ptr(x, size) || ld_x < hidden || !y || bad_ptr(y, size) || ld_y < hidden))
     return SOAP_ERR_INVALID_ARG;
-  if (rows == 0) return SOAP_OK;
+  if (rows == 0 && !tells(c)) return SOAP_OK;
   cudaStream_t s = (cudaStream_t)stream;
   ProfScope prof(kFamGemmTc, 6.0 * rows * hidden * width, 3.0 * groups * hidden * width * size, s);
   const layer_matrix_t* none[3] = {nullptr, nullptr, nullptr};
@@ -396,7 +399,7 @@ soap_status_t layer_ffn_backward(int64_t rows, int64_t hidden, int64_t width, in
       if (bad_matrix(grads[i], i < 2 ? hidden : width, i < 2 ? width : hidden, groups, size) ||
           !grads[i]->columns != !c.w[i]->columns)
         return SOAP_ERR_INVALID_ARG;
-  if (rows == 0 && !d_gate) return SOAP_OK;
+  if (rows == 0 && !d_gate && !tells(c)) return SOAP_OK;
   cudaStream_t s = (cudaStream_t)stream;
   ProfScope prof(kFamGemmTc, (d_gate ? 12.0 : 6.0) * rows * hidden * width, 3.0 * groups * hidden * width * size, s);
   const cudaError_t e = compute(c, x, ld_x, dy, ld_dy, const_cast<float*>(pre), dx, ld_dx, grads, s);

@@ -1,5 +1,5 @@
 """The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, weights of different orders,
-waits that run out."""
+calls without rows, waits that run out."""
 import pytest
 import torch
 
@@ -100,3 +100,20 @@ def test_wait_runs_out_in_what_is_kept(cuda, t, lengths):
     assert bool(grads[0].isnan().all())
     for m in grads[1:]:
         assert all(bool(m[i].isnan().all()) for i, n in enumerate(lengths) if n)
+
+
+@pytest.mark.parametrize("t", [BF, F32])
+def test_no_rows_and_bad_offsets(cuda, t):
+    w = [torch.randn(2, *s, device=cuda).to(t) for s in ((8, 16), (8, 16), (16, 8))]
+    x = torch.randn(0, 8, device=cuda).to(t)
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    for off, told in (([0, 0, 0], 0), ([0, 3, 3], S.STATUS_RANGE), ([0, 0, -1], S.STATUS_RANGE)):
+        off = torch.tensor(off, dtype=torch.int32, device=cuda)
+        status.zero_()
+        y, pre = ffn_forward(x, *w, offsets=off, keep=True, status=status)
+        assert int(status) == told
+        for params in (False, True):
+            status.zero_()
+            grads = ffn_backward(y, x, pre, *w, offsets=off, params=params, status=status)
+            assert int(status) == told and grads[0].shape == x.shape
+            assert not params or not any(bool(g.any()) for g in grads[1:])
