@@ -1,11 +1,11 @@
-"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, weights of different orders,
-calls without rows, waits that run out."""
+"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, an activation's tail, weights
+of different orders, calls without rows, waits that run out."""
 import pytest
 import torch
 
 from paper_2607_20548_gb300 import ffn_backward, ffn_forward
 from paper_2607_20548_gb300 import soap as S
-from tests.test_gpu_ffn import BF, F32, U, _act, _operands
+from tests.test_gpu_ffn import BF, F32, HALF, TINY, U, _act, _operands
 
 pytestmark = pytest.mark.gpu
 
@@ -63,6 +63,25 @@ def test_infinite_elements(cuda, hidden, width, lengths, full):
     w[0][0, 2, 1] = float("inf")
     x0[0, 2] = 0.0  # and no product with a zero
     _same(ffn_forward(x0, *w, offsets=off)[0], _exact(x0, dy0, w, lengths)[0], rel)
+
+
+@pytest.mark.parametrize("t", [F32, BF])
+def test_gelu_tail(cuda, t):
+    """One element of h per row, whose g is given: y is act(g), dx is act'(g) and act(g). With u = 2^-24: Phi within
+    4 steps of its argument's two roundings, which g^2 multiplies; the exponential within 2^-22 and g^2 / 2 roundings of
+    its argument; a few more products; for 16-bit types their two roundings."""
+    g = torch.linspace(-11, 11, 2003, device=cuda).to(t)
+    x = torch.stack([g, torch.ones_like(g)], -1)
+    w = [torch.tensor(v, device=cuda, dtype=t) for v in ([[1.0], [0.0]], [[0.0], [1.0]], [[1.0, 0.0]])]
+    dy = torch.tensor([[1.0, 0.0]], device=cuda, dtype=t).expand(2003, 2)
+    y, dx = _both(x, dy, w, act="gelu")[:2]
+    g = g.double()
+    normal, slope = 0.5 * torch.special.erfc(-g * 0.5 ** 0.5), (-g * g / 2).exp() / (2 * torch.pi) ** 0.5
+    a, da, size = g * normal, normal + g * slope, normal + g.abs() * slope  # (ndtr is 1 + erf: it cancels in 64 bits too)
+    steps = (3 * g * g + 24) * U
+    half = 2.001 * HALF[t]
+    for got, want, of in ((y[:, 0], a, a.abs()), (dx[:, 0], da, size), (dx[:, 1], a, a.abs())):
+        assert bool(((got.double() - want).abs() <= steps * of + half * want.abs() + TINY[t]).all())
 
 
 @pytest.mark.parametrize("t", [BF, F32])
