@@ -108,10 +108,11 @@ Layout layout_of(int64_t rows, int64_t hidden, int64_t width, int groups, int ty
   for (int p = 0; p < 3; ++p) {
     const int64_t parts = slices[p] * products_of(type) < kMinParted ? 1 : slices[p], longest = (slices[p] + kMaxSlices - 1) / kMaxSlices;
     l.units += l.tiles[p] * std::max(parts, longest);
-    // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights'
-    // gradients: of groups with more than kMaxSlices slices, less than three parts for each such run of all rows)
+    // parts of tiles that are fewer than the pairs; and of those too long for one accumulator (of the weights' gradients:
+    // a group of s > kMaxSlices slices has ceil(s / kMaxSlices) of them, and there are at most `longest` such groups, each
+    // of which adds less than one to what all rows together have)
     l.slots[p] = parts > 1 ? std::min<int64_t>(t.pool, l.tiles[p] * parts) : 0;
-    if (longest > 1) l.slots[p] += p < 2 ? l.tiles[p] * longest : 3 * longest * each;
+    if (longest > 1) l.slots[p] += p < 2 ? l.tiles[p] * longest : each * (longest + (groups > 1 ? std::min<int64_t>(groups, longest) : 0));
   }
   l.plan = take(sizeof(Plan));
   l.done = at;

@@ -1,5 +1,5 @@
 """The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, an activation's tail, weights
-of different orders, calls without rows, waits that run out."""
+of different orders, calls without rows, waits that run out, long sums' workspaces."""
 import pytest
 import torch
 
@@ -136,3 +136,23 @@ def test_no_rows_and_bad_offsets(cuda, t):
             grads = ffn_backward(y, x, pre, *w, offsets=off, params=params, status=status)
             assert int(status) == told and grads[0].shape == x.shape
             assert not params or not any(bool(g.any()) for g in grads[1:])
+
+
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("lengths", [[140000], [65537] * 3, [5, 65600, 0, 131073]])
+def test_long_sums_stay_in_the_workspace(cuda, t, lengths):
+    """Sums along more rows than one accumulator takes: their parts fit the size that is asked for."""
+    lib, dt, rows, hidden, width = S.load_library(), S.DTYPES[t], sum(lengths), 64, 72
+    x, dy, w, off = _operands(cuda, lengths, hidden, width, t)
+    want = _both(x, dy, w, off)
+    _, pre = ffn_forward(x, *w, offsets=off, keep=True)
+    dx, grads = torch.empty_like(x), [torch.empty_like(m) for m in w]
+    mat = lambda m: S.layer_matrix(m.data_ptr(), m.shape[-1], m.shape[-1] * m.shape[-2], 0)  # noqa: E731
+    size = lib.layer_ffn_workspace_bytes(rows, hidden, width, len(lengths), dt, 1, 1)
+    ws = torch.full((size + (1 << 20),), 0xA5, dtype=torch.uint8, device=cuda)
+    code = lib.layer_ffn_backward(
+        rows, hidden, width, len(lengths), off.data_ptr(), dy.data_ptr(), hidden, x.data_ptr(), hidden, dt,
+        *(mat(m) for m in w), 0, pre.data_ptr(), dx.data_ptr(), hidden, *(mat(m) for m in grads), None, ws.data_ptr(), size,
+        torch.cuda.current_stream(cuda).cuda_stream)
+    assert code == 0 and bool((ws[size:] == 0xA5).all())
+    assert all(torch.equal(a, b) for a, b in zip([dx, *grads], want[1:]))
