@@ -843,14 +843,17 @@ cudaError_t bwd_t(Qk a, float* dq, float* dk, cudaStream_t s) {
   for (a.lanes = 1; a.lanes * per_lane < units;) a.lanes *= 2;
   a.steps = UN;
   const size_t smem = (size_t)kWarps * a.dim * sizeof(float);
-  static std::atomic<int> per_sm{0};  // of this kernel, with the most shared memory it takes
-  int fit = per_sm.load(std::memory_order_relaxed);
+  static std::atomic<int> per_sm[64];  // of this kernel, with the most shared memory it takes, per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  int fit = dev < 64 ? per_sm[dev].load(std::memory_order_relaxed) : 0;
   if (fit == 0) {
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, qk_bwd_kernel<T, W, V, INTER, UN>,
-                                                                        32 * kWarps, kWarps * kMaxDim * sizeof(float));
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, qk_bwd_kernel<T, W, V, INTER, UN>, 32 * kWarps,
+                                                      kWarps * kMaxDim * sizeof(float));
     if (e != cudaSuccess) return e;
     fit = std::max(1, std::min(4, fit));
-    per_sm.store(fit, std::memory_order_relaxed);
+    if (dev < 64) per_sm[dev].store(fit, std::memory_order_relaxed);
   }
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
@@ -863,7 +866,7 @@ cudaError_t bwd_t(Qk a, float* dq, float* dk, cudaStream_t s) {
   uint32_t ctas[2];
   share_ctas(a, want, most, ctas);
   qk_bwd_kernel<T, W, V, INTER, UN><<<ctas[0] + ctas[1], dim3(32, kWarps), a.partial ? smem : 0, s>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  e = cudaGetLastError();
   return e == cudaSuccess ? sum_parts(a, ctas, dq, dk, s) : e;
 }
 
