@@ -117,9 +117,12 @@ typedef enum { LAYER_SILU = 0, LAYER_GELU = 1 } layer_act_t;
  * is 1 and every row its own. Offsets that fall, or are outside 0 .. rows, are raised to the largest before them and
  * cut at rows, and SOAP_STATUS_RANGE is ORed into *status.
  * pre: layer_ffn_pre_elems fp32 elements, 16-byte aligned, receives g and u for the backward pass (in an order of the
- * library's own), or NULL. Products are summed in fp32. For 16-bit types h is rounded to the type before the second
- * product (the backward pass's dg, du and h too; fp16: a value above 65504 is then infinite), but for up to 16384
- * elements of x and small weights to twice its bits; g and u are not.
+ * library's own), or NULL. Products are summed in fp32, g and u are fp32.
+ * 16-bit types: h is rounded to the type before the second product, the backward pass's dg, du and h too, so that results
+ * have two roundings, 1.4 of one in root mean square. fp16: what is above 65504 is then infinite, below 2^-14 it loses
+ * bits, below 2^-25 it is 0 (dy may have to be scaled). Where rows * hidden <= 16384 and groups * hidden * width <= 2^23,
+ * h, dg and du keep twice the type's bits and results have their own rounding alone: how exact a row is, and its last
+ * bits, depend on the rows that share its call.
  * Infinite elements give the infinities and NaN of products in the type, with two exceptions that give NaN in a sum
  * that an infinity would decide: fp32 beside elements below 2^-62, which are used in parts that may be 0, and 16-bit
  * types where h, dg and du have twice the bits.

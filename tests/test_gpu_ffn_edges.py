@@ -1,11 +1,11 @@
-"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): infinite elements, an activation's tail, weights
-of different orders, calls without rows, waits that run out, long sums' workspaces."""
+"""The feed-forward block at its edges (include/layer.h, layer_ffn_*): roundings of 16-bit types, infinite elements, an
+activation's tail, weights of different orders, calls without rows, waits that run out, long sums' workspaces."""
 import pytest
 import torch
 
 from paper_2607_20548_gb300 import ffn_backward, ffn_forward
 from paper_2607_20548_gb300 import soap as S
-from tests.test_gpu_ffn import BF, F32, HALF, TINY, U, _act, _operands
+from tests.test_gpu_ffn import BF, F32, HALF, HF, TINY, U, _act, _operands
 
 pytestmark = pytest.mark.gpu
 
@@ -27,6 +27,39 @@ def _exact(x, dy, w, lengths=None, act="silu"):
     h, dh = a * u, dy @ wd.mT
     dg, du = dh * u * da, dh * a
     return [h @ wd, dg @ wg.mT + du @ wu.mT, x.mT @ dg, x.mT @ du, h.mT @ dy]
+
+
+def _mean_error(a, b):
+    return float((a.double() - b).norm() / b.norm())
+
+
+@pytest.mark.parametrize("t", [BF, HF])
+@pytest.mark.parametrize("lengths,hidden,width,roundings", [
+    ([16], 1024, 1024, 1), ([17], 1024, 1024, 2), ([8], 2048, 4096, 1), ([8], 2048, 4104, 2),
+    ([5, 11], 1024, 4096, 1), ([5, 11], 1024, 4104, 2)])
+def test_roundings_by_size(cuda, lengths, hidden, width, roundings, t):
+    """Up to 16384 elements of x and 2^23 of all groups' weights of a kind h, dg and du keep twice the type's bits, and a
+    result has one rounding, else two independent ones, each of 0.578 of half a step in root mean square."""
+    x, dy, w, off = _operands(cuda, lengths, hidden, width, t)
+    dy = (dy * 10).to(t)  # (fp16's smallest steps do not count here)
+    for a, b in zip(_both(x, dy, w, off), _exact(x, dy, w, lengths)):
+        assert _mean_error(a, b) <= (0.6 if roundings == 1 else 0.82) * HALF[t] + 1e-5
+
+
+@pytest.mark.parametrize("t", [BF, HF])
+@pytest.mark.parametrize("lengths,hidden,width,act,columns", [
+    ([300], 2048, 8192, "silu", (False, False)), ([1], 2048, 8192, "silu", (False, False)),
+    ([24], 2048, 8192, "gelu", (True, False)), ([1000], 777, 1365, "gelu", (True, True)),
+    ([60 + 17 * (i % 5) for i in range(64)], 2048, 768, "silu", (False, False)), ([3] * 64, 2048, 768, "silu", (False, True))])
+def test_large_blocks_in_the_mean(cuda, lengths, hidden, width, act, columns, t):
+    """Two independent roundings at most, of h (or dg and du) and of the result, each of 0.578 of half a step in root
+    mean square, and sums in fp32: 1.415 x 0.578 = 0.82. (Bounds that add up magnitudes grow with the sums' length,
+    these do not.)"""
+    dense = len(lengths) == 1
+    x, dy, w, off = _operands(cuda, lengths, hidden, width, t, columns=columns, dense=dense)
+    dy = (dy * 10).to(t)  # (fp16's smallest steps do not count here)
+    for a, b in zip(_both(x, dy, w, off, act), _exact(x, dy, w, None if dense else lengths, act)):
+        assert _mean_error(a, b) <= 0.82 * HALF[t] + 1e-5
 
 
 def _same(got, want, rel):
