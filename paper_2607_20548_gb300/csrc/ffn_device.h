@@ -193,6 +193,7 @@ __device__ __forceinline__ float rest_of(float x, T rounded) {
 __device__ __forceinline__ void spoil_pre(const Args& a) {
   if (a.backward || !a.pre) return;
   float4* const p = reinterpret_cast<float4*>(a.pre);
+#pragma unroll 1
   for (int64_t i = threadIdx.x; i < a.pre_elems / 4; i += blockDim.x) p[i] = make_float4(NAN, NAN, NAN, NAN);
 }
 
