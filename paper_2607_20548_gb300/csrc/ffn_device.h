@@ -189,14 +189,6 @@ __device__ __forceinline__ float rest_of(float x, T rounded) {
   return fabsf(r) < INFINITY ? x - r : 0.f;
 }
 
-// What a forward call whose waits gave up keeps for the backward pass: NaN, as its result is. All of a CTA's threads.
-__device__ __forceinline__ void spoil_pre(const Args& a) {
-  if (a.backward || !a.pre) return;
-  float4* const p = reinterpret_cast<float4*>(a.pre);
-#pragma unroll 1
-  for (int64_t i = threadIdx.x; i < a.pre_elems / 4; i += blockDim.x) p[i] = make_float4(NAN, NAN, NAN, NAN);
-}
-
 // 32 elements of this lane's row to or from a block in which the rows' 16-byte pieces lie side by side (at p: this
 // lane's first).
 __device__ __forceinline__ void put_lines(float4* p, const float (&v)[32]) {

@@ -807,7 +807,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   if (*abort_flag) {
-    spoil_pre(a);
+    if (a.pre && !a.backward) {
+#pragma unroll 1
+      for (int64_t i = threadIdx.x; i < a.pre_elems / 4; i += kThreads)
+        reinterpret_cast<float4*>(a.pre)[i] = make_float4(NAN, NAN, NAN, NAN);
+    }
     const T nan = from_f32<T>(NAN);
     for (int r = warp; r < a.rows; r += kThreads / 32)
       for (int c = lane; c < a.hidden; c += 32) static_cast<T*>(a.y)[(int64_t)r * a.ld_y + c] = nan;
