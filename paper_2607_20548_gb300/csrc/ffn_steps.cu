@@ -872,10 +872,10 @@ __device__ __forceinline__ void copy_operands(const CopyJobs& jobs, const int* b
       for (int e = 0; e < 8; ++e) {
         if constexpr (SPLIT) {
           float x = in[e];
-          // (a NaN stays one without its lower bits)
+          // (a NaN's first plane stays one without its lower bits)
           const uint32_t quiet = x != x ? 0x40u : 0u;
 #pragma unroll
-          for (int p = 0; p < 3; ++p) out[p].v[e] = (uint16_t)((__float_as_uint(upper(x)) >> 16) | quiet);
+          for (int p = 0; p < 3; ++p) out[p].v[e] = (uint16_t)((__float_as_uint(upper(x)) >> 16) | (p == 0 ? quiet : 0u));
         } else {
           out[0].v[e] = e < n ? static_cast<const uint16_t*>(c.src)[from + e] : (uint16_t)0;
         }
