@@ -46,7 +46,8 @@ bool few_rows(int64_t rows, int groups, int type, bool backward) {
 // bf16 36 us, in one plane 33; 8 rows of 1024 x 1024 64 and 54; 24 rows of 1024 x 1024, which have one plane, 56 and 67 in
 // two. A rule on the weights alone would hold every row of a model to the same, at the price of the large calls: up to
 // 2^19 elements in two planes, 512 x 512 would take 57 us in place of 48 with 100 rows, 124 in place of 94 with 8192, 299
-// in place of 207 with 32768.
+// in place of 207 with 32768. All others round h, dg and du once, to what the tensor core multiplies: six of
+// the nine products of both passes read them, so that a second plane everywhere would be 15 products' work for 9.
 int planes_of(int64_t rows, int64_t hidden, int64_t width, int groups, int type) {
   return type == SOAP_F32 ? 3 : rows * hidden <= 16384 && groups * hidden * width <= 1 << 23 ? 2 : 1;
 }

@@ -98,6 +98,26 @@ def test_infinite_elements(cuda, hidden, width, lengths, full):
     _same(ffn_forward(x0, *w, offsets=off)[0], _exact(x0, dy0, w, lengths)[0], rel)
 
 
+@pytest.mark.parametrize("hidden,width,lengths", [(520, 300, [40]), (72, 136, [300]), (520, 72, [30, 0, 200])])
+@pytest.mark.parametrize("t", [BF, HF])
+def test_infinite_elements_of_16_bits(cuda, hidden, width, lengths, t):
+    """The same where h, dg and du are rounded to the type."""
+    x, dy, w, off = _operands(cuda, lengths, hidden, width, t)
+    x, dy, w = x.abs() + 0.01, dy.abs() + 0.01, [m.abs() + 0.01 for m in w]
+    rel = 4 * HALF[t]  # all terms have one sign: two roundings (dx: of dg or du, and its own)
+    for m, at in ((x, (3, 5)), (dy, (2, 1)), (w[2], (0, 2, 1)), (w[0], (0, 2, 1))):
+        was = m[at].clone()
+        m[at] = float("inf")
+        want = _exact(x, dy, w, lengths)
+        got = _both(x, dy, w, off)
+        if m is x or m is w[0]:  # (silu' of an infinity is a NaN in 64 bits)
+            got, want = got[:1], want[:1]
+        assert not bool(want[0].isnan().any())
+        for a, b in zip(got, want):
+            _same(a, b, rel)
+        m[at] = was
+
+
 @pytest.mark.parametrize("t", [F32, BF])
 def test_gelu_tail(cuda, t):
     """One element of h per row, whose g is given: y is act(g), dx is act'(g) and act(g). With u = 2^-24: Phi within
